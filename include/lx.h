@@ -58,6 +58,8 @@ extern "C" {
 #define LX_MAX_DEPTH 4   /* nodes on a root path, anchor included */
 #define LX_MAX_K 32      /* router top-k */
 #define LX_MAX_EXPERTS 1024
+#define LX_MAX_WIDTH 65536  /* d_model of lx_residual_norm */
+#define LX_MAX_TEACHER 1024 /* teacher entries a token in lx_distill_loss */
 
 typedef enum {
   LX_OK = 0,
@@ -458,6 +460,130 @@ LX_API lx_status lx_compress_factor(int32_t dtype, int32_t rows, int32_t cols, c
                                     const void* w_mem, const float* omega, int32_t l, int32_t r,
                                     int32_t power_iters, float* U, float* V, float* s,
                                     void* workspace, uint64_t workspace_bytes, void* stream);
+
+/*
+ * The operators around a compressed layer: the norms of the residual block it sits
+ * in, and the two losses that its surroundings are trained with after compression
+ * (a balance loss that keeps the unchanged router's loads even, distillation from
+ * the uncompressed model's stored top logits).  The paper has no counterpart.
+ * Standalone calls on plain device arrays; all parameters and statistics are fp32,
+ * sums and norms are held in fp32, and results do not depend on scheduling.  Arrays
+ * with a leading dimension (ld..., in elements) may be slices of wider ones; the
+ * others are contiguous.
+ */
+
+/*
+ * lx_residual_norm: the norm after a block, its gate, the residual with its scale
+ * and the norm before the next block.  Per token, with o = weight_offset:
+ *   u  = y / sqrt(mean(y^2) + eps) * (o + w_post)     (w_post NULL: u = y)
+ *   r' = res_scale * r + g * u                        (y NULL: r' = res_scale * r)
+ *   h  = r' / sqrt(mean(r'^2) + eps) * (o + w_pre)    (w_pre NULL: no h)
+ * h is formed from the unrounded r'.
+ *   dtype: lx_dtype of r, y, r_out, h_out and a full gate;  T tokens (0: no-op),
+ *   H in 1..LX_MAX_WIDTH
+ *   r [T][H] (rows ldr apart), y [T][H] (ldy) or NULL
+ *   w_post, w_pre: fp32 [H] or NULL
+ *   gate: LX_GATE_NONE NULL (g = 1); LX_GATE_CHANNEL fp32 [H]; LX_GATE_TOKEN fp32
+ *         [T], ldg apart; LX_GATE_FULL [T][H] in dtype, rows ldg apart
+ *   r_out [T][H] or NULL; may be r itself (ldr = H), nothing else may overlap
+ *   h_out [T][H], given exactly when w_pre is
+ *   stats: fp32 [2][T] or NULL: the two 1 / sqrt(...) of each token (1 where that
+ *          norm is absent), which the backward reads
+ * lx_residual_norm_backward: from dr_out (rows lddr apart) and dh (lddh), either
+ * NULL for zero, the gradients dr [T][H], dy [T][H], dw_post fp32 [H], dgate (in the
+ * gate's shape; fp32, or dtype for LX_GATE_FULL), dw_pre fp32 [H]; a NULL output is
+ * skipped.  It takes the forward's inputs (r as it was before the call) and stats.
+ *   workspace: device, 16-byte aligned, lx_residual_norm_workspace bytes; needed for
+ *   dw_post, dw_pre and a channel gate's gradient
+ *   T == 0: the parameter gradients are zeroed.
+ * Stream-ordered; no allocation.  Errors: LX_ERR_ARG (NULL, dtype, gate kind,
+ * alignment to the element, overlap, workspace), LX_ERR_SHAPE (H, leading dimensions).
+ */
+typedef enum { LX_GATE_NONE = 0, LX_GATE_CHANNEL = 1, LX_GATE_TOKEN = 2, LX_GATE_FULL = 3 } lx_gate_kind;
+typedef struct {
+  int32_t dtype, T, H, gate_kind;
+  int64_t ldr, ldy, ldg;
+  const void* r;
+  const void* y;
+  const void* gate;
+  const float* w_post;
+  const float* w_pre;
+  float res_scale, weight_offset, eps;
+} lx_resnorm_desc;
+LX_API lx_status lx_residual_norm(const lx_resnorm_desc* desc, void* r_out, void* h_out, float* stats,
+                                  void* stream);
+LX_API lx_status lx_residual_norm_workspace(int32_t T, int32_t H, uint64_t* bytes);
+LX_API lx_status lx_residual_norm_backward(const lx_resnorm_desc* desc, const float* stats,
+                                           const void* dr_out, int64_t lddr, const void* dh,
+                                           int64_t lddh, void* dr, void* dy, float* dw_post,
+                                           void* dgate, float* dw_pre, void* workspace,
+                                           uint64_t workspace_bytes, void* stream);
+
+/*
+ * lx_router_balance: the router's balance loss, its z loss and the experts' counts.
+ * A token counts unless mask[t] is 0 or all of its logits are -inf; n tokens count.
+ *   p = softmax(logits of the token),  P_e = mean of p_e over the n tokens,
+ *   c_e = counted tokens whose set of ids holds e (ids outside [0, E) are skipped, a
+ *         repeated id counts once, as in lx_coact_accumulate)
+ *   balance = E * sum_e (c_e / (n k)) P_e      (1 when both are uniform)
+ *   z       = mean of (log sum_e exp(logit_e))^2
+ *   loss    = balance_coef * balance + z_coef * z   (all 0 when n = 0)
+ *   logits: [T][E] (dtype; rows ld apart; lx_route's fp32 logits, or bf16)
+ *   topk_id: int32 [T][k];  mask: uint8 [T] or NULL (the logits of a masked token are
+ *         not read)
+ *   counts: int32 [E + 1] out: c_e, then n;  prob: fp32 [E] out: P_e
+ *   lse: fp32 [T] out, -inf for a token that does not count
+ *   loss: fp32 [3] out: loss, balance, z
+ *   workspace: device, 16-byte aligned, lx_router_balance_workspace bytes
+ * lx_router_balance_backward: dlogits [T][E] (dtype, contiguous; may be logits itself
+ * with ld = E) = dloss times the gradient of loss, the counts held fixed:
+ *   p_e (balance_coef E / (n^2 k) (c_e - sum_j c_j p_j) + 2 z_coef / n lse),
+ * zero rows for tokens that do not count.  lse and counts are the forward's; dloss is
+ * a device fp32 scalar or NULL for 1.
+ * Stream-ordered; no allocation.  Errors: LX_ERR_ARG (dtype, T < 0, E, k, NULL,
+ * alignment to the element, overlap, workspace), LX_ERR_SHAPE (ld).
+ */
+LX_API lx_status lx_router_balance_workspace(int32_t T, int32_t E, uint64_t* bytes);
+LX_API lx_status lx_router_balance(int32_t dtype, const void* logits, int64_t ld,
+                                   const int32_t* topk_id, const uint8_t* mask, int32_t T, int32_t E,
+                                   int32_t k, float balance_coef, float z_coef, int32_t* counts,
+                                   float* prob, float* lse, float* loss, void* workspace,
+                                   uint64_t workspace_bytes, void* stream);
+LX_API lx_status lx_router_balance_backward(int32_t dtype, const void* logits, int64_t ld,
+                                            const float* lse, const int32_t* counts,
+                                            const float* dloss, int32_t T, int32_t E, int32_t k,
+                                            float balance_coef, float z_coef, void* dlogits,
+                                            void* stream);
+
+/*
+ * lx_distill_loss: distillation of a student's logits z [V] from a teacher's stored
+ * top logits, per token, with its gradient in the same call:
+ *   q_j = softmax over the token's valid entries of t_j / temperature, or, with
+ *         teacher_lse, exp(t_j / temperature - teacher_lse) (the entries' share of the
+ *         teacher's whole distribution);  m = sum_j q_j
+ *   kd  = sum_j q_j (log q_j - log softmax(z / temperature)[id_j])
+ *   ce  = log sum_v exp(z_v) - z_label      (0 where the label is outside [0, V))
+ *   loss = weight * (kd_weight temperature^2 kd + ce_weight ce)
+ *   dz_v = weight * (kd_weight temperature (m softmax(z / temperature)_v - sum of the
+ *          q_j with id_j = v) + ce_weight (softmax(z)_v - [v = label]))
+ * A token with weight 0 (its logits and entries are not read), or whose logits are all
+ * -inf, has loss 0 and gradient 0.  Entries with an id outside [0, V) or t = -inf are
+ * skipped; entries that repeat an id add up; a token without entries has kd = 0.
+ *   logits: [T][V] (dtype; rows ld apart);  teacher_id int32, teacher_logit fp32 [T][K],
+ *   K in 1..LX_MAX_TEACHER;  teacher_lse fp32 [T] (log-sum-exp of the teacher's logits
+ *   over temperature) or NULL;  labels int32 [T] or NULL (then ce_weight must be 0);
+ *   row_weight fp32 [T] or NULL for 1 (a mean's 1 / n and any upstream gradient go here)
+ *   loss: fp32 [T] out;  dlogits: [T][V] out (dtype; rows ldd apart) or NULL; may be
+ *   logits itself (ldd = ld)
+ * Stream-ordered; no allocation.  Errors: LX_ERR_ARG (dtype, T < 0, K, temperature not
+ * positive, NULL, alignment to the element, overlap), LX_ERR_SHAPE (V, ld, ldd).
+ */
+LX_API lx_status lx_distill_loss(int32_t dtype, const void* logits, int64_t ld,
+                                 const int32_t* teacher_id, const float* teacher_logit,
+                                 const float* teacher_lse, const int32_t* labels,
+                                 const float* row_weight, int32_t T, int32_t V, int32_t K,
+                                 float temperature, float kd_weight, float ce_weight, float* loss,
+                                 void* dlogits, int64_t ldd, void* stream);
 
 /* Message of the last failed call on this thread ("" if none). */
 LX_API const char* lx_last_error(void);

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Dict, Optional
+from typing import Dict, NamedTuple, Optional
 
 import numpy as np
 import torch
@@ -23,6 +23,8 @@ STATUS_NAMES = ["LX_OK", "LX_ERR_ARG", "LX_ERR_SHAPE", "LX_ERR_CUDA", "LX_ERR_OO
 LX_F32, LX_BF16 = 0, 1
 LX_PATH_AUTO, LX_PATH_GENERIC = 0, 1
 LX_MAX_DEPTH, LX_MAX_K, LX_MAX_EXPERTS = 4, 32, 1024
+LX_MAX_WIDTH, LX_MAX_TEACHER = 65536, 1024
+LX_GATE_NONE, LX_GATE_CHANNEL, LX_GATE_TOKEN, LX_GATE_FULL = range(4)
 
 # every symbol include/lx.h declares
 EXPORTS = [
@@ -31,7 +33,9 @@ EXPORTS = [
     "lx_read_profile", "lx_last_error", "lx_bucket_noalloc", "lx_coact_accumulate",
     "lx_coact_npmi", "lx_align_cost", "lx_lap_solve", "lx_lap_solve_batch", "lx_permute_neurons",
     "lx_compress_workspace", "lx_compress_factor", "lx_set_wait_limit", "lx_inject_unmet_wait",
-    "lx_clear_device_error", "lx_inject_unmet_wait_call",
+    "lx_clear_device_error", "lx_inject_unmet_wait_call", "lx_residual_norm",
+    "lx_residual_norm_workspace", "lx_residual_norm_backward", "lx_router_balance_workspace",
+    "lx_router_balance", "lx_router_balance_backward", "lx_distill_loss",
 ]
 (LX_WAIT_NONE, LX_WAIT_STREAM_DEP, LX_WAIT_TC_MMA, LX_WAIT_ROUTER, LX_WAIT_CALL_PRODUCT,
  LX_WAIT_CALL_JACOBI) = range(6)
@@ -61,6 +65,13 @@ class LayerInfo(ctypes.Structure):
                                       "stream_path")]
 
 
+class ResnormDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "T", "H", "gate_kind")] + [
+        (n, ctypes.c_int64) for n in ("ldr", "ldy", "ldg")] + [
+        (n, ctypes.c_void_p) for n in ("r", "y", "gate", "w_post", "w_pre")] + [
+        (n, ctypes.c_float) for n in ("res_scale", "weight_offset", "eps")]
+
+
 class KernelTime(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char_p), ("ms", ctypes.c_float)]
 
@@ -76,7 +87,8 @@ def lib() -> ctypes.CDLL:
             raise RuntimeError(
                 f"{LIB_PATH} is missing: build it with `python -m paper_2608_07814_gb300.build`")
         L = ctypes.CDLL(LIB_PATH)
-        vp, i32 = ctypes.c_void_p, ctypes.c_int32
+        vp, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+        u64, f32 = ctypes.c_uint64, ctypes.c_float
         sig = {
             "lx_load_compressed_layer": [ctypes.POINTER(LayerDesc), vp, vp, vp, vp,
                                          ctypes.POINTER(vp)],
@@ -104,6 +116,16 @@ def lib() -> ctypes.CDLL:
             "lx_compress_workspace": [i32, i32, i32, i32, ctypes.POINTER(ctypes.c_uint64)],
             "lx_compress_factor": [i32, i32, i32, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp,
                                    ctypes.c_uint64, vp],
+            "lx_residual_norm": [ctypes.POINTER(ResnormDesc), vp, vp, vp, vp],
+            "lx_residual_norm_workspace": [i32, i32, ctypes.POINTER(u64)],
+            "lx_residual_norm_backward": [ctypes.POINTER(ResnormDesc), vp, vp, i64, vp, i64, vp, vp,
+                                          vp, vp, vp, vp, u64, vp],
+            "lx_router_balance_workspace": [i32, i32, ctypes.POINTER(u64)],
+            "lx_router_balance": [i32, vp, i64, vp, vp, i32, i32, i32, f32, f32, vp, vp, vp, vp, vp,
+                                  u64, vp],
+            "lx_router_balance_backward": [i32, vp, i64, vp, vp, vp, i32, i32, i32, f32, f32, vp, vp],
+            "lx_distill_loss": [i32, vp, i64, vp, vp, vp, vp, vp, i32, i32, i32, f32, f32, f32, vp,
+                                vp, i64, vp],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -431,3 +453,278 @@ def compress_member(w_doms, w_mems, omegas, r: int, power_iters: int = 2, worksp
             for t in res[-1]:  # allocated on the side stream, used on the caller's
                 t.record_stream(main)
     return res
+
+
+# ----------------------------------------------------------------------------
+# the operators around a layer: block norms, router balance loss, distillation
+# ----------------------------------------------------------------------------
+_DTYPES = {torch.bfloat16: LX_BF16, torch.float32: LX_F32}
+
+
+def _need(ok: bool, msg: str) -> None:
+    if not ok:
+        raise ValueError(msg)
+
+
+def _rows(t: torch.Tensor, name: str, shape=None, dtype=None) -> int:
+    """Checks a matrix of rows (unit stride inside a row) and returns their distance."""
+    _need(t.dim() == 2 and t.is_cuda, f"{name} must be a CUDA matrix")
+    _need(shape is None or t.shape == shape, f"{name} has another shape")
+    _need(dtype is None or t.dtype == dtype, f"{name} has another dtype")
+    ld, inner = t.stride()
+    T, n = t.shape
+    _need(inner == 1 or n <= 1, f"{name} must have unit stride inside a row")
+    return ld if T > 1 else max(n, 1)
+
+
+def _flat(t: Optional[torch.Tensor], name: str, n: int, dtype=torch.float32):
+    """Checks a contiguous array of n elements (or None) and returns its address."""
+    if t is None:
+        return None
+    _need(t.is_cuda and t.dtype == dtype and t.numel() == n and t.is_contiguous(),
+          f"{name} must be a contiguous CUDA array of {n} {dtype} elements")
+    return t.data_ptr()
+
+
+class _On:
+    """Runs a call's allocations and launches on `stream`.  Tensors made there belong
+    to it; the inputs, and the outputs towards the caller's stream, are marked as used
+    on both, so that their memory is not given away early."""
+
+    def __init__(self, stream, *tensors):
+        self.other = torch.cuda.current_stream()
+        self.side = stream is not None and stream != self.other
+        self.stream = stream if self.side else self.other
+        self.tensors = tensors
+
+    def __enter__(self):
+        if self.side:
+            self.ctx = torch.cuda.stream(self.stream)
+            self.ctx.__enter__()
+            for t in self.tensors:
+                if t is not None:
+                    t.record_stream(self.stream)
+        return self
+
+    def outputs(self, *tensors):
+        if self.side:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self.other)
+
+    def __exit__(self, *exc):
+        if self.side:
+            self.ctx.__exit__(*exc)
+        return False
+
+
+def _resnorm_desc(r, y, w_post, gate, w_pre, res_scale, weight_offset, eps) -> ResnormDesc:
+    ldr = _rows(r, "r")
+    T, H = r.shape
+    _need(r.dtype in _DTYPES, "r must be bf16 or fp32")
+    d = ResnormDesc(_DTYPES[r.dtype], T, H, LX_GATE_NONE, ldr, 0, 0, r.data_ptr(), None, None,
+                    _flat(w_post, "w_post", H), _flat(w_pre, "w_pre", H), res_scale, weight_offset, eps)
+    if y is not None:
+        d.ldy = _rows(y, "y", r.shape, r.dtype)
+        d.y = y.data_ptr()
+    if gate is not None:
+        if gate.dim() == 1:
+            d.gate_kind = LX_GATE_CHANNEL
+            d.gate = _flat(gate, "a gate of one dimension", H)
+        elif gate.shape == (T, 1) and (H != 1 or gate.dtype == torch.float32):
+            d.gate_kind = LX_GATE_TOKEN
+            d.ldg = _rows(gate, "gate", None, torch.float32)
+            d.gate = gate.data_ptr()
+        else:
+            d.gate_kind = LX_GATE_FULL
+            d.ldg = _rows(gate, "gate", r.shape, r.dtype)
+            d.gate = gate.data_ptr()
+    return d
+
+
+def residual_norm(r: torch.Tensor, y: Optional[torch.Tensor] = None, *, w_post=None, gate=None,
+                  w_pre=None, res_scale: float = 1.0, weight_offset: float = 0.0, eps: float = 1e-6,
+                  r_out=None, h_out=None, stats=None, stream=None):
+    """The norm after a block, its gate and residual, and the norm before the next:
+
+        u = rms_norm(y) * (weight_offset + w_post)        (y itself without w_post)
+        r_out = res_scale * r + gate * u
+        h = rms_norm(r_out) * (weight_offset + w_pre)
+
+    r and y are [T, H] (bf16 or fp32, rows may be slices of wider ones); w_post and
+    w_pre fp32 [H]; gate fp32 [H], fp32 [T, 1] or [T, H] in r's type.  Returns (r_out,
+    h); h is None without w_pre.  Without y only the norm is taken, and r_out is r
+    itself unless res_scale is not 1 or a buffer is given.  ``r_out`` may be r (in
+    place).  ``stats``: fp32 [2, T] for residual_norm_backward."""
+    d = _resnorm_desc(r, y, w_post, gate, w_pre, res_scale, weight_offset, eps)
+    T, H = r.shape
+    with _On(stream, r, y, w_post, gate, w_pre, r_out, h_out, stats) as on:
+        made = []
+        write_r = r_out is not None or y is not None or res_scale != 1.0
+        if write_r and r_out is None:
+            r_out = torch.empty((T, H), dtype=r.dtype, device=r.device)
+            made.append(r_out)
+        if w_pre is not None and h_out is None:
+            h_out = torch.empty((T, H), dtype=r.dtype, device=r.device)
+            made.append(h_out)
+        _check(lib().lx_residual_norm(d, _flat(r_out, "r_out", T * H, r.dtype) if write_r else None,
+                                      _flat(h_out, "h_out", T * H, r.dtype),
+                                      _flat(stats, "stats", 2 * T), on.stream.cuda_stream))
+        on.outputs(*made)
+    return (r_out if write_r else r), h_out
+
+
+class ResidualNormGrads(NamedTuple):
+    """Gradients of residual_norm; None where the input was absent."""
+    dr: torch.Tensor
+    dy: Optional[torch.Tensor]
+    dw_post: Optional[torch.Tensor]
+    dgate: Optional[torch.Tensor]
+    dw_pre: Optional[torch.Tensor]
+
+
+def residual_norm_workspace_bytes(T: int, H: int) -> int:
+    b = ctypes.c_uint64()
+    _check(lib().lx_residual_norm_workspace(T, H, b))
+    return int(b.value)
+
+
+def residual_norm_backward(dr_out, dh, r, y, stats, *, w_post=None, gate=None, w_pre=None,
+                           res_scale: float = 1.0, weight_offset: float = 0.0, workspace=None,
+                           stream=None) -> ResidualNormGrads:
+    """Gradients of residual_norm with respect to r, y, w_post, gate and w_pre, from
+    those of r_out and h (either may be None for zero).  The other arguments are the
+    forward's (r as it was before the call) and the stats it wrote."""
+    d = _resnorm_desc(r, y, w_post, gate, w_pre, res_scale, weight_offset, 0.0)
+    T, H = r.shape
+    dev = r.device
+    with _On(stream, dr_out, dh, r, y, stats, w_post, gate, w_pre, workspace) as on:
+        empty = lambda like, shape, dtype: None if like is None else torch.empty(  # noqa: E731
+            shape, dtype=dtype, device=dev)
+        g = ResidualNormGrads(empty(r, (T, H), r.dtype), empty(y, (T, H), r.dtype),
+                              empty(w_post, (H,), torch.float32),
+                              empty(gate, gate.shape if gate is not None else (),
+                                    gate.dtype if gate is not None else None),
+                              empty(w_pre, (H,), torch.float32))
+        if workspace is None:
+            workspace = torch.empty(residual_norm_workspace_bytes(T, H), dtype=torch.uint8, device=dev)
+        _check(lib().lx_residual_norm_backward(
+            d, _flat(stats, "stats", 2 * T),
+            None if dr_out is None else dr_out.data_ptr(),
+            0 if dr_out is None else _rows(dr_out, "dr_out", r.shape, r.dtype),
+            None if dh is None else dh.data_ptr(),
+            0 if dh is None else _rows(dh, "dh", r.shape, r.dtype),
+            *[None if t is None else t.data_ptr() for t in g], workspace.data_ptr(),
+            workspace.numel() * workspace.element_size(), on.stream.cuda_stream))
+        on.outputs(*g)
+    return g
+
+
+class RouterBalance(NamedTuple):
+    """What router_balance computes: loss fp32 [3] (the loss, its balance and z parts),
+    counts int32 [E + 1] (tokens of each expert, then the tokens that counted), prob
+    fp32 [E] (mean router probability), lse fp32 [T] (log-sum-exp of each token, -inf
+    where it did not count)."""
+    loss: torch.Tensor
+    counts: torch.Tensor
+    prob: torch.Tensor
+    lse: torch.Tensor
+
+
+def _mask_ptr(mask, T):
+    if mask is None:
+        return None
+    _need(mask.dtype in (torch.bool, torch.uint8), "mask must be bool or uint8")
+    return _flat(mask, "mask", T, mask.dtype)
+
+
+def router_balance_workspace_bytes(T: int, E: int) -> int:
+    b = ctypes.c_uint64()
+    _check(lib().lx_router_balance_workspace(T, E, b))
+    return int(b.value)
+
+
+def router_balance(logits: torch.Tensor, topk_id: torch.Tensor, *, mask=None,
+                   balance_coef: float = 0.01, z_coef: float = 0.0, workspace=None,
+                   stream=None) -> RouterBalance:
+    """Balance loss E sum_e (c_e / (n k)) P_e and z loss mean(lse^2) of the router's
+    logits [T, E] (fp32 as Layer.route gives them, or bf16) and its int32 ids [T, k],
+    over the tokens whose mask (bool or uint8 [T]) is not 0."""
+    ld = _rows(logits, "logits")
+    T, E = logits.shape
+    _need(logits.dtype in _DTYPES, "logits must be bf16 or fp32")
+    _need(topk_id.dim() == 2 and topk_id.shape[0] == T, "topk_id must be [T, k]")
+    k, dev = topk_id.shape[1], logits.device
+    with _On(stream, logits, topk_id, mask, workspace) as on:
+        f = torch.empty(3 + E + T, dtype=torch.float32, device=dev)
+        out = RouterBalance(f[:3], torch.empty(E + 1, dtype=torch.int32, device=dev), f[3:3 + E], f[3 + E:])
+        if workspace is None:
+            workspace = torch.empty(router_balance_workspace_bytes(T, E), dtype=torch.uint8, device=dev)
+        p = f.data_ptr()
+        _check(lib().lx_router_balance(
+            _DTYPES[logits.dtype], logits.data_ptr(), ld, _flat(topk_id, "topk_id", T * k, torch.int32),
+            _mask_ptr(mask, T), T, E, k, balance_coef, z_coef, out.counts.data_ptr(), p + 12,
+            p + 12 + 4 * E, p, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+            on.stream.cuda_stream))
+        on.outputs(*out)
+    return out
+
+
+def router_balance_backward(logits: torch.Tensor, state: RouterBalance, k: int, *, dloss=None,
+                            balance_coef: float = 0.01, z_coef: float = 0.0, out=None,
+                            stream=None) -> torch.Tensor:
+    """Gradient of router_balance's loss with respect to the logits, in their type,
+    times dloss (an fp32 device scalar; 1 when omitted); the counts are held fixed.
+    `state` and the coefficients are the forward's, k its ids per token.  ``out`` may
+    be the logits themselves."""
+    ld = _rows(logits, "logits")
+    T, E = logits.shape
+    _need(logits.dtype in _DTYPES, "logits must be bf16 or fp32")
+    with _On(stream, logits, *state, dloss, out) as on:
+        made = out is None
+        if made:
+            out = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
+        _check(lib().lx_router_balance_backward(
+            _DTYPES[logits.dtype], logits.data_ptr(), ld, _flat(state.lse, "lse", T),
+            _flat(state.counts, "counts", E + 1, torch.int32), _flat(dloss, "dloss", 1), T, E, k,
+            balance_coef, z_coef, _flat(out, "out", T * E, logits.dtype), on.stream.cuda_stream))
+        if made:
+            on.outputs(out)
+    return out
+
+
+def distill_loss(logits: torch.Tensor, teacher_id: torch.Tensor, teacher_logit: torch.Tensor, *,
+                 temperature: float = 1.0, teacher_lse=None, kd_weight: float = 1.0, labels=None,
+                 ce_weight: float = 0.0, row_weight=None, want_grad: bool = True, dlogits=None,
+                 stream=None):
+    """Distillation of the student's logits [T, V] (bf16 or fp32) from a teacher's
+    stored top entries (int32 ids and fp32 logits [T, K]), optionally mixed with the
+    cross-entropy of int32 labels [T]:
+
+        loss = row_weight * (kd_weight * temperature^2 * KL + ce_weight * CE)
+
+    teacher_lse (fp32 [T]): log-sum-exp of the teacher's logits over the temperature;
+    the entries then keep their share of its whole distribution, otherwise they are
+    normalised among themselves.  Returns (loss fp32 [T], gradient of its sum with
+    respect to the logits, or None).  ``dlogits`` may be the logits themselves."""
+    ld = _rows(logits, "logits")
+    T, V = logits.shape
+    _need(logits.dtype in _DTYPES, "logits must be bf16 or fp32")
+    _need(teacher_id.dim() == 2 and teacher_id.shape[0] == T, "teacher_id must be [T, K]")
+    K, dev = teacher_id.shape[1], logits.device
+    with _On(stream, logits, teacher_id, teacher_logit, teacher_lse, labels, row_weight, dlogits) as on:
+        loss = torch.empty(T, dtype=torch.float32, device=dev)
+        made = dlogits is None and want_grad
+        if made:
+            dlogits = torch.empty((T, V), dtype=logits.dtype, device=dev)
+        _check(lib().lx_distill_loss(
+            _DTYPES[logits.dtype], logits.data_ptr(), ld,
+            _flat(teacher_id, "teacher_id", T * K, torch.int32),
+            _flat(teacher_logit, "teacher_logit", T * K), _flat(teacher_lse, "teacher_lse", T),
+            _flat(labels, "labels", T, torch.int32), _flat(row_weight, "row_weight", T), T, V, K,
+            temperature, kd_weight, ce_weight, loss.data_ptr(),
+            None if dlogits is None else dlogits.data_ptr(),
+            0 if dlogits is None else _rows(dlogits, "dlogits", logits.shape, logits.dtype),
+            on.stream.cuda_stream))
+        on.outputs(loss, dlogits if made else None)
+    return loss, dlogits
