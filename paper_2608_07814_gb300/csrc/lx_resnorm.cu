@@ -8,16 +8,17 @@
 //   shared by,   f = g D W1,   dy = s1 (f - n mean(f n)),
 //   dw_post = sum_t g D n,   dw_pre = sum_t dh x.
 //
-// Both are bound by memory: a row is read once and stays in registers as fp32 (8
-// elements a thread), so the forward moves r, y (and a full gate), r' and h, the
-// backward r, y, dr', dh, dr and dy; r' is formed again from r and y instead of being
-// read, which costs no bytes and keeps the unrounded values.
+// Both are bound by memory: a row is read once, so the forward moves r, y (and a full
+// gate), r' and h, the backward r, y, dr', dh, dr and dy; r' is formed again from r and
+// y instead of being read, which costs no bytes and keeps the unrounded values.
 //
-// A row is held by a warp (H <= 256), by a CTA (H <= 8192) or by a cluster of CTAs
-// with 8192 columns each.  In the backward, rows are dealt to a resident grid and
-// every thread keeps its columns' parameter gradients in registers; the sums of the
-// CTAs are added in order by a second launch, so results do not change from run to
-// run.
+// A row is held by a part of a warp (H <= 256), a CTA (H <= 4096) or a cluster of CTAs,
+// 8 elements a thread (16 above 32768).  Rows are dealt to a resident grid; a thread
+// copies its own pieces of the next rows into slots of shared memory that it alone
+// reads (cp.async: no barrier), so that two rows are in flight while one is worked on,
+// and keeps its columns' parameters in registers.  In the backward it also keeps their
+// gradient sums there; the CTAs' sums are added in order by a second launch, so results
+// do not change from run to run.
 #include <algorithm>
 
 #include "lx_rows.cuh"
@@ -27,286 +28,461 @@ namespace {
 
 using namespace rows;
 
-constexpr int EPT = 8;             // elements of a row a thread holds
-constexpr int WARP_H = 32 * EPT;   // widest row of a warp
-constexpr int CTA_H = 1024 * EPT;  // widest row of a CTA
+constexpr int WARP_H = 256;       // widest row of a warp
+constexpr int CTA_T = 512;        // threads of a CTA at most
+constexpr int CTA_H = CTA_T * 8;  // widest row of a CTA with 8 elements a thread
 constexpr int MAX_CLUSTER = 8;
-static_assert(CTA_H * MAX_CLUSTER == LX_MAX_WIDTH, "the widest row");
-constexpr int WARP_ROWS = 8;       // rows (warps) of a CTA with a warp to a row
+static_assert(2 * CTA_H * MAX_CLUSTER == LX_MAX_WIDTH, "the widest row: 16 elements a thread");
+constexpr int WARP_T = 256;  // threads of a CTA whose rows are held by parts of warps
+
+// Row arrays that are read
+enum In { IN_Y = 0, IN_R = 1, IN_GATE = 2, IN_DR = 3, IN_DH = 4, N_IN = 5 };
 
 struct NormArgs {
   int T, H, gate_kind;
-  long ldr, ldy, ldg, lddr, lddh;
-  const void *r, *y, *gate;
+  int lanes;              // threads that hold a row's piece (a part of a warp; else the CTA)
+  const void* in[N_IN];   // NULL where absent
+  long ld[N_IN];
+  int slot[N_IN];         // place among the present ones
+  int slots, stages, par_at;      // stages: rows in the slots of a thread, 3 or 2
+  const float* gate;      // channel or token gate
+  long ldg;
   const float *w_post, *w_pre;
   float a, off, eps;
   void *r_out, *h_out;
   float* stats;  // [2][T]: s1, s2
   // backward
-  const void *dr_out, *dh;
   void *dr, *dy, *dgate;
-  float* part;  // [CTAs of a column range][3][H]: dw_post, dgate (channel), dw_pre
+  int sums;     // bits of the parameter gradients: dw_post, dgate (channel), dw_pre
+  float* part;  // [CTAs of a column range][3][H]: their sums
 };
+
+// Registers a thread: the launch bounds below hold the compiler to these
+constexpr int FWD_REGS = 64, BWD_REGS = 96, WIDE_REGS = 128;
 
 enum Group { WARP = 0, CTA = 1, CLUSTER = 2 };
 
-// Which row and which columns a thread works on
-template <int GRP>
-struct Place {
-  int lane, size;  // of the threads that hold a row piece
-  int col0;        // first column of the piece
-  long row, rows;  // first row, rows between two of this group's rows
-  __device__ Place() {
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* dst, const void* src) {
+  const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
+  if constexpr (BYTES == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(d), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// The rows and columns of a thread, and the slots of its pieces.  Pieces are VEC
+// elements: 16 bytes, 4 bytes where rows do not start on 16-byte boundaries, or single
+// bf16 values, which cannot be copied asynchronously and are read where they are used
+// (as are the widest rows, whose slots would not fit).
+template <typename T, int VEC, int EPT, int GRP>
+struct Rows {
+  static constexpr int NCH = EPT / VEC, BYTES = VEC * sizeof(T);
+  static constexpr bool RING = BYTES >= 4 && EPT == 8;
+  const NormArgs& A;
+  char* ring;
+  int lane, size, col0, end;
+  int count;       // pieces of the thread inside the row (they ascend)
+  long row, step;  // first row; distance of this group's rows
+  __device__ Rows(const NormArgs& args, char* smem) : A(args), ring(smem) {
+    col0 = 0;
     if constexpr (GRP == WARP) {
-      lane = threadIdx.x & 31;
-      size = 32;
-      col0 = 0;
-      row = (long)blockIdx.x * WARP_ROWS + (threadIdx.x >> 5);
-      rows = (long)gridDim.x * WARP_ROWS;
+      size = A.lanes;
+      lane = threadIdx.x & (size - 1);
+      row = (long)blockIdx.x * (WARP_T / size) + threadIdx.x / size;
+      step = (long)gridDim.x * (WARP_T / size);
     } else {
-      lane = threadIdx.x;
       size = blockDim.x;
-      col0 = GRP == CTA ? 0 : (int)blockIdx.x * CTA_H;
+      lane = threadIdx.x;
+      if constexpr (GRP == CLUSTER) col0 = blockIdx.x * (CTA_T * EPT);
       row = GRP == CTA ? blockIdx.x : blockIdx.y;
-      rows = GRP == CTA ? gridDim.x : gridDim.y;
+      step = GRP == CTA ? gridDim.x : gridDim.y;
+    }
+    end = GRP == CLUSTER ? min(A.H, col0 + CTA_T * EPT) : A.H;
+    count = 0;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) count += col(c) < end;
+  }
+  // whether some row of this warp (for CTAs: this CTA) is left at round `t` of lane 0
+  __device__ bool more(long t) const {
+    if constexpr (GRP == WARP) return __any_sync(0xffffffffu, t < A.T);
+    else return t < A.T;
+  }
+  __device__ int col(int c) const { return col0 + (c * size + lane) * VEC; }
+  __device__ const T* src(int k, long t, int e) const { return (const T*)A.in[k] + t * A.ld[k] + e; }
+  __device__ char* place(int stage, int k, int c) const {
+    return ring + ((size_t)((stage * A.slots + A.slot[k]) * NCH + c) * blockDim.x + threadIdx.x) * BYTES;
+  }
+  __device__ void fetch(int stage, long t) const {
+    if constexpr (RING) {
+      if (t < A.T)
+#pragma unroll
+        for (int k = 0; k < N_IN; ++k)
+          if (A.in[k]) {
+            const T* p = src(k, t, col(0));
+            char* d = place(stage, k, 0);
+#pragma unroll
+            for (int c = 0; c < NCH; ++c, p += size * VEC, d += blockDim.x * BYTES)
+              if (c < count) copy_async<BYTES>(d, p);
+          }
+      copy_commit();
+    }
+  }
+  // the pieces of array k of row t, zero outside the row
+  __device__ void read(int stage, int k, long t, float* v) const {
+    const char* p = RING ? place(stage, k, 0) : nullptr;
+    const T* g = RING ? nullptr : src(k, t, col(0));
+#pragma unroll
+    for (int c = 0; c < NCH; ++c, p += blockDim.x * BYTES, g += size * VEC) {
+      const bool on = c < count && t < A.T;
+      if constexpr (RING) {
+        if constexpr (BYTES == 16) {
+          load<T, VEC>((const T*)p, v + c * VEC);
+        } else if constexpr (VEC == 1) {
+          v[c] = *(const float*)p;
+        } else {
+          const uint32_t w = *(const uint32_t*)p;
+          v[2 * c] = __uint_as_float(w << 16);
+          v[2 * c + 1] = __uint_as_float(w & 0xffff0000u);
+        }
+        if (!on)
+#pragma unroll
+          for (int j = 0; j < VEC; ++j) v[c * VEC + j] = 0.f;
+      } else {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) v[c * VEC + j] = 0.f;
+        if (on) {
+          if constexpr (BYTES == 4 && VEC == 2) {
+            const uint32_t w = *(const uint32_t*)g;
+            v[2 * c] = __uint_as_float(w << 16);
+            v[2 * c + 1] = __uint_as_float(w & 0xffff0000u);
+          } else {
+            load<T, VEC>(g, v + c * VEC);
+          }
+        }
+      }
+    }
+  }
+  // starts the copies of the first rows; then, each round: those of the row stages - 1
+  // rounds ahead, and a wait for this round's
+  __device__ void begin() const {
+    for (int p = 0; p < A.stages - 1; ++p) fetch(p, row + p * step);
+  }
+  __device__ void advance(int stage, long t) const {
+    if constexpr (RING) {
+      fetch(stage == 0 ? A.stages - 1 : stage - 1, t + (A.stages - 1) * step);
+      if (A.stages == 3) copy_wait<2>();
+      else copy_wait<1>();
+    }
+  }
+  __device__ void write(void* out, long t, const float* v) const {
+    if (t >= A.T) return;
+    T* p = (T*)out + t * A.H + col(0);
+#pragma unroll
+    for (int c = 0; c < NCH; ++c, p += size * VEC)
+      if (c < count) {
+        if constexpr (BYTES == 4 && VEC == 2) {
+          const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * c], v[2 * c + 1]);
+          *(__nv_bfloat162*)p = b;
+        } else {
+          store<T, VEC>(p, v + c * VEC);
+        }
+      }
+  }
+  // fp32 parameters of the thread's columns, `rest` outside
+  __device__ void params(const float* p, float add, float rest, float* v) const {
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) v[c * VEC + j] = p && c < count ? add + p[col(c) + j] : rest;
+  }
+  // sums of N values over the row's threads, the same in each of them; buf (zero at
+  // first) is used in turn: a half is written again only after the barrier that follows
+  // its last reads
+  template <int N>
+  __device__ void sum(float (&v)[N], float (*buf)[N][CTA_T / 32], int& turn) const {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      if (GRP == WARP && o >= size) continue;
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+    }
+    if constexpr (GRP != WARP) {
+      const int nw = blockDim.x >> 5;
+      float(*b)[CTA_T / 32] = buf[turn & 1];
+      ++turn;
+      if ((threadIdx.x & 31) == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) b[i][threadIdx.x >> 5] = v[i];
+      if constexpr (GRP == CTA) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = 0.f;
+#pragma unroll
+        for (int w = 0; w < CTA_T / 32; w += 4)
+          if (w < nw)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+              const float4 p = *(const float4*)&b[i][w];
+              v[i] += (p.x + p.y) + (p.z + p.w);
+            }
+      } else {
+        cooperative_groups::cluster_group cl = cooperative_groups::this_cluster();
+        cl.sync();
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = 0.f;
+        for (unsigned c = 0; c < cl.num_blocks(); ++c) {
+          const float* q = cl.map_shared_rank(&b[0][0], c);
+#pragma unroll
+          for (int i = 0; i < N; ++i)
+            for (int w = 0; w < nw; ++w) v[i] += q[i * (CTA_T / 32) + w];
+        }
+      }
     }
   }
 };
 
-template <int GRP>
-__device__ __forceinline__ float row_sum(float v, float (*buf)[32], int& turn) {
-  if constexpr (GRP == WARP) return warp_sum(v);
-  else return group_sum<GRP == CLUSTER>(v, buf, turn);
+template <int N>
+__device__ __forceinline__ void clear(float (*buf)[N][CTA_T / 32]) {
+  for (int i = threadIdx.x; i < 2 * N * (CTA_T / 32); i += blockDim.x) (&buf[0][0][0])[i] = 0.f;
+  __syncthreads();
 }
 
-// Columns of piece c of a thread: from col(c), VEC of them, or none
-template <int GRP, int VEC>
-__device__ __forceinline__ int col_of(const Place<GRP>& p, int c) {
-  return p.col0 + (c * p.size + p.lane) * VEC;
-}
-template <int GRP>
-__device__ __forceinline__ int col_end(const Place<GRP>& p, int H) {
-  return GRP == CLUSTER ? min(H, p.col0 + CTA_H) : H;
-}
+extern __shared__ uint4 norm_ring[];
 
-// Gate value of row t, element e
-template <typename T, int VEC>
-__device__ __forceinline__ void load_gate(const NormArgs& A, long t, int e, float* g) {
-  if (A.gate_kind == LX_GATE_FULL) {
-    load<T, VEC>((const T*)A.gate + t * A.ldg + e, g);
-  } else {
-#pragma unroll
-    for (int j = 0; j < VEC; ++j)
-      g[j] = A.gate_kind == LX_GATE_CHANNEL ? ((const float*)A.gate)[e + j]
-             : A.gate_kind == LX_GATE_TOKEN ? ((const float*)A.gate)[t * A.ldg]
-                                            : 1.f;
-  }
-}
-
-template <typename T, int VEC, int GRP>
-__global__ void __launch_bounds__(GRP == WARP ? 32 * WARP_ROWS : 1024)
+template <typename T, int VEC, int EPT, int GRP>
+__global__ void __launch_bounds__(CTA_T, EPT == 8 ? 2 : 1)
 k_resnorm_fwd(const NormArgs A) {
-  constexpr int NCH = EPT / VEC;
-  __shared__ float buf[2][32];
+  __shared__ __align__(16) float buf[2][1][CTA_T / 32];
   int turn = 0;
-  const Place<GRP> P;
-  const int end = col_end<GRP>(P, A.H);
+  if (GRP == CTA) clear(buf);
+  const Rows<T, VEC, EPT, GRP> R(A, (char*)norm_ring);
   const float inv = 1.f / (float)A.H;
-  for (long t = P.row; t < A.T; t += P.rows) {
-    float x[EPT], y[EPT];
-    float s1 = 1.f;
-    if (A.y) {
-      float q = 0.f;
+  const bool chan = A.gate_kind == LX_GATE_CHANNEL;
+  float w1[EPT], w2[EPT];  // w1: with the channel gate
+  R.params(A.w_post, A.off, 1.f, w1);
+  R.params(A.w_pre, A.off, 0.f, w2);
+  if (chan) {
+    float g[EPT];
+    R.params(A.gate, 0.f, 0.f, g);
 #pragma unroll
-      for (int c = 0; c < NCH; ++c) {
-        const int e = col_of<GRP, VEC>(P, c);
+    for (int i = 0; i < EPT; ++i) w1[i] *= g[i];
+  }
+  int stage = 0;
+  R.begin();
+  const bool token = A.gate_kind == LX_GATE_TOKEN;
+  float next = token && R.row < A.T ? A.gate[R.row * A.ldg] : 1.f;  // a row's gate is read a round ahead
+  for (long t = R.row; R.more(t); t += R.step) {
+    const float tok = next;
+    if (token && t + R.step < A.T) next = A.gate[(t + R.step) * A.ldg];
+    R.advance(stage, t);
+    float x[EPT];
+    R.read(stage, IN_R, t, x);
+    float s1 = 1.f, s2 = 1.f, q[1];
+    if (A.in[IN_Y]) {
+      float y[EPT];
+      R.read(stage, IN_Y, t, y);
+      if (A.w_post) {
+        q[0] = 0.f;
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) y[c * VEC + j] = 0.f;
-        if (e < end) load<T, VEC>((const T*)A.y + t * A.ldy + e, y + c * VEC);
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) q = fmaf(y[c * VEC + j], y[c * VEC + j], q);
+        for (int i = 0; i < EPT; ++i) q[0] = fmaf(y[i], y[i], q[0]);
+        R.sum(q, buf, turn);
+        s1 = rsqrtf(q[0] * inv + A.eps);
       }
-      if (A.w_post) s1 = rsqrtf(row_sum<GRP>(q, buf, turn) * inv + A.eps);
-    }
-    float q = 0.f;
+      if (A.in[IN_GATE]) {
+        float g[EPT];
+        R.read(stage, IN_GATE, t, g);
 #pragma unroll
-    for (int c = 0; c < NCH; ++c) {
-      const int e = col_of<GRP, VEC>(P, c);
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) x[c * VEC + j] = 0.f;
-      if (e < end) {
-        load<T, VEC>((const T*)A.r + t * A.ldr + e, x + c * VEC);
-        float g[VEC];
-        if (A.y) load_gate<T, VEC>(A, t, e, g);
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          float v = A.a * x[c * VEC + j];
-          if (A.y) {
-            float u = y[c * VEC + j];
-            if (A.w_post) u *= s1 * (A.off + A.w_post[e + j]);
-            v = fmaf(g[j], u, v);
-          }
-          x[c * VEC + j] = v;
-          q = fmaf(v, v, q);
-        }
-        if (A.r_out) store<T, VEC>((T*)A.r_out + t * A.H + e, x + c * VEC);
+        for (int i = 0; i < EPT; ++i) y[i] *= g[i];
       }
+      const float f = s1 * tok;
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) x[i] = fmaf(y[i] * w1[i], f, A.a * x[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) x[i] *= A.a;
     }
-    float s2 = 1.f;
+    if (A.r_out) R.write(A.r_out, t, x);
     if (A.w_pre) {
-      s2 = rsqrtf(row_sum<GRP>(q, buf, turn) * inv + A.eps);
+      q[0] = 0.f;
 #pragma unroll
-      for (int c = 0; c < NCH; ++c) {
-        const int e = col_of<GRP, VEC>(P, c);
-        if (e < end) {
-          float v[VEC];
+      for (int i = 0; i < EPT; ++i) q[0] = fmaf(x[i], x[i], q[0]);
+      R.sum(q, buf, turn);
+      s2 = rsqrtf(q[0] * inv + A.eps);
 #pragma unroll
-          for (int j = 0; j < VEC; ++j) v[j] = x[c * VEC + j] * (s2 * (A.off + A.w_pre[e + j]));
-          store<T, VEC>((T*)A.h_out + t * A.H + e, v);
-        }
-      }
+      for (int i = 0; i < EPT; ++i) x[i] *= s2 * w2[i];
+      R.write(A.h_out, t, x);
     }
-    if (A.stats && P.lane == 0 && P.col0 == 0) {
+    if (A.stats && R.lane == 0 && R.col0 == 0 && t < A.T) {
       A.stats[t] = s1;
       A.stats[(long)A.T + t] = s2;
     }
+    stage = stage + 1 == A.stages ? 0 : stage + 1;
   }
   // a CTA's shared memory outlives its neighbours' reads
   if constexpr (GRP == CLUSTER) cooperative_groups::this_cluster().sync();
 }
 
-// Parameter-gradient sums of a thread: its columns of dw_post, the channel gate, dw_pre
-template <typename T, int VEC, int GRP>
-__global__ void __launch_bounds__(GRP == WARP ? 32 * WARP_ROWS : 1024)
+// With x, D0 = dr' + s2 e and v = g u in hand, one set of sums serves both norms:
+// mean(e x) gives D = D0 - m x, and sum(f n) = sum(D v) = sum(D0 v) - m sum(x v) (for a
+// token's gate the sums are of u, which its gradient needs, and f n is g times them).
+template <typename T, int VEC, int EPT, int GRP>
+__global__ void __launch_bounds__(EPT == 8 ? 640 : CTA_T, 1)
 k_resnorm_bwd(const NormArgs A) {
-  constexpr int NCH = EPT / VEC;
-  __shared__ float buf[2][32];
-  __shared__ float wsum[GRP == WARP ? WARP_ROWS : 1][GRP == WARP ? WARP_H : 1];
+  __shared__ __align__(16) float buf[2][3][CTA_T / 32];
   int turn = 0;
-  const Place<GRP> P;
-  const int end = col_end<GRP>(P, A.H);
+  if (GRP == CTA) clear(buf);
+  const Rows<T, VEC, EPT, GRP> R(A, (char*)norm_ring);
   const float inv = 1.f / (float)A.H;
+  const bool token = A.gate_kind == LX_GATE_TOKEN;
+  // the columns' parameters, in slots that only this thread reads: registers are short
+  float4* par = (float4*)((char*)norm_ring + A.par_at);
+  auto put = [&](int k, const float* v) {
+#pragma unroll
+    for (int i = 0; i < EPT; i += 4)
+      par[(k * (EPT / 4) + i / 4) * blockDim.x + threadIdx.x] = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+  };
+  auto get = [&](int k, float* v) {
+#pragma unroll
+    for (int i = 0; i < EPT; i += 4) {
+      const float4 p = par[(k * (EPT / 4) + i / 4) * blockDim.x + threadIdx.x];
+      v[i] = p.x;
+      v[i + 1] = p.y;
+      v[i + 2] = p.z;
+      v[i + 3] = p.w;
+    }
+  };
+  {
+    float v[EPT];
+    R.params(A.w_post, A.off, 1.f, v);
+    put(0, v);
+    R.params(A.w_pre, A.off, 0.f, v);
+    put(1, v);
+    R.params(A.gate_kind == LX_GATE_CHANNEL ? A.gate : nullptr, 0.f, 1.f, v);
+    put(2, v);
+  }
   float acc[3][EPT];
 #pragma unroll
   for (int i = 0; i < EPT; ++i) acc[0][i] = acc[1][i] = acc[2][i] = 0.f;
-  for (long t = P.row; t < A.T; t += P.rows) {
-    const float s1 = A.stats[t], s2 = A.stats[(long)A.T + t];
-    float n[EPT], D[EPT], x[EPT], g[EPT];  // n: y s1 (or y)
-    float q = 0.f;
+  int stage = 0;
+  R.begin();
+  float n1 = 0.f, n2 = 0.f, ng = 1.f;  // a row's scalars are read a round ahead
+  auto scalars = [&](long t) {
+    if (t >= A.T) return;
+    n1 = A.stats[t];
+    n2 = A.stats[(long)A.T + t];
+    if (token) ng = A.gate[t * A.ldg];
+  };
+  scalars(R.row);
+  for (long t = R.row; R.more(t); t += R.step) {
+    const bool on = t < A.T;
+    const float s1 = n1, s2 = n2, tok = ng;
+    scalars(t + R.step);
+    R.advance(stage, t);
+    float n[EPT], D[EPT], x[EPT], g[EPT];  // n: y s1
+    if (A.in[IN_DR]) R.read(stage, IN_DR, t, D);
+    else
 #pragma unroll
-    for (int c = 0; c < NCH; ++c) {
-      const int e = col_of<GRP, VEC>(P, c);
+      for (int i = 0; i < EPT; ++i) D[i] = 0.f;
+    if (A.in[IN_Y]) {
+      R.read(stage, IN_Y, t, n);
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) n[c * VEC + j] = D[c * VEC + j] = x[c * VEC + j] = g[c * VEC + j] = 0.f;
-      if (e < end) {
-        if (A.y) {
-          load<T, VEC>((const T*)A.y + t * A.ldy + e, n + c * VEC);
-          load_gate<T, VEC>(A, t, e, g + c * VEC);
-        }
-        if (A.dr_out) load<T, VEC>((const T*)A.dr_out + t * A.lddr + e, D + c * VEC);
-        if (A.dh) {
-          float dh[VEC];
-          load<T, VEC>((const T*)A.dh + t * A.lddh + e, dh);
-          load<T, VEC>((const T*)A.r + t * A.ldr + e, x + c * VEC);
+      for (int i = 0; i < EPT; ++i) n[i] *= s1;
+      if (A.in[IN_GATE]) {
+        R.read(stage, IN_GATE, t, g);
+      } else {
 #pragma unroll
-          for (int j = 0; j < VEC; ++j) {
-            const int i = c * VEC + j;
-            float v = A.a * x[i];
-            if (A.y) {
-              float u = n[i];
-              if (A.w_post) u *= s1 * (A.off + A.w_post[e + j]);
-              v = fmaf(g[i], u, v);
-            }
-            x[i] = v * s2;
-            acc[2][i] = fmaf(dh[j], x[i], acc[2][i]);
-            const float ev = dh[j] * (A.off + A.w_pre[e + j]);
-            q = fmaf(ev, x[i], q);
-            D[i] = fmaf(s2, ev, D[i]);
-          }
-        }
+        for (int i = 0; i < EPT; ++i) g[i] = 1.f;
+        if (A.gate_kind == LX_GATE_CHANNEL) get(2, g);
       }
     }
-    if (A.dh) {
-      const float m = row_sum<GRP>(q, buf, turn) * inv * s2;
+    float w1[EPT];
+    get(0, w1);
+    float q[3] = {0.f, 0.f, 0.f};
+    if (A.in[IN_DH]) {
+      float dh[EPT], w2[EPT];
+      get(1, w2);
+      R.read(stage, IN_R, t, x);
+      R.read(stage, IN_DH, t, dh);
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) D[i] = fmaf(-m, x[i], D[i]);
+      for (int i = 0; i < EPT; ++i) {
+        float v = A.a * x[i];
+        if (A.in[IN_Y]) v = fmaf(n[i] * w1[i], g[i] * tok, v);
+        x[i] = v * s2;
+        acc[2][i] = fmaf(dh[i], x[i], acc[2][i]);
+        const float e = dh[i] * w2[i];
+        q[0] = fmaf(e, x[i], q[0]);
+        D[i] = fmaf(s2, e, D[i]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) x[i] = 0.f;
     }
-    float q1 = 0.f, q2 = 0.f;  // f n and D u
+    if (A.in[IN_Y]) {
 #pragma unroll
-    for (int c = 0; c < NCH; ++c) {
-      const int e = col_of<GRP, VEC>(P, c);
-      if (e < end) {
-        float v[VEC];
-        if (A.dr) {
-#pragma unroll
-          for (int j = 0; j < VEC; ++j) v[j] = A.a * D[c * VEC + j];
-          store<T, VEC>((T*)A.dr + t * A.H + e, v);
-        }
-        if (A.y) {
-#pragma unroll
-          for (int j = 0; j < VEC; ++j) {
-            const int i = c * VEC + j;
-            const float w = A.w_post ? A.off + A.w_post[e + j] : 1.f;
-            n[i] *= s1;
-            const float du = D[i] * (n[i] * w);
-            q2 += du;
-            acc[1][i] += du;
-            v[j] = du;
-            const float f = g[i] * D[i];
-            acc[0][i] = fmaf(f, n[i], acc[0][i]);
-            D[i] = f * w;
-            q1 = fmaf(D[i], n[i], q1);
-          }
-          if (A.gate_kind == LX_GATE_FULL && A.dgate) store<T, VEC>((T*)A.dgate + t * A.H + e, v);
-        }
+      for (int i = 0; i < EPT; ++i) {
+        const float v = n[i] * w1[i] * g[i];
+        q[1] = fmaf(D[i], v, q[1]);
+        q[2] = fmaf(x[i], v, q[2]);
       }
     }
-    if (A.y) {
-      float m = 0.f;
-      if (A.w_post) m = row_sum<GRP>(q1, buf, turn) * inv;
-      if (A.gate_kind == LX_GATE_TOKEN && A.dgate) {
-        const float d = row_sum<GRP>(q2, buf, turn);
-        if (P.lane == 0 && P.col0 == 0) ((float*)A.dgate)[t] = d;
-      }
-      if (A.dy) {
+    R.sum(q, buf, turn);
+    const float m = q[0] * inv * s2;
+    const float dv = q[1] - m * q[2];
+    const float m1 = A.w_post ? dv * inv * tok : 0.f;
 #pragma unroll
-        for (int c = 0; c < NCH; ++c) {
-          const int e = col_of<GRP, VEC>(P, c);
-          if (e < end) {
-            float v[VEC];
+    for (int i = 0; i < EPT; ++i) D[i] = fmaf(-m, x[i], D[i]);
+    if (A.dr) {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) v[j] = s1 * fmaf(-m, n[c * VEC + j], D[c * VEC + j]);
-            store<T, VEC>((T*)A.dy + t * A.H + e, v);
-          }
-        }
-      }
+      for (int i = 0; i < EPT; ++i) x[i] = A.a * D[i];
+      R.write(A.dr, t, x);
     }
+    if (A.in[IN_Y]) {
+      if (token && A.dgate && R.lane == 0 && R.col0 == 0 && on) ((float*)A.dgate)[t] = dv;
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) {
+        x[i] = D[i] * (n[i] * w1[i]);
+        acc[1][i] += x[i];
+        const float f = D[i] * (g[i] * tok);
+        acc[0][i] = fmaf(f, n[i], acc[0][i]);
+        D[i] = s1 * fmaf(-m1, n[i], f * w1[i]);
+      }
+      if (A.in[IN_GATE] && A.dgate) R.write(A.dgate, t, x);
+      if (A.dy) R.write(A.dy, t, D);
+    }
+    stage = stage + 1 == A.stages ? 0 : stage + 1;
   }
   if (A.part) {
     float* part = A.part + (GRP == CLUSTER ? (long)blockIdx.y : (long)blockIdx.x) * 3 * A.H;
+    float* ws = (float*)norm_ring;  // [rows of the CTA][H], the ring's copies being done
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
+      if (!(A.sums >> k & 1)) continue;
       if constexpr (GRP == WARP) {
+        copy_wait<0>();
         __syncthreads();
 #pragma unroll
-        for (int c = 0; c < NCH; ++c)
+        for (int c = 0; c < R.NCH; ++c)
 #pragma unroll
           for (int j = 0; j < VEC; ++j)
-            wsum[threadIdx.x >> 5][col_of<GRP, VEC>(P, c) + j] = acc[k][c * VEC + j];
+            if (R.col(c) + j < A.H) ws[(threadIdx.x / R.size) * A.H + R.col(c) + j] = acc[k][c * VEC + j];
         __syncthreads();
-        for (int e = threadIdx.x; e < A.H; e += 32 * WARP_ROWS) {
+        for (int e = threadIdx.x; e < A.H; e += WARP_T) {
           float s = 0.f;
-          for (int w = 0; w < WARP_ROWS; ++w) s += wsum[w][e];
+          for (int w = 0; w < WARP_T / R.size; ++w) s += ws[w * A.H + e];
           part[(long)k * A.H + e] = s;
         }
       } else {
 #pragma unroll
-        for (int c = 0; c < NCH; ++c) {
-          const int e = col_of<GRP, VEC>(P, c);
-          if (e < end)
+        for (int c = 0; c < R.NCH; ++c)
+          if (R.col(c) < R.end)
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) part[(long)k * A.H + e + j] = acc[k][c * VEC + j];
-        }
+            for (int j = 0; j < VEC; ++j) part[(long)k * A.H + R.col(c) + j] = acc[k][c * VEC + j];
       }
     }
   }
@@ -324,6 +500,7 @@ k_resnorm_sum(const float* __restrict__ part, int n, int H, float* o0, float* o1
   const int e = blockIdx.x * 32 + lane;
   float s = 0.f;
   if (e < H)
+#pragma unroll 8
     for (int p = w; p < n; p += 8) s += part[((long)p * 3 + k) * H + e];
   sm[w][lane] = s;
   __syncthreads();
@@ -335,30 +512,52 @@ k_resnorm_sum(const float* __restrict__ part, int n, int H, float* o0, float* o1
 }
 
 struct Shape {
-  int grp, threads, cols;  // cols: CTAs to a row
-  long groups;             // rows in work at once with one CTA (or cluster) each
+  int grp, ept, threads, cols, lanes;  // cols: CTAs to a row
+  long groups;                         // CTAs (clusters) that have a row
 };
 
 Shape shape_of(int T, int H) {
   Shape s;
   s.grp = H <= WARP_H ? WARP : H <= CTA_H ? CTA : CLUSTER;
-  s.cols = s.grp == CLUSTER ? (H + CTA_H - 1) / CTA_H : 1;
-  s.threads = s.grp == WARP ? 32 * WARP_ROWS : s.grp == CTA ? (((H + EPT - 1) / EPT + 31) / 32) * 32 : 1024;
-  s.groups = s.grp == WARP ? ((long)T + WARP_ROWS - 1) / WARP_ROWS : T;
+  s.ept = H <= CTA_H * MAX_CLUSTER ? 8 : 16;
+  s.cols = s.grp == CLUSTER ? (H + CTA_T * s.ept - 1) / (CTA_T * s.ept) : 1;
+  s.lanes = 1;
+  while (s.lanes < 32 && s.lanes * 8 < H) s.lanes *= 2;
+  s.threads = s.grp == WARP ? WARP_T : s.grp == CTA ? (H + 255) / 256 * 32 : CTA_T;
+  s.groups = s.grp == WARP ? ((long)T + WARP_T / s.lanes - 1) / (WARP_T / s.lanes) : T;
   return s;
 }
 
-// CTAs (or clusters) that the backward deals its rows to: two CTAs an SM of the GB300
-long bwd_groups(const Shape& s) {
-  const long res = s.grp == CLUSTER ? 152 / s.cols : s.grp == WARP ? 152 * 4 : 152 * std::max(1, 1024 / s.threads);
-  return std::min(s.groups, std::max(1L, res));
+constexpr int SMS = 152;
+
+// CTAs (clusters) that rows are dealt to: what is resident with `regs` registers a
+// thread and `smem` bytes a CTA
+long resident(const Shape& s, int regs, size_t smem) {
+  const long ctas = std::min<long>(65536 / (regs * s.threads), (long)(227 * 1024 / (smem + 2048)));
+  return std::min(s.groups, std::max(1L, SMS * std::max(1L, ctas) / s.cols));
+}
+
+// The backward's groups fix the workspace: they do not depend on types or strides
+long bwd_groups(const Shape& s) { return resident(s, s.ept == 8 ? BWD_REGS : WIDE_REGS, 0); }
+
+// Slots of a CTA: three rows, or two where three would keep CTAs off an SM that its
+// registers have room for (fp32 with a full gate)
+size_t ring_bytes(const Shape& s, NormArgs& A, size_t es, int regs, size_t more) {
+  const size_t row = (size_t)A.slots * s.ept * es * s.threads;
+  A.stages = (3 * row + more + 1024) * (65536 / (regs * s.threads)) <= 227 * 1024 ? 3 : 2;
+  return A.stages * row;
 }
 
 template <typename... KArgs>
-lx_status launch(void (*kern)(KArgs...), const Shape& s, long groups, const NormArgs& A, cudaStream_t st) {
+lx_status launch(void (*kern)(KArgs...), const Shape& s, long groups, size_t smem, const NormArgs& A, cudaStream_t st,
+                 bool (&cap)[64]) {
+  int dev = 0;
+  LX_CUDA(cudaGetDevice(&dev));
+  LX_CUDA(smem_cap_once((const void*)kern, 224 * 1024, dev, cap));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = s.grp == CLUSTER ? dim3(s.cols, (unsigned)groups) : dim3((unsigned)groups);
   cfg.blockDim = dim3(s.threads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -370,20 +569,37 @@ lx_status launch(void (*kern)(KArgs...), const Shape& s, long groups, const Norm
   return LX_OK;
 }
 
-template <typename T, bool BWD>
-lx_status launch_type(bool vec, const Shape& s, long groups, const NormArgs& A, cudaStream_t st) {
-  constexpr int V = 16 / sizeof(T);
-#define LX_NORM_CASE(VEC, GRP) \
-  return BWD ? launch(k_resnorm_bwd<T, VEC, GRP>, s, groups, A, st) : launch(k_resnorm_fwd<T, VEC, GRP>, s, groups, A, st)
-  if (vec) {
-    if (s.grp == WARP) LX_NORM_CASE(V, WARP);
-    if (s.grp == CTA) LX_NORM_CASE(V, CTA);
-    LX_NORM_CASE(V, CLUSTER);
-  }
-  if (s.grp == WARP) LX_NORM_CASE(1, WARP);
-  if (s.grp == CTA) LX_NORM_CASE(1, CTA);
-  LX_NORM_CASE(1, CLUSTER);
-#undef LX_NORM_CASE
+template <typename T, int VEC, int EPT, int GRP, bool BWD>
+lx_status launch_one(const Shape& s, NormArgs& A, cudaStream_t st) {
+  static bool cap[64] = {};
+  constexpr int REGS = EPT == 16 ? WIDE_REGS : BWD ? BWD_REGS : FWD_REGS;
+  const size_t par = BWD ? sizeof(float) * 3 * EPT * s.threads : 0;
+  size_t smem = 0;
+  A.stages = 2;
+  if (VEC * sizeof(T) >= 4 && EPT == 8) smem = ring_bytes(s, A, sizeof(T), REGS, par);
+  A.par_at = (int)smem;
+  smem += par;
+  if (BWD && GRP == WARP) smem = std::max(smem, sizeof(float) * (WARP_T / s.lanes) * A.H);
+  if (BWD) return launch(k_resnorm_bwd<T, VEC, EPT, GRP>, s, bwd_groups(s), smem, A, st, cap);
+  return launch(k_resnorm_fwd<T, VEC, EPT, GRP>, s, resident(s, REGS, smem), smem, A, st, cap);
+}
+
+template <typename T, int VEC, bool BWD>
+lx_status launch_vec(const Shape& s, NormArgs& A, cudaStream_t st) {
+  if (s.grp == WARP) return launch_one<T, VEC, 8, WARP, BWD>(s, A, st);
+  if (s.grp == CTA) return launch_one<T, VEC, 8, CTA, BWD>(s, A, st);
+  if (s.ept == 8) return launch_one<T, VEC, 8, CLUSTER, BWD>(s, A, st);
+  return launch_one<T, VEC, 16, CLUSTER, BWD>(s, A, st);
+}
+
+// piece: bytes that divide every row's start and length (16, 4, or 2)
+template <bool BWD>
+lx_status launch_any(int dtype, int piece, const Shape& s, NormArgs& A, cudaStream_t st) {
+  if (dtype == LX_F32)
+    return piece == 16 ? launch_vec<float, 4, BWD>(s, A, st) : launch_vec<float, 1, BWD>(s, A, st);
+  if (piece == 16) return launch_vec<__nv_bfloat16, 8, BWD>(s, A, st);
+  if (piece == 4) return launch_vec<__nv_bfloat16, 2, BWD>(s, A, st);
+  return launch_vec<__nv_bfloat16, 1, BWD>(s, A, st);
 }
 
 size_t esize(int dtype) { return dtype == LX_BF16 ? 2 : 4; }
@@ -410,17 +626,23 @@ lx_status check_desc(const lx_resnorm_desc* d) {
   return LX_OK;
 }
 
-NormArgs args_of(const lx_resnorm_desc* d) {
+NormArgs args_of(const lx_resnorm_desc* d, const Shape& s) {
   NormArgs A = {};
   A.T = d->T;
   A.H = d->H;
   A.gate_kind = d->gate_kind;
-  A.ldr = d->ldr;
-  A.ldy = d->ldy;
-  A.ldg = d->ldg;
-  A.r = d->r;
-  A.y = d->y;
-  A.gate = d->gate;
+  A.lanes = s.lanes;
+  A.in[IN_Y] = d->y;
+  A.ld[IN_Y] = d->ldy;
+  A.in[IN_R] = d->r;
+  A.ld[IN_R] = d->ldr;
+  if (d->gate_kind == LX_GATE_FULL) {
+    A.in[IN_GATE] = d->gate;
+    A.ld[IN_GATE] = d->ldg;
+  } else {
+    A.gate = (const float*)d->gate;
+    A.ldg = d->ldg;
+  }
   A.w_post = d->w_post;
   A.w_pre = d->w_pre;
   A.a = d->res_scale;
@@ -429,8 +651,19 @@ NormArgs args_of(const lx_resnorm_desc* d) {
   return A;
 }
 
-// whether every row of p starts on a 16-byte boundary
-bool rows16(const void* p, long ld, size_t es) { return !p || (aligned(p, 16) && ld * es % 16 == 0); }
+// Numbers the arrays that are read and finds the widest piece that divides every row's
+// start and length: 16 bytes, 4, or one bf16
+int pieces(NormArgs& A, size_t es, std::initializer_list<const void*> outs) {
+  uintptr_t bits = (uintptr_t)A.H * es;
+  A.slots = 0;
+  for (int k = 0; k < N_IN; ++k)
+    if (A.in[k]) {
+      A.slot[k] = A.slots++;
+      bits |= (uintptr_t)A.in[k] | (uintptr_t)((size_t)A.ld[k] * es);
+    }
+  for (const void* p : outs) bits |= (uintptr_t)p;
+  return bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2;
+}
 
 }  // namespace
 }  // namespace lx
@@ -454,18 +687,12 @@ extern "C" lx_status lx_residual_norm(const lx_resnorm_desc* d, void* r_out, voi
       overlap(h_out, out, d->r, sr) || overlap(h_out, out, d->y, sy) || overlap(h_out, out, d->gate, sg) ||
       overlap(r_out, out, h_out, out))
     return fail(LX_ERR_ARG, "an output overlaps an input");
-  NormArgs A = args_of(d);
+  const Shape s = shape_of(d->T, d->H);
+  NormArgs A = args_of(d, s);
   A.r_out = r_out;
   A.h_out = h_out;
   A.stats = stats;
-  const bool vec = d->H % (16 / es) == 0 && rows16(d->r, d->ldr, es) && rows16(d->y, d->ldy, es) &&
-                   (d->gate_kind != LX_GATE_FULL || rows16(d->gate, d->ldg, es)) && aligned(r_out, 16) &&
-                   aligned(h_out, 16);
-  const Shape s = shape_of(d->T, d->H);
-  const long groups = s.grp == CLUSTER ? std::min(s.groups, 65535L) : s.groups;
-  cudaStream_t st = (cudaStream_t)stream;
-  return d->dtype == LX_BF16 ? launch_type<__nv_bfloat16, false>(vec, s, groups, A, st)
-                             : launch_type<float, false>(vec, s, groups, A, st);
+  return launch_any<false>(d->dtype, pieces(A, es, {r_out, h_out}), s, A, (cudaStream_t)stream);
 }
 
 extern "C" lx_status lx_residual_norm_workspace(int32_t T, int32_t H, uint64_t* bytes) {
@@ -506,34 +733,32 @@ extern "C" lx_status lx_residual_norm_backward(const lx_resnorm_desc* d, const f
   const void* ins[] = {d->r, d->y, d->gate_kind == LX_GATE_FULL ? d->gate : nullptr, dr_out, dh};
   const long lds[] = {(long)d->ldr, (long)d->ldy, (long)d->ldg, (long)lddr, (long)lddh};
   void* outs[] = {dr, dy, d->gate_kind == LX_GATE_FULL ? dgate : nullptr};
-  bool vec = d->H % (16 / es) == 0;
   for (int i = 0; i < 3; ++i) {
-    vec = vec && aligned(outs[i], 16);
     for (int j = 0; j < 5; ++j)
       if (overlap(outs[i], out, ins[j], span(d->T, d->H, lds[j], es)))
         return fail(LX_ERR_ARG, "an output overlaps an input");
     for (int j = 0; j < i; ++j)
       if (overlap(outs[i], out, outs[j], out)) return fail(LX_ERR_ARG, "two outputs overlap");
   }
-  for (int j = 0; j < 5; ++j) vec = vec && rows16(ins[j], lds[j], es);
   const Shape s = shape_of(d->T, d->H);
   const long groups = bwd_groups(s);
   if (params) {
     if (!workspace || !aligned(workspace, 16)) return fail(LX_ERR_ARG, "workspace is NULL or not 16-byte aligned");
     if (workspace_bytes < (uint64_t)groups * 3 * d->H * sizeof(float)) return fail(LX_ERR_ARG, "workspace too small");
   }
-  NormArgs A = args_of(d);
+  NormArgs A = args_of(d, s);
+  if (!dh) A.in[IN_R] = nullptr;  // only the second norm's gradient reads r
   A.stats = const_cast<float*>(stats);
-  A.dr_out = dr_out;
-  A.lddr = lddr;
-  A.dh = dh;
-  A.lddh = lddh;
+  A.in[IN_DR] = dr_out;
+  A.ld[IN_DR] = lddr;
+  A.in[IN_DH] = dh;
+  A.ld[IN_DH] = lddh;
   A.dr = dr;
   A.dy = dy;
   A.dgate = dgate;
   A.part = params ? (float*)workspace : nullptr;
-  LX_TRY(d->dtype == LX_BF16 ? (launch_type<__nv_bfloat16, true>(vec, s, groups, A, st))
-                             : (launch_type<float, true>(vec, s, groups, A, st)));
+  A.sums = (dw_post ? 1 : 0) | (dgc ? 2 : 0) | (dw_pre ? 4 : 0);
+  LX_TRY(launch_any<true>(d->dtype, pieces(A, es, {outs[0], outs[1], outs[2]}), s, A, st));
   if (params) {
     k_resnorm_sum<<<dim3((d->H + 31) / 32, 3), 256, 0, st>>>(A.part, (int)groups, d->H, dw_post, dgc, dw_pre);
     LX_CUDA(cudaGetLastError());

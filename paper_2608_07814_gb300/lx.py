@@ -486,60 +486,45 @@ def _flat(t: Optional[torch.Tensor], name: str, n: int, dtype=torch.float32):
     return t.data_ptr()
 
 
-class _On:
-    """Runs a call's allocations and launches on `stream`.  Tensors made there belong
-    to it; the inputs, and the outputs towards the caller's stream, are marked as used
-    on both, so that their memory is not given away early."""
-
-    def __init__(self, stream, *tensors):
-        self.other = torch.cuda.current_stream()
-        self.side = stream is not None and stream != self.other
-        self.stream = stream if self.side else self.other
-        self.tensors = tensors
-
-    def __enter__(self):
-        if self.side:
-            self.ctx = torch.cuda.stream(self.stream)
-            self.ctx.__enter__()
-            for t in self.tensors:
-                if t is not None:
-                    t.record_stream(self.stream)
-        return self
-
-    def outputs(self, *tensors):
-        if self.side:
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(self.other)
-
-    def __exit__(self, *exc):
-        if self.side:
-            self.ctx.__exit__(*exc)
-        return False
+def _run(stream, inputs, call):
+    """call(raw stream) on `stream`, or on the current one when None.  What a call on
+    another stream allocates belongs to that stream; its inputs, and the outputs towards
+    the current stream, are marked as used on both, so that no memory is given away
+    early.  The order of the two streams is the caller's."""
+    if stream is None:
+        return call(torch._C._cuda_getCurrentRawStream(inputs[0].get_device()))
+    here = torch.cuda.current_stream()
+    if stream == here:
+        return call(stream.cuda_stream)
+    for t in inputs:
+        if t is not None:
+            t.record_stream(stream)
+    with torch.cuda.stream(stream):
+        out = call(stream.cuda_stream)
+    for t in out:
+        if t is not None:
+            t.record_stream(here)
+    return out
 
 
 def _resnorm_desc(r, y, w_post, gate, w_pre, res_scale, weight_offset, eps) -> ResnormDesc:
     ldr = _rows(r, "r")
     T, H = r.shape
     _need(r.dtype in _DTYPES, "r must be bf16 or fp32")
-    d = ResnormDesc(_DTYPES[r.dtype], T, H, LX_GATE_NONE, ldr, 0, 0, r.data_ptr(), None, None,
-                    _flat(w_post, "w_post", H), _flat(w_pre, "w_pre", H), res_scale, weight_offset, eps)
+    kind = ldy = ldg = 0
+    yp = gp = None
     if y is not None:
-        d.ldy = _rows(y, "y", r.shape, r.dtype)
-        d.y = y.data_ptr()
+        ldy, yp = _rows(y, "y", r.shape, r.dtype), y.data_ptr()
     if gate is not None:
         if gate.dim() == 1:
-            d.gate_kind = LX_GATE_CHANNEL
-            d.gate = _flat(gate, "a gate of one dimension", H)
+            kind, gp = LX_GATE_CHANNEL, _flat(gate, "a gate of one dimension", H)
         elif gate.shape == (T, 1) and (H != 1 or gate.dtype == torch.float32):
-            d.gate_kind = LX_GATE_TOKEN
-            d.ldg = _rows(gate, "gate", None, torch.float32)
-            d.gate = gate.data_ptr()
+            kind, ldg, gp = LX_GATE_TOKEN, _rows(gate, "gate", None, torch.float32), gate.data_ptr()
         else:
-            d.gate_kind = LX_GATE_FULL
-            d.ldg = _rows(gate, "gate", r.shape, r.dtype)
-            d.gate = gate.data_ptr()
-    return d
+            kind, ldg, gp = LX_GATE_FULL, _rows(gate, "gate", r.shape, r.dtype), gate.data_ptr()
+    return ResnormDesc(_DTYPES[r.dtype], T, H, kind, ldr, ldy, ldg, r.data_ptr(), yp, gp,
+                       _flat(w_post, "w_post", H), _flat(w_pre, "w_pre", H), res_scale, weight_offset,
+                       eps)
 
 
 def residual_norm(r: torch.Tensor, y: Optional[torch.Tensor] = None, *, w_post=None, gate=None,
@@ -557,21 +542,19 @@ def residual_norm(r: torch.Tensor, y: Optional[torch.Tensor] = None, *, w_post=N
     itself unless res_scale is not 1 or a buffer is given.  ``r_out`` may be r (in
     place).  ``stats``: fp32 [2, T] for residual_norm_backward."""
     d = _resnorm_desc(r, y, w_post, gate, w_pre, res_scale, weight_offset, eps)
-    T, H = r.shape
-    with _On(stream, r, y, w_post, gate, w_pre, r_out, h_out, stats) as on:
-        made = []
-        write_r = r_out is not None or y is not None or res_scale != 1.0
-        if write_r and r_out is None:
-            r_out = torch.empty((T, H), dtype=r.dtype, device=r.device)
-            made.append(r_out)
-        if w_pre is not None and h_out is None:
-            h_out = torch.empty((T, H), dtype=r.dtype, device=r.device)
-            made.append(h_out)
-        _check(lib().lx_residual_norm(d, _flat(r_out, "r_out", T * H, r.dtype) if write_r else None,
-                                      _flat(h_out, "h_out", T * H, r.dtype),
-                                      _flat(stats, "stats", 2 * T), on.stream.cuda_stream))
-        on.outputs(*made)
-    return (r_out if write_r else r), h_out
+    n = r.numel()
+    write_r = r_out is not None or y is not None or res_scale != 1.0
+
+    def call(s):
+        ro = None if not write_r else r_out if r_out is not None else torch.empty(
+            r.shape, dtype=r.dtype, device=r.device)
+        h = h_out if h_out is not None or w_pre is None else torch.empty(r.shape, dtype=r.dtype,
+                                                                         device=r.device)
+        _check(lib().lx_residual_norm(d, _flat(ro, "r_out", n, r.dtype), _flat(h, "h_out", n, r.dtype),
+                                      _flat(stats, "stats", 2 * d.T), s))
+        return (ro if write_r else r), h
+
+    return _run(stream, (r, y, w_post, gate, w_pre, stats), call)
 
 
 class ResidualNormGrads(NamedTuple):
@@ -597,27 +580,24 @@ def residual_norm_backward(dr_out, dh, r, y, stats, *, w_post=None, gate=None, w
     forward's (r as it was before the call) and the stats it wrote."""
     d = _resnorm_desc(r, y, w_post, gate, w_pre, res_scale, weight_offset, 0.0)
     T, H = r.shape
-    dev = r.device
-    with _On(stream, dr_out, dh, r, y, stats, w_post, gate, w_pre, workspace) as on:
-        empty = lambda like, shape, dtype: None if like is None else torch.empty(  # noqa: E731
-            shape, dtype=dtype, device=dev)
-        g = ResidualNormGrads(empty(r, (T, H), r.dtype), empty(y, (T, H), r.dtype),
-                              empty(w_post, (H,), torch.float32),
-                              empty(gate, gate.shape if gate is not None else (),
-                                    gate.dtype if gate is not None else None),
-                              empty(w_pre, (H,), torch.float32))
-        if workspace is None:
-            workspace = torch.empty(residual_norm_workspace_bytes(T, H), dtype=torch.uint8, device=dev)
+    lddr = 0 if dr_out is None else _rows(dr_out, "dr_out", r.shape, r.dtype)
+    lddh = 0 if dh is None else _rows(dh, "dh", r.shape, r.dtype)
+
+    def call(s):
+        new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=r.device)  # noqa: E731
+        g = ResidualNormGrads(new((T, H), r.dtype), None if y is None else new((T, H), r.dtype),
+                              None if w_post is None else new((H,), torch.float32),
+                              None if gate is None else new(gate.shape, gate.dtype),
+                              None if w_pre is None else new((H,), torch.float32))
+        ws = workspace
+        if ws is None:
+            ws = new(residual_norm_workspace_bytes(T, H), torch.uint8)
         _check(lib().lx_residual_norm_backward(
-            d, _flat(stats, "stats", 2 * T),
-            None if dr_out is None else dr_out.data_ptr(),
-            0 if dr_out is None else _rows(dr_out, "dr_out", r.shape, r.dtype),
-            None if dh is None else dh.data_ptr(),
-            0 if dh is None else _rows(dh, "dh", r.shape, r.dtype),
-            *[None if t is None else t.data_ptr() for t in g], workspace.data_ptr(),
-            workspace.numel() * workspace.element_size(), on.stream.cuda_stream))
-        on.outputs(*g)
-    return g
+            d, _flat(stats, "stats", 2 * T), _ptr(dr_out), lddr, _ptr(dh), lddh, *[_ptr(t) for t in g],
+            ws.data_ptr(), ws.numel() * ws.element_size(), s))
+        return g
+
+    return _run(stream, (r, dr_out, dh, y, stats, w_post, gate, w_pre, workspace), call)
 
 
 class RouterBalance(NamedTuple):
@@ -655,19 +635,23 @@ def router_balance(logits: torch.Tensor, topk_id: torch.Tensor, *, mask=None,
     _need(logits.dtype in _DTYPES, "logits must be bf16 or fp32")
     _need(topk_id.dim() == 2 and topk_id.shape[0] == T, "topk_id must be [T, k]")
     k, dev = topk_id.shape[1], logits.device
-    with _On(stream, logits, topk_id, mask, workspace) as on:
+    ids = _flat(topk_id, "topk_id", T * k, torch.int32)
+    m = _mask_ptr(mask, T)
+
+    def call(s):
         f = torch.empty(3 + E + T, dtype=torch.float32, device=dev)
-        out = RouterBalance(f[:3], torch.empty(E + 1, dtype=torch.int32, device=dev), f[3:3 + E], f[3 + E:])
-        if workspace is None:
-            workspace = torch.empty(router_balance_workspace_bytes(T, E), dtype=torch.uint8, device=dev)
+        loss, prob, lse = f.split((3, E, T))
+        counts = torch.empty(E + 1, dtype=torch.int32, device=dev)
+        ws = workspace
+        if ws is None:
+            ws = torch.empty(router_balance_workspace_bytes(T, E), dtype=torch.uint8, device=dev)
         p = f.data_ptr()
-        _check(lib().lx_router_balance(
-            _DTYPES[logits.dtype], logits.data_ptr(), ld, _flat(topk_id, "topk_id", T * k, torch.int32),
-            _mask_ptr(mask, T), T, E, k, balance_coef, z_coef, out.counts.data_ptr(), p + 12,
-            p + 12 + 4 * E, p, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-            on.stream.cuda_stream))
-        on.outputs(*out)
-    return out
+        _check(lib().lx_router_balance(_DTYPES[logits.dtype], logits.data_ptr(), ld, ids, m, T, E, k,
+                                       balance_coef, z_coef, counts.data_ptr(), p + 12, p + 12 + 4 * E, p,
+                                       ws.data_ptr(), ws.numel() * ws.element_size(), s))
+        return RouterBalance(loss, counts, prob, lse)
+
+    return _run(stream, (logits, topk_id, mask, workspace), call)
 
 
 def router_balance_backward(logits: torch.Tensor, state: RouterBalance, k: int, *, dloss=None,
@@ -680,17 +664,16 @@ def router_balance_backward(logits: torch.Tensor, state: RouterBalance, k: int, 
     ld = _rows(logits, "logits")
     T, E = logits.shape
     _need(logits.dtype in _DTYPES, "logits must be bf16 or fp32")
-    with _On(stream, logits, *state, dloss, out) as on:
-        made = out is None
-        if made:
-            out = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
+
+    def call(s):
+        d = out if out is not None else torch.empty((T, E), dtype=logits.dtype, device=logits.device)
         _check(lib().lx_router_balance_backward(
             _DTYPES[logits.dtype], logits.data_ptr(), ld, _flat(state.lse, "lse", T),
             _flat(state.counts, "counts", E + 1, torch.int32), _flat(dloss, "dloss", 1), T, E, k,
-            balance_coef, z_coef, _flat(out, "out", T * E, logits.dtype), on.stream.cuda_stream))
-        if made:
-            on.outputs(out)
-    return out
+            balance_coef, z_coef, _flat(d, "out", T * E, logits.dtype), s))
+        return (d,)
+
+    return _run(stream, (logits, *state, dloss), call)[0]
 
 
 def distill_loss(logits: torch.Tensor, teacher_id: torch.Tensor, teacher_logit: torch.Tensor, *,
@@ -712,19 +695,18 @@ def distill_loss(logits: torch.Tensor, teacher_id: torch.Tensor, teacher_logit: 
     _need(logits.dtype in _DTYPES, "logits must be bf16 or fp32")
     _need(teacher_id.dim() == 2 and teacher_id.shape[0] == T, "teacher_id must be [T, K]")
     K, dev = teacher_id.shape[1], logits.device
-    with _On(stream, logits, teacher_id, teacher_logit, teacher_lse, labels, row_weight, dlogits) as on:
-        loss = torch.empty(T, dtype=torch.float32, device=dev)
-        made = dlogits is None and want_grad
-        if made:
-            dlogits = torch.empty((T, V), dtype=logits.dtype, device=dev)
-        _check(lib().lx_distill_loss(
-            _DTYPES[logits.dtype], logits.data_ptr(), ld,
-            _flat(teacher_id, "teacher_id", T * K, torch.int32),
+    ptrs = (_flat(teacher_id, "teacher_id", T * K, torch.int32),
             _flat(teacher_logit, "teacher_logit", T * K), _flat(teacher_lse, "teacher_lse", T),
-            _flat(labels, "labels", T, torch.int32), _flat(row_weight, "row_weight", T), T, V, K,
-            temperature, kd_weight, ce_weight, loss.data_ptr(),
-            None if dlogits is None else dlogits.data_ptr(),
-            0 if dlogits is None else _rows(dlogits, "dlogits", logits.shape, logits.dtype),
-            on.stream.cuda_stream))
-        on.outputs(loss, dlogits if made else None)
-    return loss, dlogits
+            _flat(labels, "labels", T, torch.int32), _flat(row_weight, "row_weight", T))
+
+    def call(s):
+        loss = torch.empty(T, dtype=torch.float32, device=dev)
+        d = dlogits
+        if d is None and want_grad:
+            d = torch.empty((T, V), dtype=logits.dtype, device=dev)
+        ldd = 0 if d is None else _rows(d, "dlogits", logits.shape, logits.dtype)
+        _check(lib().lx_distill_loss(_DTYPES[logits.dtype], logits.data_ptr(), ld, *ptrs, T, V, K,
+                                     temperature, kd_weight, ce_weight, loss.data_ptr(), _ptr(d), ldd, s))
+        return loss, d
+
+    return _run(stream, (logits, teacher_id, teacher_logit, teacher_lse, labels, row_weight), call)
