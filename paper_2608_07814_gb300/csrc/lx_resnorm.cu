@@ -42,9 +42,10 @@ struct NormArgs {
   int T, H, gate_kind;
   int lanes;              // threads that hold a row's piece (a part of a warp; else the CTA)
   const void* in[N_IN];   // NULL where absent
-  long ld[N_IN];
-  int slot[N_IN];         // place among the present ones
-  int slots, stages, par_at;      // stages: rows in the slots of a thread, 3 or 2
+  uint32_t ldb[N_IN];     // bytes between rows
+  uint32_t slot_at[N_IN]; // bytes from a stage's start to the array's slots
+  uint32_t stage_bytes, stages;  // of a CTA's slots for one row; rows they hold, 3 or 2
+  uint32_t par_at;        // bytes from the slots' start to the parameters'
   const float* gate;      // channel or token gate
   long ldg;
   const float *w_post, *w_pre;
@@ -79,127 +80,157 @@ __device__ __forceinline__ void copy_wait() {
 // The rows and columns of a thread, and the slots of its pieces.  Pieces are VEC
 // elements: 16 bytes, 4 bytes where rows do not start on 16-byte boundaries, or single
 // bf16 values, which cannot be copied asynchronously and are read where they are used
-// (as are the widest rows, whose slots would not fit).
+// (as are the widest rows, whose slots would not fit).  Values are held as pairs, for
+// the two-wide fp32 instructions.
 template <typename T, int VEC, int EPT, int GRP>
 struct Rows {
-  static constexpr int NCH = EPT / VEC, BYTES = VEC * sizeof(T);
+  static constexpr int NCH = EPT / VEC, BYTES = VEC * sizeof(T), N2 = EPT / 2;
   static constexpr bool RING = BYTES >= 4 && EPT == 8;
   const NormArgs& A;
-  char* ring;
-  int lane, size, col0, end;
-  int count;       // pieces of the thread inside the row (they ascend)
-  long row, step;  // first row; distance of this group's rows
-  __device__ Rows(const NormArgs& args, char* smem) : A(args), ring(smem) {
-    col0 = 0;
+  char* ring;     // the thread's first slot
+  uint32_t at;    // the round's stage, in bytes
+  int lane, size;  // of the threads that hold a row
+  int col0;        // first column of the thread
+  int count;       // its pieces inside the row (they ascend)
+  int row, step;   // first row; distance of this group's rows
+  __device__ Rows(const NormArgs& args, char* smem) : A(args), ring(smem + threadIdx.x * BYTES), at(0) {
+    int first = 0, end = A.H;
     if constexpr (GRP == WARP) {
       size = A.lanes;
       lane = threadIdx.x & (size - 1);
-      row = (long)blockIdx.x * (WARP_T / size) + threadIdx.x / size;
-      step = (long)gridDim.x * (WARP_T / size);
+      row = blockIdx.x * (WARP_T / size) + threadIdx.x / size;
+      step = gridDim.x * (WARP_T / size);
     } else {
       size = blockDim.x;
       lane = threadIdx.x;
-      if constexpr (GRP == CLUSTER) col0 = blockIdx.x * (CTA_T * EPT);
       row = GRP == CTA ? blockIdx.x : blockIdx.y;
       step = GRP == CTA ? gridDim.x : gridDim.y;
+      if constexpr (GRP == CLUSTER) {
+        first = blockIdx.x * (CTA_T * EPT);
+        end = min(A.H, first + CTA_T * EPT);
+      }
     }
-    end = GRP == CLUSTER ? min(A.H, col0 + CTA_T * EPT) : A.H;
+    col0 = first + lane * VEC;
     count = 0;
 #pragma unroll
     for (int c = 0; c < NCH; ++c) count += col(c) < end;
   }
-  // whether some row of this warp (for CTAs: this CTA) is left at round `t` of lane 0
-  __device__ bool more(long t) const {
-    if constexpr (GRP == WARP) return __any_sync(0xffffffffu, t < A.T);
-    else return t < A.T;
+  __device__ bool writer() const { return col0 == 0; }  // one thread of the row
+  // whether a row is left for this warp (for CTAs: this CTA) in round t of lane 0; t is
+  // below 2 * T, and T + step below 2^31 + 2^20: compared as unsigned
+  __device__ bool more(unsigned t) const {
+    if constexpr (GRP == WARP) return __any_sync(0xffffffffu, t < (unsigned)A.T);
+    else return t < (unsigned)A.T;
   }
-  __device__ int col(int c) const { return col0 + (c * size + lane) * VEC; }
-  __device__ const T* src(int k, long t, int e) const { return (const T*)A.in[k] + t * A.ld[k] + e; }
-  __device__ char* place(int stage, int k, int c) const {
-    return ring + ((size_t)((stage * A.slots + A.slot[k]) * NCH + c) * blockDim.x + threadIdx.x) * BYTES;
+  __device__ int col(int c) const { return col0 + c * size * VEC; }
+  __device__ const T* src(int k, unsigned t) const {
+    return (const T*)((const char*)A.in[k] + (uint64_t)t * A.ldb[k]) + col0;
   }
-  __device__ void fetch(int stage, long t) const {
+  __device__ char* place(uint32_t stage, int k) const { return ring + (stage + A.slot_at[k]); }
+  __device__ void fetch(uint32_t stage, unsigned t) const {
+    if (t < (unsigned)A.T)
+#pragma unroll
+      for (int k = 0; k < N_IN; ++k)
+        if (A.in[k]) {
+          const T* p = src(k, t);
+          char* d = place(stage, k);
+#pragma unroll
+          for (int c = 0; c < NCH; ++c)
+            if (c < count) copy_async<BYTES>(d + c * blockDim.x * BYTES, p + c * size * VEC);
+        }
+    copy_commit();
+  }
+  // zeroes the slots of the pieces outside the row and starts the copies of the first
+  // rows; then, each round: those of the row stages - 1 rounds ahead, and a wait for
+  // this round's
+  __device__ void begin() const {
     if constexpr (RING) {
-      if (t < A.T)
+      for (int s = 0; s < A.stages; ++s) {
 #pragma unroll
         for (int k = 0; k < N_IN; ++k)
-          if (A.in[k]) {
-            const T* p = src(k, t, col(0));
-            char* d = place(stage, k, 0);
+          if (A.in[k])
 #pragma unroll
-            for (int c = 0; c < NCH; ++c, p += size * VEC, d += blockDim.x * BYTES)
-              if (c < count) copy_async<BYTES>(d, p);
-          }
-      copy_commit();
-    }
-  }
-  // the pieces of array k of row t, zero outside the row
-  __device__ void read(int stage, int k, long t, float* v) const {
-    const char* p = RING ? place(stage, k, 0) : nullptr;
-    const T* g = RING ? nullptr : src(k, t, col(0));
+            for (int c = 0; c < NCH; ++c)
+              if (c >= count)
 #pragma unroll
-    for (int c = 0; c < NCH; ++c, p += blockDim.x * BYTES, g += size * VEC) {
-      const bool on = c < count && t < A.T;
-      if constexpr (RING) {
-        if constexpr (BYTES == 16) {
-          load<T, VEC>((const T*)p, v + c * VEC);
-        } else if constexpr (VEC == 1) {
-          v[c] = *(const float*)p;
-        } else {
-          const uint32_t w = *(const uint32_t*)p;
-          v[2 * c] = __uint_as_float(w << 16);
-          v[2 * c + 1] = __uint_as_float(w & 0xffff0000u);
-        }
-        if (!on)
-#pragma unroll
-          for (int j = 0; j < VEC; ++j) v[c * VEC + j] = 0.f;
-      } else {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) v[c * VEC + j] = 0.f;
-        if (on) {
-          if constexpr (BYTES == 4 && VEC == 2) {
-            const uint32_t w = *(const uint32_t*)g;
-            v[2 * c] = __uint_as_float(w << 16);
-            v[2 * c + 1] = __uint_as_float(w & 0xffff0000u);
-          } else {
-            load<T, VEC>(g, v + c * VEC);
-          }
-        }
+                for (int q = 0; q < BYTES / 4; ++q)
+                  ((uint32_t*)(place(s * A.stage_bytes, k) + c * blockDim.x * BYTES))[q] = 0u;
+        if (s < A.stages - 1) fetch(s * A.stage_bytes, (unsigned)row + (unsigned)s * step);
       }
     }
   }
-  // starts the copies of the first rows; then, each round: those of the row stages - 1
-  // rounds ahead, and a wait for this round's
-  __device__ void begin() const {
-    for (int p = 0; p < A.stages - 1; ++p) fetch(p, row + p * step);
-  }
-  __device__ void advance(int stage, long t) const {
+  __device__ void advance(unsigned t) const {
     if constexpr (RING) {
-      fetch(stage == 0 ? A.stages - 1 : stage - 1, t + (A.stages - 1) * step);
+      fetch(at == 0 ? (A.stages - 1) * A.stage_bytes : at - A.stage_bytes, t + (unsigned)(A.stages - 1) * step);
       if (A.stages == 3) copy_wait<2>();
       else copy_wait<1>();
     }
   }
-  __device__ void write(void* out, long t, const float* v) const {
-    if (t >= A.T) return;
-    T* p = (T*)out + t * A.H + col(0);
+  __device__ void next() { at = at + A.stage_bytes == A.stages * A.stage_bytes ? 0 : at + A.stage_bytes; }
+  // the pieces of array k of row t, zero outside the row
+  __device__ void read(int k, unsigned t, float2* v) const {
+    const T* g = RING ? (const T*)place(at, k) : src(k, t);
+    const int apart = RING ? blockDim.x * VEC : size * VEC;
 #pragma unroll
-    for (int c = 0; c < NCH; ++c, p += size * VEC)
-      if (c < count) {
-        if constexpr (BYTES == 4 && VEC == 2) {
-          const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * c], v[2 * c + 1]);
-          *(__nv_bfloat162*)p = b;
+    for (int c = 0; c < NCH; ++c) {
+      const bool on = RING || (c < count && t < (unsigned)A.T);
+      const T* p = g + c * apart;
+      if constexpr (BYTES == 16) {
+        const uint4 w = on ? *(const uint4*)p : make_uint4(0u, 0u, 0u, 0u);
+        if constexpr (sizeof(T) == 4) {
+          v[2 * c] = make_float2(__uint_as_float(w.x), __uint_as_float(w.y));
+          v[2 * c + 1] = make_float2(__uint_as_float(w.z), __uint_as_float(w.w));
         } else {
-          store<T, VEC>(p, v + c * VEC);
+          v[4 * c] = bf2(w.x);
+          v[4 * c + 1] = bf2(w.y);
+          v[4 * c + 2] = bf2(w.z);
+          v[4 * c + 3] = bf2(w.w);
+        }
+      } else if constexpr (VEC == 2) {
+        v[c] = bf2(on ? *(const uint32_t*)p : 0u);
+      } else {
+        const float x = on ? to_f32(*p) : 0.f;
+        if (c & 1) v[c / 2].y = x;
+        else v[c / 2].x = x;
+      }
+    }
+    if (GRP == WARP && RING && t >= (unsigned)A.T)  // what an earlier row left
+#pragma unroll
+      for (int i = 0; i < N2; ++i) v[i] = make_float2(0.f, 0.f);
+  }
+  __device__ void write(void* out, unsigned t, const float2* v) const {
+    if (GRP == WARP && t >= (unsigned)A.T) return;
+    T* g = (T*)out + (uint64_t)t * (unsigned)A.H + col0;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+      if (c < count) {
+        T* p = g + c * size * VEC;
+        if constexpr (BYTES == 16) {
+          uint4 w;
+          if constexpr (sizeof(T) == 4)
+            w = make_uint4(__float_as_uint(v[2 * c].x), __float_as_uint(v[2 * c].y), __float_as_uint(v[2 * c + 1].x),
+                           __float_as_uint(v[2 * c + 1].y));
+          else
+            w = make_uint4(to_bf2(v[4 * c]), to_bf2(v[4 * c + 1]), to_bf2(v[4 * c + 2]), to_bf2(v[4 * c + 3]));
+          *(uint4*)p = w;
+        } else if constexpr (VEC == 2) {
+          *(uint32_t*)p = to_bf2(v[c]);
+        } else {
+          *p = from_f32<T>(c & 1 ? v[c / 2].y : v[c / 2].x);
         }
       }
   }
-  // fp32 parameters of the thread's columns, `rest` outside
-  __device__ void params(const float* p, float add, float rest, float* v) const {
+  // element j of piece c in a thread's pairs
+  static __device__ float& elem(float2* v, int c, int j) {
+    float2& p = v[(c * VEC + j) / 2];
+    return (c * VEC + j) & 1 ? p.y : p.x;
+  }
+  // fp32 parameters of the thread's columns, `rest` where absent
+  __device__ void params(const float* p, float add, float rest, float2* v) const {
 #pragma unroll
     for (int c = 0; c < NCH; ++c)
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) v[c * VEC + j] = p && c < count ? add + p[col(c) + j] : rest;
+      for (int j = 0; j < VEC; ++j) elem(v, c, j) = p && c < count ? add + p[col(c) + j] : rest;
   }
   // sums of N values over the row's threads, the same in each of them; buf (zero at
   // first) is used in turn: a half is written again only after the barrier that follows
@@ -214,8 +245,8 @@ struct Rows {
     }
     if constexpr (GRP != WARP) {
       const int nw = blockDim.x >> 5;
-      float(*b)[CTA_T / 32] = buf[turn & 1];
-      ++turn;
+      float(*b)[CTA_T / 32] = buf[turn];
+      turn ^= 1;
       if ((threadIdx.x & 31) == 0)
 #pragma unroll
         for (int i = 0; i < N; ++i) b[i][threadIdx.x >> 5] = v[i];
@@ -257,72 +288,73 @@ extern __shared__ uint4 norm_ring[];
 
 template <typename T, int VEC, int EPT, int GRP>
 __global__ void __launch_bounds__(CTA_T, EPT == 8 ? 2 : 1)
-k_resnorm_fwd(const NormArgs A) {
+k_resnorm_fwd(const __grid_constant__ NormArgs A) {
+  constexpr int N2 = EPT / 2;
   __shared__ __align__(16) float buf[2][1][CTA_T / 32];
   int turn = 0;
   if (GRP == CTA) clear(buf);
-  const Rows<T, VEC, EPT, GRP> R(A, (char*)norm_ring);
+  Rows<T, VEC, EPT, GRP> R(A, (char*)norm_ring);
+  R.begin();
   const float inv = 1.f / (float)A.H;
-  const bool chan = A.gate_kind == LX_GATE_CHANNEL;
-  float w1[EPT], w2[EPT];  // w1: with the channel gate
+  const float2 a2 = both(A.a);
+  const bool has_y = A.in[IN_Y], post = A.w_post, token = A.gate_kind == LX_GATE_TOKEN;
+  float2 w1[N2], w2[N2];  // w1: with the channel gate
   R.params(A.w_post, A.off, 1.f, w1);
   R.params(A.w_pre, A.off, 0.f, w2);
-  if (chan) {
-    float g[EPT];
+  if (A.gate_kind == LX_GATE_CHANNEL) {
+    float2 g[N2];
     R.params(A.gate, 0.f, 0.f, g);
 #pragma unroll
-    for (int i = 0; i < EPT; ++i) w1[i] *= g[i];
+    for (int i = 0; i < N2; ++i) w1[i] = mul2(w1[i], g[i]);
   }
-  int stage = 0;
-  R.begin();
-  const bool token = A.gate_kind == LX_GATE_TOKEN;
-  float next = token && R.row < A.T ? A.gate[R.row * A.ldg] : 1.f;  // a row's gate is read a round ahead
-  for (long t = R.row; R.more(t); t += R.step) {
+  // a row's gate is read a round ahead
+  float next = token && R.row < A.T ? A.gate[R.row * A.ldg] : 1.f;
+  for (unsigned t = R.row; R.more(t); t += R.step, R.next()) {
     const float tok = next;
-    if (token && t + R.step < A.T) next = A.gate[(t + R.step) * A.ldg];
-    R.advance(stage, t);
-    float x[EPT];
-    R.read(stage, IN_R, t, x);
-    float s1 = 1.f, s2 = 1.f, q[1];
-    if (A.in[IN_Y]) {
-      float y[EPT];
-      R.read(stage, IN_Y, t, y);
-      if (A.w_post) {
-        q[0] = 0.f;
+    if (token && t + R.step < (unsigned)A.T) next = A.gate[(long)(t + R.step) * A.ldg];
+    R.advance(t);
+    float2 x[N2];
+    R.read(IN_R, t, x);
 #pragma unroll
-        for (int i = 0; i < EPT; ++i) q[0] = fmaf(y[i], y[i], q[0]);
+    for (int i = 0; i < N2; ++i) x[i] = mul2(x[i], a2);
+    float s1 = 1.f, s2 = 1.f, q[1];
+    if (has_y) {
+      float2 y[N2];
+      R.read(IN_Y, t, y);
+      if (post) {
+        float2 p = mul2(y[0], y[0]);
+#pragma unroll
+        for (int i = 1; i < N2; ++i) p = fma2(y[i], y[i], p);
+        q[0] = p.x + p.y;
         R.sum(q, buf, turn);
         s1 = rsqrtf(q[0] * inv + A.eps);
       }
       if (A.in[IN_GATE]) {
-        float g[EPT];
-        R.read(stage, IN_GATE, t, g);
+        float2 g[N2];
+        R.read(IN_GATE, t, g);
 #pragma unroll
-        for (int i = 0; i < EPT; ++i) y[i] *= g[i];
+        for (int i = 0; i < N2; ++i) y[i] = mul2(y[i], g[i]);
       }
-      const float f = s1 * tok;
+      const float2 f = both(s1 * tok);
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) x[i] = fmaf(y[i] * w1[i], f, A.a * x[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < EPT; ++i) x[i] *= A.a;
+      for (int i = 0; i < N2; ++i) x[i] = fma2(mul2(y[i], w1[i]), f, x[i]);
     }
     if (A.r_out) R.write(A.r_out, t, x);
     if (A.w_pre) {
-      q[0] = 0.f;
+      float2 p = mul2(x[0], x[0]);
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) q[0] = fmaf(x[i], x[i], q[0]);
+      for (int i = 1; i < N2; ++i) p = fma2(x[i], x[i], p);
+      q[0] = p.x + p.y;
       R.sum(q, buf, turn);
       s2 = rsqrtf(q[0] * inv + A.eps);
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) x[i] *= s2 * w2[i];
+      for (int i = 0; i < N2; ++i) x[i] = mul2(mul2(x[i], both(s2)), w2[i]);
       R.write(A.h_out, t, x);
     }
-    if (A.stats && R.lane == 0 && R.col0 == 0 && t < A.T) {
+    if (A.stats && R.writer() && t < (unsigned)A.T) {
       A.stats[t] = s1;
       A.stats[(long)A.T + t] = s2;
     }
-    stage = stage + 1 == A.stages ? 0 : stage + 1;
   }
   // a CTA's shared memory outlives its neighbours' reads
   if constexpr (GRP == CLUSTER) cooperative_groups::this_cluster().sync();
@@ -333,32 +365,33 @@ k_resnorm_fwd(const NormArgs A) {
 // token's gate the sums are of u, which its gradient needs, and f n is g times them).
 template <typename T, int VEC, int EPT, int GRP>
 __global__ void __launch_bounds__(EPT == 8 ? 640 : CTA_T, 1)
-k_resnorm_bwd(const NormArgs A) {
+k_resnorm_bwd(const __grid_constant__ NormArgs A) {
+  constexpr int N2 = EPT / 2;
   __shared__ __align__(16) float buf[2][3][CTA_T / 32];
   int turn = 0;
   if (GRP == CTA) clear(buf);
-  const Rows<T, VEC, EPT, GRP> R(A, (char*)norm_ring);
+  Rows<T, VEC, EPT, GRP> R(A, (char*)norm_ring);
+  R.begin();
   const float inv = 1.f / (float)A.H;
-  const bool token = A.gate_kind == LX_GATE_TOKEN;
+  const bool has_y = A.in[IN_Y], post = A.w_post, token = A.gate_kind == LX_GATE_TOKEN;
+  const float2 zero = make_float2(0.f, 0.f);
   // the columns' parameters, in slots that only this thread reads: registers are short
-  float4* par = (float4*)((char*)norm_ring + A.par_at);
-  auto put = [&](int k, const float* v) {
+  float4* par = (float4*)((char*)norm_ring + A.par_at) + threadIdx.x;
+  auto put = [&](int k, const float2* v) {
 #pragma unroll
-    for (int i = 0; i < EPT; i += 4)
-      par[(k * (EPT / 4) + i / 4) * blockDim.x + threadIdx.x] = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+    for (int i = 0; i < N2; i += 2)
+      par[(k * (EPT / 4) + i / 2) * blockDim.x] = make_float4(v[i].x, v[i].y, v[i + 1].x, v[i + 1].y);
   };
-  auto get = [&](int k, float* v) {
+  auto get = [&](int k, float2* v) {
 #pragma unroll
-    for (int i = 0; i < EPT; i += 4) {
-      const float4 p = par[(k * (EPT / 4) + i / 4) * blockDim.x + threadIdx.x];
-      v[i] = p.x;
-      v[i + 1] = p.y;
-      v[i + 2] = p.z;
-      v[i + 3] = p.w;
+    for (int i = 0; i < N2; i += 2) {
+      const float4 p = par[(k * (EPT / 4) + i / 2) * blockDim.x];
+      v[i] = make_float2(p.x, p.y);
+      v[i + 1] = make_float2(p.z, p.w);
     }
   };
   {
-    float v[EPT];
+    float2 v[N2];
     R.params(A.w_post, A.off, 1.f, v);
     put(0, v);
     R.params(A.w_pre, A.off, 0.f, v);
@@ -366,100 +399,90 @@ k_resnorm_bwd(const NormArgs A) {
     R.params(A.gate_kind == LX_GATE_CHANNEL ? A.gate : nullptr, 0.f, 1.f, v);
     put(2, v);
   }
-  float acc[3][EPT];
+  float2 acc[3][N2];
 #pragma unroll
-  for (int i = 0; i < EPT; ++i) acc[0][i] = acc[1][i] = acc[2][i] = 0.f;
-  int stage = 0;
-  R.begin();
+  for (int i = 0; i < N2; ++i) acc[0][i] = acc[1][i] = acc[2][i] = zero;
   float n1 = 0.f, n2 = 0.f, ng = 1.f;  // a row's scalars are read a round ahead
-  auto scalars = [&](long t) {
-    if (t >= A.T) return;
+  auto scalars = [&](unsigned t) {
+    if (t >= (unsigned)A.T) return;
     n1 = A.stats[t];
     n2 = A.stats[(long)A.T + t];
-    if (token) ng = A.gate[t * A.ldg];
+    if (token) ng = A.gate[(long)t * A.ldg];
   };
   scalars(R.row);
-  for (long t = R.row; R.more(t); t += R.step) {
-    const bool on = t < A.T;
+  for (unsigned t = R.row; R.more(t); t += R.step, R.next()) {
     const float s1 = n1, s2 = n2, tok = ng;
     scalars(t + R.step);
-    R.advance(stage, t);
-    float n[EPT], D[EPT], x[EPT], g[EPT];  // n: y s1
-    if (A.in[IN_DR]) R.read(stage, IN_DR, t, D);
+    R.advance(t);
+    float2 n[N2], D[N2], x[N2], g[N2], w1[N2];  // n: y s1
+    get(0, w1);
+    if (A.in[IN_DR]) R.read(IN_DR, t, D);
     else
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) D[i] = 0.f;
-    if (A.in[IN_Y]) {
-      R.read(stage, IN_Y, t, n);
+      for (int i = 0; i < N2; ++i) D[i] = zero;
+    if (has_y) {
+      R.read(IN_Y, t, n);
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) n[i] *= s1;
-      if (A.in[IN_GATE]) {
-        R.read(stage, IN_GATE, t, g);
-      } else {
-#pragma unroll
-        for (int i = 0; i < EPT; ++i) g[i] = 1.f;
-        if (A.gate_kind == LX_GATE_CHANNEL) get(2, g);
-      }
+      for (int i = 0; i < N2; ++i) n[i] = mul2(n[i], both(s1));
+      if (A.in[IN_GATE]) R.read(IN_GATE, t, g);
+      else get(2, g);
     }
-    float w1[EPT];
-    get(0, w1);
-    float q[3] = {0.f, 0.f, 0.f};
+    float2 q0 = zero, q1 = zero, q2 = zero;
     if (A.in[IN_DH]) {
-      float dh[EPT], w2[EPT];
+      float2 dh[N2], w2[N2];
       get(1, w2);
-      R.read(stage, IN_R, t, x);
-      R.read(stage, IN_DH, t, dh);
+      R.read(IN_R, t, x);
+      R.read(IN_DH, t, dh);
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) {
-        float v = A.a * x[i];
-        if (A.in[IN_Y]) v = fmaf(n[i] * w1[i], g[i] * tok, v);
-        x[i] = v * s2;
-        acc[2][i] = fmaf(dh[i], x[i], acc[2][i]);
-        const float e = dh[i] * w2[i];
-        q[0] = fmaf(e, x[i], q[0]);
-        D[i] = fmaf(s2, e, D[i]);
+      for (int i = 0; i < N2; ++i) {
+        x[i] = mul2(x[i], both(A.a));
+        if (has_y) x[i] = fma2(mul2(n[i], w1[i]), mul2(g[i], both(tok)), x[i]);
+        x[i] = mul2(x[i], both(s2));
+        acc[2][i] = fma2(dh[i], x[i], acc[2][i]);
+        const float2 e = mul2(dh[i], w2[i]);
+        q0 = fma2(e, x[i], q0);
+        D[i] = fma2(both(s2), e, D[i]);
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) x[i] = 0.f;
+      for (int i = 0; i < N2; ++i) x[i] = zero;
     }
-    if (A.in[IN_Y]) {
+    if (has_y)
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) {
-        const float v = n[i] * w1[i] * g[i];
-        q[1] = fmaf(D[i], v, q[1]);
-        q[2] = fmaf(x[i], v, q[2]);
+      for (int i = 0; i < N2; ++i) {
+        const float2 v = mul2(mul2(n[i], w1[i]), g[i]);
+        q1 = fma2(D[i], v, q1);
+        q2 = fma2(x[i], v, q2);
       }
-    }
+    float q[3] = {q0.x + q0.y, q1.x + q1.y, q2.x + q2.y};
     R.sum(q, buf, turn);
     const float m = q[0] * inv * s2;
     const float dv = q[1] - m * q[2];
-    const float m1 = A.w_post ? dv * inv * tok : 0.f;
 #pragma unroll
-    for (int i = 0; i < EPT; ++i) D[i] = fmaf(-m, x[i], D[i]);
+    for (int i = 0; i < N2; ++i) D[i] = fma2(both(-m), x[i], D[i]);
     if (A.dr) {
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) x[i] = A.a * D[i];
+      for (int i = 0; i < N2; ++i) x[i] = mul2(D[i], both(A.a));
       R.write(A.dr, t, x);
     }
-    if (A.in[IN_Y]) {
-      if (token && A.dgate && R.lane == 0 && R.col0 == 0 && on) ((float*)A.dgate)[t] = dv;
+    if (has_y) {
+      const float m1 = post ? dv * inv * tok : 0.f;
+      if (token && A.dgate && R.writer() && t < (unsigned)A.T) ((float*)A.dgate)[t] = dv;
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) {
-        x[i] = D[i] * (n[i] * w1[i]);
-        acc[1][i] += x[i];
-        const float f = D[i] * (g[i] * tok);
-        acc[0][i] = fmaf(f, n[i], acc[0][i]);
-        D[i] = s1 * fmaf(-m1, n[i], f * w1[i]);
+      for (int i = 0; i < N2; ++i) {
+        x[i] = mul2(D[i], mul2(n[i], w1[i]));
+        acc[1][i] = add2(acc[1][i], x[i]);
+        const float2 f = mul2(D[i], mul2(g[i], both(tok)));
+        acc[0][i] = fma2(f, n[i], acc[0][i]);
+        D[i] = mul2(both(s1), fma2(both(-m1), n[i], mul2(f, w1[i])));
       }
       if (A.in[IN_GATE] && A.dgate) R.write(A.dgate, t, x);
       if (A.dy) R.write(A.dy, t, D);
     }
-    stage = stage + 1 == A.stages ? 0 : stage + 1;
   }
   if (A.part) {
     float* part = A.part + (GRP == CLUSTER ? (long)blockIdx.y : (long)blockIdx.x) * 3 * A.H;
-    float* ws = (float*)norm_ring;  // [rows of the CTA][H], the ring's copies being done
+    float* ws = (float*)norm_ring;  // [rows of the CTA][H], the slots' copies being done
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
       if (!(A.sums >> k & 1)) continue;
@@ -468,9 +491,9 @@ k_resnorm_bwd(const NormArgs A) {
         __syncthreads();
 #pragma unroll
         for (int c = 0; c < R.NCH; ++c)
+          if (c < R.count)
 #pragma unroll
-          for (int j = 0; j < VEC; ++j)
-            if (R.col(c) + j < A.H) ws[(threadIdx.x / R.size) * A.H + R.col(c) + j] = acc[k][c * VEC + j];
+            for (int j = 0; j < VEC; ++j) ws[(threadIdx.x / R.size) * A.H + R.col(c) + j] = R.elem(acc[k], c, j);
         __syncthreads();
         for (int e = threadIdx.x; e < A.H; e += WARP_T) {
           float s = 0.f;
@@ -480,9 +503,9 @@ k_resnorm_bwd(const NormArgs A) {
       } else {
 #pragma unroll
         for (int c = 0; c < R.NCH; ++c)
-          if (R.col(c) < R.end)
+          if (c < R.count)
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) part[(long)k * A.H + R.col(c) + j] = acc[k][c * VEC + j];
+            for (int j = 0; j < VEC; ++j) part[(long)k * A.H + R.col(c) + j] = R.elem(acc[k], c, j);
       }
     }
   }
@@ -543,7 +566,13 @@ long bwd_groups(const Shape& s) { return resident(s, s.ept == 8 ? BWD_REGS : WID
 // Slots of a CTA: three rows, or two where three would keep CTAs off an SM that its
 // registers have room for (fp32 with a full gate)
 size_t ring_bytes(const Shape& s, NormArgs& A, size_t es, int regs, size_t more) {
-  const size_t row = (size_t)A.slots * s.ept * es * s.threads;
+  size_t row = 0;
+  for (int k = 0; k < N_IN; ++k)
+    if (A.in[k]) {
+      A.slot_at[k] = (uint32_t)row;
+      row += (size_t)s.ept * es * s.threads;
+    }
+  A.stage_bytes = (uint32_t)row;
   A.stages = (3 * row + more + 1024) * (65536 / (regs * s.threads)) <= 227 * 1024 ? 3 : 2;
   return A.stages * row;
 }
@@ -602,6 +631,7 @@ lx_status launch_any(int dtype, int piece, const Shape& s, NormArgs& A, cudaStre
   return launch_vec<__nv_bfloat16, 1, BWD>(s, A, st);
 }
 
+constexpr int64_t MAX_LD = (1 << 30) - 1;  // elements between rows: a distance in bytes fits 32 bits
 size_t esize(int dtype) { return dtype == LX_BF16 ? 2 : 4; }
 
 lx_status check_desc(const lx_resnorm_desc* d) {
@@ -619,12 +649,16 @@ lx_status check_desc(const lx_resnorm_desc* d) {
   if (d->ldr < d->H || (d->y && d->ldy < d->H) || (d->gate_kind == LX_GATE_FULL && d->ldg < d->H) ||
       (d->gate_kind == LX_GATE_TOKEN && d->ldg < 0))
     return fail(LX_ERR_SHAPE, "rows are closer than H elements");
+  if (d->T > 1 && (d->ldr > MAX_LD || (d->y && d->ldy > MAX_LD) || (d->gate && d->ldg > MAX_LD)))
+    return fail(LX_ERR_SHAPE, "rows are 2^30 elements apart or more");
   const size_t es = esize(d->dtype);
   if (!aligned(d->r, es) || !aligned(d->y, es) || !aligned(d->gate, d->gate_kind == LX_GATE_FULL ? es : 4) ||
       !aligned(d->w_post, 4) || !aligned(d->w_pre, 4))
     return fail(LX_ERR_ARG, "a pointer is not aligned to its element");
   return LX_OK;
 }
+
+uint32_t row_bytes(const lx_resnorm_desc* d, int64_t ld) { return (uint32_t)(d->T > 1 ? ld * (int64_t)esize(d->dtype) : 0); }
 
 NormArgs args_of(const lx_resnorm_desc* d, const Shape& s) {
   NormArgs A = {};
@@ -633,12 +667,12 @@ NormArgs args_of(const lx_resnorm_desc* d, const Shape& s) {
   A.gate_kind = d->gate_kind;
   A.lanes = s.lanes;
   A.in[IN_Y] = d->y;
-  A.ld[IN_Y] = d->ldy;
+  A.ldb[IN_Y] = row_bytes(d, d->ldy);
   A.in[IN_R] = d->r;
-  A.ld[IN_R] = d->ldr;
+  A.ldb[IN_R] = row_bytes(d, d->ldr);
   if (d->gate_kind == LX_GATE_FULL) {
     A.in[IN_GATE] = d->gate;
-    A.ld[IN_GATE] = d->ldg;
+    A.ldb[IN_GATE] = row_bytes(d, d->ldg);
   } else {
     A.gate = (const float*)d->gate;
     A.ldg = d->ldg;
@@ -651,16 +685,11 @@ NormArgs args_of(const lx_resnorm_desc* d, const Shape& s) {
   return A;
 }
 
-// Numbers the arrays that are read and finds the widest piece that divides every row's
-// start and length: 16 bytes, 4, or one bf16
-int pieces(NormArgs& A, size_t es, std::initializer_list<const void*> outs) {
+// The widest piece that divides every row's start and length: 16 bytes, 4, or one bf16
+int pieces(const NormArgs& A, size_t es, std::initializer_list<const void*> outs) {
   uintptr_t bits = (uintptr_t)A.H * es;
-  A.slots = 0;
   for (int k = 0; k < N_IN; ++k)
-    if (A.in[k]) {
-      A.slot[k] = A.slots++;
-      bits |= (uintptr_t)A.in[k] | (uintptr_t)((size_t)A.ld[k] * es);
-    }
+    if (A.in[k]) bits |= (uintptr_t)A.in[k] | (uintptr_t)A.ldb[k];
   for (const void* p : outs) bits |= (uintptr_t)p;
   return bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2;
 }
@@ -730,6 +759,8 @@ extern "C" lx_status lx_residual_norm_backward(const lx_resnorm_desc* d, const f
   if (!stats) return fail(LX_ERR_ARG, "stats is NULL");
   if (!dr_out && !dh) return fail(LX_ERR_ARG, "dr_out and dh are both NULL");
   if ((dr_out && lddr < d->H) || (dh && lddh < d->H)) return fail(LX_ERR_SHAPE, "rows are closer than H elements");
+  if (d->T > 1 && ((dr_out && lddr > MAX_LD) || (dh && lddh > MAX_LD)))
+    return fail(LX_ERR_SHAPE, "rows are 2^30 elements apart or more");
   const void* ins[] = {d->r, d->y, d->gate_kind == LX_GATE_FULL ? d->gate : nullptr, dr_out, dh};
   const long lds[] = {(long)d->ldr, (long)d->ldy, (long)d->ldg, (long)lddr, (long)lddh};
   void* outs[] = {dr, dy, d->gate_kind == LX_GATE_FULL ? dgate : nullptr};
@@ -750,9 +781,9 @@ extern "C" lx_status lx_residual_norm_backward(const lx_resnorm_desc* d, const f
   if (!dh) A.in[IN_R] = nullptr;  // only the second norm's gradient reads r
   A.stats = const_cast<float*>(stats);
   A.in[IN_DR] = dr_out;
-  A.ld[IN_DR] = lddr;
+  A.ldb[IN_DR] = row_bytes(d, lddr);
   A.in[IN_DH] = dh;
-  A.ld[IN_DH] = lddh;
+  A.ldb[IN_DH] = row_bytes(d, lddh);
   A.dr = dr;
   A.dy = dy;
   A.dgate = dgate;
