@@ -12,8 +12,9 @@
 // gate), r' and h, the backward r, y, dr', dh, dr and dy; r' is formed again from r and
 // y instead of being read, which costs no bytes and keeps the unrounded values.
 //
-// A row is held by a part of a warp (H <= 256), a CTA (H <= 4096) or a cluster of CTAs,
-// 8 elements a thread (16 above 32768).  Rows are dealt to a resident grid; a thread
+// A row is held by a part of a warp (H <= 512), a CTA (H <= 4096) or a cluster of CTAs,
+// 16 elements a thread: what a row costs besides its elements (two barriers, the sums,
+// the copies' addresses) bounded the kernels with 8.  Rows are dealt to a resident grid; a thread
 // copies its own pieces of the next rows into slots of shared memory that it alone
 // reads (cp.async: no barrier), so that two rows are in flight while one is worked on,
 // and keeps its columns' parameters in registers.  In the backward it also keeps their
@@ -28,12 +29,12 @@ namespace {
 
 using namespace rows;
 
-constexpr int WARP_H = 256;       // widest row of a warp
-constexpr int CTA_T = 512;        // threads of a CTA at most
-constexpr int CTA_H = CTA_T * 8;  // widest row of a CTA with 8 elements a thread
+constexpr int EPT = 16, N2 = EPT / 2;  // elements of a row a thread holds, in pairs
+constexpr int WARP_H = 32 * EPT;       // widest row of a warp
+constexpr int CTA_T = 256;             // threads of a CTA at most,
+constexpr int WIDE_T = 512;            // or for the widest rows
 constexpr int MAX_CLUSTER = 8;
-static_assert(2 * CTA_H * MAX_CLUSTER == LX_MAX_WIDTH, "the widest row: 16 elements a thread");
-constexpr int WARP_T = 256;  // threads of a CTA whose rows are held by parts of warps
+static_assert(EPT * WIDE_T * MAX_CLUSTER == LX_MAX_WIDTH, "the widest row");
 
 // Row arrays that are read
 enum In { IN_Y = 0, IN_R = 1, IN_GATE = 2, IN_DR = 3, IN_DH = 4, N_IN = 5 };
@@ -58,10 +59,10 @@ struct NormArgs {
   float* part;  // [CTAs of a column range][3][H]: their sums
 };
 
-// Registers a thread: the launch bounds below hold the compiler to these
-constexpr int FWD_REGS = 64, BWD_REGS = 96, WIDE_REGS = 128;
+constexpr int REGS = 128;  // a thread: the launch bounds hold the compiler to these
 
-enum Group { WARP = 0, CTA = 1, CLUSTER = 2 };
+enum Group { WARP = 0, CTA = 1, CLUSTER = 2, WIDE = 3 };  // WIDE: a cluster of larger CTAs
+constexpr int max_threads(int grp) { return grp == WIDE ? WIDE_T : CTA_T; }
 
 template <int BYTES>
 __device__ __forceinline__ void copy_async(void* dst, const void* src) {
@@ -82,10 +83,10 @@ __device__ __forceinline__ void copy_wait() {
 // bf16 values, which cannot be copied asynchronously and are read where they are used
 // (as are the widest rows, whose slots would not fit).  Values are held as pairs, for
 // the two-wide fp32 instructions.
-template <typename T, int VEC, int EPT, int GRP>
+template <typename T, int VEC, int GRP>
 struct Rows {
-  static constexpr int NCH = EPT / VEC, BYTES = VEC * sizeof(T), N2 = EPT / 2;
-  static constexpr bool RING = BYTES >= 4 && EPT == 8;
+  static constexpr int NCH = EPT / VEC, BYTES = VEC * sizeof(T), MAX_T = max_threads(GRP), MAX_W = MAX_T / 32;
+  static constexpr bool RING = BYTES >= 4 && GRP != WIDE;
   const NormArgs& A;
   char* ring;     // the thread's first slot
   uint32_t at;    // the round's stage, in bytes
@@ -98,16 +99,16 @@ struct Rows {
     if constexpr (GRP == WARP) {
       size = A.lanes;
       lane = threadIdx.x & (size - 1);
-      row = blockIdx.x * (WARP_T / size) + threadIdx.x / size;
-      step = gridDim.x * (WARP_T / size);
+      row = blockIdx.x * (CTA_T / size) + threadIdx.x / size;
+      step = gridDim.x * (CTA_T / size);
     } else {
       size = blockDim.x;
       lane = threadIdx.x;
       row = GRP == CTA ? blockIdx.x : blockIdx.y;
       step = GRP == CTA ? gridDim.x : gridDim.y;
-      if constexpr (GRP == CLUSTER) {
-        first = blockIdx.x * (CTA_T * EPT);
-        end = min(A.H, first + CTA_T * EPT);
+      if constexpr (GRP >= CLUSTER) {
+        first = blockIdx.x * (MAX_T * EPT);
+        end = min(A.H, first + MAX_T * EPT);
       }
     }
     col0 = first + lane * VEC;
@@ -167,14 +168,19 @@ struct Rows {
     }
   }
   __device__ void next() { at = at + A.stage_bytes == A.stages * A.stage_bytes ? 0 : at + A.stage_bytes; }
-  // the pieces of array k of row t, zero outside the row
+  // the pieces of array k of row t, zero outside the row: all, or half h of them
   __device__ void read(int k, unsigned t, float2* v) const {
+    read_half(k, t, v, 0);
+    read_half(k, t, v + N2 / 2, 1);
+  }
+  __device__ void read_half(int k, unsigned t, float2* v, int h) const {
     const T* g = RING ? (const T*)place(at, k) : src(k, t);
     const int apart = RING ? blockDim.x * VEC : size * VEC;
 #pragma unroll
-    for (int c = 0; c < NCH; ++c) {
-      const bool on = RING || (c < count && t < (unsigned)A.T);
-      const T* p = g + c * apart;
+    for (int c = 0; c < NCH / 2; ++c) {
+      const int d = h * (NCH / 2) + c;
+      const bool on = RING || (d < count && t < (unsigned)A.T);
+      const T* p = g + d * apart;
       if constexpr (BYTES == 16) {
         const uint4 w = on ? *(const uint4*)p : make_uint4(0u, 0u, 0u, 0u);
         if constexpr (sizeof(T) == 4) {
@@ -196,15 +202,19 @@ struct Rows {
     }
     if (GRP == WARP && RING && t >= (unsigned)A.T)  // what an earlier row left
 #pragma unroll
-      for (int i = 0; i < N2; ++i) v[i] = make_float2(0.f, 0.f);
+      for (int i = 0; i < N2 / 2; ++i) v[i] = make_float2(0.f, 0.f);
   }
   __device__ void write(void* out, unsigned t, const float2* v) const {
+    write_half(out, t, v, 0);
+    write_half(out, t, v + N2 / 2, 1);
+  }
+  __device__ void write_half(void* out, unsigned t, const float2* v, int h) const {
     if (GRP == WARP && t >= (unsigned)A.T) return;
     T* g = (T*)out + (uint64_t)t * (unsigned)A.H + col0;
 #pragma unroll
-    for (int c = 0; c < NCH; ++c)
-      if (c < count) {
-        T* p = g + c * size * VEC;
+    for (int c = 0; c < NCH / 2; ++c)
+      if (h * (NCH / 2) + c < count) {
+        T* p = g + (h * (NCH / 2) + c) * size * VEC;
         if constexpr (BYTES == 16) {
           uint4 w;
           if constexpr (sizeof(T) == 4)
@@ -232,68 +242,80 @@ struct Rows {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) elem(v, c, j) = p && c < count ? add + p[col(c) + j] : rest;
   }
-  // sums of N values over the row's threads, the same in each of them; buf (zero at
-  // first) is used in turn: a half is written again only after the barrier that follows
-  // its last reads
+  // sums of N (1 or 3) values over the row's threads, the same in each of them; buf is
+  // used in turn: a half is written again only after the barrier that follows its last
+  // reads
   template <int N>
-  __device__ void sum(float (&v)[N], float (*buf)[N][CTA_T / 32], int& turn) const {
+  __device__ void sum(float (&v)[N], float (*buf)[N][MAX_W], int& turn) const {
+    if constexpr (GRP == WARP) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      if (GRP == WARP && o >= size) continue;
+      for (int o = 16; o > 0; o >>= 1)
+        if (o < size)
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+          for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+      return;
     }
-    if constexpr (GRP != WARP) {
-      const int nw = blockDim.x >> 5;
-      float(*b)[CTA_T / 32] = buf[turn];
-      turn ^= 1;
-      if ((threadIdx.x & 31) == 0)
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
+    float(*b)[MAX_W] = buf[turn];
+    turn ^= 1;
+    if constexpr (N == 1) {
+      v[0] = warp_sum(v[0]);
+      if (lane == 0) b[0][warp] = v[0];
+    } else {
+      // three sums in six exchanges: value i ends in the lanes with lane % 4 == i
+      const bool o1 = lane & 1, o2 = lane & 2;
+      float p = o1 ? v[1] : v[0], q = o1 ? 0.f : v[2];
+      p += __shfl_xor_sync(0xffffffffu, o1 ? v[0] : v[1], 1);
+      q += __shfl_xor_sync(0xffffffffu, o1 ? v[2] : 0.f, 1);
+      float u = o2 ? q : p;
+      u += __shfl_xor_sync(0xffffffffu, o2 ? p : q, 2);
 #pragma unroll
-        for (int i = 0; i < N; ++i) b[i][threadIdx.x >> 5] = v[i];
-      if constexpr (GRP == CTA) {
-        __syncthreads();
+      for (int o = 4; o < 32; o <<= 1) u += __shfl_xor_sync(0xffffffffu, u, o);
+      if (lane < 3) b[lane][warp] = u;
+    }
+    if constexpr (GRP == CTA) {
+      __syncthreads();
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = 0.f;
-#pragma unroll
-        for (int w = 0; w < CTA_T / 32; w += 4)
-          if (w < nw)
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-              const float4 p = *(const float4*)&b[i][w];
-              v[i] += (p.x + p.y) + (p.z + p.w);
-            }
-      } else {
-        cooperative_groups::cluster_group cl = cooperative_groups::this_cluster();
-        cl.sync();
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = 0.f;
-        for (unsigned c = 0; c < cl.num_blocks(); ++c) {
-          const float* q = cl.map_shared_rank(&b[0][0], c);
-#pragma unroll
-          for (int i = 0; i < N; ++i)
-            for (int w = 0; w < nw; ++w) v[i] += q[i * (CTA_T / 32) + w];
+      for (int i = 0; i < N; ++i) {
+        const float4 p = *(const float4*)&b[i][0];
+        v[i] = (p.x + p.y) + (p.z + p.w);
+        if (nw > 4) {
+          const float4 r = *(const float4*)&b[i][4];
+          v[i] += (r.x + r.y) + (r.z + r.w);
         }
+      }
+    } else {
+      cooperative_groups::cluster_group cl = cooperative_groups::this_cluster();
+      cl.sync();
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = 0.f;
+      for (unsigned c = 0; c < cl.num_blocks(); ++c) {
+        const float* q = cl.map_shared_rank(&b[0][0], c);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          for (int w = 0; w < nw; ++w) v[i] += q[i * MAX_W + w];
       }
     }
   }
 };
+static_assert(CTA_T / 32 == 8, "sum() reads eight warps");
 
-template <int N>
-__device__ __forceinline__ void clear(float (*buf)[N][CTA_T / 32]) {
-  for (int i = threadIdx.x; i < 2 * N * (CTA_T / 32); i += blockDim.x) (&buf[0][0][0])[i] = 0.f;
+// the places of warps that a CTA does not have stay zero
+template <int N, int W>
+__device__ __forceinline__ void clear(float (*buf)[N][W]) {
+  for (int i = threadIdx.x; i < 2 * N * W; i += blockDim.x) (&buf[0][0][0])[i] = 0.f;
   __syncthreads();
 }
 
 extern __shared__ uint4 norm_ring[];
 
-template <typename T, int VEC, int EPT, int GRP>
-__global__ void __launch_bounds__(CTA_T, EPT == 8 ? 2 : 1)
+template <typename T, int VEC, int GRP>
+__global__ void __launch_bounds__(max_threads(GRP), 65536 / REGS / max_threads(GRP))
 k_resnorm_fwd(const __grid_constant__ NormArgs A) {
-  constexpr int N2 = EPT / 2;
-  __shared__ __align__(16) float buf[2][1][CTA_T / 32];
+  __shared__ __align__(16) float buf[2][1][max_threads(GRP) / 32];
   int turn = 0;
   if (GRP == CTA) clear(buf);
-  Rows<T, VEC, EPT, GRP> R(A, (char*)norm_ring);
+  Rows<T, VEC, GRP> R(A, (char*)norm_ring);
   R.begin();
   const float inv = 1.f / (float)A.H;
   const float2 a2 = both(A.a);
@@ -357,20 +379,19 @@ k_resnorm_fwd(const __grid_constant__ NormArgs A) {
     }
   }
   // a CTA's shared memory outlives its neighbours' reads
-  if constexpr (GRP == CLUSTER) cooperative_groups::this_cluster().sync();
+  if constexpr (GRP >= CLUSTER) cooperative_groups::this_cluster().sync();
 }
 
 // With x, D0 = dr' + s2 e and v = g u in hand, one set of sums serves both norms:
 // mean(e x) gives D = D0 - m x, and sum(f n) = sum(D v) = sum(D0 v) - m sum(x v) (for a
 // token's gate the sums are of u, which its gradient needs, and f n is g times them).
-template <typename T, int VEC, int EPT, int GRP>
-__global__ void __launch_bounds__(EPT == 8 ? 640 : CTA_T, 1)
+template <typename T, int VEC, int GRP>
+__global__ void __launch_bounds__(max_threads(GRP), 65536 / REGS / max_threads(GRP))
 k_resnorm_bwd(const __grid_constant__ NormArgs A) {
-  constexpr int N2 = EPT / 2;
-  __shared__ __align__(16) float buf[2][3][CTA_T / 32];
+  __shared__ __align__(16) float buf[2][3][max_threads(GRP) / 32];
   int turn = 0;
   if (GRP == CTA) clear(buf);
-  Rows<T, VEC, EPT, GRP> R(A, (char*)norm_ring);
+  Rows<T, VEC, GRP> R(A, (char*)norm_ring);
   R.begin();
   const float inv = 1.f / (float)A.H;
   const bool has_y = A.in[IN_Y], post = A.w_post, token = A.gate_kind == LX_GATE_TOKEN;
@@ -382,10 +403,10 @@ k_resnorm_bwd(const __grid_constant__ NormArgs A) {
     for (int i = 0; i < N2; i += 2)
       par[(k * (EPT / 4) + i / 2) * blockDim.x] = make_float4(v[i].x, v[i].y, v[i + 1].x, v[i + 1].y);
   };
-  auto get = [&](int k, float2* v) {
+  auto get = [&](int k, float2* v, int h) {  // half h of them
 #pragma unroll
-    for (int i = 0; i < N2; i += 2) {
-      const float4 p = par[(k * (EPT / 4) + i / 2) * blockDim.x];
+    for (int i = 0; i < N2 / 2; i += 2) {
+      const float4 p = par[(k * (EPT / 4) + h * (EPT / 8) + i / 2) * blockDim.x];
       v[i] = make_float2(p.x, p.y);
       v[i + 1] = make_float2(p.z, p.w);
     }
@@ -414,74 +435,90 @@ k_resnorm_bwd(const __grid_constant__ NormArgs A) {
     const float s1 = n1, s2 = n2, tok = ng;
     scalars(t + R.step);
     R.advance(t);
-    float2 n[N2], D[N2], x[N2], g[N2], w1[N2];  // n: y s1
-    get(0, w1);
-    if (A.in[IN_DR]) R.read(IN_DR, t, D);
-    else
+    // by halves, so that few values wait; n = y s1, u and g are formed where they are
+    // used, before and after the sums
+    constexpr int H2 = N2 / 2;
+    auto block = [&](float2* n, float2* u, float2* g, int h) {
+      R.read_half(IN_Y, t, n, h);
+      get(0, u, h);
+      if (A.in[IN_GATE]) R.read_half(IN_GATE, t, g, h);
+      else get(2, g, h);
 #pragma unroll
-      for (int i = 0; i < N2; ++i) D[i] = zero;
-    if (has_y) {
-      R.read(IN_Y, t, n);
-#pragma unroll
-      for (int i = 0; i < N2; ++i) n[i] = mul2(n[i], both(s1));
-      if (A.in[IN_GATE]) R.read(IN_GATE, t, g);
-      else get(2, g);
-    }
-    float2 q0 = zero, q1 = zero, q2 = zero;
-    if (A.in[IN_DH]) {
-      float2 dh[N2], w2[N2];
-      get(1, w2);
-      R.read(IN_R, t, x);
-      R.read(IN_DH, t, dh);
-#pragma unroll
-      for (int i = 0; i < N2; ++i) {
-        x[i] = mul2(x[i], both(A.a));
-        if (has_y) x[i] = fma2(mul2(n[i], w1[i]), mul2(g[i], both(tok)), x[i]);
-        x[i] = mul2(x[i], both(s2));
-        acc[2][i] = fma2(dh[i], x[i], acc[2][i]);
-        const float2 e = mul2(dh[i], w2[i]);
-        q0 = fma2(e, x[i], q0);
-        D[i] = fma2(both(s2), e, D[i]);
+      for (int i = 0; i < H2; ++i) {
+        n[i] = mul2(n[i], both(s1));
+        u[i] = mul2(n[i], u[i]);
       }
-    } else {
+    };
+    float2 D[N2], x[N2], q0 = zero, q1 = zero, q2 = zero;
 #pragma unroll
-      for (int i = 0; i < N2; ++i) x[i] = zero;
-    }
-    if (has_y)
+    for (int h = 0; h < 2; ++h) {
+      float2 u[H2], n[H2], g[H2], *Dh = D + h * H2, *xh = x + h * H2;
+      if (A.in[IN_DR]) R.read_half(IN_DR, t, Dh, h);
+      else
 #pragma unroll
-      for (int i = 0; i < N2; ++i) {
-        const float2 v = mul2(mul2(n[i], w1[i]), g[i]);
-        q1 = fma2(D[i], v, q1);
-        q2 = fma2(x[i], v, q2);
+        for (int i = 0; i < H2; ++i) Dh[i] = zero;
+      if (has_y) block(n, u, g, h);
+      if (A.in[IN_DH]) {
+        float2 dh[H2], w2[H2];
+        get(1, w2, h);
+        R.read_half(IN_R, t, xh, h);
+        R.read_half(IN_DH, t, dh, h);
+#pragma unroll
+        for (int i = 0; i < H2; ++i) {
+          xh[i] = mul2(xh[i], both(A.a));
+          if (has_y) xh[i] = fma2(u[i], mul2(g[i], both(tok)), xh[i]);
+          xh[i] = mul2(xh[i], both(s2));
+          acc[2][h * H2 + i] = fma2(dh[i], xh[i], acc[2][h * H2 + i]);
+          const float2 e = mul2(dh[i], w2[i]);
+          q0 = fma2(e, xh[i], q0);
+          Dh[i] = fma2(both(s2), e, Dh[i]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < H2; ++i) xh[i] = zero;
       }
+      if (has_y)
+#pragma unroll
+        for (int i = 0; i < H2; ++i) {
+          const float2 v = mul2(u[i], g[i]);
+          q1 = fma2(Dh[i], v, q1);
+          q2 = fma2(xh[i], v, q2);
+        }
+    }
     float q[3] = {q0.x + q0.y, q1.x + q1.y, q2.x + q2.y};
     R.sum(q, buf, turn);
     const float m = q[0] * inv * s2;
     const float dv = q[1] - m * q[2];
+    const float m1 = post ? dv * inv * tok : 0.f;
+    if (token && A.dgate && R.writer() && t < (unsigned)A.T) ((float*)A.dgate)[t] = dv;
 #pragma unroll
-    for (int i = 0; i < N2; ++i) D[i] = fma2(both(-m), x[i], D[i]);
-    if (A.dr) {
+    for (int h = 0; h < 2; ++h) {
+      float2 *Dh = D + h * H2, *xh = x + h * H2;
 #pragma unroll
-      for (int i = 0; i < N2; ++i) x[i] = mul2(D[i], both(A.a));
-      R.write(A.dr, t, x);
-    }
-    if (has_y) {
-      const float m1 = post ? dv * inv * tok : 0.f;
-      if (token && A.dgate && R.writer() && t < (unsigned)A.T) ((float*)A.dgate)[t] = dv;
-#pragma unroll
-      for (int i = 0; i < N2; ++i) {
-        x[i] = mul2(D[i], mul2(n[i], w1[i]));
-        acc[1][i] = add2(acc[1][i], x[i]);
-        const float2 f = mul2(D[i], mul2(g[i], both(tok)));
-        acc[0][i] = fma2(f, n[i], acc[0][i]);
-        D[i] = mul2(both(s1), fma2(both(-m1), n[i], mul2(f, w1[i])));
+      for (int i = 0; i < H2; ++i) {
+        Dh[i] = fma2(both(-m), xh[i], Dh[i]);
+        xh[i] = mul2(Dh[i], both(A.a));
       }
-      if (A.in[IN_GATE] && A.dgate) R.write(A.dgate, t, x);
-      if (A.dy) R.write(A.dy, t, D);
+      if (A.dr) R.write_half(A.dr, t, xh, h);
+      if (has_y) {
+        float2 u[H2], n[H2], g[H2], w1[H2];
+        block(n, u, g, h);
+        get(0, w1, h);
+#pragma unroll
+        for (int i = 0; i < H2; ++i) {
+          u[i] = mul2(Dh[i], u[i]);
+          acc[1][h * H2 + i] = add2(acc[1][h * H2 + i], u[i]);
+          const float2 f = mul2(Dh[i], mul2(g[i], both(tok)));
+          acc[0][h * H2 + i] = fma2(f, n[i], acc[0][h * H2 + i]);
+          Dh[i] = mul2(both(s1), fma2(both(-m1), n[i], mul2(f, w1[i])));
+        }
+        if (A.in[IN_GATE] && A.dgate) R.write_half(A.dgate, t, u, h);
+        if (A.dy) R.write_half(A.dy, t, Dh, h);
+      }
     }
   }
   if (A.part) {
-    float* part = A.part + (GRP == CLUSTER ? (long)blockIdx.y : (long)blockIdx.x) * 3 * A.H;
+    float* part = A.part + (GRP >= CLUSTER ? (long)blockIdx.y : (long)blockIdx.x) * 3 * A.H;
     float* ws = (float*)norm_ring;  // [rows of the CTA][H], the slots' copies being done
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
@@ -495,9 +532,9 @@ k_resnorm_bwd(const __grid_constant__ NormArgs A) {
 #pragma unroll
             for (int j = 0; j < VEC; ++j) ws[(threadIdx.x / R.size) * A.H + R.col(c) + j] = R.elem(acc[k], c, j);
         __syncthreads();
-        for (int e = threadIdx.x; e < A.H; e += WARP_T) {
+        for (int e = threadIdx.x; e < A.H; e += CTA_T) {
           float s = 0.f;
-          for (int w = 0; w < WARP_T / R.size; ++w) s += ws[w * A.H + e];
+          for (int w = 0; w < CTA_T / R.size; ++w) s += ws[w * A.H + e];
           part[(long)k * A.H + e] = s;
         }
       } else {
@@ -509,7 +546,7 @@ k_resnorm_bwd(const __grid_constant__ NormArgs A) {
       }
     }
   }
-  if constexpr (GRP == CLUSTER) cooperative_groups::this_cluster().sync();
+  if constexpr (GRP >= CLUSTER) cooperative_groups::this_cluster().sync();
 }
 
 // out[k][e] = sum over p of part[p][k][e], in a fixed order: 32 columns and 8 ranges
@@ -535,56 +572,51 @@ k_resnorm_sum(const float* __restrict__ part, int n, int H, float* o0, float* o1
 }
 
 struct Shape {
-  int grp, ept, threads, cols, lanes;  // cols: CTAs to a row
-  long groups;                         // CTAs (clusters) that have a row
+  int grp, threads, cols, lanes;  // cols: CTAs to a row
+  long groups;                    // CTAs (clusters) that have a row
 };
 
 Shape shape_of(int T, int H) {
   Shape s;
-  s.grp = H <= WARP_H ? WARP : H <= CTA_H ? CTA : CLUSTER;
-  s.ept = H <= CTA_H * MAX_CLUSTER ? 8 : 16;
-  s.cols = s.grp == CLUSTER ? (H + CTA_T * s.ept - 1) / (CTA_T * s.ept) : 1;
+  s.grp = H <= WARP_H ? WARP : H <= CTA_T * EPT ? CTA : H <= CTA_T * EPT * MAX_CLUSTER ? CLUSTER : WIDE;
+  s.threads = s.grp == CTA ? (H + 32 * EPT - 1) / (32 * EPT) * 32 : max_threads(s.grp);
+  s.cols = s.grp >= CLUSTER ? (H + s.threads * EPT - 1) / (s.threads * EPT) : 1;
   s.lanes = 1;
-  while (s.lanes < 32 && s.lanes * 8 < H) s.lanes *= 2;
-  s.threads = s.grp == WARP ? WARP_T : s.grp == CTA ? (H + 255) / 256 * 32 : CTA_T;
-  s.groups = s.grp == WARP ? ((long)T + WARP_T / s.lanes - 1) / (WARP_T / s.lanes) : T;
+  while (s.lanes < 32 && s.lanes * EPT < H) s.lanes *= 2;
+  const int rows = s.grp == WARP ? CTA_T / s.lanes : 1;
+  s.groups = ((long)T + rows - 1) / rows;
   return s;
 }
 
 constexpr int SMS = 152;
 
-// CTAs (clusters) that rows are dealt to: what is resident with `regs` registers a
-// thread and `smem` bytes a CTA
-long resident(const Shape& s, int regs, size_t smem) {
-  const long ctas = std::min<long>(65536 / (regs * s.threads), (long)(227 * 1024 / (smem + 2048)));
-  return std::min(s.groups, std::max(1L, SMS * std::max(1L, ctas) / s.cols));
-}
+// CTAs (clusters) that rows are dealt to: as many as the registers of the SMs hold.  It
+// fixes the backward's workspace, so it does not depend on types or strides.
+int ctas_per_sm(const Shape& s) { return std::max(1, 65536 / (REGS * s.threads)); }
+long resident(const Shape& s) { return std::min(s.groups, std::max(1L, (long)SMS * ctas_per_sm(s) / s.cols)); }
 
-// The backward's groups fix the workspace: they do not depend on types or strides
-long bwd_groups(const Shape& s) { return resident(s, s.ept == 8 ? BWD_REGS : WIDE_REGS, 0); }
-
-// Slots of a CTA: three rows, or two where three would keep CTAs off an SM that its
-// registers have room for (fp32 with a full gate)
-size_t ring_bytes(const Shape& s, NormArgs& A, size_t es, int regs, size_t more) {
+// Slots of a CTA: three rows, or two where three would not fit beside the SM's other CTAs
+size_t ring_bytes(const Shape& s, NormArgs& A, size_t es, size_t more) {
   size_t row = 0;
   for (int k = 0; k < N_IN; ++k)
     if (A.in[k]) {
       A.slot_at[k] = (uint32_t)row;
-      row += (size_t)s.ept * es * s.threads;
+      row += EPT * es * s.threads;
     }
   A.stage_bytes = (uint32_t)row;
-  A.stages = (3 * row + more + 1024) * (65536 / (regs * s.threads)) <= 227 * 1024 ? 3 : 2;
+  A.stages = (3 * row + more + 1024) * ctas_per_sm(s) <= 227 * 1024 ? 3 : 2;
   return A.stages * row;
 }
 
 template <typename... KArgs>
-lx_status launch(void (*kern)(KArgs...), const Shape& s, long groups, size_t smem, const NormArgs& A, cudaStream_t st,
+lx_status launch(void (*kern)(KArgs...), const Shape& s, size_t smem, const NormArgs& A, cudaStream_t st,
                  bool (&cap)[64]) {
   int dev = 0;
   LX_CUDA(cudaGetDevice(&dev));
   LX_CUDA(smem_cap_once((const void*)kern, 224 * 1024, dev, cap));
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = s.grp == CLUSTER ? dim3(s.cols, (unsigned)groups) : dim3((unsigned)groups);
+  const unsigned groups = (unsigned)resident(s);
+  cfg.gridDim = s.grp >= CLUSTER ? dim3(s.cols, groups) : dim3(groups);
   cfg.blockDim = dim3(s.threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
@@ -593,32 +625,31 @@ lx_status launch(void (*kern)(KArgs...), const Shape& s, long groups, size_t sme
   attr[0].val.clusterDim.x = s.cols;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = s.grp == CLUSTER ? 1 : 0;
+  cfg.numAttrs = s.grp >= CLUSTER ? 1 : 0;
   LX_CUDA(cudaLaunchKernelEx(&cfg, kern, A));
   return LX_OK;
 }
 
-template <typename T, int VEC, int EPT, int GRP, bool BWD>
+template <typename T, int VEC, int GRP, bool BWD>
 lx_status launch_one(const Shape& s, NormArgs& A, cudaStream_t st) {
   static bool cap[64] = {};
-  constexpr int REGS = EPT == 16 ? WIDE_REGS : BWD ? BWD_REGS : FWD_REGS;
   const size_t par = BWD ? sizeof(float) * 3 * EPT * s.threads : 0;
   size_t smem = 0;
   A.stages = 2;
-  if (VEC * sizeof(T) >= 4 && EPT == 8) smem = ring_bytes(s, A, sizeof(T), REGS, par);
-  A.par_at = (int)smem;
+  if (Rows<T, VEC, GRP>::RING) smem = ring_bytes(s, A, sizeof(T), par);
+  A.par_at = (uint32_t)smem;
   smem += par;
-  if (BWD && GRP == WARP) smem = std::max(smem, sizeof(float) * (WARP_T / s.lanes) * A.H);
-  if (BWD) return launch(k_resnorm_bwd<T, VEC, EPT, GRP>, s, bwd_groups(s), smem, A, st, cap);
-  return launch(k_resnorm_fwd<T, VEC, EPT, GRP>, s, resident(s, REGS, smem), smem, A, st, cap);
+  if (BWD && GRP == WARP) smem = std::max(smem, sizeof(float) * (CTA_T / s.lanes) * A.H);
+  if (BWD) return launch(k_resnorm_bwd<T, VEC, GRP>, s, smem, A, st, cap);
+  return launch(k_resnorm_fwd<T, VEC, GRP>, s, smem, A, st, cap);
 }
 
 template <typename T, int VEC, bool BWD>
 lx_status launch_vec(const Shape& s, NormArgs& A, cudaStream_t st) {
-  if (s.grp == WARP) return launch_one<T, VEC, 8, WARP, BWD>(s, A, st);
-  if (s.grp == CTA) return launch_one<T, VEC, 8, CTA, BWD>(s, A, st);
-  if (s.ept == 8) return launch_one<T, VEC, 8, CLUSTER, BWD>(s, A, st);
-  return launch_one<T, VEC, 16, CLUSTER, BWD>(s, A, st);
+  if (s.grp == WARP) return launch_one<T, VEC, WARP, BWD>(s, A, st);
+  if (s.grp == CTA) return launch_one<T, VEC, CTA, BWD>(s, A, st);
+  if (s.grp == CLUSTER) return launch_one<T, VEC, CLUSTER, BWD>(s, A, st);
+  return launch_one<T, VEC, WIDE, BWD>(s, A, st);
 }
 
 // piece: bytes that divide every row's start and length (16, 4, or 2)
@@ -729,7 +760,7 @@ extern "C" lx_status lx_residual_norm_workspace(int32_t T, int32_t H, uint64_t* 
   if (!bytes) return fail(LX_ERR_ARG, "bytes is NULL");
   if (T < 0) return fail(LX_ERR_ARG, "T < 0");
   if (H < 1 || H > LX_MAX_WIDTH) return fail(LX_ERR_SHAPE, "H must be in 1..LX_MAX_WIDTH");
-  *bytes = (uint64_t)bwd_groups(shape_of(T, H)) * 3 * H * sizeof(float);
+  *bytes = (uint64_t)resident(shape_of(T, H)) * 3 * H * sizeof(float);
   return LX_OK;
 }
 
@@ -772,7 +803,7 @@ extern "C" lx_status lx_residual_norm_backward(const lx_resnorm_desc* d, const f
       if (overlap(outs[i], out, outs[j], out)) return fail(LX_ERR_ARG, "two outputs overlap");
   }
   const Shape s = shape_of(d->T, d->H);
-  const long groups = bwd_groups(s);
+  const long groups = resident(s);
   if (params) {
     if (!workspace || !aligned(workspace, 16)) return fail(LX_ERR_ARG, "workspace is NULL or not 16-byte aligned");
     if (workspace_bytes < (uint64_t)groups * 3 * d->H * sizeof(float)) return fail(LX_ERR_ARG, "workspace too small");
