@@ -55,14 +55,15 @@ struct NormArgs {
   float* stats;  // [2][T]: s1, s2
   // backward
   void *dr, *dy, *dgate;
-  int sums;     // bits of the parameter gradients: dw_post, dgate (channel), dw_pre
-  float* part;  // [CTAs of a column range][3][H]: their sums
+  int sums;     // bits of the column sums wanted: of s1 D y, of dh x
+  float* part;  // [CTAs of a column range][2][H]: those sums
 };
 
 constexpr int REGS = 128;  // a thread: the launch bounds hold the compiler to these
 
 enum Group { WARP = 0, CTA = 1, CLUSTER = 2, WIDE = 3 };  // WIDE: a cluster of larger CTAs
 constexpr int max_threads(int grp) { return grp == WIDE ? WIDE_T : CTA_T; }
+constexpr int max_cols(int grp) { return grp >= CLUSTER ? MAX_CLUSTER : 1; }
 
 template <int BYTES>
 __device__ __forceinline__ void copy_async(void* dst, const void* src) {
@@ -87,6 +88,7 @@ template <typename T, int VEC, int GRP>
 struct Rows {
   static constexpr int NCH = EPT / VEC, BYTES = VEC * sizeof(T), MAX_T = max_threads(GRP), MAX_W = MAX_T / 32;
   static constexpr bool RING = BYTES >= 4 && GRP != WIDE;
+  static constexpr int COLS = max_cols(GRP);
   const NormArgs& A;
   char* ring;     // the thread's first slot
   uint32_t at;    // the round's stage, in bytes
@@ -246,7 +248,7 @@ struct Rows {
   // used in turn: a half is written again only after the barrier that follows its last
   // reads
   template <int N>
-  __device__ void sum(float (&v)[N], float (*buf)[N][MAX_W], int& turn) const {
+  __device__ void sum(float (&v)[N], float (*buf)[N][COLS][MAX_W], int& turn) const {
     if constexpr (GRP == WARP) {
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1)
@@ -256,54 +258,51 @@ struct Rows {
       return;
     }
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
-    float(*b)[MAX_W] = buf[turn];
+    float(*b)[COLS][MAX_W] = buf[turn];
     turn ^= 1;
+    float u;
     if constexpr (N == 1) {
-      v[0] = warp_sum(v[0]);
-      if (lane == 0) b[0][warp] = v[0];
+      u = warp_sum(v[0]);
     } else {
       // three sums in six exchanges: value i ends in the lanes with lane % 4 == i
       const bool o1 = lane & 1, o2 = lane & 2;
       float p = o1 ? v[1] : v[0], q = o1 ? 0.f : v[2];
       p += __shfl_xor_sync(0xffffffffu, o1 ? v[0] : v[1], 1);
       q += __shfl_xor_sync(0xffffffffu, o1 ? v[2] : 0.f, 1);
-      float u = o2 ? q : p;
+      u = o2 ? q : p;
       u += __shfl_xor_sync(0xffffffffu, o2 ? p : q, 2);
 #pragma unroll
       for (int o = 4; o < 32; o <<= 1) u += __shfl_xor_sync(0xffffffffu, u, o);
-      if (lane < 3) b[lane][warp] = u;
     }
+    int cols = 1;
     if constexpr (GRP == CTA) {
+      if (lane < N) b[lane][0][warp] = u;
       __syncthreads();
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float4 p = *(const float4*)&b[i][0];
-        v[i] = (p.x + p.y) + (p.z + p.w);
-        if (nw > 4) {
-          const float4 r = *(const float4*)&b[i][4];
-          v[i] += (r.x + r.y) + (r.z + r.w);
-        }
-      }
-    } else {
+    } else {  // every CTA of the cluster gets every warp's sums
       cooperative_groups::cluster_group cl = cooperative_groups::this_cluster();
+      cols = cl.num_blocks();
+      const int i = lane & 3, c = lane >> 2;
+      if (i < N && c < cols) *cl.map_shared_rank(&b[i][cl.block_rank()][warp], c) = u;
       cl.sync();
-#pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = 0.f;
-      for (unsigned c = 0; c < cl.num_blocks(); ++c) {
-        const float* q = cl.map_shared_rank(&b[0][0], c);
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-          for (int w = 0; w < nw; ++w) v[i] += q[i * MAX_W + w];
-      }
     }
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = 0.f;
+    for (int c = 0; c < cols; ++c)
+#pragma unroll
+      for (int w = 0; w < MAX_W; w += 4)
+        if (w < nw)
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            const float4 p = *(const float4*)&b[i][c][w];
+            v[i] += (p.x + p.y) + (p.z + p.w);
+          }
   }
 };
-static_assert(CTA_T / 32 == 8, "sum() reads eight warps");
 
 // the places of warps that a CTA does not have stay zero
-template <int N, int W>
-__device__ __forceinline__ void clear(float (*buf)[N][W]) {
-  for (int i = threadIdx.x; i < 2 * N * W; i += blockDim.x) (&buf[0][0][0])[i] = 0.f;
+template <int N, int C, int W>
+__device__ __forceinline__ void clear(float (*buf)[N][C][W]) {
+  for (int i = threadIdx.x; i < 2 * N * C * W; i += blockDim.x) (&buf[0][0][0][0])[i] = 0.f;
   __syncthreads();
 }
 
@@ -312,11 +311,12 @@ extern __shared__ uint4 norm_ring[];
 template <typename T, int VEC, int GRP>
 __global__ void __launch_bounds__(max_threads(GRP), 65536 / REGS / max_threads(GRP))
 k_resnorm_fwd(const __grid_constant__ NormArgs A) {
-  __shared__ __align__(16) float buf[2][1][max_threads(GRP) / 32];
+  __shared__ __align__(16) float buf[2][1][max_cols(GRP)][max_threads(GRP) / 32];
   int turn = 0;
   if (GRP == CTA) clear(buf);
   Rows<T, VEC, GRP> R(A, (char*)norm_ring);
   R.begin();
+  if constexpr (GRP >= CLUSTER) cooperative_groups::this_cluster().sync();  // all have started
   const float inv = 1.f / (float)A.H;
   const float2 a2 = both(A.a);
   const bool has_y = A.in[IN_Y], post = A.w_post, token = A.gate_kind == LX_GATE_TOKEN;
@@ -378,25 +378,32 @@ k_resnorm_fwd(const __grid_constant__ NormArgs A) {
       A.stats[(long)A.T + t] = s2;
     }
   }
-  // a CTA's shared memory outlives its neighbours' reads
+  // a CTA's shared memory outlives its neighbours' writes
   if constexpr (GRP >= CLUSTER) cooperative_groups::this_cluster().sync();
 }
 
-// With x, D0 = dr' + s2 e and v = g u in hand, one set of sums serves both norms:
-// mean(e x) gives D = D0 - m x, and sum(f n) = sum(D v) = sum(D0 v) - m sum(x v) (for a
-// token's gate the sums are of u, which its gradient needs, and f n is g times them).
+// In the thread's terms, with X = r' = a r + s1 Y, Y = y g W1, E = s2 dh W2, D0 = dr' + E:
+// one set of sums, q0 = sum(E X), q1 = sum(D0 Y), q2 = sum(X Y), serves both norms:
+//   M = s2^2 q0 / H,  D = D0 - M X,  V = sum(D Y) = q1 - M q2,
+//   dy = s1 (D g W1) - s1^3 V / H y        (sum(f n) = s1 V)
+// A token's gate is left out of Y (its gradient is s1 V) and put to s1 instead.  A column's
+// sum B of s1 D y (with a full or token gate: of s1 g D y) gives dw_post = g B and a channel
+// gate's gradient W1 B.
 template <typename T, int VEC, int GRP>
 __global__ void __launch_bounds__(max_threads(GRP), 65536 / REGS / max_threads(GRP))
 k_resnorm_bwd(const __grid_constant__ NormArgs A) {
-  __shared__ __align__(16) float buf[2][3][max_threads(GRP) / 32];
+  __shared__ __align__(16) float buf[2][3][max_cols(GRP)][max_threads(GRP) / 32];
   int turn = 0;
   if (GRP == CTA) clear(buf);
   Rows<T, VEC, GRP> R(A, (char*)norm_ring);
   R.begin();
+  if constexpr (GRP >= CLUSTER) cooperative_groups::this_cluster().sync();  // all have started
   const float inv = 1.f / (float)A.H;
-  const bool has_y = A.in[IN_Y], post = A.w_post, token = A.gate_kind == LX_GATE_TOKEN;
+  const bool has_y = A.in[IN_Y], post = A.w_post, token = A.gate_kind == LX_GATE_TOKEN, full = A.in[IN_GATE];
   const float2 zero = make_float2(0.f, 0.f);
-  // the columns' parameters, in slots that only this thread reads: registers are short
+  constexpr int H2 = N2 / 2;
+  // the columns' parameters g W1 (W1 with a full gate) and W2, in slots that only this
+  // thread reads: registers are short
   float4* par = (float4*)((char*)norm_ring + A.par_at) + threadIdx.x;
   auto put = [&](int k, const float2* v) {
 #pragma unroll
@@ -405,24 +412,27 @@ k_resnorm_bwd(const __grid_constant__ NormArgs A) {
   };
   auto get = [&](int k, float2* v, int h) {  // half h of them
 #pragma unroll
-    for (int i = 0; i < N2 / 2; i += 2) {
+    for (int i = 0; i < H2; i += 2) {
       const float4 p = par[(k * (EPT / 4) + h * (EPT / 8) + i / 2) * blockDim.x];
       v[i] = make_float2(p.x, p.y);
       v[i + 1] = make_float2(p.z, p.w);
     }
   };
   {
-    float2 v[N2];
+    float2 v[N2], g[N2];
     R.params(A.w_post, A.off, 1.f, v);
+    R.params(A.gate_kind == LX_GATE_CHANNEL ? A.gate : nullptr, 0.f, 1.f, g);
+#pragma unroll
+    for (int i = 0; i < N2; ++i) v[i] = mul2(v[i], g[i]);
     put(0, v);
     R.params(A.w_pre, A.off, 0.f, v);
     put(1, v);
-    R.params(A.gate_kind == LX_GATE_CHANNEL ? A.gate : nullptr, 0.f, 1.f, v);
-    put(2, v);
   }
-  float2 acc[3][N2];
+  // this launch started after its predecessors had ended: the next may be scheduled
+  if (A.part) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  float2 acc[2][N2];  // B, dw_pre
 #pragma unroll
-  for (int i = 0; i < N2; ++i) acc[0][i] = acc[1][i] = acc[2][i] = zero;
+  for (int i = 0; i < N2; ++i) acc[0][i] = acc[1][i] = zero;
   float n1 = 0.f, n2 = 0.f, ng = 1.f;  // a row's scalars are read a round ahead
   auto scalars = [&](unsigned t) {
     if (t >= (unsigned)A.T) return;
@@ -432,96 +442,100 @@ k_resnorm_bwd(const __grid_constant__ NormArgs A) {
   };
   scalars(R.row);
   for (unsigned t = R.row; R.more(t); t += R.step, R.next()) {
-    const float s1 = n1, s2 = n2, tok = ng;
+    const float s1 = n1, s2 = n2, sg = n1 * ng;  // sg: with the token's gate
     scalars(t + R.step);
     R.advance(t);
-    // by halves, so that few values wait; n = y s1, u and g are formed where they are
-    // used, before and after the sums
-    constexpr int H2 = N2 / 2;
-    auto block = [&](float2* n, float2* u, float2* g, int h) {
-      R.read_half(IN_Y, t, n, h);
-      get(0, u, h);
-      if (A.in[IN_GATE]) R.read_half(IN_GATE, t, g, h);
-      else get(2, g, h);
-#pragma unroll
-      for (int i = 0; i < H2; ++i) {
-        n[i] = mul2(n[i], both(s1));
-        u[i] = mul2(n[i], u[i]);
-      }
-    };
-    float2 D[N2], x[N2], q0 = zero, q1 = zero, q2 = zero;
+    // by halves, so that few values wait; y and Y are formed before and after the sums
+    float2 D[N2], X[N2], q0 = zero, q1 = zero, q2 = zero;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      float2 u[H2], n[H2], g[H2], *Dh = D + h * H2, *xh = x + h * H2;
+      float2 Y[H2], *Dh = D + h * H2, *Xh = X + h * H2;
       if (A.in[IN_DR]) R.read_half(IN_DR, t, Dh, h);
       else
 #pragma unroll
         for (int i = 0; i < H2; ++i) Dh[i] = zero;
-      if (has_y) block(n, u, g, h);
+      if (has_y) {
+        float2 w[H2];
+        get(0, w, h);
+        R.read_half(IN_Y, t, Y, h);
+#pragma unroll
+        for (int i = 0; i < H2; ++i) Y[i] = mul2(Y[i], w[i]);
+        if (full) {
+          R.read_half(IN_GATE, t, w, h);
+#pragma unroll
+          for (int i = 0; i < H2; ++i) Y[i] = mul2(Y[i], w[i]);
+        }
+      }
       if (A.in[IN_DH]) {
         float2 dh[H2], w2[H2];
         get(1, w2, h);
-        R.read_half(IN_R, t, xh, h);
+        R.read_half(IN_R, t, Xh, h);
         R.read_half(IN_DH, t, dh, h);
 #pragma unroll
         for (int i = 0; i < H2; ++i) {
-          xh[i] = mul2(xh[i], both(A.a));
-          if (has_y) xh[i] = fma2(u[i], mul2(g[i], both(tok)), xh[i]);
-          xh[i] = mul2(xh[i], both(s2));
-          acc[2][h * H2 + i] = fma2(dh[i], xh[i], acc[2][h * H2 + i]);
-          const float2 e = mul2(dh[i], w2[i]);
-          q0 = fma2(e, xh[i], q0);
-          Dh[i] = fma2(both(s2), e, Dh[i]);
+          Xh[i] = mul2(Xh[i], both(A.a));
+          if (has_y) Xh[i] = fma2(both(sg), Y[i], Xh[i]);
+          dh[i] = mul2(dh[i], both(s2));
+          acc[1][h * H2 + i] = fma2(dh[i], Xh[i], acc[1][h * H2 + i]);
+          const float2 E = mul2(dh[i], w2[i]);
+          q0 = fma2(E, Xh[i], q0);
+          Dh[i] = add2(Dh[i], E);
         }
       } else {
 #pragma unroll
-        for (int i = 0; i < H2; ++i) xh[i] = zero;
+        for (int i = 0; i < H2; ++i) Xh[i] = zero;
       }
       if (has_y)
 #pragma unroll
         for (int i = 0; i < H2; ++i) {
-          const float2 v = mul2(u[i], g[i]);
-          q1 = fma2(Dh[i], v, q1);
-          q2 = fma2(xh[i], v, q2);
+          q1 = fma2(Dh[i], Y[i], q1);
+          q2 = fma2(Xh[i], Y[i], q2);
         }
     }
     float q[3] = {q0.x + q0.y, q1.x + q1.y, q2.x + q2.y};
     R.sum(q, buf, turn);
-    const float m = q[0] * inv * s2;
-    const float dv = q[1] - m * q[2];
-    const float m1 = post ? dv * inv * tok : 0.f;
-    if (token && A.dgate && R.writer() && t < (unsigned)A.T) ((float*)A.dgate)[t] = dv;
+    const float M = q[0] * inv * s2 * s2;
+    const float V = q[1] - M * q[2];
+    const float m1 = post ? sg * s1 * s1 * inv * V : 0.f;
+    if (token && A.dgate && R.writer() && t < (unsigned)A.T) ((float*)A.dgate)[t] = s1 * V;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      float2 *Dh = D + h * H2, *xh = x + h * H2;
+      float2 *Dh = D + h * H2, *Xh = X + h * H2;
 #pragma unroll
       for (int i = 0; i < H2; ++i) {
-        Dh[i] = fma2(both(-m), xh[i], Dh[i]);
-        xh[i] = mul2(Dh[i], both(A.a));
+        Dh[i] = fma2(both(-M), Xh[i], Dh[i]);
+        Xh[i] = mul2(Dh[i], both(A.a));
       }
-      if (A.dr) R.write_half(A.dr, t, xh, h);
+      if (A.dr) R.write_half(A.dr, t, Xh, h);
       if (has_y) {
-        float2 u[H2], n[H2], g[H2], w1[H2];
-        block(n, u, g, h);
-        get(0, w1, h);
+        float2 y[H2], w[H2];
+        R.read_half(IN_Y, t, y, h);
+        get(0, w, h);
+        if (full) {
+          float2 g[H2];
+          R.read_half(IN_GATE, t, g, h);
+          if (A.dgate) {
+#pragma unroll
+            for (int i = 0; i < H2; ++i) Xh[i] = mul2(mul2(Dh[i], y[i]), mul2(w[i], both(s1)));
+            R.write_half(A.dgate, t, Xh, h);
+          }
+#pragma unroll
+          for (int i = 0; i < H2; ++i) Dh[i] = mul2(Dh[i], g[i]);
+        }
 #pragma unroll
         for (int i = 0; i < H2; ++i) {
-          u[i] = mul2(Dh[i], u[i]);
-          acc[1][h * H2 + i] = add2(acc[1][h * H2 + i], u[i]);
-          const float2 f = mul2(Dh[i], mul2(g[i], both(tok)));
-          acc[0][h * H2 + i] = fma2(f, n[i], acc[0][h * H2 + i]);
-          Dh[i] = mul2(both(s1), fma2(both(-m1), n[i], mul2(f, w1[i])));
+          acc[0][h * H2 + i] = fma2(mul2(Dh[i], y[i]), both(sg), acc[0][h * H2 + i]);
+          Dh[i] = fma2(both(-m1), y[i], mul2(mul2(Dh[i], w[i]), both(sg)));
         }
-        if (A.in[IN_GATE] && A.dgate) R.write_half(A.dgate, t, u, h);
         if (A.dy) R.write_half(A.dy, t, Dh, h);
       }
     }
   }
   if (A.part) {
-    float* part = A.part + (GRP >= CLUSTER ? (long)blockIdx.y : (long)blockIdx.x) * 3 * A.H;
+    float* part = A.part + (GRP >= CLUSTER ? (long)blockIdx.y : (long)blockIdx.x) * 2 * A.H;
     float* ws = (float*)norm_ring;  // [rows of the CTA][H], the slots' copies being done
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
+    for (int k = 0; k < 2; ++k) {
       if (!(A.sums >> k & 1)) continue;
       if constexpr (GRP == WARP) {
         copy_wait<0>();
@@ -549,25 +563,29 @@ k_resnorm_bwd(const __grid_constant__ NormArgs A) {
   if constexpr (GRP >= CLUSTER) cooperative_groups::this_cluster().sync();
 }
 
-// out[k][e] = sum over p of part[p][k][e], in a fixed order: 32 columns and 8 ranges
-// of p a CTA
-__global__ void __launch_bounds__(256)
-k_resnorm_sum(const float* __restrict__ part, int n, int H, float* o0, float* o1, float* o2) {
-  __shared__ float sm[8][32];
-  const int k = blockIdx.y, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  float* out = k == 0 ? o0 : k == 1 ? o1 : o2;
-  if (!out) return;
+// Adds part[p][k][e] over p in a fixed order: 32 columns and 32 ranges of p a CTA; k = 0
+// gives dw_post and a channel gate's gradient, 1 dw_pre.  Starts beside the backward's
+// last CTAs.
+__global__ void __launch_bounds__(1024)
+k_resnorm_sum(const __grid_constant__ NormArgs A, int n, float* dw_post, float* dgate, float* dw_pre) {
+  __shared__ float sm[32][33];
+  const int k = A.sums == 2 ? 1 : blockIdx.y, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int e = blockIdx.x * 32 + lane;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   float s = 0.f;
-  if (e < H)
+  if (e < A.H)
 #pragma unroll 8
-    for (int p = w; p < n; p += 8) s += part[((long)p * 3 + k) * H + e];
+    for (int p = w; p < n; p += 32) s += A.part[((long)p * 2 + k) * A.H + e];
   sm[w][lane] = s;
   __syncthreads();
-  if (w == 0 && e < H) {
-#pragma unroll
-    for (int i = 1; i < 8; ++i) s += sm[i][lane];
-    out[e] = s;
+  s = warp_sum(sm[lane][w]);  // column w
+  const int c = blockIdx.x * 32 + w;
+  if (lane != 0 || c >= A.H) return;
+  if (k == 1) {
+    dw_pre[c] = s;
+  } else {
+    if (dw_post) dw_post[c] = A.gate_kind == LX_GATE_CHANNEL ? s * A.gate[c] : s;
+    if (dgate) dgate[c] = A.w_post ? s * (A.off + A.w_post[c]) : s;
   }
 }
 
@@ -590,10 +608,13 @@ Shape shape_of(int T, int H) {
 
 constexpr int SMS = 152;
 
-// CTAs (clusters) that rows are dealt to: as many as the registers of the SMs hold.  It
-// fixes the backward's workspace, so it does not depend on types or strides.
+// CTAs (clusters) that rows are dealt to: as many as the SMs hold, by their registers
+// (this bounds the backward's workspace) and with `smem` bytes each
 int ctas_per_sm(const Shape& s) { return std::max(1, 65536 / (REGS * s.threads)); }
-long resident(const Shape& s) { return std::min(s.groups, std::max(1L, (long)SMS * ctas_per_sm(s) / s.cols)); }
+int resident(const Shape& s, size_t smem) {
+  const long ctas = std::min<long>(ctas_per_sm(s), std::max<long>(1, 227 * 1024 / (smem + 2048)));
+  return (int)std::min(s.groups, std::max(1L, SMS * ctas / s.cols));
+}
 
 // Slots of a CTA: three rows, or two where three would not fit beside the SM's other CTAs
 size_t ring_bytes(const Shape& s, NormArgs& A, size_t es, size_t more) {
@@ -609,14 +630,13 @@ size_t ring_bytes(const Shape& s, NormArgs& A, size_t es, size_t more) {
 }
 
 template <typename... KArgs>
-lx_status launch(void (*kern)(KArgs...), const Shape& s, size_t smem, const NormArgs& A, cudaStream_t st,
+lx_status launch(void (*kern)(KArgs...), const Shape& s, int groups, size_t smem, const NormArgs& A, cudaStream_t st,
                  bool (&cap)[64]) {
   int dev = 0;
   LX_CUDA(cudaGetDevice(&dev));
   LX_CUDA(smem_cap_once((const void*)kern, 224 * 1024, dev, cap));
   cudaLaunchConfig_t cfg = {};
-  const unsigned groups = (unsigned)resident(s);
-  cfg.gridDim = s.grp >= CLUSTER ? dim3(s.cols, groups) : dim3(groups);
+  cfg.gridDim = s.grp >= CLUSTER ? dim3(s.cols, (unsigned)groups) : dim3((unsigned)groups);
   cfg.blockDim = dim3(s.threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
@@ -631,35 +651,42 @@ lx_status launch(void (*kern)(KArgs...), const Shape& s, size_t smem, const Norm
 }
 
 template <typename T, int VEC, int GRP, bool BWD>
-lx_status launch_one(const Shape& s, NormArgs& A, cudaStream_t st) {
+lx_status launch_one(const Shape& s, NormArgs& A, cudaStream_t st, int& groups) {
   static bool cap[64] = {};
-  const size_t par = BWD ? sizeof(float) * 3 * EPT * s.threads : 0;
+  const size_t par = BWD ? sizeof(float) * 2 * EPT * s.threads : 0;
   size_t smem = 0;
   A.stages = 2;
   if (Rows<T, VEC, GRP>::RING) smem = ring_bytes(s, A, sizeof(T), par);
   A.par_at = (uint32_t)smem;
   smem += par;
   if (BWD && GRP == WARP) smem = std::max(smem, sizeof(float) * (CTA_T / s.lanes) * A.H);
-  if (BWD) return launch(k_resnorm_bwd<T, VEC, GRP>, s, smem, A, st, cap);
-  return launch(k_resnorm_fwd<T, VEC, GRP>, s, smem, A, st, cap);
+  groups = resident(s, smem);
+  // A backward of few rows: a CTA an SM with its rows in flight, as long as that leaves
+  // a CTA under 7 rows: every CTA more writes column sums as large as a row (1031 rows of
+  // 2048 bf16: 152 CTAs 17.6 us, 304 19.2, 608 23.7; 4000 of 2560: 43.9, 36.0, 35.2).
+  // Rows that are read where they are used need all CTAs (1031 of 2047: 69.6, 48.3, 35.7).
+  if (BWD && GRP == CTA && Rows<T, VEC, GRP>::RING) groups = std::min(groups, std::max(SMS, A.T / 7));
+  if (BWD) return launch(k_resnorm_bwd<T, VEC, GRP>, s, groups, smem, A, st, cap);
+  return launch(k_resnorm_fwd<T, VEC, GRP>, s, groups, smem, A, st, cap);
 }
 
 template <typename T, int VEC, bool BWD>
-lx_status launch_vec(const Shape& s, NormArgs& A, cudaStream_t st) {
-  if (s.grp == WARP) return launch_one<T, VEC, WARP, BWD>(s, A, st);
-  if (s.grp == CTA) return launch_one<T, VEC, CTA, BWD>(s, A, st);
-  if (s.grp == CLUSTER) return launch_one<T, VEC, CLUSTER, BWD>(s, A, st);
-  return launch_one<T, VEC, WIDE, BWD>(s, A, st);
+lx_status launch_vec(const Shape& s, NormArgs& A, cudaStream_t st, int& groups) {
+  if (s.grp == WARP) return launch_one<T, VEC, WARP, BWD>(s, A, st, groups);
+  if (s.grp == CTA) return launch_one<T, VEC, CTA, BWD>(s, A, st, groups);
+  if (s.grp == CLUSTER) return launch_one<T, VEC, CLUSTER, BWD>(s, A, st, groups);
+  return launch_one<T, VEC, WIDE, BWD>(s, A, st, groups);
 }
 
-// piece: bytes that divide every row's start and length (16, 4, or 2)
+// piece: bytes that divide every row's start and length (16, 4, or 2); groups: out, the
+// CTAs (clusters) launched
 template <bool BWD>
-lx_status launch_any(int dtype, int piece, const Shape& s, NormArgs& A, cudaStream_t st) {
+lx_status launch_any(int dtype, int piece, const Shape& s, NormArgs& A, cudaStream_t st, int& groups) {
   if (dtype == LX_F32)
-    return piece == 16 ? launch_vec<float, 4, BWD>(s, A, st) : launch_vec<float, 1, BWD>(s, A, st);
-  if (piece == 16) return launch_vec<__nv_bfloat16, 8, BWD>(s, A, st);
-  if (piece == 4) return launch_vec<__nv_bfloat16, 2, BWD>(s, A, st);
-  return launch_vec<__nv_bfloat16, 1, BWD>(s, A, st);
+    return piece == 16 ? launch_vec<float, 4, BWD>(s, A, st, groups) : launch_vec<float, 1, BWD>(s, A, st, groups);
+  if (piece == 16) return launch_vec<__nv_bfloat16, 8, BWD>(s, A, st, groups);
+  if (piece == 4) return launch_vec<__nv_bfloat16, 2, BWD>(s, A, st, groups);
+  return launch_vec<__nv_bfloat16, 1, BWD>(s, A, st, groups);
 }
 
 constexpr int64_t MAX_LD = (1 << 30) - 1;  // elements between rows: a distance in bytes fits 32 bits
@@ -752,7 +779,8 @@ extern "C" lx_status lx_residual_norm(const lx_resnorm_desc* d, void* r_out, voi
   A.r_out = r_out;
   A.h_out = h_out;
   A.stats = stats;
-  return launch_any<false>(d->dtype, pieces(A, es, {r_out, h_out}), s, A, (cudaStream_t)stream);
+  int groups;
+  return launch_any<false>(d->dtype, pieces(A, es, {r_out, h_out}), s, A, (cudaStream_t)stream, groups);
 }
 
 extern "C" lx_status lx_residual_norm_workspace(int32_t T, int32_t H, uint64_t* bytes) {
@@ -760,7 +788,7 @@ extern "C" lx_status lx_residual_norm_workspace(int32_t T, int32_t H, uint64_t* 
   if (!bytes) return fail(LX_ERR_ARG, "bytes is NULL");
   if (T < 0) return fail(LX_ERR_ARG, "T < 0");
   if (H < 1 || H > LX_MAX_WIDTH) return fail(LX_ERR_SHAPE, "H must be in 1..LX_MAX_WIDTH");
-  *bytes = (uint64_t)resident(shape_of(T, H)) * 3 * H * sizeof(float);
+  *bytes = (uint64_t)resident(shape_of(T, H), 0) * 2 * H * sizeof(float);
   return LX_OK;
 }
 
@@ -803,10 +831,9 @@ extern "C" lx_status lx_residual_norm_backward(const lx_resnorm_desc* d, const f
       if (overlap(outs[i], out, outs[j], out)) return fail(LX_ERR_ARG, "two outputs overlap");
   }
   const Shape s = shape_of(d->T, d->H);
-  const long groups = resident(s);
   if (params) {
     if (!workspace || !aligned(workspace, 16)) return fail(LX_ERR_ARG, "workspace is NULL or not 16-byte aligned");
-    if (workspace_bytes < (uint64_t)groups * 3 * d->H * sizeof(float)) return fail(LX_ERR_ARG, "workspace too small");
+    if (workspace_bytes < (uint64_t)resident(s, 0) * 2 * d->H * sizeof(float)) return fail(LX_ERR_ARG, "workspace too small");
   }
   NormArgs A = args_of(d, s);
   if (!dh) A.in[IN_R] = nullptr;  // only the second norm's gradient reads r
@@ -819,11 +846,20 @@ extern "C" lx_status lx_residual_norm_backward(const lx_resnorm_desc* d, const f
   A.dy = dy;
   A.dgate = dgate;
   A.part = params ? (float*)workspace : nullptr;
-  A.sums = (dw_post ? 1 : 0) | (dgc ? 2 : 0) | (dw_pre ? 4 : 0);
-  LX_TRY(launch_any<true>(d->dtype, pieces(A, es, {outs[0], outs[1], outs[2]}), s, A, st));
+  A.sums = (dw_post || dgc ? 1 : 0) | (dw_pre ? 2 : 0);
+  int groups;
+  LX_TRY(launch_any<true>(d->dtype, pieces(A, es, {outs[0], outs[1], outs[2]}), s, A, st, groups));
   if (params) {
-    k_resnorm_sum<<<dim3((d->H + 31) / 32, 3), 256, 0, st>>>(A.part, (int)groups, d->H, dw_post, dgc, dw_pre);
-    LX_CUDA(cudaGetLastError());
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((d->H + 31) / 32, A.sums == 3 ? 2 : 1);
+    cfg.blockDim = dim3(1024);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    LX_CUDA(cudaLaunchKernelEx(&cfg, k_resnorm_sum, A, groups, dw_post, dgc, dw_pre));
   }
   return LX_OK;
 }
