@@ -461,68 +461,77 @@ def compress_member(w_doms, w_mems, omegas, r: int, power_iters: int = 2, worksp
 _DTYPES = {torch.bfloat16: LX_BF16, torch.float32: LX_F32}
 
 
-def _need(ok: bool, msg: str) -> None:
-    if not ok:
-        raise ValueError(msg)
-
-
 def _rows(t: torch.Tensor, name: str, shape=None, dtype=None) -> int:
-    """Checks a matrix of rows (unit stride inside a row) and returns their distance."""
-    _need(t.dim() == 2 and t.is_cuda, f"{name} must be a CUDA matrix")
-    _need(shape is None or t.shape == shape, f"{name} has another shape")
-    _need(dtype is None or t.dtype == dtype, f"{name} has another dtype")
-    ld, inner = t.stride()
+    """Checks a CUDA matrix of rows (unit stride inside a row) and returns their distance."""
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA matrix")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} must have the shape {tuple(shape)}")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} must have the dtype {dtype}")
     T, n = t.shape
-    _need(inner == 1 or n <= 1, f"{name} must have unit stride inside a row")
+    ld, inner = t.stride()
+    if inner != 1 and n > 1:
+        raise ValueError(f"{name} must have unit stride inside a row")
     return ld if T > 1 else max(n, 1)
 
 
 def _flat(t: Optional[torch.Tensor], name: str, n: int, dtype=torch.float32):
-    """Checks a contiguous array of n elements (or None) and returns its address."""
+    """Checks a contiguous CUDA array of n elements (or None) and returns its address."""
     if t is None:
         return None
-    _need(t.is_cuda and t.dtype == dtype and t.numel() == n and t.is_contiguous(),
-          f"{name} must be a contiguous CUDA array of {n} {dtype} elements")
+    if t.dtype != dtype or t.numel() != n or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous CUDA array of {n} {dtype} elements")
     return t.data_ptr()
 
 
-def _run(stream, inputs, call):
-    """call(raw stream) on `stream`, or on the current one when None.  What a call on
-    another stream allocates belongs to that stream; its inputs, and the outputs towards
-    the current stream, are marked as used on both, so that no memory is given away
-    early.  The order of the two streams is the caller's."""
-    if stream is None:
-        return call(torch._C._cuda_getCurrentRawStream(inputs[0].get_device()))
+def _type(t: torch.Tensor, name: str) -> int:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} must be bf16 or fp32")
+    return code
+
+
+def _raw_stream(t: torch.Tensor) -> int:
+    """cudaStream_t of the current stream of the tensor's device."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
+
+
+def _elsewhere(stream, fn, args, kwargs):
+    """fn(*args, **kwargs) with `stream` current.  What it allocates belongs to that
+    stream; its inputs there, and its outputs on the caller's stream, are marked as used,
+    so that no memory is given away early.  The order of the streams is the caller's."""
     here = torch.cuda.current_stream()
-    if stream == here:
-        return call(stream.cuda_stream)
-    for t in inputs:
-        if t is not None:
-            t.record_stream(stream)
     with torch.cuda.stream(stream):
-        out = call(stream.cuda_stream)
-    for t in out:
-        if t is not None:
-            t.record_stream(here)
+        if stream != here:
+            for t in (*args, *kwargs.values()):
+                for u in t if isinstance(t, tuple) else (t,):
+                    if isinstance(u, torch.Tensor) and u.is_cuda:
+                        u.record_stream(stream)
+        out = fn(*args, **kwargs)
+    if stream != here:
+        for t in out if isinstance(out, tuple) else (out,):
+            if t is not None:
+                t.record_stream(here)
     return out
 
 
 def _resnorm_desc(r, y, w_post, gate, w_pre, res_scale, weight_offset, eps) -> ResnormDesc:
     ldr = _rows(r, "r")
     T, H = r.shape
-    _need(r.dtype in _DTYPES, "r must be bf16 or fp32")
+    dtype = r.dtype
     kind = ldy = ldg = 0
     yp = gp = None
     if y is not None:
-        ldy, yp = _rows(y, "y", r.shape, r.dtype), y.data_ptr()
+        ldy, yp = _rows(y, "y", r.shape, dtype), y.data_ptr()
     if gate is not None:
         if gate.dim() == 1:
             kind, gp = LX_GATE_CHANNEL, _flat(gate, "a gate of one dimension", H)
         elif gate.shape == (T, 1) and (H != 1 or gate.dtype == torch.float32):
             kind, ldg, gp = LX_GATE_TOKEN, _rows(gate, "gate", None, torch.float32), gate.data_ptr()
         else:
-            kind, ldg, gp = LX_GATE_FULL, _rows(gate, "gate", r.shape, r.dtype), gate.data_ptr()
-    return ResnormDesc(_DTYPES[r.dtype], T, H, kind, ldr, ldy, ldg, r.data_ptr(), yp, gp,
+            kind, ldg, gp = LX_GATE_FULL, _rows(gate, "gate", r.shape, dtype), gate.data_ptr()
+    return ResnormDesc(_type(r, "r"), T, H, kind, ldr, ldy, ldg, r.data_ptr(), yp, gp,
                        _flat(w_post, "w_post", H), _flat(w_pre, "w_pre", H), res_scale, weight_offset,
                        eps)
 
@@ -541,20 +550,21 @@ def residual_norm(r: torch.Tensor, y: Optional[torch.Tensor] = None, *, w_post=N
     h); h is None without w_pre.  Without y only the norm is taken, and r_out is r
     itself unless res_scale is not 1 or a buffer is given.  ``r_out`` may be r (in
     place).  ``stats``: fp32 [2, T] for residual_norm_backward."""
+    if stream is not None:
+        return _elsewhere(stream, residual_norm, (r, y), dict(
+            w_post=w_post, gate=gate, w_pre=w_pre, res_scale=res_scale, weight_offset=weight_offset,
+            eps=eps, r_out=r_out, h_out=h_out, stats=stats))
     d = _resnorm_desc(r, y, w_post, gate, w_pre, res_scale, weight_offset, eps)
-    n = r.numel()
-    write_r = r_out is not None or y is not None or res_scale != 1.0
-
-    def call(s):
-        ro = None if not write_r else r_out if r_out is not None else torch.empty(
-            r.shape, dtype=r.dtype, device=r.device)
-        h = h_out if h_out is not None or w_pre is None else torch.empty(r.shape, dtype=r.dtype,
-                                                                         device=r.device)
-        _check(lib().lx_residual_norm(d, _flat(ro, "r_out", n, r.dtype), _flat(h, "h_out", n, r.dtype),
-                                      _flat(stats, "stats", 2 * d.T), s))
-        return (ro if write_r else r), h
-
-    return _run(stream, (r, y, w_post, gate, w_pre, stats), call)
+    n, dtype = r.numel(), r.dtype
+    if r_out is None and (y is not None or res_scale != 1.0):
+        r_out = torch.empty(r.shape, dtype=dtype, device=r.device)
+    if h_out is None and w_pre is not None:
+        h_out = torch.empty(r.shape, dtype=dtype, device=r.device)
+    status = lib().lx_residual_norm(d, _flat(r_out, "r_out", n, dtype), _flat(h_out, "h_out", n, dtype),
+                                    _flat(stats, "stats", 2 * d.T), _raw_stream(r))
+    if status:
+        _check(status)
+    return (r if r_out is None else r_out), h_out
 
 
 class ResidualNormGrads(NamedTuple):
@@ -566,10 +576,18 @@ class ResidualNormGrads(NamedTuple):
     dw_pre: Optional[torch.Tensor]
 
 
+def _empty_for(t: Optional[torch.Tensor], shape):
+    """(uninitialised tensor of t's type, its address), or Nones for None."""
+    if t is None:
+        return None, None
+    e = torch.empty(shape, dtype=t.dtype, device=t.device)
+    return e, e.data_ptr()
+
+
 def residual_norm_workspace_bytes(T: int, H: int) -> int:
     b = ctypes.c_uint64()
     _check(lib().lx_residual_norm_workspace(T, H, b))
-    return int(b.value)
+    return b.value
 
 
 def residual_norm_backward(dr_out, dh, r, y, stats, *, w_post=None, gate=None, w_pre=None,
@@ -578,26 +596,31 @@ def residual_norm_backward(dr_out, dh, r, y, stats, *, w_post=None, gate=None, w
     """Gradients of residual_norm with respect to r, y, w_post, gate and w_pre, from
     those of r_out and h (either may be None for zero).  The other arguments are the
     forward's (r as it was before the call) and the stats it wrote."""
+    if stream is not None:
+        return _elsewhere(stream, residual_norm_backward, (dr_out, dh, r, y, stats), dict(
+            w_post=w_post, gate=gate, w_pre=w_pre, res_scale=res_scale, weight_offset=weight_offset,
+            workspace=workspace))
     d = _resnorm_desc(r, y, w_post, gate, w_pre, res_scale, weight_offset, 0.0)
-    T, H = r.shape
-    lddr = 0 if dr_out is None else _rows(dr_out, "dr_out", r.shape, r.dtype)
-    lddh = 0 if dh is None else _rows(dh, "dh", r.shape, r.dtype)
-
-    def call(s):
-        new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=r.device)  # noqa: E731
-        g = ResidualNormGrads(new((T, H), r.dtype), None if y is None else new((T, H), r.dtype),
-                              None if w_post is None else new((H,), torch.float32),
-                              None if gate is None else new(gate.shape, gate.dtype),
-                              None if w_pre is None else new((H,), torch.float32))
-        ws = workspace
-        if ws is None:
-            ws = new(residual_norm_workspace_bytes(T, H), torch.uint8)
-        _check(lib().lx_residual_norm_backward(
-            d, _flat(stats, "stats", 2 * T), _ptr(dr_out), lddr, _ptr(dh), lddh, *[_ptr(t) for t in g],
-            ws.data_ptr(), ws.numel() * ws.element_size(), s))
-        return g
-
-    return _run(stream, (r, dr_out, dh, y, stats, w_post, gate, w_pre, workspace), call)
+    shape, H = r.shape, d.H
+    lddr = lddh = 0
+    drp = dhp = None
+    if dr_out is not None:
+        lddr, drp = _rows(dr_out, "dr_out", shape, r.dtype), dr_out.data_ptr()
+    if dh is not None:
+        lddh, dhp = _rows(dh, "dh", shape, r.dtype), dh.data_ptr()
+    dr, p0 = _empty_for(r, shape)
+    dy, p1 = _empty_for(y, shape)
+    dw_post, p2 = _empty_for(w_post, H)
+    dgate, p3 = _empty_for(gate, None if gate is None else gate.shape)
+    dw_pre, p4 = _empty_for(w_pre, H)
+    if workspace is None:
+        workspace = torch.empty(residual_norm_workspace_bytes(d.T, H), dtype=torch.uint8, device=r.device)
+    status = lib().lx_residual_norm_backward(
+        d, _flat(stats, "stats", 2 * d.T), drp, lddr, dhp, lddh, p0, p1, p2, p3, p4,
+        workspace.data_ptr(), workspace.nbytes, _raw_stream(r))
+    if status:
+        _check(status)
+    return ResidualNormGrads(dr, dy, dw_post, dgate, dw_pre)
 
 
 class RouterBalance(NamedTuple):
@@ -611,17 +634,10 @@ class RouterBalance(NamedTuple):
     lse: torch.Tensor
 
 
-def _mask_ptr(mask, T):
-    if mask is None:
-        return None
-    _need(mask.dtype in (torch.bool, torch.uint8), "mask must be bool or uint8")
-    return _flat(mask, "mask", T, mask.dtype)
-
-
 def router_balance_workspace_bytes(T: int, E: int) -> int:
     b = ctypes.c_uint64()
     _check(lib().lx_router_balance_workspace(T, E, b))
-    return int(b.value)
+    return b.value
 
 
 def router_balance(logits: torch.Tensor, topk_id: torch.Tensor, *, mask=None,
@@ -630,28 +646,32 @@ def router_balance(logits: torch.Tensor, topk_id: torch.Tensor, *, mask=None,
     """Balance loss E sum_e (c_e / (n k)) P_e and z loss mean(lse^2) of the router's
     logits [T, E] (fp32 as Layer.route gives them, or bf16) and its int32 ids [T, k],
     over the tokens whose mask (bool or uint8 [T]) is not 0."""
+    if stream is not None:
+        return _elsewhere(stream, router_balance, (logits, topk_id), dict(
+            mask=mask, balance_coef=balance_coef, z_coef=z_coef, workspace=workspace))
     ld = _rows(logits, "logits")
     T, E = logits.shape
-    _need(logits.dtype in _DTYPES, "logits must be bf16 or fp32")
-    _need(topk_id.dim() == 2 and topk_id.shape[0] == T, "topk_id must be [T, k]")
+    if topk_id.dim() != 2 or topk_id.shape[0] != T:
+        raise ValueError("topk_id must be [T, k]")
     k, dev = topk_id.shape[1], logits.device
     ids = _flat(topk_id, "topk_id", T * k, torch.int32)
-    m = _mask_ptr(mask, T)
-
-    def call(s):
-        f = torch.empty(3 + E + T, dtype=torch.float32, device=dev)
-        loss, prob, lse = f.split((3, E, T))
-        counts = torch.empty(E + 1, dtype=torch.int32, device=dev)
-        ws = workspace
-        if ws is None:
-            ws = torch.empty(router_balance_workspace_bytes(T, E), dtype=torch.uint8, device=dev)
-        p = f.data_ptr()
-        _check(lib().lx_router_balance(_DTYPES[logits.dtype], logits.data_ptr(), ld, ids, m, T, E, k,
-                                       balance_coef, z_coef, counts.data_ptr(), p + 12, p + 12 + 4 * E, p,
-                                       ws.data_ptr(), ws.numel() * ws.element_size(), s))
-        return RouterBalance(loss, counts, prob, lse)
-
-    return _run(stream, (logits, topk_id, mask, workspace), call)
+    if mask is not None:
+        if mask.dtype not in (torch.bool, torch.uint8):
+            raise ValueError("mask must be bool or uint8")
+        mask = _flat(mask, "mask", T, mask.dtype)
+    loss = torch.empty(3, dtype=torch.float32, device=dev)
+    counts = torch.empty(E + 1, dtype=torch.int32, device=dev)
+    prob = torch.empty(E, dtype=torch.float32, device=dev)
+    lse = torch.empty(T, dtype=torch.float32, device=dev)
+    if workspace is None:
+        workspace = torch.empty(router_balance_workspace_bytes(T, E), dtype=torch.uint8, device=dev)
+    status = lib().lx_router_balance(
+        _type(logits, "logits"), logits.data_ptr(), ld, ids, mask, T, E, k, balance_coef, z_coef,
+        counts.data_ptr(), prob.data_ptr(), lse.data_ptr(), loss.data_ptr(), workspace.data_ptr(),
+        workspace.nbytes, _raw_stream(logits))
+    if status:
+        _check(status)
+    return RouterBalance(loss, counts, prob, lse)
 
 
 def router_balance_backward(logits: torch.Tensor, state: RouterBalance, k: int, *, dloss=None,
@@ -661,19 +681,20 @@ def router_balance_backward(logits: torch.Tensor, state: RouterBalance, k: int, 
     times dloss (an fp32 device scalar; 1 when omitted); the counts are held fixed.
     `state` and the coefficients are the forward's, k its ids per token.  ``out`` may
     be the logits themselves."""
+    if stream is not None:
+        return _elsewhere(stream, router_balance_backward, (logits, state, k), dict(
+            dloss=dloss, balance_coef=balance_coef, z_coef=z_coef, out=out))
     ld = _rows(logits, "logits")
     T, E = logits.shape
-    _need(logits.dtype in _DTYPES, "logits must be bf16 or fp32")
-
-    def call(s):
-        d = out if out is not None else torch.empty((T, E), dtype=logits.dtype, device=logits.device)
-        _check(lib().lx_router_balance_backward(
-            _DTYPES[logits.dtype], logits.data_ptr(), ld, _flat(state.lse, "lse", T),
-            _flat(state.counts, "counts", E + 1, torch.int32), _flat(dloss, "dloss", 1), T, E, k,
-            balance_coef, z_coef, _flat(d, "out", T * E, logits.dtype), s))
-        return (d,)
-
-    return _run(stream, (logits, *state, dloss), call)[0]
+    if out is None:
+        out = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
+    status = lib().lx_router_balance_backward(
+        _type(logits, "logits"), logits.data_ptr(), ld, _flat(state.lse, "lse", T),
+        _flat(state.counts, "counts", E + 1, torch.int32), _flat(dloss, "dloss", 1), T, E, k, balance_coef,
+        z_coef, _flat(out, "out", T * E, logits.dtype), _raw_stream(logits))
+    if status:
+        _check(status)
+    return out
 
 
 def distill_loss(logits: torch.Tensor, teacher_id: torch.Tensor, teacher_logit: torch.Tensor, *,
@@ -690,23 +711,30 @@ def distill_loss(logits: torch.Tensor, teacher_id: torch.Tensor, teacher_logit: 
     the entries then keep their share of its whole distribution, otherwise they are
     normalised among themselves.  Returns (loss fp32 [T], gradient of its sum with
     respect to the logits, or None).  ``dlogits`` may be the logits themselves."""
+    if stream is not None:
+        return _elsewhere(stream, distill_loss, (logits, teacher_id, teacher_logit), dict(
+            temperature=temperature, teacher_lse=teacher_lse, kd_weight=kd_weight, labels=labels,
+            ce_weight=ce_weight, row_weight=row_weight, want_grad=want_grad, dlogits=dlogits))
     ld = _rows(logits, "logits")
     T, V = logits.shape
-    _need(logits.dtype in _DTYPES, "logits must be bf16 or fp32")
-    _need(teacher_id.dim() == 2 and teacher_id.shape[0] == T, "teacher_id must be [T, K]")
+    dtype = logits.dtype
+    if teacher_id.dim() != 2 or teacher_id.shape[0] != T:
+        raise ValueError("teacher_id must be [T, K]")
     K, dev = teacher_id.shape[1], logits.device
-    ptrs = (_flat(teacher_id, "teacher_id", T * K, torch.int32),
-            _flat(teacher_logit, "teacher_logit", T * K), _flat(teacher_lse, "teacher_lse", T),
-            _flat(labels, "labels", T, torch.int32), _flat(row_weight, "row_weight", T))
-
-    def call(s):
-        loss = torch.empty(T, dtype=torch.float32, device=dev)
-        d = dlogits
-        if d is None and want_grad:
-            d = torch.empty((T, V), dtype=logits.dtype, device=dev)
-        ldd = 0 if d is None else _rows(d, "dlogits", logits.shape, logits.dtype)
-        _check(lib().lx_distill_loss(_DTYPES[logits.dtype], logits.data_ptr(), ld, *ptrs, T, V, K,
-                                     temperature, kd_weight, ce_weight, loss.data_ptr(), _ptr(d), ldd, s))
-        return loss, d
-
-    return _run(stream, (logits, teacher_id, teacher_logit, teacher_lse, labels, row_weight), call)
+    code = _type(logits, "logits")
+    ids = _flat(teacher_id, "teacher_id", T * K, torch.int32)
+    top = _flat(teacher_logit, "teacher_logit", T * K)
+    loss = torch.empty(T, dtype=torch.float32, device=dev)
+    ldd, dp = V, None
+    if dlogits is not None:
+        ldd, dp = _rows(dlogits, "dlogits", logits.shape, dtype), dlogits.data_ptr()
+    elif want_grad:
+        dlogits = torch.empty((T, V), dtype=dtype, device=dev)
+        dp = dlogits.data_ptr()
+    status = lib().lx_distill_loss(
+        code, logits.data_ptr(), ld, ids, top, _flat(teacher_lse, "teacher_lse", T),
+        _flat(labels, "labels", T, torch.int32), _flat(row_weight, "row_weight", T), T, V, K, temperature,
+        kd_weight, ce_weight, loss.data_ptr(), dp, ldd, _raw_stream(logits))
+    if status:
+        _check(status)
+    return loss, dlogits
