@@ -530,7 +530,7 @@ LX_API lx_status lx_residual_norm_backward(const lx_resnorm_desc* desc, const fl
  *   loss    = balance_coef * balance + z_coef * z   (all 0 when n = 0)
  *   logits: [T][E] (dtype; rows ld apart; lx_route's fp32 logits, or bf16)
  *   topk_id: int32 [T][k];  mask: uint8 [T] or NULL (the logits of a masked token are
- *         not read)
+ *         not used)
  *   counts: int32 [E + 1] out: c_e, then n;  prob: fp32 [E] out: P_e
  *   lse: fp32 [T] out, -inf for a token that does not count
  *   loss: fp32 [3] out: loss, balance, z
