@@ -851,7 +851,8 @@ CallWaits take_call_waits() {
 }  // namespace lx
 
 extern "C" lx_status lx_inject_unmet_wait_call(int32_t site, uint64_t cycles) {
-  if (site != LX_WAIT_NONE && site != LX_WAIT_CALL_PRODUCT && site != LX_WAIT_CALL_JACOBI)
+  if (site != LX_WAIT_NONE && site != LX_WAIT_CALL_PRODUCT && site != LX_WAIT_CALL_JACOBI &&
+      site != LX_WAIT_CALL_SUMS)
     return fail(LX_ERR_ARG, "unknown wait site");
   lx::g_call_waits = lx::CallWaits{};
   lx::g_call_waits.unmet = site;

@@ -10,25 +10,34 @@
 // once.  A CTA (or a cluster of CTAs, where a row is long or rows are few) works on one row
 // at a time.  Its threads hold their part of the row as 16-byte pieces in shared memory,
 // each thread its own (cp.async, no barrier between copy and use).  The first pass over a
-// row sums the exponentials against a running reference, one barrier joins the sums, the
+// row sums the exponentials against a running reference, an exchange joins the sums, the
 // second pass writes the gradient.  The second pass of a row runs together with the first
-// of the next one: a thread finishes a piece, asks for the one AHEAD + (pieces of a row)
-// later in its place, and takes the next row's piece, which was asked for AHEAD pieces
-// ago; reads and writes go on all the time (with the passes one after the other all CTAs
-// drew on memory in the same halves of their rows: 489 us for 4096 rows of 131072 bf16).
-// Rows that do not fit the shared memory of eight CTAs are read a second time from L2.  A
-// warp of its own prepares the teacher's entries a row ahead.  The entries' places are
-// written once more, behind the dense values, by the warp that wrote those; entries of
-// one id add up.
+// of the next one: a thread finishes a batch of pieces, asks for the ones AHEAD + (pieces
+// of a row) later in their place, and takes the next row's batch, which was asked for AHEAD
+// pieces ago; reads and writes go on all the time (with the passes one after the other all
+// CTAs drew on memory in the same halves of their rows).  Rows that do not fit the shared
+// memory of eight CTAs are read a second time from L2.
+//
+// Two warps of their own prepare the teacher's entries, up to four rows ahead, and write the
+// losses: their chains of loads take longer than a row.  The entries' places are written
+// once more, behind the dense values, by the warp that wrote those; entries of one id add
+// up.
+//
+// The roles meet at mbarriers alone: sums_bar when every data warp of the row's CTAs has
+// sent its partial sums (to every CTA: a barrier of the whole cluster would also wait for
+// the stores under way), ready_bar when a row's entries are prepared, result_bar when its
+// sums are known, released_bar when the data warps are done with its entries.  Every wait is
+// bounded; one that gives up makes the row's loss and gradient NaN, and the CTA waits no
+// more.
 //
 // The reference of a sum is a whole number n of powers of two: exp(z / tau) is taken as
-// 2^n 2^(z log2(e) / tau - n), one fused multiply-add from z, exact in n, and partial sums
-// are joined by powers of two without rounding.  A row whose every logit lies below -2^30
-// powers of two sums to zero against the lowest reference and is done again with its
-// maximum subtracted first.
+// 2^n 2^(z log2(e) / tau - n), one fused multiply-add from z, exact in n.  A row whose every
+// logit lies below -2^30 powers of two sums to zero against the lowest reference and is done
+// again with its maximum subtracted first.
 #include <algorithm>
 
 #include "lx_rows.cuh"
+#include "lx_tcgen05.cuh"
 
 namespace lx {
 namespace {
@@ -36,12 +45,14 @@ namespace {
 using namespace rows;
 
 constexpr int SMS = 152;
-constexpr int MAX_WARPS = 16;      // data warps of a CTA
+constexpr int MAX_WARPS = 16;    // data warps of a CTA
+constexpr int TEACHERS = 2;      // warps that prepare entries
+constexpr int BUFS = 4;          // rows whose entries are held, a multiple of TEACHERS
 constexpr int MAX_CLUSTER = 8;
-constexpr int SMEM = 222 * 1024;   // dynamic shared memory of a CTA at most
-constexpr int U = 2;               // pieces of a thread taken together
-constexpr int AHEAD = 8;           // pieces asked for before they are used, a multiple of U
-constexpr int REGS = 112;          // registers a thread: the launch bound holds the compiler to it
+constexpr int SMEM = 222 * 1024; // dynamic shared memory of a CTA at most
+constexpr int U = 2;             // pieces of a thread taken together
+constexpr int AHEAD = 8;         // pieces asked for before they are used, a multiple of U
+constexpr int REGS = 96;         // registers a thread: the launch bound holds the compiler to it
 constexpr float LOWEST = -1073741824.f;  // -2^30
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
@@ -58,9 +69,12 @@ struct DistillArgs {
   float* loss;
   void* dlogits;
   long ldd;
-  int slice;  // columns of a CTA
-  int rounds; // pieces of a thread, rounded up to a multiple of U
-  int slots;  // of them in shared memory at a time, a multiple of U
+  int slice;   // columns of a CTA
+  int table;   // places of a table of ids, a power of two
+  int rounds;  // pieces of a thread, rounded up to a multiple of U
+  int slots;   // of them in shared memory at a time, a multiple of U
+  unsigned long long wait_cycles;
+  int unmet;   // test hook: the sums' barrier waits for what nobody sends
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -80,10 +94,16 @@ __device__ __forceinline__ void join(float& n, float& s, float on, float os) {
   s = s * ex2(n - N) + os * ex2(on - N);
   n = N;
 }
-template <bool TWO>
-__device__ __forceinline__ void join(Run& r, float4 o) {
-  join(r.n, r.s, o.x, o.y);
-  if (TWO) join(r.n1, r.s1, o.z, o.w);
+__device__ __forceinline__ float warp_max(float x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+  return x;
+}
+// over the lanes of a warp; the same in each
+__device__ __forceinline__ void join_warp(float& n, float& s) {
+  const float N = warp_max(n);
+  s = warp_sum(s * ex2(n - N));
+  n = N;
 }
 
 // A row part: elements before its first 16-byte boundary, 16-byte pieces, the rest
@@ -114,6 +134,19 @@ __device__ __forceinline__ void unpack(uint4 w, float2* v) {
   }
 }
 template <typename T>
+__device__ __forceinline__ uint4 pack(const float2* v) {
+  if constexpr (sizeof(T) == 4)
+    return make_uint4(__float_as_uint(v[0].x), __float_as_uint(v[0].y), __float_as_uint(v[1].x), __float_as_uint(v[1].y));
+  else
+    return make_uint4(to_bf2(v[0]), to_bf2(v[1]), to_bf2(v[2]), to_bf2(v[3]));
+}
+// a piece of -inf, which adds nothing
+template <typename T>
+__device__ __forceinline__ uint4 no_piece() {
+  const uint32_t w = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+  return make_uint4(w, w, w, w);
+}
+template <typename T>
 __device__ __forceinline__ float piece_max(uint4 w) {  // a NaN is left out: it shows in the sums
   if constexpr (sizeof(T) == 4) {
     return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
@@ -124,9 +157,8 @@ __device__ __forceinline__ float piece_max(uint4 w) {  // a NaN is left out: it 
   }
 }
 
-// Adds the U pieces at q (those with `have` set) to sums p against reference n.  While the
-// values lie less than 2^40 above the reference no maximum is needed; then it is raised
-// to the pieces' maximum.
+// Adds U pieces to sums p against reference n.  While the values lie less than 2^40 above
+// the reference no maximum is needed; then it is raised to the pieces' maximum.
 template <typename T>
 __device__ __forceinline__ void add_pieces(float& n, float2& p, const uint4* q, float c) {
   constexpr int N2 = 8 / sizeof(T);
@@ -165,399 +197,457 @@ __device__ __forceinline__ void add_value(float& n, float2& p, float v, float c)
   p.x += ex2(fmaf(v, c, -n));
 }
 
+// What a row's sums came to.  `again`: the sums are of the values less `top`.
+struct Result {
+  float n, s, n1, s1, top;
+  bool again;
+  __device__ float rel(float z, float ct) const { return again ? (z - top) * ct : fmaf(z, ct, -n); }
+  __device__ float rel1(float z) const { return again ? (z - top) * LOG2E : fmaf(z, LOG2E, -n1); }
+};
+
 extern __shared__ uint4 distill_smem[];
 
 // TWO: a hard-label term at another temperature than the teacher's.  HELD: rows fit shared
-// memory.  blockDim: the data threads and one warp more, which prepares the entries;
-// gridDim: (CTAs of a row, rows)
+// memory.  blockDim: the data threads and the TEACHERS' warps; gridDim: (CTAs of a row,
+// rows)
 template <typename T, bool TWO, bool CL, bool HELD>
 __global__ void __launch_bounds__(576, 1)
 k_distill(const __grid_constant__ DistillArgs A) {
   constexpr int N = Span<T>::N, N2 = N / 2;
-  __shared__ float4 red[2][CL ? MAX_CLUSTER : 1][MAX_WARPS];
-  __shared__ float msum[2];
-  const int D = blockDim.x - 32, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = D >> 5;
-  const bool teacher = warp == nw, grad = A.dlogits != nullptr;
+  __shared__ float4 red[2][CL ? MAX_CLUSTER : 1][MAX_WARPS];  // the warps' sums
+  __shared__ Result res[BUFS];
+  __shared__ float msum[BUFS];
+  __shared__ int repeats[BUFS];  // whether an id occurs twice
+  __shared__ uint64_t sums_bar[2], ready_bar[BUFS], result_bar[BUFS], released_bar[BUFS];
+  __shared__ volatile int gave_up;
+  const int D = blockDim.x - 32 * TEACHERS, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = D >> 5;
+  const bool teacher = warp >= nw;
   const int E1 = A.K + 1, rank = CL ? blockIdx.x : 0, cols = CL ? gridDim.x : 1;
-  // entries of the row and of the next: id, z, q, log q; entry K is the label
-  int* eid = (int*)distill_smem;
-  float* ez = (float*)distill_smem + 2 * E1;
-  float* eq = ez + 2 * E1;
-  float* elq = eq + 2 * E1;
-  const uint4* slot = distill_smem + (8 * E1 + 3) / 4 + tid;  // slot k at slot[k * D]
-  const uint32_t slot_at = (uint32_t)__cvta_generic_to_shared(slot);
-  const int v0 = rank * A.slice, vn = min(A.slice, A.V - v0);
+  // entries of BUFS rows: id, z, q, log q; entry K is the label
+  int* const eid = (int*)distill_smem;
+  float* const ez = (float*)distill_smem + BUFS * E1;
+  float* const eq = ez + BUFS * E1;
+  float* const elq = eq + BUFS * E1;
   const float ct = A.ct;
   const long first = blockIdx.y, step = gridDim.y;
   auto weight = [&](long t) { return t >= A.T ? 0.f : A.weight ? A.weight[t] : 1.f; };
-  auto span = [&](long t) { return Span<T>((const T*)A.logits + (t < A.T ? t : first) * A.ld + v0, vn); };
-  // the copies, U pieces a group, in the order of use: rows of weight 0 and pieces that a
-  // thread does not have leave their slots as they are
-  auto mine = [&](const Span<T>& S) { return (S.pieces - tid + D - 1) / D; };
-  long ask_t = first;
-  float ask_wn = weight(first);
-  const T* ask_at = nullptr;
-  int ask_left = 0, ask_rounds = 0;  // pieces of the thread, rounds of the row not asked for yet
-  auto ask = [&](uint32_t to) {
-    if (ask_rounds == 0) {
-      const Span<T> S = span(ask_t);
-      ask_at = S.piece(tid);
-      ask_left = ask_wn != 0.f ? mine(S) : 0;
-      ask_rounds = A.rounds;
-      ask_t += step;
-      ask_wn = weight(ask_t);
+
+  auto bar = [](uint64_t* b) { return (uint32_t)__cvta_generic_to_shared(b); };
+  if (tid == 0) {
+    gave_up = 0;
+    for (int i = 0; i < 2; ++i) tcg::mbar_init(bar(&sums_bar[i]), CL ? 1 : nw);
+    for (int i = 0; i < BUFS; ++i) {
+      tcg::mbar_init(bar(&ready_bar[i]), 1);
+      tcg::mbar_init(bar(&result_bar[i]), 1);
+      tcg::mbar_init(bar(&released_bar[i]), nw);
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (u < ask_left)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(slot_at + to + u * D * 16), "l"(ask_at + (long)u * D * N)
-                     : "memory");
-    asm volatile("cp.async.commit_group;" ::: "memory");
-    ask_at += (long)U * D * N;
-    ask_left -= U;
-    ask_rounds -= U;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  if constexpr (CL) cooperative_groups::this_cluster().sync();  // all have started
+  bool lost = false;  // a wait of this thread gave up
+  auto wait = [&](uint64_t* b, uint32_t parity) {
+    if (lost) return;
+    if (gave_up || !tcg::mbar_wait(bar(b), parity, &gave_up, A.wait_cycles)) {
+      lost = true;
+      gave_up = 1;
+    }
   };
-  const uint32_t batch = U * D * 16, ring = A.slots * D * 16;  // bytes
-  auto advance = [&](uint32_t& k) { k = k + batch == ring ? 0 : k + batch; };
-  // U pieces from slot offset k, -inf (which adds nothing) where the thread has fewer
-  auto fetch = [&](uint32_t k, int have, uint4* q) {
-    const uint32_t none = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      q[u] = u < have ? *(const uint4*)((const char*)slot + k + u * D * 16) : make_uint4(none, none, none, none);
-  };
-  // the CTAs of the row meet
-  auto meet = [&] {
-    if constexpr (CL) cooperative_groups::this_cluster().sync();
-    else __syncthreads();
-  };
-  // joins the threads' sums over the row; the same in every thread (the teacher's too)
-  int turn = 0;
-  auto joined = [&](Run r) {
-    r.s += r.p.x + r.p.y;
-    if (TWO) r.s1 += r.p1.x + r.p1.y;
-    if (!teacher) {
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1)
-        join<TWO>(r, make_float4(__shfl_xor_sync(0xffffffffu, r.n, o), __shfl_xor_sync(0xffffffffu, r.s, o),
-                                 TWO ? __shfl_xor_sync(0xffffffffu, r.n1, o) : 0.f,
-                                 TWO ? __shfl_xor_sync(0xffffffffu, r.s1, o) : 0.f));
-      const float4 mine = make_float4(r.n, r.s, r.n1, r.s1);
-      if constexpr (CL) {
-        if (lane < cols) *cooperative_groups::this_cluster().map_shared_rank(&red[turn][rank][warp], lane) = mine;
-      } else {
-        if (lane == 0) red[turn][0][warp] = mine;
+
+  if (teacher) {
+    // Row k of the CTA's (h, h + TEACHERS, ... are this warp's) has its entries in buffer
+    // k % BUFS.
+    const int h = warp - nw;
+    int* table = (int*)(elq + BUFS * E1) + h * A.table;
+    auto prepare = [&](long t, int b) {
+      if (weight(t) == 0.f) return;
+      int* id = eid + b * E1;
+      float *z = ez + b * E1, *q = eq + b * E1, *lq = elq + b * E1;
+      const T* row = (const T*)A.logits + t * A.ld;
+      for (int i = lane; i < A.table; i += 32) table[i] = -1;
+      __syncwarp();
+      float tm = -INFINITY;
+      bool twice = false;
+      for (int j = lane; j < A.K; j += 32) {
+        const int e = A.ids[t * A.K + j];
+        const bool ok = e >= 0 && e < A.V;
+        const float v = ok ? A.top[t * A.K + j] : -INFINITY;
+        id[j] = ok ? e : -1;
+        z[j] = ok ? to_f32(row[e]) : 0.f;
+        q[j] = v;
+        tm = fmaxf(tm, v);
+        if (ok)  // at least half of the places stay free
+          for (int i = e;; ++i) {
+            const int was = atomicCAS(&table[i & (A.table - 1)], -1, e);
+            twice |= was == e;
+            if (was == -1 || was == e) break;
+          }
       }
+      twice = __any_sync(0xffffffffu, twice);
+      if (lane == 0) {
+        const int e = A.labels ? A.labels[t] : -1;
+        const bool ok = e >= 0 && e < A.V;
+        id[A.K] = ok ? e : -1;
+        z[A.K] = ok ? to_f32(row[e]) : 0.f;
+        q[A.K] = 0.f;
+        repeats[b] = twice;
+      }
+      tm = warp_max(tm);
+      float lz;  // log of the distribution's sum, relative to tm / tau
+      if (A.top_lse) {
+        lz = A.top_lse[t] - tm / A.tau;
+      } else {
+        float s = 0.f;
+        for (int j = lane; j < A.K; j += 32)
+          if (id[j] >= 0) s += tm == -INFINITY ? 0.f : expf((q[j] - tm) / A.tau);
+        lz = logf(warp_sum(s));
+      }
+      float m = 0.f;
+      for (int j = lane; j < A.K; j += 32) {
+        const float l = id[j] >= 0 && q[j] != -INFINITY ? (q[j] - tm) / A.tau - lz : -INFINITY;
+        const float p = expf(l);
+        lq[j] = l;
+        q[j] = p;
+        m += p;
+      }
+      m = warp_sum(m);
+      if (lane == 0) msum[b] = m;
+    };
+    auto provide = [&](long k) {
+      const long t = first + k * step;
+      if (t >= A.T) return;
+      if (k >= BUFS) wait(&released_bar[k % BUFS], (uint32_t)(k / BUFS - 1) & 1);
+      if (!__any_sync(0xffffffffu, lost)) prepare(t, (int)(k % BUFS));
+      __syncwarp();
+      if (lane == 0) tcg::mbar_arrive(bar(&ready_bar[k % BUFS]));
+    };
+    for (long k = h; k < BUFS; k += TEACHERS) provide(k);
+    for (long k = h; first + k * step < A.T; k += TEACHERS) {
+      const long t = first + k * step;
+      const int b = (int)(k % BUFS);
+      wait(&result_bar[b], (uint32_t)(k / BUFS) & 1);
+      const float w = weight(t);
+      const Result r = res[b];
+      const int* id = eid + b * E1;
+      const float *zj = ez + b * E1, *q = eq + b * E1, *lq = elq + b * E1;
+      float loss = 0.f;
+      if (w != 0.f && r.s != 0.f) {
+        const float ls = logf(r.s);
+        for (int j = lane; j < A.K; j += 32)
+          if (q[j] != 0.f) loss += q[j] * (lq[j] - (r.rel(zj[j], ct) * LN2 - ls));
+        loss = warp_sum(loss) * A.a * A.tau * A.tau;
+        if (A.b != 0.f && id[A.K] >= 0)
+          loss += A.b * (logf(r.s1) - (TWO ? r.rel1(zj[A.K]) : r.rel(zj[A.K], ct)) * LN2);
+        loss *= w;
+      }
+      if (__any_sync(0xffffffffu, lost)) loss = NAN;
+      if (lane == 0 && rank == 0) A.loss[t] = loss;
+      __syncwarp();
+      provide(k + BUFS);
     }
-    meet();
-    r = Run();
-    for (int i = lane; i < cols * MAX_WARPS; i += 32)
-      if ((i & (MAX_WARPS - 1)) < nw) join<TWO>(r, red[turn][i / MAX_WARPS][i & (MAX_WARPS - 1)]);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-      join<TWO>(r, make_float4(__shfl_xor_sync(0xffffffffu, r.n, o), __shfl_xor_sync(0xffffffffu, r.s, o),
-                               TWO ? __shfl_xor_sync(0xffffffffu, r.n1, o) : 0.f,
-                               TWO ? __shfl_xor_sync(0xffffffffu, r.s1, o) : 0.f));
-    turn ^= 1;
-    return r;
-  };
+  } else {
+    const int v0 = rank * A.slice, vn = min(A.slice, A.V - v0);
+    const char* const slot = (const char*)(distill_smem + (4 * BUFS * E1 + TEACHERS * A.table + 3) / 4 + tid);
+    const uint32_t slot_at = (uint32_t)__cvta_generic_to_shared(slot);
+    const uint32_t apart = D * 16, batch = U * apart, ring = A.slots * apart;  // bytes between a thread's pieces
+    auto advance = [&](uint32_t& k) { k = k + batch == ring ? 0 : k + batch; };
+    auto span = [&](long t) { return Span<T>((const T*)A.logits + (t < A.T ? t : first) * A.ld + v0, vn); };
+    auto pieces_of = [&](const Span<T>& S) { return (S.pieces - tid + D - 1) / D; };  // of this thread
 
-  // the teacher's entries of row t into half `half`
-  auto prepare = [&](long t, int half) {
-    if (weight(t) == 0.f) return;
-    int* id = eid + half * E1;
-    float *z = ez + half * E1, *q = eq + half * E1, *lq = elq + half * E1;
-    const T* row = (const T*)A.logits + t * A.ld;
-    float tm = -INFINITY;
-    for (int j = lane; j < A.K; j += 32) {
-      const int e = A.ids[t * A.K + j];
-      const bool ok = e >= 0 && e < A.V;
-      const float v = ok ? A.top[t * A.K + j] : -INFINITY;
-      id[j] = ok ? e : -1;
-      z[j] = ok ? to_f32(row[e]) : 0.f;
-      q[j] = v;
-      tm = fmaxf(tm, v);
-    }
-    if (lane == 0) {
-      const int e = A.labels ? A.labels[t] : -1;
-      const bool ok = e >= 0 && e < A.V;
-      id[A.K] = ok ? e : -1;
-      z[A.K] = ok ? to_f32(row[e]) : 0.f;
-      q[A.K] = 0.f;
-    }
+    // The copies, a batch to a group, in the order of use: rows of weight 0 and pieces that
+    // a thread does not have leave their slots as they are.
+    long ask_t = first;
+    float ask_w = weight(first);
+    const T* ask_at = nullptr;
+    int ask_left = 0, ask_rounds = 0;  // pieces of the thread, rounds of the row not asked for yet
+    auto ask = [&](uint32_t to) {
+      if (ask_rounds == 0) {
+        const Span<T> S = span(ask_t);
+        ask_at = S.piece(tid);
+        ask_left = ask_w != 0.f ? pieces_of(S) : 0;
+        ask_rounds = A.rounds;
+        ask_t += step;
+        ask_w = weight(ask_t);
+      }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) tm = fmaxf(tm, __shfl_xor_sync(0xffffffffu, tm, o));
-    float lz;  // log of the distribution's sum, relative to tm / tau
-    if (A.top_lse) {
-      lz = A.top_lse[t] - tm / A.tau;
-    } else {
-      float s = 0.f;
-      for (int j = lane; j < A.K; j += 32)
-        if (id[j] >= 0) s += tm == -INFINITY ? 0.f : expf((q[j] - tm) / A.tau);
-      lz = logf(warp_sum(s));
-    }
-    float m = 0.f;
-    for (int j = lane; j < A.K; j += 32) {
-      const float l = id[j] >= 0 && q[j] != -INFINITY ? (q[j] - tm) / A.tau - lz : -INFINITY;
-      const float p = expf(l);
-      lq[j] = l;
-      q[j] = p;
-      m += p;
-    }
-    m = warp_sum(m);
-    if (lane == 0) msum[half] = m;
-  };
+      for (int u = 0; u < U; ++u)
+        if (u < ask_left)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(slot_at + to + u * apart),
+                       "l"(ask_at + (long)u * D * N)
+                       : "memory");
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      ask_at += (long)U * D * N;
+      ask_left -= U;
+      ask_rounds -= U;
+    };
+    auto landed = [] { asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD / U) : "memory"); };
 
-  // the first pass: U pieces of the thread into the sums
-  auto take = [&](Run& r, const uint4* q) {
-    add_pieces<T>(r.n, r.p, q, ct);
-    if (TWO) add_pieces<T>(r.n1, r.p1, q, LOG2E);
-  };
-  auto take_edge = [&](Run& r, float v) {
-    add_value(r.n, r.p, v, ct);
-    if (TWO) add_value(r.n1, r.p1, v, LOG2E);
-  };
-  auto landed = [] { asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD / U) : "memory"); };
-  uint32_t k0 = 0, k1 = 0;  // slot offsets of the copies and of the first pass
-  // the first pass of a whole row by itself: the first row, and every row without gradient
-  auto pass1 = [&](const Span<T>& S, float w, Run& r) {
-    const int n = w != 0.f ? mine(S) : 0;
-    uint4 q[U];
-    if constexpr (HELD) {
-      for (int p = 0; p < A.rounds; p += U) {
-        ask(k0);
-        advance(k0);
-        landed();
-        if (p < n) {
-          fetch(k1, n - p, q);
+    // The first pass: a batch of the thread's pieces, of which it has `have`, into the sums
+    auto take = [&](Run& r, const uint4* q) {
+      add_pieces<T>(r.n, r.p, q, ct);
+      if (TWO) add_pieces<T>(r.n1, r.p1, q, LOG2E);
+    };
+    auto take_edge = [&](Run& r, float v) {
+      add_value(r.n, r.p, v, ct);
+      if (TWO) add_value(r.n1, r.p1, v, LOG2E);
+    };
+    auto take_slots = [&](Run& r, uint32_t k, int have) {
+      uint4 q[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) q[u] = u < have ? *(const uint4*)(slot + k + u * apart) : no_piece<T>();
+      take(r, q);
+    };
+    uint32_t k0 = 0, k1 = 0, k2 = 0;  // slots of the copies, of the first and of the second pass
+    // of a whole row by itself: the first row, and every row where there is no gradient
+    auto pass1 = [&](const Span<T>& S, float w, Run& r) {
+      const int n = w != 0.f ? pieces_of(S) : 0;
+      if constexpr (HELD) {
+        for (int p = 0; p < A.rounds; p += U) {
+          ask(k0);
+          advance(k0);
+          landed();
+          if (p < n) take_slots(r, k1, n - p);
+          advance(k1);
+        }
+      } else {
+        for (int p = 0; p < n; p += U) {
+          uint4 q[U];
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+            q[u] = p + u < n ? *(const uint4*)S.piece((p + u) * D + tid) : no_piece<T>();
           take(r, q);
         }
-        advance(k1);
       }
-    } else {
-      const uint32_t none = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
-      for (int p = 0; p < n; p += U) {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-          q[u] = p + u < n ? *(const uint4*)S.piece((p + u) * D + tid) : make_uint4(none, none, none, none);
-        take(r, q);
-      }
-    }
-    if (w != 0.f && tid < S.edges) take_edge(r, to_f32(S.row[S.edge(tid)]));
-  };
+      if (w != 0.f && tid < S.edges) take_edge(r, to_f32(S.row[S.edge(tid)]));
+    };
 
-  float w = weight(first), wn = weight(first + step);
-  Run r;
-  if (teacher) {
-    prepare(first, 0);
-  } else {
+    // Every data warp's v of the row's CTAs, in red[]; returns which half
+    int sent = 0;
+    auto exchange = [&](float4 v) {
+      const int turn = sent & 1;
+      if (__any_sync(0xffffffffu, lost)) return turn;
+      if constexpr (CL) {
+        if (tid == 0) tcg::mbar_expect_tx(bar(&sums_bar[turn]), cols * nw * 16 + (A.unmet ? 16 : 0));
+        if (lane < cols) {
+          uint32_t to, at;
+          asm("mapa.shared::cluster.u32 %0, %1, %2;"
+              : "=r"(to)
+              : "r"((uint32_t)__cvta_generic_to_shared(&red[turn][rank][warp])), "r"(lane));
+          asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(bar(&sums_bar[turn])), "r"(lane));
+          asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(
+                           to),
+                       "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w), "r"(at)
+                       : "memory");
+        }
+      } else if (lane == 0) {
+        red[turn][0][warp] = v;
+        if (!(A.unmet && warp == 0)) tcg::mbar_arrive(bar(&sums_bar[turn]));
+      }
+      __syncwarp();
+      wait(&sums_bar[turn], (sent >> 1) & 1);
+      ++sent;
+      return turn;
+    };
+    // The threads' sums over the row, the same in every data thread
+    auto joined = [&](Run r) {
+      r.s += r.p.x + r.p.y;
+      join_warp(r.n, r.s);
+      if (TWO) {
+        r.s1 += r.p1.x + r.p1.y;
+        join_warp(r.n1, r.s1);
+      }
+      const int turn = exchange(make_float4(r.n, r.s, r.n1, r.s1));
+      r = Run();
+      for (int i = lane; i < cols * MAX_WARPS; i += 32)
+        if ((i & (MAX_WARPS - 1)) < nw) {
+          const float4 o = red[turn][i / MAX_WARPS][i & (MAX_WARPS - 1)];
+          join(r.n, r.s, o.x, o.y);
+          if (TWO) join(r.n1, r.s1, o.z, o.w);
+        }
+      join_warp(r.n, r.s);
+      if (TWO) join_warp(r.n1, r.s1);
+      if (__any_sync(0xffffffffu, lost)) r.s = r.s1 = NAN;
+      return r;
+    };
+
+    float w = weight(first), wn = weight(first + step);
+    Run run;  // the sums of row t
     if constexpr (HELD)
       for (int p = 0; p < AHEAD; p += U) {
         ask(k0);
         advance(k0);
       }
-    pass1(span(first), w, r);
-  }
-  if constexpr (CL) cooperative_groups::this_cluster().sync();  // all have started
-  int half = 0;
-  uint32_t k2 = 0;  // slot offset of the second pass
-  for (long t = first; t < A.T; t += step, half ^= 1) {
-    const Span<T> S = span(t), Sn = span(t + step);
-    const float wn2 = weight(t + 2 * step);
-    bool slow = false, dead = w == 0.f;  // dead: nothing to learn
-    float top = 0.f;                     // slow: the row's maximum
-    if (!dead) {
-      r = joined(r);
-      if (r.s == 0.f) {  // every logit is -inf or out of the references' reach
-        slow = true;
-        top = -INFINITY;
-        if (!teacher) {
+    pass1(span(first), w, run);
+    long k = 0;  // the CTA's rows
+    for (long t = first; t < A.T; t += step, ++k) {
+      const Span<T> S = span(t), Sn = span(t + step);
+      const float wn2 = weight(t + 2 * step);
+      const int b = (int)(k % BUFS);
+      bool dead = w == 0.f;  // nothing to learn
+      Result r = {0.f, 0.f, 0.f, 0.f, 0.f, false};
+      wait(&ready_bar[b], (uint32_t)(k / BUFS) & 1);
+      if (!dead) {
+        run = joined(run);
+        if (run.s == 0.f) {  // every logit is -inf or out of the references' reach
+          r.again = true;
+          float top = -INFINITY;
           for (int i = tid; i < S.pieces; i += D) top = fmaxf(top, piece_max<T>(*(const uint4*)S.piece(i)));
           if (tid < S.edges) top = fmaxf(top, to_f32(S.row[S.edge(tid)]));
-        }
-        auto max_of = [&](float x) {
-#pragma unroll
-          for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
-          return x;
-        };
-        top = max_of(top);
-        if (!teacher) {
-          if constexpr (CL) {
-            if (lane < cols) cooperative_groups::this_cluster().map_shared_rank(&red[turn][rank][warp], lane)->x = top;
-          } else {
-            if (lane == 0) red[turn][0][warp].x = top;
-          }
-        }
-        meet();
-        top = -INFINITY;
-        for (int i = lane; i < cols * MAX_WARPS; i += 32)
-          if ((i & (MAX_WARPS - 1)) < nw) top = fmaxf(top, red[turn][i / MAX_WARPS][i & (MAX_WARPS - 1)].x);
-        top = max_of(top);
-        turn ^= 1;
-        dead = top == -INFINITY;
-        if (!dead) {
-          r = Run();
-          r.n = r.n1 = 0.f;
-          if (!teacher) {
+          const int turn = exchange(make_float4(warp_max(top), 0.f, 0.f, 0.f));
+          top = -INFINITY;
+          for (int i = lane; i < cols * MAX_WARPS; i += 32)
+            if ((i & (MAX_WARPS - 1)) < nw) top = fmaxf(top, red[turn][i / MAX_WARPS][i & (MAX_WARPS - 1)].x);
+          r.top = top = warp_max(top);
+          dead = top == -INFINITY;
+          if (!dead) {
+            run = Run();
+            run.n = run.n1 = 0.f;
             auto add = [&](float v) {
-              r.s += ex2((v - top) * ct);
-              if (TWO) r.s1 += ex2((v - top) * LOG2E);
+              run.s += ex2((v - top) * ct);
+              if (TWO) run.s1 += ex2((v - top) * LOG2E);
             };
             for (int i = tid; i < S.pieces * N; i += D) add(to_f32(S.row[S.head + i]));
             if (tid < S.edges) add(to_f32(S.row[S.edge(tid)]));
+            run = joined(run);
           }
-          r = joined(r);
         }
+        r.n = run.n;
+        r.s = dead ? 0.f : run.s;
+        r.n1 = TWO ? run.n1 : run.n;
+        r.s1 = TWO ? run.s1 : run.s;
       }
-      if (!TWO) r.n1 = r.n, r.s1 = r.s;
-    } else {
-      __syncthreads();  // the entries' other half is free for the teacher's warp
-    }
-    // z relative to the references, in powers of two
-    auto rel = [&](float z) { return slow ? (z - top) * ct : fmaf(z, ct, -r.n); };
-    auto rel1 = [&](float z) { return slow ? (z - top) * LOG2E : fmaf(z, LOG2E, -r.n1); };
-    const int* id = eid + half * E1;
-    const float *zj = ez + half * E1, *q = eq + half * E1, *lq = elq + half * E1;
-    Run rn;  // the next row's sums
-    if (teacher) {
-      float loss = 0.f;
-      if (!dead) {
-        const float ls = logf(r.s);
-        for (int j = lane; j < A.K; j += 32)
-          if (q[j] != 0.f) loss += q[j] * (lq[j] - (rel(zj[j]) * LN2 - ls));
-        loss = warp_sum(loss) * A.a * A.tau * A.tau;
-        if (A.b != 0.f && id[A.K] >= 0) loss += A.b * (logf(r.s1) - (TWO ? rel1(zj[A.K]) : rel(zj[A.K])) * LN2);
-        loss *= w;
+      if (tid == 0) {
+        res[b] = r;
+        tcg::mbar_arrive(bar(&result_bar[b]));
       }
-      if (lane == 0 && rank == 0) A.loss[t] = loss;
-      if (t + step < A.T) prepare(t + step, half ^ 1);
-    } else if (!grad) {
-      if (t + step < A.T) pass1(Sn, wn, rn);
-    } else {
-      T* dz = (T*)A.dlogits + t * A.ldd + v0;
-      const bool same = (((uintptr_t)dz ^ (uintptr_t)S.row) & 15) == 0;
-      const int label = dead ? -1 : id[A.K];
-      const float qa = dead ? 0.f : w * A.a * A.tau;
-      const float hb = dead || label < 0 ? 0.f : w * A.b;
-      const float pa = dead ? 0.f : qa * msum[half] / r.s, pb = dead ? 0.f : hb / r.s1;
-      auto value = [&](float z) {
-        if (dead) return 0.f;
-        return TWO ? pa * ex2(rel(z)) + pb * ex2(rel1(z)) : (pa + pb) * ex2(rel(z));
-      };
-      const float2 pa2 = both(TWO ? pa : pa + pb), pb2 = both(pb), nn = both(-r.n), nn1 = both(-r.n1);
-      auto gradient = [&](uint4 w4) {
-        float2 v[N2];
-        unpack<T>(w4, v);
-#pragma unroll
-        for (int j = 0; j < N2; ++j) {
-          const float2 x = fma2(v[j], both(ct), nn);
-          float2 o = mul2(make_float2(ex2(x.x), ex2(x.y)), pa2);
-          if (TWO) {
-            const float2 x1 = fma2(v[j], both(LOG2E), nn1);
-            o = fma2(make_float2(ex2(x1.x), ex2(x1.y)), pb2, o);
-          }
-          v[j] = o;
-        }
-        if constexpr (sizeof(T) == 4)
-          return make_uint4(__float_as_uint(v[0].x), __float_as_uint(v[0].y), __float_as_uint(v[1].x),
-                            __float_as_uint(v[1].y));
-        else
-          return make_uint4(to_bf2(v[0]), to_bf2(v[1]), to_bf2(v[2]), to_bf2(v[3]));
-      };
-      // a piece of a row that is dead or slow, or whose gradient lies at other addresses
-      auto odd_piece = [&](const uint4* from, T* out) {
-        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (!dead) {
-          x = *from;
-          if (slow) {
-            float2 v[N2];
-            unpack<T>(x, v);
-            alignas(16) T o[N];
-#pragma unroll
-            for (int j = 0; j < N2; ++j) {
-              o[2 * j] = from_f32<T>(value(v[j].x));
-              o[2 * j + 1] = from_f32<T>(value(v[j].y));
-            }
-            x = *(const uint4*)o;
-          } else {
-            x = gradient(x);
-          }
-        }
-        if (same) {
-          *(uint4*)out = x;
-        } else {
-          const T* o = (const T*)&x;
-#pragma unroll
-          for (int j = 0; j < N; ++j) out[j] = o[j];
-        }
-      };
-      T* out = dz + S.head + (long)tid * N;
-      const int n = mine(S), nn_row = wn != 0.f ? mine(Sn) : 0;
-      const bool plain = same && !slow && !dead;
-      if constexpr (HELD) {
-        const float en = wn != 0.f && tid < Sn.edges ? to_f32(Sn.row[Sn.edge(tid)]) : 0.f;
-        // the thread's batches that are whole in both rows, and the rest
-        const int full = plain ? min(n, nn_row) / U * U : 0;
-        int p = 0;
-        uint4 x[U];
-        for (; p < full; p += U) {
-#pragma unroll
-          for (int u = 0; u < U; ++u) x[u] = *(const uint4*)((const char*)slot + k2 + u * D * 16);
-#pragma unroll
-          for (int u = 0; u < U; ++u) *(uint4*)(out + (long)u * D * N) = gradient(x[u]);
-          ask(k2);  // the values have been used: the place is free
-          advance(k2);
-          landed();
-#pragma unroll
-          for (int u = 0; u < U; ++u) x[u] = *(const uint4*)((const char*)slot + k1 + u * D * 16);
-          take(rn, x);
-          advance(k1);
-          out += (long)U * D * N;
-        }
-        for (; p < A.rounds; p += U) {
-          for (int u = 0; u < U && p + u < n; ++u)
-            odd_piece((const uint4*)((const char*)slot + k2 + u * D * 16), out + (long)u * D * N);
-          ask(k2);
-          advance(k2);
-          landed();
-          if (p < nn_row) {
-            fetch(k1, nn_row - p, x);
-            take(rn, x);
-          }
-          advance(k1);
-          out += (long)U * D * N;
-        }
-        if (wn != 0.f && tid < Sn.edges) take_edge(rn, en);
+      Run next;  // the sums of row t + step
+      if (!A.dlogits) {
+        if (t + step < A.T) pass1(Sn, wn, next);
       } else {
-        for (int p = 0; p < n; ++p, out += (long)D * N) {
-          const uint4* from = (const uint4*)S.piece(p * D + tid);
-          if (plain) *(uint4*)out = gradient(*from);
-          else odd_piece(from, out);
+        const int* id = eid + b * E1;
+        const float *zj = ez + b * E1, *q = eq + b * E1;
+        T* dz = (T*)A.dlogits + t * A.ldd + v0;
+        const bool same = (((uintptr_t)dz ^ (uintptr_t)S.row) & 15) == 0;
+        const int label = dead ? -1 : id[A.K];
+        const float qa = dead ? 0.f : w * A.a * A.tau, hb = label < 0 ? 0.f : w * A.b;
+        const float pb = dead ? 0.f : hb / r.s1, pa = dead ? 0.f : qa * msum[b] / r.s + (TWO ? 0.f : pb);
+        auto value = [&](float z) {
+          if (dead) return 0.f;
+          return TWO ? pa * ex2(r.rel(z, ct)) + pb * ex2(r.rel1(z)) : pa * ex2(r.rel(z, ct));
+        };
+        const float2 pa2 = both(pa), pb2 = both(pb), neg = both(-r.n), neg1 = both(-r.n1);
+        auto gradient = [&](uint4 x4) {
+          float2 v[N2];
+          unpack<T>(x4, v);
+#pragma unroll
+          for (int j = 0; j < N2; ++j) {
+            const float2 x = fma2(v[j], both(ct), neg);
+            float2 o = mul2(make_float2(ex2(x.x), ex2(x.y)), pa2);
+            if (TWO) {
+              const float2 x1 = fma2(v[j], both(LOG2E), neg1);
+              o = fma2(make_float2(ex2(x1.x), ex2(x1.y)), pb2, o);
+            }
+            v[j] = o;
+          }
+          return pack<T>(v);
+        };
+        // a piece of a row that is dead or done again, or whose gradient starts elsewhere
+        // within 16 bytes
+        auto odd_piece = [&](const uint4* from, T* out) {
+          uint4 x = make_uint4(0u, 0u, 0u, 0u);
+          if (!dead) {
+            x = *from;
+            if (r.again) {
+              float2 v[N2];
+              unpack<T>(x, v);
+#pragma unroll
+              for (int j = 0; j < N2; ++j) v[j] = make_float2(value(v[j].x), value(v[j].y));
+              x = pack<T>(v);
+            } else {
+              x = gradient(x);
+            }
+          }
+          if (same) {
+            *(uint4*)out = x;
+          } else {
+            const T* o = (const T*)&x;
+#pragma unroll
+            for (int j = 0; j < N; ++j) out[j] = o[j];
+          }
+        };
+        T* out = dz + S.head + (long)tid * N;
+        const int n = pieces_of(S), n_next = wn != 0.f ? pieces_of(Sn) : 0;
+        const bool plain = same && !r.again && !dead;
+        if constexpr (HELD) {
+          const float edge = wn != 0.f && tid < Sn.edges ? to_f32(Sn.row[Sn.edge(tid)]) : 0.f;
+          // the thread's batches that are whole in both rows, then the others
+          const int full = plain ? min(n, n_next) / U * U : 0;
+          int p = 0;
+          for (; p < full; p += U) {
+            uint4 x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) x[u] = *(const uint4*)(slot + k2 + u * apart);
+#pragma unroll
+            for (int u = 0; u < U; ++u) *(uint4*)(out + (long)u * D * N) = gradient(x[u]);
+            ask(k2);  // the values have been used: the places are free
+            advance(k2);
+            landed();
+            take_slots(next, k1, U);
+            advance(k1);
+            out += (long)U * D * N;
+          }
+          for (; p < A.rounds; p += U) {
+            for (int u = 0; u < U && p + u < n; ++u)
+              odd_piece((const uint4*)(slot + k2 + u * apart), out + (long)u * D * N);
+            ask(k2);
+            advance(k2);
+            landed();
+            if (p < n_next) take_slots(next, k1, n_next - p);
+            advance(k1);
+            out += (long)U * D * N;
+          }
+          if (wn != 0.f && tid < Sn.edges) take_edge(next, edge);
+        } else {
+          for (int p = 0; p < n; ++p, out += (long)D * N) {
+            const uint4* from = (const uint4*)S.piece(p * D + tid);
+            if (plain) *(uint4*)out = gradient(*from);
+            else odd_piece(from, out);
+          }
         }
+        if (tid < S.edges) dz[S.edge(tid)] = from_f32<T>(value(dead ? 0.f : to_f32(S.row[S.edge(tid)])));
+        __syncwarp();
+        if (!dead)  // the entries that lie among this warp's values
+          for (int j = lane; j <= A.K; j += 32) {
+            const int e = id[j] - v0;
+            if (id[j] < 0 || e < 0 || e >= vn) continue;
+            const int i = e - S.head;
+            const bool piece = i >= 0 && i < S.pieces * N;
+            if ((piece ? i / N % D : i < 0 ? e : e - S.pieces * N) / 32 != warp) continue;
+            float x = q[j];
+            if (repeats[b] || id[j] == label) {  // (the label may be one of the entries)
+              x = 0.f;
+              for (int i = 0; i < A.K; ++i) x += id[i] == id[j] ? q[i] : 0.f;
+            }
+            dz[e] = from_f32<T>(value(zj[j]) - qa * x - (id[j] == label ? hb : 0.f));
+          }
+        if constexpr (!HELD)
+          if (t + step < A.T) pass1(Sn, wn, next);
       }
-      if (tid < S.edges) dz[S.edge(tid)] = from_f32<T>(value(dead ? 0.f : to_f32(S.row[S.edge(tid)])));
       __syncwarp();
-      if (!dead)  // the entries that lie among this warp's values
-        for (int j = lane; j <= A.K; j += 32) {
-          const int e = id[j] - v0;
-          if (id[j] < 0 || e < 0 || e >= vn) continue;
-          const int i = e - S.head;
-          const bool piece = i >= 0 && i < S.pieces * N;
-          if ((piece ? i / N % D : i < 0 ? e : e - S.pieces * N) / 32 != warp) continue;
-          float x = 0.f;
-          for (int k = 0; k < A.K; ++k) x += id[k] == id[j] ? q[k] : 0.f;
-          dz[e] = from_f32<T>(value(zj[j]) - qa * x - (id[j] == label ? hb : 0.f));
-        }
-      if constexpr (!HELD)
-        if (t + step < A.T) pass1(Sn, wn, rn);
+      if (lane == 0) tcg::mbar_arrive(bar(&released_bar[b]));
+      run = next;
+      w = wn;
+      wn = wn2;
     }
-    r = rn;
-    w = wn;
-    wn = wn2;
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
   }
-  // shared memory outlives the copies and the neighbours' writes
-  asm volatile("cp.async.wait_group 0;" ::: "memory");
-  if constexpr (CL) cooperative_groups::this_cluster().sync();
+  if constexpr (CL) {
+    // A CTA's shared memory outlives what its neighbours send; after a wait that gave up
+    // that may still be on its way: some ten microseconds for it.
+    if (gave_up)
+      for (const long long c0 = clock64(); clock64() - c0 < 20000;) {}
+    cooperative_groups::this_cluster().sync();
+  }
 }
 
 template <typename T, bool TWO, bool CL, bool HELD>
@@ -568,7 +658,7 @@ lx_status launch_distill(const DistillArgs& A, int threads, int cols, int groups
   LX_CUDA(smem_cap_once((const void*)k_distill<T, TWO, CL, HELD>, SMEM, dev, cap));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(cols, groups);
-  cfg.blockDim = dim3(threads + 32);
+  cfg.blockDim = dim3(threads + 32 * TEACHERS);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
@@ -636,9 +726,14 @@ extern "C" lx_status lx_distill_loss(int32_t dtype, const void* logits, int64_t 
   A.loss = loss;
   A.dlogits = dlogits;
   A.ldd = ldd;
+  const CallWaits waits = take_call_waits();
+  A.wait_cycles = waits.cycles;
+  A.unmet = waits.unmet == LX_WAIT_CALL_SUMS;
   // Data threads that hold `bytes` of a row, and the CTAs of a row: as many as it takes to
   // hold it, and more where rows are few, in slices of 4096 columns at least
-  const size_t entries = ((8 * (size_t)(K + 1) + 3) / 4) * 16;
+  A.table = 32;
+  while (A.table < 2 * K) A.table *= 2;
+  const size_t entries = ((4 * BUFS * (size_t)(K + 1) + TEACHERS * A.table + 3) / 4) * 16;
   const int most = ((int)((SMEM - entries) / (16 * 512)) - AHEAD) / U * U;  // pieces of each of 512 threads
   const long row = (long)V * es;
   int cols = 1;
@@ -654,7 +749,7 @@ extern "C" lx_status lx_distill_loss(int32_t dtype, const void* logits, int64_t 
   if (A.rounds == 0) A.rounds = U;
   A.slots = !held ? 0 : dlogits ? A.rounds + AHEAD : AHEAD + U;
   const size_t smem = entries + (size_t)16 * threads * A.slots;
-  const int ctas = std::max(1, std::min((int)(65536 / (REGS * (threads + 32))), (int)(227 * 1024 / (smem + 5120))));
+  const int ctas = std::max(1, std::min((int)(65536 / (REGS * (threads + 32 * TEACHERS))), (int)(227 * 1024 / (smem + 5120))));
   const int groups = std::min(T, std::max(1, SMS * ctas / cols));
   const bool two = ce_weight != 0.f && temperature != 1.f;
   cudaStream_t s = (cudaStream_t)stream;

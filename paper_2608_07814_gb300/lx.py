@@ -38,7 +38,7 @@ EXPORTS = [
     "lx_router_balance", "lx_router_balance_backward", "lx_distill_loss",
 ]
 (LX_WAIT_NONE, LX_WAIT_STREAM_DEP, LX_WAIT_TC_MMA, LX_WAIT_ROUTER, LX_WAIT_CALL_PRODUCT,
- LX_WAIT_CALL_JACOBI) = range(6)
+ LX_WAIT_CALL_JACOBI, LX_WAIT_CALL_SUMS) = range(7)
 LX_NOALLOC_SCRATCH_BYTES = 16 << 20
 
 
@@ -345,7 +345,7 @@ def align_cost(dom, mem, stream=None) -> torch.Tensor:
 
 
 def inject_unmet_wait_call(site: int, cycles: int = 0) -> None:
-    """Test hook: in this thread's next align_cost / compress_factor the wait at
+    """Test hook: in this thread's next align_cost / compress_factor / distill_loss the wait at
     `site` (LX_WAIT_CALL_*) runs out after `cycles` SM clock cycles."""
     _check(lib().lx_inject_unmet_wait_call(int(site), int(cycles)))
 
