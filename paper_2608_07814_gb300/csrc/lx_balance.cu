@@ -130,10 +130,10 @@ __device__ __forceinline__ float exp_row(float2* v, float& lse) {
   float2 s2 = make_float2(0.f, 0.f);
 #pragma unroll
   for (int i = 0; i < N2; ++i) {
-    v[i] = mul2(add2(v[i], neg), l2e);
+    v[i] = muls(adds(v[i], neg), l2e);
     v[i].x = ex2(v[i].x);
     v[i].y = ex2(v[i].y);
-    s2 = add2(s2, v[i]);
+    s2 = adds(s2, v[i]);
   }
   const float s = lanes_sum<G>(s2.x + s2.y);
   lse = s == 0.f ? -INFINITY : m0 + logf(s);
@@ -214,7 +214,7 @@ k_balance_fwd(const __grid_constant__ BalArgs A) {
       if (row < t_end && lane == 0) A.lse[row] = lse;
       if (lse != -INFINITY) {
 #pragma unroll
-        for (int i = 0; i < N2; ++i) acc[i] = fma2(v[i], both(inv), acc[i]);
+        for (int i = 0; i < N2; ++i) acc[i] = fmas(v[i], both(inv), acc[i]);
         if (lane == 0) {
           z = fmaf(lse, lse, z);
           ++n;
@@ -389,8 +389,8 @@ k_balance_bwd(const __grid_constant__ BalArgs A) {
     float2 d2 = make_float2(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < N2; ++i) {
-      v[i] = mul2(v[i], both(inv));
-      d2 = fma2(cnt[i], v[i], d2);
+      v[i] = muls(v[i], both(inv));
+      d2 = fmas(cnt[i], v[i], d2);
     }
     const float d = lanes_sum<G>(d2.x + d2.y);
     if (t >= A.T) continue;
@@ -410,7 +410,7 @@ k_balance_bwd(const __grid_constant__ BalArgs A) {
 #pragma unroll
         for (int j = 0; j < VEC / 2; ++j) {
           const int i = c * (VEC / 2) + j;
-          const float2 w = mul2(v[i], fma2(a2, add2(cnt[i], nd), base));
+          const float2 w = muls(v[i], fmas(a2, adds(cnt[i], nd), base));
           o[2 * j] = w.x;
           o[2 * j + 1] = w.y;
         }

@@ -11,22 +11,22 @@
 // at a time.  Its threads hold their part of the row as 16-byte pieces in shared memory,
 // each thread its own (cp.async, no barrier between copy and use).  The first pass over a
 // row sums the exponentials against a running reference, an exchange joins the sums, the
-// second pass writes the gradient.  The second pass of a row runs together with the first
-// of the next one: a thread finishes a batch of pieces, asks for the ones AHEAD + (pieces
-// of a row) later in their place, and takes the next row's batch, which was asked for AHEAD
-// pieces ago; reads and writes go on all the time (with the passes one after the other all
-// CTAs drew on memory in the same halves of their rows).  Rows that do not fit the shared
-// memory of eight CTAs are read a second time from L2.
+// second pass writes the gradient.  The passes run together, the first a row and `lead`
+// pieces before the second: a thread finishes a batch of pieces, asks for later ones in
+// their place, and takes the first pass's next batch, which was asked for AHEAD pieces ago.
+// So reads and writes go on all the time (with the passes one after the other all CTAs
+// drew on memory in the same halves of their rows), and a row's sums are on their way while
+// the second pass finishes the row before.  Rows that do not fit the shared memory of eight
+// CTAs are read a second time from L2.
 //
-// Two warps of their own prepare the teacher's entries, up to four rows ahead, and write the
-// losses: their chains of loads take longer than a row.  The entries' places are written
-// once more, behind the dense values, by the warp that wrote those; entries of one id add
-// up.
+// Two warps of their own prepare the teacher's entries, up to four rows ahead (their chains
+// of loads take longer than a row), write the losses and, once the dense values of a row are
+// written, the entries' places once more; entries of one id add up.
 //
 // The roles meet at mbarriers alone: sums_bar when every data warp of the row's CTAs has
 // sent its partial sums (to every CTA: a barrier of the whole cluster would also wait for
 // the stores under way), ready_bar when a row's entries are prepared, result_bar when its
-// sums are known, released_bar when the data warps are done with its entries.  Every wait is
+// sums are known, released_bar when the data warps have written it.  Every wait is
 // bounded; one that gives up makes the row's loss and gradient NaN, and the CTA waits no
 // more.
 //
@@ -49,9 +49,11 @@ constexpr int MAX_WARPS = 16;    // data warps of a CTA
 constexpr int TEACHERS = 2;      // warps that prepare entries
 constexpr int BUFS = 4;          // rows whose entries are held, a multiple of TEACHERS
 constexpr int MAX_CLUSTER = 8;
-constexpr int SMEM = 222 * 1024; // dynamic shared memory of a CTA at most
+constexpr int SMEM = 219392;     // dynamic shared memory of an SM's CTAs at most
 constexpr int U = 2;             // pieces of a thread taken together
-constexpr int AHEAD = 8;         // pieces asked for before they are used, a multiple of U
+constexpr int AHEAD = 6;         // pieces asked for before they are used, a multiple of U
+constexpr int LEAD = 4;          // of the first pass, a multiple of U (or a row, if that is less)
+constexpr int SENDS = 4;         // exchanges whose sums are held
 constexpr int REGS = 96;         // registers a thread: the launch bound holds the compiler to it
 constexpr float LOWEST = -1073741824.f;  // -2^30
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -70,9 +72,11 @@ struct DistillArgs {
   void* dlogits;
   long ldd;
   int slice;   // columns of a CTA
+  int log_d;   // log2 of a CTA's data threads
   int table;   // places of a table of ids, a power of two
   int rounds;  // pieces of a thread, rounded up to a multiple of U
   int slots;   // of them in shared memory at a time, a multiple of U
+  int lead;
   unsigned long long wait_cycles;
   int unmet;   // test hook: the sums' barrier waits for what nobody sends
 };
@@ -170,8 +174,8 @@ __device__ __forceinline__ void add_pieces(float& n, float2& p, const uint4* q, 
       unpack<T>(q[u], v);
 #pragma unroll
       for (int j = 0; j < N2; ++j) {
-        const float2 x = fma2(v[j], both(c), both(neg));
-        s = add2(s, make_float2(ex2(x.x), ex2(x.y)));
+        const float2 x = fmas(v[j], both(c), both(neg));
+        s = adds(s, make_float2(ex2(x.x), ex2(x.y)));
       }
     }
     return s;
@@ -181,17 +185,17 @@ __device__ __forceinline__ void add_pieces(float& n, float2& p, const uint4* q, 
     float mx = piece_max<T>(q[0]);
     for (int u = 1; u < U; ++u) mx = fmaxf(mx, piece_max<T>(q[u]));
     const float N = ceilf(mx * c);
-    p = mul2(p, both(ex2(n - N)));
+    p = muls(p, both(ex2(n - N)));
     n = N;
     s = sum(-n);
   }
-  p = add2(p, s);
+  p = adds(p, s);
 }
 __device__ __forceinline__ void add_value(float& n, float2& p, float v, float c) {
   const float t = v * c;
   if (t > n + 16.f) {
     const float N = ceilf(t);
-    p = mul2(p, both(ex2(n - N)));
+    p = muls(p, both(ex2(n - N)));
     n = N;
   }
   p.x += ex2(fmaf(v, c, -n));
@@ -205,6 +209,23 @@ struct Result {
   __device__ float rel1(float z) const { return again ? (z - top) * LOG2E : fmaf(z, LOG2E, -n1); }
 };
 
+// A row's gradient is pa 2^rel + pb 2^rel1 (one term without a second temperature), less
+// qa q at an entry and hb at the label
+struct Factors {
+  float qa, hb, pa, pb;
+  __device__ float value(const Result& r, float z, float ct, bool two) const {
+    return two ? pa * ex2(r.rel(z, ct)) + pb * ex2(r.rel1(z)) : pa * ex2(r.rel(z, ct));
+  }
+};
+__device__ __forceinline__ Factors factors(const DistillArgs& A, const Result& r, float w, float m, int label, bool two) {
+  Factors f;
+  f.qa = w * A.a * A.tau;
+  f.hb = label < 0 ? 0.f : w * A.b;
+  f.pb = f.hb / r.s1;
+  f.pa = f.qa * m / r.s + (two ? 0.f : f.pb);
+  return f;
+}
+
 extern __shared__ uint4 distill_smem[];
 
 // TWO: a hard-label term at another temperature than the teacher's.  HELD: rows fit shared
@@ -214,13 +235,14 @@ template <typename T, bool TWO, bool CL, bool HELD>
 __global__ void __launch_bounds__(576, 1)
 k_distill(const __grid_constant__ DistillArgs A) {
   constexpr int N = Span<T>::N, N2 = N / 2;
-  __shared__ float4 red[2][CL ? MAX_CLUSTER : 1][MAX_WARPS];  // the warps' sums
+  // the warps' sums of SENDS rows, and of a row that is done again
+  __shared__ float4 red[SENDS + 2][CL ? MAX_CLUSTER : 1][MAX_WARPS];
   __shared__ Result res[BUFS];
   __shared__ float msum[BUFS];
   __shared__ int repeats[BUFS];  // whether an id occurs twice
-  __shared__ uint64_t sums_bar[2], ready_bar[BUFS], result_bar[BUFS], released_bar[BUFS];
+  __shared__ uint64_t sums_bar[SENDS + 2], ready_bar[BUFS], result_bar[BUFS], released_bar[BUFS];
   __shared__ volatile int gave_up;
-  const int D = blockDim.x - 32 * TEACHERS, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = D >> 5;
+  const int log_d = A.log_d, D = 1 << log_d, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = D >> 5;
   const bool teacher = warp >= nw;
   const int E1 = A.K + 1, rank = CL ? blockIdx.x : 0, cols = CL ? gridDim.x : 1;
   // entries of BUFS rows: id, z, q, log q; entry K is the label
@@ -235,7 +257,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
   auto bar = [](uint64_t* b) { return (uint32_t)__cvta_generic_to_shared(b); };
   if (tid == 0) {
     gave_up = 0;
-    for (int i = 0; i < 2; ++i) tcg::mbar_init(bar(&sums_bar[i]), CL ? 1 : nw);
+    for (int i = 0; i < SENDS + 2; ++i) tcg::mbar_init(bar(&sums_bar[i]), CL ? 1 : nw);
     for (int i = 0; i < BUFS; ++i) {
       tcg::mbar_init(bar(&ready_bar[i]), 1);
       tcg::mbar_init(bar(&result_bar[i]), 1);
@@ -316,7 +338,6 @@ k_distill(const __grid_constant__ DistillArgs A) {
     auto provide = [&](long k) {
       const long t = first + k * step;
       if (t >= A.T) return;
-      if (k >= BUFS) wait(&released_bar[k % BUFS], (uint32_t)(k / BUFS - 1) & 1);
       if (!__any_sync(0xffffffffu, lost)) prepare(t, (int)(k % BUFS));
       __syncwarp();
       if (lane == 0) tcg::mbar_arrive(bar(&ready_bar[k % BUFS]));
@@ -325,13 +346,15 @@ k_distill(const __grid_constant__ DistillArgs A) {
     for (long k = h; first + k * step < A.T; k += TEACHERS) {
       const long t = first + k * step;
       const int b = (int)(k % BUFS);
-      wait(&result_bar[b], (uint32_t)(k / BUFS) & 1);
+      const uint32_t parity = (uint32_t)(k / BUFS) & 1;
+      wait(&result_bar[b], parity);
       const float w = weight(t);
       const Result r = res[b];
       const int* id = eid + b * E1;
       const float *zj = ez + b * E1, *q = eq + b * E1, *lq = elq + b * E1;
+      const bool dead = w == 0.f || r.s == 0.f;
       float loss = 0.f;
-      if (w != 0.f && r.s != 0.f) {
+      if (!dead) {
         const float ls = logf(r.s);
         for (int j = lane; j < A.K; j += 32)
           if (q[j] != 0.f) loss += q[j] * (lq[j] - (r.rel(zj[j], ct) * LN2 - ls));
@@ -342,6 +365,23 @@ k_distill(const __grid_constant__ DistillArgs A) {
       }
       if (__any_sync(0xffffffffu, lost)) loss = NAN;
       if (lane == 0 && rank == 0) A.loss[t] = loss;
+      wait(&released_bar[b], parity);
+      if (A.dlogits && !dead && !__any_sync(0xffffffffu, lost)) {
+        // the entries of this CTA's columns; the label may be one of them
+        T* dz = (T*)A.dlogits + t * A.ldd;
+        const int label = id[A.K], v0 = rank * A.slice, vn = min(A.slice, A.V - v0);
+        const Factors f = factors(A, r, w, msum[b], label, TWO);
+        for (int j = lane; j <= A.K; j += 32) {
+          const int e = id[j];
+          if (e < v0 || e >= v0 + vn) continue;
+          float x = q[j];
+          if (repeats[b] || e == label) {
+            x = 0.f;
+            for (int i = 0; i < A.K; ++i) x += id[i] == e ? q[i] : 0.f;
+          }
+          dz[e] = from_f32<T>(f.value(r, zj[j], ct, TWO) - f.qa * x - (e == label ? f.hb : 0.f));
+        }
+      }
       __syncwarp();
       provide(k + BUFS);
     }
@@ -352,115 +392,77 @@ k_distill(const __grid_constant__ DistillArgs A) {
     const uint32_t apart = D * 16, batch = U * apart, ring = A.slots * apart;  // bytes between a thread's pieces
     auto advance = [&](uint32_t& k) { k = k + batch == ring ? 0 : k + batch; };
     auto span = [&](long t) { return Span<T>((const T*)A.logits + (t < A.T ? t : first) * A.ld + v0, vn); };
-    auto pieces_of = [&](const Span<T>& S) { return (S.pieces - tid + D - 1) / D; };  // of this thread
+    auto pieces_of = [&](const Span<T>& S) { return (S.pieces - tid + D - 1) >> log_d; };  // of this thread
 
     // The copies, a batch to a group, in the order of use: rows of weight 0 and pieces that
     // a thread does not have leave their slots as they are.
     long ask_t = first;
     float ask_w = weight(first);
     const T* ask_at = nullptr;
-    int ask_left = 0, ask_rounds = 0;  // pieces of the thread, rounds of the row not asked for yet
+    // not asked for yet: pieces of the thread, pieces that every thread has, rounds of the row
+    int ask_left = 0, ask_whole = 0, ask_rounds = 0;
+    auto copy = [](uint32_t dst, const void* src) {
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    };
     auto ask = [&](uint32_t to) {
       if (ask_rounds == 0) {
         const Span<T> S = span(ask_t);
         ask_at = S.piece(tid);
         ask_left = ask_w != 0.f ? pieces_of(S) : 0;
+        ask_whole = ask_w != 0.f ? S.pieces >> log_d : 0;
         ask_rounds = A.rounds;
         ask_t += step;
         ask_w = weight(ask_t);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (u < ask_left)
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(slot_at + to + u * apart),
-                       "l"(ask_at + (long)u * D * N)
-                       : "memory");
+        if (u < ask_left) copy(slot_at + to + u * apart, ask_at + (long)u * D * N);
       asm volatile("cp.async.commit_group;" ::: "memory");
       ask_at += (long)U * D * N;
       ask_left -= U;
+      ask_whole -= U;
       ask_rounds -= U;
     };
-    auto landed = [] { asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD / U) : "memory"); };
-
-    // The first pass: a batch of the thread's pieces, of which it has `have`, into the sums
-    auto take = [&](Run& r, const uint4* q) {
-      add_pieces<T>(r.n, r.p, q, ct);
-      if (TWO) add_pieces<T>(r.n1, r.p1, q, LOG2E);
-    };
-    auto take_edge = [&](Run& r, float v) {
-      add_value(r.n, r.p, v, ct);
-      if (TWO) add_value(r.n1, r.p1, v, LOG2E);
-    };
-    auto take_slots = [&](Run& r, uint32_t k, int have) {
-      uint4 q[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) q[u] = u < have ? *(const uint4*)(slot + k + u * apart) : no_piece<T>();
-      take(r, q);
-    };
-    uint32_t k0 = 0, k1 = 0, k2 = 0;  // slots of the copies, of the first and of the second pass
-    // of a whole row by itself: the first row, and every row where there is no gradient
-    auto pass1 = [&](const Span<T>& S, float w, Run& r) {
-      const int n = w != 0.f ? pieces_of(S) : 0;
-      if constexpr (HELD) {
-        for (int p = 0; p < A.rounds; p += U) {
-          ask(k0);
-          advance(k0);
-          landed();
-          if (p < n) take_slots(r, k1, n - p);
-          advance(k1);
-        }
-      } else {
-        for (int p = 0; p < n; p += U) {
-          uint4 q[U];
-#pragma unroll
-          for (int u = 0; u < U; ++u)
-            q[u] = p + u < n ? *(const uint4*)S.piece((p + u) * D + tid) : no_piece<T>();
-          take(r, q);
-        }
-      }
-      if (w != 0.f && tid < S.edges) take_edge(r, to_f32(S.row[S.edge(tid)]));
-    };
-
-    // Every data warp's v of the row's CTAs, in red[]; returns which half
-    int sent = 0;
-    auto exchange = [&](float4 v) {
-      const int turn = sent & 1;
-      if (__any_sync(0xffffffffu, lost)) return turn;
+    // Sums of the row's CTAs: every data warp's v goes to red[i] of each of them
+    auto send = [&](int i, float4 v) {
+      if (__any_sync(0xffffffffu, lost)) return;
       if constexpr (CL) {
-        if (tid == 0) tcg::mbar_expect_tx(bar(&sums_bar[turn]), cols * nw * 16 + (A.unmet ? 16 : 0));
+        if (tid == 0) tcg::mbar_expect_tx(bar(&sums_bar[i]), cols * nw * 16 + (A.unmet ? 16 : 0));
         if (lane < cols) {
           uint32_t to, at;
           asm("mapa.shared::cluster.u32 %0, %1, %2;"
               : "=r"(to)
-              : "r"((uint32_t)__cvta_generic_to_shared(&red[turn][rank][warp])), "r"(lane));
-          asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(bar(&sums_bar[turn])), "r"(lane));
+              : "r"((uint32_t)__cvta_generic_to_shared(&red[i][rank][warp])), "r"(lane));
+          asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(bar(&sums_bar[i])), "r"(lane));
           asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(
                            to),
                        "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w), "r"(at)
                        : "memory");
         }
       } else if (lane == 0) {
-        red[turn][0][warp] = v;
-        if (!(A.unmet && warp == 0)) tcg::mbar_arrive(bar(&sums_bar[turn]));
+        red[i][0][warp] = v;
+        if (!(A.unmet && warp == 0)) tcg::mbar_arrive(bar(&sums_bar[i]));
       }
       __syncwarp();
-      wait(&sums_bar[turn], (sent >> 1) & 1);
-      ++sent;
-      return turn;
     };
-    // The threads' sums over the row, the same in every data thread
-    auto joined = [&](Run r) {
+    // A place is written again SENDS rows later: a warp that sends row x + 4 has received
+    // row x + 2, so every warp has sent that, and had received row x before.  (Of a row that
+    // is done again, the two exchanges alternate and are waited for at once.)
+    auto send_run = [&](int i, Run r) {
       r.s += r.p.x + r.p.y;
       join_warp(r.n, r.s);
       if (TWO) {
         r.s1 += r.p1.x + r.p1.y;
         join_warp(r.n1, r.s1);
       }
-      const int turn = exchange(make_float4(r.n, r.s, r.n1, r.s1));
-      r = Run();
-      for (int i = lane; i < cols * MAX_WARPS; i += 32)
-        if ((i & (MAX_WARPS - 1)) < nw) {
-          const float4 o = red[turn][i / MAX_WARPS][i & (MAX_WARPS - 1)];
+      send(i, make_float4(r.n, r.s, r.n1, r.s1));
+    };
+    auto receive = [&](int i, uint32_t parity) {  // the same in every data thread
+      wait(&sums_bar[i], parity);
+      Run r;
+      for (int j = lane; j < cols * MAX_WARPS; j += 32)
+        if ((j & (MAX_WARPS - 1)) < nw) {
+          const float4 o = red[i][j / MAX_WARPS][j & (MAX_WARPS - 1)];
           join(r.n, r.s, o.x, o.y);
           if (TWO) join(r.n1, r.s1, o.z, o.w);
         }
@@ -470,46 +472,124 @@ k_distill(const __grid_constant__ DistillArgs A) {
       return r;
     };
 
-    float w = weight(first), wn = weight(first + step);
-    Run run;  // the sums of row t
-    if constexpr (HELD)
+    // The first pass, a batch of the thread's pieces at a time
+    auto take = [&](Run& r, const uint4* q) {
+      add_pieces<T>(r.n, r.p, q, ct);
+      if (TWO) add_pieces<T>(r.n1, r.p1, q, LOG2E);
+    };
+    uint32_t k0 = 0, k1 = 0, k2 = 0;  // slots of the copies, of the first and of the second pass
+    // its row: number, place, weight, the thread's pieces, those taken, the edge and the sums
+    long feed_k = 0, feed_t = first;
+    float feed_w = weight(first), feed_wn = weight(first + step), feed_edge = 0.f;
+    int feed_n = 0, feed_whole = 0, feed_p = 0, feed_sent = 0, edges = 0;
+    Run feed;
+    auto feed_row = [&] {  // starts on row feed_t
+      const Span<T> S = span(feed_t);
+      feed = Run();
+      feed_p = 0;
+      feed_n = feed_w != 0.f ? pieces_of(S) : 0;
+      feed_whole = feed_w != 0.f ? S.pieces >> log_d : 0;
+      edges = feed_w != 0.f ? S.edges : 0;
+      if (tid < edges) feed_edge = to_f32(S.row[S.edge(tid)]);
+    };
+    auto feed_end = [&] {  // sends row feed_t's sums, once its entries are read
+      if (tid < edges) {
+        add_value(feed.n, feed.p, feed_edge, ct);
+        if (TWO) add_value(feed.n1, feed.p1, feed_edge, LOG2E);
+      }
+      if (feed_t < A.T) {
+        wait(&ready_bar[feed_k % BUFS], (uint32_t)(feed_k / BUFS) & 1);
+        if (feed_w != 0.f) send_run(feed_sent++ % SENDS, feed);
+      }
+      ++feed_k;
+      feed_t += step;
+      feed_w = feed_wn;
+      feed_wn = weight(feed_t + step);
+      feed_row();
+    };
+    auto feed_batch = [&] {
+      asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD / U) : "memory");
+      if (feed_p < feed_n) {
+        uint4 q[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          q[u] = feed_p + u < feed_n ? *(const uint4*)(slot + k1 + u * apart) : no_piece<T>();
+        take(feed, q);
+      }
+      advance(k1);
+      feed_p += U;
+      if (feed_p == A.rounds) feed_end();
+    };
+    auto feed_direct = [&] {  // a whole row that is not held
+      const Span<T> S = span(feed_t);
+      for (int p = 0; p < feed_n; p += U) {
+        uint4 q[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          q[u] = p + u < feed_n ? *(const uint4*)S.piece((p + u) * D + tid) : no_piece<T>();
+        take(feed, q);
+      }
+      feed_end();
+    };
+
+    feed_row();
+    if constexpr (HELD) {
       for (int p = 0; p < AHEAD; p += U) {
         ask(k0);
         advance(k0);
       }
-    pass1(span(first), w, run);
-    long k = 0;  // the CTA's rows
+      for (int p = 0; p < A.rounds + (A.dlogits ? A.lead : 0); p += U) {
+        ask(k0);
+        advance(k0);
+        feed_batch();
+      }
+    } else {
+      feed_direct();
+    }
+    float w = weight(first), wn = weight(first + step);
+    int got = 0, again = 0;  // exchanges received
+    long k = 0;              // the CTA's rows
     for (long t = first; t < A.T; t += step, ++k) {
-      const Span<T> S = span(t), Sn = span(t + step);
+      const Span<T> S = span(t);
       const float wn2 = weight(t + 2 * step);
       const int b = (int)(k % BUFS);
+      if (HELD && !A.dlogits)  // without gradient the next row's first pass hides the exchange
+        for (int p = 0; p < A.rounds; p += U) {
+          ask(k0);
+          advance(k0);
+          feed_batch();
+        }
       bool dead = w == 0.f;  // nothing to learn
       Result r = {0.f, 0.f, 0.f, 0.f, 0.f, false};
-      wait(&ready_bar[b], (uint32_t)(k / BUFS) & 1);
       if (!dead) {
-        run = joined(run);
+        Run run = receive(got % SENDS, (uint32_t)(got / SENDS) & 1);
+        ++got;
         if (run.s == 0.f) {  // every logit is -inf or out of the references' reach
           r.again = true;
           float top = -INFINITY;
           for (int i = tid; i < S.pieces; i += D) top = fmaxf(top, piece_max<T>(*(const uint4*)S.piece(i)));
           if (tid < S.edges) top = fmaxf(top, to_f32(S.row[S.edge(tid)]));
-          const int turn = exchange(make_float4(warp_max(top), 0.f, 0.f, 0.f));
+          const uint32_t parity = again & 1;
+          ++again;
+          send(SENDS, make_float4(warp_max(top), 0.f, 0.f, 0.f));
+          wait(&sums_bar[SENDS], parity);
           top = -INFINITY;
-          for (int i = lane; i < cols * MAX_WARPS; i += 32)
-            if ((i & (MAX_WARPS - 1)) < nw) top = fmaxf(top, red[turn][i / MAX_WARPS][i & (MAX_WARPS - 1)].x);
+          for (int j = lane; j < cols * MAX_WARPS; j += 32)
+            if ((j & (MAX_WARPS - 1)) < nw) top = fmaxf(top, red[SENDS][j / MAX_WARPS][j & (MAX_WARPS - 1)].x);
           r.top = top = warp_max(top);
           dead = top == -INFINITY;
+          run = Run();
+          run.n = run.n1 = 0.f;
           if (!dead) {
-            run = Run();
-            run.n = run.n1 = 0.f;
             auto add = [&](float v) {
               run.s += ex2((v - top) * ct);
               if (TWO) run.s1 += ex2((v - top) * LOG2E);
             };
             for (int i = tid; i < S.pieces * N; i += D) add(to_f32(S.row[S.head + i]));
             if (tid < S.edges) add(to_f32(S.row[S.edge(tid)]));
-            run = joined(run);
           }
+          send_run(SENDS + 1, run);
+          run = receive(SENDS + 1, parity);
         }
         r.n = run.n;
         r.s = dead ? 0.f : run.s;
@@ -520,44 +600,41 @@ k_distill(const __grid_constant__ DistillArgs A) {
         res[b] = r;
         tcg::mbar_arrive(bar(&result_bar[b]));
       }
-      Run next;  // the sums of row t + step
-      if (!A.dlogits) {
-        if (t + step < A.T) pass1(Sn, wn, next);
-      } else {
-        const int* id = eid + b * E1;
-        const float *zj = ez + b * E1, *q = eq + b * E1;
+      if (A.dlogits) {
         T* dz = (T*)A.dlogits + t * A.ldd + v0;
         const bool same = (((uintptr_t)dz ^ (uintptr_t)S.row) & 15) == 0;
-        const int label = dead ? -1 : id[A.K];
-        const float qa = dead ? 0.f : w * A.a * A.tau, hb = label < 0 ? 0.f : w * A.b;
-        const float pb = dead ? 0.f : hb / r.s1, pa = dead ? 0.f : qa * msum[b] / r.s + (TWO ? 0.f : pb);
-        auto value = [&](float z) {
-          if (dead) return 0.f;
-          return TWO ? pa * ex2(r.rel(z, ct)) + pb * ex2(r.rel1(z)) : pa * ex2(r.rel(z, ct));
-        };
-        const float2 pa2 = both(pa), pb2 = both(pb), neg = both(-r.n), neg1 = both(-r.n1);
+        Factors f = {};
+        if (!dead) f = factors(A, r, w, msum[b], eid[b * E1 + A.K], TWO);
+        auto value = [&](float z) { return dead ? 0.f : f.value(r, z, ct, TWO); };
+        // bf16: the factors go into the exponents (a 2^x = 2^(x + log2 a), which rounds to
+        // about 1e-6 of the value); fp32, and a negative factor: multiplied
+        constexpr bool FOLD = sizeof(T) == 2;
+        const float2 pa2 = both(f.pa), pb2 = both(f.pb);
+        const float2 neg = both((FOLD ? __log2f(f.pa) : 0.f) - r.n), neg1 = both((FOLD ? __log2f(f.pb) : 0.f) - r.n1);
         auto gradient = [&](uint4 x4) {
           float2 v[N2];
           unpack<T>(x4, v);
 #pragma unroll
           for (int j = 0; j < N2; ++j) {
-            const float2 x = fma2(v[j], both(ct), neg);
-            float2 o = mul2(make_float2(ex2(x.x), ex2(x.y)), pa2);
+            const float2 x = fmas(v[j], both(ct), neg);
+            float2 o = make_float2(ex2(x.x), ex2(x.y));
+            if (!FOLD) o = muls(o, pa2);
             if (TWO) {
-              const float2 x1 = fma2(v[j], both(LOG2E), neg1);
-              o = fma2(make_float2(ex2(x1.x), ex2(x1.y)), pb2, o);
+              const float2 x1 = fmas(v[j], both(LOG2E), neg1), o1 = make_float2(ex2(x1.x), ex2(x1.y));
+              o = FOLD ? adds(o, o1) : fmas(o1, pb2, o);
             }
             v[j] = o;
           }
           return pack<T>(v);
         };
-        // a piece of a row that is dead or done again, or whose gradient starts elsewhere
-        // within 16 bytes
+        const bool slow = r.again || (FOLD && (f.pa < 0.f || f.pb < 0.f));
+        // a piece of a row that is dead or slow, or whose gradient starts elsewhere within
+        // 16 bytes
         auto odd_piece = [&](const uint4* from, T* out) {
           uint4 x = make_uint4(0u, 0u, 0u, 0u);
           if (!dead) {
             x = *from;
-            if (r.again) {
+            if (slow) {
               float2 v[N2];
               unpack<T>(x, v);
 #pragma unroll
@@ -575,67 +652,73 @@ k_distill(const __grid_constant__ DistillArgs A) {
             for (int j = 0; j < N; ++j) out[j] = o[j];
           }
         };
-        T* out = dz + S.head + (long)tid * N;
-        const int n = pieces_of(S), n_next = wn != 0.f ? pieces_of(Sn) : 0;
-        const bool plain = same && !r.again && !dead;
+        char* const out = (char*)(dz + S.head) + tid * 16;
+        const int n = pieces_of(S);
+        const bool plain = same && !slow;
         if constexpr (HELD) {
-          const float edge = wn != 0.f && tid < Sn.edges ? to_f32(Sn.row[Sn.edge(tid)]) : 0.f;
-          // the thread's batches that are whole in both rows, then the others
-          const int full = plain ? min(n, n_next) / U * U : 0;
+          const int whole = plain ? S.pieces >> log_d : 0;  // pieces that every thread has
           int p = 0;
-          for (; p < full; p += U) {
-            uint4 x[U];
+          while (p < A.rounds) {
+            // batches in which every thread has its pieces of this row, of the first pass's
+            // and of the one that is asked for, none of which ends before
+            const int f_left = min(feed_whole - feed_p, A.rounds - feed_p - U);
+            const int run = min(min(whole - p, f_left), min(ask_whole, ask_rounds)) / U;
+            if (run > 0) {
+              char* o = out + (size_t)p * apart;
+              const char* a = (const char*)ask_at;
+              for (int i = 0; i < run; ++i) {
+                uint4 x[U];
+                if (!dead) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) x[u] = *(const uint4*)(slot + k2 + u * apart);
+                  for (int u = 0; u < U; ++u) x[u] = *(const uint4*)(slot + k2 + u * apart);
 #pragma unroll
-            for (int u = 0; u < U; ++u) *(uint4*)(out + (long)u * D * N) = gradient(x[u]);
-            ask(k2);  // the values have been used: the places are free
-            advance(k2);
-            landed();
-            take_slots(next, k1, U);
-            advance(k1);
-            out += (long)U * D * N;
+                  for (int u = 0; u < U; ++u) x[u] = gradient(x[u]);
+                } else {
+#pragma unroll
+                  for (int u = 0; u < U; ++u) x[u] = make_uint4(0u, 0u, 0u, 0u);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) *(uint4*)(o + u * apart) = x[u];
+#pragma unroll
+                for (int u = 0; u < U; ++u) copy(slot_at + k2 + u * apart, a + u * apart);  // the places are free
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                advance(k2);
+                asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD / U) : "memory");
+#pragma unroll
+                for (int u = 0; u < U; ++u) x[u] = *(const uint4*)(slot + k1 + u * apart);
+                take(feed, x);
+                advance(k1);
+                o += batch;
+                a += batch;
+              }
+              p += run * U;
+              feed_p += run * U;
+              ask_at = (const T*)a;
+              ask_left -= run * U;
+              ask_whole -= run * U;
+              ask_rounds -= run * U;
+            } else {
+              for (int u = 0; u < U && p + u < n; ++u)
+                odd_piece((const uint4*)(slot + k2 + u * apart), (T*)(out + (size_t)(p + u) * apart));
+              ask(k2);
+              advance(k2);
+              feed_batch();
+              p += U;
+            }
           }
-          for (; p < A.rounds; p += U) {
-            for (int u = 0; u < U && p + u < n; ++u)
-              odd_piece((const uint4*)(slot + k2 + u * apart), out + (long)u * D * N);
-            ask(k2);
-            advance(k2);
-            landed();
-            if (p < n_next) take_slots(next, k1, n_next - p);
-            advance(k1);
-            out += (long)U * D * N;
-          }
-          if (wn != 0.f && tid < Sn.edges) take_edge(next, edge);
         } else {
-          for (int p = 0; p < n; ++p, out += (long)D * N) {
+          for (int p = 0; p < n; ++p) {
             const uint4* from = (const uint4*)S.piece(p * D + tid);
-            if (plain) *(uint4*)out = gradient(*from);
-            else odd_piece(from, out);
+            T* o = (T*)(out + (size_t)p * apart);
+            if (plain && !dead) *(uint4*)o = gradient(*from);
+            else odd_piece(from, o);
           }
         }
         if (tid < S.edges) dz[S.edge(tid)] = from_f32<T>(value(dead ? 0.f : to_f32(S.row[S.edge(tid)])));
-        __syncwarp();
-        if (!dead)  // the entries that lie among this warp's values
-          for (int j = lane; j <= A.K; j += 32) {
-            const int e = id[j] - v0;
-            if (id[j] < 0 || e < 0 || e >= vn) continue;
-            const int i = e - S.head;
-            const bool piece = i >= 0 && i < S.pieces * N;
-            if ((piece ? i / N % D : i < 0 ? e : e - S.pieces * N) / 32 != warp) continue;
-            float x = q[j];
-            if (repeats[b] || id[j] == label) {  // (the label may be one of the entries)
-              x = 0.f;
-              for (int i = 0; i < A.K; ++i) x += id[i] == id[j] ? q[i] : 0.f;
-            }
-            dz[e] = from_f32<T>(value(zj[j]) - qa * x - (id[j] == label ? hb : 0.f));
-          }
-        if constexpr (!HELD)
-          if (t + step < A.T) pass1(Sn, wn, next);
       }
+      if constexpr (!HELD) feed_direct();
       __syncwarp();
       if (lane == 0) tcg::mbar_arrive(bar(&released_bar[b]));
-      run = next;
       w = wn;
       wn = wn2;
     }
@@ -667,6 +750,11 @@ lx_status launch_distill(const DistillArgs& A, int threads, int cols, int groups
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = CL ? 1 : 0;
+  if (CL && cols > 2) {  // clusters that the GPCs have room for at a time: a second round would run alone
+    int most = 0;
+    LX_CUDA(cudaOccupancyMaxActiveClusters(&most, k_distill<T, TWO, CL, HELD>, &cfg));
+    cfg.gridDim.y = std::max(1, std::min(groups, most));
+  }
   LX_CUDA(cudaLaunchKernelEx(&cfg, k_distill<T, TWO, CL, HELD>, A));
   return LX_OK;
 }
@@ -729,27 +817,35 @@ extern "C" lx_status lx_distill_loss(int32_t dtype, const void* logits, int64_t 
   const CallWaits waits = take_call_waits();
   A.wait_cycles = waits.cycles;
   A.unmet = waits.unmet == LX_WAIT_CALL_SUMS;
-  // Data threads that hold `bytes` of a row, and the CTAs of a row: as many as it takes to
-  // hold it, and more where rows are few, in slices of 4096 columns at least
+  // A CTA of 256 data threads with half of an SM's shared memory (128 and a quarter for short
+  // rows) where a row fits it, else CTAs of 512 with all of it, as many as hold a row; rows
+  // too long for eight of those are not held.  Few rows are spread further, in slices of
+  // 4096 columns at least.
   A.table = 32;
   while (A.table < 2 * K) A.table *= 2;
   const size_t entries = ((4 * BUFS * (size_t)(K + 1) + TEACHERS * A.table + 3) / 4) * 16;
-  const int most = ((int)((SMEM - entries) / (16 * 512)) - AHEAD) / U * U;  // pieces of each of 512 threads
   const long row = (long)V * es;
+  auto holds = [&](int threads, size_t smem) {  // bytes of a row
+    const long pieces = ((long)smem - (long)entries) / (16 * threads) - AHEAD - U;
+    return std::max(0L, pieces / U * U * 16 * threads);
+  };
+  const long whole = holds(512, SMEM);
+  const bool held = row <= std::max(whole * MAX_CLUSTER, holds(256, SMEM / 2));
   int cols = 1;
-  while (cols < MAX_CLUSTER && row > 16L * 512 * most * cols) cols *= 2;
-  const bool held = row <= 16L * 512 * most * cols;
-  if (!held) cols = 1;
-  else
+  if (held) {
+    while (row > holds(256, SMEM / 2) && row > whole * cols) cols *= 2;
     while (cols < MAX_CLUSTER && (long)T * cols * 2 <= SMS && V / (cols * 2) >= 4096) cols *= 2;
+  }
   A.slice = cols == 1 ? V : ((V + cols - 1) / cols + 63) / 64 * 64;
   const long bytes = (long)A.slice * es;
-  const int threads = bytes > 16L * 256 * most ? 512 : bytes > 16L * 128 * most ? 256 : 128;
-  A.rounds = (int)((bytes / 16 + threads - 1) / threads + U - 1) / U * U;
-  if (A.rounds == 0) A.rounds = U;
-  A.slots = !held ? 0 : dlogits ? A.rounds + AHEAD : AHEAD + U;
+  const int threads = !held || bytes > holds(256, SMEM / 2) ? 512 : bytes > holds(128, SMEM / 4) ? 256 : 128;
+  A.log_d = threads == 512 ? 9 : threads == 256 ? 8 : 7;
+  A.rounds = std::max(U, (int)((bytes / 16 + threads - 1) / threads + U - 1) / U * U);
+  const int room = (int)(((threads == 512 ? SMEM : threads == 256 ? SMEM / 2 : SMEM / 4) - (long)entries) / (16 * threads));
+  A.lead = std::max(U, std::min({LEAD, A.rounds, (room - A.rounds - AHEAD) / U * U}));
+  A.slots = !held ? 0 : dlogits ? A.rounds + A.lead + AHEAD : AHEAD + U;
   const size_t smem = entries + (size_t)16 * threads * A.slots;
-  const int ctas = std::max(1, std::min((int)(65536 / (REGS * (threads + 32 * TEACHERS))), (int)(227 * 1024 / (smem + 5120))));
+  const int ctas = std::max(1, std::min((int)(65536 / (REGS * (threads + 32 * TEACHERS))), (int)(227 * 1024 / (smem + 14 * 1024))));
   const int groups = std::min(T, std::max(1, SMS * ctas / cols));
   const bool two = ce_weight != 0.f && temperature != 1.f;
   cudaStream_t s = (cudaStream_t)stream;

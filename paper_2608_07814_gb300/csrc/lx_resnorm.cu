@@ -327,7 +327,7 @@ k_resnorm_fwd(const __grid_constant__ NormArgs A) {
     float2 g[N2];
     R.params(A.gate, 0.f, 0.f, g);
 #pragma unroll
-    for (int i = 0; i < N2; ++i) w1[i] = mul2(w1[i], g[i]);
+    for (int i = 0; i < N2; ++i) w1[i] = muls(w1[i], g[i]);
   }
   // a row's gate is read a round ahead
   float next = token && R.row < A.T ? A.gate[R.row * A.ldg] : 1.f;
@@ -338,15 +338,15 @@ k_resnorm_fwd(const __grid_constant__ NormArgs A) {
     float2 x[N2];
     R.read(IN_R, t, x);
 #pragma unroll
-    for (int i = 0; i < N2; ++i) x[i] = mul2(x[i], a2);
+    for (int i = 0; i < N2; ++i) x[i] = muls(x[i], a2);
     float s1 = 1.f, s2 = 1.f, q[1];
     if (has_y) {
       float2 y[N2];
       R.read(IN_Y, t, y);
       if (post) {
-        float2 p = mul2(y[0], y[0]);
+        float2 p = muls(y[0], y[0]);
 #pragma unroll
-        for (int i = 1; i < N2; ++i) p = fma2(y[i], y[i], p);
+        for (int i = 1; i < N2; ++i) p = fmas(y[i], y[i], p);
         q[0] = p.x + p.y;
         R.sum(q, buf, turn);
         s1 = rsqrtf(q[0] * inv + A.eps);
@@ -355,22 +355,22 @@ k_resnorm_fwd(const __grid_constant__ NormArgs A) {
         float2 g[N2];
         R.read(IN_GATE, t, g);
 #pragma unroll
-        for (int i = 0; i < N2; ++i) y[i] = mul2(y[i], g[i]);
+        for (int i = 0; i < N2; ++i) y[i] = muls(y[i], g[i]);
       }
       const float2 f = both(s1 * tok);
 #pragma unroll
-      for (int i = 0; i < N2; ++i) x[i] = fma2(mul2(y[i], w1[i]), f, x[i]);
+      for (int i = 0; i < N2; ++i) x[i] = fmas(muls(y[i], w1[i]), f, x[i]);
     }
     if (A.r_out) R.write(A.r_out, t, x);
     if (A.w_pre) {
-      float2 p = mul2(x[0], x[0]);
+      float2 p = muls(x[0], x[0]);
 #pragma unroll
-      for (int i = 1; i < N2; ++i) p = fma2(x[i], x[i], p);
+      for (int i = 1; i < N2; ++i) p = fmas(x[i], x[i], p);
       q[0] = p.x + p.y;
       R.sum(q, buf, turn);
       s2 = rsqrtf(q[0] * inv + A.eps);
 #pragma unroll
-      for (int i = 0; i < N2; ++i) x[i] = mul2(mul2(x[i], both(s2)), w2[i]);
+      for (int i = 0; i < N2; ++i) x[i] = muls(muls(x[i], both(s2)), w2[i]);
       R.write(A.h_out, t, x);
     }
     if (A.stats && R.writer() && t < (unsigned)A.T) {

@@ -53,7 +53,10 @@ __device__ __forceinline__ void store(T* p, const float* v) {
   }
 }
 
-// Two fp32 operations in one instruction, each rounded as the single one
+// A pair's operations in one instruction (add2, mul2, fma2), each rounded as the single one,
+// or in two (adds, muls, fmas).  One instruction takes the issue slot of one but the pipe
+// and the latency of two: it won where issue slots bound a kernel (block norms backward: 83
+// against 91 us), two where chains of operations did (distillation: 494 and 410 us).
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   float2 d;
   asm("{\n\t.reg .b64 ra, rb, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\t"
@@ -77,6 +80,11 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
       : "=f"(d.x), "=f"(d.y)
       : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
   return d;
+}
+__device__ __forceinline__ float2 adds(float2 a, float2 b) { return make_float2(a.x + b.x, a.y + b.y); }
+__device__ __forceinline__ float2 muls(float2 a, float2 b) { return make_float2(a.x * b.x, a.y * b.y); }
+__device__ __forceinline__ float2 fmas(float2 a, float2 b, float2 c) {
+  return make_float2(fmaf(a.x, b.x, c.x), fmaf(a.y, b.y, c.y));
 }
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 __device__ __forceinline__ float2 bf2(uint32_t w) {  // two bf16: each is the upper half of its fp32
