@@ -569,7 +569,7 @@ LX_API lx_status lx_router_balance_backward(int32_t dtype, const void* logits, i
  *   loss = weight * (kd_weight temperature^2 kd + ce_weight ce)
  *   dz_v = weight * (kd_weight temperature (m softmax(z / temperature)_v - sum of the
  *          q_j with id_j = v) + ce_weight (softmax(z)_v - [v = label]))
- * A token with weight 0 (its logits and entries are not read), or whose logits are all
+ * A token with weight 0 (its logits and entries are not used), or whose logits are all
  * -inf, has loss 0 and gradient 0.  Entries with an id outside [0, V) or t = -inf are
  * skipped; entries that repeat an id add up; a token without entries has kd = 0.
  *   logits: [T][V] (dtype; rows ld apart);  teacher_id int32, teacher_logit fp32 [T][K],

@@ -51,7 +51,9 @@ constexpr int BUFS = 4;          // rows whose entries are held, a multiple of T
 constexpr int MAX_CLUSTER = 8;
 constexpr int SMEM = 219392;     // dynamic shared memory of an SM's CTAs at most
 constexpr int U = 2;             // pieces of a thread taken together
-constexpr int AHEAD = 6;         // pieces asked for before they are used, a multiple of U
+// pieces asked for before they are used, a multiple of U: rows held for a gradient leave
+// less room
+constexpr int ahead_of(bool grad) { return grad ? 6 : 12; }
 constexpr int LEAD = 4;          // of the first pass, a multiple of U (or a row, if that is less)
 constexpr int SENDS = 4;         // exchanges whose sums are held
 constexpr int REGS = 96;         // registers a thread: the launch bound holds the compiler to it
@@ -231,15 +233,14 @@ extern __shared__ uint4 distill_smem[];
 // TWO: a hard-label term at another temperature than the teacher's.  HELD: rows fit shared
 // memory.  blockDim: the data threads and the TEACHERS' warps; gridDim: (CTAs of a row,
 // rows)
-template <typename T, bool TWO, bool CL, bool HELD>
+template <typename T, bool TWO, bool CL, bool HELD, bool GRAD>
 __global__ void __launch_bounds__(576, 1)
 k_distill(const __grid_constant__ DistillArgs A) {
-  constexpr int N = Span<T>::N, N2 = N / 2;
+  constexpr int N = Span<T>::N, N2 = N / 2, AHEAD = ahead_of(GRAD);
   // the warps' sums of SENDS rows, and of a row that is done again
   __shared__ float4 red[SENDS + 2][CL ? MAX_CLUSTER : 1][MAX_WARPS];
   __shared__ Result res[BUFS];
   __shared__ float msum[BUFS];
-  __shared__ int repeats[BUFS];  // whether an id occurs twice
   __shared__ uint64_t sums_bar[SENDS + 2], ready_bar[BUFS], result_bar[BUFS], released_bar[BUFS];
   __shared__ volatile int gave_up;
   const int log_d = A.log_d, D = 1 << log_d, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = D >> 5;
@@ -251,8 +252,8 @@ k_distill(const __grid_constant__ DistillArgs A) {
   float* const eq = ez + BUFS * E1;
   float* const elq = eq + BUFS * E1;
   const float ct = A.ct;
-  const long first = blockIdx.y, step = gridDim.y;
-  auto weight = [&](long t) { return t >= A.T ? 0.f : A.weight ? A.weight[t] : 1.f; };
+  const unsigned T0 = A.T, first = blockIdx.y, step = gridDim.y;  // (row + 3 * step stays below 2^32)
+  auto weight = [&](unsigned t) { return t >= T0 ? 0.f : A.weight ? A.weight[t] : 1.f; };
 
   auto bar = [](uint64_t* b) { return (uint32_t)__cvta_generic_to_shared(b); };
   if (tid == 0) {
@@ -269,11 +270,14 @@ k_distill(const __grid_constant__ DistillArgs A) {
   if constexpr (CL) cooperative_groups::this_cluster().sync();  // all have started
   bool lost = false;  // a wait of this thread gave up
   auto wait = [&](uint64_t* b, uint32_t parity) {
-    if (lost) return;
-    if (gave_up || !tcg::mbar_wait(bar(b), parity, &gave_up, A.wait_cycles)) {
-      lost = true;
-      gave_up = 1;
+    if (lost || (!gave_up && tcg::mbar_try_wait(bar(b), parity))) return;
+    const long long c0 = clock64();
+    while (!gave_up && clock64() - c0 < (long long)A.wait_cycles) {
+      if (teacher) __nanosleep(200);  // its polls would take the data warps' issue slots
+      if (tcg::mbar_try_wait(bar(b), parity)) return;
     }
+    lost = true;
+    gave_up = 1;
   };
 
   if (teacher) {
@@ -281,43 +285,33 @@ k_distill(const __grid_constant__ DistillArgs A) {
     // k % BUFS.
     const int h = warp - nw;
     int* table = (int*)(elq + BUFS * E1) + h * A.table;
-    auto prepare = [&](long t, int b) {
-      if (weight(t) == 0.f) return;
+    auto prepare = [&](unsigned t, int b) {
       int* id = eid + b * E1;
       float *z = ez + b * E1, *q = eq + b * E1, *lq = elq + b * E1;
-      const T* row = (const T*)A.logits + t * A.ld;
-      for (int i = lane; i < A.table; i += 32) table[i] = -1;
-      __syncwarp();
+      const T* row = (const T*)A.logits + (long)t * A.ld;
+      const float w = weight(t), stored = A.top_lse ? A.top_lse[t] : 0.f;
+      const int label = A.labels ? A.labels[t] : -1;
       float tm = -INFINITY;
-      bool twice = false;
       for (int j = lane; j < A.K; j += 32) {
-        const int e = A.ids[t * A.K + j];
+        const int e = A.ids[(long)t * A.K + j];
+        const float v = A.top[(long)t * A.K + j];
         const bool ok = e >= 0 && e < A.V;
-        const float v = ok ? A.top[t * A.K + j] : -INFINITY;
         id[j] = ok ? e : -1;
-        z[j] = ok ? to_f32(row[e]) : 0.f;
-        q[j] = v;
-        tm = fmaxf(tm, v);
-        if (ok)  // at least half of the places stay free
-          for (int i = e;; ++i) {
-            const int was = atomicCAS(&table[i & (A.table - 1)], -1, e);
-            twice |= was == e;
-            if (was == -1 || was == e) break;
-          }
+        q[j] = ok ? v : -INFINITY;
+        tm = fmaxf(tm, q[j]);
       }
-      twice = __any_sync(0xffffffffu, twice);
+      if (w == 0.f) return;
+      for (int j = lane; j < A.K; j += 32) z[j] = id[j] >= 0 ? to_f32(row[id[j]]) : 0.f;
       if (lane == 0) {
-        const int e = A.labels ? A.labels[t] : -1;
-        const bool ok = e >= 0 && e < A.V;
-        id[A.K] = ok ? e : -1;
-        z[A.K] = ok ? to_f32(row[e]) : 0.f;
+        const bool ok = label >= 0 && label < A.V;
+        id[A.K] = ok ? label : -1;
+        z[A.K] = ok ? to_f32(row[label]) : 0.f;
         q[A.K] = 0.f;
-        repeats[b] = twice;
       }
       tm = warp_max(tm);
       float lz;  // log of the distribution's sum, relative to tm / tau
       if (A.top_lse) {
-        lz = A.top_lse[t] - tm / A.tau;
+        lz = stored - tm / A.tau;
       } else {
         float s = 0.f;
         for (int j = lane; j < A.K; j += 32)
@@ -335,18 +329,33 @@ k_distill(const __grid_constant__ DistillArgs A) {
       m = warp_sum(m);
       if (lane == 0) msum[b] = m;
     };
-    auto provide = [&](long k) {
-      const long t = first + k * step;
-      if (t >= A.T) return;
-      if (!__any_sync(0xffffffffu, lost)) prepare(t, (int)(k % BUFS));
+    auto provide = [&](unsigned k, unsigned t) {
+      if (t >= T0) return;
+      if (!__any_sync(0xffffffffu, lost)) prepare(t, k % BUFS);
       __syncwarp();
       if (lane == 0) tcg::mbar_arrive(bar(&ready_bar[k % BUFS]));
     };
-    for (long k = h; k < BUFS; k += TEACHERS) provide(k);
-    for (long k = h; first + k * step < A.T; k += TEACHERS) {
-      const long t = first + k * step;
-      const int b = (int)(k % BUFS);
-      const uint32_t parity = (uint32_t)(k / BUFS) & 1;
+    // whether an id of the row occurs twice, by a table in which at least half of the places
+    // stay free
+    auto repeated = [&](const int* id) {
+      for (int i = lane; i < A.table; i += 32) table[i] = -1;
+      __syncwarp();
+      bool twice = false;
+      for (int j = lane; j < A.K; j += 32)
+        if (id[j] >= 0)
+          for (int i = id[j];; ++i) {
+            const int was = atomicCAS(&table[i & (A.table - 1)], -1, id[j]);
+            twice |= was == id[j];
+            if (was == -1 || was == id[j]) break;
+          }
+      twice = __any_sync(0xffffffffu, twice);
+      return twice;
+    };
+    for (unsigned k = h; k < BUFS; k += TEACHERS) provide(k, first + k * step);
+    unsigned t = first + h * step;
+    for (unsigned k = h; t < T0; k += TEACHERS, t += TEACHERS * step) {
+      const int b = k % BUFS;
+      const uint32_t parity = k / BUFS & 1;
       wait(&result_bar[b], parity);
       const float w = weight(t);
       const Result r = res[b];
@@ -365,17 +374,18 @@ k_distill(const __grid_constant__ DistillArgs A) {
       }
       if (__any_sync(0xffffffffu, lost)) loss = NAN;
       if (lane == 0 && rank == 0) A.loss[t] = loss;
+      const bool twice = GRAD && !dead && repeated(id);
       wait(&released_bar[b], parity);
-      if (A.dlogits && !dead && !__any_sync(0xffffffffu, lost)) {
+      if (GRAD && !dead && !__any_sync(0xffffffffu, lost)) {
         // the entries of this CTA's columns; the label may be one of them
-        T* dz = (T*)A.dlogits + t * A.ldd;
+        T* dz = (T*)A.dlogits + (long)t * A.ldd;
         const int label = id[A.K], v0 = rank * A.slice, vn = min(A.slice, A.V - v0);
         const Factors f = factors(A, r, w, msum[b], label, TWO);
         for (int j = lane; j <= A.K; j += 32) {
           const int e = id[j];
           if (e < v0 || e >= v0 + vn) continue;
           float x = q[j];
-          if (repeats[b] || e == label) {
+          if (twice || e == label) {
             x = 0.f;
             for (int i = 0; i < A.K; ++i) x += id[i] == e ? q[i] : 0.f;
           }
@@ -383,7 +393,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
         }
       }
       __syncwarp();
-      provide(k + BUFS);
+      provide(k + BUFS, t + BUFS * step);
     }
   } else {
     const int v0 = rank * A.slice, vn = min(A.slice, A.V - v0);
@@ -391,12 +401,12 @@ k_distill(const __grid_constant__ DistillArgs A) {
     const uint32_t slot_at = (uint32_t)__cvta_generic_to_shared(slot);
     const uint32_t apart = D * 16, batch = U * apart, ring = A.slots * apart;  // bytes between a thread's pieces
     auto advance = [&](uint32_t& k) { k = k + batch == ring ? 0 : k + batch; };
-    auto span = [&](long t) { return Span<T>((const T*)A.logits + (t < A.T ? t : first) * A.ld + v0, vn); };
+    auto span = [&](unsigned t) { return Span<T>((const T*)A.logits + (long)(t < T0 ? t : first) * A.ld + v0, vn); };
     auto pieces_of = [&](const Span<T>& S) { return (S.pieces - tid + D - 1) >> log_d; };  // of this thread
 
     // The copies, a batch to a group, in the order of use: rows of weight 0 and pieces that
     // a thread does not have leave their slots as they are.
-    long ask_t = first;
+    unsigned ask_t = first;
     float ask_w = weight(first);
     const T* ask_at = nullptr;
     // not asked for yet: pieces of the thread, pieces that every thread has, rounds of the row
@@ -479,7 +489,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
     };
     uint32_t k0 = 0, k1 = 0, k2 = 0;  // slots of the copies, of the first and of the second pass
     // its row: number, place, weight, the thread's pieces, those taken, the edge and the sums
-    long feed_k = 0, feed_t = first;
+    unsigned feed_k = 0, feed_t = first;
     float feed_w = weight(first), feed_wn = weight(first + step), feed_edge = 0.f;
     int feed_n = 0, feed_whole = 0, feed_p = 0, feed_sent = 0, edges = 0;
     Run feed;
@@ -497,8 +507,8 @@ k_distill(const __grid_constant__ DistillArgs A) {
         add_value(feed.n, feed.p, feed_edge, ct);
         if (TWO) add_value(feed.n1, feed.p1, feed_edge, LOG2E);
       }
-      if (feed_t < A.T) {
-        wait(&ready_bar[feed_k % BUFS], (uint32_t)(feed_k / BUFS) & 1);
+      if (feed_t < T0) {
+        wait(&ready_bar[feed_k % BUFS], feed_k / BUFS & 1);
         if (feed_w != 0.f) send_run(feed_sent++ % SENDS, feed);
       }
       ++feed_k;
@@ -520,6 +530,37 @@ k_distill(const __grid_constant__ DistillArgs A) {
       feed_p += U;
       if (feed_p == A.rounds) feed_end();
     };
+    // asks for and takes a row's batches where there is no second pass
+    auto feed_only = [&] {
+      for (int p = 0; p < A.rounds;) {
+        const int run = min(min(feed_whole - feed_p, A.rounds - feed_p - U), min(ask_whole, ask_rounds)) / U;
+        for (int i = 0; i < run; ++i) {
+          uint4 x[U];
+#pragma unroll
+          for (int u = 0; u < U; ++u) copy(slot_at + k0 + u * apart, (const char*)ask_at + u * apart);
+          asm volatile("cp.async.commit_group;" ::: "memory");
+          advance(k0);
+          asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD / U) : "memory");
+#pragma unroll
+          for (int u = 0; u < U; ++u) x[u] = *(const uint4*)(slot + k1 + u * apart);
+          take(feed, x);
+          advance(k1);
+          ask_at += (long)U * D * N;
+        }
+        if (run > 0) {
+          p += run * U;
+          feed_p += run * U;
+          ask_left -= run * U;
+          ask_whole -= run * U;
+          ask_rounds -= run * U;
+        } else {
+          ask(k0);
+          advance(k0);
+          feed_batch();
+          p += U;
+        }
+      }
+    };
     auto feed_direct = [&] {  // a whole row that is not held
       const Span<T> S = span(feed_t);
       for (int p = 0; p < feed_n; p += U) {
@@ -538,27 +579,24 @@ k_distill(const __grid_constant__ DistillArgs A) {
         ask(k0);
         advance(k0);
       }
-      for (int p = 0; p < A.rounds + (A.dlogits ? A.lead : 0); p += U) {
-        ask(k0);
-        advance(k0);
-        feed_batch();
-      }
+      feed_only();
+      if (GRAD)
+        for (int p = 0; p < A.lead; p += U) {
+          ask(k0);
+          advance(k0);
+          feed_batch();
+        }
     } else {
       feed_direct();
     }
     float w = weight(first), wn = weight(first + step);
     int got = 0, again = 0;  // exchanges received
-    long k = 0;              // the CTA's rows
-    for (long t = first; t < A.T; t += step, ++k) {
+    unsigned k = 0;          // the CTA's rows
+    for (unsigned t = first; t < T0; t += step, ++k) {
       const Span<T> S = span(t);
       const float wn2 = weight(t + 2 * step);
-      const int b = (int)(k % BUFS);
-      if (HELD && !A.dlogits)  // without gradient the next row's first pass hides the exchange
-        for (int p = 0; p < A.rounds; p += U) {
-          ask(k0);
-          advance(k0);
-          feed_batch();
-        }
+      const int b = k % BUFS;
+      if (HELD && !GRAD) feed_only();  // without gradient the next row's first pass hides the exchange
       bool dead = w == 0.f;  // nothing to learn
       Result r = {0.f, 0.f, 0.f, 0.f, 0.f, false};
       if (!dead) {
@@ -600,8 +638,8 @@ k_distill(const __grid_constant__ DistillArgs A) {
         res[b] = r;
         tcg::mbar_arrive(bar(&result_bar[b]));
       }
-      if (A.dlogits) {
-        T* dz = (T*)A.dlogits + t * A.ldd + v0;
+      if constexpr (GRAD) {
+        T* dz = (T*)A.dlogits + (long)t * A.ldd + v0;
         const bool same = (((uintptr_t)dz ^ (uintptr_t)S.row) & 15) == 0;
         Factors f = {};
         if (!dead) f = factors(A, r, w, msum[b], eid[b * E1 + A.K], TWO);
@@ -733,12 +771,12 @@ k_distill(const __grid_constant__ DistillArgs A) {
   }
 }
 
-template <typename T, bool TWO, bool CL, bool HELD>
+template <typename T, bool TWO, bool CL, bool HELD, bool GRAD>
 lx_status launch_distill(const DistillArgs& A, int threads, int cols, int groups, size_t smem, cudaStream_t s) {
   static bool cap[64] = {};
   int dev = 0;
   LX_CUDA(cudaGetDevice(&dev));
-  LX_CUDA(smem_cap_once((const void*)k_distill<T, TWO, CL, HELD>, SMEM, dev, cap));
+  LX_CUDA(smem_cap_once((const void*)k_distill<T, TWO, CL, HELD, GRAD>, SMEM, dev, cap));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(cols, groups);
   cfg.blockDim = dim3(threads + 32 * TEACHERS);
@@ -752,23 +790,28 @@ lx_status launch_distill(const DistillArgs& A, int threads, int cols, int groups
   cfg.numAttrs = CL ? 1 : 0;
   if (CL && cols > 2) {  // clusters that the GPCs have room for at a time: a second round would run alone
     int most = 0;
-    LX_CUDA(cudaOccupancyMaxActiveClusters(&most, k_distill<T, TWO, CL, HELD>, &cfg));
+    LX_CUDA(cudaOccupancyMaxActiveClusters(&most, k_distill<T, TWO, CL, HELD, GRAD>, &cfg));
     cfg.gridDim.y = std::max(1, std::min(groups, most));
   }
-  LX_CUDA(cudaLaunchKernelEx(&cfg, k_distill<T, TWO, CL, HELD>, A));
+  LX_CUDA(cudaLaunchKernelEx(&cfg, k_distill<T, TWO, CL, HELD, GRAD>, A));
   return LX_OK;
 }
 
-template <typename T, bool CL, bool HELD>
-lx_status launch_two(const DistillArgs& A, bool two, int threads, int cols, int groups, size_t smem, cudaStream_t s) {
-  return two ? launch_distill<T, true, CL, HELD>(A, threads, cols, groups, smem, s)
-             : launch_distill<T, false, CL, HELD>(A, threads, cols, groups, smem, s);
+struct Shape {
+  int threads, cols, groups;  // data threads of a CTA, CTAs of a row, rows at a time
+  size_t smem;
+};
+
+template <typename T, bool CL, bool HELD, bool GRAD>
+lx_status launch_two(const DistillArgs& A, const Shape& S, cudaStream_t s) {
+  return A.b != 0.f && A.tau != 1.f ? launch_distill<T, true, CL, HELD, GRAD>(A, S.threads, S.cols, S.groups, S.smem, s)
+                                    : launch_distill<T, false, CL, HELD, GRAD>(A, S.threads, S.cols, S.groups, S.smem, s);
 }
 template <typename T>
-lx_status launch_type(const DistillArgs& A, bool two, int threads, int cols, int groups, size_t smem, cudaStream_t s) {
-  if (A.slots == 0) return launch_two<T, false, false>(A, two, threads, cols, groups, smem, s);
-  if (cols > 1) return launch_two<T, true, true>(A, two, threads, cols, groups, smem, s);
-  return launch_two<T, false, true>(A, two, threads, cols, groups, smem, s);
+lx_status launch_type(const DistillArgs& A, const Shape& S, cudaStream_t s) {
+  if (!A.dlogits) return S.cols > 1 ? launch_two<T, true, true, false>(A, S, s) : launch_two<T, false, true, false>(A, S, s);
+  if (A.slots == 0) return launch_two<T, false, false, true>(A, S, s);
+  return S.cols > 1 ? launch_two<T, true, true, true>(A, S, s) : launch_two<T, false, true, true>(A, S, s);
 }
 
 }  // namespace
@@ -817,38 +860,38 @@ extern "C" lx_status lx_distill_loss(int32_t dtype, const void* logits, int64_t 
   const CallWaits waits = take_call_waits();
   A.wait_cycles = waits.cycles;
   A.unmet = waits.unmet == LX_WAIT_CALL_SUMS;
-  // A CTA of 256 data threads with half of an SM's shared memory (128 and a quarter for short
+  // CTAs of 256 data threads with half of an SM's shared memory (128 and a quarter for short
   // rows) where a row fits it, else CTAs of 512 with all of it, as many as hold a row; rows
-  // too long for eight of those are not held.  Few rows are spread further, in slices of
-  // 4096 columns at least.
+  // too long for eight of those are not held.  Few rows are spread over more CTAs, in slices
+  // of 4096 columns at least.  The shape does not depend on whether a gradient is asked for,
+  // so the losses do not either.
   A.table = 32;
   while (A.table < 2 * K) A.table *= 2;
+  const bool grad = dlogits != nullptr;
   const size_t entries = ((4 * BUFS * (size_t)(K + 1) + TEACHERS * A.table + 3) / 4) * 16;
   const long row = (long)V * es;
-  auto holds = [&](int threads, size_t smem) {  // bytes of a row
-    const long pieces = ((long)smem - (long)entries) / (16 * threads) - AHEAD - U;
-    return std::max(0L, pieces / U * U * 16 * threads);
+  auto places = [&](int threads) { return ((long)SMEM * threads / 512 - (long)entries) / (16 * threads); };
+  auto holds = [&](int threads) {  // bytes of a row
+    return std::max(0L, (places(threads) - ahead_of(true) - U) / U * U * 16 * threads);
   };
-  const long whole = holds(512, SMEM);
-  const bool held = row <= std::max(whole * MAX_CLUSTER, holds(256, SMEM / 2));
-  int cols = 1;
+  const bool held = row <= std::max(holds(512) * MAX_CLUSTER, holds(256));
+  Shape S = {};
+  S.cols = 1;
   if (held) {
-    while (row > holds(256, SMEM / 2) && row > whole * cols) cols *= 2;
-    while (cols < MAX_CLUSTER && (long)T * cols * 2 <= SMS && V / (cols * 2) >= 4096) cols *= 2;
+    while (row > holds(256) && row > holds(512) * S.cols) S.cols *= 2;
+    while (S.cols < MAX_CLUSTER && (long)T * S.cols * 2 <= SMS && V / (S.cols * 2) >= 4096) S.cols *= 2;
   }
-  A.slice = cols == 1 ? V : ((V + cols - 1) / cols + 63) / 64 * 64;
+  A.slice = S.cols == 1 ? V : ((V + S.cols - 1) / S.cols + 63) / 64 * 64;
   const long bytes = (long)A.slice * es;
-  const int threads = !held || bytes > holds(256, SMEM / 2) ? 512 : bytes > holds(128, SMEM / 4) ? 256 : 128;
-  A.log_d = threads == 512 ? 9 : threads == 256 ? 8 : 7;
-  A.rounds = std::max(U, (int)((bytes / 16 + threads - 1) / threads + U - 1) / U * U);
-  const int room = (int)(((threads == 512 ? SMEM : threads == 256 ? SMEM / 2 : SMEM / 4) - (long)entries) / (16 * threads));
-  A.lead = std::max(U, std::min({LEAD, A.rounds, (room - A.rounds - AHEAD) / U * U}));
-  A.slots = !held ? 0 : dlogits ? A.rounds + A.lead + AHEAD : AHEAD + U;
-  const size_t smem = entries + (size_t)16 * threads * A.slots;
-  const int ctas = std::max(1, std::min((int)(65536 / (REGS * (threads + 32 * TEACHERS))), (int)(227 * 1024 / (smem + 14 * 1024))));
-  const int groups = std::min(T, std::max(1, SMS * ctas / cols));
-  const bool two = ce_weight != 0.f && temperature != 1.f;
+  S.threads = !held || bytes > holds(256) ? 512 : bytes > holds(128) ? 256 : 128;
+  A.log_d = S.threads == 512 ? 9 : S.threads == 256 ? 8 : 7;
+  A.rounds = std::max(U, (int)((bytes / 16 + S.threads - 1) / S.threads + U - 1) / U * U);
+  const long room = (places(S.threads) - A.rounds - ahead_of(true)) / U * U;
+  A.lead = (int)std::max<long>(U, std::min<long>({LEAD, A.rounds, room}));
+  A.slots = !grad ? ahead_of(false) + U : held ? A.rounds + A.lead + ahead_of(true) : 0;
+  S.smem = entries + (size_t)16 * S.threads * A.slots;
+  const int ctas = std::max(1, std::min((int)(65536 / (REGS * (S.threads + 32 * TEACHERS))), (int)(227 * 1024 / (S.smem + 14 * 1024))));
+  S.groups = std::min(T, std::max(1, SMS * ctas / S.cols));
   cudaStream_t s = (cudaStream_t)stream;
-  return dtype == LX_BF16 ? launch_type<__nv_bfloat16>(A, two, threads, cols, groups, smem, s)
-                          : launch_type<float>(A, two, threads, cols, groups, smem, s);
+  return dtype == LX_BF16 ? launch_type<__nv_bfloat16>(A, S, s) : launch_type<float>(A, S, s);
 }
