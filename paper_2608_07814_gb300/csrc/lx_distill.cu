@@ -49,7 +49,7 @@ constexpr int MAX_WARPS = 16;    // data warps of a CTA
 constexpr int TEACHERS = 2;      // warps that prepare entries
 constexpr int BUFS = 4;          // rows whose entries are held, a multiple of TEACHERS
 constexpr int MAX_CLUSTER = 8;
-constexpr int SMEM = 219392;     // dynamic shared memory of an SM's CTAs at most
+constexpr int SMEM = 218880;     // dynamic shared memory of an SM's CTAs at most
 constexpr int U = 2;             // pieces of a thread taken together
 // pieces asked for before they are used, a multiple of U: rows held for a gradient leave
 // less room
@@ -240,6 +240,10 @@ k_distill(const __grid_constant__ DistillArgs A) {
   // the warps' sums of SENDS rows, and of a row that is done again
   __shared__ float4 red[SENDS + 2][CL ? MAX_CLUSTER : 1][MAX_WARPS];
   __shared__ Result res[BUFS];
+  __shared__ struct {
+    Result r;
+    Factors f;
+  } own[MAX_WARPS];  // a data warp's copy for its odd pieces, which keep no registers
   __shared__ float msum[BUFS];
   __shared__ uint64_t sums_bar[SENDS + 2], ready_bar[BUFS], result_bar[BUFS], released_bar[BUFS];
   __shared__ volatile int gave_up;
@@ -397,8 +401,12 @@ k_distill(const __grid_constant__ DistillArgs A) {
     }
   } else {
     const int v0 = rank * A.slice, vn = min(A.slice, A.V - v0);
-    const char* const slot = (const char*)(distill_smem + (4 * BUFS * E1 + TEACHERS * A.table + 3) / 4 + tid);
-    const uint32_t slot_at = (uint32_t)__cvta_generic_to_shared(slot);
+    const uint32_t slot = (uint32_t)__cvta_generic_to_shared(distill_smem + (4 * BUFS * E1 + TEACHERS * A.table + 3) / 4 + tid);
+    auto from_slot = [](uint32_t at) {
+      uint4 q;
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(at) : "memory");
+      return q;
+    };
     const uint32_t apart = D * 16, batch = U * apart, ring = A.slots * apart;  // bytes between a thread's pieces
     auto advance = [&](uint32_t& k) { k = k + batch == ring ? 0 : k + batch; };
     auto span = [&](unsigned t) { return Span<T>((const T*)A.logits + (long)(t < T0 ? t : first) * A.ld + v0, vn); };
@@ -414,7 +422,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
     auto copy = [](uint32_t dst, const void* src) {
       asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
     };
-    auto ask = [&](uint32_t to) {
+    auto ask_row = [&] {
       if (ask_rounds == 0) {
         const Span<T> S = span(ask_t);
         ask_at = S.piece(tid);
@@ -424,9 +432,12 @@ k_distill(const __grid_constant__ DistillArgs A) {
         ask_t += step;
         ask_w = weight(ask_t);
       }
+    };
+    auto ask = [&](uint32_t to) {
+      ask_row();
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (u < ask_left) copy(slot_at + to + u * apart, ask_at + (long)u * D * N);
+        if (u < ask_left) copy(slot + to + u * apart, ask_at + (long)u * D * N);
       asm volatile("cp.async.commit_group;" ::: "memory");
       ask_at += (long)U * D * N;
       ask_left -= U;
@@ -523,7 +534,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
         uint4 q[U];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          q[u] = feed_p + u < feed_n ? *(const uint4*)(slot + k1 + u * apart) : no_piece<T>();
+          q[u] = feed_p + u < feed_n ? from_slot(slot + k1 + u * apart) : no_piece<T>();
         take(feed, q);
       }
       advance(k1);
@@ -533,16 +544,17 @@ k_distill(const __grid_constant__ DistillArgs A) {
     // asks for and takes a row's batches where there is no second pass
     auto feed_only = [&] {
       for (int p = 0; p < A.rounds;) {
-        const int run = min(min(feed_whole - feed_p, A.rounds - feed_p - U), min(ask_whole, ask_rounds)) / U;
+        ask_row();
+        const int run = min(feed_whole - feed_p, min(ask_whole, ask_rounds)) / U;
         for (int i = 0; i < run; ++i) {
           uint4 x[U];
 #pragma unroll
-          for (int u = 0; u < U; ++u) copy(slot_at + k0 + u * apart, (const char*)ask_at + u * apart);
+          for (int u = 0; u < U; ++u) copy(slot + k0 + u * apart, (const char*)ask_at + u * apart);
           asm volatile("cp.async.commit_group;" ::: "memory");
           advance(k0);
           asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD / U) : "memory");
 #pragma unroll
-          for (int u = 0; u < U; ++u) x[u] = *(const uint4*)(slot + k1 + u * apart);
+          for (int u = 0; u < U; ++u) x[u] = from_slot(slot + k1 + u * apart);
           take(feed, x);
           advance(k1);
           ask_at += (long)U * D * N;
@@ -553,6 +565,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
           ask_left -= run * U;
           ask_whole -= run * U;
           ask_rounds -= run * U;
+          if (feed_p == A.rounds) feed_end();
         } else {
           ask(k0);
           advance(k0);
@@ -643,7 +656,16 @@ k_distill(const __grid_constant__ DistillArgs A) {
         const bool same = (((uintptr_t)dz ^ (uintptr_t)S.row) & 15) == 0;
         Factors f = {};
         if (!dead) f = factors(A, r, w, msum[b], eid[b * E1 + A.K], TWO);
-        auto value = [&](float z) { return dead ? 0.f : f.value(r, z, ct, TWO); };
+        // the elements outside the pieces
+        if (tid < S.edges) {
+          const int e = S.edge(tid);
+          dz[e] = from_f32<T>(dead ? 0.f : f.value(r, to_f32(S.row[e]), ct, TWO));
+        }
+        if (lane == 0) {
+          own[warp].r = r;
+          own[warp].f = f;
+        }
+        __syncwarp();
         // bf16: the factors go into the exponents (a 2^x = 2^(x + log2 a), which rounds to
         // about 1e-6 of the value); fp32, and a negative factor: multiplied
         constexpr bool FOLD = sizeof(T) == 2;
@@ -668,15 +690,16 @@ k_distill(const __grid_constant__ DistillArgs A) {
         const bool slow = r.again || (FOLD && (f.pa < 0.f || f.pb < 0.f));
         // a piece of a row that is dead or slow, or whose gradient starts elsewhere within
         // 16 bytes
-        auto odd_piece = [&](const uint4* from, T* out) {
-          uint4 x = make_uint4(0u, 0u, 0u, 0u);
-          if (!dead) {
-            x = *from;
+        auto odd_piece = [&](uint4 x, T* out) {
+          if (dead) {
+            x = make_uint4(0u, 0u, 0u, 0u);
+          } else {
             if (slow) {
               float2 v[N2];
               unpack<T>(x, v);
 #pragma unroll
-              for (int j = 0; j < N2; ++j) v[j] = make_float2(value(v[j].x), value(v[j].y));
+              for (int j = 0; j < N2; ++j)
+                v[j] = make_float2(own[warp].f.value(own[warp].r, v[j].x, ct, TWO), own[warp].f.value(own[warp].r, v[j].y, ct, TWO));
               x = pack<T>(v);
             } else {
               x = gradient(x);
@@ -698,9 +721,9 @@ k_distill(const __grid_constant__ DistillArgs A) {
           int p = 0;
           while (p < A.rounds) {
             // batches in which every thread has its pieces of this row, of the first pass's
-            // and of the one that is asked for, none of which ends before
-            const int f_left = min(feed_whole - feed_p, A.rounds - feed_p - U);
-            const int run = min(min(whole - p, f_left), min(ask_whole, ask_rounds)) / U;
+            // and of the one that is asked for
+            ask_row();
+            const int run = min(min(whole - p, feed_whole - feed_p), min(ask_whole, ask_rounds)) / U;
             if (run > 0) {
               char* o = out + (size_t)p * apart;
               const char* a = (const char*)ask_at;
@@ -708,7 +731,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
                 uint4 x[U];
                 if (!dead) {
 #pragma unroll
-                  for (int u = 0; u < U; ++u) x[u] = *(const uint4*)(slot + k2 + u * apart);
+                  for (int u = 0; u < U; ++u) x[u] = from_slot(slot + k2 + u * apart);
 #pragma unroll
                   for (int u = 0; u < U; ++u) x[u] = gradient(x[u]);
                 } else {
@@ -718,12 +741,12 @@ k_distill(const __grid_constant__ DistillArgs A) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) *(uint4*)(o + u * apart) = x[u];
 #pragma unroll
-                for (int u = 0; u < U; ++u) copy(slot_at + k2 + u * apart, a + u * apart);  // the places are free
+                for (int u = 0; u < U; ++u) copy(slot + k2 + u * apart, a + u * apart);  // the places are free
                 asm volatile("cp.async.commit_group;" ::: "memory");
                 advance(k2);
                 asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD / U) : "memory");
 #pragma unroll
-                for (int u = 0; u < U; ++u) x[u] = *(const uint4*)(slot + k1 + u * apart);
+                for (int u = 0; u < U; ++u) x[u] = from_slot(slot + k1 + u * apart);
                 take(feed, x);
                 advance(k1);
                 o += batch;
@@ -735,9 +758,10 @@ k_distill(const __grid_constant__ DistillArgs A) {
               ask_left -= run * U;
               ask_whole -= run * U;
               ask_rounds -= run * U;
+              if (feed_p == A.rounds) feed_end();
             } else {
               for (int u = 0; u < U && p + u < n; ++u)
-                odd_piece((const uint4*)(slot + k2 + u * apart), (T*)(out + (size_t)(p + u) * apart));
+                odd_piece(from_slot(slot + k2 + u * apart), (T*)(out + (size_t)(p + u) * apart));
               ask(k2);
               advance(k2);
               feed_batch();
@@ -746,13 +770,12 @@ k_distill(const __grid_constant__ DistillArgs A) {
           }
         } else {
           for (int p = 0; p < n; ++p) {
-            const uint4* from = (const uint4*)S.piece(p * D + tid);
+            const uint4 x = dead ? no_piece<T>() : *(const uint4*)S.piece(p * D + tid);
             T* o = (T*)(out + (size_t)p * apart);
-            if (plain && !dead) *(uint4*)o = gradient(*from);
-            else odd_piece(from, o);
+            if (plain && !dead) *(uint4*)o = gradient(x);
+            else odd_piece(x, o);
           }
         }
-        if (tid < S.edges) dz[S.edge(tid)] = from_f32<T>(value(dead ? 0.f : to_f32(S.row[S.edge(tid)])));
       }
       if constexpr (!HELD) feed_direct();
       __syncwarp();
