@@ -46,8 +46,8 @@ using namespace rows;
 
 constexpr int SMS = 152;
 constexpr int MAX_WARPS = 16;    // data warps of a CTA
-constexpr int TEACHERS = 2;      // warps that prepare entries
-constexpr int BUFS = 4;          // rows whose entries are held, a multiple of TEACHERS
+constexpr int BUFS = 4;          // rows whose entries are held
+constexpr int MAX_TEACHERS = 4;  // warps that prepare entries: 2, or 4 beside 16 data warps
 constexpr int MAX_CLUSTER = 8;
 constexpr int SMEM = 218880;     // dynamic shared memory of an SM's CTAs at most
 constexpr int U = 2;             // pieces of a thread taken together
@@ -75,6 +75,7 @@ struct DistillArgs {
   long ldd;
   int slice;   // columns of a CTA
   int log_d;   // log2 of a CTA's data threads
+  int teachers;
   int table;   // places of a table of ids, a power of two
   int rounds;  // pieces of a thread, rounded up to a multiple of U
   int slots;   // of them in shared memory at a time, a multiple of U
@@ -182,11 +183,11 @@ __device__ __forceinline__ void add_pieces(float& n, float2& p, const uint4* q, 
     }
     return s;
   };
-  float2 s = sum(-n);
-  if (fmaxf(s.x, s.y) > 1099511627776.f) {  // (a NaN goes on as it is)
+  float2 s;
+  if (n == LOWEST || (s = sum(-n), fmaxf(s.x, s.y) > 1099511627776.f)) {  // (a NaN goes on as it is)
     float mx = piece_max<T>(q[0]);
     for (int u = 1; u < U; ++u) mx = fmaxf(mx, piece_max<T>(q[u]));
-    const float N = ceilf(mx * c);
+    const float N = fmaxf(LOWEST, ceilf(mx * c));
     p = muls(p, both(ex2(n - N)));
     n = N;
     s = sum(-n);
@@ -231,10 +232,10 @@ __device__ __forceinline__ Factors factors(const DistillArgs& A, const Result& r
 extern __shared__ uint4 distill_smem[];
 
 // TWO: a hard-label term at another temperature than the teacher's.  HELD: rows fit shared
-// memory.  blockDim: the data threads and the TEACHERS' warps; gridDim: (CTAs of a row,
+// memory.  blockDim: the data threads and the teachers' warps; gridDim: (CTAs of a row,
 // rows)
 template <typename T, bool TWO, bool CL, bool HELD, bool GRAD>
-__global__ void __launch_bounds__(576, 1)
+__global__ void __launch_bounds__(640, 1)
 k_distill(const __grid_constant__ DistillArgs A) {
   constexpr int N = Span<T>::N, N2 = N / 2, AHEAD = ahead_of(GRAD);
   // the warps' sums of SENDS rows, and of a row that is done again
@@ -285,7 +286,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
   };
 
   if (teacher) {
-    // Row k of the CTA's (h, h + TEACHERS, ... are this warp's) has its entries in buffer
+    // Row k of the CTA's (h, h + A.teachers, ... are this warp's) has its entries in buffer
     // k % BUFS.
     const int h = warp - nw;
     int* table = (int*)(elq + BUFS * E1) + h * A.table;
@@ -355,9 +356,9 @@ k_distill(const __grid_constant__ DistillArgs A) {
       twice = __any_sync(0xffffffffu, twice);
       return twice;
     };
-    for (unsigned k = h; k < BUFS; k += TEACHERS) provide(k, first + k * step);
+    for (unsigned k = h; k < BUFS; k += A.teachers) provide(k, first + k * step);
     unsigned t = first + h * step;
-    for (unsigned k = h; t < T0; k += TEACHERS, t += TEACHERS * step) {
+    for (unsigned k = h; t < T0; k += A.teachers, t += A.teachers * step) {
       const int b = k % BUFS;
       const uint32_t parity = k / BUFS & 1;
       wait(&result_bar[b], parity);
@@ -401,7 +402,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
     }
   } else {
     const int v0 = rank * A.slice, vn = min(A.slice, A.V - v0);
-    const uint32_t slot = (uint32_t)__cvta_generic_to_shared(distill_smem + (4 * BUFS * E1 + TEACHERS * A.table + 3) / 4 + tid);
+    const uint32_t slot = (uint32_t)__cvta_generic_to_shared(distill_smem + (4 * BUFS * E1 + A.teachers * A.table + 3) / 4 + tid);
     auto from_slot = [](uint32_t at) {
       uint4 q;
       asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(at) : "memory");
@@ -802,7 +803,7 @@ lx_status launch_distill(const DistillArgs& A, int threads, int cols, int groups
   LX_CUDA(smem_cap_once((const void*)k_distill<T, TWO, CL, HELD, GRAD>, SMEM, dev, cap));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(cols, groups);
-  cfg.blockDim = dim3(threads + 32 * TEACHERS);
+  cfg.blockDim = dim3(threads + 32 * A.teachers);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
@@ -891,7 +892,7 @@ extern "C" lx_status lx_distill_loss(int32_t dtype, const void* logits, int64_t 
   A.table = 32;
   while (A.table < 2 * K) A.table *= 2;
   const bool grad = dlogits != nullptr;
-  const size_t entries = ((4 * BUFS * (size_t)(K + 1) + TEACHERS * A.table + 3) / 4) * 16;
+  const size_t entries = ((4 * BUFS * (size_t)(K + 1) + MAX_TEACHERS * A.table + 3) / 4) * 16;
   const long row = (long)V * es;
   auto places = [&](int threads) { return ((long)SMEM * threads / 512 - (long)entries) / (16 * threads); };
   auto holds = [&](int threads) {  // bytes of a row
@@ -907,13 +908,14 @@ extern "C" lx_status lx_distill_loss(int32_t dtype, const void* logits, int64_t 
   A.slice = S.cols == 1 ? V : ((V + S.cols - 1) / S.cols + 63) / 64 * 64;
   const long bytes = (long)A.slice * es;
   S.threads = !held || bytes > holds(256) ? 512 : bytes > holds(128) ? 256 : 128;
+  A.teachers = S.threads == 512 ? MAX_TEACHERS : 2;
   A.log_d = S.threads == 512 ? 9 : S.threads == 256 ? 8 : 7;
   A.rounds = std::max(U, (int)((bytes / 16 + S.threads - 1) / S.threads + U - 1) / U * U);
   const long room = (places(S.threads) - A.rounds - ahead_of(true)) / U * U;
   A.lead = (int)std::max<long>(U, std::min<long>({LEAD, A.rounds, room}));
   A.slots = !grad ? ahead_of(false) + U : held ? A.rounds + A.lead + ahead_of(true) : 0;
   S.smem = entries + (size_t)16 * S.threads * A.slots;
-  const int ctas = std::max(1, std::min((int)(65536 / (REGS * (S.threads + 32 * TEACHERS))), (int)(227 * 1024 / (S.smem + 14 * 1024))));
+  const int ctas = std::max(1, std::min((int)(65536 / (REGS * (S.threads + 32 * A.teachers))), (int)(227 * 1024 / (S.smem + 14 * 1024))));
   S.groups = std::min(T, std::max(1, SMS * ctas / S.cols));
   cudaStream_t s = (cudaStream_t)stream;
   return dtype == LX_BF16 ? launch_type<__nv_bfloat16>(A, S, s) : launch_type<float>(A, S, s);
