@@ -7,8 +7,8 @@
 //   dl = dloss p (alpha E / (n^2 k) (c_e - sum_j c_j p_j) + 2 beta / n lse).
 //
 // Both are bound by reading the logits (and writing their gradient) once.  A token's
-// row is held in the registers of 4 to 32 lanes (16 logits a lane, 32 above 512
-// experts), so that a warp has several rows in flight and the shuffles of a row's
+// row is held in the registers of 1 to 32 lanes (16 logits a lane; the forward 32 above 64
+// experts, the backward above 512), so that a warp has several rows in flight and the shuffles of a row's
 // maximum and sums serve all of them; the forward loads a lane's next row before it
 // works on one.  The column sums of p stay in registers over the rows of a lane and are
 // added up per CTA, then over the CTAs by a second launch that starts beside the first's
@@ -425,7 +425,7 @@ static_assert(LX_MAX_EXPERTS * 4 * (1 + BAL_WARPS) <= 47 * 1024, "no more shared
 
 // Lanes to a row
 int lanes_of(int E, bool bwd) {
-  int g = 4;
+  int g = 1;
   while (g < 32 && g * (bwd || E <= 64 ? 16 : 32) < E) g *= 2;
   return g;
 }
@@ -438,7 +438,9 @@ lx_status launch_bal(const BalArgs& A, int grid, size_t smem, cudaStream_t s) {
     else k_balance_fwd<T, VEC, G, EPL><<<grid, BAL_THREADS, smem, s>>>(A);           \
   }
   const int lanes = lanes_of(A.E, BWD);
-  if (A.E <= 64) LX_BAL_CASE(4, 16)
+  if (A.E <= 16) LX_BAL_CASE(1, 16)
+  else if (A.E <= 32) LX_BAL_CASE(2, 16)
+  else if (A.E <= 64) LX_BAL_CASE(4, 16)
   else if (A.E > 512) LX_BAL_CASE(32, 32)
   else if constexpr (BWD) {
     if (lanes == 8) LX_BAL_CASE(8, 16)

@@ -61,17 +61,21 @@ struct NormArgs {
 
 constexpr int REGS = 128;  // a thread: the launch bounds hold the compiler to these
 
+// bytes of the slots of one array's columns of a group: `members` threads' and a block more
+__host__ __device__ constexpr int group_bytes(int members, int es) { return members * EPT * es + 16; }
+
 enum Group { WARP = 0, CTA = 1, CLUSTER = 2, WIDE = 3 };  // WIDE: a cluster of larger CTAs
 constexpr int max_threads(int grp) { return grp == WIDE ? WIDE_T : CTA_T; }
 constexpr int max_cols(int grp) { return grp >= CLUSTER ? MAX_CLUSTER : 1; }
 
-template <int BYTES>
 __device__ __forceinline__ void copy_async(void* dst, const void* src) {
   const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
-  if constexpr (BYTES == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
-  else
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(d), "l"(src) : "memory");
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
+}
+// the first `bytes` of 16, the rest of them zero
+__device__ __forceinline__ void copy_async(void* dst, const void* src, uint32_t bytes) {
+  const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -79,24 +83,27 @@ __device__ __forceinline__ void copy_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-// The rows and columns of a thread, and the slots of its pieces.  Pieces are VEC
-// elements: 16 bytes, 4 bytes where rows do not start on 16-byte boundaries, or single
-// bf16 values, which cannot be copied asynchronously and are read where they are used
-// (as are the widest rows, whose slots would not fit).  Values are held as pairs, for
-// the two-wide fp32 instructions.
+// The rows and columns of a thread, and the slots of its pieces.  Where every row starts on
+// a 16-byte boundary, pieces are 16 bytes (VEC elements) and a thread copies its own.
+// Elsewhere (VEC = 1) a warp, or the part of one that holds a row, copies the 16-byte blocks
+// that its columns of the row touch, and a thread picks every 32nd element: the shift of a
+// row within its blocks is known when it is read.  (Single loads: 1031
+// rows of 2047 bf16 16.5 us forward, 33.2 backward; blocks 13.6, 27.2.)  The widest rows, whose slots would not fit, are read
+// where they are used.  Values are held as pairs.
 template <typename T, int VEC, int GRP>
 struct Rows {
-  static constexpr int NCH = EPT / VEC, BYTES = VEC * sizeof(T), MAX_T = max_threads(GRP), MAX_W = MAX_T / 32;
-  static constexpr bool RING = BYTES >= 4 && GRP != WIDE;
+  static constexpr int NCH = EPT / VEC, MAX_T = max_threads(GRP), MAX_W = MAX_T / 32;
+  static constexpr bool RING = GRP != WIDE, BLOCK = RING && VEC == 1;
   static constexpr int COLS = max_cols(GRP);
+  static_assert(VEC == 1 || VEC * sizeof(T) == 16, "single elements or 16 bytes");
   const NormArgs& A;
-  char* ring;     // the thread's first slot
+  char* ring;     // the thread's first slot (BLOCK: its group's)
   uint32_t at;    // the round's stage, in bytes
   int lane, size;  // of the threads that hold a row
   int col0;        // first column of the thread
   int count;       // its pieces inside the row (they ascend)
   int row, step;   // first row; distance of this group's rows
-  __device__ Rows(const NormArgs& args, char* smem) : A(args), ring(smem + threadIdx.x * BYTES), at(0) {
+  __device__ Rows(const NormArgs& args, char* smem) : A(args), at(0) {
     int first = 0, end = A.H;
     if constexpr (GRP == WARP) {
       size = A.lanes;
@@ -113,7 +120,14 @@ struct Rows {
         end = min(A.H, first + MAX_T * EPT);
       }
     }
-    col0 = first + lane * VEC;
+    if constexpr (BLOCK) {
+      const int group = threadIdx.x / members();
+      col0 = (GRP == WARP ? 0 : first + group * 32 * EPT) + lane % members();
+      ring = smem + group * group_bytes(members(), sizeof(T));
+    } else {
+      col0 = first + lane * VEC;
+      ring = smem + threadIdx.x * 16;
+    }
     count = 0;
 #pragma unroll
     for (int c = 0; c < NCH; ++c) count += col(c) < end;
@@ -125,9 +139,20 @@ struct Rows {
     if constexpr (GRP == WARP) return __any_sync(0xffffffffu, t < (unsigned)A.T);
     else return t < (unsigned)A.T;
   }
-  __device__ int col(int c) const { return col0 + c * size * VEC; }
-  __device__ const T* src(int k, unsigned t) const {
-    return (const T*)((const char*)A.in[k] + (uint64_t)t * A.ldb[k]) + col0;
+  __device__ int members() const { return GRP == WARP ? size : 32; }  // BLOCK: threads of a group
+  __device__ int apart() const { return BLOCK ? members() : size * VEC; }  // columns between pieces
+  __device__ int seg() const { return col0 - lane % members(); }           // BLOCK: the group's first column,
+  __device__ int seg_n() const {                                           // and its columns
+    const int end = GRP >= CLUSTER ? min(A.H, (int)(blockIdx.x + 1) * MAX_T * EPT) : A.H;
+    return max(0, min(end - seg(), members() * EPT));
+  }
+  __device__ int col(int c) const { return BLOCK ? col0 + c * members() : col0 + c * size * VEC; }
+  __device__ const T* src(int k, unsigned t, int col) const {
+    return (const T*)((const char*)A.in[k] + (uint64_t)t * A.ldb[k]) + col;
+  }
+  // BLOCK: bytes from a 16-byte boundary to the group's first element
+  __device__ int shift(int k, unsigned t) const {
+    return ((uint32_t)(uintptr_t)A.in[k] + t * A.ldb[k] + (uint32_t)seg() * (uint32_t)sizeof(T)) & 15;
   }
   __device__ char* place(uint32_t stage, int k) const { return ring + (stage + A.slot_at[k]); }
   __device__ void fetch(uint32_t stage, unsigned t) const {
@@ -135,11 +160,32 @@ struct Rows {
 #pragma unroll
       for (int k = 0; k < N_IN; ++k)
         if (A.in[k]) {
-          const T* p = src(k, t);
           char* d = place(stage, k);
+          if constexpr (BLOCK) {
+            const int step_b = members() * 16, me = lane % members() * 16;
+            const int off = shift(k, t), bytes = off + seg_n() * (int)sizeof(T);  // from the first block on
+            const char* block = (const char*)src(k, t, seg()) - off + me;
+            d += me;
+            if (seg_n() > 0 && t != 0 && t != (unsigned)A.T - 1) {
+              for (int b = me; b < bytes; b += step_b, block += step_b, d += step_b)
+                copy_async(d, block);
+            } else if (seg_n() > 0) {
+              for (int b = me; b < bytes; b += step_b, block += step_b, d += step_b) {
+                if (block >= (const char*)A.in[k]) {
+                  // nothing is read behind the array's last element
+                  copy_async(d, block, (uint32_t)min((int64_t)16, (int64_t)((const char*)src(k, A.T - 1, A.H) - block)));
+                } else {  // nor before its first
+                  for (int j = 0; j < 16; j += sizeof(T))
+                    if (b + j >= off && b + j < bytes) *(T*)(d + j) = *(const T*)(block + j);
+                }
+              }
+            }
+          } else {
+            const T* p = src(k, t, col0);
 #pragma unroll
-          for (int c = 0; c < NCH; ++c)
-            if (c < count) copy_async<BYTES>(d + c * blockDim.x * BYTES, p + c * size * VEC);
+            for (int c = 0; c < NCH; ++c)
+              if (c < count) copy_async(d + c * blockDim.x * 16, p + c * size * VEC);
+          }
         }
     copy_commit();
   }
@@ -149,24 +195,26 @@ struct Rows {
   __device__ void begin() const {
     if constexpr (RING) {
       for (int s = 0; s < A.stages; ++s) {
+        if constexpr (!BLOCK) {
 #pragma unroll
-        for (int k = 0; k < N_IN; ++k)
-          if (A.in[k])
+          for (int k = 0; k < N_IN; ++k)
+            if (A.in[k])
 #pragma unroll
-            for (int c = 0; c < NCH; ++c)
-              if (c >= count)
-#pragma unroll
-                for (int q = 0; q < BYTES / 4; ++q)
-                  ((uint32_t*)(place(s * A.stage_bytes, k) + c * blockDim.x * BYTES))[q] = 0u;
+              for (int c = 0; c < NCH; ++c)
+                if (c >= count)
+                  *(uint4*)(place(s * A.stage_bytes, k) + c * blockDim.x * 16) = make_uint4(0u, 0u, 0u, 0u);
+        }
         if (s < A.stages - 1) fetch(s * A.stage_bytes, (unsigned)row + (unsigned)s * step);
       }
     }
   }
   __device__ void advance(unsigned t) const {
     if constexpr (RING) {
+      if constexpr (BLOCK) __syncwarp();  // the others have read the stage that is filled now
       fetch(at == 0 ? (A.stages - 1) * A.stage_bytes : at - A.stage_bytes, t + (unsigned)(A.stages - 1) * step);
       if (A.stages == 3) copy_wait<2>();
       else copy_wait<1>();
+      if constexpr (BLOCK) __syncwarp();  // what the others copied is here
     }
   }
   __device__ void next() { at = at + A.stage_bytes == A.stages * A.stage_bytes ? 0 : at + A.stage_bytes; }
@@ -176,14 +224,22 @@ struct Rows {
     read_half(k, t, v + N2 / 2, 1);
   }
   __device__ void read_half(int k, unsigned t, float2* v, int h) const {
-    const T* g = RING ? (const T*)place(at, k) : src(k, t);
-    const int apart = RING ? blockDim.x * VEC : size * VEC;
+    const T* g;
+    int step_c = apart();
+    if constexpr (BLOCK) {
+      g = (const T*)(place(at, k) + shift(k, t)) + lane % members();
+    } else if constexpr (RING) {
+      g = (const T*)place(at, k);
+      step_c = blockDim.x * VEC;
+    } else {
+      g = src(k, t, col0);
+    }
 #pragma unroll
     for (int c = 0; c < NCH / 2; ++c) {
       const int d = h * (NCH / 2) + c;
-      const bool on = RING || (d < count && t < (unsigned)A.T);
-      const T* p = g + d * apart;
-      if constexpr (BYTES == 16) {
+      const bool on = (RING && !BLOCK) || (d < count && t < (unsigned)A.T);
+      const T* p = g + d * step_c;
+      if constexpr (VEC > 1) {
         const uint4 w = on ? *(const uint4*)p : make_uint4(0u, 0u, 0u, 0u);
         if constexpr (sizeof(T) == 4) {
           v[2 * c] = make_float2(__uint_as_float(w.x), __uint_as_float(w.y));
@@ -194,15 +250,13 @@ struct Rows {
           v[4 * c + 2] = bf2(w.z);
           v[4 * c + 3] = bf2(w.w);
         }
-      } else if constexpr (VEC == 2) {
-        v[c] = bf2(on ? *(const uint32_t*)p : 0u);
       } else {
         const float x = on ? to_f32(*p) : 0.f;
         if (c & 1) v[c / 2].y = x;
         else v[c / 2].x = x;
       }
     }
-    if (GRP == WARP && RING && t >= (unsigned)A.T)  // what an earlier row left
+    if (GRP == WARP && RING && !BLOCK && t >= (unsigned)A.T)  // what an earlier row left
 #pragma unroll
       for (int i = 0; i < N2 / 2; ++i) v[i] = make_float2(0.f, 0.f);
   }
@@ -216,8 +270,8 @@ struct Rows {
 #pragma unroll
     for (int c = 0; c < NCH / 2; ++c)
       if (h * (NCH / 2) + c < count) {
-        T* p = g + (h * (NCH / 2) + c) * size * VEC;
-        if constexpr (BYTES == 16) {
+        T* p = BLOCK ? g + (h * (NCH / 2) + c) * members() : g + (h * (NCH / 2) + c) * size * VEC;
+        if constexpr (VEC > 1) {
           uint4 w;
           if constexpr (sizeof(T) == 4)
             w = make_uint4(__float_as_uint(v[2 * c].x), __float_as_uint(v[2 * c].y), __float_as_uint(v[2 * c + 1].x),
@@ -225,8 +279,6 @@ struct Rows {
           else
             w = make_uint4(to_bf2(v[4 * c]), to_bf2(v[4 * c + 1]), to_bf2(v[4 * c + 2]), to_bf2(v[4 * c + 3]));
           *(uint4*)p = w;
-        } else if constexpr (VEC == 2) {
-          *(uint32_t*)p = to_bf2(v[c]);
         } else {
           *p = from_f32<T>(c & 1 ? v[c / 2].y : v[c / 2].x);
         }
@@ -599,7 +651,7 @@ Shape shape_of(int T, int H) {
   s.grp = H <= WARP_H ? WARP : H <= CTA_T * EPT ? CTA : H <= CTA_T * EPT * MAX_CLUSTER ? CLUSTER : WIDE;
   s.threads = s.grp == CTA ? (H + 32 * EPT - 1) / (32 * EPT) * 32 : max_threads(s.grp);
   s.cols = s.grp >= CLUSTER ? (H + s.threads * EPT - 1) / (s.threads * EPT) : 1;
-  s.lanes = 1;
+  s.lanes = 4;  // (a group's slots have a block more than its columns)
   while (s.lanes < 32 && s.lanes * EPT < H) s.lanes *= 2;
   const int rows = s.grp == WARP ? CTA_T / s.lanes : 1;
   s.groups = ((long)T + rows - 1) / rows;
@@ -617,12 +669,13 @@ int resident(const Shape& s, size_t smem) {
 }
 
 // Slots of a CTA: three rows, or two where three would not fit beside the SM's other CTAs
-size_t ring_bytes(const Shape& s, NormArgs& A, size_t es, size_t more) {
+size_t ring_bytes(const Shape& s, NormArgs& A, size_t es, size_t more, bool block) {
+  const int members = s.grp == WARP ? s.lanes : 32;
   size_t row = 0;
   for (int k = 0; k < N_IN; ++k)
     if (A.in[k]) {
       A.slot_at[k] = (uint32_t)row;
-      row += EPT * es * s.threads;
+      row += block ? (size_t)(s.threads / members) * group_bytes(members, es) : EPT * es * s.threads;
     }
   A.stage_bytes = (uint32_t)row;
   A.stages = (3 * row + more + 1024) * ctas_per_sm(s) <= 227 * 1024 ? 3 : 2;
@@ -656,16 +709,17 @@ lx_status launch_one(const Shape& s, NormArgs& A, cudaStream_t st, int& groups) 
   const size_t par = BWD ? sizeof(float) * 2 * EPT * s.threads : 0;
   size_t smem = 0;
   A.stages = 2;
-  if (Rows<T, VEC, GRP>::RING) smem = ring_bytes(s, A, sizeof(T), par);
-  A.par_at = (uint32_t)smem;
+  if (Rows<T, VEC, GRP>::RING) smem = ring_bytes(s, A, sizeof(T), par, Rows<T, VEC, GRP>::BLOCK);
+  A.par_at = (uint32_t)smem;  // (a multiple of 16)
   smem += par;
   if (BWD && GRP == WARP) smem = std::max(smem, sizeof(float) * (CTA_T / s.lanes) * A.H);
   groups = resident(s, smem);
-  // A backward of few rows: a CTA an SM with its rows in flight, as long as that leaves
-  // a CTA under 7 rows: every CTA more writes column sums as large as a row (1031 rows of
-  // 2048 bf16: 152 CTAs 17.6 us, 304 19.2, 608 23.7; 4000 of 2560: 43.9, 36.0, 35.2).
-  // Rows that are read where they are used need all CTAs (1031 of 2047: 69.6, 48.3, 35.7).
-  if (BWD && GRP == CTA && Rows<T, VEC, GRP>::RING) groups = std::min(groups, std::max(SMS, A.T / 7));
+  // A backward of few rows: a CTA an SM (two where rows are copied in blocks) as long as that
+  // leaves a CTA under 7 rows: every CTA more writes column sums as large as a row (2048
+  // bf16: 300 rows 11.2 us with 152 CTAs, 13.4 with 304; 1031 rows 17.0, 16.5, 21.8 with 608;
+  // 4000 of 2560: 44.8, 33.6, 34.4; 1031 of 2047: 31.7, 27.2, 27.6).
+  using R = Rows<T, VEC, GRP>;
+  if (BWD && GRP == CTA && R::RING) groups = std::min(groups, std::max(R::BLOCK ? 2 * SMS : SMS, A.T / 7));
   if (BWD) return launch(k_resnorm_bwd<T, VEC, GRP>, s, groups, smem, A, st, cap);
   return launch(k_resnorm_fwd<T, VEC, GRP>, s, groups, smem, A, st, cap);
 }
@@ -678,15 +732,14 @@ lx_status launch_vec(const Shape& s, NormArgs& A, cudaStream_t st, int& groups) 
   return launch_one<T, VEC, WIDE, BWD>(s, A, st, groups);
 }
 
-// piece: bytes that divide every row's start and length (16, 4, or 2); groups: out, the
-// CTAs (clusters) launched
+// wide: every row starts on a 16-byte boundary and is a multiple of 16 bytes; groups: out,
+// the CTAs (clusters) launched
 template <bool BWD>
-lx_status launch_any(int dtype, int piece, const Shape& s, NormArgs& A, cudaStream_t st, int& groups) {
+lx_status launch_any(int dtype, bool wide, const Shape& s, NormArgs& A, cudaStream_t st, int& groups) {
   if (dtype == LX_F32)
-    return piece == 16 ? launch_vec<float, 4, BWD>(s, A, st, groups) : launch_vec<float, 1, BWD>(s, A, st, groups);
-  if (piece == 16) return launch_vec<__nv_bfloat16, 8, BWD>(s, A, st, groups);
-  if (piece == 4) return launch_vec<__nv_bfloat16, 2, BWD>(s, A, st, groups);
-  return launch_vec<__nv_bfloat16, 1, BWD>(s, A, st, groups);
+    return wide ? launch_vec<float, 4, BWD>(s, A, st, groups) : launch_vec<float, 1, BWD>(s, A, st, groups);
+  return wide ? launch_vec<__nv_bfloat16, 8, BWD>(s, A, st, groups)
+              : launch_vec<__nv_bfloat16, 1, BWD>(s, A, st, groups);
 }
 
 constexpr int64_t MAX_LD = (1 << 30) - 1;  // elements between rows: a distance in bytes fits 32 bits
@@ -743,13 +796,12 @@ NormArgs args_of(const lx_resnorm_desc* d, const Shape& s) {
   return A;
 }
 
-// The widest piece that divides every row's start and length: 16 bytes, 4, or one bf16
-int pieces(const NormArgs& A, size_t es, std::initializer_list<const void*> outs) {
+bool rows16(const NormArgs& A, size_t es, std::initializer_list<const void*> outs) {
   uintptr_t bits = (uintptr_t)A.H * es;
   for (int k = 0; k < N_IN; ++k)
     if (A.in[k]) bits |= (uintptr_t)A.in[k] | (uintptr_t)A.ldb[k];
   for (const void* p : outs) bits |= (uintptr_t)p;
-  return bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2;
+  return bits % 16 == 0;
 }
 
 }  // namespace
@@ -780,7 +832,7 @@ extern "C" lx_status lx_residual_norm(const lx_resnorm_desc* d, void* r_out, voi
   A.h_out = h_out;
   A.stats = stats;
   int groups;
-  return launch_any<false>(d->dtype, pieces(A, es, {r_out, h_out}), s, A, (cudaStream_t)stream, groups);
+  return launch_any<false>(d->dtype, rows16(A, es, {r_out, h_out}), s, A, (cudaStream_t)stream, groups);
 }
 
 extern "C" lx_status lx_residual_norm_workspace(int32_t T, int32_t H, uint64_t* bytes) {
@@ -848,7 +900,7 @@ extern "C" lx_status lx_residual_norm_backward(const lx_resnorm_desc* d, const f
   A.part = params ? (float*)workspace : nullptr;
   A.sums = (dw_post || dgc ? 1 : 0) | (dw_pre ? 2 : 0);
   int groups;
-  LX_TRY(launch_any<true>(d->dtype, pieces(A, es, {outs[0], outs[1], outs[2]}), s, A, st, groups));
+  LX_TRY(launch_any<true>(d->dtype, rows16(A, es, {outs[0], outs[1], outs[2]}), s, A, st, groups));
   if (params) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((d->H + 31) / 32, A.sums == 3 ? 2 : 1);
