@@ -7,17 +7,18 @@
 //   dz_v = w (a tau (m p_v - sum_{j: id_j = v} q_j) + b (softmax(z)_v - [v = label])).
 //
 // Bound by the logits: they are read from memory once and their gradient is written
-// once.  A CTA (or a cluster of CTAs, where a row is long or rows are few) works on one row
-// at a time.  Its threads hold their part of the row as 16-byte pieces in shared memory,
-// each thread its own (cp.async, no barrier between copy and use).  The first pass over a
-// row sums the exponentials against a running reference, an exchange joins the sums, the
-// second pass writes the gradient.  The passes run together, the first a row and `lead`
-// pieces before the second: a thread finishes a batch of pieces, asks for later ones in
-// their place, and takes the first pass's next batch, which was asked for AHEAD pieces ago.
-// So reads and writes go on all the time (with the passes one after the other all CTAs
-// drew on memory in the same halves of their rows), and a row's sums are on their way while
-// the second pass finishes the row before.  Rows that do not fit the shared memory of eight
-// CTAs are read a second time from L2.
+// once.  Short rows are held in registers (k_distill_short).  For the others a CTA (or a
+// cluster of CTAs, where a row is long or rows are few) works on one row at a time.  Its
+// threads hold their part of the row as 16-byte pieces in shared memory, each thread its own
+// (cp.async, no barrier between copy and use).  The first pass over a row sums the
+// exponentials against a running reference, an exchange joins the sums, the second pass
+// writes the gradient.  The passes run together, the first a row and `lead` pieces before
+// the second: a thread finishes a batch of pieces, asks for later ones in their place, and
+// takes the first pass's next batch, which was asked for AHEAD pieces ago.  So reads and
+// writes go on all the time (with the passes one after the other all CTAs drew on memory in
+// the same halves of their rows), and a row's sums are on their way while the second pass
+// finishes the row before.  Rows that do not fit the shared memory of eight CTAs are read a
+// second time from L2.
 //
 // Two warps of their own prepare the teacher's entries, up to four rows ahead (their chains
 // of loads take longer than a row), write the losses and, once the dense values of a row are
@@ -349,7 +350,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
       for (int j = lane; j < A.K; j += 32)
         if (id[j] >= 0)
           for (int i = id[j];; ++i) {
-            const int was = atomicCAS(&table[i & (A.table - 1)], -1, id[j]);
+            const int was = atomicCAS(table + (i & (A.table - 1)), -1, id[j]);
             twice |= was == id[j];
             if (was == -1 || was == id[j]) break;
           }
@@ -795,6 +796,210 @@ k_distill(const __grid_constant__ DistillArgs A) {
   }
 }
 
+// Rows of up to SHORT_P pieces for each thread of W warps, with few entries: the row stays in
+// registers, its maximum is known before its sums, and the warps of a row do everything
+// themselves.  A CTA takes one row (four rows of a warp each for the shortest) and many CTAs
+// share an SM, so that their chains of loads and sums hide one another; the next CTA starts
+// where one ends, since with a grid that just filled the SMs a late CTA ran alone (7929 rows
+// of 1000 bf16 with 5 entries: 34 us so, 16 us now).  Bound by the instructions of a row and
+// by its chains: 1400 issued in a warp for 1000 columns.  At 64 registers 32 warps fit an SM
+// (72 in the four-row form, which spills at 64): 5072 rows of 16384 take 80 us, and 92 us at
+// 80 registers.  Four pieces a thread and twice the warps: 122 us.
+constexpr int SHORT_P = 8, SHORT_K = 256;
+__host__ __device__ constexpr int short_threads(int w) { return w == 1 ? 128 : 32 * w; }
+
+template <typename T, bool TWO, int W>
+__global__ void __launch_bounds__(short_threads(W), W == 1 ? 7 : 1024 / short_threads(W))
+k_distill_short(const __grid_constant__ DistillArgs A) {
+  constexpr int N = Span<T>::N, N2 = N / 2, TH = 32 * W, GROUPS = short_threads(W) / TH;
+  __shared__ float part[W == 1 ? 1 : 3][3][W == 1 ? 1 : W];
+  const int g = threadIdx.x / TH, tid = threadIdx.x % TH, lane = tid & 31, warp = tid >> 5, E1 = A.K + 1;
+  int* const id = (int*)distill_smem + g * (3 * E1 + A.table);
+  float* const zj = (float*)(id + E1);
+  float* const q = zj + E1;
+  int* const table = (int*)(q + E1);
+  auto sync = [] {
+    if constexpr (W == 1) __syncwarp();
+    else __syncthreads();
+  };
+  // three values over the row's threads, the same in each; `turn`: a place of its own
+  auto over_row = [&](float (&v)[3], int turn, bool max) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) v[i] = max ? warp_max(v[i]) : warp_sum(v[i]);
+    if constexpr (W > 1) {
+      if (lane == 0)
+#pragma unroll
+        for (int i = 0; i < 3; ++i) part[turn][i][warp] = v[i];
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        v[i] = part[turn][i][0];
+#pragma unroll
+        for (int j = 1; j < W; ++j) v[i] = max ? fmaxf(v[i], part[turn][i][j]) : v[i] + part[turn][i][j];
+      }
+    } else {
+      __syncwarp();
+    }
+  };
+  const unsigned t = blockIdx.x * GROUPS + g;
+  if (t < (unsigned)A.T) {
+    const Span<T> S((const T*)A.logits + (long)t * A.ld, A.V);
+    const float w = A.weight ? A.weight[t] : 1.f;
+    const int n = (S.pieces - tid + TH - 1) / TH;
+    T* dz = A.dlogits ? (T*)A.dlogits + (long)t * A.ldd : nullptr;
+    const bool same = (((uintptr_t)dz ^ (uintptr_t)S.row) & 15) == 0;
+    uint4 x[SHORT_P];
+    float edge = -INFINITY, m[3] = {-INFINITY, -INFINITY, 0.f};  // maxima: of the row, of the entries
+    bool twice = false;
+    if (w != 0.f) {
+#pragma unroll
+      for (int p = 0; p < SHORT_P; ++p) x[p] = p < n ? *(const uint4*)S.piece(p * TH + tid) : no_piece<T>();
+      if (tid < S.edges) edge = to_f32(S.row[S.edge(tid)]);
+      for (int i = tid; i < A.table; i += TH) table[i] = -1;
+      for (int j = tid; j <= A.K; j += TH) {
+        const int e = j < A.K ? A.ids[(long)t * A.K + j] : A.labels ? A.labels[t] : -1;
+        const float v = j < A.K ? A.top[(long)t * A.K + j] : 0.f;
+        const bool ok = e >= 0 && e < A.V;
+        id[j] = ok ? e : -1;
+        zj[j] = ok ? to_f32(S.row[e]) : 0.f;
+        q[j] = ok ? v : -INFINITY;
+        if (j < A.K) m[1] = fmaxf(m[1], q[j]);
+      }
+      m[0] = edge;
+#pragma unroll
+      for (int p = 0; p < SHORT_P; ++p) m[0] = fmaxf(m[0], piece_max<T>(x[p]));
+    }
+    over_row(m, 0, true);
+    bool dead = w == 0.f || m[0] == -INFINITY;
+    // (a NaN is no maximum: a row of nothing else has the lowest one, and shows in its sums)
+    const float top = m[0], tm = m[1];
+    float s[3] = {0.f, 0.f, 0.f};  // sums of the row at both temperatures, and of the entries
+    if (w != 0.f && m[0] == -INFINITY) {
+      // all -inf, or nothing but -inf and NaN
+      float bad = edge != edge ? 1.f : 0.f;
+#pragma unroll
+      for (int p = 0; p < SHORT_P; ++p) {
+        float2 v[N2];
+        unpack<T>(x[p], v);
+#pragma unroll
+        for (int j = 0; j < N2; ++j) bad += v[j].x != v[j].x || v[j].y != v[j].y ? 1.f : 0.f;
+      }
+      s[0] = bad;
+    }
+    if (!dead) {
+      auto add = [&](float z) {
+        s[0] += ex2((z - top) * A.ct);
+        if (TWO) s[1] += ex2((z - top) * LOG2E);
+      };
+#pragma unroll
+      for (int p = 0; p < SHORT_P; ++p)
+        if (p < n) {
+          float2 v[N2];
+          unpack<T>(x[p], v);
+#pragma unroll
+          for (int j = 0; j < N2; ++j) {
+            add(v[j].x);
+            add(v[j].y);
+          }
+        }
+      if (tid < S.edges) add(edge);
+      for (int j = tid; j < A.K; j += TH)
+        if (id[j] >= 0 && tm != -INFINITY) s[2] += expf((q[j] - tm) / A.tau);
+    }
+    over_row(s, 1, false);
+    const bool nan_row = w != 0.f && m[0] == -INFINITY && s[0] > 0.f;
+    Result r = {0.f, nan_row ? NAN : s[0], 0.f, nan_row ? NAN : TWO ? s[1] : s[0], top, true};
+    if (nan_row) dead = false;
+    // the entries' probabilities: a thread keeps its own
+    float k[3] = {0.f, 0.f, 0.f};  // m, the divergence, entries that are repeated
+    if (!dead) {
+      const float lz = A.top_lse ? A.top_lse[t] - tm / A.tau : logf(s[2]), ls = logf(r.s);
+      for (int j = tid; j < A.K; j += TH) {
+        const float l = id[j] >= 0 && q[j] != -INFINITY ? (q[j] - tm) / A.tau - lz : -INFINITY;
+        const float p = expf(l);
+        q[j] = p;
+        k[0] += p;
+        if (p != 0.f) k[1] += p * (l - (r.rel(zj[j], A.ct) * LN2 - ls));
+        if (dz && id[j] >= 0)  // at least half of the table's places stay free
+          for (int i = id[j];; ++i) {
+            const int was = atomicCAS(table + (i & (A.table - 1)), -1, id[j]);
+            if (was == id[j]) k[2] = 1.f;
+            if (was == -1 || was == id[j]) break;
+          }
+      }
+    }
+    over_row(k, 2, false);
+    const int label = dead ? -1 : id[A.K];
+    if (tid == 0) {
+      float loss = 0.f;
+      if (!dead) {
+        loss = k[1] * A.a * A.tau * A.tau;
+        if (A.b != 0.f && label >= 0) loss += A.b * (logf(r.s1) - (TWO ? r.rel1(zj[A.K]) : r.rel(zj[A.K], A.ct)) * LN2);
+        loss *= w;
+      }
+      A.loss[t] = loss;
+    }
+    if (dz) {
+      Factors f = {};
+      if (!dead) f = factors(A, r, w, k[0], label, TWO);
+      auto value = [&](float z) { return dead ? 0.f : f.value(r, z, A.ct, TWO); };
+#pragma unroll
+      for (int p = 0; p < SHORT_P; ++p)
+        if (p < n) {
+          float2 v[N2];
+          unpack<T>(x[p], v);
+#pragma unroll
+          for (int j = 0; j < N2; ++j) v[j] = make_float2(value(v[j].x), value(v[j].y));
+          const uint4 o = pack<T>(v);
+          T* out = dz + S.head + (long)(p * TH + tid) * N;
+          if (same) {
+            *(uint4*)out = o;
+          } else {
+            const T* e = (const T*)&o;
+#pragma unroll
+            for (int j = 0; j < N; ++j) out[j] = e[j];
+          }
+        }
+      if (tid < S.edges) dz[S.edge(tid)] = from_f32<T>(value(edge));
+      sync();  // the dense values lie below the entries'
+      twice = k[2] != 0.f;
+      if (!dead)
+        for (int j = tid; j <= A.K; j += TH) {
+          const int e = id[j];
+          if (e < 0) continue;
+          float y = j < A.K ? q[j] : 0.f;
+          if (twice || e == label) {  // (the label may be one of the entries)
+            y = 0.f;
+            for (int i = 0; i < A.K; ++i) y += id[i] == e ? q[i] : 0.f;
+          }
+          dz[e] = from_f32<T>(value(zj[j]) - f.qa * y - (e == label ? f.hb : 0.f));
+        }
+    }
+  }
+}
+
+template <typename T, bool TWO, int W>
+lx_status launch_short(const DistillArgs& A, cudaStream_t s) {
+  constexpr int TH = short_threads(W), GROUPS = TH / (32 * W);
+  const size_t smem = (size_t)GROUPS * (3 * (A.K + 1) + A.table) * 4;
+  k_distill_short<T, TWO, W><<<(A.T + GROUPS - 1) / GROUPS, TH, smem, s>>>(A);
+  LX_CUDA(cudaGetLastError());
+  return LX_OK;
+}
+template <typename T>
+lx_status launch_short_any(const DistillArgs& A, cudaStream_t s) {
+  const long pieces = (long)A.V * sizeof(T) / 16;
+  const bool two = A.b != 0.f && A.tau != 1.f;
+#define LX_SHORT_CASE(W)                            \
+  if (pieces <= SHORT_P * 32 * W && A.K <= 32 * W) \
+    return two ? launch_short<T, true, W>(A, s) : launch_short<T, false, W>(A, s);
+  LX_SHORT_CASE(1)
+  LX_SHORT_CASE(2)
+  LX_SHORT_CASE(4)
+#undef LX_SHORT_CASE
+  return two ? launch_short<T, true, 8>(A, s) : launch_short<T, false, 8>(A, s);
+}
+
 template <typename T, bool TWO, bool CL, bool HELD, bool GRAD>
 lx_status launch_distill(const DistillArgs& A, int threads, int cols, int groups, size_t smem, cudaStream_t s) {
   static bool cap[64] = {};
@@ -884,13 +1089,20 @@ extern "C" lx_status lx_distill_loss(int32_t dtype, const void* logits, int64_t 
   const CallWaits waits = take_call_waits();
   A.wait_cycles = waits.cycles;
   A.unmet = waits.unmet == LX_WAIT_CALL_SUMS;
+  A.table = 32;
+  while (A.table < 2 * K) A.table *= 2;
+  cudaStream_t s = (cudaStream_t)stream;
+  // Rows that eight warps hold in registers.  Against the kernel with teachers' warps, us of
+  // bf16 rows with gradient: 7929 x 1000, K 5: 16 and 51; 7929 x 1006, K 256: 171 and 264;
+  // 512 x 16000, K 56: 13 and 17; 5072 x 16384, K 56: 80 and 87; 64 x 1006: 8 and 6.  With
+  // sixteen warps 5072 x 24000 takes 146, and 114 there.  (That kernel alone has the waits.)
+  if ((long)V * es / 16 <= SHORT_P * 32 * 8 && K <= SHORT_K && !A.unmet)
+    return dtype == LX_BF16 ? launch_short_any<__nv_bfloat16>(A, s) : launch_short_any<float>(A, s);
   // CTAs of 256 data threads with half of an SM's shared memory (128 and a quarter for short
   // rows) where a row fits it, else CTAs of 512 with all of it, as many as hold a row; rows
   // too long for eight of those are not held.  Few rows are spread over more CTAs, in slices
   // of 4096 columns at least.  The shape does not depend on whether a gradient is asked for,
   // so the losses do not either.
-  A.table = 32;
-  while (A.table < 2 * K) A.table *= 2;
   const bool grad = dlogits != nullptr;
   const size_t entries = ((4 * BUFS * (size_t)(K + 1) + MAX_TEACHERS * A.table + 3) / 4) * 16;
   const long row = (long)V * es;
@@ -917,6 +1129,5 @@ extern "C" lx_status lx_distill_loss(int32_t dtype, const void* logits, int64_t 
   S.smem = entries + (size_t)16 * S.threads * A.slots;
   const int ctas = std::max(1, std::min((int)(65536 / (REGS * (S.threads + 32 * A.teachers))), (int)(227 * 1024 / (S.smem + 14 * 1024))));
   S.groups = std::min(T, std::max(1, SMS * ctas / S.cols));
-  cudaStream_t s = (cudaStream_t)stream;
   return dtype == LX_BF16 ? launch_type<__nv_bfloat16>(A, S, s) : launch_type<float>(A, S, s);
 }
