@@ -472,7 +472,8 @@ LX_API lx_status lx_compress_factor(int32_t dtype, int32_t rows, int32_t cols, c
  * Standalone calls on plain device arrays; all parameters and statistics are fp32,
  * sums and norms are held in fp32, and results do not depend on scheduling.  Arrays
  * with a leading dimension (ld..., in elements) may be slices of wider ones; the
- * others are contiguous.
+ * others are contiguous.  Arrays of any alignment to their element are taken; rows that
+ * start on 16-byte boundaries are faster.
  */
 
 /*
@@ -499,6 +500,7 @@ LX_API lx_status lx_compress_factor(int32_t dtype, int32_t rows, int32_t cols, c
  *   workspace: device, 16-byte aligned, lx_residual_norm_workspace bytes; needed for
  *   dw_post, dw_pre and a channel gate's gradient
  *   T == 0: the parameter gradients are zeroed.
+ * Leading dimensions are below 2^30 elements.
  * Stream-ordered; no allocation.  Errors: LX_ERR_ARG (NULL, dtype, gate kind,
  * alignment to the element, overlap, workspace), LX_ERR_SHAPE (H, leading dimensions).
  */

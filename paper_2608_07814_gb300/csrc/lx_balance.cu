@@ -13,6 +13,8 @@
 // works on one.  The column sums of p stay in registers over the rows of a lane and are
 // added up per CTA, then over the CTAs by a second launch that starts beside the first's
 // last CTAs, each in a fixed order; one CTA finishes by itself.
+#include <cooperative_groups.h>
+
 #include <algorithm>
 
 #include "lx_rows.cuh"

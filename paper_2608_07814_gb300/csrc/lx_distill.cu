@@ -35,6 +35,8 @@
 // 2^n 2^(z log2(e) / tau - n), one fused multiply-add from z, exact in n.  A row whose every
 // logit lies below -2^30 powers of two sums to zero against the lowest reference and is done
 // again with its maximum subtracted first.
+#include <cooperative_groups.h>
+
 #include <algorithm>
 
 #include "lx_rows.cuh"
@@ -413,6 +415,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
     auto advance = [&](uint32_t& k) { k = k + batch == ring ? 0 : k + batch; };
     auto span = [&](unsigned t) { return Span<T>((const T*)A.logits + (long)(t < T0 ? t : first) * A.ld + v0, vn); };
     auto pieces_of = [&](const Span<T>& S) { return (S.pieces - tid + D - 1) >> log_d; };  // of this thread
+    auto whole_of = [&](const Span<T>& S) { return (S.pieces - (tid | 31) + D - 1) >> log_d; };  // of each of its warp's
 
     // The copies, a batch to a group, in the order of use: rows of weight 0 and pieces that
     // a thread does not have leave their slots as they are.
@@ -429,7 +432,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
         const Span<T> S = span(ask_t);
         ask_at = S.piece(tid);
         ask_left = ask_w != 0.f ? pieces_of(S) : 0;
-        ask_whole = ask_w != 0.f ? S.pieces >> log_d : 0;
+        ask_whole = ask_w != 0.f ? whole_of(S) : 0;
         ask_rounds = A.rounds;
         ask_t += step;
         ask_w = weight(ask_t);
@@ -511,7 +514,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
       feed = Run();
       feed_p = 0;
       feed_n = feed_w != 0.f ? pieces_of(S) : 0;
-      feed_whole = feed_w != 0.f ? S.pieces >> log_d : 0;
+      feed_whole = feed_w != 0.f ? whole_of(S) : 0;
       edges = feed_w != 0.f ? S.edges : 0;
       if (tid < edges) feed_edge = to_f32(S.row[S.edge(tid)]);
     };
@@ -719,11 +722,11 @@ k_distill(const __grid_constant__ DistillArgs A) {
         const int n = pieces_of(S);
         const bool plain = same && !slow;
         if constexpr (HELD) {
-          const int whole = plain ? S.pieces >> log_d : 0;  // pieces that every thread has
+          const int whole = plain ? whole_of(S) : 0;
           int p = 0;
           while (p < A.rounds) {
-            // batches in which every thread has its pieces of this row, of the first pass's
-            // and of the one that is asked for
+            // batches in which every thread of the warp has its pieces of this row, of the first
+            // pass's and of the one that is asked for
             ask_row();
             const int run = min(min(whole - p, feed_whole - feed_p), min(ask_whole, ask_rounds)) / U;
             if (run > 0) {
@@ -762,8 +765,14 @@ k_distill(const __grid_constant__ DistillArgs A) {
               ask_rounds -= run * U;
               if (feed_p == A.rounds) feed_end();
             } else {
-              for (int u = 0; u < U && p + u < n; ++u)
-                odd_piece(from_slot(slot + k2 + u * apart), (T*)(out + (size_t)(p + u) * apart));
+              if (plain && !dead) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                  if (p + u < n) *(uint4*)(out + (size_t)(p + u) * apart) = gradient(from_slot(slot + k2 + u * apart));
+              } else {
+                for (int u = 0; u < U && p + u < n; ++u)
+                  odd_piece(from_slot(slot + k2 + u * apart), (T*)(out + (size_t)(p + u) * apart));
+              }
               ask(k2);
               advance(k2);
               feed_batch();

@@ -20,6 +20,8 @@
 // and keeps its columns' parameters in registers.  In the backward it also keeps their
 // gradient sums there; the CTAs' sums are added in order by a second launch, so results
 // do not change from run to run.
+#include <cooperative_groups.h>
+
 #include <algorithm>
 
 #include "lx_rows.cuh"

@@ -1,43 +1,21 @@
 // Helpers of the row-wise operators (block norms, router balance loss,
-// distillation): 16-byte or single-element pieces of a row held as fp32, and sums
-// over a warp, a CTA and a cluster of CTAs in a fixed order.
+// distillation): 16-byte or single-element pieces of a row held as fp32, operations on
+// pairs of them, sums over a warp, and the entry points' checks of addresses.
 #pragma once
-
-#include <cooperative_groups.h>
 
 #include "lx_internal.cuh"
 
 namespace lx {
 namespace rows {
 
-// VEC consecutive elements at p as fp32; VEC * sizeof(T) is 16 (p 16-byte aligned) or
-// VEC is 1
-template <typename T, int VEC>
-__device__ __forceinline__ void load(const T* p, float* v) {
-  if constexpr (VEC == 1) {
-    v[0] = to_f32(*p);
-  } else {
-    static_assert(VEC * sizeof(T) == 16, "one 16-byte piece");
-    const uint4 q = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(w[j]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {  // a bf16 is the upper half of its fp32
-        v[2 * j] = __uint_as_float(w[j] << 16);
-        v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-      }
-    }
-  }
-}
-
+// VEC fp32 values to consecutive elements at p; VEC * sizeof(T) is 16 (p 16-byte aligned)
+// or VEC is 1
 template <typename T, int VEC>
 __device__ __forceinline__ void store(T* p, const float* v) {
   if constexpr (VEC == 1) {
     *p = from_f32<T>(v[0]);
   } else {
+    static_assert(VEC * sizeof(T) == 16, "one 16-byte piece");
     uint32_t w[4];
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
@@ -99,30 +77,6 @@ __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
-}
-
-// Sum of v over the CTA (CL = false) or over the cluster, the same in every thread.
-// buf: [2][32] floats of shared memory, the two halves used in turn (`turn` is the
-// caller's, zero at first): a thread can only write a half again after every thread
-// has passed the barrier that follows its reads.
-template <bool CL>
-__device__ __forceinline__ float group_sum(float v, float (*buf)[32], int& turn) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = (blockDim.x + 31) >> 5;
-  float* b = buf[turn & 1];
-  ++turn;
-  v = warp_sum(v);
-  if (lane == 0) b[warp] = v;
-  if constexpr (!CL) {
-    __syncthreads();
-    return warp_sum(lane < nw ? b[lane] : 0.f);
-  } else {
-    cooperative_groups::cluster_group cl = cooperative_groups::this_cluster();
-    cl.sync();
-    float s = 0.f;
-    for (unsigned c = 0; c < cl.num_blocks(); ++c)
-      s += warp_sum(lane < nw ? cl.map_shared_rank(b, c)[lane] : 0.f);
-    return s;
-  }
 }
 
 inline bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
