@@ -32,12 +32,13 @@
 // more.
 //
 // The reference of a sum is a whole number n of powers of two: exp(z / tau) is taken as
-// 2^n 2^(z log2(e) / tau - n), one fused multiply-add from z, exact in n.  A row whose every
-// logit lies below -2^30 powers of two sums to zero against the lowest reference and is done
-// again with its maximum subtracted first.
+// 2^n 2^(z log2(e) / tau - n), one fused multiply-add from z, exact in n.  A row whose
+// largest logit lies some 2^30 powers of two from zero or further, where n is off by its own
+// rounding, sums to zero or infinity and is done again with its maximum subtracted first.
 #include <cooperative_groups.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "lx_rows.cuh"
 #include "lx_tcgen05.cuh"
@@ -90,6 +91,12 @@ struct DistillArgs {
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ float lg2(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 
@@ -231,6 +238,44 @@ __device__ __forceinline__ Factors factors(const DistillArgs& A, const Result& r
   f.pa = f.qa * m / r.s + (two ? 0.f : f.pb);
   return f;
 }
+
+// The gradient of a piece.  bf16: the factors go into the exponents (a 2^x = 2^(x + log2 a),
+// which rounds to 5e-5 of the value at most while the reference is below 2^10, a fortieth of
+// what the bf16 rounds to); fp32: multiplied.
+template <typename T, bool TWO>
+struct Gradient {
+  static constexpr int N2 = 8 / sizeof(T);
+  static constexpr bool FOLD = sizeof(T) == 2;
+  float ct;
+  float2 pa2, pb2, neg, neg1;
+  __device__ Gradient(const DistillArgs& A, const Result& r, const Factors& f)
+      : ct(A.ct),
+        pa2(both(f.pa)),
+        pb2(both(f.pb)),
+        neg(both((FOLD ? lg2(f.pa) : 0.f) - r.n)),
+        neg1(both((FOLD ? lg2(f.pb) : 0.f) - r.n1)) {}
+  // whether it does not hold: negative factors, references that would swallow the factors,
+  // and a maximum that was subtracted
+  __device__ static bool slow(const Result& r, const Factors& f) {
+    return r.again || (FOLD && (f.pa < 0.f || f.pb < 0.f || fmaxf(fabsf(r.n), TWO ? fabsf(r.n1) : 0.f) > 1024.f));
+  }
+  __device__ uint4 operator()(uint4 x4) const {
+    float2 v[N2];
+    unpack<T>(x4, v);
+#pragma unroll
+    for (int j = 0; j < N2; ++j) {
+      const float2 x = fmas(v[j], both(ct), neg);
+      float2 o = make_float2(ex2(x.x), ex2(x.y));
+      if (!FOLD) o = muls(o, pa2);
+      if (TWO) {
+        const float2 x1 = fmas(v[j], both(LOG2E), neg1), o1 = make_float2(ex2(x1.x), ex2(x1.y));
+        o = FOLD ? adds(o, o1) : fmas(o1, pb2, o);
+      }
+      v[j] = o;
+    }
+    return pack<T>(v);
+  }
+};
 
 extern __shared__ uint4 distill_smem[];
 
@@ -620,7 +665,12 @@ k_distill(const __grid_constant__ DistillArgs A) {
       if (!dead) {
         Run run = receive(got % SENDS, (uint32_t)(got / SENDS) & 1);
         ++got;
-        if (run.s == 0.f) {  // every logit is -inf or out of the references' reach
+        // Every logit is -inf, or the largest is out of the references' reach: the sum against
+        // a reference that is off by its own rounding is nothing or infinite (NaN, once joined
+        // to another's); or there is a NaN.
+        auto off = [](float s) { return !(s > 0.f && s < INFINITY); };
+        if ((off(run.s) || (TWO && off(run.s1))) && !__any_sync(0xffffffffu, lost)) {
+          const bool nan = run.s != run.s || run.s1 != run.s1;
           r.again = true;
           float top = -INFINITY;
           for (int i = tid; i < S.pieces; i += D) top = fmaxf(top, piece_max<T>(*(const uint4*)S.piece(i)));
@@ -633,7 +683,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
           for (int j = lane; j < cols * MAX_WARPS; j += 32)
             if ((j & (MAX_WARPS - 1)) < nw) top = fmaxf(top, red[SENDS][j / MAX_WARPS][j & (MAX_WARPS - 1)].x);
           r.top = top = warp_max(top);
-          dead = top == -INFINITY;
+          dead = top == -INFINITY && !nan;
           run = Run();
           run.n = run.n1 = 0.f;
           if (!dead) {
@@ -671,28 +721,8 @@ k_distill(const __grid_constant__ DistillArgs A) {
           own[warp].f = f;
         }
         __syncwarp();
-        // bf16: the factors go into the exponents (a 2^x = 2^(x + log2 a), which rounds to
-        // about 1e-6 of the value); fp32, and a negative factor: multiplied
-        constexpr bool FOLD = sizeof(T) == 2;
-        const float2 pa2 = both(f.pa), pb2 = both(f.pb);
-        const float2 neg = both((FOLD ? __log2f(f.pa) : 0.f) - r.n), neg1 = both((FOLD ? __log2f(f.pb) : 0.f) - r.n1);
-        auto gradient = [&](uint4 x4) {
-          float2 v[N2];
-          unpack<T>(x4, v);
-#pragma unroll
-          for (int j = 0; j < N2; ++j) {
-            const float2 x = fmas(v[j], both(ct), neg);
-            float2 o = make_float2(ex2(x.x), ex2(x.y));
-            if (!FOLD) o = muls(o, pa2);
-            if (TWO) {
-              const float2 x1 = fmas(v[j], both(LOG2E), neg1), o1 = make_float2(ex2(x1.x), ex2(x1.y));
-              o = FOLD ? adds(o, o1) : fmas(o1, pb2, o);
-            }
-            v[j] = o;
-          }
-          return pack<T>(v);
-        };
-        const bool slow = r.again || (FOLD && (f.pa < 0.f || f.pb < 0.f));
+        const Gradient<T, TWO> gradient(A, r, f);
+        const bool slow = gradient.slow(r, f);
         // a piece of a row that is dead or slow, or whose gradient starts elsewhere within
         // 16 bytes
         auto odd_piece = [&](uint4 x, T* out) {
@@ -812,7 +842,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
 // where one ends, since with a grid that just filled the SMs a late CTA ran alone (7929 rows
 // of 1000 bf16 with 5 entries: 34 us so, 16 us now).  Bound by the instructions of a row and
 // by its chains: 1400 issued in a warp for 1000 columns.  At 64 registers 32 warps fit an SM
-// (72 in the four-row form, which spills at 64): 5072 rows of 16384 take 80 us, and 92 us at
+// (72 in the four-row form, which spills at 64): 5072 rows of 16384 take 78 us, and 92 us at
 // 80 registers.  Four pieces a thread and twice the warps: 122 us.
 constexpr int SHORT_P = 8, SHORT_K = 256;
 __host__ __device__ constexpr int short_threads(int w) { return w == 1 ? 128 : 32 * w; }
@@ -882,6 +912,10 @@ k_distill_short(const __grid_constant__ DistillArgs A) {
     bool dead = w == 0.f || m[0] == -INFINITY;
     // (a NaN is no maximum: a row of nothing else has the lowest one, and shows in its sums)
     const float top = m[0], tm = m[1];
+    // the references are whole numbers of powers of two while they and what they are off by
+    // are small enough, else the maximum is subtracted first
+    const float ref = rintf(top * A.ct), ref1 = rintf(top * LOG2E);
+    Result r = {ref, 0.f, TWO ? ref1 : ref, 0.f, top, !(fmaxf(fabsf(ref), TWO ? fabsf(ref1) : 0.f) <= -LOWEST)};
     float s[3] = {0.f, 0.f, 0.f};  // sums of the row at both temperatures, and of the entries
     if (w != 0.f && m[0] == -INFINITY) {
       // all -inf, or nothing but -inf and NaN
@@ -896,28 +930,40 @@ k_distill_short(const __grid_constant__ DistillArgs A) {
       s[0] = bad;
     }
     if (!dead) {
-      auto add = [&](float z) {
-        s[0] += ex2((z - top) * A.ct);
-        if (TWO) s[1] += ex2((z - top) * LOG2E);
-      };
+      float2 sum = make_float2(0.f, 0.f), sum1 = sum;
+      auto add = [&](auto again) {
 #pragma unroll
-      for (int p = 0; p < SHORT_P; ++p)
-        if (p < n) {
-          float2 v[N2];
-          unpack<T>(x[p], v);
+        for (int p = 0; p < SHORT_P; ++p)
+          if (p < n) {
+            float2 v[N2];
+            unpack<T>(x[p], v);
 #pragma unroll
-          for (int j = 0; j < N2; ++j) {
-            add(v[j].x);
-            add(v[j].y);
+            for (int j = 0; j < N2; ++j) {
+              const float2 d = again ? make_float2(v[j].x - top, v[j].y - top) : v[j];
+              const float2 e = again ? muls(d, both(A.ct)) : fmas(d, both(A.ct), both(-r.n));
+              sum = adds(sum, make_float2(ex2(e.x), ex2(e.y)));
+              if (TWO) {
+                const float2 e1 = again ? muls(d, both(LOG2E)) : fmas(d, both(LOG2E), both(-r.n1));
+                sum1 = adds(sum1, make_float2(ex2(e1.x), ex2(e1.y)));
+              }
+            }
           }
-        }
-      if (tid < S.edges) add(edge);
+      };
+      if (r.again) add(std::true_type{});
+      else add(std::false_type{});
+      if (tid < S.edges) {
+        sum.x += ex2(r.rel(edge, A.ct));
+        if (TWO) sum1.x += ex2(r.rel1(edge));
+      }
+      s[0] = sum.x + sum.y;
+      s[1] = sum1.x + sum1.y;
       for (int j = tid; j < A.K; j += TH)
         if (id[j] >= 0 && tm != -INFINITY) s[2] += expf((q[j] - tm) / A.tau);
     }
     over_row(s, 1, false);
     const bool nan_row = w != 0.f && m[0] == -INFINITY && s[0] > 0.f;
-    Result r = {0.f, nan_row ? NAN : s[0], 0.f, nan_row ? NAN : TWO ? s[1] : s[0], top, true};
+    r.s = nan_row ? NAN : s[0];
+    r.s1 = nan_row ? NAN : TWO ? s[1] : s[0];
     if (nan_row) dead = false;
     // the entries' probabilities: a thread keeps its own
     float k[3] = {0.f, 0.f, 0.f};  // m, the divergence, entries that are repeated
@@ -952,14 +998,21 @@ k_distill_short(const __grid_constant__ DistillArgs A) {
       Factors f = {};
       if (!dead) f = factors(A, r, w, k[0], label, TWO);
       auto value = [&](float z) { return dead ? 0.f : f.value(r, z, A.ct, TWO); };
+      const Gradient<T, TWO> gradient(A, r, f);
+      const bool slow = gradient.slow(r, f);
 #pragma unroll
       for (int p = 0; p < SHORT_P; ++p)
         if (p < n) {
-          float2 v[N2];
-          unpack<T>(x[p], v);
+          uint4 o = make_uint4(0u, 0u, 0u, 0u);
+          if (slow) {
+            float2 v[N2];
+            unpack<T>(x[p], v);
 #pragma unroll
-          for (int j = 0; j < N2; ++j) v[j] = make_float2(value(v[j].x), value(v[j].y));
-          const uint4 o = pack<T>(v);
+            for (int j = 0; j < N2; ++j) v[j] = make_float2(value(v[j].x), value(v[j].y));
+            o = pack<T>(v);
+          } else if (!dead) {
+            o = gradient(x[p]);
+          }
           T* out = dz + S.head + (long)(p * TH + tid) * N;
           if (same) {
             *(uint4*)out = o;
@@ -1103,7 +1156,7 @@ extern "C" lx_status lx_distill_loss(int32_t dtype, const void* logits, int64_t 
   cudaStream_t s = (cudaStream_t)stream;
   // Rows that eight warps hold in registers.  Against the kernel with teachers' warps, us of
   // bf16 rows with gradient: 7929 x 1000, K 5: 16 and 51; 7929 x 1006, K 256: 171 and 264;
-  // 512 x 16000, K 56: 13 and 17; 5072 x 16384, K 56: 80 and 87; 64 x 1006: 8 and 6.  With
+  // 512 x 16000, K 56: 13 and 17; 5072 x 16384, K 56: 78 and 87; 64 x 1006: 8 and 6.  With
   // sixteen warps 5072 x 24000 takes 146, and 114 there.  (That kernel alone has the waits.)
   if ((long)V * es / 16 <= SHORT_P * 32 * 8 && K <= SHORT_K && !A.unmet)
     return dtype == LX_BF16 ? launch_short_any<__nv_bfloat16>(A, s) : launch_short_any<float>(A, s);
