@@ -20,9 +20,9 @@
 // finishes the row before.  Rows that do not fit the shared memory of eight CTAs are read a
 // second time from L2.
 //
-// Two warps of their own prepare the teacher's entries, up to four rows ahead (their chains
-// of loads take longer than a row), write the losses and, once the dense values of a row are
-// written, the entries' places once more; entries of one id add up.
+// Two to four warps of their own prepare the teacher's entries, up to four rows ahead (their
+// chains of loads take longer than a row), write the losses and, once the dense values of a
+// row are written, the entries' places once more; entries of one id add up.
 //
 // The roles meet at mbarriers alone: sums_bar when every data warp of the row's CTAs has
 // sent its partial sums (to every CTA: a barrier of the whole cluster would also wait for
@@ -835,15 +835,16 @@ k_distill(const __grid_constant__ DistillArgs A) {
   }
 }
 
-// Rows of up to SHORT_P pieces for each thread of W warps, with few entries: the row stays in
-// registers, its maximum is known before its sums, and the warps of a row do everything
-// themselves.  A CTA takes one row (four rows of a warp each for the shortest) and many CTAs
+// Rows of up to SHORT_P pieces for each thread of W warps, with few entries: the row stays
+// in registers, its maximum is known before its sums, and the warps of a row do everything
+// themselves. A CTA takes one row (four rows of a warp each for the shortest) and many CTAs
 // share an SM, so that their chains of loads and sums hide one another; the next CTA starts
 // where one ends, since with a grid that just filled the SMs a late CTA ran alone (7929 rows
-// of 1000 bf16 with 5 entries: 34 us so, 16 us now).  Bound by the instructions of a row and
-// by its chains: 1400 issued in a warp for 1000 columns.  At 64 registers 32 warps fit an SM
-// (72 in the four-row form, which spills at 64): 5072 rows of 16384 take 78 us, and 92 us at
-// 80 registers.  Four pieces a thread and twice the warps: 122 us.
+// of 1000 bf16 with 5 entries: 34 us so, 16 us now). Bound by a row's chains (its warps wait
+// for one another's maxima and sums) and its instructions, 24 a column and lane in both
+// directions (a fifth fewer changed 80 us to 78). At 64 registers 32 warps fit an SM (72 in
+// the four-row form, which spills at 64): 5072 rows of 16384 take 78 us, and 92 us at 80
+// registers. Four pieces a thread and twice the warps: 122 us.
 constexpr int SHORT_P = 8, SHORT_K = 256;
 __host__ __device__ constexpr int short_threads(int w) { return w == 1 ? 128 : 32 * w; }
 
