@@ -277,6 +277,16 @@ struct Gradient {
   }
 };
 
+// Whether an id lies in a table of a row's ids (open addressing, a free place is -1, at least
+// half of the places are)
+__device__ __forceinline__ bool has_id(const int* table, int size, int e) {
+  for (unsigned i = e;; ++i) {
+    const int was = table[i & (size - 1)];
+    if (was == e) return true;
+    if (was == -1) return false;
+  }
+}
+
 extern __shared__ uint4 distill_smem[];
 
 // TWO: a hard-label term at another temperature than the teacher's.  HELD: rows fit shared
@@ -396,12 +406,13 @@ k_distill(const __grid_constant__ DistillArgs A) {
       bool twice = false;
       for (int j = lane; j < A.K; j += 32)
         if (id[j] >= 0)
-          for (int i = id[j];; ++i) {
+          for (unsigned i = id[j];; ++i) {
             const int was = atomicCAS(table + (i & (A.table - 1)), -1, id[j]);
             twice |= was == id[j];
             if (was == -1 || was == id[j]) break;
           }
       twice = __any_sync(0xffffffffu, twice);
+      __syncwarp();  // the table may be read
       return twice;
     };
     for (unsigned k = h; k < BUFS; k += A.teachers) provide(k, first + k * step);
@@ -438,7 +449,8 @@ k_distill(const __grid_constant__ DistillArgs A) {
           const int e = id[j];
           if (e < v0 || e >= v0 + vn) continue;
           float x = q[j];
-          if (twice || e == label) {
+          if (!twice && j == A.K && has_id(table, A.table, e)) continue;  // its entry writes it
+          if (twice) {
             x = 0.f;
             for (int i = 0; i < A.K; ++i) x += id[i] == e ? q[i] : 0.f;
           }
@@ -977,7 +989,7 @@ k_distill_short(const __grid_constant__ DistillArgs A) {
         k[0] += p;
         if (p != 0.f) k[1] += p * (l - (r.rel(zj[j], A.ct) * LN2 - ls));
         if (dz && id[j] >= 0)  // at least half of the table's places stay free
-          for (int i = id[j];; ++i) {
+          for (unsigned i = id[j];; ++i) {
             const int was = atomicCAS(table + (i & (A.table - 1)), -1, id[j]);
             if (was == id[j]) k[2] = 1.f;
             if (was == -1 || was == id[j]) break;
@@ -1031,7 +1043,8 @@ k_distill_short(const __grid_constant__ DistillArgs A) {
           const int e = id[j];
           if (e < 0) continue;
           float y = j < A.K ? q[j] : 0.f;
-          if (twice || e == label) {  // (the label may be one of the entries)
+          if (!twice && j == A.K && has_id(table, A.table, e)) continue;  // its entry writes it
+          if (twice) {
             y = 0.f;
             for (int i = 0; i < A.K; ++i) y += id[i] == e ? q[i] : 0.f;
           }
