@@ -847,9 +847,8 @@ k_distill(const __grid_constant__ DistillArgs A) {
   }
 }
 
-// Rows of up to SHORT_P pieces for each thread of W warps, with few entries: the row stays
-// in registers, its maximum is known before its sums, and the warps of a row do everything
-// themselves. A CTA takes one row (four rows of a warp each for the shortest) and many CTAs
+// Rows of up to SHORT_P pieces for each thread of W warps: the row stays in registers, its
+// maximum is known before its sums, and the warps of a row do everything themselves. A CTA takes one row (four rows of a warp each for the shortest) and many CTAs
 // share an SM, so that their chains of loads and sums hide one another; the next CTA starts
 // where one ends, since with a grid that just filled the SMs a late CTA ran alone (7929 rows
 // of 1000 bf16 with 5 entries: 34 us so, 16 us now). Bound by a row's chains (its warps wait
@@ -857,7 +856,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
 // directions (a fifth fewer changed 80 us to 78). At 64 registers 32 warps fit an SM (72 in
 // the four-row form, which spills at 64): 5072 rows of 16384 take 78 us, and 92 us at 80
 // registers. Four pieces a thread and twice the warps: 122 us.
-constexpr int SHORT_P = 8, SHORT_K = 256;
+constexpr int SHORT_P = 8;
 __host__ __device__ constexpr int short_threads(int w) { return w == 1 ? 128 : 32 * w; }
 
 template <typename T, bool TWO, int W>
@@ -1066,8 +1065,16 @@ template <typename T>
 lx_status launch_short_any(const DistillArgs& A, cudaStream_t s) {
   const long pieces = (long)A.V * sizeof(T) / 16;
   const bool two = A.b != 0.f && A.tau != 1.f;
-#define LX_SHORT_CASE(W)                            \
-  if (pieces <= SHORT_P * 32 * W && A.K <= 32 * W) \
+  // Entries a thread: with few rows one, for the row's time (64 rows of 1006 bf16, 256
+  // entries: 8.2 us, 12.8 with four; 1200 rows: 18.3 and 20.4); with many four, since each
+  // further warp repeats what is done once a row (7929 rows: 101 us with one, 56 with four;
+  // 5072 rows of 4096, 200 entries: 65 and 43).  A single warp takes eight where the row
+  // leaves it time (7929 rows of 256, 200 entries: 23 us, 39 in two warps), and one where it
+  // does not (5072 rows of 2048, 100 entries: 35 us, 25 in two warps).
+  const int each = A.T <= 8 * SMS ? 1 : 4;
+  const int alone = each == 1 || pieces > SHORT_P * 32 / 2 ? 1 : 8;
+#define LX_SHORT_CASE(W)                                                      \
+  if (pieces <= SHORT_P * 32 * W && A.K <= (W == 1 ? alone : each) * 32 * W) \
     return two ? launch_short<T, true, W>(A, s) : launch_short<T, false, W>(A, s);
   LX_SHORT_CASE(1)
   LX_SHORT_CASE(2)
@@ -1169,10 +1176,11 @@ extern "C" lx_status lx_distill_loss(int32_t dtype, const void* logits, int64_t 
   while (A.table < 2 * K) A.table *= 2;
   cudaStream_t s = (cudaStream_t)stream;
   // Rows that eight warps hold in registers.  Against the kernel with teachers' warps, us of
-  // bf16 rows with gradient: 7929 x 1000, K 5: 16 and 51; 7929 x 1006, K 256: 171 and 264;
-  // 512 x 16000, K 56: 13 and 17; 5072 x 16384, K 56: 78 and 87; 64 x 1006: 8 and 6.  With
-  // sixteen warps 5072 x 24000 takes 146, and 114 there.  (That kernel alone has the waits.)
-  if ((long)V * es / 16 <= SHORT_P * 32 * 8 && K <= SHORT_K && !A.unmet)
+  // bf16 rows with gradient: 7929 x 1000, K 5: 16 and 51; 512 x 16000, K 56: 13 and 17; 5072 x
+  // 16384, K 56: 78 and 87, K 300: 99 and 283, K 1000: 166 and 562; 64 x 1006: 8 and 6; 64 x
+  // 16384, K 512: 12 and 26.  With sixteen warps 5072 x 24000 takes 146, and 114 there.  (That
+  // kernel alone has the waits.)
+  if ((long)V * es / 16 <= SHORT_P * 32 * 8 && !A.unmet)
     return dtype == LX_BF16 ? launch_short_any<__nv_bfloat16>(A, s) : launch_short_any<float>(A, s);
   // CTAs of 256 data threads with half of an SM's shared memory (128 and a quarter for short
   // rows) where a row fits it, else CTAs of 512 with all of it, as many as hold a row; rows
