@@ -277,14 +277,42 @@ struct Gradient {
   }
 };
 
-// Whether an id lies in a table of a row's ids (open addressing, a free place is -1, at least
-// half of the places are)
-__device__ __forceinline__ bool has_id(const int* table, int size, int e) {
+// A table of a row's ids: open addressing, a free place is -1 and at least half of the places
+// are; an id e that was put in more than once is kept as -2 - e.
+__device__ __forceinline__ bool put_id(int* table, int size, int e) {  // whether it was there
+  for (unsigned i = e;; ++i) {
+    int* const at = table + (i & (size - 1));
+    const int was = atomicCAS(at, -1, e);
+    if (was == -1) return false;
+    if (was == e || was == -2 - e) {
+      *(volatile int*)at = -2 - e;
+      return true;
+    }
+  }
+}
+__device__ __forceinline__ int times_of(const int* table, int size, int e) {  // 0, 1, or 2 for more
   for (unsigned i = e;; ++i) {
     const int was = table[i & (size - 1)];
-    if (was == e) return true;
-    if (was == -1) return false;
+    if (was == -1) return 0;
+    if (was == e) return 1;
+    if (was == -2 - e) return 2;
   }
+}
+// What the entries of id[j], entry j's, add up to, in their order; -1 where entry K, the label,
+// has its place written by another entry.  Only ids that are repeated are added up: a store
+// of top logits has few (5072 rows of 16384 bf16, 56 entries: 74 us, 78 where a repeat sent
+// all of its row's entries here; 1000 random ids, an eighth of them repeats: 1428 and 1005 us
+// at 4096 columns).
+__device__ __forceinline__ float entries_of(const int* id, const float* q, int K, int j, bool twice, const int* table,
+                                            int size) {
+  const int e = id[j];
+  if (!twice && j < K) return q[j];
+  const int times = times_of(table, size, e);
+  if (j == K) return times == 0 ? 0.f : -1.f;
+  if (times == 1) return q[j];
+  float x = 0.f;
+  for (int i = 0; i < K; ++i) x += id[i] == e ? q[i] : 0.f;
+  return x;
 }
 
 extern __shared__ uint4 distill_smem[];
@@ -398,19 +426,13 @@ k_distill(const __grid_constant__ DistillArgs A) {
       __syncwarp();
       if (lane == 0) tcg::mbar_arrive(bar(&ready_bar[k % BUFS]));
     };
-    // whether an id of the row occurs twice, by a table in which at least half of the places
-    // stay free
+    // fills the table; whether an id of the row occurs twice
     auto repeated = [&](const int* id) {
       for (int i = lane; i < A.table; i += 32) table[i] = -1;
       __syncwarp();
       bool twice = false;
       for (int j = lane; j < A.K; j += 32)
-        if (id[j] >= 0)
-          for (unsigned i = id[j];; ++i) {
-            const int was = atomicCAS(table + (i & (A.table - 1)), -1, id[j]);
-            twice |= was == id[j];
-            if (was == -1 || was == id[j]) break;
-          }
+        if (id[j] >= 0) twice |= put_id(table, A.table, id[j]);
       twice = __any_sync(0xffffffffu, twice);
       __syncwarp();  // the table may be read
       return twice;
@@ -448,12 +470,8 @@ k_distill(const __grid_constant__ DistillArgs A) {
         for (int j = lane; j <= A.K; j += 32) {
           const int e = id[j];
           if (e < v0 || e >= v0 + vn) continue;
-          float x = q[j];
-          if (!twice && j == A.K && has_id(table, A.table, e)) continue;  // its entry writes it
-          if (twice) {
-            x = 0.f;
-            for (int i = 0; i < A.K; ++i) x += id[i] == e ? q[i] : 0.f;
-          }
+          const float x = entries_of(id, q, A.K, j, twice, table, A.table);
+          if (x == -1.f) continue;
           dz[e] = from_f32<T>(f.value(r, zj[j], ct, TWO) - f.qa * x - (e == label ? f.hb : 0.f));
         }
       }
@@ -854,8 +872,8 @@ k_distill(const __grid_constant__ DistillArgs A) {
 // of 1000 bf16 with 5 entries: 34 us so, 16 us now). Bound by a row's chains (its warps wait
 // for one another's maxima and sums) and its instructions, 24 a column and lane in both
 // directions (a fifth fewer changed 80 us to 78). At 64 registers 32 warps fit an SM (72 in
-// the four-row form, which spills at 64): 5072 rows of 16384 take 78 us, and 92 us at 80
-// registers. Four pieces a thread and twice the warps: 122 us.
+// the four-row form, which spills at 64): 5072 rows of 16384 took 78 us (74 now), and 92 us
+// at 80 registers. Four pieces a thread and twice the warps: 122 us.
 constexpr int SHORT_P = 8;
 __host__ __device__ constexpr int short_threads(int w) { return w == 1 ? 128 : 32 * w; }
 
@@ -987,12 +1005,7 @@ k_distill_short(const __grid_constant__ DistillArgs A) {
         q[j] = p;
         k[0] += p;
         if (p != 0.f) k[1] += p * (l - (r.rel(zj[j], A.ct) * LN2 - ls));
-        if (dz && id[j] >= 0)  // at least half of the table's places stay free
-          for (unsigned i = id[j];; ++i) {
-            const int was = atomicCAS(table + (i & (A.table - 1)), -1, id[j]);
-            if (was == id[j]) k[2] = 1.f;
-            if (was == -1 || was == id[j]) break;
-          }
+        if (dz && id[j] >= 0 && put_id(table, A.table, id[j])) k[2] = 1.f;
       }
     }
     over_row(k, 2, false);
@@ -1041,12 +1054,8 @@ k_distill_short(const __grid_constant__ DistillArgs A) {
         for (int j = tid; j <= A.K; j += TH) {
           const int e = id[j];
           if (e < 0) continue;
-          float y = j < A.K ? q[j] : 0.f;
-          if (!twice && j == A.K && has_id(table, A.table, e)) continue;  // its entry writes it
-          if (twice) {
-            y = 0.f;
-            for (int i = 0; i < A.K; ++i) y += id[i] == e ? q[i] : 0.f;
-          }
+          const float y = entries_of(id, q, A.K, j, twice, table, A.table);
+          if (y == -1.f) continue;
           dz[e] = from_f32<T>(value(zj[j]) - f.qa * y - (e == label ? f.hb : 0.f));
         }
     }
@@ -1177,8 +1186,8 @@ extern "C" lx_status lx_distill_loss(int32_t dtype, const void* logits, int64_t 
   cudaStream_t s = (cudaStream_t)stream;
   // Rows that eight warps hold in registers.  Against the kernel with teachers' warps, us of
   // bf16 rows with gradient: 7929 x 1000, K 5: 16 and 51; 512 x 16000, K 56: 13 and 17; 5072 x
-  // 16384, K 56: 78 and 87, K 300: 99 and 283, K 1000: 166 and 562; 64 x 1006: 8 and 6; 64 x
-  // 16384, K 512: 12 and 26.  With sixteen warps 5072 x 24000 takes 146, and 114 there.  (That
+  // 16384, K 56: 74 and 87, K 300: 95 and 283, K 1000: 160 and 562; 64 x 1006, K 5: 6 either
+  // way; 64 x 16384, K 512: 11 and 26.  With sixteen warps 5072 x 24000 takes 146, and 114 there.  (That
   // kernel alone has the waits.)
   if ((long)V * es / 16 <= SHORT_P * 32 * 8 && !A.unmet)
     return dtype == LX_BF16 ? launch_short_any<__nv_bfloat16>(A, s) : launch_short_any<float>(A, s);
