@@ -28,8 +28,8 @@
 // sent its partial sums (to every CTA: a barrier of the whole cluster would also wait for
 // the stores under way), ready_bar when a row's entries are prepared, result_bar when its
 // sums are known, released_bar when the data warps have written it.  Every wait is
-// bounded; one that gives up makes the row's loss and gradient NaN, and the CTA waits no
-// more.
+// bounded; one that gives up makes the row's loss and gradient NaN, and the row's CTAs wait
+// no more.
 //
 // The reference of a sum is a whole number n of powers of two: exp(z / tau) is taken as
 // 2^n 2^(z log2(e) / tau - n), one fused multiply-add from z, exact in n.  A row whose
@@ -315,6 +315,29 @@ __device__ __forceinline__ float entries_of(const int* id, const float* q, int K
   return x;
 }
 
+// Waits, after a wait that gave up, until all that was sent to barrier i of this CTA has landed.
+// Every warp counted (modulo 2^16) the rows for which it sent 16 bytes to each CTA, and the barrier
+// expects as many rows as warp 0 sent for, `unmet` bytes more each than the warps send.  At most
+// one phase is open: a warp sends for row x + 4 after it received row x + 2, for which every
+// warp had sent, each after it received row x, the barrier's last.  The open phase's account
+// is brought to what was sent, so that it ends with the last byte.
+__device__ __noinline__ void await_sent(uint32_t bar, unsigned short (*sent)[MAX_WARPS], int i, int cols, int nw,
+                                        int unmet, unsigned long long cycles) {
+  uint32_t rows = sent[i][0];
+  int bytes = -(int)rows * unmet;  // sent, less expected
+  for (int c = 0; c < cols; ++c)
+    for (int w = 0; w < nw; ++w)
+      bytes += 16 * (short)(*cooperative_groups::this_cluster().map_shared_rank(&sent[i][w], c) - rows);
+  if (bytes < 0)
+    asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(-bytes) : "memory");
+  if (bytes > 0) {
+    tcg::mbar_expect_tx(bar, bytes);
+    ++rows;
+  }
+  const long long c0 = clock64();  // (a barrier of no rows counts as past its phase 1)
+  while (!tcg::mbar_try_wait(bar, (rows - 1) & 1) && clock64() - c0 < (long long)cycles) {}
+}
+
 extern __shared__ uint4 distill_smem[];
 
 // TWO: a hard-label term at another temperature than the teacher's.  HELD: rows fit shared
@@ -333,7 +356,8 @@ k_distill(const __grid_constant__ DistillArgs A) {
   } own[MAX_WARPS];  // a data warp's copy for its odd pieces, which keep no registers
   __shared__ float msum[BUFS];
   __shared__ uint64_t sums_bar[SENDS + 2], ready_bar[BUFS], result_bar[BUFS], released_bar[BUFS];
-  __shared__ volatile int gave_up;
+  __shared__ unsigned short sent[CL ? SENDS + 2 : 1][MAX_WARPS];  // rows a warp sent for, by barrier
+  __shared__ volatile int gave_up;  // a wait of the row's CTAs did
   const int log_d = A.log_d, D = 1 << log_d, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = D >> 5;
   const bool teacher = warp >= nw;
   const int E1 = A.K + 1, rank = CL ? blockIdx.x : 0, cols = CL ? gridDim.x : 1;
@@ -347,6 +371,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
   auto weight = [&](unsigned t) { return t >= T0 ? 0.f : A.weight ? A.weight[t] : 1.f; };
 
   auto bar = [](uint64_t* b) { return (uint32_t)__cvta_generic_to_shared(b); };
+  if (CL && tid < (SENDS + 2) * MAX_WARPS) (&sent[0][0])[tid] = 0;
   if (tid == 0) {
     gave_up = 0;
     for (int i = 0; i < SENDS + 2; ++i) tcg::mbar_init(bar(&sums_bar[i]), CL ? 1 : nw);
@@ -369,6 +394,9 @@ k_distill(const __grid_constant__ DistillArgs A) {
     }
     lost = true;
     gave_up = 1;
+    if constexpr (CL)  // (its CTAs run until the cluster's last barrier)
+      for (int c = 0; c < cols; ++c)
+        *(volatile int*)cooperative_groups::this_cluster().map_shared_rank((int*)&gave_up, c) = 1;
   };
 
   if (teacher) {
@@ -529,6 +557,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
       if (__any_sync(0xffffffffu, lost)) return;
       if constexpr (CL) {
         if (tid == 0) tcg::mbar_expect_tx(bar(&sums_bar[i]), cols * nw * 16 + (A.unmet ? 16 : 0));
+        if (lane == 0) ++sent[i][warp];
         if (lane < cols) {
           uint32_t to, at;
           asm("mapa.shared::cluster.u32 %0, %1, %2;"
@@ -857,11 +886,13 @@ k_distill(const __grid_constant__ DistillArgs A) {
     asm volatile("cp.async.wait_group 0;" ::: "memory");
   }
   if constexpr (CL) {
-    // A CTA's shared memory outlives what its neighbours send; after a wait that gave up
-    // that may still be on its way: some ten microseconds for it.
-    if (gave_up)
-      for (const long long c0 = clock64(); clock64() - c0 < 20000;) {}
+    // A CTA's shared memory outlives what its neighbours send: rows that were waited for have
+    // landed, after a wait that gave up the rest is waited for now.
     cooperative_groups::this_cluster().sync();
+    if (gave_up) {  // the same in all of the row's CTAs
+      if (tid < SENDS + 2) await_sent(bar(&sums_bar[tid]), sent, tid, cols, nw, A.unmet ? 16 : 0, A.wait_cycles);
+      cooperative_groups::this_cluster().sync();  // the others have read sent
+    }
   }
 }
 
