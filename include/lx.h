@@ -265,7 +265,10 @@ typedef enum {
   LX_WAIT_ROUTER = 3,
   LX_WAIT_CALL_PRODUCT = 4,
   LX_WAIT_CALL_JACOBI = 5,
-  LX_WAIT_CALL_SUMS = 6
+  LX_WAIT_CALL_SUMS = 6,
+  LX_WAIT_CALL_ENTRIES = 7,
+  LX_WAIT_CALL_WRITTEN = 8,
+  LX_WAIT_CALL_AGAIN = 9
 } lx_wait_site;
 LX_API lx_status lx_set_wait_limit(lx_layer* layer, uint64_t cycles);
 LX_API lx_status lx_inject_unmet_wait(lx_layer* layer, int32_t site);
@@ -274,14 +277,17 @@ LX_API lx_status lx_clear_device_error(lx_layer* layer);
 /*
  * The calls without a layer (lx_compress_factor, lx_align_cost, lx_distill_loss) have
  * bounded waits too (default bound), and no error word of a layer: when one gives up,
- * every value that the call writes is NaN (lx_distill_loss: every loss and gradient of a
- * row that was not done by then, rows of weight 0 apart).
+ * every value that the call writes is NaN (lx_distill_loss: the loss and the whole
+ * gradient of every row that was not done by then, rows of weight 0 apart).
  * lx_inject_unmet_wait_call (test hook): in the calling thread's next such call,
  * waits have the bound `cycles` (0: the default) and the one at `site` runs out --
  * LX_WAIT_CALL_PRODUCT: in the tensor-core products (bf16; lx_align_cost also needs
  * d_model a multiple of 256); LX_WAIT_CALL_JACOBI: in lx_compress_factor's Jacobi (l
- * above 2); LX_WAIT_CALL_SUMS: for the partial sums of a row in lx_distill_loss;
- * LX_WAIT_NONE: none.  Errors: LX_ERR_ARG (another site).
+ * above 2); in lx_distill_loss, LX_WAIT_CALL_SUMS: for the partial sums of a row,
+ * LX_WAIT_CALL_AGAIN: for those of a row whose logits lie too far from zero for the
+ * first ones, LX_WAIT_CALL_ENTRIES and LX_WAIT_CALL_WRITTEN: from a CTA's third row
+ * on, for the teacher's entries and for the dense gradient; LX_WAIT_NONE: none.
+ * Errors: LX_ERR_ARG (another site).
  */
 LX_API lx_status lx_inject_unmet_wait_call(int32_t site, uint64_t cycles);
 

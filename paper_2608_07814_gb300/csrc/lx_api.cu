@@ -852,7 +852,7 @@ CallWaits take_call_waits() {
 
 extern "C" lx_status lx_inject_unmet_wait_call(int32_t site, uint64_t cycles) {
   if (site != LX_WAIT_NONE && site != LX_WAIT_CALL_PRODUCT && site != LX_WAIT_CALL_JACOBI &&
-      site != LX_WAIT_CALL_SUMS)
+      (site < LX_WAIT_CALL_SUMS || site > LX_WAIT_CALL_AGAIN))
     return fail(LX_ERR_ARG, "unknown wait site");
   lx::g_call_waits = lx::CallWaits{};
   lx::g_call_waits.unmet = site;

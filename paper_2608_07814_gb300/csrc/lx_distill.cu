@@ -28,8 +28,8 @@
 // sent its partial sums (to every CTA: a barrier of the whole cluster would also wait for
 // the stores under way), ready_bar when a row's entries are prepared, result_bar when its
 // sums are known, released_bar when the data warps have written it.  Every wait is
-// bounded; one that gives up makes the row's loss and gradient NaN, and the row's CTAs wait
-// no more.
+// bounded.  When one gives up, the row's CTAs wait no more, run to their ends, and make
+// the rows that were not done by then NaN.
 //
 // The reference of a sum is a whole number n of powers of two: exp(z / tau) is taken as
 // 2^n 2^(z log2(e) / tau - n), one fused multiply-add from z, exact in n.  A row whose
@@ -85,7 +85,7 @@ struct DistillArgs {
   int slots;   // of them in shared memory at a time, a multiple of U
   int lead;
   unsigned long long wait_cycles;
-  int unmet;   // test hook: the sums' barrier waits for what nobody sends
+  int unmet;   // test hook: lx_wait_site whose barriers wait for what nobody sends
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -338,6 +338,20 @@ __device__ __noinline__ void await_sent(uint32_t bar, unsigned short (*sent)[MAX
   while (!tcg::mbar_try_wait(bar, (rows - 1) & 1) && clock64() - c0 < (long long)cycles) {}
 }
 
+// What is left of the CTA's rows (first, first + step, ...) after a wait that gave up: loss and
+// gradient become NaN in row k from lost[k % teachers] on, apart from rows of weight 0, which
+// wait for nothing.  `losses`: this CTA writes the losses.
+template <typename T>
+__device__ __noinline__ void rows_lost(const unsigned* lost, int teachers, unsigned first, unsigned step, unsigned T0,
+                                       const float* weight, float* loss, T* dz, long ldd, int vn, bool losses) {
+  for (unsigned k = 0, t = first; t < T0; ++k, t += step) {
+    if (k < lost[k % teachers] || (weight && weight[t] == 0.f)) continue;
+    if (losses && threadIdx.x == 0) loss[t] = NAN;
+    if (dz)
+      for (int e = threadIdx.x; e < vn; e += blockDim.x) dz[(long)t * ldd + e] = from_f32<T>(NAN);
+  }
+}
+
 extern __shared__ uint4 distill_smem[];
 
 // TWO: a hard-label term at another temperature than the teacher's.  HELD: rows fit shared
@@ -358,6 +372,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
   __shared__ uint64_t sums_bar[SENDS + 2], ready_bar[BUFS], result_bar[BUFS], released_bar[BUFS];
   __shared__ unsigned short sent[CL ? SENDS + 2 : 1][MAX_WARPS];  // rows a warp sent for, by barrier
   __shared__ volatile int gave_up;  // a wait of the row's CTAs did
+  __shared__ unsigned lost_from[2][MAX_TEACHERS];  // a teacher's first row that was not done then; the CTAs' first
   const int log_d = A.log_d, D = 1 << log_d, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = D >> 5;
   const bool teacher = warp >= nw;
   const int E1 = A.K + 1, rank = CL ? blockIdx.x : 0, cols = CL ? gridDim.x : 1;
@@ -374,6 +389,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
   if (CL && tid < (SENDS + 2) * MAX_WARPS) (&sent[0][0])[tid] = 0;
   if (tid == 0) {
     gave_up = 0;
+    for (int i = 0; i < MAX_TEACHERS; ++i) lost_from[0][i] = ~0u;
     for (int i = 0; i < SENDS + 2; ++i) tcg::mbar_init(bar(&sums_bar[i]), CL ? 1 : nw);
     for (int i = 0; i < BUFS; ++i) {
       tcg::mbar_init(bar(&ready_bar[i]), 1);
@@ -384,6 +400,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
   }
   __syncthreads();
   if constexpr (CL) cooperative_groups::this_cluster().sync();  // all have started
+  auto is_unmet = [&](int i) { return A.unmet == LX_WAIT_CALL_SUMS || (A.unmet == LX_WAIT_CALL_AGAIN && i >= SENDS); };
   bool lost = false;  // a wait of this thread gave up
   auto wait = [&](uint64_t* b, uint32_t parity) {
     if (lost || (!gave_up && tcg::mbar_try_wait(bar(b), parity))) return;
@@ -452,7 +469,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
       if (t >= T0) return;
       if (!__any_sync(0xffffffffu, lost)) prepare(t, k % BUFS);
       __syncwarp();
-      if (lane == 0) tcg::mbar_arrive(bar(&ready_bar[k % BUFS]));
+      if (lane == 0 && !(A.unmet == LX_WAIT_CALL_ENTRIES && k >= 2)) tcg::mbar_arrive(bar(&ready_bar[k % BUFS]));
     };
     // fills the table; whether an id of the row occurs twice
     auto repeated = [&](const int* id) {
@@ -486,11 +503,14 @@ k_distill(const __grid_constant__ DistillArgs A) {
           loss += A.b * (logf(r.s1) - (TWO ? r.rel1(zj[A.K]) : r.rel(zj[A.K], ct)) * LN2);
         loss *= w;
       }
-      if (__any_sync(0xffffffffu, lost)) loss = NAN;
       if (lane == 0 && rank == 0) A.loss[t] = loss;
       const bool twice = GRAD && !dead && repeated(id);
       wait(&released_bar[b], parity);
-      if (GRAD && !dead && !__any_sync(0xffffffffu, lost)) {
+      // A row is done once its dense values lie there and nothing gave up before, in any of its
+      // CTAs; else all of it is written anew at the end.
+      const bool done = !__any_sync(0xffffffffu, lost || gave_up);
+      if (!done && lane == 0 && k < lost_from[0][h]) lost_from[0][h] = k;
+      if (GRAD && !dead && done) {
         // the entries of this CTA's columns; the label may be one of them
         T* dz = (T*)A.dlogits + (long)t * A.ldd;
         const int label = id[A.K], v0 = rank * A.slice, vn = min(A.slice, A.V - v0);
@@ -555,8 +575,9 @@ k_distill(const __grid_constant__ DistillArgs A) {
     // Sums of the row's CTAs: every data warp's v goes to red[i] of each of them
     auto send = [&](int i, float4 v) {
       if (__any_sync(0xffffffffu, lost)) return;
+      const bool unmet = is_unmet(i);
       if constexpr (CL) {
-        if (tid == 0) tcg::mbar_expect_tx(bar(&sums_bar[i]), cols * nw * 16 + (A.unmet ? 16 : 0));
+        if (tid == 0) tcg::mbar_expect_tx(bar(&sums_bar[i]), cols * nw * 16 + (unmet ? 16 : 0));
         if (lane == 0) ++sent[i][warp];
         if (lane < cols) {
           uint32_t to, at;
@@ -571,7 +592,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
         }
       } else if (lane == 0) {
         red[i][0][warp] = v;
-        if (!(A.unmet && warp == 0)) tcg::mbar_arrive(bar(&sums_bar[i]));
+        if (!(unmet && warp == 0)) tcg::mbar_arrive(bar(&sums_bar[i]));
       }
       __syncwarp();
     };
@@ -598,7 +619,6 @@ k_distill(const __grid_constant__ DistillArgs A) {
         }
       join_warp(r.n, r.s);
       if (TWO) join_warp(r.n1, r.s1);
-      if (__any_sync(0xffffffffu, lost)) r.s = r.s1 = NAN;
       return r;
     };
 
@@ -879,7 +899,8 @@ k_distill(const __grid_constant__ DistillArgs A) {
       }
       if constexpr (!HELD) feed_direct();
       __syncwarp();
-      if (lane == 0) tcg::mbar_arrive(bar(&released_bar[b]));
+      if (lane == 0 && !(A.unmet == LX_WAIT_CALL_WRITTEN && warp == 0 && k >= 2))
+        tcg::mbar_arrive(bar(&released_bar[b]));
       w = wn;
       wn = wn2;
     }
@@ -889,10 +910,24 @@ k_distill(const __grid_constant__ DistillArgs A) {
     // A CTA's shared memory outlives what its neighbours send: rows that were waited for have
     // landed, after a wait that gave up the rest is waited for now.
     cooperative_groups::this_cluster().sync();
-    if (gave_up) {  // the same in all of the row's CTAs
-      if (tid < SENDS + 2) await_sent(bar(&sums_bar[tid]), sent, tid, cols, nw, A.unmet ? 16 : 0, A.wait_cycles);
-      cooperative_groups::this_cluster().sync();  // the others have read sent
+    if (gave_up && tid < SENDS + 2)
+      await_sent(bar(&sums_bar[tid]), sent, tid, cols, nw, is_unmet(tid) ? 16 : 0, A.wait_cycles);
+  } else {
+    __syncthreads();
+  }
+  if (gave_up) {  // the same in all of the row's CTAs
+    if (tid < A.teachers) {
+      unsigned k = lost_from[0][tid];
+      if constexpr (CL)
+        for (int c = 0; c < cols; ++c)
+          k = min(k, *cooperative_groups::this_cluster().map_shared_rank(&lost_from[0][tid], c));
+      lost_from[1][tid] = k;
     }
+    __syncthreads();
+    const int v0 = rank * A.slice;
+    rows_lost<T>(lost_from[1], A.teachers, first, step, T0, A.weight, A.loss, GRAD ? (T*)A.dlogits + v0 : nullptr, A.ldd,
+                 min(A.slice, A.V - v0), rank == 0);
+    if constexpr (CL) cooperative_groups::this_cluster().sync();  // the others have read sent and lost_from
   }
 }
 
@@ -1211,7 +1246,7 @@ extern "C" lx_status lx_distill_loss(int32_t dtype, const void* logits, int64_t 
   A.ldd = ldd;
   const CallWaits waits = take_call_waits();
   A.wait_cycles = waits.cycles;
-  A.unmet = waits.unmet == LX_WAIT_CALL_SUMS;
+  A.unmet = waits.unmet;
   A.table = 32;
   while (A.table < 2 * K) A.table *= 2;
   cudaStream_t s = (cudaStream_t)stream;

@@ -38,7 +38,8 @@ EXPORTS = [
     "lx_router_balance", "lx_router_balance_backward", "lx_distill_loss",
 ]
 (LX_WAIT_NONE, LX_WAIT_STREAM_DEP, LX_WAIT_TC_MMA, LX_WAIT_ROUTER, LX_WAIT_CALL_PRODUCT,
- LX_WAIT_CALL_JACOBI, LX_WAIT_CALL_SUMS) = range(7)
+ LX_WAIT_CALL_JACOBI, LX_WAIT_CALL_SUMS, LX_WAIT_CALL_ENTRIES, LX_WAIT_CALL_WRITTEN,
+ LX_WAIT_CALL_AGAIN) = range(10)
 LX_NOALLOC_SCRATCH_BYTES = 16 << 20
 
 
