@@ -28,8 +28,8 @@
 // sent its partial sums (to every CTA: a barrier of the whole cluster would also wait for
 // the stores under way), ready_bar when a row's entries are prepared, result_bar when its
 // sums are known, released_bar when the data warps have written it.  Every wait is
-// bounded.  When one gives up, the row's CTAs wait no more, run to their ends, and make
-// the rows that were not done by then NaN.
+// bounded.  After one that gives up its CTA waits no more and runs to its end, where the
+// rows that were not done by then are made NaN, in all of their CTAs.
 //
 // The reference of a sum is a whole number n of powers of two: exp(z / tau) is taken as
 // 2^n 2^(z log2(e) / tau - n), one fused multiply-add from z, exact in n.  A row whose
@@ -85,7 +85,9 @@ struct DistillArgs {
   int slots;   // of them in shared memory at a time, a multiple of U
   int lead;
   unsigned long long wait_cycles;
-  int unmet;   // test hook: lx_wait_site whose barriers wait for what nobody sends
+  // test hook: barriers that nobody tells of what they wait for
+  int sums_met;                       // exchanges that are told of, SENDS + 2 for all
+  unsigned entries_met, written_met;  // a CTA's rows whose entries, whose dense gradient are told of
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -315,40 +317,40 @@ __device__ __forceinline__ float entries_of(const int* id, const float* q, int K
   return x;
 }
 
-// Waits, after a wait that gave up, until all that was sent to barrier i of this CTA has landed.
-// Every warp counted (modulo 2^16) the rows for which it sent 16 bytes to each CTA, and the barrier
-// expects as many rows as warp 0 sent for, `unmet` bytes more each than the warps send.  At most
-// one phase is open: a warp sends for row x + 4 after it received row x + 2, for which every
-// warp had sent, each after it received row x, the barrier's last.  The open phase's account
-// is brought to what was sent, so that it ends with the last byte.
-__device__ __noinline__ void await_sent(uint32_t bar, unsigned short (*sent)[MAX_WARPS], int i, int cols, int nw,
-                                        int unmet, unsigned long long cycles) {
-  uint32_t rows = sent[i][0];
-  int bytes = -(int)rows * unmet;  // sent, less expected
-  for (int c = 0; c < cols; ++c)
-    for (int w = 0; w < nw; ++w)
-      bytes += 16 * (short)(*cooperative_groups::this_cluster().map_shared_rank(&sent[i][w], c) - rows);
-  if (bytes < 0)
-    asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(-bytes) : "memory");
-  if (bytes > 0) {
-    tcg::mbar_expect_tx(bar, bytes);
-    ++rows;
+// Waits, after a wait that gave up, until all that was sent to a barrier of this CTA has landed.
+// `sent` counts the 16-byte sums that a CTA's warps sent to each CTA (in every CTA), `told` the rows
+// that the barrier was told to expect, `each` sums a row.  At most one phase is open: a warp
+// sends for row x + 4 after it received row x + 2, for which every warp had sent, each after
+// it received row x, the barrier's last.  The open phase's account is brought to what was
+// sent, so that it ends with the last byte.
+__device__ __forceinline__ void await_sent(uint32_t bar, unsigned* sent, unsigned told, int each, int cols,
+                                           unsigned long long cycles) {
+  unsigned sums = 0;
+#pragma unroll 1
+  for (int c = 0; c < cols; ++c) sums += *cooperative_groups::this_cluster().map_shared_rank(sent, c);
+  const int more = (int)(sums - told * each);  // sent, less expected
+  if (more < 0)
+    asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(-16 * more) : "memory");
+  if (more > 0) {
+    tcg::mbar_expect_tx(bar, 16 * more);
+    ++told;
   }
   const long long c0 = clock64();  // (a barrier of no rows counts as past its phase 1)
-  while (!tcg::mbar_try_wait(bar, (rows - 1) & 1) && clock64() - c0 < (long long)cycles) {}
+  while (!tcg::mbar_try_wait(bar, (told - 1) & 1) && clock64() - c0 < (long long)cycles) {}
 }
 
-// What is left of the CTA's rows (first, first + step, ...) after a wait that gave up: loss and
-// gradient become NaN in row k from lost[k % teachers] on, apart from rows of weight 0, which
-// wait for nothing.  `losses`: this CTA writes the losses.
+// What a wait that gave up left of the CTA's rows (first, first + step, ...): row k's gradient, and
+// its loss unless NULL, become NaN from lost[k % teachers] on, rows of weight 0 apart, which
+// wait for nothing.  (Inlined, as a call's registers cost the rows before 3 %.)
 template <typename T>
-__device__ __noinline__ void rows_lost(const unsigned* lost, int teachers, unsigned first, unsigned step, unsigned T0,
-                                       const float* weight, float* loss, T* dz, long ldd, int vn, bool losses) {
+__device__ __forceinline__ void rows_lost(const unsigned* lost, int teachers, unsigned first, unsigned step, unsigned T0,
+                                          const float* weight, float* loss, T* dz, long ldd, int vn) {
+#pragma unroll 1
   for (unsigned k = 0, t = first; t < T0; ++k, t += step) {
     if (k < lost[k % teachers] || (weight && weight[t] == 0.f)) continue;
-    if (losses && threadIdx.x == 0) loss[t] = NAN;
-    if (dz)
-      for (int e = threadIdx.x; e < vn; e += blockDim.x) dz[(long)t * ldd + e] = from_f32<T>(NAN);
+    if (loss && threadIdx.x == 0) loss[t] = NAN;
+#pragma unroll 1
+    for (int e = threadIdx.x; e < vn; e += blockDim.x) dz[(long)t * ldd + e] = from_f32<T>(NAN);
   }
 }
 
@@ -370,9 +372,9 @@ k_distill(const __grid_constant__ DistillArgs A) {
   } own[MAX_WARPS];  // a data warp's copy for its odd pieces, which keep no registers
   __shared__ float msum[BUFS];
   __shared__ uint64_t sums_bar[SENDS + 2], ready_bar[BUFS], result_bar[BUFS], released_bar[BUFS];
-  __shared__ unsigned short sent[CL ? SENDS + 2 : 1][MAX_WARPS];  // rows a warp sent for, by barrier
-  __shared__ volatile int gave_up;  // a wait of the row's CTAs did
-  __shared__ unsigned lost_from[2][MAX_TEACHERS];  // a teacher's first row that was not done then; the CTAs' first
+  __shared__ unsigned sent[CL ? SENDS + 2 : 1], told[CL ? SENDS + 2 : 1];  // of await_sent, by barrier
+  __shared__ volatile int gave_up;  // a wait of the CTA did
+  __shared__ unsigned lost_from[MAX_TEACHERS];  // a teacher's first row that was not done then, in any CTA
   const int log_d = A.log_d, D = 1 << log_d, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = D >> 5;
   const bool teacher = warp >= nw;
   const int E1 = A.K + 1, rank = CL ? blockIdx.x : 0, cols = CL ? gridDim.x : 1;
@@ -386,11 +388,13 @@ k_distill(const __grid_constant__ DistillArgs A) {
   auto weight = [&](unsigned t) { return t >= T0 ? 0.f : A.weight ? A.weight[t] : 1.f; };
 
   auto bar = [](uint64_t* b) { return (uint32_t)__cvta_generic_to_shared(b); };
-  if (CL && tid < (SENDS + 2) * MAX_WARPS) (&sent[0][0])[tid] = 0;
   if (tid == 0) {
     gave_up = 0;
-    for (int i = 0; i < MAX_TEACHERS; ++i) lost_from[0][i] = ~0u;
-    for (int i = 0; i < SENDS + 2; ++i) tcg::mbar_init(bar(&sums_bar[i]), CL ? 1 : nw);
+    for (int i = 0; i < MAX_TEACHERS; ++i) lost_from[i] = ~0u;
+    for (int i = 0; i < SENDS + 2; ++i) {
+      tcg::mbar_init(bar(&sums_bar[i]), CL ? 1 : nw);
+      if (CL) sent[i] = told[i] = 0;
+    }
     for (int i = 0; i < BUFS; ++i) {
       tcg::mbar_init(bar(&ready_bar[i]), 1);
       tcg::mbar_init(bar(&result_bar[i]), 1);
@@ -400,7 +404,6 @@ k_distill(const __grid_constant__ DistillArgs A) {
   }
   __syncthreads();
   if constexpr (CL) cooperative_groups::this_cluster().sync();  // all have started
-  auto is_unmet = [&](int i) { return A.unmet == LX_WAIT_CALL_SUMS || (A.unmet == LX_WAIT_CALL_AGAIN && i >= SENDS); };
   bool lost = false;  // a wait of this thread gave up
   auto wait = [&](uint64_t* b, uint32_t parity) {
     if (lost || (!gave_up && tcg::mbar_try_wait(bar(b), parity))) return;
@@ -411,9 +414,6 @@ k_distill(const __grid_constant__ DistillArgs A) {
     }
     lost = true;
     gave_up = 1;
-    if constexpr (CL)  // (its CTAs run until the cluster's last barrier)
-      for (int c = 0; c < cols; ++c)
-        *(volatile int*)cooperative_groups::this_cluster().map_shared_rank((int*)&gave_up, c) = 1;
   };
 
   if (teacher) {
@@ -421,6 +421,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
     // k % BUFS.
     const int h = warp - nw;
     int* table = (int*)(elq + BUFS * E1) + h * A.table;
+    unsigned lost_k = ~0u;  // the first row that was not done when a wait gave up
     auto prepare = [&](unsigned t, int b) {
       int* id = eid + b * E1;
       float *z = ez + b * E1, *q = eq + b * E1, *lq = elq + b * E1;
@@ -469,7 +470,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
       if (t >= T0) return;
       if (!__any_sync(0xffffffffu, lost)) prepare(t, k % BUFS);
       __syncwarp();
-      if (lane == 0 && !(A.unmet == LX_WAIT_CALL_ENTRIES && k >= 2)) tcg::mbar_arrive(bar(&ready_bar[k % BUFS]));
+      if (lane == 0 && k < A.entries_met) tcg::mbar_arrive(bar(&ready_bar[k % BUFS]));
     };
     // fills the table; whether an id of the row occurs twice
     auto repeated = [&](const int* id) {
@@ -503,13 +504,14 @@ k_distill(const __grid_constant__ DistillArgs A) {
           loss += A.b * (logf(r.s1) - (TWO ? r.rel1(zj[A.K]) : r.rel(zj[A.K], ct)) * LN2);
         loss *= w;
       }
+      if (!GRAD && w != 0.f && __any_sync(0xffffffffu, lost || gave_up)) loss = NAN;  // (rows_lost does it else)
       if (lane == 0 && rank == 0) A.loss[t] = loss;
       const bool twice = GRAD && !dead && repeated(id);
       wait(&released_bar[b], parity);
       // A row is done once its dense values lie there and nothing gave up before, in any of its
       // CTAs; else all of it is written anew at the end.
       const bool done = !__any_sync(0xffffffffu, lost || gave_up);
-      if (!done && lane == 0 && k < lost_from[0][h]) lost_from[0][h] = k;
+      if (!done) lost_k = min(lost_k, k);
       if (GRAD && !dead && done) {
         // the entries of this CTA's columns; the label may be one of them
         T* dz = (T*)A.dlogits + (long)t * A.ldd;
@@ -525,6 +527,13 @@ k_distill(const __grid_constant__ DistillArgs A) {
       }
       __syncwarp();
       provide(k + BUFS, t + BUFS * step);
+    }
+    if (lane == 0 && lost_k != ~0u) {
+      if constexpr (CL)
+#pragma unroll 1
+        for (int c = 0; c < cols; ++c)
+          atomicMin(cooperative_groups::this_cluster().map_shared_rank(&lost_from[h], c), lost_k);
+      else lost_from[h] = lost_k;
     }
   } else {
     const int v0 = rank * A.slice, vn = min(A.slice, A.V - v0);
@@ -572,13 +581,16 @@ k_distill(const __grid_constant__ DistillArgs A) {
       ask_whole -= U;
       ask_rounds -= U;
     };
-    // Sums of the row's CTAs: every data warp's v goes to red[i] of each of them
+    int feed_sent = 0;  // rows whose sums this warp sent
+    // Sums of the row's CTAs: every data warp's v goes to red[i] of each of them.  A warp that gave
+    // up sends no more.
     auto send = [&](int i, float4 v) {
-      if (__any_sync(0xffffffffu, lost)) return;
-      const bool unmet = is_unmet(i);
+      if (__any_sync(0xffffffffu, lost)) {
+        --feed_sent;  // (of a row that is done again, nothing is sent then)
+        return;
+      }
       if constexpr (CL) {
-        if (tid == 0) tcg::mbar_expect_tx(bar(&sums_bar[i]), cols * nw * 16 + (unmet ? 16 : 0));
-        if (lane == 0) ++sent[i][warp];
+        if (tid == 0 && i < A.sums_met) tcg::mbar_expect_tx(bar(&sums_bar[i]), cols * nw * 16);
         if (lane < cols) {
           uint32_t to, at;
           asm("mapa.shared::cluster.u32 %0, %1, %2;"
@@ -592,9 +604,13 @@ k_distill(const __grid_constant__ DistillArgs A) {
         }
       } else if (lane == 0) {
         red[i][0][warp] = v;
-        if (!(unmet && warp == 0)) tcg::mbar_arrive(bar(&sums_bar[i]));
+        if (i < A.sums_met) tcg::mbar_arrive(bar(&sums_bar[i]));
       }
       __syncwarp();
+    };
+    auto count = [&](int i, unsigned rows) {  // of this warp, sent to barrier i
+      if (lane == 0) atomicAdd(&sent[i], rows);
+      if (tid == 0 && i < A.sums_met) told[i] += rows;
     };
     // A place is written again SENDS rows later: a warp that sends row x + 4 has received
     // row x + 2, so every warp has sent that, and had received row x before.  (Of a row that
@@ -631,7 +647,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
     // its row: number, place, weight, the thread's pieces, those taken, the edge and the sums
     unsigned feed_k = 0, feed_t = first;
     float feed_w = weight(first), feed_wn = weight(first + step), feed_edge = 0.f;
-    int feed_n = 0, feed_whole = 0, feed_p = 0, feed_sent = 0, edges = 0;
+    int feed_n = 0, feed_whole = 0, feed_p = 0, edges = 0;
     Run feed;
     auto feed_row = [&] {  // starts on row feed_t
       const Span<T> S = span(feed_t);
@@ -757,6 +773,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
           const uint32_t parity = again & 1;
           ++again;
           send(SENDS, make_float4(warp_max(top), 0.f, 0.f, 0.f));
+          if (CL) count(SENDS, 1);
           wait(&sums_bar[SENDS], parity);
           top = -INFINITY;
           for (int j = lane; j < cols * MAX_WARPS; j += 32)
@@ -773,7 +790,10 @@ k_distill(const __grid_constant__ DistillArgs A) {
             for (int i = tid; i < S.pieces * N; i += D) add(to_f32(S.row[S.head + i]));
             if (tid < S.edges) add(to_f32(S.row[S.edge(tid)]));
           }
-          send_run(SENDS + 1, run);
+          if (!__any_sync(0xffffffffu, lost)) {
+            send_run(SENDS + 1, run);
+            if (CL) count(SENDS + 1, 1);
+          }
           run = receive(SENDS + 1, parity);
         }
         r.n = run.n;
@@ -899,35 +919,33 @@ k_distill(const __grid_constant__ DistillArgs A) {
       }
       if constexpr (!HELD) feed_direct();
       __syncwarp();
-      if (lane == 0 && !(A.unmet == LX_WAIT_CALL_WRITTEN && warp == 0 && k >= 2))
-        tcg::mbar_arrive(bar(&released_bar[b]));
+      if (lane == 0 && (warp > 0 || k < A.written_met)) tcg::mbar_arrive(bar(&released_bar[b]));
       w = wn;
       wn = wn2;
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
+    if (CL)
+#pragma unroll 1
+      for (int i = 0; i < SENDS; ++i) count(i, (feed_sent + SENDS - 1 - i) / SENDS);
   }
-  if constexpr (CL) {
-    // A CTA's shared memory outlives what its neighbours send: rows that were waited for have
-    // landed, after a wait that gave up the rest is waited for now.
-    cooperative_groups::this_cluster().sync();
-    if (gave_up && tid < SENDS + 2)
-      await_sent(bar(&sums_bar[tid]), sent, tid, cols, nw, is_unmet(tid) ? 16 : 0, A.wait_cycles);
-  } else {
-    __syncthreads();
-  }
-  if (gave_up) {  // the same in all of the row's CTAs
-    if (tid < A.teachers) {
-      unsigned k = lost_from[0][tid];
-      if constexpr (CL)
-        for (int c = 0; c < cols; ++c)
-          k = min(k, *cooperative_groups::this_cluster().map_shared_rank(&lost_from[0][tid], c));
-      lost_from[1][tid] = k;
+  // A CTA's shared memory outlives what its neighbours send: rows that were waited for have
+  // landed, after a wait that gave up the rest is waited for now.
+  if constexpr (CL) cooperative_groups::this_cluster().sync();
+  else if constexpr (GRAD) __syncthreads();
+  if constexpr (CL || GRAD) {
+    bool any = false;  // the same in all of the row's CTAs
+#pragma unroll
+    for (int i = 0; i < MAX_TEACHERS; ++i) any |= lost_from[i] != ~0u;
+    if (any) {
+      if (CL && tid < SENDS + 2)
+        await_sent(bar(&sums_bar[tid]), &sent[tid], told[tid], cols * nw, cols, A.wait_cycles);
+      if constexpr (GRAD) {
+        const int v0 = rank * A.slice;
+        rows_lost<T>(lost_from, A.teachers, first, step, T0, A.weight, rank == 0 ? A.loss : nullptr, (T*)A.dlogits + v0,
+                     A.ldd, min(A.slice, A.V - v0));
+      }
+      if constexpr (CL) cooperative_groups::this_cluster().sync();  // the others have read sent
     }
-    __syncthreads();
-    const int v0 = rank * A.slice;
-    rows_lost<T>(lost_from[1], A.teachers, first, step, T0, A.weight, A.loss, GRAD ? (T*)A.dlogits + v0 : nullptr, A.ldd,
-                 min(A.slice, A.V - v0), rank == 0);
-    if constexpr (CL) cooperative_groups::this_cluster().sync();  // the others have read sent and lost_from
   }
 }
 
@@ -1246,7 +1264,9 @@ extern "C" lx_status lx_distill_loss(int32_t dtype, const void* logits, int64_t 
   A.ldd = ldd;
   const CallWaits waits = take_call_waits();
   A.wait_cycles = waits.cycles;
-  A.unmet = waits.unmet;
+  A.sums_met = waits.unmet == LX_WAIT_CALL_SUMS ? 0 : waits.unmet == LX_WAIT_CALL_AGAIN ? SENDS : SENDS + 2;
+  A.entries_met = waits.unmet == LX_WAIT_CALL_ENTRIES ? 2 : ~0u;
+  A.written_met = waits.unmet == LX_WAIT_CALL_WRITTEN ? 2 : ~0u;
   A.table = 32;
   while (A.table < 2 * K) A.table *= 2;
   cudaStream_t s = (cudaStream_t)stream;
@@ -1255,7 +1275,7 @@ extern "C" lx_status lx_distill_loss(int32_t dtype, const void* logits, int64_t 
   // 16384, K 56: 74 and 87, K 300: 95 and 283, K 1000: 160 and 562; 64 x 1006, K 5: 6 either
   // way; 64 x 16384, K 512: 11 and 26.  With sixteen warps 5072 x 24000 takes 146, and 114 there.  (That
   // kernel alone has the waits.)
-  if ((long)V * es / 16 <= SHORT_P * 32 * 8 && !A.unmet)
+  if ((long)V * es / 16 <= SHORT_P * 32 * 8 && waits.unmet == LX_WAIT_NONE)
     return dtype == LX_BF16 ? launch_short_any<__nv_bfloat16>(A, s) : launch_short_any<float>(A, s);
   // CTAs of 256 data threads with half of an SM's shared memory (128 and a quarter for short
   // rows) where a row fits it, else CTAs of 512 with all of it, as many as hold a row; rows

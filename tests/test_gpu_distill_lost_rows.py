@@ -43,7 +43,9 @@ def test_a_row_is_right_or_nan(T, V, dtype, in_place, site):
         bad, db = run(want_grad=grad, dlogits=z if in_place and grad else None)
         torch.cuda.synchronize()
         lost = torch.isnan(bad)
-        assert lost.any() and not lost[off].any()
+        assert not lost[off].any()
+        # (losses alone are right before the wait for a row's dense values)
+        assert lost.any() or (not grad and site == lx.LX_WAIT_CALL_WRITTEN)
         assert torch.equal(bad[~lost], loss[~lost])
         if grad:
             assert torch.isnan(db[lost]).all()
