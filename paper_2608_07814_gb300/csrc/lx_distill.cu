@@ -432,7 +432,7 @@ k_distill(const __grid_constant__ DistillArgs A) {
       for (int j = lane; j < A.K; j += 32) {
         const int e = A.ids[(long)t * A.K + j];
         const float v = A.top[(long)t * A.K + j];
-        const bool ok = e >= 0 && e < A.V;
+        const bool ok = e >= 0 && e < A.V && v != -INFINITY;  // (a store's padding may hold any id)
         id[j] = ok ? e : -1;
         q[j] = ok ? v : -INFINITY;
         tm = fmaxf(tm, q[j]);
@@ -452,12 +452,12 @@ k_distill(const __grid_constant__ DistillArgs A) {
       } else {
         float s = 0.f;
         for (int j = lane; j < A.K; j += 32)
-          if (id[j] >= 0) s += tm == -INFINITY ? 0.f : expf((q[j] - tm) / A.tau);
+          if (id[j] >= 0) s += expf((q[j] - tm) / A.tau);
         lz = logf(warp_sum(s));
       }
       float m = 0.f;
       for (int j = lane; j < A.K; j += 32) {
-        const float l = id[j] >= 0 && q[j] != -INFINITY ? (q[j] - tm) / A.tau - lz : -INFINITY;
+        const float l = id[j] >= 0 ? (q[j] - tm) / A.tau - lz : -INFINITY;
         const float p = expf(l);
         lq[j] = l;
         q[j] = p;
@@ -1012,9 +1012,9 @@ k_distill_short(const __grid_constant__ DistillArgs A) {
       for (int j = tid; j <= A.K; j += TH) {
         const int e = j < A.K ? A.ids[(long)t * A.K + j] : A.labels ? A.labels[t] : -1;
         const float v = j < A.K ? A.top[(long)t * A.K + j] : 0.f;
-        const bool ok = e >= 0 && e < A.V;
+        const bool in = e >= 0 && e < A.V, ok = in && v != -INFINITY;  // (a store's padding may hold any id)
         id[j] = ok ? e : -1;
-        zj[j] = ok ? to_f32(S.row[e]) : 0.f;
+        zj[j] = in ? to_f32(S.row[e]) : 0.f;
         q[j] = ok ? v : -INFINITY;
         if (j < A.K) m[1] = fmaxf(m[1], q[j]);
       }
@@ -1072,7 +1072,7 @@ k_distill_short(const __grid_constant__ DistillArgs A) {
       s[0] = sum.x + sum.y;
       s[1] = sum1.x + sum1.y;
       for (int j = tid; j < A.K; j += TH)
-        if (id[j] >= 0 && tm != -INFINITY) s[2] += expf((q[j] - tm) / A.tau);
+        if (id[j] >= 0) s[2] += expf((q[j] - tm) / A.tau);
     }
     over_row(s, 1, false);
     const bool nan_row = w != 0.f && m[0] == -INFINITY && s[0] > 0.f;
@@ -1084,7 +1084,7 @@ k_distill_short(const __grid_constant__ DistillArgs A) {
     if (!dead) {
       const float lz = A.top_lse ? A.top_lse[t] - tm / A.tau : logf(s[2]), ls = logf(r.s);
       for (int j = tid; j < A.K; j += TH) {
-        const float l = id[j] >= 0 && q[j] != -INFINITY ? (q[j] - tm) / A.tau - lz : -INFINITY;
+        const float l = id[j] >= 0 ? (q[j] - tm) / A.tau - lz : -INFINITY;
         const float p = expf(l);
         q[j] = p;
         k[0] += p;
