@@ -47,6 +47,7 @@ struct NormArgs {
   const void* in[N_IN];   // NULL where absent
   uint32_t ldb[N_IN];     // bytes between rows
   uint32_t slot_at[N_IN]; // bytes from a stage's start to the array's slots
+  uint32_t ends;          // rows at either end of the arrays whose blocks may reach beyond
   uint32_t stage_bytes, stages;  // of a CTA's slots for one row; rows they hold, 3 or 2
   uint32_t par_at;        // bytes from the slots' start to the parameters'
   const float* gate;      // channel or token gate
@@ -168,7 +169,7 @@ struct Rows {
             const int off = shift(k, t), bytes = off + seg_n() * (int)sizeof(T);  // from the first block on
             const char* block = (const char*)src(k, t, seg()) - off + me;
             d += me;
-            if (seg_n() > 0 && t != 0 && t != (unsigned)A.T - 1) {
+            if (seg_n() > 0 && t >= A.ends && t + A.ends < (unsigned)A.T) {
               for (int b = me; b < bytes; b += step_b, block += step_b, d += step_b)
                 copy_async(d, block);
             } else if (seg_n() > 0) {
@@ -674,8 +675,10 @@ int resident(const Shape& s, size_t smem) {
 size_t ring_bytes(const Shape& s, NormArgs& A, size_t es, size_t more, bool block) {
   const int members = s.grp == WARP ? s.lanes : 32;
   size_t row = 0;
+  A.ends = 1;
   for (int k = 0; k < N_IN; ++k)
     if (A.in[k]) {
+      A.ends = std::max(A.ends, end_rows(A.ldb[k]));
       A.slot_at[k] = (uint32_t)row;
       row += block ? (size_t)(s.threads / members) * group_bytes(members, es) : EPT * es * s.threads;
     }

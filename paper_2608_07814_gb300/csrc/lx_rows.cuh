@@ -79,6 +79,11 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
+// Rows `ldb` bytes apart that are copied as the 16-byte blocks they touch: so many rows at either end
+// of their array lie so close to it that a block of theirs may reach beyond (a block starts
+// up to 15 bytes before its row and ends up to 15 behind it).  ldb = 0: a single row.
+__host__ __device__ constexpr uint32_t end_rows(uint32_t ldb) { return ldb == 0 || ldb >= 15 ? 1 : (14 + ldb) / ldb; }
+
 inline bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 // whether [a, a + na) and [b, b + nb) share a byte
 inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
