@@ -459,43 +459,58 @@ def compress_member(w_doms, w_mems, omegas, r: int, power_iters: int = 2, worksp
 # ----------------------------------------------------------------------------
 # the operators around a layer: block norms, router balance loss, distillation
 # ----------------------------------------------------------------------------
+# The tensors of a call, a workspace among them, lie on the current device: the library
+# launches there.
 _DTYPES = {torch.bfloat16: LX_BF16, torch.float32: LX_F32}
 
+# the current device, and the cudaStream_t of a device's current stream
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
-def _rows(t: torch.Tensor, name: str, shape=None, dtype=None) -> int:
-    """Checks a CUDA matrix of rows (unit stride inside a row) and returns their distance."""
-    if t.dim() != 2 or not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA matrix")
-    if shape is not None and t.shape != shape:
+
+def _device(t: torch.Tensor, name: str) -> int:
+    """Checks that a tensor is on the current device, where the launches go; its index."""
+    dev = t.get_device()
+    if dev < 0 or dev != _current_device():
+        raise ValueError(f"{name} must be a CUDA tensor on the current device")
+    return dev
+
+
+def _rows(t: torch.Tensor, name: str, dev: int, shape=None, dtype=None) -> int:
+    """Checks a matrix of rows (unit stride inside a row) on device dev and returns their distance."""
+    if t.dim() != 2 or t.get_device() != dev:
+        raise ValueError(f"{name} must be a matrix on cuda:{dev}")
+    have = t.shape
+    if shape is not None and have != shape:
         raise ValueError(f"{name} must have the shape {tuple(shape)}")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{name} must have the dtype {dtype}")
-    T, n = t.shape
+    T, n = have
     ld, inner = t.stride()
     if inner != 1 and n > 1:
         raise ValueError(f"{name} must have unit stride inside a row")
     return ld if T > 1 else max(n, 1)
 
 
-def _flat(t: Optional[torch.Tensor], name: str, n: int, dtype=torch.float32):
-    """Checks a contiguous CUDA array of n elements (or None) and returns its address."""
+def _flat(t: Optional[torch.Tensor], name: str, dev: int, n: int, dtype=torch.float32):
+    """Checks a contiguous array of n elements (or None) on device dev and returns its address."""
     if t is None:
         return None
-    if t.dtype != dtype or t.numel() != n or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous CUDA array of {n} {dtype} elements")
+    if t.dtype != dtype or t.numel() != n or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous array of {n} {dtype} elements on cuda:{dev}")
     return t.data_ptr()
 
 
-def _type(t: torch.Tensor, name: str) -> int:
-    code = _DTYPES.get(t.dtype)
+def _check_workspace(t: torch.Tensor, dev: int) -> None:
+    if t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous array on cuda:{dev}")
+
+
+def _type(dtype: torch.dtype, name: str) -> int:
+    code = _DTYPES.get(dtype)
     if code is None:
         raise ValueError(f"{name} must be bf16 or fp32")
     return code
-
-
-def _raw_stream(t: torch.Tensor) -> int:
-    """cudaStream_t of the current stream of the tensor's device."""
-    return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
 def _elsewhere(stream, fn, args, kwargs):
@@ -517,24 +532,25 @@ def _elsewhere(stream, fn, args, kwargs):
     return out
 
 
-def _resnorm_desc(r, y, w_post, gate, w_pre, res_scale, weight_offset, eps) -> ResnormDesc:
-    ldr = _rows(r, "r")
-    T, H = r.shape
-    dtype = r.dtype
+def _resnorm_desc(dev, r, y, w_post, gate, w_pre, res_scale, weight_offset, eps):
+    """(descriptor, r's shape, its dtype)."""
+    ldr = _rows(r, "r", dev)
+    shape, dtype = r.shape, r.dtype
+    T, H = shape
     kind = ldy = ldg = 0
     yp = gp = None
     if y is not None:
-        ldy, yp = _rows(y, "y", r.shape, dtype), y.data_ptr()
+        ldy, yp = _rows(y, "y", dev, shape, dtype), y.data_ptr()
     if gate is not None:
         if gate.dim() == 1:
-            kind, gp = LX_GATE_CHANNEL, _flat(gate, "a gate of one dimension", H)
+            kind, gp = LX_GATE_CHANNEL, _flat(gate, "a gate of one dimension", dev, H)
         elif gate.shape == (T, 1) and (H != 1 or gate.dtype == torch.float32):
-            kind, ldg, gp = LX_GATE_TOKEN, _rows(gate, "gate", None, torch.float32), gate.data_ptr()
+            kind, ldg, gp = LX_GATE_TOKEN, _rows(gate, "gate", dev, None, torch.float32), gate.data_ptr()
         else:
-            kind, ldg, gp = LX_GATE_FULL, _rows(gate, "gate", r.shape, dtype), gate.data_ptr()
-    return ResnormDesc(_type(r, "r"), T, H, kind, ldr, ldy, ldg, r.data_ptr(), yp, gp,
-                       _flat(w_post, "w_post", H), _flat(w_pre, "w_pre", H), res_scale, weight_offset,
-                       eps)
+            kind, ldg, gp = LX_GATE_FULL, _rows(gate, "gate", dev, shape, dtype), gate.data_ptr()
+    return ResnormDesc(_type(dtype, "r"), T, H, kind, ldr, ldy, ldg, r.data_ptr(), yp, gp,
+                       _flat(w_post, "w_post", dev, H), _flat(w_pre, "w_pre", dev, H), res_scale,
+                       weight_offset, eps), shape, dtype
 
 
 def residual_norm(r: torch.Tensor, y: Optional[torch.Tensor] = None, *, w_post=None, gate=None,
@@ -555,14 +571,15 @@ def residual_norm(r: torch.Tensor, y: Optional[torch.Tensor] = None, *, w_post=N
         return _elsewhere(stream, residual_norm, (r, y), dict(
             w_post=w_post, gate=gate, w_pre=w_pre, res_scale=res_scale, weight_offset=weight_offset,
             eps=eps, r_out=r_out, h_out=h_out, stats=stats))
-    d = _resnorm_desc(r, y, w_post, gate, w_pre, res_scale, weight_offset, eps)
-    n, dtype = r.numel(), r.dtype
+    dev = _device(r, "r")
+    d, shape, dtype = _resnorm_desc(dev, r, y, w_post, gate, w_pre, res_scale, weight_offset, eps)
+    n = shape[0] * shape[1]
+    rp, hp = _flat(r_out, "r_out", dev, n, dtype), _flat(h_out, "h_out", dev, n, dtype)
     if r_out is None and (y is not None or res_scale != 1.0):
-        r_out = torch.empty(r.shape, dtype=dtype, device=r.device)
+        r_out, rp = _empty_for(r, shape)
     if h_out is None and w_pre is not None:
-        h_out = torch.empty(r.shape, dtype=dtype, device=r.device)
-    status = lib().lx_residual_norm(d, _flat(r_out, "r_out", n, dtype), _flat(h_out, "h_out", n, dtype),
-                                    _flat(stats, "stats", 2 * d.T), _raw_stream(r))
+        h_out, hp = _empty_for(r, shape)
+    status = lib().lx_residual_norm(d, rp, hp, _flat(stats, "stats", dev, 2 * shape[0]), _raw_stream(dev))
     if status:
         _check(status)
     return (r if r_out is None else r_out), h_out
@@ -601,24 +618,27 @@ def residual_norm_backward(dr_out, dh, r, y, stats, *, w_post=None, gate=None, w
         return _elsewhere(stream, residual_norm_backward, (dr_out, dh, r, y, stats), dict(
             w_post=w_post, gate=gate, w_pre=w_pre, res_scale=res_scale, weight_offset=weight_offset,
             workspace=workspace))
-    d = _resnorm_desc(r, y, w_post, gate, w_pre, res_scale, weight_offset, 0.0)
-    shape, H = r.shape, d.H
+    dev = _device(r, "r")
+    d, shape, dtype = _resnorm_desc(dev, r, y, w_post, gate, w_pre, res_scale, weight_offset, 0.0)
+    T, H = shape
     lddr = lddh = 0
     drp = dhp = None
     if dr_out is not None:
-        lddr, drp = _rows(dr_out, "dr_out", shape, r.dtype), dr_out.data_ptr()
+        lddr, drp = _rows(dr_out, "dr_out", dev, shape, dtype), dr_out.data_ptr()
     if dh is not None:
-        lddh, dhp = _rows(dh, "dh", shape, r.dtype), dh.data_ptr()
+        lddh, dhp = _rows(dh, "dh", dev, shape, dtype), dh.data_ptr()
     dr, p0 = _empty_for(r, shape)
     dy, p1 = _empty_for(y, shape)
     dw_post, p2 = _empty_for(w_post, H)
     dgate, p3 = _empty_for(gate, None if gate is None else gate.shape)
     dw_pre, p4 = _empty_for(w_pre, H)
     if workspace is None:
-        workspace = torch.empty(residual_norm_workspace_bytes(d.T, H), dtype=torch.uint8, device=r.device)
+        workspace = torch.empty(residual_norm_workspace_bytes(T, H), dtype=torch.uint8, device=r.device)
+    else:
+        _check_workspace(workspace, dev)
     status = lib().lx_residual_norm_backward(
-        d, _flat(stats, "stats", 2 * d.T), drp, lddr, dhp, lddh, p0, p1, p2, p3, p4,
-        workspace.data_ptr(), workspace.nbytes, _raw_stream(r))
+        d, _flat(stats, "stats", dev, 2 * T), drp, lddr, dhp, lddh, p0, p1, p2, p3, p4,
+        workspace.data_ptr(), workspace.nbytes, _raw_stream(dev))
     if status:
         _check(status)
     return ResidualNormGrads(dr, dy, dw_post, dgate, dw_pre)
@@ -650,26 +670,29 @@ def router_balance(logits: torch.Tensor, topk_id: torch.Tensor, *, mask=None,
     if stream is not None:
         return _elsewhere(stream, router_balance, (logits, topk_id), dict(
             mask=mask, balance_coef=balance_coef, z_coef=z_coef, workspace=workspace))
-    ld = _rows(logits, "logits")
+    at = _device(logits, "logits")
+    ld = _rows(logits, "logits", at)
     T, E = logits.shape
     if topk_id.dim() != 2 or topk_id.shape[0] != T:
         raise ValueError("topk_id must be [T, k]")
     k, dev = topk_id.shape[1], logits.device
-    ids = _flat(topk_id, "topk_id", T * k, torch.int32)
+    ids = _flat(topk_id, "topk_id", at, T * k, torch.int32)
     if mask is not None:
         if mask.dtype not in (torch.bool, torch.uint8):
             raise ValueError("mask must be bool or uint8")
-        mask = _flat(mask, "mask", T, mask.dtype)
+        mask = _flat(mask, "mask", at, T, mask.dtype)
     loss = torch.empty(3, dtype=torch.float32, device=dev)
     counts = torch.empty(E + 1, dtype=torch.int32, device=dev)
     prob = torch.empty(E, dtype=torch.float32, device=dev)
     lse = torch.empty(T, dtype=torch.float32, device=dev)
     if workspace is None:
         workspace = torch.empty(router_balance_workspace_bytes(T, E), dtype=torch.uint8, device=dev)
+    else:
+        _check_workspace(workspace, at)
     status = lib().lx_router_balance(
-        _type(logits, "logits"), logits.data_ptr(), ld, ids, mask, T, E, k, balance_coef, z_coef,
+        _type(logits.dtype, "logits"), logits.data_ptr(), ld, ids, mask, T, E, k, balance_coef, z_coef,
         counts.data_ptr(), prob.data_ptr(), lse.data_ptr(), loss.data_ptr(), workspace.data_ptr(),
-        workspace.nbytes, _raw_stream(logits))
+        workspace.nbytes, _raw_stream(at))
     if status:
         _check(status)
     return RouterBalance(loss, counts, prob, lse)
@@ -685,14 +708,16 @@ def router_balance_backward(logits: torch.Tensor, state: RouterBalance, k: int, 
     if stream is not None:
         return _elsewhere(stream, router_balance_backward, (logits, state, k), dict(
             dloss=dloss, balance_coef=balance_coef, z_coef=z_coef, out=out))
-    ld = _rows(logits, "logits")
+    dev = _device(logits, "logits")
+    ld = _rows(logits, "logits", dev)
     T, E = logits.shape
+    op = _flat(out, "out", dev, T * E, logits.dtype)
     if out is None:
-        out = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
+        out, op = _empty_for(logits, (T, E))
     status = lib().lx_router_balance_backward(
-        _type(logits, "logits"), logits.data_ptr(), ld, _flat(state.lse, "lse", T),
-        _flat(state.counts, "counts", E + 1, torch.int32), _flat(dloss, "dloss", 1), T, E, k, balance_coef,
-        z_coef, _flat(out, "out", T * E, logits.dtype), _raw_stream(logits))
+        _type(logits.dtype, "logits"), logits.data_ptr(), ld, _flat(state.lse, "lse", dev, T),
+        _flat(state.counts, "counts", dev, E + 1, torch.int32), _flat(dloss, "dloss", dev, 1), T, E, k,
+        balance_coef, z_coef, op, _raw_stream(dev))
     if status:
         _check(status)
     return out
@@ -716,26 +741,27 @@ def distill_loss(logits: torch.Tensor, teacher_id: torch.Tensor, teacher_logit: 
         return _elsewhere(stream, distill_loss, (logits, teacher_id, teacher_logit), dict(
             temperature=temperature, teacher_lse=teacher_lse, kd_weight=kd_weight, labels=labels,
             ce_weight=ce_weight, row_weight=row_weight, want_grad=want_grad, dlogits=dlogits))
-    ld = _rows(logits, "logits")
+    at = _device(logits, "logits")
+    ld = _rows(logits, "logits", at)
     T, V = logits.shape
     dtype = logits.dtype
     if teacher_id.dim() != 2 or teacher_id.shape[0] != T:
         raise ValueError("teacher_id must be [T, K]")
     K, dev = teacher_id.shape[1], logits.device
-    code = _type(logits, "logits")
-    ids = _flat(teacher_id, "teacher_id", T * K, torch.int32)
-    top = _flat(teacher_logit, "teacher_logit", T * K)
+    code = _type(dtype, "logits")
+    ids = _flat(teacher_id, "teacher_id", at, T * K, torch.int32)
+    top = _flat(teacher_logit, "teacher_logit", at, T * K)
     loss = torch.empty(T, dtype=torch.float32, device=dev)
     ldd, dp = V, None
     if dlogits is not None:
-        ldd, dp = _rows(dlogits, "dlogits", logits.shape, dtype), dlogits.data_ptr()
+        ldd, dp = _rows(dlogits, "dlogits", at, logits.shape, dtype), dlogits.data_ptr()
     elif want_grad:
         dlogits = torch.empty((T, V), dtype=dtype, device=dev)
         dp = dlogits.data_ptr()
     status = lib().lx_distill_loss(
-        code, logits.data_ptr(), ld, ids, top, _flat(teacher_lse, "teacher_lse", T),
-        _flat(labels, "labels", T, torch.int32), _flat(row_weight, "row_weight", T), T, V, K, temperature,
-        kd_weight, ce_weight, loss.data_ptr(), dp, ldd, _raw_stream(logits))
+        code, logits.data_ptr(), ld, ids, top, _flat(teacher_lse, "teacher_lse", at, T),
+        _flat(labels, "labels", at, T, torch.int32), _flat(row_weight, "row_weight", at, T), T, V, K,
+        temperature, kd_weight, ce_weight, loss.data_ptr(), dp, ldd, _raw_stream(at))
     if status:
         _check(status)
     return loss, dlogits
