@@ -6,12 +6,13 @@ layers (`lx.Layer`) inside residual blocks (`lx.residual_norm`).  The norms afte
 student's blocks, their gates and the last norm are then trained on
 
     distillation from the teacher's stored top logits  (`lx.distill_loss`)
-  + the routers' balance and z loss                    (`lx.router_balance`)
+  + the later routers' balance and z loss              (`lx.router_balance`)
 
 with `lx.residual_norm_backward` and `lx.router_balance_backward`.  The compressed experts
 stay as they are, and no gradient is taken through them: a block's gradient reaches
 earlier blocks along the residual and through the routers.  The norms before the blocks
-act through the experts, so they stay as they are, too.
+act through the experts, so they stay as they are, too, and so does what the first
+block's router sees: it has no part in the loss.
 
     python examples/heal.py [--steps 30]
 """
@@ -144,10 +145,10 @@ def heal(steps=30, lr=0.01, temperature=2.0, seed=0):
     for _ in range(steps):
         r, h = lx.residual_norm(x, w_pre=first, eps=EPS)
         kept, balances = [], []
-        for b in student:
+        for i, b in enumerate(student):
             r, h, k = b.forward(r, h, keep=True)
             kept.append(k)
-            balances.append(lx.router_balance(k[4], k[3], balance_coef=BALANCE, z_coef=Z))
+            balances.append(lx.router_balance(k[4], k[3], balance_coef=BALANCE, z_coef=Z) if i else None)
         logits = h @ head.t()
         # the gradient takes the logits' place
         loss, dlogits = lx.distill_loss(logits, ids, top, temperature=temperature, teacher_lse=lse,
@@ -155,13 +156,16 @@ def heal(steps=30, lr=0.01, temperature=2.0, seed=0):
         dh, dr = dlogits @ head, None
         for b, (r_in, y, stats, _, rl), bal in zip(reversed(student), reversed(kept), reversed(balances)):
             g = lx.residual_norm_backward(dr, dh, r_in, y, stats, w_post=b.w_post, gate=b.gate, w_pre=b.w_pre)
-            b.w_post.grad, b.gate.grad, b.w_pre.grad = g.dw_post, g.dgate, g.dw_pre
-            # the router's logits came from the block's input
-            drouter = lx.router_balance_backward(rl, bal, K, balance_coef=BALANCE, z_coef=Z)
-            dr, dh = g.dr, (drouter @ b.router.float()).bfloat16()
+            b.w_post.grad, b.gate.grad = g.dw_post, g.dgate
+            if b is student[-1]:
+                b.w_pre.grad = g.dw_pre
+            if bal is not None:
+                # the router's logits came from the block's input
+                drouter = lx.router_balance_backward(rl, bal, K, balance_coef=BALANCE, z_coef=Z)
+                dr, dh = g.dr, (drouter @ b.router.float()).bfloat16()
         optimiser.step()
-        history.append((torch.stack([loss.sum() + sum(v.loss[0] for v in balances), loss.sum(),
-                                     sum(v.loss[1] for v in balances)]), balances[-1].counts))
+        history.append((torch.stack([loss.sum() + sum(v.loss[0] for v in balances[1:]), loss.sum(),
+                                     sum(v.loss[1] for v in balances[1:])]), balances[-1].counts))
     return [(v.tolist(), c.tolist()) for v, c in history]
 
 
