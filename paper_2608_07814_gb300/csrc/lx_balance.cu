@@ -28,7 +28,6 @@ constexpr int BAL_THREADS = 256;
 constexpr int BAL_WARPS = BAL_THREADS / 32;
 constexpr int TILE = 256, TILE_WORDS = TILE / 32;  // tokens whose sets a CTA holds as bits
 static_assert(TILE_WORDS == BAL_WARPS, "the warps' column sums take the bits' place");
-constexpr int SMS = 152;
 constexpr int SUM_CTAS = 8, SUM_THREADS = 1024;  // the second launch: one cluster
 
 struct BalArgs {
@@ -112,12 +111,6 @@ struct Raw {
     }
   }
 };
-
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 
 // v becomes exp(v - max); returns its sum's reciprocal, 0 for a row of nothing but -inf
 // (a NaN shows in the sum), and the row's log-sum-exp
@@ -578,6 +571,6 @@ extern "C" lx_status lx_router_balance_backward(int32_t dtype, const void* logit
   A.dlogits = dlogits;
   const bool vec = E % (16 / es) == 0 && aligned(logits, 16) && ld * es % 16 == 0 && aligned(dlogits, 16);
   const long rows = BAL_THREADS / lanes_of(E, true);
-  const int grid = (int)std::min(((long)T + rows - 1) / rows, 8L * 152);
+  const int grid = (int)std::min(((long)T + rows - 1) / rows, 8L * SMS);
   return launch_any<true>(dtype, vec, A, grid, 0, (cudaStream_t)stream);
 }

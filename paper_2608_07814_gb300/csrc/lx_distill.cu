@@ -48,7 +48,6 @@ namespace {
 
 using namespace rows;
 
-constexpr int SMS = 152;
 constexpr int MAX_WARPS = 16;    // data warps of a CTA
 constexpr int BUFS = 4;          // rows whose entries are held
 constexpr int MAX_TEACHERS = 4;  // warps that prepare entries: 2, or 4 beside 16 data warps
@@ -89,12 +88,6 @@ struct DistillArgs {
   int sums_met;                       // exchanges that are told of, SENDS + 2 for all
   unsigned entries_met, written_met;  // a CTA's rows whose entries, whose dense gradient are told of
 };
-
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 
 __device__ __forceinline__ float lg2(float x) {
   float y;

@@ -661,8 +661,6 @@ Shape shape_of(int T, int H) {
   return s;
 }
 
-constexpr int SMS = 152;
-
 // CTAs (clusters) that rows are dealt to: as many as the SMs hold, by their registers
 // (this bounds the backward's workspace) and with `smem` bytes each
 int ctas_per_sm(const Shape& s) { return std::max(1, 65536 / (REGS * s.threads)); }

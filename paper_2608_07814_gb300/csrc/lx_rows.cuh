@@ -8,6 +8,8 @@
 namespace lx {
 namespace rows {
 
+constexpr int SMS = 152;  // of the GPU: shapes grids alone
+
 // VEC fp32 values to consecutive elements at p; VEC * sizeof(T) is 16 (p 16-byte aligned)
 // or VEC is 1
 template <typename T, int VEC>
@@ -73,6 +75,11 @@ __device__ __forceinline__ uint32_t to_bf2(float2 v) {
   return *reinterpret_cast<const uint32_t*>(&b);
 }
 
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
