@@ -72,7 +72,7 @@ typedef enum {
   LX_ERR_UNSUPPORTED = 7   /* valid request the library does not implement */
 } lx_status;
 
-typedef enum { LX_F32 = 0, LX_BF16 = 1 } lx_dtype;
+typedef enum { LX_F32 = 0, LX_BF16 = 1, LX_E4M3 = 2 } lx_dtype; /* LX_E4M3: lx_linear alone */
 
 typedef struct lx_layer lx_layer; /* opaque, library-owned */
 
@@ -595,6 +595,92 @@ LX_API lx_status lx_distill_loss(int32_t dtype, const void* logits, int64_t ld,
                                  const float* row_weight, int32_t T, int32_t V, int32_t K,
                                  float temperature, float kd_weight, float ce_weight, float* loss,
                                  void* dlogits, int64_t ldd, void* stream);
+
+/*
+ * Products around a compressed layer: the norm before a dense block with its output in 8
+ * bits, the block's products with their epilogue and gradients, and the loss on the head's
+ * product.  Standalone calls on plain device arrays, stream-ordered, without allocation;
+ * products accumulate in fp32, and results do not depend on scheduling.  If one of their
+ * bounded waits gives up, the outputs that depend on it are NaN.
+ */
+
+/*
+ * lx_residual_norm_q8: lx_residual_norm (which see for desc, r_out and stats) with h in
+ * e4m3 and a scale for each token, as lx_linear reads it:
+ *   scale_t = max(max_i |h_ti| / 448, 2^-126),  q_ti = e4m3(h_ti / scale_t)  (to nearest even)
+ * A row that holds a NaN or an infinity has NaNs in q and a NaN or infinite scale.
+ *   desc: w_pre is given;  q_out: e4m3 [T][H];  scale: fp32 [T]
+ *   h_out: [T][H] in dtype, h itself beside q, or NULL
+ *   q_out and scale overlap nothing.  Errors as lx_residual_norm.
+ * The gradients with respect to h are lx_residual_norm_backward's (with stats).
+ */
+LX_API lx_status lx_residual_norm_q8(const lx_resnorm_desc* desc, void* r_out, void* q_out, float* scale,
+                                     void* h_out, float* stats, void* stream);
+
+/*
+ * lx_linear: a dense product with its epilogue, per token t and output n:
+ *   z = (sum_k x_tk w_nk) x_scale_t w_scale_n + bias_n      (the scales with LX_E4M3 alone)
+ *   y = act(z) + residual_tn
+ * act: none, max(z, 0), z / (1 + exp(-z)), z (1 + erf(z / sqrt 2)) / 2.
+ *   dtype: of x and w: LX_BF16, or LX_E4M3 (what lx_residual_norm_q8 gives, and weights
+ *          with a scale for each output)
+ *   x [T][K] (rows ldx apart), w [N][K] (ldw): 16-byte aligned, K, ldx and ldw multiples of 16
+ *   bytes; T tokens (0: no-op) up to 2^30, N and K up to 2^24
+ *   x_scale fp32 [T], w_scale fp32 [N];  bias bf16 [N] or NULL;  residual bf16 [T][N] (ldr)
+ *   or NULL
+ *   y bf16 [T][N] (ldy), may be residual itself (ldr = ldy);  pre: bf16 [T][N] or NULL: z,
+ *   which the backward of an activation reads;  outputs overlap nothing else
+ * lx_linear_backward (LX_BF16; desc's scales, bias and residual are not read): from dy (rows
+ * lddy apart) and pre (given exactly with an activation), with dz = dy act'(pre):
+ *   dx [T][K] = dz w,  dw [N][K] = dz^T x,  dbias [N] = sum_t dz, all bf16 and 16-byte
+ *   aligned (dbias: 2-byte), each or NULL.  (The residual's gradient is dy.)  dz is rounded
+ *   to bf16 for the two products.
+ *   workspace: device, 256-byte aligned, lx_linear_workspace bytes;  T == 0: dw and dbias
+ *   are zeroed
+ * Errors: LX_ERR_ARG (NULL, dtype, activation, alignment, overlap, workspace), LX_ERR_SHAPE
+ * (sizes, leading dimensions), LX_ERR_UNSUPPORTED (gradients of LX_E4M3).
+ */
+typedef enum { LX_ACT_NONE = 0, LX_ACT_RELU = 1, LX_ACT_SILU = 2, LX_ACT_GELU = 3 } lx_activation;
+typedef struct {
+  int32_t dtype, T, N, K, act;
+  int64_t ldx, ldw, ldr;
+  const void* x;
+  const void* w;
+  const float* x_scale;
+  const float* w_scale;
+  const void* bias;
+  const void* residual;
+} lx_linear_desc;
+LX_API lx_status lx_linear(const lx_linear_desc* desc, void* y, int64_t ldy, void* pre, void* stream);
+LX_API lx_status lx_linear_workspace(int32_t T, int32_t N, int32_t K, uint64_t* bytes);
+LX_API lx_status lx_linear_backward(const lx_linear_desc* desc, const void* dy, int64_t lddy,
+                                    const void* pre, void* dx, void* dw, void* dbias, void* workspace,
+                                    uint64_t workspace_bytes, void* stream);
+
+/*
+ * lx_head_loss: softmax cross-entropy over the vocabulary from the last hidden states h and
+ * the head's weights w, with its gradients, the logits not kept:
+ *   z = h w^T,  loss_t = row_weight_t (log sum_v exp(z_tv) - z_t,label_t)
+ *   dz_tv = row_weight_t (softmax(z_t)_v - [v = label_t]),  dh = dz w,  dw = dz^T h
+ * A token whose label is outside [0, V) or whose weight is 0 takes no part: loss 0, dh 0,
+ * and its hidden state, whatever it holds, is not used.  dz is rounded to bf16 for the two
+ * gradient products.
+ *   h bf16 [T][H] (rows ldh apart), w bf16 [V][H] (ldw): 16-byte aligned; H, ldh and ldw
+ *   multiples of 8;  T up to 2^24 (0: dw is zeroed), V up to 2^24, H up to 2^20
+ *   labels int32 [T];  row_weight fp32 [T] or NULL for 1 (a mean's 1 / n goes here)
+ *   loss fp32 [T] out;  dh bf16 [T][H], dw bf16 [V][H] out, 16-byte aligned, each or NULL:
+ *   the gradients of the losses' sum
+ *   workspace: device, 256-byte aligned, lx_head_loss_workspace bytes (which of dh and dw
+ *   are wanted): it grows with T H and, eight bytes for 128 logits, with T V; the
+ *   vocabulary is worked on in pieces whose dz takes at most 256 MiB, or 256 columns
+ * Errors: LX_ERR_ARG (NULL, alignment, overlap, workspace), LX_ERR_SHAPE (sizes, leading
+ * dimensions).
+ */
+LX_API lx_status lx_head_loss_workspace(int32_t T, int32_t V, int32_t H, int32_t want_dh, int32_t want_dw,
+                                        uint64_t* bytes);
+LX_API lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int64_t ldw, const int32_t* labels,
+                              const float* row_weight, int32_t T, int32_t V, int32_t H, float* loss,
+                              void* dh, void* dw, void* workspace, uint64_t workspace_bytes, void* stream);
 
 /* Message of the last failed call on this thread ("" if none). */
 LX_API const char* lx_last_error(void);

@@ -108,6 +108,22 @@ bool encode_bf16_2d(CUtensorMap* m, const void* base, long inner, long outer, in
          CUDA_SUCCESS;
 }
 
+namespace prod {
+// (lx_product.cuh) rows of `inner` bytes, ld bytes apart, in boxes of 128 bytes x box_rows rows
+// with the 128-byte swizzle: coordinates are bytes and rows, whatever the elements' type
+bool encode_bytes_2d(CUtensorMap* m, const void* base, long inner, long rows, long ld, int box_rows) {
+  auto encode = get_encode();
+  if (!encode) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)ld};
+  const cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
+  const cuuint32_t estr[2] = {1, 1};
+  return encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+}  // namespace prod
+
 // TMA store map of a bf16 output buffer [rows][ld]: 32 x 32 boxes staged with
 // the 64-byte swizzle (the 256-row tensor-core epilogue)
 static bool encode_store_map(CUtensorMap* m, void* base, long rows, long ld) {

@@ -1,0 +1,369 @@
+// Softmax cross-entropy over the vocabulary from the last hidden states and the head's
+// weights (lx_head_loss), without the logits:
+//   z = h W^T,  loss_t = w_t (log sum_v exp(z_tv) - z_t,label)
+//   dz_tv = w_t (softmax(z_t)_v - [v = label_t]),  dh = dz W,  dW = dz^T h
+// Tokens without a label (or of weight 0) take no part: the others' hidden states are copied
+// side by side first, so that they cost no products and what they hold reaches nothing.
+// Then (all products on lx_product.cuh):
+//   1  the logits' tiles, of which each keeps a row's largest value and sum of exponentials
+//      (fp32), 8 bytes for 128 logits;
+//   2  each row's log-sum-exp and loss;
+//   3  by pieces of the vocabulary: the logits again, now turned into dz (bf16) on their way out
+//      of the tensor core, and the two gradient products of the piece in one launch.  dh is
+//      held in fp32 between the pieces.
+// With the logits formed twice that is 8 T V H operations against the 6 that a kept [T][V]
+// needs, and a workspace that does not grow with T V.
+#include "lx_product.cuh"
+
+namespace lx {
+namespace {
+
+using namespace rows;
+using namespace prod;
+
+constexpr int ROWS = 64;                     // of a CTA of k_head_rows
+constexpr long PIECE_BYTES = 256L << 20;     // of dz at most
+constexpr int MAX_T = 1 << 24, MAX_V = 1 << 24, MAX_H = 1 << 20;
+
+struct Head {
+  int T, V, H, Tp;  // Tp: rows of the compact arrays, a multiple of 256
+  const __nv_bfloat16* h;
+  long ldh;
+  const int* labels;
+  const float* row_weight;
+  float* loss;
+  __nv_bfloat16* dh;
+  // compact
+  __nv_bfloat16* hc;
+  int *label, *row, *n;
+  float *weight, *lse2;
+  const __nv_bfloat16* w;
+  long ldw;
+  const float2* part;
+  int slots;
+  const float* blocks;
+  int slices;
+};
+
+__device__ __forceinline__ bool counts(const Head& A, int t) {
+  const int l = A.labels[t];
+  return l >= 0 && l < A.V && (!A.row_weight || A.row_weight[t] != 0.f);
+}
+
+// The rows that count, side by side in their order; loss and dh of the others are 0.  Each CTA
+// counts the rows before its own and all of them by itself: one launch, and for 8192 rows
+// as long as the copies.
+__global__ void __launch_bounds__(256) k_head_rows(const __grid_constant__ Head A) {
+  __shared__ int red[2][8];
+  __shared__ int place[ROWS], first;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t0 = blockIdx.x * ROWS;
+  int before = 0, all = 0;
+#pragma unroll 4
+  for (int t = threadIdx.x; t < A.T; t += 256) {
+    const int c = counts(A, t);
+    all += c;
+    before += t < t0 ? c : 0;
+  }
+  before = __reduce_add_sync(0xffffffffu, before);
+  all = __reduce_add_sync(0xffffffffu, all);
+  if (lane == 0) red[0][warp] = before, red[1][warp] = all;
+  __syncthreads();
+  before = all = 0;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) before += red[0][w], all += red[1][w];
+  if (threadIdx.x < ROWS) {
+    const int t = t0 + threadIdx.x;
+    const bool c = t < A.T && counts(A, t);
+    const unsigned m = __ballot_sync(0xffffffffu, c);
+    const int at = __popc(m & ((1u << lane) - 1u));
+    if (threadIdx.x == 0) first = __popc(m);  // of the first warp's rows
+    place[threadIdx.x] = c ? at : -1;
+  }
+  __syncthreads();
+  if (threadIdx.x < ROWS) {
+    const int t = t0 + threadIdx.x;
+    int at = place[threadIdx.x];
+    if (at >= 0) {
+      at += before + (warp == 1 ? first : 0);
+      place[threadIdx.x] = at;
+      A.label[at] = A.labels[t];
+      A.weight[at] = A.row_weight ? A.row_weight[t] : 1.f;
+      A.row[at] = t;
+    } else if (t < A.T) {
+      A.loss[t] = 0.f;
+    }
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) *A.n = all;
+  __syncthreads();
+  const int pieces = A.H / 8;
+  for (int r = warp; r < ROWS; r += 8) {
+    const int t = t0 + r, at = place[r];
+    if (t < A.T) {
+      if (at >= 0) {
+        const uint4* s = (const uint4*)(A.h + (long)t * A.ldh);
+        uint4* d = (uint4*)(A.hc + (long)at * A.H);
+#pragma unroll 4
+        for (int c = lane; c < pieces; c += 32) d[c] = s[c];
+      } else if (A.dh) {
+        uint4* d = (uint4*)(A.dh + (long)t * A.H);
+        for (int c = lane; c < pieces; c += 32) d[c] = make_uint4(0u, 0u, 0u, 0u);
+      }
+    }
+    // rows of the last, ragged block of a sum over the tokens
+    if (t >= all && t < (all + 63) / 64 * 64) {
+      uint4* d = (uint4*)(A.hc + (long)t * A.H);
+      for (int c = lane; c < pieces; c += 32) d[c] = make_uint4(0u, 0u, 0u, 0u);
+    }
+  }
+}
+
+// A row's log-sum-exp (in units of log 2, as the exponentials are taken) and loss.  A lane a row,
+// 32 warps a CTA side by side over the partial sums, added in the warps' order.  The label's
+// logit is formed again by a warp: the tensor core cuts its running sums off instead of
+// rounding them, 4e-6 of a logit of 2048 terms, which a loss shows and its gradient does not.
+__global__ void __launch_bounds__(1024) k_head_lse(const __grid_constant__ Head A) {
+  __shared__ float2 red[32][33];
+  __shared__ float own[32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.x * 32 + lane, n = *A.n;
+  if (blockIdx.x * 32 >= n) return;
+  auto join = [](float2 a, float2 b) {
+    const float m = fmaxf(a.x, b.x);
+    if (m == -INFINITY) return make_float2(m, a.y + b.y);
+    const float at = m * LOG2E;
+    return make_float2(m, a.y * ex2(fmaf(a.x, LOG2E, -at)) + b.y * ex2(fmaf(b.x, LOG2E, -at)));
+  };
+  float2 v = make_float2(-INFINITY, 0.f);
+  if (i < n)
+#pragma unroll 4
+    for (int s = warp; s < A.slots; s += 32) v = join(v, A.part[(long)s * A.Tp + i]);
+  red[warp][lane] = v;
+  if (blockIdx.x * 32 + warp < n) {  // a row's label's logit
+    const int r = blockIdx.x * 32 + warp;
+    const uint4* a = (const uint4*)(A.hc + (long)r * A.H);
+    const uint4* b = (const uint4*)(A.w + (long)A.label[r] * A.ldw);
+    float2 s = make_float2(0.f, 0.f);
+#pragma unroll 4
+    for (int c = lane; c < A.H / 8; c += 32) {
+      const uint4 x = a[c], y = b[c];
+      s = fmas(bf2(x.x), bf2(y.x), s);
+      s = fmas(bf2(x.y), bf2(y.y), s);
+      s = fmas(bf2(x.z), bf2(y.z), s);
+      s = fmas(bf2(x.w), bf2(y.w), s);
+    }
+    const float z = warp_sum(s.x + s.y);
+    if (lane == 0) own[warp] = z;
+  }
+  __syncthreads();
+  if (warp == 0 && i < n) {
+#pragma unroll 4
+    for (int w = 1; w < 32; ++w) v = join(v, red[w][lane]);
+    const float l2 = v.x * LOG2E + log2f(v.y);
+    A.lse2[i] = l2;
+    A.loss[A.row[i]] = A.weight[i] * (l2 * 0.69314718055994531f - own[lane]);
+  }
+}
+
+// dh from its fp32 blocks: the slices in their order, rounded once, each row to its place
+__global__ void __launch_bounds__(256) k_head_dh(const __grid_constant__ Head A) {
+  __shared__ __align__(16) char stage[8][32 * STG_LD];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int rb = blockIdx.x, cb = blockIdx.y * 8 + warp, ncb = (A.H + 31) / 32, nrb = A.Tp / 32, n = *A.n;
+  if (rb * 32 >= n || cb >= ncb) return;
+  float v[32];
+#pragma unroll
+  for (int e = 0; e < 32; ++e) v[e] = 0.f;
+  for (int s = 0; s < A.slices; ++s) {
+    const float* b = A.blocks + (((long)s * nrb + rb) * ncb + cb) * 1024 + lane;
+#pragma unroll
+    for (int e = 0; e < 32; ++e) v[e] += b[32 * e];
+  }
+  char* stg = stage[warp];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    *(uint4*)(stg + lane * STG_LD + 16 * j) =
+        make_uint4(to_bf2(make_float2(v[8 * j], v[8 * j + 1])), to_bf2(make_float2(v[8 * j + 2], v[8 * j + 3])),
+                   to_bf2(make_float2(v[8 * j + 4], v[8 * j + 5])), to_bf2(make_float2(v[8 * j + 6], v[8 * j + 7])));
+  __syncwarp();
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int r = 8 * j + lane / 4, c = cb * 32 + 8 * (lane % 4);
+    if (rb * 32 + r < n && c < A.H)
+      *(uint4*)(A.dh + (long)A.row[rb * 32 + r] * A.H + c) = *(const uint4*)(stg + r * STG_LD + 16 * (lane % 4));
+  }
+}
+
+size_t al(size_t v) { return (v + 255) / 256 * 256; }
+
+// What a call's sizes come to, and where its arrays lie in the workspace
+struct Plan {
+  long Tp, piece;  // columns of a piece, a multiple of 256
+  int slots, slices;
+  size_t hc, label, weight, row, lse2, n, part, dl, blocks, bytes;
+};
+
+Plan plan_of(int T, int V, int H, bool dh, bool dw) {
+  Plan p = {};
+  p.Tp = ((long)T + 255) / 256 * 256;
+  const long nt = ((long)V + BN - 1) / BN;
+  p.slots = (V + BN / 2 - 1) / (BN / 2);  // halves of tiles that have a column
+  p.piece = std::min(nt * BN, std::max(1L, PIECE_BYTES / (2 * p.Tp * BN)) * BN);
+  // few tiles of dh: ranges of the vocabulary side by side, so that every pair of SMs has one
+  const long tiles = p.Tp / BM * (((long)H + BN - 1) / BN);
+  p.slices = (int)std::max(1L, std::min(std::min(16L, (long)(SMS / 2) / tiles), p.piece / 512));
+  size_t at = 0;
+  auto take = [&](size_t n) {
+    const size_t v = at;
+    at += al(n);
+    return v;
+  };
+  p.hc = take(2 * (size_t)p.Tp * H);
+  p.label = take(4 * p.Tp);
+  p.weight = take(4 * p.Tp);
+  p.row = take(4 * p.Tp);
+  p.lse2 = take(4 * p.Tp);
+  p.n = take(4);
+  p.part = take(8 * (size_t)p.slots * p.Tp);
+  if (dh || dw) p.dl = take(2 * (size_t)p.Tp * p.piece);
+  if (dh) p.blocks = take(4 * (size_t)p.slices * (p.Tp / 32) * ((H + 31) / 32) * 1024);
+  p.bytes = at;
+  return p;
+}
+
+lx_status check_sizes(int32_t T, int32_t V, int32_t H) {
+  if (T < 0) return fail(LX_ERR_ARG, "T < 0");
+  if (T > MAX_T) return fail(LX_ERR_SHAPE, "T is above 2^24");
+  if (V < 1 || V > MAX_V) return fail(LX_ERR_SHAPE, "V must be in 1..2^24");
+  if (H < 8 || H > MAX_H || H % 8 != 0) return fail(LX_ERR_SHAPE, "H must be a multiple of 8 up to 2^20");
+  const long tt = ((long)T + 255) / 256, vt = ((long)V + 255) / 256, ht = ((long)H + 255) / 256;
+  if (std::max(tt * vt, std::max(tt * ht * 16, vt * ht)) > (1L << 30)) return fail(LX_ERR_SHAPE, "too many tiles");
+  return LX_OK;
+}
+
+}  // namespace
+}  // namespace lx
+
+extern "C" lx_status lx_head_loss_workspace(int32_t T, int32_t V, int32_t H, int32_t want_dh, int32_t want_dw,
+                                            uint64_t* bytes) {
+  using namespace lx;
+  if (!bytes) return fail(LX_ERR_ARG, "bytes is NULL");
+  LX_TRY(check_sizes(T, V, H));
+  *bytes = T == 0 ? 0 : plan_of(T, V, H, want_dh != 0, want_dw != 0).bytes;
+  return LX_OK;
+}
+
+extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int64_t ldw, const int32_t* labels,
+                                  const float* row_weight, int32_t T, int32_t V, int32_t H, float* loss, void* dh,
+                                  void* dw, void* workspace, uint64_t workspace_bytes, void* stream) {
+  using namespace lx;
+  LX_TRY(check_sizes(T, V, H));
+  if (ldh < H || ldh % 8 != 0 || ldh > (1L << 30)) return fail(LX_ERR_SHAPE, "ldh");
+  if (ldw < H || ldw % 8 != 0 || ldw > (1L << 30)) return fail(LX_ERR_SHAPE, "ldw");
+  if (!w || !aligned(w, 16) || !aligned(h, 16) || !aligned(dh, 16) || !aligned(dw, 16))
+    return fail(LX_ERR_ARG, "w is NULL, or h, w, dh or dw not 16-byte aligned");
+  if (!aligned(labels, 4) || !aligned(row_weight, 4) || !aligned(loss, 4))
+    return fail(LX_ERR_ARG, "a pointer is not aligned to its element");
+  cudaStream_t st = (cudaStream_t)stream;
+  if (T == 0) {
+    if (dw) LX_CUDA(cudaMemsetAsync(dw, 0, 2 * (size_t)V * H, st));
+    return LX_OK;
+  }
+  if (!h || !labels || !loss) return fail(LX_ERR_ARG, "h, labels or loss is NULL");
+  const Plan L = plan_of(T, V, H, dh != nullptr, dw != nullptr);
+  if (!workspace || !aligned(workspace, 256)) return fail(LX_ERR_ARG, "workspace is NULL or not 256-byte aligned");
+  if (workspace_bytes < L.bytes) return fail(LX_ERR_ARG, "workspace too small");
+  const void* ins[] = {h, w, labels, row_weight};
+  const size_t in_n[] = {span(T, H, ldh, 2), span(V, H, ldw, 2), 4 * (size_t)T, 4 * (size_t)T};
+  const void* outs[] = {loss, dh, dw, workspace};
+  const size_t out_n[] = {4 * (size_t)T, 2 * (size_t)T * H, 2 * (size_t)V * H, L.bytes};
+  for (int i = 0; i < 4; ++i) {
+    for (int j = 0; j < 4; ++j)
+      if (overlap(outs[i], out_n[i], ins[j], in_n[j])) return fail(LX_ERR_ARG, "an output overlaps an input");
+    for (int j = 0; j < i; ++j)
+      if (overlap(outs[i], out_n[i], outs[j], out_n[j])) return fail(LX_ERR_ARG, "two outputs overlap");
+  }
+  const CallWaits waits = take_call_waits();
+  char* ws = (char*)workspace;
+  Head A = {};
+  A.T = T, A.V = V, A.H = H, A.Tp = (int)L.Tp;
+  A.h = (const __nv_bfloat16*)h;
+  A.ldh = ldh;
+  A.labels = labels;
+  A.row_weight = row_weight;
+  A.loss = loss;
+  A.dh = (__nv_bfloat16*)dh;
+  A.hc = (__nv_bfloat16*)(ws + L.hc);
+  A.label = (int*)(ws + L.label);
+  A.row = (int*)(ws + L.row);
+  A.n = (int*)(ws + L.n);
+  A.weight = (float*)(ws + L.weight);
+  A.lse2 = (float*)(ws + L.lse2);
+  A.w = (const __nv_bfloat16*)w;
+  A.ldw = ldw;
+  A.part = (const float2*)(ws + L.part);
+  A.slots = L.slots;
+  A.blocks = (const float*)(ws + L.blocks);
+  A.slices = L.slices;
+
+  k_head_rows<<<(unsigned)(L.Tp / ROWS), 256, 0, st>>>(A);
+  LX_CUDA(cudaGetLastError());
+
+  Launch P = {};
+  P.wait_cycles = waits.cycles;
+  P.unmet = waits.unmet == LX_WAIT_CALL_PRODUCT;
+  P.n = 1;
+  P.label = A.label;
+  P.weight = A.weight;
+  P.lse2 = A.lse2;
+  P.part = (float2*)(ws + L.part);
+  P.part_ld = L.Tp;
+  P.dl = (__nv_bfloat16*)(ws + L.dl);
+  P.ldd = L.piece;
+  Problem& p = P.p[0];
+  p.M = (int)L.Tp, p.N = V, p.K = H, p.slices = 1;
+  p.rows = A.n;
+  if (!operand(&p.a, A.hc, H, L.Tp, H, 2, false) || !operand(&p.b, w, H, V, ldw, 2, false))
+    return fail(LX_ERR_CUDA, "cuTensorMapEncodeTiled(head) failed");
+  LX_TRY((launch_product<STATS, false>(P, st)));
+  k_head_lse<<<(unsigned)(L.Tp / 32), 1024, 0, st>>>(A);
+  LX_CUDA(cudaGetLastError());
+  if (!dh && !dw) return LX_OK;
+
+  Launch G = {};
+  G.wait_cycles = waits.cycles;
+  for (long v0 = 0; v0 < V; v0 += L.piece) {
+    const long n = std::min<long>(L.piece, V - v0);
+    const __nv_bfloat16* wp = (const __nv_bfloat16*)w + v0 * ldw;
+    P.v0 = (int)v0;
+    p.N = (int)((n + 31) / 32 * 32);  // (whole blocks of dz; those behind the vocabulary are not read)
+    if (!operand(&p.b, wp, H, n, ldw, 2, false)) return fail(LX_ERR_CUDA, "cuTensorMapEncodeTiled(head) failed");
+    LX_TRY((launch_product<DLOGIT, false>(P, st)));
+    G.n = 0;
+    bool ok = true;
+    if (dh) {
+      Problem& g = G.p[G.n++];
+      g = Problem{};
+      g.M = (int)L.Tp, g.N = H, g.K = (int)n, g.slices = L.slices;
+      g.b_mn = 1;
+      g.rows = A.n;
+      g.blocks = (float*)(ws + L.blocks);
+      g.add = v0 > 0;
+      ok = ok && operand(&g.a, P.dl, n, L.Tp, L.piece, 2, false) && operand(&g.b, wp, H, n, ldw, 2, true);
+    }
+    if (dw) {
+      Problem& g = G.p[G.n++];
+      g = Problem{};
+      g.M = (int)n, g.N = H, g.K = (int)L.Tp, g.slices = 1;
+      g.a_mn = g.b_mn = 1;
+      g.depth = A.n;
+      g.out = (__nv_bfloat16*)dw + v0 * H, g.ldo = H, g.vec = 1;
+      ok = ok && operand(&g.a, P.dl, n, L.Tp, L.piece, 2, true) && operand(&g.b, A.hc, H, L.Tp, H, 2, true);
+    }
+    if (!ok) return fail(LX_ERR_CUDA, "cuTensorMapEncodeTiled(head) failed");
+    LX_TRY((launch_product<GRAD, false>(G, st)));
+  }
+  if (dh) {
+    k_head_dh<<<dim3((unsigned)(L.Tp / 32), (unsigned)(((H + 31) / 32 + 7) / 8)), 256, 0, st>>>(A);
+    LX_CUDA(cudaGetLastError());
+  }
+  return LX_OK;
+}

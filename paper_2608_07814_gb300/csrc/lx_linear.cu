@@ -1,0 +1,537 @@
+// A dense product with its epilogue, and its gradients (lx_linear, lx_linear_backward):
+//   z = x W^T (x_scale w_scale) + b,  y = act(z) + residual
+//   dz = dy act'(z),  dx = dz W,  dW = dz^T x,  db = sum_t dz
+// Many tokens are bound by the tensor cores and run as tiles of 256 x 256 (lx_product.cuh).
+// Few tokens are bound by reading W: k_linear_few holds 128 rows of W as the 128 rows of the
+// tensor core's tile and up to 256 tokens as its columns, and splits K over the CTAs of a
+// cluster, so that a product of few outputs still reads W with every SM; the CTAs' partial
+// sums meet in shared memory, in the cluster's order, and the epilogue follows in the same launch.
+#include "lx_product.cuh"
+
+namespace lx {
+namespace {
+
+using namespace rows;
+using namespace prod;
+
+// ---------------------------------------------------------------------------
+// few tokens
+// ---------------------------------------------------------------------------
+constexpr int FEW_THREADS = 256, FEW_SPLIT = 8, FEW_T = 256;
+
+struct Few {
+  CUtensorMap w, x;  // boxes of 128 bytes x 128 rows, and x tn rows
+  int T, N, nkb, per;  // blocks of K: all, a CTA's
+  int tn, stages, cols;  // tokens of a tile (a multiple of 16), TMEM columns
+  Launch e;          // the epilogue's part
+  int vec;           // four outputs at a time
+};
+
+template <bool F8>
+static __device__ __forceinline__ void mma_one(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t acc) {
+  if constexpr (F8)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(id), "r"(acc)
+        : "memory");
+  else
+    tc_mma(d, a, b, id, acc);
+}
+
+static __device__ __forceinline__ float4 ld_cluster(uint32_t addr, uint32_t rank) {
+  uint32_t at;
+  float4 v;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(at)
+               : "memory");
+  return v;
+}
+
+template <bool F8>
+__global__ void __launch_bounds__(FEW_THREADS, 2) k_linear_few(const __grid_constant__ Few P) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t bars[2 * 16 + 1];
+  __shared__ uint32_t tmem_s;
+  __shared__ int lost_s;
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  volatile int* lost = &lost_s;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t base = smem_u32(smem), full0 = smem_u32(bars), empty0 = full0 + 8 * 16, done = empty0 + 8 * 16;
+  const uint32_t stage = A_BYTES + P.tn * KB;
+  const int splits = gridDim.x, rank = blockIdx.x, n0 = blockIdx.y * 128, t0 = blockIdx.z * P.tn;
+  const int kb0 = rank * P.per, nkb = max(0, min(P.per, P.nkb - kb0));
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < P.stages; ++s) {
+      mbar_init(full0 + 8 * s, 1);
+      mbar_init(empty0 + 8 * s, 1);
+    }
+    mbar_init(done, 1);
+    *lost = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)),
+                 "r"(P.cols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_s;
+  uint32_t issued = 0;
+  if (warp == 0) {
+    if (lane == 0)
+      for (int i = 0; i < nkb; ++i) {
+        const uint32_t s = i % P.stages, bar = full0 + 8 * s, as = base + s * stage;
+        if (!mbar_wait(empty0 + 8 * s, ((i / P.stages) & 1) ^ 1, lost, P.e.wait_cycles)) {
+          *lost = 1;
+          break;
+        }
+        mbar_expect_tx(bar, stage);
+        tma_load_2d(as, &P.w, KB * (kb0 + i), n0, bar);
+        tma_load_2d(as + A_BYTES, &P.x, KB * (kb0 + i), t0, bar);
+        issued = i + 1;
+      }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t id = idesc(F8, 0, 0, 128, P.tn);
+      bool ok = !P.e.unmet || mbar_wait(done, 0, lost, P.e.wait_cycles);
+      for (int i = 0; ok && i < nkb; ++i) {
+        const uint32_t s = i % P.stages, as = base + s * stage, bs = as + A_BYTES;
+        if (!mbar_wait(full0 + 8 * s, (i / P.stages) & 1, lost, P.e.wait_cycles)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          mma_one<F8>(tmem, smem_desc(as + 32 * j), smem_desc(bs + 32 * j), id, (i | j) != 0 ? 1u : 0u);
+        tc_commit(empty0 + 8 * s);
+      }
+      if (!ok) *lost = 1;
+      tc_commit(done);  // also on the way out: no product is in flight when TMEM is freed
+    }
+    __syncwarp();
+  }
+  // every warp: the sums into shared memory (the stages are free: every product has been
+  // made), a token's 128 outputs a row; warp w reads TMEM lanes 32 (w % 4) ..
+  int ok = 1;
+  if (lane == 0) {
+    ok = mbar_wait(done, 0, nullptr, 2 * P.e.wait_cycles) ? 1 : 0;  // (the issuer may have waited for the bound)
+    if (!ok) *lost = 1;
+    else if (*lost) ok = 0;
+  }
+  ok = __shfl_sync(0xffffffffu, ok, 0);
+  tc_fence_after();
+  if (!ok && warp == 0 && lane == 0) {
+    // copies in flight land before the sums take their place
+    const uint32_t first = issued > (uint32_t)P.stages ? issued - P.stages : 0;
+    for (uint32_t j = first; j < issued; ++j)
+      mbar_wait(full0 + 8 * (j % P.stages), (j / P.stages) & 1, nullptr, P.e.wait_cycles);
+  }
+  __syncthreads();
+  float* part = reinterpret_cast<float*>(smem);
+  const int q = warp & 3, T = min(P.tn, P.T - t0);
+  for (int c = (warp >> 2) * 16; c < P.tn; c += 32) {
+    uint32_t r[16];
+    if (ok && nkb > 0) {
+      tc_ld16_async(tmem + ((uint32_t)(32 * q) << 16) + c, r);
+      tc_wait_ld();
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) r[e] = ok ? 0u : 0x7fc00000u;
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (c + e < T) part[(c + e) * 128 + 32 * q + lane] = __uint_as_float(r[e]);
+  }
+  tc_fence_before();
+  if (splits > 1) cluster_sync();
+  else __syncthreads();
+  const Launch& E = P.e;
+  for (int i = rank * FEW_THREADS + threadIdx.x; i < T * 32; i += splits * FEW_THREADS) {
+    const int t = i >> 5, c = 4 * (i & 31), col = n0 + c;
+    const uint32_t at = base + 4 * (uint32_t)(t * 128 + c);
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (splits > 1) {
+      float4 u[FEW_SPLIT];
+#pragma unroll
+      for (int s = 0; s < FEW_SPLIT; ++s)
+        if (s < splits) u[s] = ld_cluster(at, s);
+#pragma unroll
+      for (int s = 0; s < FEW_SPLIT; ++s)
+        if (s < splits) v[0] += u[s].x, v[1] += u[s].y, v[2] += u[s].z, v[3] += u[s].w;
+    } else {
+      const float4 u = *(const float4*)(part + t * 128 + c);
+      v[0] = u.x, v[1] = u.y, v[2] = u.z, v[3] = u.w;
+    }
+    const long row = t0 + t;
+    const float xs = F8 ? E.x_scale[row] : 1.f;
+    float z[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool on = col + e < P.N;
+      const float s = F8 && on ? xs * E.w_scale[col + e] : 1.f;
+      z[e] = fmaf(v[e], s, E.bias && on ? to_f32(E.bias[col + e]) : 0.f);
+      v[e] = act_of(E.act, z[e]);
+    }
+    if (P.vec && col + 3 < P.N) {
+      if (E.residual) {
+        const uint2 r = *(const uint2*)(E.residual + row * E.ldr + col);
+        const float2 a = bf2(r.x), b = bf2(r.y);
+        v[0] += a.x, v[1] += a.y, v[2] += b.x, v[3] += b.y;
+      }
+      if (E.pre)
+        *(uint2*)(E.pre + row * E.ldp + col) =
+            make_uint2(to_bf2(make_float2(z[0], z[1])), to_bf2(make_float2(z[2], z[3])));
+      *(uint2*)(E.y + row * E.ldy + col) = make_uint2(to_bf2(make_float2(v[0], v[1])), to_bf2(make_float2(v[2], v[3])));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (col + e < P.N) {
+          if (E.residual) v[e] += to_f32(E.residual[row * E.ldr + col + e]);
+          if (E.pre) E.pre[row * E.ldp + col + e] = __float2bfloat16_rn(z[e]);
+          E.y[row * E.ldy + col + e] = __float2bfloat16_rn(v[e]);
+        }
+    }
+  }
+  if (splits > 1) cluster_sync();  // a CTA's shared memory outlives its neighbours' reads
+  else __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(P.cols) : "memory");
+  }
+}
+
+template <bool F8>
+lx_status launch_few(Few& P, int tb, int es, const lx_linear_desc* d, cudaStream_t st) {
+  static bool cap[64] = {};
+  int dev = 0;
+  LX_CUDA(cudaGetDevice(&dev));
+  LX_CUDA(smem_cap_once((const void*)k_linear_few<F8>, 224 * 1024, dev, cap));
+  if (!encode_bytes_2d(&P.w, d->w, (long)d->K * es, d->N, d->ldw * es, 128) ||
+      !encode_bytes_2d(&P.x, d->x, (long)d->K * es, d->T, d->ldx * es, P.tn))
+    return fail(LX_ERR_CUDA, "cuTensorMapEncodeTiled(linear) failed");
+  const int stage = A_BYTES + P.tn * KB;
+  // Two CTAs an SM up to 128 tokens (100 KiB each; with 256 columns of TMEM at most, so that
+  // neither waits for the other's), one above.
+  const int budget = P.tn <= 128 ? 100 * 1024 : 192 * 1024, per_sm = P.tn <= 128 ? 2 : 1;
+  P.stages = std::min(16, budget / stage);
+  P.cols = 32;
+  while (P.cols < P.tn) P.cols *= 2;
+  const int nt = (d->N + 127) / 128;
+  int splits = 1;
+  while (splits < FEW_SPLIT && (long)nt * tb * splits * 2 <= (long)SMS * per_sm && P.nkb >= 8 * splits) splits *= 2;
+  P.per = (P.nkb + splits - 1) / splits;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(splits, nt, tb);
+  cfg.blockDim = dim3(FEW_THREADS);
+  cfg.dynamicSmemBytes = budget + 1024;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = splits;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  LX_CUDA(cudaLaunchKernelEx(&cfg, k_linear_few<F8>, P));
+  return LX_OK;
+}
+
+// ---------------------------------------------------------------------------
+// the gradient of z, and the sums of its columns
+// ---------------------------------------------------------------------------
+struct DzArgs {
+  int T, N, act, chunk;  // rows of a CTA
+  const __nv_bfloat16 *dy, *pre;
+  long lddy, ldp;
+  __nv_bfloat16* dz;     // or NULL
+  long ldz;
+  float* part;           // [CTAs of rows][N], or NULL
+};
+
+__device__ __forceinline__ float dact_of(int act, float z) {
+  if (act == RELU) return z > 0.f ? 1.f : 0.f;
+  if (act == SILU) {
+    const float s = __fdividef(1.f, 1.f + ex2(-LOG2E * z));
+    return s * (1.f + z * (1.f - s));
+  }
+  if (act == GELU)
+    return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * 0.3989422804014327f * ex2(-0.5f * LOG2E * z * z);
+  return 1.f;
+}
+
+// dz is rounded to bf16 as the tensor cores take it (2^-9 of each term of the gradients' fp32
+// sums); the bias's gradient sums it unrounded.  A warp reads rows of 32 VEC columns.
+template <int VEC>
+__global__ void __launch_bounds__(256) k_linear_dz(const __grid_constant__ DzArgs A) {
+  __shared__ float sums[8][32 * VEC];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int col = (blockIdx.x * 32 + lane) * VEC;
+  const long t0 = (long)blockIdx.y * A.chunk;
+  const int n = (int)min((long)A.chunk, A.T - t0);
+  float s[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) s[e] = 0.f;
+  if (col < A.N) {
+#pragma unroll 4
+    for (int r = warp; r < n; r += 8) {
+      const long t = t0 + r;
+      float d[VEC], z[VEC];
+      if constexpr (VEC == 8) {
+        const uint4 v = *(const uint4*)(A.dy + t * A.lddy + col);
+        const uint32_t a[4] = {v.x, v.y, v.z, v.w};
+        uint32_t b[4] = {0u, 0u, 0u, 0u};
+        if (A.act != NONE) {
+          const uint4 u = *(const uint4*)(A.pre + t * A.ldp + col);
+          b[0] = u.x, b[1] = u.y, b[2] = u.z, b[3] = u.w;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 f = bf2(a[e]), g = bf2(b[e]);
+          d[2 * e] = f.x, d[2 * e + 1] = f.y, z[2 * e] = g.x, z[2 * e + 1] = g.y;
+        }
+      } else {
+        d[0] = to_f32(A.dy[t * A.lddy + col]);
+        z[0] = A.act != NONE ? to_f32(A.pre[t * A.ldp + col]) : 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        d[e] *= dact_of(A.act, z[e]);
+        s[e] += d[e];
+      }
+      if (A.dz) store<__nv_bfloat16, VEC>(A.dz + t * A.ldz + col, d);
+    }
+  }
+  if (!A.part) return;
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) sums[warp][lane * VEC + e] = s[e];
+  __syncthreads();
+  for (int c = threadIdx.x; c < 32 * VEC; c += 256) {
+    const int at = blockIdx.x * 32 * VEC + c;
+    if (at >= A.N) break;
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) v += sums[w][c];
+    A.part[(long)blockIdx.y * A.N + at] = v;
+  }
+}
+
+// the CTAs' sums in their order: 8 ranges of them side by side, then those
+__global__ void __launch_bounds__(256) k_linear_db(const float* part, int chunks, int N, __nv_bfloat16* db) {
+  __shared__ float sums[8][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+  const int per = (chunks + 7) / 8;
+  float v = 0.f;
+  if (c < N)
+#pragma unroll 8
+    for (int i = warp * per; i < min(chunks, (warp + 1) * per); ++i) v += part[(long)i * N + c];
+  sums[warp][lane] = v;
+  __syncthreads();
+  if (warp == 0 && c < N) {
+    v = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) v += sums[w][lane];
+    db[c] = __float2bfloat16_rn(v);
+  }
+}
+
+// rows of a CTA of k_linear_dz: about four CTAs an SM; a multiple of the warps
+int dz_chunk(int T, int N) {
+  const long cols = (N + 255) / 256;
+  const long ctas = std::max(1L, 4L * SMS / cols);
+  return (int)std::max(8L, std::min<long>(1L << 20, (((long)T + ctas - 1) / ctas + 7) / 8 * 8));
+}
+int dz_chunks(int T, int N) { return (int)(((long)T + dz_chunk(T, N) - 1) / dz_chunk(T, N)); }
+size_t al(size_t v) { return (v + 255) / 256 * 256; }
+long dz_ld(int N) { return ((long)N + 7) / 8 * 8; }
+
+constexpr int MAX_T = 1 << 30, MAX_DIM = 1 << 24;
+
+lx_status check_sizes(int32_t T, int32_t N, int32_t K, int32_t dtype) {
+  if (T < 0) return fail(LX_ERR_ARG, "T < 0");
+  if (T > MAX_T) return fail(LX_ERR_SHAPE, "T is above 2^30");
+  if (N < 1 || N > MAX_DIM || K < 1 || K > MAX_DIM) return fail(LX_ERR_SHAPE, "N and K must be in 1..2^24");
+  if (K % (dtype == LX_E4M3 ? 16 : 8) != 0) return fail(LX_ERR_SHAPE, "K must be a multiple of 16 bytes");
+  // tiles of 256 x 256 are counted in 31 bits
+  const long mt = ((long)T + 255) / 256, nt = ((long)N + 255) / 256, kt = ((long)K + 255) / 256;
+  if (std::max(mt * nt, std::max(mt * kt, nt * kt)) > (1L << 30)) return fail(LX_ERR_SHAPE, "too many tiles");
+  return LX_OK;
+}
+
+lx_status check_desc(const lx_linear_desc* d) {
+  if (!d) return fail(LX_ERR_ARG, "desc is NULL");
+  if (d->dtype != LX_BF16 && d->dtype != LX_E4M3) return fail(LX_ERR_ARG, "dtype must be LX_BF16 or LX_E4M3");
+  if (d->act < LX_ACT_NONE || d->act > LX_ACT_GELU) return fail(LX_ERR_ARG, "unknown activation");
+  LX_TRY(check_sizes(d->T, d->N, d->K, d->dtype));
+  const int64_t per = d->dtype == LX_E4M3 ? 16 : 8;
+  if (d->ldw < d->K || d->ldw % per != 0 || d->ldw > MAX_DIM) return fail(LX_ERR_SHAPE, "ldw");
+  if (d->ldx < d->K || d->ldx % per != 0 || d->ldx > MAX_DIM) return fail(LX_ERR_SHAPE, "ldx");
+  if (!d->w || !aligned(d->w, 16)) return fail(LX_ERR_ARG, "w is NULL or not 16-byte aligned");
+  if (d->T > 0 && (!d->x || !aligned(d->x, 16))) return fail(LX_ERR_ARG, "x is NULL or not 16-byte aligned");
+  return LX_OK;
+}
+
+}  // namespace
+}  // namespace lx
+
+extern "C" lx_status lx_linear(const lx_linear_desc* d, void* y, int64_t ldy, void* pre, void* stream) {
+  using namespace lx;
+  LX_TRY(check_desc(d));
+  const bool f8 = d->dtype == LX_E4M3;
+  const int es = f8 ? 1 : 2;
+  if (f8 != (d->x_scale != nullptr) || f8 != (d->w_scale != nullptr))
+    return fail(LX_ERR_ARG, "x_scale and w_scale go with LX_E4M3");
+  if (!aligned(d->x_scale, 4) || !aligned(d->w_scale, 4) || !aligned(d->bias, 2) || !aligned(d->residual, 2) ||
+      !aligned(y, 2) || !aligned(pre, 2))
+    return fail(LX_ERR_ARG, "a pointer is not aligned to its element");
+  if (d->T == 0) return LX_OK;
+  if (!y) return fail(LX_ERR_ARG, "y is NULL");
+  if (ldy < d->N || (d->residual && d->ldr < d->N)) return fail(LX_ERR_SHAPE, "rows are closer than N elements");
+  if (ldy > (1L << 30) || (d->residual && d->ldr > (1L << 30))) return fail(LX_ERR_SHAPE, "rows are above 2^30 elements apart");
+  const size_t sy = span(d->T, d->N, ldy, 2), sp = pre ? span(d->T, d->N, d->N, 2) : 0;
+  const size_t sx = span(d->T, d->K, d->ldx, es), sw = span(d->N, d->K, d->ldw, es);
+  const size_t sr = d->residual ? span(d->T, d->N, d->ldr, 2) : 0;
+  const bool in_place = y == d->residual && d->ldr == ldy;
+  const void* ins[] = {d->x, d->w, d->x_scale, d->w_scale, d->bias};
+  const size_t sizes[] = {sx, sw, 4 * (size_t)d->T, 4 * (size_t)d->N, 2 * (size_t)d->N};
+  for (int i = 0; i < 5; ++i)
+    if (overlap(y, sy, ins[i], sizes[i]) || overlap(pre, sp, ins[i], sizes[i]))
+      return fail(LX_ERR_ARG, "an output overlaps an input");
+  if ((!in_place && overlap(y, sy, d->residual, sr)) || overlap(pre, sp, d->residual, sr))
+    return fail(LX_ERR_ARG, "an output overlaps an input");
+  if (overlap(y, sy, pre, sp)) return fail(LX_ERR_ARG, "two outputs overlap");
+
+  const CallWaits waits = take_call_waits();
+  Launch P = {};
+  P.wait_cycles = waits.cycles;
+  P.unmet = waits.unmet == LX_WAIT_CALL_PRODUCT;
+  P.x_scale = d->x_scale;
+  P.w_scale = d->w_scale;
+  P.bias = (const __nv_bfloat16*)d->bias;
+  P.residual = (const __nv_bfloat16*)d->residual;
+  P.y = (__nv_bfloat16*)y;
+  P.pre = (__nv_bfloat16*)pre;
+  P.ldr = d->ldr;
+  P.ldy = ldy;
+  P.ldp = d->N;
+  P.act = d->act;
+  auto wide = [](const void* p, long ld, int b) { return !p || (((uintptr_t)p | (uintptr_t)(2 * ld)) % b) == 0; };
+  cudaStream_t st = (cudaStream_t)stream;
+  // Few tokens: tiles of 256 x 256 would leave more than half of the pairs of SMs without one
+  const long tiles = (((long)d->T + BM - 1) / BM) * (((long)d->N + BN - 1) / BN);
+  const int tb = (d->T + FEW_T - 1) / FEW_T;
+  if ((d->T <= 64 && d->N <= 65535 * 128) || tiles * 2 <= SMS / 2) {
+    Few F = {};
+    F.e = P;
+    F.T = d->T;
+    F.N = d->N;
+    F.nkb = (int)(((long)d->K * es + KB - 1) / KB);
+    F.tn = ((d->T + tb - 1) / tb + 15) / 16 * 16;
+    F.vec = wide(y, ldy, 8) && wide(pre, d->N, 8) && wide(d->residual, d->ldr, 8);
+    return f8 ? launch_few<true>(F, tb, es, d, st) : launch_few<false>(F, tb, es, d, st);
+  }
+  P.vec_y = wide(y, ldy, 16);
+  P.vec_p = wide(pre, d->N, 16);
+  P.vec_r = wide(d->residual, d->ldr, 16);
+  P.n = 1;
+  Problem& p = P.p[0];
+  p.M = d->T;
+  p.N = d->N;
+  p.K = d->K;
+  p.slices = 1;
+  if (!operand(&p.a, d->x, d->K, d->T, d->ldx, es, false) || !operand(&p.b, d->w, d->K, d->N, d->ldw, es, false))
+    return fail(LX_ERR_CUDA, "cuTensorMapEncodeTiled(linear) failed");
+  return f8 ? launch_product<LINEAR, true>(P, st) : launch_product<LINEAR, false>(P, st);
+}
+
+extern "C" lx_status lx_linear_workspace(int32_t T, int32_t N, int32_t K, uint64_t* bytes) {
+  using namespace lx;
+  if (!bytes) return fail(LX_ERR_ARG, "bytes is NULL");
+  LX_TRY(check_sizes(T, N, K, LX_BF16));
+  *bytes = T == 0 ? 0 : al(2 * (size_t)T * dz_ld(N)) + al(4 * (size_t)dz_chunks(T, N) * N);
+  return LX_OK;
+}
+
+extern "C" lx_status lx_linear_backward(const lx_linear_desc* d, const void* dy, int64_t lddy, const void* pre,
+                                        void* dx, void* dw, void* dbias, void* workspace, uint64_t workspace_bytes,
+                                        void* stream) {
+  using namespace lx;
+  LX_TRY(check_desc(d));
+  if (d->dtype != LX_BF16) return fail(LX_ERR_UNSUPPORTED, "the gradients are those of the bf16 product");
+  if (!aligned(dx, 16) || !aligned(dw, 16)) return fail(LX_ERR_ARG, "dx and dw must be 16-byte aligned");
+  if (!aligned(dy, 2) || !aligned(pre, 2) || !aligned(dbias, 2))
+    return fail(LX_ERR_ARG, "a pointer is not aligned to its element");
+  if (!dx && !dw && !dbias) return fail(LX_ERR_ARG, "no gradient is asked for");
+  const int T = d->T, N = d->N, K = d->K;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (T == 0) {
+    if (dw) LX_CUDA(cudaMemsetAsync(dw, 0, 2 * (size_t)N * K, st));
+    if (dbias) LX_CUDA(cudaMemsetAsync(dbias, 0, 2 * (size_t)N, st));
+    return LX_OK;
+  }
+  if (!dy) return fail(LX_ERR_ARG, "dy is NULL");
+  if ((d->act != LX_ACT_NONE) != (pre != nullptr)) return fail(LX_ERR_ARG, "pre goes with an activation");
+  if (lddy < N) return fail(LX_ERR_SHAPE, "rows are closer than N elements");
+  if (lddy > (1L << 30)) return fail(LX_ERR_SHAPE, "rows are above 2^30 elements apart");
+  uint64_t need = 0;
+  LX_TRY(lx_linear_workspace(T, N, K, &need));
+  if (!workspace || !aligned(workspace, 256)) return fail(LX_ERR_ARG, "workspace is NULL or not 256-byte aligned");
+  if (workspace_bytes < need) return fail(LX_ERR_ARG, "workspace too small");
+  const void* ins[] = {d->x, d->w, dy, pre};
+  const size_t in_n[] = {span(T, K, d->ldx, 2), span(N, K, d->ldw, 2), span(T, N, lddy, 2), pre ? 2 * (size_t)T * N : 0};
+  const void* outs[] = {dx, dw, dbias, workspace};
+  const size_t out_n[] = {2 * (size_t)T * K, 2 * (size_t)N * K, 2 * (size_t)N, need};
+  for (int i = 0; i < 4; ++i) {
+    for (int j = 0; j < 4; ++j)
+      if (overlap(outs[i], out_n[i], ins[j], in_n[j])) return fail(LX_ERR_ARG, "an output overlaps an input");
+    for (int j = 0; j < i; ++j)
+      if (overlap(outs[i], out_n[i], outs[j], out_n[j])) return fail(LX_ERR_ARG, "two outputs overlap");
+  }
+  const CallWaits waits = take_call_waits();
+  // dy itself is dz where nothing changes it and TMA can read it
+  const bool direct = d->act == LX_ACT_NONE && aligned(dy, 16) && lddy % 8 == 0 && lddy <= MAX_DIM;
+  __nv_bfloat16* dz = (__nv_bfloat16*)workspace;
+  float* part = (float*)((char*)workspace + al(2 * (size_t)T * dz_ld(N)));
+  const int chunk = dz_chunk(T, N), chunks = dz_chunks(T, N);
+  if (!direct || dbias) {
+    DzArgs A = {T, N, d->act, chunk, (const __nv_bfloat16*)dy, (const __nv_bfloat16*)pre, (long)lddy, (long)N,
+                direct ? nullptr : dz, dz_ld(N), dbias ? part : nullptr};
+    const bool vec = N % 8 == 0 && lddy % 8 == 0 && aligned(dy, 16) && aligned(pre, 16);
+    if (vec) k_linear_dz<8><<<dim3((N + 255) / 256, chunks), 256, 0, st>>>(A);
+    else k_linear_dz<1><<<dim3((N + 31) / 32, chunks), 256, 0, st>>>(A);
+    if (dbias) k_linear_db<<<(N + 31) / 32, 256, 0, st>>>(part, chunks, N, (__nv_bfloat16*)dbias);
+    LX_CUDA(cudaGetLastError());
+  }
+  if (!dx && !dw) return LX_OK;
+  const void* g = direct ? dy : dz;
+  const long ldg = direct ? lddy : dz_ld(N);
+  Launch P = {};
+  P.wait_cycles = waits.cycles;
+  P.unmet = waits.unmet == LX_WAIT_CALL_PRODUCT;
+  bool ok = true;
+  // the product with the longer sums first: the shorter tiles even out the SMs' ends
+  for (int i = 0; i < 2; ++i) {
+    if ((N >= T) == (i == 0)) {
+      if (!dx) continue;
+      Problem& p = P.p[P.n++];
+      p.M = T, p.N = K, p.K = N, p.slices = 1;
+      p.b_mn = 1;
+      p.out = dx, p.ldo = K, p.vec = 1;
+      ok = ok && operand(&p.a, g, N, T, ldg, 2, false) && operand(&p.b, d->w, K, N, d->ldw, 2, true);
+    } else {
+      if (!dw) continue;
+      Problem& p = P.p[P.n++];
+      p.M = N, p.N = K, p.K = T, p.slices = 1;
+      p.a_mn = p.b_mn = 1;
+      p.out = dw, p.ldo = K, p.vec = 1;
+      ok = ok && operand(&p.a, g, N, T, ldg, 2, true) && operand(&p.b, d->x, K, T, d->ldx, 2, true);
+    }
+  }
+  if (!ok) return fail(LX_ERR_CUDA, "cuTensorMapEncodeTiled(linear gradients) failed");
+  return launch_product<GRAD, false>(P, st);
+}

@@ -1,0 +1,576 @@
+// The large matrix products of lx_linear and lx_head_loss, sm_103a tcgen05:
+//   D [M][N] = sum_k A(m, k) B(n, k)      (bf16, or e4m3 where F8)
+// in tiles of 256 x 256 that a pair of CTAs holds together (cta_group::2, M = N = 256):
+// each CTA loads its 128 rows of A and half of B's 256, so an SM fetches 32 KiB for
+// 128 x 256 x 64 products where a CTA by itself fetches 48.  The two operands may be stored
+// along K (rows of D's row or column index, K contiguous) or along M / N (rows of K): the
+// gradients read the activations, the weights and the gradient of the product as they are,
+// without a transposed copy.
+//
+// One persistent pair an SM pair, 12 warps a CTA:
+//   warp 0       asks for the operands' tiles (TMA, 128-byte swizzle, STAGES deep); the bytes
+//                of both CTAs are counted by the even CTA's barrier;
+//   warp 1       of the even CTA issues tcgen05.mma and commits stages and accumulators to
+//                both CTAs; (of both) allocates 512 TMEM columns: two accumulators, so that
+//                a tile's epilogue runs beside the next tile's products;
+//   warps 4..11  epilogue: 32 rows x 32 columns at a time from TMEM, what the caller's MODE
+//                makes of them, through a warp's block of shared memory to whole row segments.
+// Tiles are dealt in an order that keeps 8 rows of tiles together, so that what runs at the
+// same time shares its operands in L2.  Every wait is bounded: when one gives up, the pair's
+// tiles from there on are NaN, copies and products in flight are waited for, and TMEM is freed.
+#pragma once
+
+#include <algorithm>
+
+#include "lx_rows.cuh"
+#include "lx_tcgen05.cuh"
+
+namespace lx {
+namespace prod {
+
+// A map of rows of `inner` bytes, ld bytes apart, in boxes of 128 bytes x box_rows rows
+bool encode_bytes_2d(CUtensorMap* m, const void* base, long inner, long rows, long ld, int box_rows);
+
+namespace {  // (each file that includes this has the kernels it launches)
+
+using namespace tcg;
+
+constexpr int BM = 256, BN = 256;      // a pair's tile
+constexpr int KB = 128;                // bytes of K a stage: 64 bf16 or 128 e4m3
+constexpr int A_BYTES = 128 * KB, STAGE = 2 * A_BYTES, STAGES = 6;
+constexpr int EPI = 8, THREADS = 128 + 32 * EPI;
+constexpr int STG_LD = 80;             // bytes of a staged row of 32 bf16: 16-byte pieces of 8 rows on distinct banks
+constexpr int STG = 32 * STG_LD, PRM = 64 * 4;
+constexpr int SMEM = STAGES * STAGE + EPI * (STG + PRM) + 8 * (2 * STAGES + 8) + 1024;
+constexpr int GROUP_M = 8;
+static_assert(SMEM <= 227 * 1024, "fits an SM");
+
+enum Mode { LINEAR = 0, STATS = 1, DLOGIT = 2, GRAD = 3 };
+enum Act { NONE = 0, RELU = 1, SILU = 2, GELU = 3 };
+
+// One product of a launch.  Its tiles: slices (ranges of K) x tiles of N x tiles of M.
+struct Problem {
+  CUtensorMap a, b;  // maps of bytes: 128 x 128 boxes of an operand along K, 128 x 64 of one along M / N
+  int a_mn, b_mn;    // stored along M / N
+  int M, N, K;       // K in elements
+  int slices;
+  const int* rows;   // device count that bounds M (NULL: M), and
+  const int* depth;  // one that bounds K
+  // GRAD: bf16 rows ldo apart, or (blocks) fp32 in blocks of 32 x 32, slice by slice
+  void* out;
+  long ldo;
+  int vec;           // 16-byte stores
+  float* blocks;
+  int add;           // to what the blocks hold
+};
+
+struct Launch {
+  Problem p[2];
+  int n;
+  unsigned long long wait_cycles;
+  int unmet;  // test hook: the issuer first waits for what nothing fulfils
+  // LINEAR
+  const float *x_scale, *w_scale;
+  const __nv_bfloat16 *bias, *residual;
+  __nv_bfloat16 *y, *pre;
+  long ldr, ldy;  // (pre: ldp)
+  long ldp;
+  int act, vec_r, vec_y, vec_p;
+  // DLOGIT: compact rows' labels, weights and log-sum-exps (in units of log 2)
+  const int* label;
+  const float *weight, *lse2;
+  __nv_bfloat16* dl;
+  long ldd;
+  int v0;            // the first column's place in the vocabulary
+  // STATS
+  float2* part;      // [halves of tiles of N][part_ld]: a row's largest logit there, sum of exp
+  long part_ld;
+};
+
+static __device__ __forceinline__ uint32_t mapa0(uint32_t addr) {  // the even CTA's
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+  return r;
+}
+static __device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+static __device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+static __device__ __forceinline__ bool try_wait_cluster(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+static __device__ __forceinline__ bool wait_cluster(uint32_t bar, uint32_t parity, volatile int* lost,
+                                                    unsigned long long limit) {
+  if (try_wait_cluster(bar, parity)) return true;
+  const unsigned long long t0 = clock64();
+  while (true) {
+    if (try_wait_cluster(bar, parity)) return true;
+    if (lost && *lost) return false;
+    if (clock64() - t0 > limit) return false;
+  }
+}
+static __device__ __forceinline__ void arrive_remote(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+static __device__ __forceinline__ void load_pair(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(bar)
+      : "memory");
+}
+static __device__ __forceinline__ void commit_pair(uint32_t bar, uint16_t mask) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+      "h"(mask)
+      : "memory");
+}
+template <bool F8>
+static __device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  if constexpr (F8)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc)
+        : "memory");
+}
+// Descriptor of an operand stored along M / N: chunks of 64 elements (128 bytes, swizzled) x
+// 64 rows of K, 8192 bytes apart (bits 16..29); 8 rows of K 1024 bytes apart (bits 32..45).
+static __device__ __forceinline__ uint64_t desc_mn(uint32_t addr) {
+  return (uint64_t)((addr >> 4) & 0x3FFF) | ((uint64_t)(8192 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
+         (1ull << 46) | (2ull << 61);
+}
+// Instruction descriptor: fp32 accumulator (bits 4..5), A and B bf16 (1 at bits 7, 10) or
+// e4m3 (0), stored along M (bit 15) / N (bit 16), N >> 3, M >> 4
+__host__ __device__ constexpr uint32_t idesc(bool f8, int a_mn, int b_mn, int M, int N) {
+  return (1u << 4) | (f8 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) |
+         ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+constexpr float LOG2E = 1.4426950408889634f;
+
+// act(z) and its derivative.  A NaN stays one; gelu by the error function.
+__device__ __forceinline__ float act_of(int act, float z) {
+  if (act == RELU) return z < 0.f ? 0.f : z;
+  if (act == SILU) return __fdividef(z, 1.f + rows::ex2(-LOG2E * z));
+  if (act == GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+  return z;
+}
+
+struct Tile {
+  int p, m0, n0, slice, kb0, nkb;
+};
+
+// Sizes of the launch's products, as the device counts bound them
+struct Sizes {
+  int M[2], mt[2], nt[2], kb[2], tiles[2];
+  template <bool F8>
+  __device__ void read(const Launch& P) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      tiles[i] = 0;
+      if (i >= P.n) continue;
+      const Problem& p = P.p[i];
+      M[i] = p.rows ? min(*p.rows, p.M) : p.M;
+      const int K = p.depth ? min(*p.depth, p.K) : p.K;
+      mt[i] = (M[i] + BM - 1) / BM;
+      nt[i] = (p.N + BN - 1) / BN;
+      kb[i] = F8 ? (K + 127) / 128 : (K + 63) / 64;
+      tiles[i] = mt[i] * nt[i] * p.slices;
+    }
+  }
+  __device__ bool at(const Launch& P, int i, Tile& t) const {
+    t.p = 0;
+    if (i >= tiles[0]) {
+      i -= tiles[0];
+      t.p = 1;
+      if (i >= tiles[1]) return false;
+    }
+    const int m_n = t.p ? mt[1] : mt[0], n_n = t.p ? nt[1] : nt[0], kbs = t.p ? kb[1] : kb[0];
+    const int slices = P.p[t.p].slices;
+    t.slice = i / (m_n * n_n);
+    i -= t.slice * m_n * n_n;
+    const int g = i / (GROUP_M * n_n), gm = min(GROUP_M, m_n - g * GROUP_M);
+    i -= g * GROUP_M * n_n;
+    t.m0 = (g * GROUP_M + i % gm) * BM;
+    t.n0 = i / gm * BN;
+    const int per = (kbs + slices - 1) / slices;
+    t.kb0 = t.slice * per;
+    t.nkb = max(0, min(per, kbs - t.kb0));
+    return true;
+  }
+};
+
+// 32 x 32 bf16 of a warp, a row a lane, through its block of shared memory to rows of
+// memory: 16 bytes a lane where vec and the block lies inside, else single elements
+__device__ __forceinline__ void put_rows(char* stg, const uint32_t (&w)[16], __nv_bfloat16* out, long ldo, int row0,
+                                         int M, int col0, int N, bool vec) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    *(uint4*)(stg + lane * STG_LD + 16 * j) = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+  __syncwarp();
+  if (vec && col0 + 32 <= N) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = 8 * j + lane / 4, q = lane % 4;
+      if (row0 + r < M) *(uint4*)(out + (long)(row0 + r) * ldo + col0 + 8 * q) = *(const uint4*)(stg + r * STG_LD + 16 * q);
+    }
+  } else if (col0 + lane < N) {
+    const int n = min(32, M - row0);
+    for (int r = 0; r < n; ++r)
+      out[(long)(row0 + r) * ldo + col0 + lane] = *(const __nv_bfloat16*)(stg + r * STG_LD + 2 * lane);
+  }
+}
+// the other way: a lane's row of 32 elements (unset outside the matrix)
+__device__ __forceinline__ void get_rows(char* stg, uint32_t (&w)[16], const __nv_bfloat16* in, long ld, int row0, int M,
+                                         int col0, int N, bool vec) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();
+  if (vec && col0 + 32 <= N) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = 8 * j + lane / 4, q = lane % 4;
+      if (row0 + r < M) *(uint4*)(stg + r * STG_LD + 16 * q) = *(const uint4*)(in + (long)(row0 + r) * ld + col0 + 8 * q);
+    }
+  } else if (col0 + lane < N) {
+    const int n = min(32, M - row0);
+    for (int r = 0; r < n; ++r)
+      *(__nv_bfloat16*)(stg + r * STG_LD + 2 * lane) = in[(long)(row0 + r) * ld + col0 + lane];
+  }
+  __syncwarp();
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint4 v = *(const uint4*)(stg + lane * STG_LD + 16 * j);
+    w[4 * j] = v.x, w[4 * j + 1] = v.y, w[4 * j + 2] = v.z, w[4 * j + 3] = v.w;
+  }
+}
+
+template <int MODE, bool F8>
+__global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ Launch P) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  char* staged = reinterpret_cast<char*>(smem + STAGES * STAGE);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(staged + EPI * (STG + PRM));
+  const uint32_t base = smem_u32(smem), full0 = smem_u32(bars), empty0 = full0 + 8 * STAGES;
+  const uint32_t tfull0 = empty0 + 8 * STAGES, tempty0 = tfull0 + 16, drain = tempty0 + 16;
+  volatile int* lost = reinterpret_cast<volatile int*>(bars + 2 * STAGES + 5);
+  uint32_t* tmem_s = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 6);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(full0 + 8 * s, 1);   // the even CTA's: its producer, and both CTAs' bytes
+      mbar_init(empty0 + 8 * s, 1);  // a commit
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(tfull0 + 8 * b, 1);             // a commit
+      mbar_init(tempty0 + 8 * b, 2 * EPI);      // the even CTA's: both CTAs' epilogue warps
+    }
+    mbar_init(drain, 1);
+    *lost = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_s)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  Sizes S;
+  S.read<F8>(P);
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();  // both CTAs' barriers are there
+  tc_fence_after();
+  const uint32_t tmem = *tmem_s;
+
+  Tile t;
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t it = 0;
+      bool ok = true;
+      for (int i = pair; ok && S.at(P, i, t); i += pairs) {
+        const Problem& p = P.p[t.p];
+        const int m = t.m0 + 128 * (int)rank, n = t.n0 + 128 * (int)rank;
+        for (int k = 0; k < t.nkb; ++k, ++it) {
+          const uint32_t s = it % STAGES;
+          if (!wait_cluster(empty0 + 8 * s, ((it / STAGES) & 1) ^ 1, lost, P.wait_cycles)) {
+            ok = false;
+            break;
+          }
+          if (rank == 0) mbar_expect_tx(full0 + 8 * s, 2 * STAGE);
+          const uint32_t bar = mapa0(full0 + 8 * s), as = base + s * STAGE, bs = as + A_BYTES;
+          const int kb = t.kb0 + k;
+          if (p.a_mn) {
+            load_pair(as, &p.a, 2 * m, 64 * kb, bar);
+            load_pair(as + 8192, &p.a, 2 * m + 128, 64 * kb, bar);
+          } else {
+            load_pair(as, &p.a, KB * kb, m, bar);
+          }
+          if (p.b_mn) {
+            load_pair(bs, &p.b, 2 * n, 64 * kb, bar);
+            load_pair(bs + 8192, &p.b, 2 * n + 128, 64 * kb, bar);
+          } else {
+            load_pair(bs, &p.b, KB * kb, n, bar);
+          }
+        }
+      }
+      // the commits of the last stages have arrived before the CTA may end
+      for (uint32_t j = it > STAGES ? it - STAGES : 0; ok && j < it; ++j)
+        ok = wait_cluster(empty0 + 8 * (j % STAGES), (j / STAGES) & 1, lost, P.wait_cycles);
+      if (!ok) {
+        *lost = 1;
+        // copies in flight land before shared memory goes away (both CTAs': the even one's
+        // barriers count them)
+        if (rank == 0)
+          for (uint32_t j = it > STAGES ? it - STAGES : 0; j < it; ++j)
+            wait_cluster(full0 + 8 * (j % STAGES), (j / STAGES) & 1, nullptr, P.wait_cycles);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      uint32_t it = 0, nt = 0;
+      bool ok = !P.unmet || wait_cluster(drain, 0, lost, P.wait_cycles);
+      for (int i = pair; ok && S.at(P, i, t); i += pairs) {
+        if (t.nkb == 0) continue;
+        const Problem& p = P.p[t.p];
+        const uint32_t id = idesc(F8, p.a_mn, p.b_mn, BM, BN), acc = nt & 1, d = tmem + acc * BN;
+        ok = wait_cluster(tempty0 + 8 * acc, ((nt >> 1) & 1) ^ 1, lost, P.wait_cycles);
+        if (!ok) break;
+        tc_fence_after();
+        for (int k = 0; k < t.nkb; ++k, ++it) {
+          const uint32_t s = it % STAGES;
+          if (!wait_cluster(full0 + 8 * s, (it / STAGES) & 1, lost, P.wait_cycles)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t as = base + s * STAGE, bs = as + A_BYTES;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint64_t da = p.a_mn ? desc_mn(as + 2048 * j) : smem_desc(as + 32 * j);
+            const uint64_t db = p.b_mn ? desc_mn(bs + 2048 * j) : smem_desc(bs + 32 * j);
+            mma_pair<F8>(d, da, db, id, (k | j) != 0 ? 1u : 0u);
+          }
+          commit_pair(empty0 + 8 * s, 3);
+        }
+        if (!ok) break;
+        commit_pair(tfull0 + 8 * acc, 3);
+        ++nt;
+      }
+      if (!ok) {
+        *lost = 1;
+        commit_pair(drain, 1);  // no product is in flight when TMEM is freed
+        wait_cluster(drain, 0, nullptr, P.wait_cycles);
+      }
+    }
+  } else if (warp >= 4) {
+    const int q = warp & 3, half = (warp - 4) >> 2;
+    char* stg = staged + (warp - 4) * (STG + PRM);
+    float* prm = reinterpret_cast<float*>(stg + STG);
+    const float nan = __int_as_float(0x7fc00000);
+    uint32_t nt = 0;
+    int ok = 1;
+    for (int i = pair; S.at(P, i, t); i += pairs) {
+      const Problem& p = P.p[t.p];
+      const int M = t.p ? S.M[1] : S.M[0];
+      const uint32_t acc = nt & 1;
+      if (t.nkb > 0) {
+        if (ok && lane == 0) {
+          ok = wait_cluster(tfull0 + 8 * acc, (nt >> 1) & 1, lost, P.wait_cycles) ? 1 : 0;
+          if (!ok) *lost = 1;
+        }
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+        tc_fence_after();
+        ++nt;
+      }
+      const int row0 = t.m0 + 128 * (int)rank + 32 * q, row = row0 + lane;
+      float best = -INFINITY, total = 0.f;  // STATS
+      int label = -1;
+      float weight = 0.f, lse2 = 0.f, xs = 1.f;
+      if (MODE == DLOGIT && row < M) label = P.label[row] - P.v0, weight = P.weight[row], lse2 = P.lse2[row];
+      if (MODE == LINEAR && F8) xs = row < M ? P.x_scale[row] : 0.f;
+#pragma unroll 1
+      for (int c = 0; c < 4; ++c) {
+        const int col0 = t.n0 + 128 * half + 32 * c;
+        uint32_t r[32];
+        __syncwarp();
+        if (t.nkb > 0 && ok) {
+          tc_ld32_async(tmem + ((uint32_t)(32 * q) << 16) + acc * BN + 128 * half + 32 * c, r);
+          tc_wait_ld();
+          if (c == 3) {  // the accumulator is read: the next tile but one may take its place
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_remote(mapa0(tempty0 + 8 * acc));
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) r[e] = ok ? 0u : __float_as_uint(nan);
+        }
+        if (col0 >= p.N || row0 >= M) {
+          if (!(MODE == DLOGIT && row0 < p.M && col0 < p.N)) continue;
+        }
+        if constexpr (MODE == STATS) {
+          const int n = min(32, p.N - col0);
+          if (n < 32)
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (e >= n) r[e] = 0xff800000u;  // -inf
+          float m = best;
+#pragma unroll
+          for (int e = 0; e < 32; ++e) m = fmaxf(m, __uint_as_float(r[e]));
+          const float at = m == -INFINITY ? 0.f : m * LOG2E;  // (a row of -inf so far)
+          float s0 = total * rows::ex2(best == -INFINITY ? -INFINITY : fmaf(best, LOG2E, -at)), s1 = 0.f;
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            s0 += rows::ex2(fmaf(__uint_as_float(r[e]), LOG2E, -at));
+            s1 += rows::ex2(fmaf(__uint_as_float(r[e + 1]), LOG2E, -at));
+          }
+          total = s0 + s1;
+          best = m;
+        } else if constexpr (MODE == DLOGIT) {
+          // rounded to bf16 as the tensor cores take it: 2^-9 of each term of the gradients' fp32 sums
+          uint32_t w[16];
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            float2 d;
+            d.x = weight * (rows::ex2(fmaf(__uint_as_float(r[e]), LOG2E, -lse2)) - (label - col0 == e ? 1.f : 0.f));
+            d.y = weight * (rows::ex2(fmaf(__uint_as_float(r[e + 1]), LOG2E, -lse2)) - (label - col0 == e + 1 ? 1.f : 0.f));
+            if (row >= M) d = make_float2(0.f, 0.f);
+            w[e / 2] = rows::to_bf2(d);
+          }
+          put_rows(stg, w, P.dl, P.ldd, row0, p.M, col0, p.N, true);
+        } else if constexpr (MODE == GRAD) {
+          if (p.blocks) {
+            float* o = p.blocks + (((long)t.slice * ((p.M + 31) / 32) + row0 / 32) * ((p.N + 31) / 32) + col0 / 32) * 1024 + lane;
+            if (p.add) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(o[32 * e] + __uint_as_float(r[e]));
+            }
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[32 * e] = __uint_as_float(r[e]);
+          } else {
+            uint32_t w[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              w[e] = rows::to_bf2(make_float2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])));
+            put_rows(stg, w, (__nv_bfloat16*)p.out, p.ldo, row0, M, col0, p.N, p.vec);
+          }
+        } else {
+          // the columns' bias and scale, read by their lane and handed to all
+          const int col = col0 + lane;
+          __syncwarp();
+          prm[lane] = P.bias && col < p.N ? to_f32(P.bias[col]) : 0.f;
+          if (F8) prm[32 + lane] = col < p.N ? P.w_scale[col] : 0.f;
+          __syncwarp();
+          uint32_t w[16];
+          if (F8 || P.bias) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              const float4 b = *(const float4*)(prm + e);
+              float4 s = make_float4(1.f, 1.f, 1.f, 1.f);
+              if (F8) {
+                s = *(const float4*)(prm + 32 + e);
+                s.x *= xs, s.y *= xs, s.z *= xs, s.w *= xs;
+              }
+              r[e] = __float_as_uint(fmaf(__uint_as_float(r[e]), s.x, b.x));
+              r[e + 1] = __float_as_uint(fmaf(__uint_as_float(r[e + 1]), s.y, b.y));
+              r[e + 2] = __float_as_uint(fmaf(__uint_as_float(r[e + 2]), s.z, b.z));
+              r[e + 3] = __float_as_uint(fmaf(__uint_as_float(r[e + 3]), s.w, b.w));
+            }
+          }
+          if (P.pre) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              w[e] = rows::to_bf2(make_float2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])));
+            put_rows(stg, w, P.pre, P.ldp, row0, M, col0, p.N, P.vec_p);
+          }
+          if (P.act != NONE) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(act_of(P.act, __uint_as_float(r[e])));
+          }
+          if (P.residual) {
+            get_rows(stg, w, P.residual, P.ldr, row0, M, col0, p.N, P.vec_r);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float2 f = rows::bf2(w[e]);
+              r[2 * e] = __float_as_uint(__uint_as_float(r[2 * e]) + f.x);
+              r[2 * e + 1] = __float_as_uint(__uint_as_float(r[2 * e + 1]) + f.y);
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            w[e] = rows::to_bf2(make_float2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])));
+          put_rows(stg, w, P.y, P.ldy, row0, M, col0, p.N, P.vec_y);
+        }
+      }
+      if (MODE == STATS && row < M && t.n0 + 128 * half < p.N)
+        P.part[(long)(t.n0 / 128 + half) * P.part_ld + row] = make_float2(ok ? best : nan, total);
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+// Operand along K: rows x K elements of es bytes, ld elements apart; along M / N: K rows
+inline bool operand(CUtensorMap* m, const void* base, long inner, long outer, long ld, int es, bool mn) {
+  return encode_bytes_2d(m, base, inner * es, outer, ld * es, mn ? 64 : 128);
+}
+
+inline long tiles_of(const Problem& p) {
+  return (long)((p.M + BM - 1) / BM) * ((p.N + BN - 1) / BN) * p.slices;
+}
+
+template <int MODE, bool F8>
+lx_status launch_product(const Launch& P, cudaStream_t st) {
+  static bool cap[64] = {};
+  int dev = 0;
+  LX_CUDA(cudaGetDevice(&dev));
+  LX_CUDA(smem_cap_once((const void*)k_product<MODE, F8>, SMEM, dev, cap));
+  long tiles = 0;
+  for (int i = 0; i < P.n; ++i) tiles += tiles_of(P.p[i]);
+  if (tiles == 0) return LX_OK;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(2 * std::min<long>(tiles, rows::SMS / 2)));
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = SMEM;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  LX_CUDA(cudaLaunchKernelEx(&cfg, k_product<MODE, F8>, P));
+  return LX_OK;
+}
+
+}  // namespace
+}  // namespace prod
+}  // namespace lx

@@ -56,6 +56,8 @@ struct NormArgs {
   float a, off, eps;
   void *r_out, *h_out;
   float* stats;  // [2][T]: s1, s2
+  void* q_out;   // Q8: e4m3 [T][H],
+  float* scale;  // and [T]
   // backward
   void *dr, *dy, *dgate;
   int sums;     // bits of the column sums wanted: of s1 D y, of dh x
@@ -63,6 +65,16 @@ struct NormArgs {
 };
 
 constexpr int REGS = 128;  // a thread: the launch bounds hold the compiler to these
+
+constexpr float E4M3_MAX = 448.f, TINY = 1.17549435e-38f;
+
+// four values in e4m3, to the nearest, what is above 448 as 448
+__device__ __forceinline__ uint32_t to_e4m3(float2 a, float2 b) {
+  uint16_t lo, hi;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %2, %1;" : "=h"(lo) : "f"(a.x), "f"(a.y));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %2, %1;" : "=h"(hi) : "f"(b.x), "f"(b.y));
+  return (uint32_t)lo | ((uint32_t)hi << 16);
+}
 
 // bytes of the slots of one array's columns of a group: `members` threads' and a block more
 __host__ __device__ constexpr int group_bytes(int members, int es) { return members * EPT * es + 16; }
@@ -287,6 +299,22 @@ struct Rows {
         }
       }
   }
+  // the row in 8 bits, a piece at a time
+  __device__ void write_q8(unsigned t, const float2* v) const {
+    if (GRP == WARP && t >= (unsigned)A.T) return;
+    uint8_t* g = (uint8_t*)A.q_out + (uint64_t)t * (unsigned)A.H;
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+      if (c < count) {
+        uint8_t* p = g + col(c);
+        if constexpr (VEC == 8)
+          *(uint2*)p = make_uint2(to_e4m3(v[4 * c], v[4 * c + 1]), to_e4m3(v[4 * c + 2], v[4 * c + 3]));
+        else if constexpr (VEC == 4)
+          *(uint32_t*)p = to_e4m3(v[2 * c], v[2 * c + 1]);
+        else
+          *p = (uint8_t)(to_e4m3(v[c / 2], v[c / 2]) >> (c & 1 ? 8 : 0));
+      }
+  }
   // element j of piece c in a thread's pairs
   static __device__ float& elem(float2* v, int c, int j) {
     float2& p = v[(c * VEC + j) / 2];
@@ -298,6 +326,33 @@ struct Rows {
     for (int c = 0; c < NCH; ++c)
 #pragma unroll
       for (int j = 0; j < VEC; ++j) elem(v, c, j) = p && c < count ? add + p[col(c) + j] : rest;
+  }
+  // largest of the threads' values (bits of what has no sign: a NaN is above infinity), in
+  // the same memory
+  __device__ uint32_t most(uint32_t v, float (*buf)[1][COLS][MAX_W], int& turn) const {
+    if constexpr (GRP == WARP) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1)
+        if (o < size) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
+      return v;
+    }
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
+    uint32_t(*b)[MAX_W] = (uint32_t(*)[MAX_W])buf[turn][0];
+    turn ^= 1;
+    v = __reduce_max_sync(0xffffffffu, v);
+    int cols = 1;
+    if constexpr (GRP == CTA) {
+      if (lane == 0) b[0][warp] = v;
+      __syncthreads();
+    } else {
+      cooperative_groups::cluster_group cl = cooperative_groups::this_cluster();
+      cols = cl.num_blocks();
+      if (lane < cols) *cl.map_shared_rank(&b[cl.block_rank()][warp], lane) = v;
+      cl.sync();
+    }
+    for (int c = 0; c < cols; ++c)
+      for (int w = 0; w < nw; ++w) v = max(v, b[c][w]);
+    return v;
   }
   // sums of N (1 or 3) values over the row's threads, the same in each of them; buf is
   // used in turn: a half is written again only after the barrier that follows its last
@@ -363,7 +418,10 @@ __device__ __forceinline__ void clear(float (*buf)[N][C][W]) {
 
 extern __shared__ uint4 norm_ring[];
 
-template <typename T, int VEC, int GRP>
+// Q8: h in e4m3 with a scale for each token, its largest magnitude over e4m3's (so that no
+// value is cut off), and not below the smallest normal fp32 (a row of zeros).  The row is in
+// registers, so the second sweep over it costs a reduction more and no bytes.
+template <typename T, int VEC, int GRP, bool Q8>
 __global__ void __launch_bounds__(max_threads(GRP), 65536 / REGS / max_threads(GRP))
 k_resnorm_fwd(const __grid_constant__ NormArgs A) {
   __shared__ __align__(16) float buf[2][1][max_cols(GRP)][max_threads(GRP) / 32];
@@ -426,7 +484,20 @@ k_resnorm_fwd(const __grid_constant__ NormArgs A) {
       s2 = rsqrtf(q[0] * inv + A.eps);
 #pragma unroll
       for (int i = 0; i < N2; ++i) x[i] = muls(muls(x[i], both(s2)), w2[i]);
-      R.write(A.h_out, t, x);
+      if (!Q8 || A.h_out) R.write(A.h_out, t, x);
+      if constexpr (Q8) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < N2; ++i)
+          m = max(m, max(__float_as_uint(x[i].x) & 0x7fffffffu, __float_as_uint(x[i].y) & 0x7fffffffu));
+        const float top = __uint_as_float(R.most(m, buf, turn));
+        const float scale = top < E4M3_MAX * TINY ? TINY : top / E4M3_MAX;  // (a NaN stays one)
+        const float2 by = both(1.f / scale);
+#pragma unroll
+        for (int i = 0; i < N2; ++i) x[i] = muls(x[i], by);
+        R.write_q8(t, x);
+        if (R.writer() && t < (unsigned)A.T) A.scale[t] = scale;
+      }
     }
     if (A.stats && R.writer() && t < (unsigned)A.T) {
       A.stats[t] = s1;
@@ -706,9 +777,12 @@ lx_status launch(void (*kern)(KArgs...), const Shape& s, int groups, size_t smem
   return LX_OK;
 }
 
-template <typename T, int VEC, int GRP, bool BWD>
+enum Kind { FWD = 0, FWD_Q8 = 1, BACKWARD = 2 };
+
+template <typename T, int VEC, int GRP, int KIND>
 lx_status launch_one(const Shape& s, NormArgs& A, cudaStream_t st, int& groups) {
   static bool cap[64] = {};
+  constexpr bool BWD = KIND == BACKWARD;
   const size_t par = BWD ? sizeof(float) * 2 * EPT * s.threads : 0;
   size_t smem = 0;
   A.stages = 2;
@@ -723,26 +797,26 @@ lx_status launch_one(const Shape& s, NormArgs& A, cudaStream_t st, int& groups) 
   // 4000 of 2560: 44.8, 33.6, 34.4; 1031 of 2047: 31.7, 27.2, 27.6).
   using R = Rows<T, VEC, GRP>;
   if (BWD && GRP == CTA && R::RING) groups = std::min(groups, std::max(R::BLOCK ? 2 * SMS : SMS, A.T / 7));
-  if (BWD) return launch(k_resnorm_bwd<T, VEC, GRP>, s, groups, smem, A, st, cap);
-  return launch(k_resnorm_fwd<T, VEC, GRP>, s, groups, smem, A, st, cap);
+  if constexpr (BWD) return launch(k_resnorm_bwd<T, VEC, GRP>, s, groups, smem, A, st, cap);
+  else return launch(k_resnorm_fwd<T, VEC, GRP, KIND == FWD_Q8>, s, groups, smem, A, st, cap);
 }
 
-template <typename T, int VEC, bool BWD>
+template <typename T, int VEC, int KIND>
 lx_status launch_vec(const Shape& s, NormArgs& A, cudaStream_t st, int& groups) {
-  if (s.grp == WARP) return launch_one<T, VEC, WARP, BWD>(s, A, st, groups);
-  if (s.grp == CTA) return launch_one<T, VEC, CTA, BWD>(s, A, st, groups);
-  if (s.grp == CLUSTER) return launch_one<T, VEC, CLUSTER, BWD>(s, A, st, groups);
-  return launch_one<T, VEC, WIDE, BWD>(s, A, st, groups);
+  if (s.grp == WARP) return launch_one<T, VEC, WARP, KIND>(s, A, st, groups);
+  if (s.grp == CTA) return launch_one<T, VEC, CTA, KIND>(s, A, st, groups);
+  if (s.grp == CLUSTER) return launch_one<T, VEC, CLUSTER, KIND>(s, A, st, groups);
+  return launch_one<T, VEC, WIDE, KIND>(s, A, st, groups);
 }
 
 // wide: every row starts on a 16-byte boundary and is a multiple of 16 bytes; groups: out,
 // the CTAs (clusters) launched
-template <bool BWD>
+template <int KIND>
 lx_status launch_any(int dtype, bool wide, const Shape& s, NormArgs& A, cudaStream_t st, int& groups) {
   if (dtype == LX_F32)
-    return wide ? launch_vec<float, 4, BWD>(s, A, st, groups) : launch_vec<float, 1, BWD>(s, A, st, groups);
-  return wide ? launch_vec<__nv_bfloat16, 8, BWD>(s, A, st, groups)
-              : launch_vec<__nv_bfloat16, 1, BWD>(s, A, st, groups);
+    return wide ? launch_vec<float, 4, KIND>(s, A, st, groups) : launch_vec<float, 1, KIND>(s, A, st, groups);
+  return wide ? launch_vec<__nv_bfloat16, 8, KIND>(s, A, st, groups)
+              : launch_vec<__nv_bfloat16, 1, KIND>(s, A, st, groups);
 }
 
 constexpr int64_t MAX_LD = (1 << 30) - 1;  // elements between rows: a distance in bytes fits 32 bits
@@ -810,13 +884,10 @@ bool rows16(const NormArgs& A, size_t es, std::initializer_list<const void*> out
 }  // namespace
 }  // namespace lx
 
-extern "C" lx_status lx_residual_norm(const lx_resnorm_desc* d, void* r_out, void* h_out, float* stats,
-                                      void* stream) {
-  using namespace lx;
-  LX_TRY(check_desc(d));
-  if (d->T == 0) return LX_OK;
-  if ((h_out != nullptr) != (d->w_pre != nullptr)) return fail(LX_ERR_ARG, "h_out goes with w_pre");
-  if (!r_out && !h_out) return fail(LX_ERR_ARG, "r_out and h_out are both NULL");
+namespace lx {
+namespace {
+// what the two forward calls check alike, with the outputs given and the arguments filled
+lx_status forward_args(const lx_resnorm_desc* d, void* r_out, void* h_out, float* stats, const Shape& s, NormArgs& A) {
   const size_t es = esize(d->dtype), out = (size_t)d->T * d->H * es;
   if (!aligned(r_out, es) || !aligned(h_out, es) || !aligned(stats, 4))
     return fail(LX_ERR_ARG, "a pointer is not aligned to its element");
@@ -829,13 +900,60 @@ extern "C" lx_status lx_residual_norm(const lx_resnorm_desc* d, void* r_out, voi
       overlap(h_out, out, d->r, sr) || overlap(h_out, out, d->y, sy) || overlap(h_out, out, d->gate, sg) ||
       overlap(r_out, out, h_out, out))
     return fail(LX_ERR_ARG, "an output overlaps an input");
-  const Shape s = shape_of(d->T, d->H);
-  NormArgs A = args_of(d, s);
+  A = args_of(d, s);
   A.r_out = r_out;
   A.h_out = h_out;
   A.stats = stats;
+  return LX_OK;
+}
+}  // namespace
+}  // namespace lx
+
+extern "C" lx_status lx_residual_norm(const lx_resnorm_desc* d, void* r_out, void* h_out, float* stats,
+                                      void* stream) {
+  using namespace lx;
+  LX_TRY(check_desc(d));
+  if (d->T == 0) return LX_OK;
+  if ((h_out != nullptr) != (d->w_pre != nullptr)) return fail(LX_ERR_ARG, "h_out goes with w_pre");
+  if (!r_out && !h_out) return fail(LX_ERR_ARG, "r_out and h_out are both NULL");
+  const Shape s = shape_of(d->T, d->H);
+  NormArgs A;
+  LX_TRY(forward_args(d, r_out, h_out, stats, s, A));
   int groups;
-  return launch_any<false>(d->dtype, rows16(A, es, {r_out, h_out}), s, A, (cudaStream_t)stream, groups);
+  return launch_any<FWD>(d->dtype, rows16(A, esize(d->dtype), {r_out, h_out}), s, A, (cudaStream_t)stream, groups);
+}
+
+extern "C" lx_status lx_residual_norm_q8(const lx_resnorm_desc* d, void* r_out, void* q_out, float* scale, void* h_out,
+                                         float* stats, void* stream) {
+  using namespace lx;
+  LX_TRY(check_desc(d));
+  if (d->T == 0) return LX_OK;
+  if (!d->w_pre) return fail(LX_ERR_ARG, "w_pre is NULL");
+  if (!q_out || !scale) return fail(LX_ERR_ARG, "q_out or scale is NULL");
+  if (!aligned(scale, 4)) return fail(LX_ERR_ARG, "a pointer is not aligned to its element");
+  const Shape s = shape_of(d->T, d->H);
+  NormArgs A;
+  LX_TRY(forward_args(d, r_out, h_out, stats, s, A));
+  const size_t es = esize(d->dtype), out = (size_t)d->T * d->H, sc = 4 * (size_t)d->T;
+  const void* others[] = {d->r, d->y, d->gate, d->w_post, d->w_pre, r_out, h_out, stats};
+  const size_t sizes[] = {span(d->T, d->H, d->ldr, es),
+                          span(d->T, d->H, d->ldy, es),
+                          d->gate_kind == LX_GATE_FULL    ? span(d->T, d->H, d->ldg, es)
+                          : d->gate_kind == LX_GATE_TOKEN ? span(d->T, 1, d->ldg, 4)
+                                                          : 4 * (size_t)d->H,
+                          4 * (size_t)d->H,
+                          4 * (size_t)d->H,
+                          out * es,
+                          out * es,
+                          2 * sc};
+  for (int i = 0; i < 8; ++i)
+    if (overlap(q_out, out, others[i], sizes[i]) || overlap(scale, sc, others[i], sizes[i]))
+      return fail(LX_ERR_ARG, "q_out or scale overlaps another array");
+  if (overlap(q_out, out, scale, sc)) return fail(LX_ERR_ARG, "two outputs overlap");
+  A.q_out = q_out;
+  A.scale = scale;
+  int groups;
+  return launch_any<FWD_Q8>(d->dtype, rows16(A, es, {r_out, h_out, q_out}), s, A, (cudaStream_t)stream, groups);
 }
 
 extern "C" lx_status lx_residual_norm_workspace(int32_t T, int32_t H, uint64_t* bytes) {
@@ -903,7 +1021,7 @@ extern "C" lx_status lx_residual_norm_backward(const lx_resnorm_desc* d, const f
   A.part = params ? (float*)workspace : nullptr;
   A.sums = (dw_post || dgc ? 1 : 0) | (dw_pre ? 2 : 0);
   int groups;
-  LX_TRY(launch_any<true>(d->dtype, rows16(A, es, {outs[0], outs[1], outs[2]}), s, A, st, groups));
+  LX_TRY(launch_any<BACKWARD>(d->dtype, rows16(A, es, {outs[0], outs[1], outs[2]}), s, A, st, groups));
   if (params) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((d->H + 31) / 32, A.sums == 3 ? 2 : 1);

@@ -20,11 +20,12 @@ LX_OK, LX_ERR_ARG, LX_ERR_SHAPE, LX_ERR_CUDA, LX_ERR_OOM, LX_ERR_TIMEOUT, LX_ERR
     LX_ERR_UNSUPPORTED = range(8)
 STATUS_NAMES = ["LX_OK", "LX_ERR_ARG", "LX_ERR_SHAPE", "LX_ERR_CUDA", "LX_ERR_OOM",
                 "LX_ERR_TIMEOUT", "LX_ERR_STATE", "LX_ERR_UNSUPPORTED"]
-LX_F32, LX_BF16 = 0, 1
+LX_F32, LX_BF16, LX_E4M3 = 0, 1, 2
 LX_PATH_AUTO, LX_PATH_GENERIC = 0, 1
 LX_MAX_DEPTH, LX_MAX_K, LX_MAX_EXPERTS = 4, 32, 1024
 LX_MAX_WIDTH, LX_MAX_TEACHER = 65536, 1024
 LX_GATE_NONE, LX_GATE_CHANNEL, LX_GATE_TOKEN, LX_GATE_FULL = range(4)
+LX_ACT_NONE, LX_ACT_RELU, LX_ACT_SILU, LX_ACT_GELU = range(4)
 
 # every symbol include/lx.h declares
 EXPORTS = [
@@ -35,7 +36,8 @@ EXPORTS = [
     "lx_compress_workspace", "lx_compress_factor", "lx_set_wait_limit", "lx_inject_unmet_wait",
     "lx_clear_device_error", "lx_inject_unmet_wait_call", "lx_residual_norm",
     "lx_residual_norm_workspace", "lx_residual_norm_backward", "lx_router_balance_workspace",
-    "lx_router_balance", "lx_router_balance_backward", "lx_distill_loss",
+    "lx_router_balance", "lx_router_balance_backward", "lx_distill_loss", "lx_residual_norm_q8",
+    "lx_linear", "lx_linear_workspace", "lx_linear_backward", "lx_head_loss_workspace", "lx_head_loss",
 ]
 (LX_WAIT_NONE, LX_WAIT_STREAM_DEP, LX_WAIT_TC_MMA, LX_WAIT_ROUTER, LX_WAIT_CALL_PRODUCT,
  LX_WAIT_CALL_JACOBI, LX_WAIT_CALL_SUMS, LX_WAIT_CALL_ENTRIES, LX_WAIT_CALL_WRITTEN,
@@ -71,6 +73,12 @@ class ResnormDesc(ctypes.Structure):
         (n, ctypes.c_int64) for n in ("ldr", "ldy", "ldg")] + [
         (n, ctypes.c_void_p) for n in ("r", "y", "gate", "w_post", "w_pre")] + [
         (n, ctypes.c_float) for n in ("res_scale", "weight_offset", "eps")]
+
+
+class LinearDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "T", "N", "K", "act")] + [
+        (n, ctypes.c_int64) for n in ("ldx", "ldw", "ldr")] + [
+        (n, ctypes.c_void_p) for n in ("x", "w", "x_scale", "w_scale", "bias", "residual")]
 
 
 class KernelTime(ctypes.Structure):
@@ -127,6 +135,12 @@ def lib() -> ctypes.CDLL:
             "lx_router_balance_backward": [i32, vp, i64, vp, vp, vp, i32, i32, i32, f32, f32, vp, vp],
             "lx_distill_loss": [i32, vp, i64, vp, vp, vp, vp, vp, i32, i32, i32, f32, f32, f32, vp,
                                 vp, i64, vp],
+            "lx_residual_norm_q8": [ctypes.POINTER(ResnormDesc), vp, vp, vp, vp, vp, vp],
+            "lx_linear": [ctypes.POINTER(LinearDesc), vp, i64, vp, vp],
+            "lx_linear_workspace": [i32, i32, i32, ctypes.POINTER(u64)],
+            "lx_linear_backward": [ctypes.POINTER(LinearDesc), vp, i64, vp, vp, vp, vp, vp, u64, vp],
+            "lx_head_loss_workspace": [i32, i32, i32, i32, i32, ctypes.POINTER(u64)],
+            "lx_head_loss": [vp, i64, vp, i64, vp, vp, i32, i32, i32, vp, vp, vp, vp, u64, vp],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -765,3 +779,186 @@ def distill_loss(logits: torch.Tensor, teacher_id: torch.Tensor, teacher_logit: 
     if status:
         _check(status)
     return loss, dlogits
+
+
+# ----------------------------------------------------------------------------
+# products around a layer: the norm's output in 8 bits, dense products, the head's loss
+# ----------------------------------------------------------------------------
+class ResidualNormQ8(NamedTuple):
+    """What residual_norm_q8 gives: r_out, and h as e4m3 [T, H] with a scale fp32 [T]."""
+    r_out: torch.Tensor
+    q: torch.Tensor
+    scale: torch.Tensor
+
+
+def residual_norm_q8(r: torch.Tensor, y: Optional[torch.Tensor] = None, *, w_pre, w_post=None, gate=None,
+                     res_scale: float = 1.0, weight_offset: float = 0.0, eps: float = 1e-6, r_out=None,
+                     q_out=None, scale_out=None, h_out=None, stats=None, stream=None) -> ResidualNormQ8:
+    """residual_norm with h in 8 bits, as `linear` reads it:
+
+        scale = max(max|h| / 448, 2^-126) of each token,  q = e4m3(h / scale)
+
+    The other arguments are residual_norm's; ``h_out`` (in r's type) takes h itself too
+    where one is given.  For weights in 8 bits, a scale for each output:
+    ``s = (w.float().abs().amax(1) / 448).clamp(min=2**-126)``,
+    ``(w.float() / s[:, None]).to(torch.float8_e4m3fn)``."""
+    if stream is not None:
+        return _elsewhere(stream, residual_norm_q8, (r, y), dict(
+            w_pre=w_pre, w_post=w_post, gate=gate, res_scale=res_scale, weight_offset=weight_offset, eps=eps,
+            r_out=r_out, q_out=q_out, scale_out=scale_out, h_out=h_out, stats=stats))
+    dev = _device(r, "r")
+    d, shape, dtype = _resnorm_desc(dev, r, y, w_post, gate, w_pre, res_scale, weight_offset, eps)
+    T, H = shape
+    n = T * H
+    rp, hp = _flat(r_out, "r_out", dev, n, dtype), _flat(h_out, "h_out", dev, n, dtype)
+    if r_out is None and (y is not None or res_scale != 1.0):
+        r_out, rp = _empty_for(r, shape)
+    if q_out is None:
+        q_out = torch.empty(shape, dtype=torch.float8_e4m3fn, device=r.device)
+    if scale_out is None:
+        scale_out = torch.empty(T, dtype=torch.float32, device=r.device)
+    status = lib().lx_residual_norm_q8(
+        d, rp, _flat(q_out, "q_out", dev, n, torch.float8_e4m3fn), _flat(scale_out, "scale_out", dev, T), hp,
+        _flat(stats, "stats", dev, 2 * T), _raw_stream(dev))
+    if status:
+        _check(status)
+    return ResidualNormQ8(r if r_out is None else r_out, q_out, scale_out)
+
+
+_ACTS = {"none": LX_ACT_NONE, "relu": LX_ACT_RELU, "silu": LX_ACT_SILU, "gelu": LX_ACT_GELU}
+_LINEAR_TYPES = {torch.bfloat16: LX_BF16, torch.float8_e4m3fn: LX_E4M3}
+
+
+def _linear_desc(dev, x, w, act):
+    code = _LINEAR_TYPES.get(x.dtype)
+    if code is None:
+        raise ValueError("x must be bf16 or e4m3")
+    if act not in _ACTS:
+        raise ValueError("act must be one of " + ", ".join(_ACTS))
+    ldx = _rows(x, "x", dev)
+    T, K = x.shape
+    ldw = _rows(w, "w", dev, None, x.dtype)
+    if w.shape[1] != K:
+        raise ValueError(f"w must be [N, {K}]")
+    return LinearDesc(code, T, w.shape[0], K, _ACTS[act], ldx, ldw, 0, x.data_ptr(), w.data_ptr())
+
+
+def linear(x: torch.Tensor, w: torch.Tensor, *, x_scale=None, w_scale=None, bias=None, act: str = "none",
+           residual=None, y=None, pre=None, stream=None) -> torch.Tensor:
+    """y = act(x w^T + bias) + residual, bf16 [T, N], of x [T, K] and w [N, K] in bf16, or in
+    e4m3 with x_scale fp32 [T] and w_scale fp32 [N] (the product times both).
+
+    act: "none", "relu", "silu" or "gelu" (by the error function); bias bf16 [N]; residual
+    bf16 [T, N]; rows of x, w, residual and y may be slices of wider ones (x's and w's on
+    16-byte boundaries, K a multiple of 16 bytes).  ``y`` may be the residual (in place);
+    ``pre`` (bf16 [T, N]) takes the sum before the activation for linear_backward."""
+    if stream is not None:
+        return _elsewhere(stream, linear, (x, w), dict(x_scale=x_scale, w_scale=w_scale, bias=bias, act=act,
+                                                       residual=residual, y=y, pre=pre))
+    dev = _device(x, "x")
+    d = _linear_desc(dev, x, w, act)
+    T, N, bf = d.T, d.N, torch.bfloat16
+    if (x_scale is None) != (d.dtype == LX_BF16) or (w_scale is None) != (d.dtype == LX_BF16):
+        raise ValueError("x_scale and w_scale go with e4m3")
+    d.x_scale, d.w_scale = _flat(x_scale, "x_scale", dev, T), _flat(w_scale, "w_scale", dev, N)
+    d.bias = _flat(bias, "bias", dev, N, bf)
+    if residual is not None:
+        d.ldr, d.residual = _rows(residual, "residual", dev, (T, N), bf), residual.data_ptr()
+    if y is None:
+        y, ldy = torch.empty((T, N), dtype=bf, device=x.device), N
+    else:
+        ldy = _rows(y, "y", dev, (T, N), bf)
+    status = lib().lx_linear(d, y.data_ptr(), ldy, _flat(pre, "pre", dev, T * N, bf), _raw_stream(dev))
+    if status:
+        _check(status)
+    return y
+
+
+class LinearGrads(NamedTuple):
+    """Gradients of linear; None where not asked for.  (The residual's is dy.)"""
+    dx: Optional[torch.Tensor]
+    dw: Optional[torch.Tensor]
+    dbias: Optional[torch.Tensor]
+
+
+def linear_workspace_bytes(T: int, N: int, K: int) -> int:
+    b = ctypes.c_uint64()
+    _check(lib().lx_linear_workspace(T, N, K, b))
+    return b.value
+
+
+def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, *, act: str = "none", pre=None,
+                    want_dx: bool = True, want_dw: bool = True, want_dbias: bool = False, workspace=None,
+                    stream=None) -> LinearGrads:
+    """Gradients of linear (bf16) with respect to x, w and bias from that of y [T, N]; x, w,
+    act and pre are the forward's (pre with an activation alone)."""
+    if stream is not None:
+        return _elsewhere(stream, linear_backward, (dy, x, w), dict(
+            act=act, pre=pre, want_dx=want_dx, want_dw=want_dw, want_dbias=want_dbias, workspace=workspace))
+    dev = _device(x, "x")
+    d = _linear_desc(dev, x, w, act)
+    T, N, K, bf = d.T, d.N, d.K, torch.bfloat16
+    lddy = _rows(dy, "dy", dev, (T, N), bf)
+    dx, p0 = _empty_for(x if want_dx else None, (T, K))
+    dw, p1 = _empty_for(w if want_dw else None, (N, K))
+    dbias, p2 = _empty_for(w if want_dbias else None, N)
+    if workspace is None:
+        workspace = torch.empty(linear_workspace_bytes(T, N, K), dtype=torch.uint8, device=x.device)
+    else:
+        _check_workspace(workspace, dev)
+    status = lib().lx_linear_backward(d, dy.data_ptr(), lddy, _flat(pre, "pre", dev, T * N, bf), p0, p1, p2,
+                                      workspace.data_ptr(), workspace.nbytes, _raw_stream(dev))
+    if status:
+        _check(status)
+    return LinearGrads(dx, dw, dbias)
+
+
+class HeadLoss(NamedTuple):
+    """What head_loss computes: loss fp32 [T], and the gradients of its sum (None where not
+    asked for)."""
+    loss: torch.Tensor
+    dh: Optional[torch.Tensor]
+    dw: Optional[torch.Tensor]
+
+
+def head_loss_workspace_bytes(T: int, V: int, H: int, want_dh: bool = True, want_dw: bool = True) -> int:
+    b = ctypes.c_uint64()
+    _check(lib().lx_head_loss_workspace(T, V, H, int(want_dh), int(want_dw), b))
+    return b.value
+
+
+def head_loss(h: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, *, row_weight=None, want_dh: bool = True,
+              want_dw: bool = True, workspace=None, stream=None) -> HeadLoss:
+    """Softmax cross-entropy of the logits h w^T, which are not kept, against int32 labels
+    [T], of the last hidden states h [T, H] and the head's weights w [V, H] (bf16):
+
+        loss = row_weight * (logsumexp(h w^T) - (h w^T)[label])
+
+    with the gradients of its sum.  A token whose label is outside [0, V) or whose weight is
+    0 takes no part (loss and gradient 0, its hidden state not used) and costs no products."""
+    if stream is not None:
+        return _elsewhere(stream, head_loss, (h, w, labels), dict(
+            row_weight=row_weight, want_dh=want_dh, want_dw=want_dw, workspace=workspace))
+    dev = _device(h, "h")
+    if h.dtype != torch.bfloat16:
+        raise ValueError("h must be bf16")
+    ldh = _rows(h, "h", dev)
+    T, H = h.shape
+    ldw = _rows(w, "w", dev, None, torch.bfloat16)
+    V = w.shape[0]
+    if w.shape[1] != H:
+        raise ValueError(f"w must be [V, {H}]")
+    lp, rp = _flat(labels, "labels", dev, T, torch.int32), _flat(row_weight, "row_weight", dev, T)
+    loss = torch.empty(T, dtype=torch.float32, device=h.device)
+    dh, p0 = _empty_for(h if want_dh else None, (T, H))
+    dw, p1 = _empty_for(w if want_dw else None, (V, H))
+    if workspace is None:
+        workspace = torch.empty(head_loss_workspace_bytes(T, V, H, want_dh, want_dw), dtype=torch.uint8,
+                                device=h.device)
+    else:
+        _check_workspace(workspace, dev)
+    status = lib().lx_head_loss(h.data_ptr(), ldh, w.data_ptr(), ldw, lp, rp, T, V, H, loss.data_ptr(), p0, p1,
+                                workspace.data_ptr(), workspace.nbytes, _raw_stream(dev))
+    if status:
+        _check(status)
+    return HeadLoss(loss, dh, dw)
