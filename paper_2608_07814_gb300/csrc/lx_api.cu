@@ -3,6 +3,7 @@
 #include <cudaTypedefs.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdlib>
 #include <cstring>
@@ -86,11 +87,16 @@ OpShape op_shape(const lx_layer* L, int op) {
 int op_max_items(const lx_layer* L) { return std::max(L->n_anchor, L->n_corr); }
 
 static PFN_cuTensorMapEncodeTiled_v12000 get_encode() {
-  void* fn = nullptr;
-  cudaDriverEntryPointQueryResult q;
-  cudaError_t ce = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000,
-                                                    cudaEnableDefault, &q);
-  if (ce != cudaSuccess || q != cudaDriverEntryPointSuccess || !fn) return nullptr;
+  // (asked for until it is there: looking it up takes longer than encoding a map)
+  static std::atomic<void*> found{nullptr};
+  void* fn = found.load(std::memory_order_relaxed);
+  if (!fn) {
+    cudaDriverEntryPointQueryResult q;
+    cudaError_t ce = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000,
+                                                      cudaEnableDefault, &q);
+    if (ce != cudaSuccess || q != cudaDriverEntryPointSuccess || !fn) return nullptr;
+    found.store(fn, std::memory_order_relaxed);
+  }
   return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
 }
 

@@ -12,7 +12,9 @@
 //      of the tensor core, and the two gradient products of the piece in one launch.  dh is
 //      held in fp32 between the pieces.
 // With the logits formed twice that is 8 T V H operations against the 6 that a kept [T][V]
-// needs, and a workspace that does not grow with T V.
+// needs, and a workspace that does not grow with T V.  Where all logits fit, as fp32, into the
+// room of a piece, they are kept there and step 3 reads them instead of W: few tokens would
+// spend as long on reading W again as on everything else.
 #include "lx_product.cuh"
 
 namespace lx {
@@ -21,14 +23,14 @@ namespace {
 using namespace rows;
 using namespace prod;
 
-constexpr int ROWS = 64;                     // of a CTA of k_head_rows
-constexpr long PIECE_BYTES = 256L << 20;     // of dz at most
+constexpr int ROWS = 8;                      // of a CTA of k_head_rows, one a warp
+constexpr long PIECE_BYTES = 256L << 20;     // of dz, or of kept logits, at most
 constexpr int MAX_T = 1 << 24, MAX_V = 1 << 24, MAX_H = 1 << 20;
 
 struct Head {
   int T, V, H, Tp;  // Tp: rows of the compact arrays, a multiple of 256
-  const __nv_bfloat16* h;
-  long ldh;
+  const __nv_bfloat16 *h, *w;
+  long ldh, ldw;
   const int* labels;
   const float* row_weight;
   float* loss;
@@ -36,148 +38,135 @@ struct Head {
   // compact
   __nv_bfloat16* hc;
   int *label, *row, *n;
-  float *weight, *lse2;
-  const __nv_bfloat16* w;
-  long ldw;
+  float *weight, *lse2, *label_logit;
   const float2* part;
   int slots;
-  const float* blocks;
+  const float* blocks;  // of dh
   int slices;
+  const float* keep;    // the logits, keep_cols blocks side by side
+  int keep_cols;
+  __nv_bfloat16* dl;
+  long ldd;
 };
 
-__device__ __forceinline__ bool counts(const Head& A, int t) {
-  const int l = A.labels[t];
-  return l >= 0 && l < A.V && (!A.row_weight || A.row_weight[t] != 0.f);
-}
-
 // The rows that count, side by side in their order; loss and dh of the others are 0.  Each CTA
-// counts the rows before its own and all of them by itself: one launch, and for 8192 rows
-// as long as the copies.
+// counts the rows before its own and all of them by itself, so that one launch does.  A
+// row's label's logit is formed here, in fp32: the tensor core cuts its running sums off
+// instead of rounding them, 4e-6 of a logit of 2048 terms, which a loss shows and its
+// gradient does not.
 __global__ void __launch_bounds__(256) k_head_rows(const __grid_constant__ Head A) {
   __shared__ int red[2][8];
-  __shared__ int place[ROWS], first;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t0 = blockIdx.x * ROWS;
+  __shared__ int live[ROWS];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t0 = blockIdx.x * ROWS, t = t0 + warp;
+  // the warp's row and its label's row of W, while the rows are counted
+  const int pieces = A.H / 8, label = t < A.T ? A.labels[t] : -1;
+  const float weight = t < A.T ? (A.row_weight ? A.row_weight[t] : 1.f) : 0.f;
+  const bool mine = label >= 0 && label < A.V && weight != 0.f;
   int before = 0, all = 0;
 #pragma unroll 4
-  for (int t = threadIdx.x; t < A.T; t += 256) {
-    const int c = counts(A, t);
+  for (int i = threadIdx.x; i < A.T; i += 256) {
+    const int l = A.labels[i];
+    const float w = A.row_weight ? A.row_weight[i] : 1.f;
+    const int c = l >= 0 && l < A.V && w != 0.f;
     all += c;
-    before += t < t0 ? c : 0;
+    before += i < t0 ? c : 0;
   }
   before = __reduce_add_sync(0xffffffffu, before);
   all = __reduce_add_sync(0xffffffffu, all);
-  if (lane == 0) red[0][warp] = before, red[1][warp] = all;
+  if (lane == 0) red[0][warp] = before, red[1][warp] = all, live[warp] = mine;
   __syncthreads();
   before = all = 0;
 #pragma unroll
-  for (int w = 0; w < 8; ++w) before += red[0][w], all += red[1][w];
-  if (threadIdx.x < ROWS) {
-    const int t = t0 + threadIdx.x;
-    const bool c = t < A.T && counts(A, t);
-    const unsigned m = __ballot_sync(0xffffffffu, c);
-    const int at = __popc(m & ((1u << lane) - 1u));
-    if (threadIdx.x == 0) first = __popc(m);  // of the first warp's rows
-    place[threadIdx.x] = c ? at : -1;
-  }
-  __syncthreads();
-  if (threadIdx.x < ROWS) {
-    const int t = t0 + threadIdx.x;
-    int at = place[threadIdx.x];
-    if (at >= 0) {
-      at += before + (warp == 1 ? first : 0);
-      place[threadIdx.x] = at;
-      A.label[at] = A.labels[t];
-      A.weight[at] = A.row_weight ? A.row_weight[t] : 1.f;
-      A.row[at] = t;
-    } else if (t < A.T) {
-      A.loss[t] = 0.f;
-    }
+  for (int i = 0; i < 8; ++i) {
+    before += red[0][i] + (i < warp ? live[i] : 0);
+    all += red[1][i];
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) *A.n = all;
-  __syncthreads();
-  const int pieces = A.H / 8;
-  for (int r = warp; r < ROWS; r += 8) {
-    const int t = t0 + r, at = place[r];
-    if (t < A.T) {
-      if (at >= 0) {
-        const uint4* s = (const uint4*)(A.h + (long)t * A.ldh);
-        uint4* d = (uint4*)(A.hc + (long)at * A.H);
-#pragma unroll 4
-        for (int c = lane; c < pieces; c += 32) d[c] = s[c];
-      } else if (A.dh) {
-        uint4* d = (uint4*)(A.dh + (long)t * A.H);
-        for (int c = lane; c < pieces; c += 32) d[c] = make_uint4(0u, 0u, 0u, 0u);
-      }
+  if (mine) {
+    const uint4* s = (const uint4*)(A.h + (long)t * A.ldh);
+    const uint4* b = (const uint4*)(A.w + (long)label * A.ldw);
+    uint4* d = (uint4*)(A.hc + (long)before * A.H);
+    float2 z = make_float2(0.f, 0.f);
+#pragma unroll 8
+    for (int c = lane; c < pieces; c += 32) {
+      const uint4 x = s[c], y = b[c];
+      d[c] = x;
+      z = fmas(bf2(x.x), bf2(y.x), z);
+      z = fmas(bf2(x.y), bf2(y.y), z);
+      z = fmas(bf2(x.z), bf2(y.z), z);
+      z = fmas(bf2(x.w), bf2(y.w), z);
     }
-    // rows of the last, ragged block of a sum over the tokens
-    if (t >= all && t < (all + 63) / 64 * 64) {
-      uint4* d = (uint4*)(A.hc + (long)t * A.H);
+    const float dot = warp_sum(z.x + z.y);
+    if (lane == 0) {
+      A.label[before] = label;
+      A.weight[before] = weight;
+      A.row[before] = t;
+      A.label_logit[before] = dot;
+    }
+  } else if (t < A.T) {
+    if (lane == 0) A.loss[t] = 0.f;
+    if (A.dh) {
+      uint4* d = (uint4*)(A.dh + (long)t * A.H);
       for (int c = lane; c < pieces; c += 32) d[c] = make_uint4(0u, 0u, 0u, 0u);
     }
+  }
+  // rows of the last, ragged block of a sum over the tokens
+  if (t >= all && t < (all + 63) / 64 * 64) {
+    uint4* d = (uint4*)(A.hc + (long)t * A.H);
+    for (int c = lane; c < pieces; c += 32) d[c] = make_uint4(0u, 0u, 0u, 0u);
   }
 }
 
 // A row's log-sum-exp (in units of log 2, as the exponentials are taken) and loss.  A lane a row,
-// 32 warps a CTA side by side over the partial sums, added in the warps' order.  The label's
-// logit is formed again by a warp: the tensor core cuts its running sums off instead of
-// rounding them, 4e-6 of a logit of 2048 terms, which a loss shows and its gradient does not.
+// 32 warps a CTA side by side over the partial sums, added in the warps' order.
 __global__ void __launch_bounds__(1024) k_head_lse(const __grid_constant__ Head A) {
   __shared__ float2 red[32][33];
-  __shared__ float own[32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.x * 32 + lane, n = *A.n;
   if (blockIdx.x * 32 >= n) return;
-  auto join = [](float2 a, float2 b) {
-    const float m = fmaxf(a.x, b.x);
-    if (m == -INFINITY) return make_float2(m, a.y + b.y);
-    const float at = m * LOG2E;
-    return make_float2(m, a.y * ex2(fmaf(a.x, LOG2E, -at)) + b.y * ex2(fmaf(b.x, LOG2E, -at)));
+  // the sums of eight more parts, all taken to the largest value first
+  auto join = [](float2& v, const float2 (&p)[8]) {
+    float m = v.x;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = fmaxf(m, p[j].x);
+    const float at = m == -INFINITY ? 0.f : m * LOG2E;
+    float s = v.y * ex2(fmaf(v.x, LOG2E, -at));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s += p[j].y * ex2(fmaf(p[j].x, LOG2E, -at));
+    v = make_float2(m, s);
   };
-  float2 v = make_float2(-INFINITY, 0.f);
+  const float2 none = make_float2(-INFINITY, 0.f);
+  float2 v = none;
   if (i < n)
-#pragma unroll 4
-    for (int s = warp; s < A.slots; s += 32) v = join(v, A.part[(long)s * A.Tp + i]);
-  red[warp][lane] = v;
-  if (blockIdx.x * 32 + warp < n) {  // a row's label's logit
-    const int r = blockIdx.x * 32 + warp;
-    const uint4* a = (const uint4*)(A.hc + (long)r * A.H);
-    const uint4* b = (const uint4*)(A.w + (long)A.label[r] * A.ldw);
-    float2 s = make_float2(0.f, 0.f);
-#pragma unroll 4
-    for (int c = lane; c < A.H / 8; c += 32) {
-      const uint4 x = a[c], y = b[c];
-      s = fmas(bf2(x.x), bf2(y.x), s);
-      s = fmas(bf2(x.y), bf2(y.y), s);
-      s = fmas(bf2(x.z), bf2(y.z), s);
-      s = fmas(bf2(x.w), bf2(y.w), s);
+    for (int s = warp; s < A.slots; s += 32 * 8) {
+      float2 p[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) p[j] = s + 32 * j < A.slots ? A.part[(long)(s + 32 * j) * A.Tp + i] : none;
+      join(v, p);
     }
-    const float z = warp_sum(s.x + s.y);
-    if (lane == 0) own[warp] = z;
-  }
+  red[warp][lane] = v;
   __syncthreads();
   if (warp == 0 && i < n) {
-#pragma unroll 4
-    for (int w = 1; w < 32; ++w) v = join(v, red[w][lane]);
+    v = none;
+#pragma unroll
+    for (int w = 0; w < 32; w += 8) {
+      float2 p[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) p[j] = red[w + j][lane];
+      join(v, p);
+    }
     const float l2 = v.x * LOG2E + log2f(v.y);
     A.lse2[i] = l2;
-    A.loss[A.row[i]] = A.weight[i] * (l2 * 0.69314718055994531f - own[lane]);
+    A.loss[A.row[i]] = A.weight[i] * (l2 * 0.69314718055994531f - A.label_logit[i]);
   }
 }
 
-// dh from its fp32 blocks: the slices in their order, rounded once, each row to its place
-__global__ void __launch_bounds__(256) k_head_dh(const __grid_constant__ Head A) {
-  __shared__ __align__(16) char stage[8][32 * STG_LD];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int rb = blockIdx.x, cb = blockIdx.y * 8 + warp, ncb = (A.H + 31) / 32, nrb = A.Tp / 32, n = *A.n;
-  if (rb * 32 >= n || cb >= ncb) return;
-  float v[32];
-#pragma unroll
-  for (int e = 0; e < 32; ++e) v[e] = 0.f;
-  for (int s = 0; s < A.slices; ++s) {
-    const float* b = A.blocks + (((long)s * nrb + rb) * ncb + cb) * 1024 + lane;
-#pragma unroll
-    for (int e = 0; e < 32; ++e) v[e] += b[32 * e];
-  }
-  char* stg = stage[warp];
+// A block of 32 x 32, a row a lane, into rows of memory (16-byte pieces; those inside the columns
+// and for which row() gives a place)
+template <typename Row>
+__device__ __forceinline__ void put_block(char* stg, const float (&v)[32], __nv_bfloat16* out, long ld, int col0, int cols,
+                                          Row row) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();
 #pragma unroll
   for (int j = 0; j < 4; ++j)
     *(uint4*)(stg + lane * STG_LD + 16 * j) =
@@ -186,10 +175,53 @@ __global__ void __launch_bounds__(256) k_head_dh(const __grid_constant__ Head A)
   __syncwarp();
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const int r = 8 * j + lane / 4, c = cb * 32 + 8 * (lane % 4);
-    if (rb * 32 + r < n && c < A.H)
-      *(uint4*)(A.dh + (long)A.row[rb * 32 + r] * A.H + c) = *(const uint4*)(stg + r * STG_LD + 16 * (lane % 4));
+    const int r = 8 * j + lane / 4, c = col0 + 8 * (lane % 4);
+    const long at = row(r);
+    if (at >= 0 && c < cols) *(uint4*)(out + at * ld + c) = *(const uint4*)(stg + r * STG_LD + 16 * (lane % 4));
   }
+}
+
+// dz of kept logits, a block a warp; rows up to the next 64 are zeros (a sum over the tokens
+// takes whole blocks)
+__global__ void __launch_bounds__(256) k_head_dz(const __grid_constant__ Head A) {
+  __shared__ __align__(16) char stage[8][32 * STG_LD];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = *A.n;
+  const int rb = blockIdx.y, cb = blockIdx.x * 8 + warp, row = rb * 32 + lane;
+  if (rb * 32 >= (n + 63) / 64 * 64 || cb >= A.keep_cols) return;
+  const float* b = A.keep + ((long)rb * A.keep_cols + cb) * 1024 + lane;
+  float v[32];
+  if (rb * 32 < n) {
+#pragma unroll
+    for (int e = 0; e < 32; ++e) v[e] = b[32 * e];
+  }
+  const bool on = row < n;
+  const float weight = on ? A.weight[row] : 0.f, lse2 = on ? A.lse2[row] : 0.f;
+  const int label = on ? A.label[row] - 32 * cb : -1;
+#pragma unroll
+  for (int e = 0; e < 32; ++e)
+    v[e] = on ? weight * (ex2(fmaf(v[e], LOG2E, -lse2)) - (label == e ? 1.f : 0.f)) : 0.f;
+  put_block(stage[warp], v, A.dl, A.ldd, 32 * cb, 32 * A.keep_cols, [&](int r) { return (long)rb * 32 + r; });
+}
+
+// dh from its fp32 blocks: the slices in their order, rounded once, each row to its place.  A CTA a
+// block, a warp four of its columns.
+__global__ void __launch_bounds__(256) k_head_dh(const __grid_constant__ Head A) {
+  __shared__ __nv_bfloat16 stage[32][40];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = *A.n;
+  const int rb = blockIdx.x, cb = blockIdx.y, ncb = gridDim.y, nrb = A.Tp / 32;
+  if (rb * 32 >= n) return;
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  const float* b = A.blocks + ((long)rb * ncb + cb) * 1024 + 128 * warp + lane;
+#pragma unroll 4
+  for (int s = 0; s < A.slices; ++s) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += b[(long)s * nrb * ncb * 1024 + 32 * e];
+  }
+  *(uint2*)&stage[lane][4 * warp] = make_uint2(to_bf2(make_float2(v[0], v[1])), to_bf2(make_float2(v[2], v[3])));
+  __syncthreads();
+  const int r = threadIdx.x / 4, c = 8 * (threadIdx.x % 4);
+  if (threadIdx.x < 128 && rb * 32 + r < n && cb * 32 + c < A.H)
+    *(uint4*)(A.dh + (long)A.row[rb * 32 + r] * A.H + cb * 32 + c) = *(const uint4*)&stage[r][c];
 }
 
 size_t al(size_t v) { return (v + 255) / 256 * 256; }
@@ -198,7 +230,8 @@ size_t al(size_t v) { return (v + 255) / 256 * 256; }
 struct Plan {
   long Tp, piece;  // columns of a piece, a multiple of 256
   int slots, slices;
-  size_t hc, label, weight, row, lse2, n, part, dl, blocks, bytes;
+  size_t hc, label, weight, row, lse2, label_logit, n, part, dl, blocks, keep, bytes;
+  int keep_cols;   // blocks of kept logits side by side, 0: not kept
 };
 
 Plan plan_of(int T, int V, int H, bool dh, bool dw) {
@@ -221,9 +254,16 @@ Plan plan_of(int T, int V, int H, bool dh, bool dw) {
   p.weight = take(4 * p.Tp);
   p.row = take(4 * p.Tp);
   p.lse2 = take(4 * p.Tp);
+  p.label_logit = take(4 * p.Tp);
   p.n = take(4);
   p.part = take(8 * (size_t)p.slots * p.Tp);
-  if (dh || dw) p.dl = take(2 * (size_t)p.Tp * p.piece);
+  if (dh || dw) {
+    p.dl = take(2 * (size_t)p.Tp * p.piece);
+    if (4 * p.Tp * nt * BN <= PIECE_BYTES) {
+      p.keep_cols = (int)(nt * BN / 32);
+      p.keep = take(4 * (size_t)p.Tp * nt * BN);
+    }
+  }
   if (dh) p.blocks = take(4 * (size_t)p.slices * (p.Tp / 32) * ((H + 31) / 32) * 1024);
   p.bytes = at;
   return p;
@@ -287,6 +327,8 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
   A.T = T, A.V = V, A.H = H, A.Tp = (int)L.Tp;
   A.h = (const __nv_bfloat16*)h;
   A.ldh = ldh;
+  A.w = (const __nv_bfloat16*)w;
+  A.ldw = ldw;
   A.labels = labels;
   A.row_weight = row_weight;
   A.loss = loss;
@@ -297,12 +339,15 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
   A.n = (int*)(ws + L.n);
   A.weight = (float*)(ws + L.weight);
   A.lse2 = (float*)(ws + L.lse2);
-  A.w = (const __nv_bfloat16*)w;
-  A.ldw = ldw;
+  A.label_logit = (float*)(ws + L.label_logit);
   A.part = (const float2*)(ws + L.part);
   A.slots = L.slots;
   A.blocks = (const float*)(ws + L.blocks);
   A.slices = L.slices;
+  A.keep = (const float*)(ws + L.keep);
+  A.keep_cols = L.keep_cols;
+  A.dl = (__nv_bfloat16*)(ws + L.dl);
+  A.ldd = L.piece;
 
   k_head_rows<<<(unsigned)(L.Tp / ROWS), 256, 0, st>>>(A);
   LX_CUDA(cudaGetLastError());
@@ -316,6 +361,8 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
   P.lse2 = A.lse2;
   P.part = (float2*)(ws + L.part);
   P.part_ld = L.Tp;
+  P.keep = L.keep_cols ? (float*)(ws + L.keep) : nullptr;
+  P.keep_cols = L.keep_cols;
   P.dl = (__nv_bfloat16*)(ws + L.dl);
   P.ldd = L.piece;
   Problem& p = P.p[0];
@@ -333,10 +380,15 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
   for (long v0 = 0; v0 < V; v0 += L.piece) {
     const long n = std::min<long>(L.piece, V - v0);
     const __nv_bfloat16* wp = (const __nv_bfloat16*)w + v0 * ldw;
-    P.v0 = (int)v0;
-    p.N = (int)((n + 31) / 32 * 32);  // (whole blocks of dz; those behind the vocabulary are not read)
-    if (!operand(&p.b, wp, H, n, ldw, 2, false)) return fail(LX_ERR_CUDA, "cuTensorMapEncodeTiled(head) failed");
-    LX_TRY((launch_product<DLOGIT, false>(P, st)));
+    if (L.keep_cols) {  // (one piece)
+      k_head_dz<<<dim3((L.keep_cols + 7) / 8, (unsigned)(L.Tp / 32)), 256, 0, st>>>(A);
+      LX_CUDA(cudaGetLastError());
+    } else {
+      P.v0 = (int)v0;
+      p.N = (int)((n + 31) / 32 * 32);  // (whole blocks of dz; those behind the vocabulary are not read)
+      if (!operand(&p.b, wp, H, n, ldw, 2, false)) return fail(LX_ERR_CUDA, "cuTensorMapEncodeTiled(head) failed");
+      LX_TRY((launch_product<DLOGIT, false>(P, st)));
+    }
     G.n = 0;
     bool ok = true;
     if (dh) {
@@ -362,7 +414,7 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
     LX_TRY((launch_product<GRAD, false>(G, st)));
   }
   if (dh) {
-    k_head_dh<<<dim3((unsigned)(L.Tp / 32), (unsigned)(((H + 31) / 32 + 7) / 8)), 256, 0, st>>>(A);
+    k_head_dh<<<dim3((unsigned)(L.Tp / 32), (H + 31) / 32), 256, 0, st>>>(A);
     LX_CUDA(cudaGetLastError());
   }
   return LX_OK;

@@ -177,8 +177,9 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) k_linear_few(const __grid_cons
       const bool on = col + e < P.N;
       const float s = F8 && on ? xs * E.w_scale[col + e] : 1.f;
       z[e] = fmaf(v[e], s, E.bias && on ? to_f32(E.bias[col + e]) : 0.f);
-      v[e] = act_of(E.act, z[e]);
+      v[e] = z[e];
     }
+    activate(E.act, v);
     if (P.vec && col + 3 < P.N) {
       if (E.residual) {
         const uint2 r = *(const uint2*)(E.residual + row * E.ldr + col);
@@ -254,22 +255,29 @@ struct DzArgs {
   float* part;           // [CTAs of rows][N], or NULL
 };
 
-__device__ __forceinline__ float dact_of(int act, float z) {
-  if (act == RELU) return z > 0.f ? 1.f : 0.f;
-  if (act == SILU) {
-    const float s = __fdividef(1.f, 1.f + ex2(-LOG2E * z));
-    return s * (1.f + z * (1.f - s));
+// d times the activation's derivative
+template <int ACT>
+__device__ __forceinline__ float through(float d, float z) {
+  if (ACT == RELU) return z > 0.f ? d : d * 0.f;
+  if (ACT == SILU) {
+    const float s = rcp(1.f + ex2(-LOG2E * z));
+    return d * (s * fmaf(z, 1.f - s, 1.f));
   }
-  if (act == GELU)
-    return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * 0.3989422804014327f * ex2(-0.5f * LOG2E * z * z);
-  return 1.f;
+  if (ACT == GELU) {
+    float e;
+    const float cdf = normal_cdf(z, e);
+    return d * fmaf(z * 0.3989422804014327f, e, cdf);
+  }
+  return d;
 }
 
 // dz is rounded to bf16 as the tensor cores take it (2^-9 of each term of the gradients' fp32
-// sums); the bias's gradient sums it unrounded.  A warp reads rows of 32 VEC columns.
-template <int VEC>
-__global__ void __launch_bounds__(256) k_linear_dz(const __grid_constant__ DzArgs A) {
+// sums); the bias's gradient sums it unrounded.  A warp reads rows of 32 VEC columns, four rows
+// ahead.
+template <int VEC, int ACT>
+__global__ void __launch_bounds__(256, 4) k_linear_dz(const __grid_constant__ DzArgs A) {
   __shared__ float sums[8][32 * VEC];
+  constexpr int W = VEC == 8 ? 4 : 1;  // words of a piece
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int col = (blockIdx.x * 32 + lane) * VEC;
   const long t0 = (long)blockIdx.y * A.chunk;
@@ -277,34 +285,38 @@ __global__ void __launch_bounds__(256) k_linear_dz(const __grid_constant__ DzArg
   float s[VEC];
 #pragma unroll
   for (int e = 0; e < VEC; ++e) s[e] = 0.f;
+  auto read = [&](const __nv_bfloat16* p, uint32_t (&w)[W]) {
+    if constexpr (VEC == 8) {
+      const uint4 v = *(const uint4*)p;
+      w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    } else {
+      w[0] = *(const uint16_t*)p;
+    }
+  };
   if (col < A.N) {
-#pragma unroll 4
-    for (int r = warp; r < n; r += 8) {
-      const long t = t0 + r;
-      float d[VEC], z[VEC];
-      if constexpr (VEC == 8) {
-        const uint4 v = *(const uint4*)(A.dy + t * A.lddy + col);
-        const uint32_t a[4] = {v.x, v.y, v.z, v.w};
-        uint32_t b[4] = {0u, 0u, 0u, 0u};
-        if (A.act != NONE) {
-          const uint4 u = *(const uint4*)(A.pre + t * A.ldp + col);
-          b[0] = u.x, b[1] = u.y, b[2] = u.z, b[3] = u.w;
+    for (int r0 = warp; r0 < n; r0 += 32) {
+      uint32_t a[4][W], b[4][W];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (r0 + 8 * i < n) {
+          const long t = t0 + r0 + 8 * i;
+          read(A.dy + t * A.lddy + col, a[i]);
+          if (ACT != NONE) read(A.pre + t * A.ldp + col, b[i]);
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 f = bf2(a[e]), g = bf2(b[e]);
-          d[2 * e] = f.x, d[2 * e + 1] = f.y, z[2 * e] = g.x, z[2 * e + 1] = g.y;
-        }
-      } else {
-        d[0] = to_f32(A.dy[t * A.lddy + col]);
-        z[0] = A.act != NONE ? to_f32(A.pre[t * A.ldp + col]) : 0.f;
-      }
+      for (int i = 0; i < 4; ++i)
+        if (r0 + 8 * i < n) {
+          float d[VEC];
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        d[e] *= dact_of(A.act, z[e]);
-        s[e] += d[e];
-      }
-      if (A.dz) store<__nv_bfloat16, VEC>(A.dz + t * A.ldz + col, d);
+          for (int e = 0; e < VEC; ++e) {
+            auto at = [e](const uint32_t (&w)[W]) {
+              return VEC == 8 && (e & 1) ? __uint_as_float(w[e / 2] & 0xffff0000u) : __uint_as_float(w[e / 2] << 16);
+            };
+            d[e] = through<ACT>(at(a[i]), ACT != NONE ? at(b[i]) : 0.f);
+            s[e] += d[e];
+          }
+          if (A.dz) store<__nv_bfloat16, VEC>(A.dz + (t0 + r0 + 8 * i) * A.ldz + col, d);
+        }
     }
   }
   if (!A.part) return;
@@ -319,6 +331,14 @@ __global__ void __launch_bounds__(256) k_linear_dz(const __grid_constant__ DzArg
     for (int w = 0; w < 8; ++w) v += sums[w][c];
     A.part[(long)blockIdx.y * A.N + at] = v;
   }
+}
+
+template <int VEC>
+void launch_dz(const DzArgs& A, dim3 grid, cudaStream_t st) {
+  if (A.act == RELU) k_linear_dz<VEC, RELU><<<grid, 256, 0, st>>>(A);
+  else if (A.act == SILU) k_linear_dz<VEC, SILU><<<grid, 256, 0, st>>>(A);
+  else if (A.act == GELU) k_linear_dz<VEC, GELU><<<grid, 256, 0, st>>>(A);
+  else k_linear_dz<VEC, NONE><<<grid, 256, 0, st>>>(A);
 }
 
 // the CTAs' sums in their order: 8 ranges of them side by side, then those
@@ -502,8 +522,8 @@ extern "C" lx_status lx_linear_backward(const lx_linear_desc* d, const void* dy,
     DzArgs A = {T, N, d->act, chunk, (const __nv_bfloat16*)dy, (const __nv_bfloat16*)pre, (long)lddy, (long)N,
                 direct ? nullptr : dz, dz_ld(N), dbias ? part : nullptr};
     const bool vec = N % 8 == 0 && lddy % 8 == 0 && aligned(dy, 16) && aligned(pre, 16);
-    if (vec) k_linear_dz<8><<<dim3((N + 255) / 256, chunks), 256, 0, st>>>(A);
-    else k_linear_dz<1><<<dim3((N + 31) / 32, chunks), 256, 0, st>>>(A);
+    if (vec) launch_dz<8>(A, dim3((N + 255) / 256, chunks), st);
+    else launch_dz<1>(A, dim3((N + 31) / 32, chunks), st);
     if (dbias) k_linear_db<<<(N + 31) / 32, 256, 0, st>>>(part, chunks, N, (__nv_bfloat16*)dbias);
     LX_CUDA(cudaGetLastError());
   }

@@ -85,6 +85,8 @@ struct Launch {
   // STATS
   float2* part;      // [halves of tiles of N][part_ld]: a row's largest logit there, sum of exp
   long part_ld;
+  float* keep;       // the logits in blocks of 32 x 32 (32 rows of each column), or NULL
+  int keep_cols;     // blocks side by side
 };
 
 static __device__ __forceinline__ uint32_t mapa0(uint32_t addr) {  // the even CTA's
@@ -167,12 +169,43 @@ __host__ __device__ constexpr uint32_t idesc(bool f8, int a_mn, int b_mn, int M,
 
 constexpr float LOG2E = 1.4426950408889634f;
 
-// act(z) and its derivative.  A NaN stays one; gelu by the error function.
-__device__ __forceinline__ float act_of(int act, float z) {
-  if (act == RELU) return z < 0.f ? 0.f : z;
-  if (act == SILU) return __fdividef(z, 1.f + rows::ex2(-LOG2E * z));
-  if (act == GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-  return z;
+// Activations.  A NaN stays one.
+__device__ __forceinline__ float rcp(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// The normal distribution's function at z, and exp(-z^2 / 2): the complementary error function by
+// Abramowitz and Stegun 7.1.26 (1.5e-7 at most, a 2^-15 of bf16's step; with erff an epilogue
+// took as long as 2500 inputs' products).
+__device__ __forceinline__ float normal_cdf(float z, float& e) {
+  const float t = rcp(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
+  e = rows::ex2(-0.5f * LOG2E * z * z);
+  float p = fmaf(1.061405429f, t, -1.453152027f);
+  p = fmaf(p, t, 1.421413741f);
+  p = fmaf(p, t, -0.284496736f);
+  p = fmaf(p, t, 0.254829592f);
+  const float c = 0.5f * p * t * e;
+  return z > 0.f ? 1.f - c : c;
+}
+__device__ __forceinline__ float relu(float z) { return z < 0.f ? 0.f : z; }
+__device__ __forceinline__ float silu(float z) { return z * rcp(1.f + rows::ex2(-LOG2E * z)); }
+__device__ __forceinline__ float gelu(float z) {
+  float e;
+  return z * normal_cdf(z, e);
+}
+template <int N>
+__device__ __forceinline__ void activate(int act, float (&v)[N]) {
+  if (act == RELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = relu(v[i]);
+  } else if (act == SILU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = silu(v[i]);
+  } else if (act == GELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = gelu(v[i]);
+  }
 }
 
 struct Tile {
@@ -432,6 +465,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
         }
         if constexpr (MODE == STATS) {
           const int n = min(32, p.N - col0);
+          if (P.keep) {
+            float* o = P.keep + ((long)(row0 / 32) * P.keep_cols + col0 / 32) * 1024 + lane;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[32 * e] = __uint_as_float(r[e]);
+          }
           if (n < 32)
 #pragma unroll
             for (int e = 0; e < 32; ++e)
@@ -505,10 +543,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
               w[e] = rows::to_bf2(make_float2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])));
             put_rows(stg, w, P.pre, P.ldp, row0, M, col0, p.N, P.vec_p);
           }
-          if (P.act != NONE) {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(act_of(P.act, __uint_as_float(r[e])));
-          }
+          activate(P.act, reinterpret_cast<float(&)[32]>(r));
           if (P.residual) {
             get_rows(stg, w, P.residual, P.ldr, row0, M, col0, p.N, P.vec_r);
 #pragma unroll

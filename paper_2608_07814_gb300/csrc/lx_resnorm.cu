@@ -327,38 +327,51 @@ struct Rows {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) elem(v, c, j) = p && c < count ? add + p[col(c) + j] : rest;
   }
-  // largest of the threads' values (bits of what has no sign: a NaN is above infinity), in
-  // the same memory
-  __device__ uint32_t most(uint32_t v, float (*buf)[1][COLS][MAX_W], int& turn) const {
+  // sum of the threads' v and largest of their m (bits of what has no sign: a NaN is above
+  // infinity) in one exchange, in a buffer of two values
+  __device__ void sum_most(float& v, uint32_t& m, float (*buf)[2][COLS][MAX_W], int& turn) const {
     if constexpr (GRP == WARP) {
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1)
-        if (o < size) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
-      return v;
+        if (o < size) {
+          v += __shfl_xor_sync(0xffffffffu, v, o);
+          m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+        }
+      return;
     }
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
-    uint32_t(*b)[MAX_W] = (uint32_t(*)[MAX_W])buf[turn][0];
+    float(*b)[COLS][MAX_W] = buf[turn];
     turn ^= 1;
-    v = __reduce_max_sync(0xffffffffu, v);
+    v = warp_sum(v);
+    m = __reduce_max_sync(0xffffffffu, m);
     int cols = 1;
     if constexpr (GRP == CTA) {
-      if (lane == 0) b[0][warp] = v;
+      if (lane == 0) b[0][0][warp] = v, b[1][0][warp] = __uint_as_float(m);
       __syncthreads();
     } else {
       cooperative_groups::cluster_group cl = cooperative_groups::this_cluster();
       cols = cl.num_blocks();
-      if (lane < cols) *cl.map_shared_rank(&b[cl.block_rank()][warp], lane) = v;
+      const int i = lane & 1, c = lane >> 1;
+      if (c < cols) *cl.map_shared_rank(&b[i][cl.block_rank()][warp], c) = i ? __uint_as_float(m) : v;
       cl.sync();
     }
+    v = 0.f;
     for (int c = 0; c < cols; ++c)
-      for (int w = 0; w < nw; ++w) v = max(v, b[c][w]);
-    return v;
+#pragma unroll
+      for (int w = 0; w < MAX_W; w += 4)
+        if (w < nw) {
+          const float4 p = *(const float4*)&b[0][c][w];
+          const uint4 q = *(const uint4*)&b[1][c][w];
+          v += (p.x + p.y) + (p.z + p.w);
+          m = max(max(m, max(q.x, q.y)), max(q.z, q.w));
+        }
   }
   // sums of N (1 or 3) values over the row's threads, the same in each of them; buf is
   // used in turn: a half is written again only after the barrier that follows its last
   // reads
-  template <int N>
-  __device__ void sum(float (&v)[N], float (*buf)[N][COLS][MAX_W], int& turn) const {
+  template <int N, int M>
+  __device__ void sum(float (&v)[N], float (*buf)[M][COLS][MAX_W], int& turn) const {
+    static_assert(N <= M, "a place for every value");
     if constexpr (GRP == WARP) {
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1)
@@ -424,7 +437,8 @@ extern __shared__ uint4 norm_ring[];
 template <typename T, int VEC, int GRP, bool Q8>
 __global__ void __launch_bounds__(max_threads(GRP), 65536 / REGS / max_threads(GRP))
 k_resnorm_fwd(const __grid_constant__ NormArgs A) {
-  __shared__ __align__(16) float buf[2][1][max_cols(GRP)][max_threads(GRP) / 32];
+  constexpr int NB = Q8 ? 2 : 1;
+  __shared__ __align__(16) float buf[2][NB][max_cols(GRP)][max_threads(GRP) / 32];
   int turn = 0;
   if (GRP == CTA) clear(buf);
   Rows<T, VEC, GRP> R(A, (char*)norm_ring);
@@ -480,23 +494,40 @@ k_resnorm_fwd(const __grid_constant__ NormArgs A) {
 #pragma unroll
       for (int i = 1; i < N2; ++i) p = fmas(x[i], x[i], p);
       q[0] = p.x + p.y;
-      R.sum(q, buf, turn);
-      s2 = rsqrtf(q[0] * inv + A.eps);
-#pragma unroll
-      for (int i = 0; i < N2; ++i) x[i] = muls(muls(x[i], both(s2)), w2[i]);
-      if (!Q8 || A.h_out) R.write(A.h_out, t, x);
       if constexpr (Q8) {
+        // the row's largest |r' w2| with its sum of squares: h is that times s2
+        float2 v[N2];
         uint32_t m = 0;
 #pragma unroll
-        for (int i = 0; i < N2; ++i)
-          m = max(m, max(__float_as_uint(x[i].x) & 0x7fffffffu, __float_as_uint(x[i].y) & 0x7fffffffu));
-        const float top = __uint_as_float(R.most(m, buf, turn));
-        const float scale = top < E4M3_MAX * TINY ? TINY : top / E4M3_MAX;  // (a NaN stays one)
-        const float2 by = both(1.f / scale);
+        for (int i = 0; i < N2; ++i) {
+          v[i] = muls(x[i], w2[i]);
+          m = max(m, max(__float_as_uint(v[i].x) & 0x7fffffffu, __float_as_uint(v[i].y) & 0x7fffffffu));
+        }
+        R.sum_most(q[0], m, buf, turn);
+        s2 = rsqrtf(q[0] * inv + A.eps);
+        if (A.h_out) {
 #pragma unroll
-        for (int i = 0; i < N2; ++i) x[i] = muls(x[i], by);
-        R.write_q8(t, x);
+          for (int i = 0; i < N2; ++i) x[i] = muls(muls(x[i], both(s2)), w2[i]);
+          R.write(A.h_out, t, x);
+        }
+        const float top = s2 * __uint_as_float(m);
+        float scale = top / E4M3_MAX, by = s2 / scale;
+        if (top < E4M3_MAX * TINY) {  // (by itself would be above fp32's range)
+          scale = TINY;
+          by = 1.f / TINY;
+#pragma unroll
+          for (int i = 0; i < N2; ++i) v[i] = muls(v[i], both(s2));
+        }
+#pragma unroll
+        for (int i = 0; i < N2; ++i) v[i] = muls(v[i], both(by));
+        R.write_q8(t, v);
         if (R.writer() && t < (unsigned)A.T) A.scale[t] = scale;
+      } else {
+        R.sum(q, buf, turn);
+        s2 = rsqrtf(q[0] * inv + A.eps);
+#pragma unroll
+        for (int i = 0; i < N2; ++i) x[i] = muls(muls(x[i], both(s2)), w2[i]);
+        R.write(A.h_out, t, x);
       }
     }
     if (A.stats && R.writer() && t < (unsigned)A.T) {
