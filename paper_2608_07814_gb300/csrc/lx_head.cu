@@ -363,8 +363,6 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
   P.part_ld = L.Tp;
   P.keep = L.keep_cols ? (float*)(ws + L.keep) : nullptr;
   P.keep_cols = L.keep_cols;
-  P.dl = (__nv_bfloat16*)(ws + L.dl);
-  P.ldd = L.piece;
   Problem& p = P.p[0];
   p.M = (int)L.Tp, p.N = V, p.K = H, p.slices = 1;
   p.rows = A.n;
@@ -386,7 +384,7 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
     } else {
       P.v0 = (int)v0;
       p.N = (int)((n + 31) / 32 * 32);  // (whole blocks of dz; those behind the vocabulary are not read)
-      if (!operand(&p.b, wp, H, n, ldw, 2, false)) return fail(LX_ERR_CUDA, "cuTensorMapEncodeTiled(head) failed");
+      if (!operand(&p.b, wp, H, n, ldw, 2, false) || !boxes(&P.map_dl, A.dl, L.piece, L.Tp, L.piece)) return fail(LX_ERR_CUDA, "cuTensorMapEncodeTiled(head) failed");
       LX_TRY((launch_product<DLOGIT, false>(P, st)));
     }
     G.n = 0;
@@ -399,7 +397,7 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
       g.rows = A.n;
       g.blocks = (float*)(ws + L.blocks);
       g.add = v0 > 0;
-      ok = ok && operand(&g.a, P.dl, n, L.Tp, L.piece, 2, false) && operand(&g.b, wp, H, n, ldw, 2, true);
+      ok = ok && operand(&g.a, A.dl, n, L.Tp, L.piece, 2, false) && operand(&g.b, wp, H, n, ldw, 2, true);
     }
     if (dw) {
       Problem& g = G.p[G.n++];
@@ -407,8 +405,7 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
       g.M = (int)n, g.N = H, g.K = (int)L.Tp, g.slices = 1;
       g.a_mn = g.b_mn = 1;
       g.depth = A.n;
-      g.out = (__nv_bfloat16*)dw + v0 * H, g.ldo = H, g.vec = 1;
-      ok = ok && operand(&g.a, P.dl, n, L.Tp, L.piece, 2, true) && operand(&g.b, A.hc, H, L.Tp, H, 2, true);
+      ok = ok && boxes(&g.out, (__nv_bfloat16*)dw + v0 * H, H, n, H) && operand(&g.a, A.dl, n, L.Tp, L.piece, 2, true) && operand(&g.b, A.hc, H, L.Tp, H, 2, true);
     }
     if (!ok) return fail(LX_ERR_CUDA, "cuTensorMapEncodeTiled(head) failed");
     LX_TRY((launch_product<GRAD, false>(G, st)));

@@ -455,9 +455,9 @@ extern "C" lx_status lx_linear(const lx_linear_desc* d, void* y, int64_t ldy, vo
     F.vec = wide(y, ldy, 8) && wide(pre, d->N, 8) && wide(d->residual, d->ldr, 8);
     return f8 ? launch_few<true>(F, tb, es, d, st) : launch_few<false>(F, tb, es, d, st);
   }
-  P.vec_y = wide(y, ldy, 16);
-  P.vec_p = wide(pre, d->N, 16);
-  P.vec_r = wide(d->residual, d->ldr, 16);
+  P.tma_y = boxes(&P.map_y, y, d->N, d->T, ldy);
+  P.tma_p = pre && boxes(&P.map_p, pre, d->N, d->T, d->N);
+  P.tma_r = d->residual && boxes(&P.map_r, d->residual, d->N, d->T, d->ldr);
   P.n = 1;
   Problem& p = P.p[0];
   p.M = d->T;
@@ -541,15 +541,13 @@ extern "C" lx_status lx_linear_backward(const lx_linear_desc* d, const void* dy,
       Problem& p = P.p[P.n++];
       p.M = T, p.N = K, p.K = N, p.slices = 1;
       p.b_mn = 1;
-      p.out = dx, p.ldo = K, p.vec = 1;
-      ok = ok && operand(&p.a, g, N, T, ldg, 2, false) && operand(&p.b, d->w, K, N, d->ldw, 2, true);
+      ok = ok && boxes(&p.out, dx, K, T, K) && operand(&p.a, g, N, T, ldg, 2, false) && operand(&p.b, d->w, K, N, d->ldw, 2, true);
     } else {
       if (!dw) continue;
       Problem& p = P.p[P.n++];
       p.M = N, p.N = K, p.K = T, p.slices = 1;
       p.a_mn = p.b_mn = 1;
-      p.out = dw, p.ldo = K, p.vec = 1;
-      ok = ok && operand(&p.a, g, N, T, ldg, 2, true) && operand(&p.b, d->x, K, T, d->ldx, 2, true);
+      ok = ok && boxes(&p.out, dw, K, N, K) && operand(&p.a, g, N, T, ldg, 2, true) && operand(&p.b, d->x, K, T, d->ldx, 2, true);
     }
   }
   if (!ok) return fail(LX_ERR_CUDA, "cuTensorMapEncodeTiled(linear gradients) failed");

@@ -13,8 +13,8 @@
 //   warp 1       of the even CTA issues tcgen05.mma and commits stages and accumulators to
 //                both CTAs; (of both) allocates 512 TMEM columns: two accumulators, so that
 //                a tile's epilogue runs beside the next tile's products;
-//   warps 4..11  epilogue: 32 rows x 32 columns at a time from TMEM, what the caller's MODE
-//                makes of them, through a warp's block of shared memory to whole row segments.
+//   warps 4..11  epilogue: 32 rows x 64 columns at a time from TMEM, what the caller's MODE
+//                makes of them, and TMA from a warp's buffers of shared memory to memory.
 // Tiles are dealt in an order that keeps 8 rows of tiles together, so that what runs at the
 // same time shares its operands in L2.  Every wait is bounded: when one gives up, the pair's
 // tiles from there on are NaN, copies and products in flight are waited for, and TMEM is freed.
@@ -37,11 +37,15 @@ using namespace tcg;
 
 constexpr int BM = 256, BN = 256;      // a pair's tile
 constexpr int KB = 128;                // bytes of K a stage: 64 bf16 or 128 e4m3
-constexpr int A_BYTES = 128 * KB, STAGE = 2 * A_BYTES, STAGES = 6;
+constexpr int A_BYTES = 128 * KB, STAGE = 2 * A_BYTES, STAGES = 5;
 constexpr int EPI = 8, THREADS = 128 + 32 * EPI;
-constexpr int STG_LD = 80;             // bytes of a staged row of 32 bf16: 16-byte pieces of 8 rows on distinct banks
-constexpr int STG = 32 * STG_LD, PRM = 64 * 4;
-constexpr int SMEM = STAGES * STAGE + EPI * (STG + PRM) + 8 * (2 * STAGES + 8) + 1024;
+// Blocks of 32 rows x 64 columns leave a warp through two buffers of 4 KiB (128-byte rows,
+// 128-byte swizzle) by TMA: stores of 16 bytes a lane took 1.8 k cycles for 32 x 32, four
+// times what the products of 64 inputs take.
+constexpr int STG = 4096, PRM = 192;
+constexpr int STG_LD = 80;             // rows TMA cannot take: 32 bf16, 16-byte pieces of 8 rows on distinct banks
+constexpr int N_BARS = 2 * STAGES + 5 + 2 * EPI;
+constexpr int SMEM = STAGES * STAGE + EPI * (2 * STG + PRM) + 8 * N_BARS + 16 + 1024;
 constexpr int GROUP_M = 8;
 static_assert(SMEM <= 227 * 1024, "fits an SM");
 
@@ -56,10 +60,8 @@ struct Problem {
   int slices;
   const int* rows;   // device count that bounds M (NULL: M), and
   const int* depth;  // one that bounds K
-  // GRAD: bf16 rows ldo apart, or (blocks) fp32 in blocks of 32 x 32, slice by slice
-  void* out;
-  long ldo;
-  int vec;           // 16-byte stores
+  // GRAD: bf16 (boxes of 128 bytes x 32 rows), or fp32 in blocks of 32 x 32, slice by slice
+  CUtensorMap out;
   float* blocks;
   int add;           // to what the blocks hold
 };
@@ -73,14 +75,13 @@ struct Launch {
   const float *x_scale, *w_scale;
   const __nv_bfloat16 *bias, *residual;
   __nv_bfloat16 *y, *pre;
-  long ldr, ldy;  // (pre: ldp)
-  long ldp;
-  int act, vec_r, vec_y, vec_p;
+  long ldr, ldy, ldp;
+  int act, tma_r, tma_y, tma_p;  // whether their rows suit TMA (boxes of 128 bytes x 32 rows):
+  CUtensorMap map_r, map_y, map_p;
   // DLOGIT: compact rows' labels, weights and log-sum-exps (in units of log 2)
   const int* label;
   const float *weight, *lse2;
-  __nv_bfloat16* dl;
-  long ldd;
+  CUtensorMap map_dl;  // dz of the piece
   int v0;            // the first column's place in the vocabulary
   // STATS
   float2* part;      // [halves of tiles of N][part_ld]: a row's largest logit there, sum of exp
@@ -252,50 +253,77 @@ struct Sizes {
   }
 };
 
-// 32 x 32 bf16 of a warp, a row a lane, through its block of shared memory to rows of
-// memory: 16 bytes a lane where vec and the block lies inside, else single elements
-__device__ __forceinline__ void put_rows(char* stg, const uint32_t (&w)[16], __nv_bfloat16* out, long ldo, int row0,
-                                         int M, int col0, int N, bool vec) {
+// 32 x 32 bf16 of a warp, a row a lane, through shared memory to rows of memory that TMA
+// cannot take, a column a lane
+__device__ __forceinline__ void put_rows(char* stg, const uint32_t* r, __nv_bfloat16* out, long ldo, int row0, int M,
+                                         int col0, int N) {
   const int lane = threadIdx.x & 31;
   __syncwarp();
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    *(uint4*)(stg + lane * STG_LD + 16 * j) = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
-  __syncwarp();
-  if (vec && col0 + 32 <= N) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int r = 8 * j + lane / 4, q = lane % 4;
-      if (row0 + r < M) *(uint4*)(out + (long)(row0 + r) * ldo + col0 + 8 * q) = *(const uint4*)(stg + r * STG_LD + 16 * q);
-    }
-  } else if (col0 + lane < N) {
-    const int n = min(32, M - row0);
-    for (int r = 0; r < n; ++r)
-      out[(long)(row0 + r) * ldo + col0 + lane] = *(const __nv_bfloat16*)(stg + r * STG_LD + 2 * lane);
+  for (int j = 0; j < 4; ++j) {
+    const float* f = reinterpret_cast<const float*>(r) + 8 * j;
+    *(uint4*)(stg + lane * STG_LD + 16 * j) =
+        make_uint4(rows::to_bf2(make_float2(f[0], f[1])), rows::to_bf2(make_float2(f[2], f[3])),
+                   rows::to_bf2(make_float2(f[4], f[5])), rows::to_bf2(make_float2(f[6], f[7])));
   }
+  __syncwarp();
+  if (col0 + lane < N) {
+    const int n = min(32, M - row0);
+    for (int i = 0; i < n; ++i)
+      out[(long)(row0 + i) * ldo + col0 + lane] = *(const __nv_bfloat16*)(stg + i * STG_LD + 2 * lane);
+  }
+  __syncwarp();
 }
-// the other way: a lane's row of 32 elements (unset outside the matrix)
-__device__ __forceinline__ void get_rows(char* stg, uint32_t (&w)[16], const __nv_bfloat16* in, long ld, int row0, int M,
-                                         int col0, int N, bool vec) {
+// the other way, added to the lane's row
+__device__ __forceinline__ void add_rows(char* stg, uint32_t* r, const __nv_bfloat16* in, long ld, int row0, int M,
+                                         int col0, int N) {
   const int lane = threadIdx.x & 31;
   __syncwarp();
-  if (vec && col0 + 32 <= N) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int r = 8 * j + lane / 4, q = lane % 4;
-      if (row0 + r < M) *(uint4*)(stg + r * STG_LD + 16 * q) = *(const uint4*)(in + (long)(row0 + r) * ld + col0 + 8 * q);
-    }
-  } else if (col0 + lane < N) {
+  if (col0 + lane < N) {
     const int n = min(32, M - row0);
-    for (int r = 0; r < n; ++r)
-      *(__nv_bfloat16*)(stg + r * STG_LD + 2 * lane) = in[(long)(row0 + r) * ld + col0 + lane];
+#pragma unroll 8
+    for (int i = 0; i < n; ++i)
+      *(__nv_bfloat16*)(stg + i * STG_LD + 2 * lane) = in[(long)(row0 + i) * ld + col0 + lane];
   }
   __syncwarp();
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const uint4 v = *(const uint4*)(stg + lane * STG_LD + 16 * j);
-    w[4 * j] = v.x, w[4 * j + 1] = v.y, w[4 * j + 2] = v.z, w[4 * j + 3] = v.w;
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = rows::bf2(w[i]);
+      r[8 * j + 2 * i] = __float_as_uint(__uint_as_float(r[8 * j + 2 * i]) + f.x);
+      r[8 * j + 2 * i + 1] = __float_as_uint(__uint_as_float(r[8 * j + 2 * i + 1]) + f.y);
+    }
   }
+  __syncwarp();
+}
+// A lane's piece j (16 bytes) of its row in a buffer of 128-byte rows with the 128-byte swizzle
+__device__ __forceinline__ uint4* piece(char* buf, int j) {
+  const int lane = threadIdx.x & 31;
+  return (uint4*)(buf + lane * 128 + ((j ^ (lane & 7)) << 4));
+}
+// 32 rows x 64 columns, a row a lane, by TMA; the buffer is free
+__device__ __forceinline__ void put_box(char* buf, const uint32_t (&r)[64], const CUtensorMap* map, int col0, int row0) {
+  const float* f = reinterpret_cast<const float*>(r);
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    *piece(buf, j) = make_uint4(
+        rows::to_bf2(make_float2(f[8 * j], f[8 * j + 1])), rows::to_bf2(make_float2(f[8 * j + 2], f[8 * j + 3])),
+        rows::to_bf2(make_float2(f[8 * j + 4], f[8 * j + 5])), rows::to_bf2(make_float2(f[8 * j + 6], f[8 * j + 7])));
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) {
+    tma_store_2d(map, 2 * col0, row0, smem_u32(buf));
+    bulk_commit();
+  }
+}
+// at most N of the warp's boxes are still being read
+template <int N>
+__device__ __forceinline__ void box_wait() {
+  if ((threadIdx.x & 31) == 0) bulk_wait_read<N>();
+  __syncwarp();
 }
 
 template <int MODE, bool F8>
@@ -303,11 +331,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   char* staged = reinterpret_cast<char*>(smem + STAGES * STAGE);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(staged + EPI * (STG + PRM));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(staged + EPI * (2 * STG + PRM));
   const uint32_t base = smem_u32(smem), full0 = smem_u32(bars), empty0 = full0 + 8 * STAGES;
-  const uint32_t tfull0 = empty0 + 8 * STAGES, tempty0 = tfull0 + 16, drain = tempty0 + 16;
-  volatile int* lost = reinterpret_cast<volatile int*>(bars + 2 * STAGES + 5);
-  uint32_t* tmem_s = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 6);
+  const uint32_t tfull0 = empty0 + 8 * STAGES, tempty0 = tfull0 + 16, drain = tempty0 + 16, res0 = drain + 8;
+  volatile int* lost = reinterpret_cast<volatile int*>(bars + N_BARS);
+  uint32_t* tmem_s = reinterpret_cast<uint32_t*>(bars + N_BARS + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
@@ -322,6 +350,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
       mbar_init(tempty0 + 8 * b, 2 * EPI);      // the even CTA's: both CTAs' epilogue warps
     }
     mbar_init(drain, 1);
+    for (int i = 0; i < 2 * EPI; ++i) mbar_init(res0 + 8 * i, 1);
     *lost = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -419,15 +448,40 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     }
   } else if (warp >= 4) {
     const int q = warp & 3, half = (warp - 4) >> 2;
-    char* stg = staged + (warp - 4) * (STG + PRM);
-    float* prm = reinterpret_cast<float*>(stg + STG);
+    char* stg = staged + (warp - 4) * 2 * STG;
+    float* prm = reinterpret_cast<float*>(staged + EPI * 2 * STG + (warp - 4) * PRM);  // scales, then the bias
+    __nv_bfloat16* prm_b = reinterpret_cast<__nv_bfloat16*>(prm + 32);
+    const uint32_t res = res0 + 16 * (warp - 4);
+    uint32_t res_turn = 0;  // bit j: phase of buffer j's barrier
     const float nan = __int_as_float(0x7fc00000);
     uint32_t nt = 0;
-    int ok = 1;
+    int ok = 1, last = -1;  // the buffer that the last box left from
+    auto box_free = [&](int j) {
+      if (last == j) box_wait<0>();
+      else box_wait<1>();
+      last = j;
+    };
     for (int i = pair; S.at(P, i, t); i += pairs) {
       const Problem& p = P.p[t.p];
       const int M = t.p ? S.M[1] : S.M[0];
       const uint32_t acc = nt & 1;
+      const int row0 = t.m0 + 128 * (int)rank + 32 * q, row = row0 + lane;
+      // dz has rows of zeros behind the last: whole tiles
+      const bool on = row0 < (MODE == DLOGIT ? p.M : M);
+      // the residual's block j by TMA into its buffer, once what left it has been read
+      auto fetch = [&](int j) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        box_wait<0>();
+        if (lane == 0) {
+          mbar_expect_tx(res + 8 * j, STG);
+          tma_load_2d(smem_u32(stg + j * STG), &P.map_r, 2 * (t.n0 + 128 * half + 64 * j), row0, res + 8 * j);
+        }
+      };
+      const bool ahead = MODE == LINEAR && P.tma_r && on;
+      if (ahead) {
+        if (t.n0 + 128 * half < p.N) fetch(0);
+        if (!P.pre && t.n0 + 128 * half + 64 < p.N) fetch(1);
+      }
       if (t.nkb > 0) {
         if (ok && lane == 0) {
           ok = wait_cluster(tfull0 + 8 * acc, (nt >> 1) & 1, lost, P.wait_cycles) ? 1 : 0;
@@ -437,50 +491,50 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
         tc_fence_after();
         ++nt;
       }
-      const int row0 = t.m0 + 128 * (int)rank + 32 * q, row = row0 + lane;
       float best = -INFINITY, total = 0.f;  // STATS
       int label = -1;
       float weight = 0.f, lse2 = 0.f, xs = 1.f;
       if (MODE == DLOGIT && row < M) label = P.label[row] - P.v0, weight = P.weight[row], lse2 = P.lse2[row];
       if (MODE == LINEAR && F8) xs = row < M ? P.x_scale[row] : 0.f;
 #pragma unroll 1
-      for (int c = 0; c < 4; ++c) {
-        const int col0 = t.n0 + 128 * half + 32 * c;
-        uint32_t r[32];
+      for (int j = 0; j < 2; ++j) {
+        const int col0 = t.n0 + 128 * half + 64 * j;
+        char* buf = stg + j * STG;
+        uint32_t r[64];
         __syncwarp();
         if (t.nkb > 0 && ok) {
-          tc_ld32_async(tmem + ((uint32_t)(32 * q) << 16) + acc * BN + 128 * half + 32 * c, r);
+          const uint32_t at = tmem + ((uint32_t)(32 * q) << 16) + acc * BN + 128 * half + 64 * j;
+          tc_ld32_async(at, *reinterpret_cast<uint32_t(*)[32]>(r));
+          tc_ld32_async(at + 32, *reinterpret_cast<uint32_t(*)[32]>(r + 32));
           tc_wait_ld();
-          if (c == 3) {  // the accumulator is read: the next tile but one may take its place
+          if (j == 1) {  // the accumulator is read: the next tile but one may take its place
             tc_fence_before();
             __syncwarp();
             if (lane == 0) arrive_remote(mapa0(tempty0 + 8 * acc));
           }
         } else {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) r[e] = ok ? 0u : __float_as_uint(nan);
+          for (int e = 0; e < 64; ++e) r[e] = ok ? 0u : __float_as_uint(nan);
         }
-        if (col0 >= p.N || row0 >= M) {
-          if (!(MODE == DLOGIT && row0 < p.M && col0 < p.N)) continue;
-        }
+        if (col0 >= p.N || !on) continue;
         if constexpr (MODE == STATS) {
-          const int n = min(32, p.N - col0);
+          const int n = min(64, p.N - col0);
           if (P.keep) {
             float* o = P.keep + ((long)(row0 / 32) * P.keep_cols + col0 / 32) * 1024 + lane;
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[32 * e] = __uint_as_float(r[e]);
+            for (int e = 0; e < 64; ++e) o[32 * e] = __uint_as_float(r[e]);  // (keep_cols is even)
           }
-          if (n < 32)
+          if (n < 64)
 #pragma unroll
-            for (int e = 0; e < 32; ++e)
+            for (int e = 0; e < 64; ++e)
               if (e >= n) r[e] = 0xff800000u;  // -inf
           float m = best;
 #pragma unroll
-          for (int e = 0; e < 32; ++e) m = fmaxf(m, __uint_as_float(r[e]));
+          for (int e = 0; e < 64; ++e) m = fmaxf(m, __uint_as_float(r[e]));
           const float at = m == -INFINITY ? 0.f : m * LOG2E;  // (a row of -inf so far)
           float s0 = total * rows::ex2(best == -INFINITY ? -INFINITY : fmaf(best, LOG2E, -at)), s1 = 0.f;
 #pragma unroll
-          for (int e = 0; e < 32; e += 2) {
+          for (int e = 0; e < 64; e += 2) {
             s0 += rows::ex2(fmaf(__uint_as_float(r[e]), LOG2E, -at));
             s1 += rows::ex2(fmaf(__uint_as_float(r[e + 1]), LOG2E, -at));
           }
@@ -488,80 +542,116 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
           best = m;
         } else if constexpr (MODE == DLOGIT) {
           // rounded to bf16 as the tensor cores take it: 2^-9 of each term of the gradients' fp32 sums
-          uint32_t w[16];
+          const int at = label - col0;
 #pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            float2 d;
-            d.x = weight * (rows::ex2(fmaf(__uint_as_float(r[e]), LOG2E, -lse2)) - (label - col0 == e ? 1.f : 0.f));
-            d.y = weight * (rows::ex2(fmaf(__uint_as_float(r[e + 1]), LOG2E, -lse2)) - (label - col0 == e + 1 ? 1.f : 0.f));
-            if (row >= M) d = make_float2(0.f, 0.f);
-            w[e / 2] = rows::to_bf2(d);
+          for (int e = 0; e < 64; ++e) {
+            const float d = weight * (rows::ex2(fmaf(__uint_as_float(r[e]), LOG2E, -lse2)) - (at == e ? 1.f : 0.f));
+            r[e] = row < M ? __float_as_uint(d) : 0u;
           }
-          put_rows(stg, w, P.dl, P.ldd, row0, p.M, col0, p.N, true);
+          box_free(j);
+          put_box(buf, r, &P.map_dl, col0, row0);
         } else if constexpr (MODE == GRAD) {
           if (p.blocks) {
-            float* o = p.blocks + (((long)t.slice * ((p.M + 31) / 32) + row0 / 32) * ((p.N + 31) / 32) + col0 / 32) * 1024 + lane;
-            if (p.add) {
+            const int ncb = (p.N + 31) / 32;
+            float* o = p.blocks + (((long)t.slice * ((p.M + 31) / 32) + row0 / 32) * ncb + col0 / 32) * 1024 + lane;
+            const int n = min(2, ncb - col0 / 32);
 #pragma unroll
-              for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(o[32 * e] + __uint_as_float(r[e]));
-            }
+            for (int h = 0; h < 2; ++h)
+              if (h < n) {
+                if (p.add) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[32 * e] = __uint_as_float(r[e]);
+                  for (int e = 32 * h; e < 32 * h + 32; ++e)
+                    r[e] = __float_as_uint(o[32 * e] + __uint_as_float(r[e]));
+                }
+#pragma unroll
+                for (int e = 32 * h; e < 32 * h + 32; ++e) o[32 * e] = __uint_as_float(r[e]);
+              }
           } else {
-            uint32_t w[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-              w[e] = rows::to_bf2(make_float2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])));
-            put_rows(stg, w, (__nv_bfloat16*)p.out, p.ldo, row0, M, col0, p.N, p.vec);
+            box_free(j);
+            put_box(buf, r, &p.out, col0, row0);
           }
         } else {
-          // the columns' bias and scale, read by their lane and handed to all
-          const int col = col0 + lane;
-          __syncwarp();
-          prm[lane] = P.bias && col < p.N ? to_f32(P.bias[col]) : 0.f;
-          if (F8) prm[32 + lane] = col < p.N ? P.w_scale[col] : 0.f;
-          __syncwarp();
-          uint32_t w[16];
+          if (ahead && P.pre && j == 1) fetch(1);
+          // the columns' scale and bias, read by their lane and handed to all
           if (F8 || P.bias) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-              const float4 b = *(const float4*)(prm + e);
-              float4 s = make_float4(1.f, 1.f, 1.f, 1.f);
-              if (F8) {
-                s = *(const float4*)(prm + 32 + e);
-                s.x *= xs, s.y *= xs, s.z *= xs, s.w *= xs;
+            for (int h = 0; h < 2; ++h) {
+              const int col = col0 + 32 * h + lane;
+              __syncwarp();
+              prm_b[lane] = P.bias && col < p.N ? P.bias[col] : __float2bfloat16_rn(0.f);
+              if (F8) prm[lane] = col < p.N ? P.w_scale[col] : 0.f;
+              __syncwarp();
+#pragma unroll
+              for (int e = 0; e < 32; e += 4) {
+                const uint2 w = *(const uint2*)(prm_b + e);
+                const float2 b0 = rows::bf2(w.x), b1 = rows::bf2(w.y);
+                float4 s = make_float4(1.f, 1.f, 1.f, 1.f);
+                if (F8) {
+                  s = *(const float4*)(prm + e);
+                  s.x *= xs, s.y *= xs, s.z *= xs, s.w *= xs;
+                }
+                uint32_t* z = r + 32 * h + e;
+                z[0] = __float_as_uint(fmaf(__uint_as_float(z[0]), s.x, b0.x));
+                z[1] = __float_as_uint(fmaf(__uint_as_float(z[1]), s.y, b0.y));
+                z[2] = __float_as_uint(fmaf(__uint_as_float(z[2]), s.z, b1.x));
+                z[3] = __float_as_uint(fmaf(__uint_as_float(z[3]), s.w, b1.y));
               }
-              r[e] = __float_as_uint(fmaf(__uint_as_float(r[e]), s.x, b.x));
-              r[e + 1] = __float_as_uint(fmaf(__uint_as_float(r[e + 1]), s.y, b.y));
-              r[e + 2] = __float_as_uint(fmaf(__uint_as_float(r[e + 2]), s.z, b.z));
-              r[e + 3] = __float_as_uint(fmaf(__uint_as_float(r[e + 3]), s.w, b.w));
             }
           }
-          if (P.pre) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-              w[e] = rows::to_bf2(make_float2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])));
-            put_rows(stg, w, P.pre, P.ldp, row0, M, col0, p.N, P.vec_p);
+          if (P.pre) {  // through the other buffer
+            box_wait<0>();
+            if (P.tma_p) {
+              put_box(stg + (j ^ 1) * STG, r, &P.map_p, col0, row0);
+            } else {
+              for (int h = 0; h < 2; ++h)
+                put_rows(stg + (j ^ 1) * STG, r + 32 * h, P.pre, P.ldp, row0, M, col0 + 32 * h, p.N);
+            }
           }
-          activate(P.act, reinterpret_cast<float(&)[32]>(r));
+          activate(P.act, reinterpret_cast<float(&)[64]>(r));
           if (P.residual) {
-            get_rows(stg, w, P.residual, P.ldr, row0, M, col0, p.N, P.vec_r);
+            if (P.tma_r) {
+              int got = 1;
+              if (lane == 0)
+                got = mbar_wait(res + 8 * j, (res_turn >> j) & 1, nullptr, P.wait_cycles) ||
+                      mbar_wait(res + 8 * j, (res_turn >> j) & 1, nullptr, P.wait_cycles);
+              got = __shfl_sync(0xffffffffu, got, 0);
+              res_turn ^= 1u << j;
+              if (!got) {
+                ok = 0;
+                *lost = 1;
+              }
+              __syncwarp();
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float2 f = rows::bf2(w[e]);
-              r[2 * e] = __float_as_uint(__uint_as_float(r[2 * e]) + f.x);
-              r[2 * e + 1] = __float_as_uint(__uint_as_float(r[2 * e + 1]) + f.y);
+              for (int k = 0; k < 8; ++k) {
+                const uint4 v = *piece(buf, k);
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                  const float2 f = rows::bf2(w[u]);
+                  r[8 * k + 2 * u] = __float_as_uint(got ? __uint_as_float(r[8 * k + 2 * u]) + f.x : nan);
+                  r[8 * k + 2 * u + 1] = __float_as_uint(got ? __uint_as_float(r[8 * k + 2 * u + 1]) + f.y : nan);
+                }
+              }
+            } else {
+              box_wait<0>();
+#pragma unroll
+              for (int h = 0; h < 2; ++h) add_rows(buf, r + 32 * h, P.residual, P.ldr, row0, M, col0 + 32 * h, p.N);
             }
           }
+          if (P.tma_y) {
+            if (!P.pre && !ahead) box_free(j);  // (else the buffer has been waited for)
+            put_box(buf, r, &P.map_y, col0, row0);
+          } else {
+            box_wait<0>();
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            w[e] = rows::to_bf2(make_float2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])));
-          put_rows(stg, w, P.y, P.ldy, row0, M, col0, p.N, P.vec_y);
+            for (int h = 0; h < 2; ++h) put_rows(buf, r + 32 * h, P.y, P.ldy, row0, M, col0 + 32 * h, p.N);
+          }
         }
       }
       if (MODE == STATS && row < M && t.n0 + 128 * half < p.N)
         P.part[(long)(t.n0 / 128 + half) * P.part_ld + row] = make_float2(ok ? best : nan, total);
     }
+    if (lane == 0) bulk_wait_all();
   }
   __syncwarp();
   tc_fence_before();
@@ -576,6 +666,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
 // Operand along K: rows x K elements of es bytes, ld elements apart; along M / N: K rows
 inline bool operand(CUtensorMap* m, const void* base, long inner, long outer, long ld, int es, bool mn) {
   return encode_bytes_2d(m, base, inner * es, outer, ld * es, mn ? 64 : 128);
+}
+
+// bf16 rows written (or read) in boxes of 128 bytes x 32 rows, where TMA can
+inline bool boxes(CUtensorMap* m, const void* base, long cols, long rows_, long ld) {
+  return rows::aligned(base, 16) && ld % 8 == 0 && ld < (1L << 31) && encode_bytes_2d(m, base, 2 * cols, rows_, 2 * ld, 32);
 }
 
 inline long tiles_of(const Problem& p) {
