@@ -103,29 +103,8 @@ static __device__ __forceinline__ uint32_t cluster_rank() {
 static __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-static __device__ __forceinline__ bool try_wait_cluster(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-static __device__ __forceinline__ bool wait_cluster(uint32_t bar, uint32_t parity, volatile int* lost,
-                                                    unsigned long long limit) {
-  if (try_wait_cluster(bar, parity)) return true;
-  const unsigned long long t0 = clock64();
-  while (true) {
-    if (try_wait_cluster(bar, parity)) return true;
-    if (lost && *lost) return false;
-    if (clock64() - t0 > limit) return false;
-  }
-}
 static __device__ __forceinline__ void arrive_remote(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 static __device__ __forceinline__ void load_pair(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar) {
   asm volatile(
@@ -215,7 +194,7 @@ struct Tile {
 
 // Sizes of the launch's products, as the device counts bound them
 struct Sizes {
-  int M[2], mt[2], nt[2], kb[2], tiles[2];
+  int M[2], mt[2], nt[2], kb[2], per[2], tiles[2];
   template <bool F8>
   __device__ void read(const Launch& P) {
 #pragma unroll
@@ -229,6 +208,7 @@ struct Sizes {
       nt[i] = (p.N + BN - 1) / BN;
       kb[i] = F8 ? (K + 127) / 128 : (K + 63) / 64;
       tiles[i] = mt[i] * nt[i] * p.slices;
+      per[i] = (kb[i] + p.slices - 1) / p.slices;
     }
   }
   __device__ bool at(const Launch& P, int i, Tile& t) const {
@@ -239,16 +219,16 @@ struct Sizes {
       if (i >= tiles[1]) return false;
     }
     const int m_n = t.p ? mt[1] : mt[0], n_n = t.p ? nt[1] : nt[0], kbs = t.p ? kb[1] : kb[0];
-    const int slices = P.p[t.p].slices;
+    const int run = t.p ? per[1] : per[0];
     t.slice = i / (m_n * n_n);
     i -= t.slice * m_n * n_n;
     const int g = i / (GROUP_M * n_n), gm = min(GROUP_M, m_n - g * GROUP_M);
     i -= g * GROUP_M * n_n;
-    t.m0 = (g * GROUP_M + i % gm) * BM;
-    t.n0 = i / gm * BN;
-    const int per = (kbs + slices - 1) / slices;
-    t.kb0 = t.slice * per;
-    t.nkb = max(0, min(per, kbs - t.kb0));
+    const int n = gm == GROUP_M ? i / GROUP_M : i / gm;
+    t.m0 = (g * GROUP_M + i - n * gm) * BM;
+    t.n0 = n * BN;
+    t.kb0 = t.slice * run;
+    t.nkb = max(0, min(run, kbs - t.kb0));
     return true;
   }
 };
@@ -376,7 +356,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
         const int m = t.m0 + 128 * (int)rank, n = t.n0 + 128 * (int)rank;
         for (int k = 0; k < t.nkb; ++k, ++it) {
           const uint32_t s = it % STAGES;
-          if (!wait_cluster(empty0 + 8 * s, ((it / STAGES) & 1) ^ 1, lost, P.wait_cycles)) {
+          if (!mbar_wait(empty0 + 8 * s, ((it / STAGES) & 1) ^ 1, lost, P.wait_cycles)) {
             ok = false;
             break;
           }
@@ -399,30 +379,30 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
       }
       // the commits of the last stages have arrived before the CTA may end
       for (uint32_t j = it > STAGES ? it - STAGES : 0; ok && j < it; ++j)
-        ok = wait_cluster(empty0 + 8 * (j % STAGES), (j / STAGES) & 1, lost, P.wait_cycles);
+        ok = mbar_wait(empty0 + 8 * (j % STAGES), (j / STAGES) & 1, lost, P.wait_cycles);
       if (!ok) {
         *lost = 1;
         // copies in flight land before shared memory goes away (both CTAs': the even one's
         // barriers count them)
         if (rank == 0)
           for (uint32_t j = it > STAGES ? it - STAGES : 0; j < it; ++j)
-            wait_cluster(full0 + 8 * (j % STAGES), (j / STAGES) & 1, nullptr, P.wait_cycles);
+            mbar_wait(full0 + 8 * (j % STAGES), (j / STAGES) & 1, nullptr, P.wait_cycles);
       }
     }
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
       uint32_t it = 0, nt = 0;
-      bool ok = !P.unmet || wait_cluster(drain, 0, lost, P.wait_cycles);
+      bool ok = !P.unmet || mbar_wait(drain, 0, lost, P.wait_cycles);
       for (int i = pair; ok && S.at(P, i, t); i += pairs) {
         if (t.nkb == 0) continue;
         const Problem& p = P.p[t.p];
         const uint32_t id = idesc(F8, p.a_mn, p.b_mn, BM, BN), acc = nt & 1, d = tmem + acc * BN;
-        ok = wait_cluster(tempty0 + 8 * acc, ((nt >> 1) & 1) ^ 1, lost, P.wait_cycles);
+        ok = mbar_wait(tempty0 + 8 * acc, ((nt >> 1) & 1) ^ 1, lost, P.wait_cycles);
         if (!ok) break;
         tc_fence_after();
         for (int k = 0; k < t.nkb; ++k, ++it) {
           const uint32_t s = it % STAGES;
-          if (!wait_cluster(full0 + 8 * s, (it / STAGES) & 1, lost, P.wait_cycles)) {
+          if (!mbar_wait(full0 + 8 * s, (it / STAGES) & 1, lost, P.wait_cycles)) {
             ok = false;
             break;
           }
@@ -443,7 +423,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
       if (!ok) {
         *lost = 1;
         commit_pair(drain, 1);  // no product is in flight when TMEM is freed
-        wait_cluster(drain, 0, nullptr, P.wait_cycles);
+        mbar_wait(drain, 0, nullptr, P.wait_cycles);
       }
     }
   } else if (warp >= 4) {
@@ -484,7 +464,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
       }
       if (t.nkb > 0) {
         if (ok && lane == 0) {
-          ok = wait_cluster(tfull0 + 8 * acc, (nt >> 1) & 1, lost, P.wait_cycles) ? 1 : 0;
+          ok = mbar_wait(tfull0 + 8 * acc, (nt >> 1) & 1, lost, P.wait_cycles) ? 1 : 0;
           if (!ok) *lost = 1;
         }
         ok = __shfl_sync(0xffffffffu, ok, 0);
