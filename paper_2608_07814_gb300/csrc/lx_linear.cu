@@ -255,6 +255,17 @@ struct DzArgs {
   float* part;           // [CTAs of rows][N], or NULL
 };
 
+// The normal distribution's function at z, and exp(-z^2 / 2) (see gelu2)
+__device__ __forceinline__ float normal_cdf(float z, float& e) {
+  const float t = rcp(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
+  e = ex2(-0.5f * LOG2E * z * z);
+  float p = fmaf(1.061405429f, t, -1.453152027f);
+  p = fmaf(p, t, 1.421413741f);
+  p = fmaf(p, t, -0.284496736f);
+  p = fmaf(p, t, 0.254829592f);
+  const float c = 0.5f * p * t * e;
+  return z > 0.f ? 1.f - c : c;
+}
 // d times the activation's derivative
 template <int ACT>
 __device__ __forceinline__ float through(float d, float z) {

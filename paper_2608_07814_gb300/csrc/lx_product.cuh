@@ -155,36 +155,46 @@ __device__ __forceinline__ float rcp(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// The normal distribution's function at z, and exp(-z^2 / 2): the complementary error function by
-// Abramowitz and Stegun 7.1.26 (1.5e-7 at most, a 2^-15 of bf16's step; with erff an epilogue
-// took as long as 2500 inputs' products).
-__device__ __forceinline__ float normal_cdf(float z, float& e) {
-  const float t = rcp(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
-  e = rows::ex2(-0.5f * LOG2E * z * z);
-  float p = fmaf(1.061405429f, t, -1.453152027f);
-  p = fmaf(p, t, 1.421413741f);
-  p = fmaf(p, t, -0.284496736f);
-  p = fmaf(p, t, 0.254829592f);
-  const float c = 0.5f * p * t * e;
-  return z > 0.f ? 1.f - c : c;
+// The complementary error function by Abramowitz and Stegun 7.1.26: a polynomial in t = 1 / (1 + p x)
+// times exp(-x^2), 1.5e-7 off at most, a 2^-15 of bf16's step.  (With erff the epilogue took as
+// long as 2500 inputs' products.)
+// (a NaN stays one)
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
 }
-__device__ __forceinline__ float relu(float z) { return z < 0.f ? 0.f : z; }
 __device__ __forceinline__ float silu(float z) { return z * rcp(1.f + rows::ex2(-LOG2E * z)); }
-__device__ __forceinline__ float gelu(float z) {
-  float e;
-  return z * normal_cdf(z, e);
+// relu(z) - |z| times the function's tail, in pairs: 9 instructions a value, which bound the epilogue
+// of 8-bit products of 2048 inputs.  |z| is held below 100, where the tail is 0.
+__device__ __forceinline__ float2 gelu2(float2 z) {
+  using rows::both;
+  const float2 a = make_float2(fminf(fabsf(z.x), 100.f), fminf(fabsf(z.y), 100.f));
+  const float2 q = rows::fma2(a, both(0.3275911f * 0.70710678f), both(1.f));
+  const float2 t = make_float2(rcp(q.x), rcp(q.y));
+  const float2 s = rows::mul2(rows::mul2(a, a), both(-0.5f * LOG2E));
+  const float2 e = make_float2(rows::ex2(s.x), rows::ex2(s.y));
+  float2 p = rows::fma2(both(0.5f * 1.061405429f), t, both(0.5f * -1.453152027f));
+  p = rows::fma2(p, t, both(0.5f * 1.421413741f));
+  p = rows::fma2(p, t, both(0.5f * -0.284496736f));
+  p = rows::fma2(p, t, both(0.5f * 0.254829592f));
+  p = rows::mul2(rows::mul2(p, t), e);
+  return rows::fma2(make_float2(-a.x, -a.y), p, make_float2(max_nan(z.x, 0.f), max_nan(z.y, 0.f)));
 }
 template <int N>
 __device__ __forceinline__ void activate(int act, float (&v)[N]) {
   if (act == RELU) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = relu(v[i]);
+    for (int i = 0; i < N; ++i) v[i] = max_nan(v[i], 0.f);
   } else if (act == SILU) {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = silu(v[i]);
   } else if (act == GELU) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = gelu(v[i]);
+    for (int i = 0; i < N; i += 2) {
+      const float2 y = gelu2(make_float2(v[i], v[i + 1]));
+      v[i] = y.x, v[i + 1] = y.y;
+    }
   }
 }
 
@@ -462,6 +472,22 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
         if (t.n0 + 128 * half < p.N) fetch(0);
         if (!P.pre && t.n0 + 128 * half + 64 < p.N) fetch(1);
       }
+      // what the tile needs besides its sums, on the way while those are formed: the row's, and
+      // the scales and biases of the columns 32 h + lane
+      int label = -1;
+      float weight = 0.f, lse2 = 0.f, xs = 1.f, col_s[4];
+      __nv_bfloat16 col_b[4];
+      if (MODE == DLOGIT && row < M) label = P.label[row] - P.v0, weight = P.weight[row], lse2 = P.lse2[row];
+      if (MODE == LINEAR) {
+        if (F8 && row < M) xs = P.x_scale[row];
+        if (F8 || P.bias)
+#pragma unroll
+          for (int h = 0; h < 4; ++h) {
+            const int col = t.n0 + 128 * half + 32 * h + lane;
+            col_b[h] = P.bias && col < p.N ? P.bias[col] : __float2bfloat16_rn(0.f);
+            if (F8) col_s[h] = col < p.N ? P.w_scale[col] : 0.f;
+          }
+      }
       if (t.nkb > 0) {
         if (ok && lane == 0) {
           ok = mbar_wait(tfull0 + 8 * acc, (nt >> 1) & 1, lost, P.wait_cycles) ? 1 : 0;
@@ -472,10 +498,6 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
         ++nt;
       }
       float best = -INFINITY, total = 0.f;  // STATS
-      int label = -1;
-      float weight = 0.f, lse2 = 0.f, xs = 1.f;
-      if (MODE == DLOGIT && row < M) label = P.label[row] - P.v0, weight = P.weight[row], lse2 = P.lse2[row];
-      if (MODE == LINEAR && F8) xs = row < M ? P.x_scale[row] : 0.f;
 #pragma unroll 1
       for (int j = 0; j < 2; ++j) {
         const int col0 = t.n0 + 128 * half + 64 * j;
@@ -552,14 +574,13 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
           }
         } else {
           if (ahead && P.pre && j == 1) fetch(1);
-          // the columns' scale and bias, read by their lane and handed to all
+          // the columns' scale and bias, handed to all lanes
           if (F8 || P.bias) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const int col = col0 + 32 * h + lane;
               __syncwarp();
-              prm_b[lane] = P.bias && col < p.N ? P.bias[col] : __float2bfloat16_rn(0.f);
-              if (F8) prm[lane] = col < p.N ? P.w_scale[col] : 0.f;
+              prm_b[lane] = j ? col_b[2 + h] : col_b[h];
+              if (F8) prm[lane] = j ? col_s[2 + h] : col_s[h];
               __syncwarp();
 #pragma unroll
               for (int e = 0; e < 32; e += 4) {
