@@ -41,8 +41,6 @@ struct Head {
   float *weight, *lse2, *label_logit;
   const float2* part;
   int slots;
-  const float* blocks;  // of dh
-  int slices;
   const float* keep;    // the logits, keep_cols blocks side by side
   int keep_cols;
   __nv_bfloat16* dl;
@@ -57,6 +55,7 @@ struct Head {
 __global__ void __launch_bounds__(256) k_head_rows(const __grid_constant__ Head A) {
   __shared__ int red[2][8];
   __shared__ int live[ROWS];
+  pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t0 = blockIdx.x * ROWS, t = t0 + warp;
   // the warp's row and its label's row of W, while the rows are counted
   const int pieces = A.H / 8, label = t < A.T ? A.labels[t] : -1;
@@ -121,6 +120,7 @@ __global__ void __launch_bounds__(256) k_head_rows(const __grid_constant__ Head 
 // 32 warps a CTA side by side over the partial sums, added in the warps' order.
 __global__ void __launch_bounds__(1024) k_head_lse(const __grid_constant__ Head A) {
   __shared__ float2 red[32][33];
+  pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.x * 32 + lane, n = *A.n;
   if (blockIdx.x * 32 >= n) return;
   // the sums of eight more parts, all taken to the largest value first
@@ -185,6 +185,7 @@ __device__ __forceinline__ void put_block(char* stg, const float (&v)[32], __nv_
 // takes whole blocks)
 __global__ void __launch_bounds__(256) k_head_dz(const __grid_constant__ Head A) {
   __shared__ __align__(16) char stage[8][32 * STG_LD];
+  pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = *A.n;
   const int rb = blockIdx.y, cb = blockIdx.x * 8 + warp, row = rb * 32 + lane;
   if (rb * 32 >= (n + 63) / 64 * 64 || cb >= A.keep_cols) return;
@@ -201,27 +202,6 @@ __global__ void __launch_bounds__(256) k_head_dz(const __grid_constant__ Head A)
   for (int e = 0; e < 32; ++e)
     v[e] = on ? weight * (ex2(fmaf(v[e], LOG2E, -lse2)) - (label == e ? 1.f : 0.f)) : 0.f;
   put_block(stage[warp], v, A.dl, A.ldd, 32 * cb, 32 * A.keep_cols, [&](int r) { return (long)rb * 32 + r; });
-}
-
-// dh from its fp32 blocks: the slices in their order, rounded once, each row to its place.  A CTA a
-// block, a warp four of its columns.
-__global__ void __launch_bounds__(256) k_head_dh(const __grid_constant__ Head A) {
-  __shared__ __nv_bfloat16 stage[32][40];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = *A.n;
-  const int rb = blockIdx.x, cb = blockIdx.y, ncb = gridDim.y, nrb = A.Tp / 32;
-  if (rb * 32 >= n) return;
-  float v[4] = {0.f, 0.f, 0.f, 0.f};
-  const float* b = A.blocks + ((long)rb * ncb + cb) * 1024 + 128 * warp + lane;
-#pragma unroll 4
-  for (int s = 0; s < A.slices; ++s) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] += b[(long)s * nrb * ncb * 1024 + 32 * e];
-  }
-  *(uint2*)&stage[lane][4 * warp] = make_uint2(to_bf2(make_float2(v[0], v[1])), to_bf2(make_float2(v[2], v[3])));
-  __syncthreads();
-  const int r = threadIdx.x / 4, c = 8 * (threadIdx.x % 4);
-  if (threadIdx.x < 128 && rb * 32 + r < n && cb * 32 + c < A.H)
-    *(uint4*)(A.dh + (long)A.row[rb * 32 + r] * A.H + cb * 32 + c) = *(const uint4*)&stage[r][c];
 }
 
 size_t al(size_t v) { return (v + 255) / 256 * 256; }
@@ -242,7 +222,7 @@ Plan plan_of(int T, int V, int H, bool dh, bool dw) {
   p.piece = std::min(nt * BN, std::max(1L, PIECE_BYTES / (2 * p.Tp * BN)) * BN);
   // few tiles of dh: ranges of the vocabulary side by side, so that every pair of SMs has one
   const long tiles = p.Tp / BM * (((long)H + BN - 1) / BN);
-  p.slices = (int)std::max(1L, std::min(std::min(16L, (long)(SMS / 2) / tiles), p.piece / 512));
+  p.slices = (int)std::max(1L, std::min((long)MAX_SLICES, (long)(SMS / 2) / tiles));
   size_t at = 0;
   auto take = [&](size_t n) {
     const size_t v = at;
@@ -264,7 +244,7 @@ Plan plan_of(int T, int V, int H, bool dh, bool dw) {
       p.keep = take(4 * (size_t)p.Tp * nt * BN);
     }
   }
-  if (dh) p.blocks = take(4 * (size_t)p.slices * (p.Tp / 32) * ((H + 31) / 32) * 1024);
+  if (dh) p.blocks = take(4 * block_floats(p.Tp, H, p.slices));
   p.bytes = at;
   return p;
 }
@@ -342,8 +322,6 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
   A.label_logit = (float*)(ws + L.label_logit);
   A.part = (const float2*)(ws + L.part);
   A.slots = L.slots;
-  A.blocks = (const float*)(ws + L.blocks);
-  A.slices = L.slices;
   A.keep = (const float*)(ws + L.keep);
   A.keep_cols = L.keep_cols;
   A.dl = (__nv_bfloat16*)(ws + L.dl);
@@ -369,8 +347,7 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
   if (!operand(&p.a, A.hc, H, L.Tp, H, 2, false) || !operand(&p.b, w, H, V, ldw, 2, false))
     return fail(LX_ERR_CUDA, "cuTensorMapEncodeTiled(head) failed");
   LX_TRY((launch_product<STATS, false>(P, st)));
-  k_head_lse<<<(unsigned)(L.Tp / 32), 1024, 0, st>>>(A);
-  LX_CUDA(cudaGetLastError());
+  LX_TRY(launch_after(k_head_lse, dim3((unsigned)(L.Tp / 32)), dim3(1024), 0, 1, st, A));
   if (!dh && !dw) return LX_OK;
 
   Launch G = {};
@@ -379,40 +356,42 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
     const long n = std::min<long>(L.piece, V - v0);
     const __nv_bfloat16* wp = (const __nv_bfloat16*)w + v0 * ldw;
     if (L.keep_cols) {  // (one piece)
-      k_head_dz<<<dim3((L.keep_cols + 7) / 8, (unsigned)(L.Tp / 32)), 256, 0, st>>>(A);
-      LX_CUDA(cudaGetLastError());
+      LX_TRY(launch_after(k_head_dz, dim3((L.keep_cols + 7) / 8, (unsigned)(L.Tp / 32)), dim3(256), 0, 1, st, A));
     } else {
       P.v0 = (int)v0;
       p.N = (int)((n + 31) / 32 * 32);  // (whole blocks of dz; those behind the vocabulary are not read)
       if (!operand(&p.b, wp, H, n, ldw, 2, false) || !boxes(&P.map_dl, A.dl, L.piece, L.Tp, L.piece)) return fail(LX_ERR_CUDA, "cuTensorMapEncodeTiled(head) failed");
       LX_TRY((launch_product<DLOGIT, false>(P, st)));
     }
+    // the gradient with the longer sums first
     G.n = 0;
     bool ok = true;
-    if (dh) {
+    for (int i = 0; i < 2; ++i) {
+      const bool of_h = (n >= T) == (i == 0);
+      if (!(of_h ? dh : dw)) continue;
       Problem& g = G.p[G.n++];
       g = Problem{};
-      g.M = (int)L.Tp, g.N = H, g.K = (int)n, g.slices = L.slices;
       g.b_mn = 1;
-      g.rows = A.n;
-      g.blocks = (float*)(ws + L.blocks);
-      g.add = v0 > 0;
-      ok = ok && operand(&g.a, A.dl, n, L.Tp, L.piece, 2, false) && operand(&g.b, wp, H, n, ldw, 2, true);
-    }
-    if (dw) {
-      Problem& g = G.p[G.n++];
-      g = Problem{};
-      g.M = (int)n, g.N = H, g.K = (int)L.Tp, g.slices = 1;
-      g.a_mn = g.b_mn = 1;
-      g.depth = A.n;
-      ok = ok && boxes(&g.out, (__nv_bfloat16*)dw + v0 * H, H, n, H) && operand(&g.a, A.dl, n, L.Tp, L.piece, 2, true) && operand(&g.b, A.hc, H, L.Tp, H, 2, true);
+      if (of_h) {
+        g.M = (int)L.Tp, g.N = H, g.K = (int)n, g.slices = L.slices;
+        g.rows = A.n;
+        g.blocks = (float*)(ws + L.blocks);
+        g.add = v0 > 0;
+        ok = ok && operand(&g.a, A.dl, n, L.Tp, L.piece, 2, false) && operand(&g.b, wp, H, n, ldw, 2, true);
+      } else {
+        g.M = (int)n, g.N = H, g.K = (int)L.Tp, g.slices = 1;
+        g.a_mn = 1;
+        g.depth = A.n;
+        ok = ok && boxes(&g.out, (__nv_bfloat16*)dw + v0 * H, H, n, H) &&
+             operand(&g.a, A.dl, n, L.Tp, L.piece, 2, true) && operand(&g.b, A.hc, H, L.Tp, H, 2, true);
+      }
     }
     if (!ok) return fail(LX_ERR_CUDA, "cuTensorMapEncodeTiled(head) failed");
     LX_TRY((launch_product<GRAD, false>(G, st)));
   }
   if (dh) {
-    k_head_dh<<<dim3((unsigned)(L.Tp / 32), (H + 31) / 32), 256, 0, st>>>(A);
-    LX_CUDA(cudaGetLastError());
+    const Join J = {(const float*)(ws + L.blocks), (int)L.Tp, H, L.slices, A.n, A.row, A.dh};
+    LX_TRY(launch_join(J, st));
   }
   return LX_OK;
 }

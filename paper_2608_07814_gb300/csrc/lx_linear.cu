@@ -218,16 +218,18 @@ lx_status launch_few(Few& P, int tb, int es, const lx_linear_desc* d, cudaStream
       !encode_bytes_2d(&P.x, d->x, (long)d->K * es, d->T, d->ldx * es, P.tn))
     return fail(LX_ERR_CUDA, "cuTensorMapEncodeTiled(linear) failed");
   const int stage = A_BYTES + P.tn * KB;
-  // Two CTAs an SM up to 128 tokens (100 KiB each; with 256 columns of TMEM at most, so that
-  // neither waits for the other's), one above.
-  const int budget = P.tn <= 128 ? 100 * 1024 : 192 * 1024, per_sm = P.tn <= 128 ? 2 : 1;
-  P.stages = std::min(16, budget / stage);
+  // Two CTAs an SM up to 128 tokens (108 KiB each; with 128 columns of TMEM at most, so that
+  // neither waits for the other's), one above.  (200 KiB for 128 CTAs or fewer: 64 tokens of 2048 x 8192
+  // in 8 bits 15.8 us instead of 9.9, as clusters of eight then need eight free SMs of a GPC.)
+  const int per_sm = P.tn <= 128 ? 2 : 1;
   P.cols = 32;
   while (P.cols < P.tn) P.cols *= 2;
   const int nt = (d->N + 127) / 128;
   int splits = 1;
   while (splits < FEW_SPLIT && (long)nt * tb * splits * 2 <= (long)SMS * per_sm && P.nkb >= 8 * splits) splits *= 2;
   P.per = (P.nkb + splits - 1) / splits;
+  const int budget = per_sm == 1 ? 200 * 1024 : 108 * 1024;
+  P.stages = std::min(16, budget / stage);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(splits, nt, tb);
   cfg.blockDim = dim3(FEW_THREADS);
@@ -255,29 +257,30 @@ struct DzArgs {
   float* part;           // [CTAs of rows][N], or NULL
 };
 
-// The normal distribution's function at z, and exp(-z^2 / 2) (see gelu2)
-__device__ __forceinline__ float normal_cdf(float z, float& e) {
-  const float t = rcp(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
-  e = ex2(-0.5f * LOG2E * z * z);
-  float p = fmaf(1.061405429f, t, -1.453152027f);
-  p = fmaf(p, t, 1.421413741f);
-  p = fmaf(p, t, -0.284496736f);
-  p = fmaf(p, t, 0.254829592f);
-  const float c = 0.5f * p * t * e;
-  return z > 0.f ? 1.f - c : c;
-}
-// d times the activation's derivative
+// d times the activation's derivative, in pairs (gelu: see gelu2)
 template <int ACT>
-__device__ __forceinline__ float through(float d, float z) {
-  if (ACT == RELU) return z > 0.f ? d : d * 0.f;
+__device__ __forceinline__ float2 through(float2 d, float2 z) {
+  const float2 one = both(1.f);
+  if (ACT == RELU) return make_float2(z.x > 0.f ? d.x : d.x * 0.f, z.y > 0.f ? d.y : d.y * 0.f);
   if (ACT == SILU) {
-    const float s = rcp(1.f + ex2(-LOG2E * z));
-    return d * (s * fmaf(z, 1.f - s, 1.f));
+    const float2 a = mul2(z, both(-LOG2E));
+    const float2 q = add2(make_float2(ex2(a.x), ex2(a.y)), one);
+    const float2 s = make_float2(rcp(q.x), rcp(q.y));
+    return mul2(d, mul2(s, fma2(z, fma2(s, both(-1.f), one), one)));
   }
   if (ACT == GELU) {
-    float e;
-    const float cdf = normal_cdf(z, e);
-    return d * fmaf(z * 0.3989422804014327f, e, cdf);
+    const float2 a = make_float2(fminf(fabsf(z.x), 100.f), fminf(fabsf(z.y), 100.f));
+    const float2 q = fma2(a, both(0.3275911f * 0.70710678f), one);
+    const float2 t = make_float2(rcp(q.x), rcp(q.y));
+    const float2 s = mul2(mul2(a, a), both(-0.5f * LOG2E));
+    const float2 e = make_float2(ex2(s.x), ex2(s.y));
+    float2 p = fma2(both(-0.5f * 1.061405429f), t, both(0.5f * 1.453152027f));
+    p = fma2(p, t, both(-0.5f * 1.421413741f));
+    p = fma2(p, t, both(0.5f * 0.284496736f));
+    p = fma2(p, t, both(-0.5f * 0.254829592f));
+    p = fma2(mul2(p, t), e, both(0.5f));  // half the probability of (-|z|, |z|)
+    const float2 cdf = add2(make_float2(copysignf(p.x, z.x), copysignf(p.y, z.y)), both(0.5f));
+    return mul2(d, fma2(mul2(z, both(0.3989422804014327f)), e, cdf));
   }
   return d;
 }
@@ -287,6 +290,7 @@ __device__ __forceinline__ float through(float d, float z) {
 // ahead.
 template <int VEC, int ACT>
 __global__ void __launch_bounds__(256, 4) k_linear_dz(const __grid_constant__ DzArgs A) {
+  pdl_wait();
   __shared__ float sums[8][32 * VEC];
   constexpr int W = VEC == 8 ? 4 : 1;  // words of a piece
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -319,13 +323,13 @@ __global__ void __launch_bounds__(256, 4) k_linear_dz(const __grid_constant__ Dz
         if (r0 + 8 * i < n) {
           float d[VEC];
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) {
-            auto at = [e](const uint32_t (&w)[W]) {
-              return VEC == 8 && (e & 1) ? __uint_as_float(w[e / 2] & 0xffff0000u) : __uint_as_float(w[e / 2] << 16);
-            };
-            d[e] = through<ACT>(at(a[i]), ACT != NONE ? at(b[i]) : 0.f);
-            s[e] += d[e];
+          for (int e = 0; e < VEC; e += 2) {
+            const float2 v = through<ACT>(bf2(a[i][e / 2]), ACT != NONE ? bf2(b[i][e / 2]) : make_float2(0.f, 0.f));
+            d[e] = v.x;
+            if constexpr (VEC > 1) d[e + 1] = v.y;
           }
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) s[e] += d[e];
           if (A.dz) store<__nv_bfloat16, VEC>(A.dz + (t0 + r0 + 8 * i) * A.ldz + col, d);
         }
     }
@@ -355,6 +359,7 @@ void launch_dz(const DzArgs& A, dim3 grid, cudaStream_t st) {
 // the CTAs' sums in their order: 8 ranges of them side by side, then those
 __global__ void __launch_bounds__(256) k_linear_db(const float* part, int chunks, int N, __nv_bfloat16* db) {
   __shared__ float sums[8][32];
+  pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
   const int per = (chunks + 7) / 8;
   float v = 0.f;
@@ -379,6 +384,16 @@ int dz_chunk(int T, int N) {
 }
 int dz_chunks(int T, int N) { return (int)(((long)T + dz_chunk(T, N) - 1) / dz_chunk(T, N)); }
 size_t al(size_t v) { return (v + 255) / 256 * 256; }
+// ranges of K of a product of M x N outputs: few tiles of long sums are cut, so that every pair of
+// SMs has one, into ranges of 2048 at least
+int grad_slices(long M, long N, long K) {
+  const long tiles = ((M + BM - 1) / BM) * ((N + BN - 1) / BN);
+  return (int)std::max(1L, std::min(std::min((long)MAX_SLICES, (long)(SMS / 2) / tiles), K / 2048));
+}
+size_t grad_blocks(long M, long N, long K) {
+  const int s = grad_slices(M, N, K);
+  return s > 1 ? al(4 * block_floats(M, N, s)) : 0;
+}
 long dz_ld(int N) { return ((long)N + 7) / 8 * 8; }
 
 constexpr int MAX_T = 1 << 30, MAX_DIM = 1 << 24;
@@ -484,7 +499,9 @@ extern "C" lx_status lx_linear_workspace(int32_t T, int32_t N, int32_t K, uint64
   using namespace lx;
   if (!bytes) return fail(LX_ERR_ARG, "bytes is NULL");
   LX_TRY(check_sizes(T, N, K, LX_BF16));
-  *bytes = T == 0 ? 0 : al(2 * (size_t)T * dz_ld(N)) + al(4 * (size_t)dz_chunks(T, N) * N);
+  *bytes = T == 0 ? 0
+                  : al(2 * (size_t)T * dz_ld(N)) + al(4 * (size_t)dz_chunks(T, N) * N) + grad_blocks(T, K, N) +
+                        grad_blocks(N, K, T);
   return LX_OK;
 }
 
@@ -535,8 +552,10 @@ extern "C" lx_status lx_linear_backward(const lx_linear_desc* d, const void* dy,
     const bool vec = N % 8 == 0 && lddy % 8 == 0 && aligned(dy, 16) && aligned(pre, 16);
     if (vec) launch_dz<8>(A, dim3((N + 255) / 256, chunks), st);
     else launch_dz<1>(A, dim3((N + 31) / 32, chunks), st);
-    if (dbias) k_linear_db<<<(N + 31) / 32, 256, 0, st>>>(part, chunks, N, (__nv_bfloat16*)dbias);
     LX_CUDA(cudaGetLastError());
+    if (dbias)
+      LX_TRY(launch_after(k_linear_db, dim3((N + 31) / 32), dim3(256), 0, 1, st, (const float*)part, chunks, N,
+                          (__nv_bfloat16*)dbias));
   }
   if (!dx && !dw) return LX_OK;
   const void* g = direct ? dy : dz;
@@ -545,22 +564,36 @@ extern "C" lx_status lx_linear_backward(const lx_linear_desc* d, const void* dy,
   P.wait_cycles = waits.cycles;
   P.unmet = waits.unmet == LX_WAIT_CALL_PRODUCT;
   bool ok = true;
+  Join joins[2];
+  int n_joins = 0;
+  float* blocks = (float*)((char*)part + al(4 * (size_t)chunks * N));
+  // out by TMA, or its ranges' sums into the workspace, to be joined
+  auto target = [&](Problem& p, void* out) {
+    p.slices = grad_slices(p.M, p.N, p.K);
+    if (p.slices == 1) return boxes(&p.out, out, p.N, p.M, p.N);
+    p.blocks = blocks;
+    joins[n_joins++] = Join{blocks, p.M, p.N, p.slices, nullptr, nullptr, (__nv_bfloat16*)out};
+    blocks += grad_blocks(p.M, p.N, p.K) / 4;
+    return true;
+  };
   // the product with the longer sums first: the shorter tiles even out the SMs' ends
   for (int i = 0; i < 2; ++i) {
     if ((N >= T) == (i == 0)) {
       if (!dx) continue;
       Problem& p = P.p[P.n++];
-      p.M = T, p.N = K, p.K = N, p.slices = 1;
+      p.M = T, p.N = K, p.K = N;
       p.b_mn = 1;
-      ok = ok && boxes(&p.out, dx, K, T, K) && operand(&p.a, g, N, T, ldg, 2, false) && operand(&p.b, d->w, K, N, d->ldw, 2, true);
+      ok = ok && target(p, dx) && operand(&p.a, g, N, T, ldg, 2, false) && operand(&p.b, d->w, K, N, d->ldw, 2, true);
     } else {
       if (!dw) continue;
       Problem& p = P.p[P.n++];
-      p.M = N, p.N = K, p.K = T, p.slices = 1;
+      p.M = N, p.N = K, p.K = T;
       p.a_mn = p.b_mn = 1;
-      ok = ok && boxes(&p.out, dw, K, N, K) && operand(&p.a, g, N, T, ldg, 2, true) && operand(&p.b, d->x, K, T, d->ldx, 2, true);
+      ok = ok && target(p, dw) && operand(&p.a, g, N, T, ldg, 2, true) && operand(&p.b, d->x, K, T, d->ldx, 2, true);
     }
   }
   if (!ok) return fail(LX_ERR_CUDA, "cuTensorMapEncodeTiled(linear gradients) failed");
-  return launch_product<GRAD, false>(P, st);
+  LX_TRY((launch_product<GRAD, false>(P, st)));
+  for (int i = 0; i < n_joins; ++i) LX_TRY(launch_join(joins[i], st));
+  return LX_OK;
 }

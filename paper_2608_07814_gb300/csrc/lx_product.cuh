@@ -46,7 +46,8 @@ constexpr int STG = 4096, PRM = 192;
 constexpr int STG_LD = 80;             // rows TMA cannot take: 32 bf16, 16-byte pieces of 8 rows on distinct banks
 constexpr int N_BARS = 2 * STAGES + 5 + 2 * EPI;
 constexpr int SMEM = STAGES * STAGE + EPI * (2 * STG + PRM) + 8 * N_BARS + 16 + 1024;
-constexpr int GROUP_M = 8;
+constexpr int GROUP_M = 8, MAX_SLICES = 16;
+constexpr int LEAVING = 5;  // blocks of K whose products take as long as a tile's way out (1.9 us)
 static_assert(SMEM <= 227 * 1024, "fits an SM");
 
 enum Mode { LINEAR = 0, STATS = 1, DLOGIT = 2, GRAD = 3 };
@@ -57,12 +58,12 @@ struct Problem {
   CUtensorMap a, b;  // maps of bytes: 128 x 128 boxes of an operand along K, 128 x 64 of one along M / N
   int a_mn, b_mn;    // stored along M / N
   int M, N, K;       // K in elements
-  int slices;
+  int slices;        // ranges of K side by side (into blocks, with `rows`: as slices_of has them)
   const int* rows;   // device count that bounds M (NULL: M), and
   const int* depth;  // one that bounds K
   // GRAD: bf16 (boxes of 128 bytes x 32 rows), or fp32 in blocks of 32 x 32, slice by slice
   CUtensorMap out;
-  float* blocks;
+  float* blocks;     // [slice][rows of tiles x 8][blocks of columns], a block's columns of 32 rows
   int add;           // to what the blocks hold
 };
 
@@ -202,30 +203,57 @@ struct Tile {
   int p, m0, n0, slice, kb0, nkb;
 };
 
-// Sizes of the launch's products, as the device counts bound them
+// Ranges of K of a product whose M is known on the device alone: as many more as there are
+// fewer rows of tiles, in the same room
+__host__ __device__ inline int slices_of(int slices, int M, int live) {
+  const int mt = (M + BM - 1) / BM, lt = (live + BM - 1) / BM;
+  const int n = lt > 0 ? slices * mt / lt : slices;
+  return n < MAX_SLICES ? n : (slices > MAX_SLICES ? slices : MAX_SLICES);
+}
+
+// Sizes of the launch's products, as the device counts bound them, and the deal of their tiles:
+// the first product's (whose sums are the longer) go round the pairs; the pairs that have one
+// fewer are given `extra` of the second's, as many as take its time; the others go round again,
+// from the last pair to the first.  (A plain round of both left 12 % of the pairs' time unused in
+// the head's gradients of 4096 rows.)
 struct Sizes {
   int M[2], mt[2], nt[2], kb[2], per[2], tiles[2];
+  int pair, pairs, rest, extra, dealt;  // rest: pairs with one more of the first
   template <bool F8>
   __device__ void read(const Launch& P) {
+    pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       tiles[i] = 0;
+      per[i] = 1;
       if (i >= P.n) continue;
       const Problem& p = P.p[i];
       M[i] = p.rows ? min(*p.rows, p.M) : p.M;
       const int K = p.depth ? min(*p.depth, p.K) : p.K;
+      const int slices = p.rows && p.blocks ? slices_of(p.slices, p.M, M[i]) : p.slices;
       mt[i] = (M[i] + BM - 1) / BM;
       nt[i] = (p.N + BN - 1) / BN;
       kb[i] = F8 ? (K + 127) / 128 : (K + 63) / 64;
-      tiles[i] = mt[i] * nt[i] * p.slices;
-      per[i] = (kb[i] + p.slices - 1) / p.slices;
+      tiles[i] = mt[i] * nt[i] * slices;
+      per[i] = (kb[i] + slices - 1) / slices;
     }
+    rest = tiles[0] % pairs;
+    extra = 0;
+    if (rest) extra = min((per[0] + LEAVING / 2) / max(per[1], LEAVING), tiles[1] / (pairs - rest));
+    dealt = extra * (pairs - rest);
   }
-  __device__ bool at(const Launch& P, int i, Tile& t) const {
-    t.p = 0;
-    if (i >= tiles[0]) {
-      i -= tiles[0];
+  // the pair's tile j
+  __device__ bool at(int j, Tile& t) const {
+    const int own = tiles[0] / pairs + (pair < rest);
+    int i;
+    if (j < own) {
+      t.p = 0;
+      i = pair + j * pairs;
+    } else {
       t.p = 1;
+      j -= own;
+      const int mine = pair >= rest ? extra : 0;
+      i = j < mine ? pair - rest + j * (pairs - rest) : dealt + pairs - 1 - pair + (j - mine) * pairs;
       if (i >= tiles[1]) return false;
     }
     const int m_n = t.p ? mt[1] : mt[0], n_n = t.p ? nt[1] : nt[0], kbs = t.p ? kb[1] : kb[0];
@@ -234,7 +262,7 @@ struct Sizes {
     i -= t.slice * m_n * n_n;
     const int g = i / (GROUP_M * n_n), gm = min(GROUP_M, m_n - g * GROUP_M);
     i -= g * GROUP_M * n_n;
-    const int n = gm == GROUP_M ? i / GROUP_M : i / gm;
+    const int n = i / gm;
     t.m0 = (g * GROUP_M + i - n * gm) * BM;
     t.n0 = n * BN;
     t.kb0 = t.slice * run;
@@ -328,7 +356,6 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
   uint32_t* tmem_s = reinterpret_cast<uint32_t*>(bars + N_BARS + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
-  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
@@ -348,6 +375,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_s)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
+  pdl_wait();
   Sizes S;
   S.read<F8>(P);
   tc_fence_before();
@@ -361,7 +389,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     if (lane == 0) {
       uint32_t it = 0;
       bool ok = true;
-      for (int i = pair; ok && S.at(P, i, t); i += pairs) {
+      for (int i = 0; ok && S.at(i, t); ++i) {
         const Problem& p = P.p[t.p];
         const int m = t.m0 + 128 * (int)rank, n = t.n0 + 128 * (int)rank;
         for (int k = 0; k < t.nkb; ++k, ++it) {
@@ -403,7 +431,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     if (lane == 0 && rank == 0) {
       uint32_t it = 0, nt = 0;
       bool ok = !P.unmet || mbar_wait(drain, 0, lost, P.wait_cycles);
-      for (int i = pair; ok && S.at(P, i, t); i += pairs) {
+      for (int i = 0; ok && S.at(i, t); ++i) {
         if (t.nkb == 0) continue;
         const Problem& p = P.p[t.p];
         const uint32_t id = idesc(F8, p.a_mn, p.b_mn, BM, BN), acc = nt & 1, d = tmem + acc * BN;
@@ -451,7 +479,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
       else box_wait<1>();
       last = j;
     };
-    for (int i = pair; S.at(P, i, t); i += pairs) {
+    for (int i = 0; S.at(i, t); ++i) {
       const Problem& p = P.p[t.p];
       const int M = t.p ? S.M[1] : S.M[0];
       const uint32_t acc = nt & 1;
@@ -555,7 +583,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
         } else if constexpr (MODE == GRAD) {
           if (p.blocks) {
             const int ncb = (p.N + 31) / 32;
-            float* o = p.blocks + (((long)t.slice * ((p.M + 31) / 32) + row0 / 32) * ncb + col0 / 32) * 1024 + lane;
+            float* o = p.blocks + (((long)t.slice * ((M + BM - 1) / BM * (BM / 32)) + row0 / 32) * ncb + col0 / 32) * 1024 + lane;
             const int n = min(2, ncb - col0 / 32);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
@@ -664,6 +692,67 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
   }
 }
 
+// A launch that may start while the one before it in the stream ends: its kernel waits for
+// that (pdl_wait) before it reads or writes anything
+template <typename... KArgs, typename... Args>
+lx_status launch_after(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, int cluster, cudaStream_t st,
+                       const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  LX_CUDA(cudaLaunchKernelEx(&cfg, kern, args...));
+  return LX_OK;
+}
+
+// A product from its fp32 blocks: the slices in their order, rounded once, each row to its
+// place.  A CTA a block, a warp four of its columns.
+struct Join {
+  const float* blocks;
+  int M, N, slices;   // as the product's
+  const int* rows;    // device count that bounds M, or NULL
+  const int* place;   // a row's place, or NULL: itself
+  __nv_bfloat16* out; // rows of N (a multiple of 8)
+};
+__global__ void __launch_bounds__(256) k_join(const __grid_constant__ Join A) {
+  __shared__ __nv_bfloat16 stage[32][40];
+  pdl_wait();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int n = A.rows ? min(*A.rows, A.M) : A.M, slices = A.rows ? slices_of(A.slices, A.M, n) : A.slices;
+  const int rb = blockIdx.x, cb = blockIdx.y, ncb = gridDim.y;
+  if (rb * 32 >= n) return;
+  const long slice = (long)((n + BM - 1) / BM * (BM / 32)) * ncb * 1024;
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  const float* b = A.blocks + ((long)rb * ncb + cb) * 1024 + 128 * warp + lane;
+#pragma unroll 4
+  for (int s = 0; s < slices; ++s) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += b[s * slice + 32 * e];
+  }
+  *(uint2*)&stage[lane][4 * warp] =
+      make_uint2(rows::to_bf2(make_float2(v[0], v[1])), rows::to_bf2(make_float2(v[2], v[3])));
+  __syncthreads();
+  const int r = threadIdx.x / 4, c = 8 * (threadIdx.x % 4), row = rb * 32 + r;
+  if (threadIdx.x < 128 && row < n && cb * 32 + c < A.N)
+    *(uint4*)(A.out + (long)(A.place ? A.place[row] : row) * A.N + cb * 32 + c) = *(const uint4*)&stage[r][c];
+}
+inline lx_status launch_join(const Join& J, cudaStream_t st) {
+  return launch_after(k_join, dim3((J.M + 31) / 32, (J.N + 31) / 32), dim3(256), 0, 1, st, J);
+}
+// floats of a product's blocks
+inline size_t block_floats(long M, long N, int slices) {
+  return (size_t)slices * ((M + BM - 1) / BM * (BM / 32)) * ((N + 31) / 32) * 1024;
+}
+
 // Operand along K: rows x K elements of es bytes, ld elements apart; along M / N: K rows
 inline bool operand(CUtensorMap* m, const void* base, long inner, long outer, long ld, int es, bool mn) {
   return encode_bytes_2d(m, base, inner * es, outer, ld * es, mn ? 64 : 128);
@@ -687,19 +776,8 @@ lx_status launch_product(const Launch& P, cudaStream_t st) {
   long tiles = 0;
   for (int i = 0; i < P.n; ++i) tiles += tiles_of(P.p[i]);
   if (tiles == 0) return LX_OK;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(2 * std::min<long>(tiles, rows::SMS / 2)));
-  cfg.blockDim = dim3(THREADS);
-  cfg.dynamicSmemBytes = SMEM;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = 2;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  LX_CUDA(cudaLaunchKernelEx(&cfg, k_product<MODE, F8>, P));
-  return LX_OK;
+  const unsigned pairs = (unsigned)std::min<long>(tiles, rows::SMS / 2);
+  return launch_after(k_product<MODE, F8>, dim3(2 * pairs), dim3(THREADS), SMEM, 2, st, P);
 }
 
 }  // namespace
