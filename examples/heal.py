@@ -14,7 +14,12 @@ earlier blocks along the residual and through the routers.  The norms before the
 act through the experts, so they stay as they are, too, and so does what the first
 block's router sees: it has no part in the loss.
 
-    python examples/heal.py [--steps 30]
+With --labels, a dense expert shared by all tokens (`lx.linear`) is then added beside the
+last block's routed ones and trained, with the head and that block's norms, on the text's own
+next tokens (`lx.head_loss`, which keeps no logits); `shared_8bit` serves it in 8 bits, from the
+norm's own 8-bit output (`lx.residual_norm_q8`).
+
+    python examples/heal.py [--steps 30] [--labels 0]
 """
 from __future__ import annotations
 
@@ -169,8 +174,88 @@ def heal(steps=30, lr=0.01, temperature=2.0, seed=0):
     return [(v.tolist(), c.tolist()) for v, c in history]
 
 
+class Shared:
+    """A dense expert of every token: y += gelu(h up^T + bias) down^T, bf16."""
+
+    def __init__(self, g, width=320):
+        randn = lambda *s, std: (torch.randn(*s, generator=g, device="cuda") * std).bfloat16()  # noqa: E731
+        self.up, self.bias, self.down = randn(width, H, std=H ** -0.5), randn(width, std=0.1), randn(H, width, std=0.02)
+
+    def forward(self, h, y):
+        """(y + the expert's output, what the backward needs)"""
+        pre = torch.empty(h.shape[0], self.up.shape[0], dtype=torch.bfloat16, device=h.device)
+        a = lx.linear(h, self.up, bias=self.bias, act="gelu", pre=pre)
+        return lx.linear(a, self.down, residual=y), (h, pre, a)
+
+    def backward(self, dy, kept):
+        """Gradients of up, bias and down (the block's input is not trained through it)."""
+        h, pre, a = kept
+        d = lx.linear_backward(dy, a, self.down)
+        u = lx.linear_backward(d.dx, h, self.up, act="gelu", pre=pre, want_dx=False, want_dbias=True)
+        return u.dw, u.dbias, d.dw
+
+
+def to_8bit(w):
+    """(e4m3, a scale for each output) of a weight."""
+    scale = (w.float().abs().amax(1) / 448).clamp(min=2.0 ** -126)
+    return (w.float() / scale[:, None]).to(torch.float8_e4m3fn), scale
+
+
+def shared_8bit(expert, r, y, w_pre):
+    """The expert as it is served: the norm of r + y gives its input in 8 bits.  Returns
+    (r + y, the expert's output)."""
+    up, up_scale = to_8bit(expert.up)
+    n = lx.residual_norm_q8(r, y, w_pre=w_pre, eps=EPS)
+    a = lx.linear(n.q, up, x_scale=n.scale, w_scale=up_scale, bias=expert.bias, act="gelu")
+    return n.r_out, lx.linear(a, expert.down)
+
+
+def labels_step(student, expert, first, x, head, labels, weight):
+    """(loss, gradients by name) of one batch: what is before the last block stays as it is."""
+    r, h = lx.residual_norm(x, w_pre=first, eps=EPS)
+    for b in student[:-1]:
+        r, h, _ = b.forward(r, h)
+    b = student[-1]
+    y, kept = expert.forward(h, b.layer.moe_forward(h, K))
+    stats = torch.empty(2, r.shape[0], device=r.device)
+    norm = dict(w_post=b.w_post, gate=b.gate, w_pre=b.w_pre)
+    _, h_out = lx.residual_norm(r, y, eps=EPS, stats=stats, **norm)
+    out = lx.head_loss(h_out, head, labels, row_weight=weight)
+    g = lx.residual_norm_backward(None, out.dh, r, y, stats, **norm)
+    up, bias, down = expert.backward(g.dy, kept)
+    return out.loss.sum(), dict(head=out.dw, up=up, bias=bias, down=down, w_post=g.dw_post, gate=g.dgate, w_pre=g.dw_pre)
+
+
+def train_on_labels(student, first, x, head, steps=10, lr=0.01, seed=1):
+    """Trains a shared expert, the head and the last block's norms; returns (the losses, the expert)."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    expert, b = Shared(g), student[-1]
+    labels = torch.randint(0, VOCAB, (TOKENS,), generator=g, device="cuda", dtype=torch.int32)
+    labels[: TOKENS // 8] = -100  # a prompt
+    weight = torch.full((TOKENS,), 1.0 / int((labels >= 0).sum()), device="cuda")
+    params = dict(head=head, up=expert.up, bias=expert.bias, down=expert.down, w_post=b.w_post, gate=b.gate, w_pre=b.w_pre)
+    master = {n: p.float() for n, p in params.items()}
+    optimiser = torch.optim.Adam(master.values(), lr=lr)
+    losses = []
+    for _ in range(steps):
+        loss, grads = labels_step(student, expert, first, x, head, labels, weight)
+        losses.append(loss)
+        for n, p in master.items():
+            p.grad = grads[n].float()
+        optimiser.step()
+        for n, p in params.items():
+            p.copy_(master[n])
+    return [v.item() for v in losses], expert
+
+
 if __name__ == "__main__":
     ap = argparse.ArgumentParser()
     ap.add_argument("--steps", type=int, default=30)
-    for i, ((total, kd, bal), counts) in enumerate(heal(ap.parse_args().steps)):
+    ap.add_argument("--labels", type=int, default=0)
+    args = ap.parse_args()
+    for i, ((total, kd, bal), counts) in enumerate(heal(args.steps)):
         print(f"step {i:3d}  loss {total:.4f}  distillation {kd:.4f}  balance {bal:.3f}  tokens {counts[:-1]}")
+    if args.labels:
+        _, student, first, x, head = build()
+        for i, loss in enumerate(train_on_labels(student, first, x, head, args.labels)[0]):
+            print(f"labels, step {i:3d}  loss {loss:.4f}")
