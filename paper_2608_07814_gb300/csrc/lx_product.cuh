@@ -87,6 +87,7 @@ struct Launch {
   // STATS
   float2* part;      // [halves of tiles of N][part_ld]: a row's largest logit there, sum of exp
   long part_ld;
+  int two;           // both accumulators to a tile, half of its sum each
   float* keep;       // the logits in blocks of 32 x 32 (32 rows of each column), or NULL
   int keep_cols;     // blocks side by side
 };
@@ -384,6 +385,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
   tc_fence_after();
   const uint32_t tmem = *tmem_s;
 
+  const bool two = MODE == STATS && P.two;
   Tile t;
   if (warp == 0) {
     if (lane == 0) {
@@ -434,11 +436,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
       for (int i = 0; ok && S.at(i, t); ++i) {
         if (t.nkb == 0) continue;
         const Problem& p = P.p[t.p];
-        const uint32_t id = idesc(F8, p.a_mn, p.b_mn, BM, BN), acc = nt & 1, d = tmem + acc * BN;
-        ok = mbar_wait(tempty0 + 8 * acc, ((nt >> 1) & 1) ^ 1, lost, P.wait_cycles);
+        const uint32_t id = idesc(F8, p.a_mn, p.b_mn, BM, BN), acc = two ? 0 : nt & 1, turn = two ? nt : nt >> 1;
+        uint32_t d = tmem + acc * BN;
+        ok = mbar_wait(tempty0 + 8 * acc, (turn & 1) ^ 1, lost, P.wait_cycles);
         if (!ok) break;
         tc_fence_after();
+        const int half = two ? (t.nkb + 1) / 2 : t.nkb;
         for (int k = 0; k < t.nkb; ++k, ++it) {
+          if (k == half) d += BN;
           const uint32_t s = it % STAGES;
           if (!mbar_wait(full0 + 8 * s, (it / STAGES) & 1, lost, P.wait_cycles)) {
             ok = false;
@@ -450,7 +455,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
           for (int j = 0; j < 4; ++j) {
             const uint64_t da = p.a_mn ? desc_mn(as + 2048 * j) : smem_desc(as + 32 * j);
             const uint64_t db = p.b_mn ? desc_mn(bs + 2048 * j) : smem_desc(bs + 32 * j);
-            mma_pair<F8>(d, da, db, id, (k | j) != 0 ? 1u : 0u);
+            mma_pair<F8>(d, da, db, id, (k != 0 && k != half) || j != 0 ? 1u : 0u);
           }
           commit_pair(empty0 + 8 * s, 3);
         }
@@ -482,7 +487,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     for (int i = 0; S.at(i, t); ++i) {
       const Problem& p = P.p[t.p];
       const int M = t.p ? S.M[1] : S.M[0];
-      const uint32_t acc = nt & 1;
+      const uint32_t acc = two ? 0 : nt & 1, turn = two ? nt : nt >> 1;
       const int row0 = t.m0 + 128 * (int)rank + 32 * q, row = row0 + lane;
       // dz has rows of zeros behind the last: whole tiles
       const bool on = row0 < (MODE == DLOGIT ? p.M : M);
@@ -518,7 +523,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
       }
       if (t.nkb > 0) {
         if (ok && lane == 0) {
-          ok = mbar_wait(tfull0 + 8 * acc, (nt >> 1) & 1, lost, P.wait_cycles) ? 1 : 0;
+          ok = mbar_wait(tfull0 + 8 * acc, turn & 1, lost, P.wait_cycles) ? 1 : 0;
           if (!ok) *lost = 1;
         }
         ok = __shfl_sync(0xffffffffu, ok, 0);
@@ -537,6 +542,17 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
           tc_ld32_async(at, *reinterpret_cast<uint32_t(*)[32]>(r));
           tc_ld32_async(at + 32, *reinterpret_cast<uint32_t(*)[32]>(r + 32));
           tc_wait_ld();
+          if (MODE == STATS && two && t.nkb > 1) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              uint32_t s[32];
+              tc_ld32_async(at + BN + 32 * h, s);
+              tc_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                r[32 * h + e] = __float_as_uint(__uint_as_float(r[32 * h + e]) + __uint_as_float(s[e]));
+            }
+          }
           if (j == 1) {  // the accumulator is read: the next tile but one may take its place
             tc_fence_before();
             __syncwarp();
