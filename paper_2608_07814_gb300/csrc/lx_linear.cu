@@ -23,8 +23,8 @@ struct Few {
   CUtensorMap w, x;  // boxes of 128 bytes x 128 rows, and x tn rows
   int T, N, nkb, per;  // blocks of K: all, a CTA's
   int tn, stages, cols;  // tokens of a tile (a multiple of 16), TMEM columns
-  Launch e;          // the epilogue's part
   int vec;           // four outputs at a time
+  Epilogue e;
 };
 
 template <bool F8>
@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) k_linear_few(const __grid_cons
   tc_fence_before();
   if (splits > 1) cluster_sync();
   else __syncthreads();
-  const Launch& E = P.e;
+  const Epilogue& E = P.e;
   for (int i = rank * FEW_THREADS + threadIdx.x; i < T * 32; i += splits * FEW_THREADS) {
     const int t = i >> 5, c = 4 * (i & 31), col = n0 + c;
     const uint32_t at = base + 4 * (uint32_t)(t * 128 + c);
@@ -286,13 +286,13 @@ __device__ __forceinline__ float2 through(float2 d, float2 z) {
 }
 
 // dz is rounded to bf16 as the tensor cores take it (2^-9 of each term of the gradients' fp32
-// sums); the bias's gradient sums it unrounded.  A warp reads rows of 32 VEC columns, four rows
-// ahead.
+// sums); the bias's gradient sums it unrounded.  A warp reads rows of 32 VEC columns, AHEAD of them at
+// a time.
 template <int VEC, int ACT>
 __global__ void __launch_bounds__(256, 4) k_linear_dz(const __grid_constant__ DzArgs A) {
   pdl_wait();
   __shared__ float sums[8][32 * VEC];
-  constexpr int W = VEC == 8 ? 4 : 1;  // words of a piece
+  constexpr int W = VEC == 8 ? 4 : 1, AHEAD = 4;  // words of a piece; rows
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int col = (blockIdx.x * 32 + lane) * VEC;
   const long t0 = (long)blockIdx.y * A.chunk;
@@ -309,17 +309,17 @@ __global__ void __launch_bounds__(256, 4) k_linear_dz(const __grid_constant__ Dz
     }
   };
   if (col < A.N) {
-    for (int r0 = warp; r0 < n; r0 += 32) {
-      uint32_t a[4][W], b[4][W];
+    for (int r0 = warp; r0 < n; r0 += 8 * AHEAD) {
+      uint32_t a[AHEAD][W], b[AHEAD][W];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < AHEAD; ++i)
         if (r0 + 8 * i < n) {
           const long t = t0 + r0 + 8 * i;
           read(A.dy + t * A.lddy + col, a[i]);
           if (ACT != NONE) read(A.pre + t * A.ldp + col, b[i]);
         }
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < AHEAD; ++i)
         if (r0 + 8 * i < n) {
           float d[VEC];
 #pragma unroll
@@ -376,7 +376,8 @@ __global__ void __launch_bounds__(256) k_linear_db(const float* part, int chunks
   }
 }
 
-// rows of a CTA of k_linear_dz: about four CTAs an SM; a multiple of the warps
+// rows of a CTA of k_linear_dz: about four CTAs an SM; a multiple of the warps.  (Few rows in one
+// CTA, which would save k_linear_db: 257 rows of 1003 14 us instead of 10.)
 int dz_chunk(int T, int N) {
   const long cols = (N + 255) / 256;
   const long ctas = std::max(1L, 4L * SMS / cols);

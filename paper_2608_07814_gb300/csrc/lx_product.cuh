@@ -67,17 +67,22 @@ struct Problem {
   int add;           // to what the blocks hold
 };
 
-struct Launch {
-  Problem p[2];
-  int n;
-  unsigned long long wait_cycles;
-  int unmet;  // test hook: the issuer first waits for what nothing fulfils
-  // LINEAR
+// What becomes of a sum of lx_linear: y = act(sum x_scale w_scale + bias) + residual
+struct Epilogue {
   const float *x_scale, *w_scale;
   const __nv_bfloat16 *bias, *residual;
   __nv_bfloat16 *y, *pre;
   long ldr, ldy, ldp;
-  int act, tma_r, tma_y, tma_p;  // whether their rows suit TMA (boxes of 128 bytes x 32 rows):
+  int act;
+  int unmet;  // test hook: the issuer first waits for what nothing fulfils
+  unsigned long long wait_cycles;
+};
+
+struct Launch : Epilogue {
+  Problem p[2];
+  int n;
+  // LINEAR
+  int tma_r, tma_y, tma_p;  // whether the residual's, y's and pre's rows suit TMA (boxes of 128 bytes x 32 rows):
   CUtensorMap map_r, map_y, map_p;
   // DLOGIT: compact rows' labels, weights and log-sum-exps (in units of log 2)
   const int* label;
