@@ -600,8 +600,9 @@ LX_API lx_status lx_distill_loss(int32_t dtype, const void* logits, int64_t ld,
  * Products around a compressed layer: the norm before a dense block with its output in 8
  * bits, the block's products with their epilogue and gradients, and the loss on the head's
  * product.  Standalone calls on plain device arrays, stream-ordered, without allocation;
- * products accumulate in fp32, and results do not depend on scheduling.  If one of their
- * bounded waits gives up, the outputs that depend on it are NaN.
+ * products accumulate in fp32, and results do not depend on scheduling.  A workspace
+ * belongs to one call at a time: calls (and captured graphs) that may run at the same time need
+ * one each.  If one of their bounded waits gives up, the outputs that depend on it are NaN.
  */
 
 /*

@@ -24,6 +24,7 @@ using namespace rows;
 using namespace prod;
 
 constexpr int ROWS = 8;                      // of a CTA of k_head_rows, one a warp
+constexpr int RUN = 2048;                    // rows that k_head_rows counts by itself
 constexpr long PIECE_BYTES = 256L << 20;     // of dz, or of kept logits, at most
 constexpr int MAX_T = 1 << 24, MAX_V = 1 << 24, MAX_H = 1 << 20;
 
@@ -38,6 +39,7 @@ struct Head {
   // compact
   __nv_bfloat16* hc;
   int *label, *row, *n;
+  int* runs;  // rows that count of each RUN, where there are more
   float *weight, *lse2, *label_logit;
   const float2* part;
   int slots;
@@ -47,9 +49,36 @@ struct Head {
   long ldd;
 };
 
+__device__ __forceinline__ int counts(const Head& A, int t) {
+  const int l = A.labels[t];
+  const float w = A.row_weight ? A.row_weight[t] : 1.f;
+  return l >= 0 && l < A.V && w != 0.f;
+}
+
+// rows that count of each RUN
+__global__ void __launch_bounds__(256) k_head_runs(const __grid_constant__ Head A) {
+  __shared__ int red[8];
+  pdl_wait();
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < RUN; i += 256) {
+    const int t = blockIdx.x * RUN + i + threadIdx.x;
+    if (t < A.T) n += counts(A, t);
+  }
+  n = __reduce_add_sync(0xffffffffu, n);
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x / 32] = n;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    n = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) n += red[i];
+    A.runs[blockIdx.x] = n;
+  }
+}
+
 // The rows that count, side by side in their order; loss and dh of the others are 0.  Each CTA
-// counts the rows before its own and all of them by itself, so that one launch does.  A
-// row's label's logit is formed here, in fp32: the tensor core cuts its running sums off
+// counts the rows before its own and all of them by itself, so that one launch does, or takes
+// whole runs of them from k_head_runs.  A row's label's logit is formed here, in fp32: the tensor core cuts its running sums off
 // instead of rounding them, 4e-6 of a logit of 2048 terms, which a loss shows and its
 // gradient does not.
 __global__ void __launch_bounds__(256) k_head_rows(const __grid_constant__ Head A) {
@@ -62,13 +91,22 @@ __global__ void __launch_bounds__(256) k_head_rows(const __grid_constant__ Head 
   const float weight = t < A.T ? (A.row_weight ? A.row_weight[t] : 1.f) : 0.f;
   const bool mine = label >= 0 && label < A.V && weight != 0.f;
   int before = 0, all = 0;
+  if (A.T <= RUN) {
 #pragma unroll 4
-  for (int i = threadIdx.x; i < A.T; i += 256) {
-    const int l = A.labels[i];
-    const float w = A.row_weight ? A.row_weight[i] : 1.f;
-    const int c = l >= 0 && l < A.V && w != 0.f;
-    all += c;
-    before += i < t0 ? c : 0;
+    for (int i = threadIdx.x; i < A.T; i += 256) {
+      const int c = counts(A, i);
+      all += c;
+      before += i < t0 ? c : 0;
+    }
+  } else {
+    const int run = t0 / RUN, runs = (A.T + RUN - 1) / RUN;
+    for (int i = threadIdx.x; i < runs; i += 256) {
+      const int c = A.runs[i];
+      all += c;
+      before += i < run ? c : 0;
+    }
+#pragma unroll 4
+    for (int i = run * RUN + threadIdx.x; i < min(t0, A.T); i += 256) before += counts(A, i);
   }
   before = __reduce_add_sync(0xffffffffu, before);
   all = __reduce_add_sync(0xffffffffu, all);
@@ -210,7 +248,7 @@ size_t al(size_t v) { return (v + 255) / 256 * 256; }
 struct Plan {
   long Tp, piece;  // columns of a piece, a multiple of 256
   int slots, slices;
-  size_t hc, label, weight, row, lse2, label_logit, n, part, dl, blocks, keep, bytes;
+  size_t hc, label, weight, row, lse2, label_logit, n, runs, part, dl, blocks, keep, bytes;
   int keep_cols;   // blocks of kept logits side by side, 0: not kept
 };
 
@@ -236,6 +274,7 @@ Plan plan_of(int T, int V, int H, bool dh, bool dw) {
   p.lse2 = take(4 * p.Tp);
   p.label_logit = take(4 * p.Tp);
   p.n = take(4);
+  p.runs = take(4 * (p.Tp / RUN + 1));
   p.part = take(8 * (size_t)p.slots * p.Tp);
   if (dh || dw) {
     p.dl = take(2 * (size_t)p.Tp * p.piece);
@@ -317,6 +356,7 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
   A.label = (int*)(ws + L.label);
   A.row = (int*)(ws + L.row);
   A.n = (int*)(ws + L.n);
+  A.runs = (int*)(ws + L.runs);
   A.weight = (float*)(ws + L.weight);
   A.lse2 = (float*)(ws + L.lse2);
   A.label_logit = (float*)(ws + L.label_logit);
@@ -327,8 +367,8 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
   A.dl = (__nv_bfloat16*)(ws + L.dl);
   A.ldd = L.piece;
 
-  k_head_rows<<<(unsigned)(L.Tp / ROWS), 256, 0, st>>>(A);
-  LX_CUDA(cudaGetLastError());
+  if (T > RUN) LX_TRY(launch_after(k_head_runs, dim3((T + RUN - 1) / RUN), dim3(256), 0, 1, st, A));
+  LX_TRY(launch_after(k_head_rows, dim3((unsigned)(L.Tp / ROWS)), dim3(256), 0, 1, st, A));
 
   Launch P = {};
   P.wait_cycles = waits.cycles;

@@ -623,6 +623,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
           }
         } else {
           if (ahead && P.pre && j == 1) fetch(1);
+          // TMA stores whole pieces of 16 bytes: a last block that ends inside one goes by columns
+          const bool whole = col0 + 64 <= p.N || p.N % 8 == 0;
           // the columns' scale and bias, handed to all lanes
           if (F8 || P.bias) {
 #pragma unroll
@@ -650,7 +652,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
           }
           if (P.pre) {  // through the other buffer
             box_wait<0>();
-            if (P.tma_p) {
+            if (P.tma_p && whole) {
               put_box(stg + (j ^ 1) * STG, r, &P.map_p, col0, row0);
             } else {
               for (int h = 0; h < 2; ++h)
@@ -688,7 +690,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
               for (int h = 0; h < 2; ++h) add_rows(buf, r + 32 * h, P.residual, P.ldr, row0, M, col0 + 32 * h, p.N);
             }
           }
-          if (P.tma_y) {
+          if (P.tma_y && whole) {
             if (!P.pre && !ahead) box_free(j);  // (else the buffer has been waited for)
             put_box(buf, r, &P.map_y, col0, row0);
           } else {

@@ -80,6 +80,19 @@ def test_wide_vocabulary_in_several_pieces():
     assert not got.loss[dead].any() and not got.dh[dead].any()
 
 
+@pytest.mark.parametrize("T,V,H", [(2048, 300, 64), (2049, 300, 64), (9000, 130, 72), (70001, 33, 16)])
+def test_many_rows(T, V, H):
+    h, w, labels, weight = _case(T, V, H, 0.3, seed=4)
+    labels[T // 3: T // 3 + 2100] = -100  # a whole run of rows takes no part
+    _check(lx.head_loss(h, w, labels, row_weight=weight), h, w, labels, weight)
+
+
+@pytest.mark.parametrize("T,V,H", [(40, 700, 2056), (300, 600, 4104)])
+def test_long_sums(T, V, H):
+    h, w, labels, weight = _case(T, V, H, 0.1, seed=6)
+    _check(lx.head_loss(h, w, labels, row_weight=weight), h, w, labels, weight)
+
+
 @pytest.mark.parametrize("T", [5, 300])
 def test_rows_that_take_no_part_are_not_used(T):
     h, w, labels, weight = _case(T, 500, 128, 0.4, seed=2)

@@ -94,6 +94,21 @@ def test_strides_in_place_and_what_lies_beside(T, N):
     assert torch.equal(lx.linear(x, w, residual=res, act="silu"), lx.linear(x.contiguous(), w.contiguous(), residual=before[1:-1, 3:3 + N], act="silu"))
 
 
+@pytest.mark.parametrize("T,N,ld", [(600, 2011, 2016), (1000, 1999, 2056), (5000, 130, 136), (513, 4095, 4096),
+                                    (2000, 3001, 3008), (9000, 515, 520), (2500, 2052, 2056)])
+def test_rows_on_16_byte_boundaries_that_end_elsewhere(T, N, ld):
+    """Columns behind the last and rows below it are left as they were; the residual's are not read."""
+    x, w, _, X, W = _case(T, N, 72, BF)
+    out = torch.full((T + 40, ld), 7.0, dtype=BF, device="cuda")
+    res = torch.full((T, ld), float("nan"), dtype=BF, device="cuda")
+    res[:, :N] = torch.randn(T, N, generator=_gen(2)).to(BF).cuda()
+    pre = torch.empty(T, N, dtype=BF, device="cuda")
+    y = lx.linear(x, w, act="silu", residual=res[:, :N], y=out[:T, :N])
+    _check_y(y, X, W, "silu", None, res[:, :N].contiguous())
+    assert (out[:, N:] == 7).all() and (out[T:] == 7).all()
+    assert torch.equal(lx.linear(x, w, act="silu", residual=res[:, :N], pre=pre), y)
+
+
 def test_what_is_no_number_stays_in_its_row():
     for T, N in ((9, 100), (600, 4000)):
         x, w, _, X, W = _case(T, N, 64, BF)
@@ -202,7 +217,7 @@ def test_a_wait_that_runs_out_gives_nan(T, N):
     dy = torch.randn(T, N, generator=_gen(1)).to(BF).cuda()
     want, grads = lx.linear(x, w), lx.linear_backward(dy, x, w)
     lx.inject_unmet_wait_call(lx.LX_WAIT_CALL_PRODUCT, 2_000_000)
-    bad = lx.linear(x, w, act="relu")
+    bad = lx.linear(x, w, act="relu", residual=dy)
     torch.cuda.synchronize()
     assert torch.isnan(bad).all()
     lx.inject_unmet_wait_call(lx.LX_WAIT_CALL_PRODUCT, 2_000_000)
