@@ -356,28 +356,15 @@ void launch_dz(const DzArgs& A, dim3 grid, cudaStream_t st) {
   else k_linear_dz<VEC, NONE><<<grid, 256, 0, st>>>(A);
 }
 
-// the CTAs' sums in their order: 8 ranges of them side by side, then those
-__global__ void __launch_bounds__(256) k_linear_db(const float* part, int chunks, int N, __nv_bfloat16* db) {
-  __shared__ float sums[8][32];
+// the bias's gradient by itself (otherwise it is added up beside the products)
+__global__ void __launch_bounds__(64) k_linear_db(const float* part, int chunks, int N, __nv_bfloat16* db) {
   pdl_wait();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
-  const int per = (chunks + 7) / 8;
-  float v = 0.f;
-  if (c < N)
-#pragma unroll 8
-    for (int i = warp * per; i < min(chunks, (warp + 1) * per); ++i) v += part[(long)i * N + c];
-  sums[warp][lane] = v;
-  __syncthreads();
-  if (warp == 0 && c < N) {
-    v = 0.f;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) v += sums[w][lane];
-    db[c] = __float2bfloat16_rn(v);
-  }
+  const int c = blockIdx.x * 64 + threadIdx.x;
+  if (c < N) db[c] = __float2bfloat16_rn(column_sum(part, chunks, N, c));
 }
 
-// rows of a CTA of k_linear_dz: about four CTAs an SM; a multiple of the warps.  (Few rows in one
-// CTA, which would save k_linear_db: 257 rows of 1003 14 us instead of 10.)
+// rows of a CTA of k_linear_dz: about four CTAs an SM; a multiple of the warps.  (All of few rows in one
+// CTA, which would save the parts: 257 rows of 1003 14 us instead of 5.)
 int dz_chunk(int T, int N) {
   const long cols = (N + 255) / 256;
   const long ctas = std::max(1L, 4L * SMS / cols);
@@ -554,8 +541,8 @@ extern "C" lx_status lx_linear_backward(const lx_linear_desc* d, const void* dy,
     if (vec) launch_dz<8>(A, dim3((N + 255) / 256, chunks), st);
     else launch_dz<1>(A, dim3((N + 31) / 32, chunks), st);
     LX_CUDA(cudaGetLastError());
-    if (dbias)
-      LX_TRY(launch_after(k_linear_db, dim3((N + 31) / 32), dim3(256), 0, 1, st, (const float*)part, chunks, N,
+    if (dbias && !dx && !dw)
+      LX_TRY(launch_after(k_linear_db, dim3((N + 63) / 64), dim3(64), 0, 1, st, (const float*)part, chunks, N,
                           (__nv_bfloat16*)dbias));
   }
   if (!dx && !dw) return LX_OK;
@@ -564,6 +551,12 @@ extern "C" lx_status lx_linear_backward(const lx_linear_desc* d, const void* dy,
   Launch P = {};
   P.wait_cycles = waits.cycles;
   P.unmet = waits.unmet == LX_WAIT_CALL_PRODUCT;
+  if (dbias) {
+    P.db = (__nv_bfloat16*)dbias;
+    P.db_part = part;
+    P.db_chunks = chunks;
+    P.db_n = N;
+  }
   bool ok = true;
   Join joins[2];
   int n_joins = 0;

@@ -81,6 +81,10 @@ struct Epilogue {
 struct Launch : Epilogue {
   Problem p[2];
   int n;
+  // GRAD: columns' sums to be added up beside the products
+  const float* db_part;
+  int db_chunks, db_n;
+  __nv_bfloat16* db;
   // LINEAR
   int tma_r, tma_y, tma_p;  // whether the residual's, y's and pre's rows suit TMA (boxes of 128 bytes x 32 rows):
   CUtensorMap map_r, map_y, map_p;
@@ -350,6 +354,19 @@ __device__ __forceinline__ void box_wait() {
   __syncwarp();
 }
 
+// sum of a column's parts: 8 ranges of them, then those in order
+__device__ __forceinline__ float column_sum(const float* part, int chunks, int n, int c) {
+  const int per = (chunks + 7) / 8;
+  float v = 0.f;
+  for (int w = 0; w < 8; ++w) {
+    float s = 0.f;
+#pragma unroll 8
+    for (int i = w * per; i < min(chunks, (w + 1) * per); ++i) s += part[(long)i * n + c];
+    v += s;
+  }
+  return v;
+}
+
 template <int MODE, bool F8>
 __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ Launch P) {
   extern __shared__ uint8_t smem_raw[];
@@ -474,6 +491,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
         mbar_wait(drain, 0, nullptr, P.wait_cycles);
       }
     }
+  } else if (MODE == GRAD && warp < 4) {
+    for (int c = (blockIdx.x * 2 + warp - 2) * 32 + lane; c < P.db_n; c += gridDim.x * 64)
+      P.db[c] = __float2bfloat16_rn(column_sum(P.db_part, P.db_chunks, P.db_n, c));
   } else if (warp >= 4) {
     const int q = warp & 3, half = (warp - 4) >> 2;
     char* stg = staged + (warp - 4) * 2 * STG;
