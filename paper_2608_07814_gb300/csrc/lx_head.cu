@@ -386,10 +386,6 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
   p.rows = A.n;
   if (!operand(&p.a, A.hc, H, L.Tp, H, 2, false) || !operand(&p.b, w, H, V, ldw, 2, false))
     return fail(LX_ERR_CUDA, "cuTensorMapEncodeTiled(head) failed");
-  // The tensor core cuts a running sum off at every 16 terms: beyond 2048 a logit is summed in two
-  // halves, or the losses would be 1.1e-6 off (2560 terms) where fp32 sums are 1e-7.  Their tiles' epilogues
-  // then do not run beside the next products: 58 us instead of 52 for 100 x 50021 x 2560.
-  P.two = H > 2048;
   LX_TRY((launch_product<STATS, false>(P, st)));
   LX_TRY(launch_after(k_head_lse, dim3((unsigned)(L.Tp / 32)), dim3(1024), 0, 1, st, A));
   if (!dh && !dw) return LX_OK;

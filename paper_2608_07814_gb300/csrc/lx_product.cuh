@@ -96,7 +96,6 @@ struct Launch : Epilogue {
   // STATS
   float2* part;      // [halves of tiles of N][part_ld]: a row's largest logit there, sum of exp
   long part_ld;
-  int two;           // both accumulators to a tile, half of its sum each
   float* keep;       // the logits in blocks of 32 x 32 (32 rows of each column), or NULL
   int keep_cols;     // blocks side by side
 };
@@ -367,8 +366,14 @@ __device__ __forceinline__ float column_sum(const float* part, int chunks, int n
   return v;
 }
 
+// The tensor core cuts a running sum off at every instruction (16 terms, 32 of e4m3): a sum of
+// 2048 is 1e-6 to 4e-6 of itself short.  That is lost in a bf16 output, but not in a loss: the logits'
+// statistics are taken of sums in parts of 1024 terms (16 blocks of K), each in an accumulator of
+// its own, added as fp32 on their way out.  (Losses were 8e-7 off, at 2560 terms 1.2e-6, and are
+// 4e-7; it costs these tiles 4 %.  In the gradients' tiles the registers for it cost 10 to 50 %.)
 template <int MODE, bool F8>
 __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ Launch P) {
+  constexpr int PART = MODE == STATS ? 16 : 1 << 30;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   char* staged = reinterpret_cast<char*>(smem + STAGES * STAGE);
@@ -407,7 +412,6 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
   tc_fence_after();
   const uint32_t tmem = *tmem_s;
 
-  const bool two = MODE == STATS && P.two;
   Tile t;
   if (warp == 0) {
     if (lane == 0) {
@@ -458,32 +462,30 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
       for (int i = 0; ok && S.at(i, t); ++i) {
         if (t.nkb == 0) continue;
         const Problem& p = P.p[t.p];
-        const uint32_t id = idesc(F8, p.a_mn, p.b_mn, BM, BN), acc = two ? 0 : nt & 1, turn = two ? nt : nt >> 1;
-        uint32_t d = tmem + acc * BN;
-        ok = mbar_wait(tempty0 + 8 * acc, (turn & 1) ^ 1, lost, P.wait_cycles);
-        if (!ok) break;
-        tc_fence_after();
-        const int half = two ? (t.nkb + 1) / 2 : t.nkb;
+        const uint32_t id = idesc(F8, p.a_mn, p.b_mn, BM, BN);
+        uint32_t d = tmem;
         for (int k = 0; k < t.nkb; ++k, ++it) {
-          if (k == half) d += BN;
           const uint32_t s = it % STAGES;
-          if (!mbar_wait(full0 + 8 * s, (it / STAGES) & 1, lost, P.wait_cycles)) {
-            ok = false;
-            break;
+          if (k % PART == 0) {  // an accumulator for the next part of the sum
+            if (k) commit_pair(tfull0 + 8 * (nt++ & 1), 3);
+            ok = mbar_wait(tempty0 + 8 * (nt & 1), ((nt >> 1) & 1) ^ 1, lost, P.wait_cycles);
+            if (!ok) break;
+            tc_fence_after();
+            d = tmem + (nt & 1) * BN;
           }
+          ok = mbar_wait(full0 + 8 * s, (it / STAGES) & 1, lost, P.wait_cycles);
+          if (!ok) break;
           tc_fence_after();
           const uint32_t as = base + s * STAGE, bs = as + A_BYTES;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const uint64_t da = p.a_mn ? desc_mn(as + 2048 * j) : smem_desc(as + 32 * j);
             const uint64_t db = p.b_mn ? desc_mn(bs + 2048 * j) : smem_desc(bs + 32 * j);
-            mma_pair<F8>(d, da, db, id, (k != 0 && k != half) || j != 0 ? 1u : 0u);
+            mma_pair<F8>(d, da, db, id, k % PART != 0 || j != 0 ? 1u : 0u);
           }
           commit_pair(empty0 + 8 * s, 3);
         }
-        if (!ok) break;
-        commit_pair(tfull0 + 8 * acc, 3);
-        ++nt;
+        if (ok) commit_pair(tfull0 + 8 * (nt++ & 1), 3);
       }
       if (!ok) {
         *lost = 1;
@@ -512,7 +514,6 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     for (int i = 0; S.at(i, t); ++i) {
       const Problem& p = P.p[t.p];
       const int M = t.p ? S.M[1] : S.M[0];
-      const uint32_t acc = two ? 0 : nt & 1, turn = two ? nt : nt >> 1;
       const int row0 = t.m0 + 128 * (int)rank + 32 * q, row = row0 + lane;
       // dz has rows of zeros behind the last: whole tiles
       const bool on = row0 < (MODE == DLOGIT ? p.M : M);
@@ -546,48 +547,28 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             if (F8) col_s[h] = col < p.N ? P.w_scale[col] : 0.f;
           }
       }
-      if (t.nkb > 0) {
+      // the next part of the sum is there
+      auto arrived = [&] {
         if (ok && lane == 0) {
-          ok = mbar_wait(tfull0 + 8 * acc, turn & 1, lost, P.wait_cycles) ? 1 : 0;
+          ok = mbar_wait(tfull0 + 8 * (nt & 1), (nt >> 1) & 1, lost, P.wait_cycles) ? 1 : 0;
           if (!ok) *lost = 1;
         }
         ok = __shfl_sync(0xffffffffu, ok, 0);
         tc_fence_after();
-        ++nt;
-      }
+      };
+      // it has been read: its accumulator may take the next part but one
+      auto release = [&] {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_remote(mapa0(tempty0 + 8 * (nt & 1)));
+      };
+      const uint32_t mine = tmem + ((uint32_t)(32 * q) << 16) + 128 * half;
       float best = -INFINITY, total = 0.f;  // STATS
-#pragma unroll 1
-      for (int j = 0; j < 2; ++j) {
+      // 64 columns of the warp's rows
+      auto leave = [&](int j, uint32_t(&r)[64]) {
         const int col0 = t.n0 + 128 * half + 64 * j;
         char* buf = stg + j * STG;
-        uint32_t r[64];
-        __syncwarp();
-        if (t.nkb > 0 && ok) {
-          const uint32_t at = tmem + ((uint32_t)(32 * q) << 16) + acc * BN + 128 * half + 64 * j;
-          tc_ld32_async(at, *reinterpret_cast<uint32_t(*)[32]>(r));
-          tc_ld32_async(at + 32, *reinterpret_cast<uint32_t(*)[32]>(r + 32));
-          tc_wait_ld();
-          if (MODE == STATS && two && t.nkb > 1) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              uint32_t s[32];
-              tc_ld32_async(at + BN + 32 * h, s);
-              tc_wait_ld();
-#pragma unroll
-              for (int e = 0; e < 32; ++e)
-                r[32 * h + e] = __float_as_uint(__uint_as_float(r[32 * h + e]) + __uint_as_float(s[e]));
-            }
-          }
-          if (j == 1) {  // the accumulator is read: the next tile but one may take its place
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) arrive_remote(mapa0(tempty0 + 8 * acc));
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 64; ++e) r[e] = ok ? 0u : __float_as_uint(nan);
-        }
-        if (col0 >= p.N || !on) continue;
+        if (col0 >= p.N || !on) return;
         if constexpr (MODE == STATS) {
           const int n = min(64, p.N - col0);
           if (P.keep) {
@@ -719,6 +700,58 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             for (int h = 0; h < 2; ++h) put_rows(buf, r + 32 * h, P.y, P.ldy, row0, M, col0 + 32 * h, p.N);
           }
         }
+      };
+      if constexpr (MODE == STATS) {
+        uint32_t r[2][64];
+        for (int k = 0; k < t.nkb; k += PART, ++nt) {
+          arrived();
+          if (!ok) continue;
+          const uint32_t at = mine + (nt & 1) * BN;
+          if (k == 0) {
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+              tc_ld32_async(at + 32 * h, *reinterpret_cast<uint32_t(*)[32]>(&r[h / 2][32 * (h & 1)]));
+            tc_wait_ld();
+          } else {
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+              uint32_t s[32];
+              tc_ld32_async(at + 32 * h, s);
+              tc_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 32; ++e) {
+                uint32_t& v = r[h / 2][32 * (h & 1) + e];
+                v = __float_as_uint(__uint_as_float(v) + __uint_as_float(s[e]));
+              }
+            }
+          }
+          release();
+        }
+        if (t.nkb == 0 || !ok) {
+#pragma unroll
+          for (int e = 0; e < 64; ++e) r[0][e] = r[1][e] = ok ? 0u : __float_as_uint(nan);
+        }
+        leave(0, r[0]);
+        leave(1, r[1]);
+      } else {
+        if (t.nkb > 0) arrived();
+#pragma unroll 1
+        for (int j = 0; j < 2; ++j) {
+          uint32_t r[64];
+          __syncwarp();
+          if (t.nkb > 0 && ok) {
+            const uint32_t at = mine + (nt & 1) * BN + 64 * j;
+            tc_ld32_async(at, *reinterpret_cast<uint32_t(*)[32]>(r));
+            tc_ld32_async(at + 32, *reinterpret_cast<uint32_t(*)[32]>(r + 32));
+            tc_wait_ld();
+            if (j == 1) release();
+          } else {
+#pragma unroll
+            for (int e = 0; e < 64; ++e) r[e] = ok ? 0u : __float_as_uint(nan);
+          }
+          leave(j, r);
+        }
+        if (t.nkb > 0) ++nt;
       }
       if (MODE == STATS && row < M && t.n0 + 128 * half < p.N)
         P.part[(long)(t.n0 / 128 + half) * P.part_ld + row] = make_float2(ok ? best : nan, total);
