@@ -662,10 +662,10 @@ LX_API lx_status lx_linear_backward(const lx_linear_desc* desc, const void* dy, 
  * lx_head_loss: softmax cross-entropy over the vocabulary from the last hidden states h and
  * the head's weights w, with its gradients, the logits not kept:
  *   z = h w^T,  loss_t = row_weight_t (log sum_v exp(z_tv) - z_t,label_t)
- *   dz_tv = row_weight_t (softmax(z_t)_v - [v = label_t]),  dh = dz w,  dw = dz^T h
+ *   dz_tv = softmax(z_t)_v - [v = label_t],  dh = row_weight (dz w),  dw = dz^T (row_weight h)
  * A token whose label is outside [0, V) or whose weight is 0 takes no part: loss 0, dh 0,
- * and its hidden state, whatever it holds, is not used.  dz is rounded to bf16 for the two
- * gradient products.
+ * and its hidden state, whatever it holds, is not used.  dz, and with weights row_weight h, are
+ * rounded to bf16 for the two gradient products.
  *   h bf16 [T][H] (rows ldh apart), w bf16 [V][H] (ldw): 16-byte aligned; H, ldh and ldw
  *   multiples of 8;  T up to 2^24 (0: dw is zeroed), V up to 2^24, H up to 2^20
  *   labels int32 [T];  row_weight fp32 [T] or NULL for 1 (a mean's 1 / n goes here)

@@ -1,7 +1,10 @@
 // Softmax cross-entropy over the vocabulary from the last hidden states and the head's
 // weights (lx_head_loss), without the logits:
 //   z = h W^T,  loss_t = w_t (log sum_v exp(z_tv) - z_t,label)
-//   dz_tv = w_t (softmax(z_t)_v - [v = label_t]),  dh = dz W,  dW = dz^T h
+//   dz_tv = softmax(z_t)_v - [v = label_t],  dh = w (dz W),  dW = dz^T (w h)
+// dz is rounded to bf16 as the tensor cores take it.  The weights stay outside of it: a label's
+// entry, which is most of its row, is then about -1 and loses next to nothing, where a row of one
+// or a few tokens showed the rounding of its weight in all of its gradient.
 // Tokens without a label (or of weight 0) take no part: the others' hidden states are copied
 // side by side first, so that they cost no products and what they hold reaches nothing.
 // Then (all products on lx_product.cuh):
@@ -37,7 +40,7 @@ struct Head {
   float* loss;
   __nv_bfloat16* dh;
   // compact
-  __nv_bfloat16* hc;
+  __nv_bfloat16 *hc, *hw;  // hidden states, and those times the weights (hc itself without weights)
   int *label, *row, *n;
   int* runs;  // rows that count of each RUN, where there are more
   float *weight, *lse2, *label_logit;
@@ -128,6 +131,11 @@ __global__ void __launch_bounds__(256) k_head_rows(const __grid_constant__ Head 
     for (int c = lane; c < pieces; c += 32) {
       const uint4 x = s[c], y = b[c];
       d[c] = x;
+      if (A.hw && A.hw != A.hc) {
+        const float2 f = both(weight);
+        ((uint4*)(A.hw + (long)before * A.H))[c] =
+            make_uint4(to_bf2(muls(bf2(x.x), f)), to_bf2(muls(bf2(x.y), f)), to_bf2(muls(bf2(x.z), f)), to_bf2(muls(bf2(x.w), f)));
+      }
       z = fmas(bf2(x.x), bf2(y.x), z);
       z = fmas(bf2(x.y), bf2(y.y), z);
       z = fmas(bf2(x.z), bf2(y.z), z);
@@ -148,8 +156,8 @@ __global__ void __launch_bounds__(256) k_head_rows(const __grid_constant__ Head 
     }
   }
   // rows of the last, ragged block of a sum over the tokens
-  if (t >= all && t < (all + 63) / 64 * 64) {
-    uint4* d = (uint4*)(A.hc + (long)t * A.H);
+  if (A.hw && t >= all && t < (all + 63) / 64 * 64) {
+    uint4* d = (uint4*)(A.hw + (long)t * A.H);
     for (int c = lane; c < pieces; c += 32) d[c] = make_uint4(0u, 0u, 0u, 0u);
   }
 }
@@ -234,11 +242,11 @@ __global__ void __launch_bounds__(256) k_head_dz(const __grid_constant__ Head A)
     for (int e = 0; e < 32; ++e) v[e] = b[32 * e];
   }
   const bool on = row < n;
-  const float weight = on ? A.weight[row] : 0.f, lse2 = on ? A.lse2[row] : 0.f;
+  const float lse2 = on ? A.lse2[row] : 0.f;
   const int label = on ? A.label[row] - 32 * cb : -1;
 #pragma unroll
   for (int e = 0; e < 32; ++e)
-    v[e] = on ? weight * (ex2(fmaf(v[e], LOG2E, -lse2)) - (label == e ? 1.f : 0.f)) : 0.f;
+    v[e] = on ? ex2(fmaf(v[e], LOG2E, -lse2)) - (label == e ? 1.f : 0.f) : 0.f;
   put_block(stage[warp], v, A.dl, A.ldd, 32 * cb, 32 * A.keep_cols, [&](int r) { return (long)rb * 32 + r; });
 }
 
@@ -248,11 +256,11 @@ size_t al(size_t v) { return (v + 255) / 256 * 256; }
 struct Plan {
   long Tp, piece;  // columns of a piece, a multiple of 256
   int slots, slices;
-  size_t hc, label, weight, row, lse2, label_logit, n, runs, part, dl, blocks, keep, bytes;
+  size_t hc, hw, label, weight, row, lse2, label_logit, n, runs, part, dl, blocks, keep, bytes;
   int keep_cols;   // blocks of kept logits side by side, 0: not kept
 };
 
-Plan plan_of(int T, int V, int H, bool dh, bool dw) {
+Plan plan_of(int T, int V, int H, bool dh, bool dw) {  // (the same with weights and without)
   Plan p = {};
   p.Tp = ((long)T + 255) / 256 * 256;
   const long nt = ((long)V + BN - 1) / BN;
@@ -268,6 +276,7 @@ Plan plan_of(int T, int V, int H, bool dh, bool dw) {
     return v;
   };
   p.hc = take(2 * (size_t)p.Tp * H);
+  if (dw) p.hw = take(2 * (size_t)p.Tp * H);
   p.label = take(4 * p.Tp);
   p.weight = take(4 * p.Tp);
   p.row = take(4 * p.Tp);
@@ -353,6 +362,7 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
   A.loss = loss;
   A.dh = (__nv_bfloat16*)dh;
   A.hc = (__nv_bfloat16*)(ws + L.hc);
+  A.hw = !dw ? nullptr : row_weight ? (__nv_bfloat16*)(ws + L.hw) : A.hc;
   A.label = (int*)(ws + L.label);
   A.row = (int*)(ws + L.row);
   A.n = (int*)(ws + L.n);
@@ -375,7 +385,6 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
   P.unmet = waits.unmet == LX_WAIT_CALL_PRODUCT;
   P.n = 1;
   P.label = A.label;
-  P.weight = A.weight;
   P.lse2 = A.lse2;
   P.part = (float2*)(ws + L.part);
   P.part_ld = L.Tp;
@@ -423,14 +432,14 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
         g.a_mn = 1;
         g.depth = A.n;
         ok = ok && boxes(&g.out, (__nv_bfloat16*)dw + v0 * H, H, n, H) &&
-             operand(&g.a, A.dl, n, L.Tp, L.piece, 2, true) && operand(&g.b, A.hc, H, L.Tp, H, 2, true);
+             operand(&g.a, A.dl, n, L.Tp, L.piece, 2, true) && operand(&g.b, A.hw, H, L.Tp, H, 2, true);
       }
     }
     if (!ok) return fail(LX_ERR_CUDA, "cuTensorMapEncodeTiled(head) failed");
     LX_TRY((launch_product<GRAD, false>(G, st)));
   }
   if (dh) {
-    const Join J = {(const float*)(ws + L.blocks), (int)L.Tp, H, L.slices, A.n, A.row, A.dh};
+    const Join J = {(const float*)(ws + L.blocks), (int)L.Tp, H, L.slices, A.n, A.row, A.weight, A.dh};
     LX_TRY(launch_join(J, st));
   }
   return LX_OK;

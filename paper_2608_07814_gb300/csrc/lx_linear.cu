@@ -566,7 +566,7 @@ extern "C" lx_status lx_linear_backward(const lx_linear_desc* d, const void* dy,
     p.slices = grad_slices(p.M, p.N, p.K);
     if (p.slices == 1) return boxes(&p.out, out, p.N, p.M, p.N);
     p.blocks = blocks;
-    joins[n_joins++] = Join{blocks, p.M, p.N, p.slices, nullptr, nullptr, (__nv_bfloat16*)out};
+    joins[n_joins++] = Join{blocks, p.M, p.N, p.slices, nullptr, nullptr, nullptr, (__nv_bfloat16*)out};
     blocks += grad_blocks(p.M, p.N, p.K) / 4;
     return true;
   };

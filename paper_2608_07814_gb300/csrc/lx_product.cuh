@@ -88,9 +88,9 @@ struct Launch : Epilogue {
   // LINEAR
   int tma_r, tma_y, tma_p;  // whether the residual's, y's and pre's rows suit TMA (boxes of 128 bytes x 32 rows):
   CUtensorMap map_r, map_y, map_p;
-  // DLOGIT: compact rows' labels, weights and log-sum-exps (in units of log 2)
+  // DLOGIT: compact rows' labels and log-sum-exps (in units of log 2)
   const int* label;
-  const float *weight, *lse2;
+  const float* lse2;
   CUtensorMap map_dl;  // dz of the piece
   int v0;            // the first column's place in the vocabulary
   // STATS
@@ -534,9 +534,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
       // what the tile needs besides its sums, on the way while those are formed: the row's, and
       // the scales and biases of the columns 32 h + lane
       int label = -1;
-      float weight = 0.f, lse2 = 0.f, xs = 1.f, col_s[4];
+      float lse2 = 0.f, xs = 1.f, col_s[4];
       __nv_bfloat16 col_b[4];
-      if (MODE == DLOGIT && row < M) label = P.label[row] - P.v0, weight = P.weight[row], lse2 = P.lse2[row];
+      if (MODE == DLOGIT && row < M) label = P.label[row] - P.v0, lse2 = P.lse2[row];
       if (MODE == LINEAR) {
         if (F8 && row < M) xs = P.x_scale[row];
         if (F8 || P.bias)
@@ -597,7 +597,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
           const int at = label - col0;
 #pragma unroll
           for (int e = 0; e < 64; ++e) {
-            const float d = weight * (rows::ex2(fmaf(__uint_as_float(r[e]), LOG2E, -lse2)) - (at == e ? 1.f : 0.f));
+            const float d = rows::ex2(fmaf(__uint_as_float(r[e]), LOG2E, -lse2)) - (at == e ? 1.f : 0.f);
             r[e] = row < M ? __float_as_uint(d) : 0u;
           }
           box_free(j);
@@ -796,7 +796,8 @@ struct Join {
   const float* blocks;
   int M, N, slices;   // as the product's
   const int* rows;    // device count that bounds M, or NULL
-  const int* place;   // a row's place, or NULL: itself
+  const int* place;   // a row's place, or NULL: itself,
+  const float* scale; // and factor, or NULL: 1
   __nv_bfloat16* out; // rows of N (a multiple of 8)
 };
 __global__ void __launch_bounds__(256) k_join(const __grid_constant__ Join A) {
@@ -814,8 +815,9 @@ __global__ void __launch_bounds__(256) k_join(const __grid_constant__ Join A) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] += b[s * slice + 32 * e];
   }
-  *(uint2*)&stage[lane][4 * warp] =
-      make_uint2(rows::to_bf2(make_float2(v[0], v[1])), rows::to_bf2(make_float2(v[2], v[3])));
+  const float f = A.scale && rb * 32 + lane < n ? A.scale[rb * 32 + lane] : 1.f;
+  *(uint2*)&stage[lane][4 * warp] = make_uint2(rows::to_bf2(make_float2(v[0] * f, v[1] * f)),
+                                               rows::to_bf2(make_float2(v[2] * f, v[3] * f)));
   __syncthreads();
   const int r = threadIdx.x / 4, c = 8 * (threadIdx.x % 4), row = rb * 32 + r;
   if (threadIdx.x < 128 && row < n && cb * 32 + c < A.N)

@@ -3,7 +3,7 @@
 Bounds.  A logit of H terms is off by (H / 16 + 16) 2^-23 of its terms' magnitudes (the tensor
 core's sums, see test_gpu_linear), e at most over the rows; a loss by 2 e and 2^-20 of its parts;
 a softmax by 2 e + 2^-19 of itself; dz is rounded to bf16 (2^-8 of each term of the gradients'
-sums), and so are dh and dw."""
+sums), and so are, for dw, the hidden states times the weights (as much again), dh and dw."""
 import numpy as np
 import pytest
 import torch
@@ -45,7 +45,8 @@ def _check(got, h, w, labels, weight=None):
         err = term @ np.abs(W) + mm(V) * (np.abs(dz) @ np.abs(W))
         assert (np.abs(f64(got.dh) - dh) <= err * 1.01 + R * np.abs(dh) + 1e-37).all()
     if got.dw is not None:
-        err = term.T @ np.abs(used) + mm(T) * (np.abs(dz).T @ np.abs(used))
+        weighted = 0 if weight is None else R * (1 + R) * (np.abs(dz).T @ np.abs(used))
+        err = term.T @ np.abs(used) + weighted + mm(T) * (np.abs(dz).T @ np.abs(used))
         assert (np.abs(f64(got.dw) - dw) <= err * 1.01 + R * np.abs(dw) + 1e-37).all()
 
 
