@@ -150,6 +150,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) k_linear_few(const __grid_cons
       if (c + e < T) part[(c + e) * 128 + 32 * q + lane] = __uint_as_float(r[e]);
   }
   tc_fence_before();
+  __syncwarp();
   if (splits > 1) cluster_sync();
   else __syncthreads();
   const Epilogue& E = P.e;
@@ -200,6 +201,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) k_linear_few(const __grid_cons
         }
     }
   }
+  __syncwarp();
   if (splits > 1) cluster_sync();  // a CTA's shared memory outlives its neighbours' reads
   else __syncthreads();
   if (warp == 1) {
