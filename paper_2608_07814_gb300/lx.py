@@ -829,18 +829,21 @@ _ACTS = {"none": LX_ACT_NONE, "relu": LX_ACT_RELU, "silu": LX_ACT_SILU, "gelu": 
 _LINEAR_TYPES = {torch.bfloat16: LX_BF16, torch.float8_e4m3fn: LX_E4M3}
 
 
-def _linear_desc(dev, x, w, act):
-    code = _LINEAR_TYPES.get(x.dtype)
+def _linear_args(dev, x, w, act):
+    """(type, T, N, K, activation, ldx, ldw): what a product is described by."""
+    dtype = x.dtype
+    code = _LINEAR_TYPES.get(dtype)
     if code is None:
         raise ValueError("x must be bf16 or e4m3")
-    if act not in _ACTS:
+    a = _ACTS.get(act)
+    if a is None:
         raise ValueError("act must be one of " + ", ".join(_ACTS))
-    ldx = _rows(x, "x", dev)
+    ldx, ldw = _rows(x, "x", dev), _rows(w, "w", dev, None, dtype)
     T, K = x.shape
-    ldw = _rows(w, "w", dev, None, x.dtype)
-    if w.shape[1] != K:
+    N, k = w.shape
+    if k != K:
         raise ValueError(f"w must be [N, {K}]")
-    return LinearDesc(code, T, w.shape[0], K, _ACTS[act], ldx, ldw, 0, x.data_ptr(), w.data_ptr())
+    return code, T, N, K, a, ldx, ldw
 
 
 def linear(x: torch.Tensor, w: torch.Tensor, *, x_scale=None, w_scale=None, bias=None, act: str = "none",
@@ -856,19 +859,29 @@ def linear(x: torch.Tensor, w: torch.Tensor, *, x_scale=None, w_scale=None, bias
         return _elsewhere(stream, linear, (x, w), dict(x_scale=x_scale, w_scale=w_scale, bias=bias, act=act,
                                                        residual=residual, y=y, pre=pre))
     dev = _device(x, "x")
-    d = _linear_desc(dev, x, w, act)
-    T, N, bf = d.T, d.N, torch.bfloat16
-    if (x_scale is None) != (d.dtype == LX_BF16) or (w_scale is None) != (d.dtype == LX_BF16):
+    code, T, N, K, a, ldx, ldw = _linear_args(dev, x, w, act)
+    bf = torch.bfloat16
+    xs = ws = bp = rp = pp = None
+    if code == LX_E4M3:
+        if x_scale is None or w_scale is None:
+            raise ValueError("x_scale and w_scale go with e4m3")
+        xs, ws = _flat(x_scale, "x_scale", dev, T), _flat(w_scale, "w_scale", dev, N)
+    elif x_scale is not None or w_scale is not None:
         raise ValueError("x_scale and w_scale go with e4m3")
-    d.x_scale, d.w_scale = _flat(x_scale, "x_scale", dev, T), _flat(w_scale, "w_scale", dev, N)
-    d.bias = _flat(bias, "bias", dev, N, bf)
+    if bias is not None:
+        bp = _flat(bias, "bias", dev, N, bf)
+    ldr = 0
     if residual is not None:
-        d.ldr, d.residual = _rows(residual, "residual", dev, (T, N), bf), residual.data_ptr()
+        ldr, rp = _rows(residual, "residual", dev, (T, N), bf), residual.data_ptr()
+    if pre is not None:
+        pp = _flat(pre, "pre", dev, T * N, bf)
     if y is None:
         y, ldy = torch.empty((T, N), dtype=bf, device=x.device), N
     else:
         ldy = _rows(y, "y", dev, (T, N), bf)
-    status = lib().lx_linear(d, y.data_ptr(), ldy, _flat(pre, "pre", dev, T * N, bf), _raw_stream(dev))
+    status = lib().lx_linear(
+        LinearDesc(code, T, N, K, a, ldx, ldw, ldr, x.data_ptr(), w.data_ptr(), xs, ws, bp, rp), y.data_ptr(), ldy, pp,
+        _raw_stream(dev))
     if status:
         _check(status)
     return y
@@ -896,8 +909,8 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, *, act: 
         return _elsewhere(stream, linear_backward, (dy, x, w), dict(
             act=act, pre=pre, want_dx=want_dx, want_dw=want_dw, want_dbias=want_dbias, workspace=workspace))
     dev = _device(x, "x")
-    d = _linear_desc(dev, x, w, act)
-    T, N, K, bf = d.T, d.N, d.K, torch.bfloat16
+    code, T, N, K, a, ldx, ldw = _linear_args(dev, x, w, act)
+    bf = torch.bfloat16
     lddy = _rows(dy, "dy", dev, (T, N), bf)
     dx, p0 = _empty_for(x if want_dx else None, (T, K))
     dw, p1 = _empty_for(w if want_dw else None, (N, K))
@@ -906,6 +919,7 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, *, act: 
         workspace = torch.empty(linear_workspace_bytes(T, N, K), dtype=torch.uint8, device=x.device)
     else:
         _check_workspace(workspace, dev)
+    d = LinearDesc(code, T, N, K, a, ldx, ldw, 0, x.data_ptr(), w.data_ptr())
     status = lib().lx_linear_backward(d, dy.data_ptr(), lddy, _flat(pre, "pre", dev, T * N, bf), p0, p1, p2,
                                       workspace.data_ptr(), workspace.nbytes, _raw_stream(dev))
     if status:
