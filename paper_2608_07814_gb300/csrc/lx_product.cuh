@@ -370,7 +370,7 @@ __device__ __forceinline__ float column_sum(const float* part, int chunks, int n
 // 2048 is 1e-6 to 4e-6 of itself short.  That is lost in a bf16 output, but not in a loss: the logits'
 // statistics are taken of sums in parts of 1024 terms (16 blocks of K), each in an accumulator of
 // its own, added as fp32 on their way out.  (Losses were 8e-7 off, at 2560 terms 1.2e-6, and are
-// 4e-7; it costs these tiles 4 %.  In the gradients' tiles the registers for it cost 10 to 50 %.)
+// 4e-7; it costs these tiles 3 %.  In the gradients' tiles the registers for it cost 10 to 50 %.)
 template <int MODE, bool F8>
 __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ Launch P) {
   constexpr int PART = MODE == STATS ? 16 : 1 << 30;
@@ -714,13 +714,13 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             tc_wait_ld();
           } else {
 #pragma unroll
-            for (int h = 0; h < 4; ++h) {
-              uint32_t s[32];
-              tc_ld32_async(at + 32 * h, s);
+            for (int h = 0; h < 8; ++h) {
+              uint32_t s[16];
+              tc_ld16_async(at + 16 * h, s);
               tc_wait_ld();
 #pragma unroll
-              for (int e = 0; e < 32; ++e) {
-                uint32_t& v = r[h / 2][32 * (h & 1) + e];
+              for (int e = 0; e < 16; ++e) {
+                uint32_t& v = r[h / 4][16 * (h & 3) + e];
                 v = __float_as_uint(__uint_as_float(v) + __uint_as_float(s[e]));
               }
             }
