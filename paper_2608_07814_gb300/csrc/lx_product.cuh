@@ -113,6 +113,25 @@ static __device__ __forceinline__ uint32_t cluster_rank() {
 static __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// A bounded wait (see mbar_wait) whose tries suspend the thread for up to 0.2 ms instead of
+// polling: what the many waiting warps read of shared memory the products would have to wait for.
+static __device__ __forceinline__ bool wait_quiet(uint32_t bar, uint32_t parity, volatile int* lost,
+                                                  unsigned long long limit) {
+  const unsigned long long t0 = clock64();
+  while (true) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "r"(200000u)
+        : "memory");
+    if (ok) return true;
+    if (lost && *lost) return false;
+    if (clock64() - t0 > limit) return false;
+  }
+}
 static __device__ __forceinline__ void arrive_remote(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
@@ -422,7 +441,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
         const int m = t.m0 + 128 * (int)rank, n = t.n0 + 128 * (int)rank;
         for (int k = 0; k < t.nkb; ++k, ++it) {
           const uint32_t s = it % STAGES;
-          if (!mbar_wait(empty0 + 8 * s, ((it / STAGES) & 1) ^ 1, lost, P.wait_cycles)) {
+          if (!wait_quiet(empty0 + 8 * s, ((it / STAGES) & 1) ^ 1, lost, P.wait_cycles)) {
             ok = false;
             break;
           }
@@ -445,20 +464,20 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
       }
       // the commits of the last stages have arrived before the CTA may end
       for (uint32_t j = it > STAGES ? it - STAGES : 0; ok && j < it; ++j)
-        ok = mbar_wait(empty0 + 8 * (j % STAGES), (j / STAGES) & 1, lost, P.wait_cycles);
+        ok = wait_quiet(empty0 + 8 * (j % STAGES), (j / STAGES) & 1, lost, P.wait_cycles);
       if (!ok) {
         *lost = 1;
         // copies in flight land before shared memory goes away (both CTAs': the even one's
         // barriers count them)
         if (rank == 0)
           for (uint32_t j = it > STAGES ? it - STAGES : 0; j < it; ++j)
-            mbar_wait(full0 + 8 * (j % STAGES), (j / STAGES) & 1, nullptr, P.wait_cycles);
+            wait_quiet(full0 + 8 * (j % STAGES), (j / STAGES) & 1, nullptr, P.wait_cycles);
       }
     }
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
       uint32_t it = 0, nt = 0;
-      bool ok = !P.unmet || mbar_wait(drain, 0, lost, P.wait_cycles);
+      bool ok = !P.unmet || wait_quiet(drain, 0, lost, P.wait_cycles);
       for (int i = 0; ok && S.at(i, t); ++i) {
         if (t.nkb == 0) continue;
         const Problem& p = P.p[t.p];
@@ -468,12 +487,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
           const uint32_t s = it % STAGES;
           if (k % PART == 0) {  // an accumulator for the next part of the sum
             if (k) commit_pair(tfull0 + 8 * (nt++ & 1), 3);
-            ok = mbar_wait(tempty0 + 8 * (nt & 1), ((nt >> 1) & 1) ^ 1, lost, P.wait_cycles);
+            ok = wait_quiet(tempty0 + 8 * (nt & 1), ((nt >> 1) & 1) ^ 1, lost, P.wait_cycles);
             if (!ok) break;
             tc_fence_after();
             d = tmem + (nt & 1) * BN;
           }
-          ok = mbar_wait(full0 + 8 * s, (it / STAGES) & 1, lost, P.wait_cycles);
+          ok = wait_quiet(full0 + 8 * s, (it / STAGES) & 1, lost, P.wait_cycles);
           if (!ok) break;
           tc_fence_after();
           const uint32_t as = base + s * STAGE, bs = as + A_BYTES;
@@ -490,7 +509,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
       if (!ok) {
         *lost = 1;
         commit_pair(drain, 1);  // no product is in flight when TMEM is freed
-        mbar_wait(drain, 0, nullptr, P.wait_cycles);
+        wait_quiet(drain, 0, nullptr, P.wait_cycles);
       }
     }
   } else if (MODE == GRAD && warp < 4) {
@@ -550,7 +569,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
       // the next part of the sum is there
       auto arrived = [&] {
         if (ok && lane == 0) {
-          ok = mbar_wait(tfull0 + 8 * (nt & 1), (nt >> 1) & 1, lost, P.wait_cycles) ? 1 : 0;
+          ok = wait_quiet(tfull0 + 8 * (nt & 1), (nt >> 1) & 1, lost, P.wait_cycles) ? 1 : 0;
           if (!ok) *lost = 1;
         }
         ok = __shfl_sync(0xffffffffu, ok, 0);
@@ -665,8 +684,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             if (P.tma_r) {
               int got = 1;
               if (lane == 0)
-                got = mbar_wait(res + 8 * j, (res_turn >> j) & 1, nullptr, P.wait_cycles) ||
-                      mbar_wait(res + 8 * j, (res_turn >> j) & 1, nullptr, P.wait_cycles);
+                got = wait_quiet(res + 8 * j, (res_turn >> j) & 1, nullptr, P.wait_cycles) ||
+                      wait_quiet(res + 8 * j, (res_turn >> j) & 1, nullptr, P.wait_cycles);
               got = __shfl_sync(0xffffffffu, got, 0);
               res_turn ^= 1u << j;
               if (!got) {
