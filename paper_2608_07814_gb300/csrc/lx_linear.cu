@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) k_linear_few(const __grid_cons
     if (lane == 0)
       for (int i = 0; i < nkb; ++i) {
         const uint32_t s = i % P.stages, bar = full0 + 8 * s, as = base + s * stage;
-        if (!mbar_wait(empty0 + 8 * s, ((i / P.stages) & 1) ^ 1, lost, P.e.wait_cycles)) {
+        if (!wait_quiet(empty0 + 8 * s, ((i / P.stages) & 1) ^ 1, lost, P.e.wait_cycles)) {
           *lost = 1;
           break;
         }
@@ -99,10 +99,10 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) k_linear_few(const __grid_cons
   } else if (warp == 1) {
     if (lane == 0) {
       const uint32_t id = idesc(F8, 0, 0, 128, P.tn);
-      bool ok = !P.e.unmet || mbar_wait(done, 0, lost, P.e.wait_cycles);
+      bool ok = !P.e.unmet || wait_quiet(done, 0, lost, P.e.wait_cycles);
       for (int i = 0; ok && i < nkb; ++i) {
         const uint32_t s = i % P.stages, as = base + s * stage, bs = as + A_BYTES;
-        if (!mbar_wait(full0 + 8 * s, (i / P.stages) & 1, lost, P.e.wait_cycles)) {
+        if (!wait_quiet(full0 + 8 * s, (i / P.stages) & 1, lost, P.e.wait_cycles)) {
           ok = false;
           break;
         }
@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) k_linear_few(const __grid_cons
   // made), a token's 128 outputs a row; warp w reads TMEM lanes 32 (w % 4) ..
   int ok = 1;
   if (lane == 0) {
-    ok = mbar_wait(done, 0, nullptr, 2 * P.e.wait_cycles) ? 1 : 0;  // (the issuer may have waited for the bound)
+    ok = wait_quiet(done, 0, nullptr, 2 * P.e.wait_cycles) ? 1 : 0;  // (the issuer may have waited for the bound)
     if (!ok) *lost = 1;
     else if (*lost) ok = 0;
   }
@@ -131,7 +131,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) k_linear_few(const __grid_cons
     // copies in flight land before the sums take their place
     const uint32_t first = issued > (uint32_t)P.stages ? issued - P.stages : 0;
     for (uint32_t j = first; j < issued; ++j)
-      mbar_wait(full0 + 8 * (j % P.stages), (j / P.stages) & 1, nullptr, P.e.wait_cycles);
+      wait_quiet(full0 + 8 * (j % P.stages), (j / P.stages) & 1, nullptr, P.e.wait_cycles);
   }
   __syncthreads();
   float* part = reinterpret_cast<float*>(smem);

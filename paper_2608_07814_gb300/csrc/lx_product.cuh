@@ -37,21 +37,32 @@ using namespace tcg;
 
 constexpr int BM = 256, BN = 256;      // a pair's tile
 constexpr int KB = 128;                // bytes of K a stage: 64 bf16 or 128 e4m3
-constexpr int A_BYTES = 128 * KB, STAGE = 2 * A_BYTES, STAGES = 5;
+constexpr int A_BYTES = 128 * KB, STAGE = 2 * A_BYTES;
 constexpr int EPI = 8, THREADS = 128 + 32 * EPI;
-// Blocks of 32 rows x 64 columns leave a warp through two buffers of 4 KiB (128-byte rows,
+// Blocks of 32 rows x 64 columns leave a warp through buffers of 4 KiB (128-byte rows,
 // 128-byte swizzle) by TMA: stores of 16 bytes a lane took 1.8 k cycles for 32 x 32, four
 // times what the products of 64 inputs take.
 constexpr int STG = 4096, PRM = 192;
 constexpr int STG_LD = 80;             // rows TMA cannot take: 32 bf16, 16-byte pieces of 8 rows on distinct banks
-constexpr int N_BARS = 2 * STAGES + 5 + 2 * EPI;
-constexpr int SMEM = STAGES * STAGE + EPI * (2 * STG + PRM) + 8 * N_BARS + 16 + 1024;
-constexpr int GROUP_M = 8, MAX_SLICES = 16;
+constexpr int GROUP_M = 16, MAX_SLICES = 16;
 constexpr int LEAVING = 5;  // blocks of K whose products take as long as a tile's way out (1.9 us)
-static_assert(SMEM <= 227 * 1024, "fits an SM");
 
 enum Mode { LINEAR = 0, STATS = 1, DLOGIT = 2, GRAD = 3 };
 enum Act { NONE = 0, RELU = 1, SILU = 2, GELU = 3 };
+
+// What the stages and an epilogue warp's buffers make of an SM's shared memory.  DEEP: six stages and
+// one buffer, else five and two, which a residual and the sums before the activation pass through.
+// (8192 x 8192 x 2048: 155.6 us with six, 159.2 with five, 179.9 with four.  The gradients show no
+// difference between six and five, not of short sums either, and the statistics none above five.)
+template <int MODE, bool DEEP>
+struct Cfg {
+  static constexpr int NBUF = MODE == STATS ? 0 : DEEP ? 1 : 2;
+  static constexpr int STAGES = MODE == STATS ? 5 : DEEP ? 6 : 5;
+  static constexpr int PARAMS = MODE == LINEAR ? PRM : 0;
+  static constexpr int BARS = 2 * STAGES + 5 + (MODE == LINEAR && !DEEP ? 2 * EPI : 0);
+  static constexpr int SMEM = STAGES * STAGE + EPI * (NBUF * STG + PARAMS) + 8 * BARS + 16 + 1024;
+  static_assert(SMEM <= 227 * 1024, "fits an SM");
+};
 
 // One product of a launch.  Its tiles: slices (ranges of K) x tiles of N x tiles of M.
 struct Problem {
@@ -390,17 +401,20 @@ __device__ __forceinline__ float column_sum(const float* part, int chunks, int n
 // statistics are taken of sums in parts of 1024 terms (16 blocks of K), each in an accumulator of
 // its own, added as fp32 on their way out.  (Losses were 8e-7 off, at 2560 terms 1.2e-6, and are
 // 4e-7; it costs these tiles 3 %.  In the gradients' tiles the registers for it cost 10 to 50 %.)
-template <int MODE, bool F8>
+template <int MODE, bool F8, bool DEEP>
 __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ Launch P) {
+  using C = Cfg<MODE, DEEP>;
+  constexpr int STAGES = C::STAGES, NBUF = C::NBUF;
+  constexpr bool PASS = MODE == LINEAR && !DEEP;  // takes a residual and keeps the sums
   constexpr int PART = MODE == STATS ? 16 : 1 << 30;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   char* staged = reinterpret_cast<char*>(smem + STAGES * STAGE);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(staged + EPI * (2 * STG + PRM));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(staged + EPI * (NBUF * STG + C::PARAMS));
   const uint32_t base = smem_u32(smem), full0 = smem_u32(bars), empty0 = full0 + 8 * STAGES;
   const uint32_t tfull0 = empty0 + 8 * STAGES, tempty0 = tfull0 + 16, drain = tempty0 + 16, res0 = drain + 8;
-  volatile int* lost = reinterpret_cast<volatile int*>(bars + N_BARS);
-  uint32_t* tmem_s = reinterpret_cast<uint32_t*>(bars + N_BARS + 1);
+  volatile int* lost = reinterpret_cast<volatile int*>(bars + C::BARS);
+  uint32_t* tmem_s = reinterpret_cast<uint32_t*>(bars + C::BARS + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
 
@@ -414,7 +428,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
       mbar_init(tempty0 + 8 * b, 2 * EPI);      // the even CTA's: both CTAs' epilogue warps
     }
     mbar_init(drain, 1);
-    for (int i = 0; i < 2 * EPI; ++i) mbar_init(res0 + 8 * i, 1);
+    if (PASS)
+      for (int i = 0; i < 2 * EPI; ++i) mbar_init(res0 + 8 * i, 1);
     *lost = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -517,8 +532,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
       P.db[c] = __float2bfloat16_rn(column_sum(P.db_part, P.db_chunks, P.db_n, c));
   } else if (warp >= 4) {
     const int q = warp & 3, half = (warp - 4) >> 2;
-    char* stg = staged + (warp - 4) * 2 * STG;
-    float* prm = reinterpret_cast<float*>(staged + EPI * 2 * STG + (warp - 4) * PRM);  // scales, then the bias
+    char* stg = staged + (warp - 4) * NBUF * STG;
+    float* prm = reinterpret_cast<float*>(staged + EPI * NBUF * STG + (warp - 4) * C::PARAMS);  // scales, then the bias
     __nv_bfloat16* prm_b = reinterpret_cast<__nv_bfloat16*>(prm + 32);
     const uint32_t res = res0 + 16 * (warp - 4);
     uint32_t res_turn = 0;  // bit j: phase of buffer j's barrier
@@ -526,7 +541,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
     uint32_t nt = 0;
     int ok = 1, last = -1;  // the buffer that the last box left from
     auto box_free = [&](int j) {
-      if (last == j) box_wait<0>();
+      if (NBUF < 2 || last == j) box_wait<0>();
       else box_wait<1>();
       last = j;
     };
@@ -545,7 +560,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
           tma_load_2d(smem_u32(stg + j * STG), &P.map_r, 2 * (t.n0 + 128 * half + 64 * j), row0, res + 8 * j);
         }
       };
-      const bool ahead = MODE == LINEAR && P.tma_r && on;
+      const bool ahead = PASS && P.tma_r && on;
       if (ahead) {
         if (t.n0 + 128 * half < p.N) fetch(0);
         if (!P.pre && t.n0 + 128 * half + 64 < p.N) fetch(1);
@@ -586,7 +601,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
       // 64 columns of the warp's rows
       auto leave = [&](int j, uint32_t(&r)[64]) {
         const int col0 = t.n0 + 128 * half + 64 * j;
-        char* buf = stg + j * STG;
+        char* buf = stg + (NBUF == 2 ? j * STG : 0);
         if (col0 >= p.N || !on) return;
         if constexpr (MODE == STATS) {
           const int n = min(64, p.N - col0);
@@ -642,7 +657,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             put_box(buf, r, &p.out, col0, row0);
           }
         } else {
-          if (ahead && P.pre && j == 1) fetch(1);
+          if (PASS && ahead && P.pre && j == 1) fetch(1);
           // TMA stores whole pieces of 16 bytes: a last block that ends inside one goes by columns
           const bool whole = col0 + 64 <= p.N || p.N % 8 == 0;
           // the columns' scale and bias, handed to all lanes
@@ -670,7 +685,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
               }
             }
           }
-          if (P.pre) {  // through the other buffer
+          if (PASS && P.pre) {  // through the other buffer
             box_wait<0>();
             if (P.tma_p && whole) {
               put_box(stg + (j ^ 1) * STG, r, &P.map_p, col0, row0);
@@ -680,7 +695,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             }
           }
           activate(P.act, reinterpret_cast<float(&)[64]>(r));
-          if (P.residual) {
+          if (PASS && P.residual) {
             if (P.tma_r) {
               int got = 1;
               if (lane == 0)
@@ -711,7 +726,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             }
           }
           if (P.tma_y && whole) {
-            if (!P.pre && !ahead) box_free(j);  // (else the buffer has been waited for)
+            if (!PASS || (!P.pre && !ahead)) box_free(j);  // (else the buffer has been waited for)
             put_box(buf, r, &P.map_y, col0, row0);
           } else {
             box_wait<0>();
@@ -864,17 +879,24 @@ inline long tiles_of(const Problem& p) {
   return (long)((p.M + BM - 1) / BM) * ((p.N + BN - 1) / BN) * p.slices;
 }
 
-template <int MODE, bool F8>
-lx_status launch_product(const Launch& P, cudaStream_t st) {
+template <int MODE, bool F8, bool DEEP>
+lx_status launch_as(const Launch& P, unsigned pairs, cudaStream_t st) {
   static bool cap[64] = {};
   int dev = 0;
   LX_CUDA(cudaGetDevice(&dev));
-  LX_CUDA(smem_cap_once((const void*)k_product<MODE, F8>, SMEM, dev, cap));
+  LX_CUDA(smem_cap_once((const void*)k_product<MODE, F8, DEEP>, Cfg<MODE, DEEP>::SMEM, dev, cap));
+  return launch_after(k_product<MODE, F8, DEEP>, dim3(2 * pairs), dim3(THREADS), Cfg<MODE, DEEP>::SMEM, 2, st, P);
+}
+
+template <int MODE, bool F8>
+lx_status launch_product(const Launch& P, cudaStream_t st) {
   long tiles = 0;
   for (int i = 0; i < P.n; ++i) tiles += tiles_of(P.p[i]);
   if (tiles == 0) return LX_OK;
   const unsigned pairs = (unsigned)std::min<long>(tiles, rows::SMS / 2);
-  return launch_after(k_product<MODE, F8>, dim3(2 * pairs), dim3(THREADS), SMEM, 2, st, P);
+  if constexpr (MODE == LINEAR)
+    if (P.residual || P.pre) return launch_as<MODE, F8, false>(P, pairs, st);
+  return launch_as<MODE, F8, true>(P, pairs, st);
 }
 
 }  // namespace
