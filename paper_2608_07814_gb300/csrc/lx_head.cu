@@ -9,15 +9,17 @@
 // side by side first, so that they cost no products and what they hold reaches nothing.
 // Then (all products on lx_product.cuh):
 //   1  the logits' tiles, of which each keeps a row's largest value and sum of exponentials
-//      (fp32), 8 bytes for 128 logits;
-//   2  each row's log-sum-exp and loss;
+//      (fp32), 8 bytes for 128 logits, and one of them the label's logit;
+//   2  each row's log-sum-exp and loss, (largest - label's) + log of the sum: what a sure row's
+//      is made of is not the difference of two large numbers, and no loss is below 0;
 //   3  by pieces of the vocabulary: the logits again, now turned into dz (bf16) on their way out
 //      of the tensor core, and the two gradient products of the piece in one launch.  dh is
 //      held in fp32 between the pieces.
 // With the logits formed twice that is 8 T V H operations against the 6 that a kept [T][V]
-// needs, and a workspace that does not grow with T V.  Where all logits fit, as fp32, into the
-// room of a piece, they are kept there and step 3 reads them instead of W: few tokens would
-// spend as long on reading W again as on everything else.
+// needs, and a workspace that grows with T V by those 8 bytes alone.  The label's dz comes from step
+// 2 as well, from its loss.  Where all logits fit, as fp32, into the room of a piece, they are kept
+// there and step 3 reads them instead of W: few tokens would spend as long on reading W again as on
+// everything else.
 #include "lx_product.cuh"
 
 namespace lx {
@@ -33,8 +35,8 @@ constexpr int MAX_T = 1 << 24, MAX_V = 1 << 24, MAX_H = 1 << 20;
 
 struct Head {
   int T, V, H, Tp;  // Tp: rows of the compact arrays, a multiple of 256
-  const __nv_bfloat16 *h, *w;
-  long ldh, ldw;
+  const __nv_bfloat16* h;
+  long ldh;
   const int* labels;
   const float* row_weight;
   float* loss;
@@ -43,7 +45,8 @@ struct Head {
   __nv_bfloat16 *hc, *hw;  // hidden states, and those times the weights (hc itself without weights)
   int *label, *row, *n;
   int* runs;  // rows that count of each RUN, where there are more
-  float *weight, *lse2, *label_logit;
+  float *weight, *lse2;
+  float* own;           // the label's logit, then its dz
   const float2* part;
   int slots;
   const float* keep;    // the logits, keep_cols blocks side by side
@@ -81,15 +84,12 @@ __global__ void __launch_bounds__(256) k_head_runs(const __grid_constant__ Head 
 
 // The rows that count, side by side in their order; loss and dh of the others are 0.  Each CTA
 // counts the rows before its own and all of them by itself, so that one launch does, or takes
-// whole runs of them from k_head_runs.  A row's label's logit is formed here, in fp32: the tensor core cuts its running sums off
-// instead of rounding them, 4e-6 of a logit of 2048 terms, which a loss shows and its
-// gradient does not.
+// whole runs of them from k_head_runs.
 __global__ void __launch_bounds__(256) k_head_rows(const __grid_constant__ Head A) {
   __shared__ int red[2][8];
   __shared__ int live[ROWS];
   pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t0 = blockIdx.x * ROWS, t = t0 + warp;
-  // the warp's row and its label's row of W, while the rows are counted
   const int pieces = A.H / 8, label = t < A.T ? A.labels[t] : -1;
   const float weight = t < A.T ? (A.row_weight ? A.row_weight[t] : 1.f) : 0.f;
   const bool mine = label >= 0 && label < A.V && weight != 0.f;
@@ -124,29 +124,21 @@ __global__ void __launch_bounds__(256) k_head_rows(const __grid_constant__ Head 
   if (blockIdx.x == 0 && threadIdx.x == 0) *A.n = all;
   if (mine) {
     const uint4* s = (const uint4*)(A.h + (long)t * A.ldh);
-    const uint4* b = (const uint4*)(A.w + (long)label * A.ldw);
     uint4* d = (uint4*)(A.hc + (long)before * A.H);
-    float2 z = make_float2(0.f, 0.f);
 #pragma unroll 8
     for (int c = lane; c < pieces; c += 32) {
-      const uint4 x = s[c], y = b[c];
+      const uint4 x = s[c];
       d[c] = x;
       if (A.hw && A.hw != A.hc) {
         const float2 f = both(weight);
         ((uint4*)(A.hw + (long)before * A.H))[c] =
             make_uint4(to_bf2(muls(bf2(x.x), f)), to_bf2(muls(bf2(x.y), f)), to_bf2(muls(bf2(x.z), f)), to_bf2(muls(bf2(x.w), f)));
       }
-      z = fmas(bf2(x.x), bf2(y.x), z);
-      z = fmas(bf2(x.y), bf2(y.y), z);
-      z = fmas(bf2(x.z), bf2(y.z), z);
-      z = fmas(bf2(x.w), bf2(y.w), z);
     }
-    const float dot = warp_sum(z.x + z.y);
     if (lane == 0) {
       A.label[before] = label;
       A.weight[before] = weight;
       A.row[before] = t;
-      A.label_logit[before] = dot;
     }
   } else if (t < A.T) {
     if (lane == 0) A.loss[t] = 0.f;
@@ -174,10 +166,10 @@ __global__ void __launch_bounds__(1024) k_head_lse(const __grid_constant__ Head 
     float m = v.x;
 #pragma unroll
     for (int j = 0; j < 8; ++j) m = fmaxf(m, p[j].x);
-    const float at = m == -INFINITY ? 0.f : m * LOG2E;
-    float s = v.y * ex2(fmaf(v.x, LOG2E, -at));
+    const float at = m == -INFINITY ? 0.f : m;
+    float s = v.y * ex2((v.x - at) * LOG2E);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s += p[j].y * ex2(fmaf(p[j].x, LOG2E, -at));
+    for (int j = 0; j < 8; ++j) s += p[j].y * ex2((p[j].x - at) * LOG2E);
     v = make_float2(m, s);
   };
   const float2 none = make_float2(-INFINITY, 0.f);
@@ -200,9 +192,10 @@ __global__ void __launch_bounds__(1024) k_head_lse(const __grid_constant__ Head 
       for (int j = 0; j < 8; ++j) p[j] = red[w + j][lane];
       join(v, p);
     }
-    const float l2 = v.x * LOG2E + log2f(v.y);
-    A.lse2[i] = l2;
-    A.loss[A.row[i]] = A.weight[i] * (l2 * 0.69314718055994531f - A.label_logit[i]);
+    const float l = log2f(v.y), loss = (v.x - A.own[i]) + l * 0.69314718055994531f;
+    A.lse2[i] = v.x * LOG2E + l;
+    A.loss[A.row[i]] = A.weight[i] * loss;
+    A.own[i] = expm1f(-loss);
   }
 }
 
@@ -242,11 +235,11 @@ __global__ void __launch_bounds__(256) k_head_dz(const __grid_constant__ Head A)
     for (int e = 0; e < 32; ++e) v[e] = b[32 * e];
   }
   const bool on = row < n;
-  const float lse2 = on ? A.lse2[row] : 0.f;
+  const float lse2 = on ? A.lse2[row] : 0.f, own = on ? A.own[row] : 0.f;
   const int label = on ? A.label[row] - 32 * cb : -1;
 #pragma unroll
   for (int e = 0; e < 32; ++e)
-    v[e] = on ? ex2(fmaf(v[e], LOG2E, -lse2)) - (label == e ? 1.f : 0.f) : 0.f;
+    v[e] = !on ? 0.f : label == e ? own : ex2(fmaf(v[e], LOG2E, -lse2));
   put_block(stage[warp], v, A.dl, A.ldd, 32 * cb, 32 * A.keep_cols, [&](int r) { return (long)rb * 32 + r; });
 }
 
@@ -256,7 +249,7 @@ size_t al(size_t v) { return (v + 255) / 256 * 256; }
 struct Plan {
   long Tp, piece;  // columns of a piece, a multiple of 256
   int slots, slices;
-  size_t hc, hw, label, weight, row, lse2, label_logit, n, runs, part, dl, blocks, keep, bytes;
+  size_t hc, hw, label, weight, row, lse2, own, n, runs, part, dl, blocks, keep, bytes;
   int keep_cols;   // blocks of kept logits side by side, 0: not kept
 };
 
@@ -281,7 +274,7 @@ Plan plan_of(int T, int V, int H, bool dh, bool dw) {  // (the same with weights
   p.weight = take(4 * p.Tp);
   p.row = take(4 * p.Tp);
   p.lse2 = take(4 * p.Tp);
-  p.label_logit = take(4 * p.Tp);
+  p.own = take(4 * p.Tp);
   p.n = take(4);
   p.runs = take(4 * (p.Tp / RUN + 1));
   p.part = take(8 * (size_t)p.slots * p.Tp);
@@ -355,8 +348,6 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
   A.T = T, A.V = V, A.H = H, A.Tp = (int)L.Tp;
   A.h = (const __nv_bfloat16*)h;
   A.ldh = ldh;
-  A.w = (const __nv_bfloat16*)w;
-  A.ldw = ldw;
   A.labels = labels;
   A.row_weight = row_weight;
   A.loss = loss;
@@ -369,7 +360,7 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
   A.runs = (int*)(ws + L.runs);
   A.weight = (float*)(ws + L.weight);
   A.lse2 = (float*)(ws + L.lse2);
-  A.label_logit = (float*)(ws + L.label_logit);
+  A.own = (float*)(ws + L.own);
   A.part = (const float2*)(ws + L.part);
   A.slots = L.slots;
   A.keep = (const float*)(ws + L.keep);
@@ -386,6 +377,7 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
   P.n = 1;
   P.label = A.label;
   P.lse2 = A.lse2;
+  P.own = A.own;
   P.part = (float2*)(ws + L.part);
   P.part_ld = L.Tp;
   P.keep = L.keep_cols ? (float*)(ws + L.keep) : nullptr;

@@ -99,9 +99,11 @@ struct Launch : Epilogue {
   // LINEAR
   int tma_r, tma_y, tma_p;  // whether the residual's, y's and pre's rows suit TMA (boxes of 128 bytes x 32 rows):
   CUtensorMap map_r, map_y, map_p;
-  // DLOGIT: compact rows' labels and log-sum-exps (in units of log 2)
-  const int* label;
+  // DLOGIT: compact rows' log-sum-exps (in units of log 2); STATS too: labels, and out of it the
+  // label's logit, into DLOGIT its dz
   const float* lse2;
+  const int* label;
+  float* own;
   CUtensorMap map_dl;  // dz of the piece
   int v0;            // the first column's place in the vocabulary
   // STATS
@@ -399,8 +401,8 @@ __device__ __forceinline__ float column_sum(const float* part, int chunks, int n
 // The tensor core cuts a running sum off at every instruction (16 terms, 32 of e4m3): a sum of
 // 2048 is 1e-6 to 4e-6 of itself short.  That is lost in a bf16 output, but not in a loss: the logits'
 // statistics are taken of sums in parts of 1024 terms (16 blocks of K), each in an accumulator of
-// its own, added as fp32 on their way out.  (Losses were 8e-7 off, at 2560 terms 1.2e-6, and are
-// 4e-7; it costs these tiles 3 %.  In the gradients' tiles the registers for it cost 10 to 50 %.)
+// its own, added as fp32 on their way out.  (Losses were 1e-6 off, at 2560 terms 1.3e-6, and are
+// 3e-7 to 6e-7; it costs these tiles 3 %.  In the gradients' tiles the registers for it cost 10 to 50 %.)
 template <int MODE, bool F8, bool DEEP>
 __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ Launch P) {
   using C = Cfg<MODE, DEEP>;
@@ -568,9 +570,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
       // what the tile needs besides its sums, on the way while those are formed: the row's, and
       // the scales and biases of the columns 32 h + lane
       int label = -1;
-      float lse2 = 0.f, xs = 1.f, col_s[4];
+      float lse2 = 0.f, own = 0.f, xs = 1.f, col_s[4];
       __nv_bfloat16 col_b[4];
-      if (MODE == DLOGIT && row < M) label = P.label[row] - P.v0, lse2 = P.lse2[row];
+      if (MODE == STATS && row < M) label = P.label[row];
+      if (MODE == DLOGIT && row < M) label = P.label[row] - P.v0, lse2 = P.lse2[row], own = P.own[row];
       if (MODE == LINEAR) {
         if (F8 && row < M) xs = P.x_scale[row];
         if (F8 || P.bias)
@@ -604,7 +607,15 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
         char* buf = stg + (NBUF == 2 ? j * STG : 0);
         if (col0 >= p.N || !on) return;
         if constexpr (MODE == STATS) {
-          const int n = min(64, p.N - col0);
+          const int n = min(64, p.N - col0), at_label = label - col0;
+          if (at_label >= 0 && at_label < n) {
+            float z = 0.f;
+#pragma unroll
+            for (int e = 0; e < 64; ++e)
+              if (at_label == e) z = __uint_as_float(r[e]);
+            P.own[row] = z;
+          }
+          __syncwarp();
           if (P.keep) {
             float* o = P.keep + ((long)(row0 / 32) * P.keep_cols + col0 / 32) * 1024 + lane;
 #pragma unroll
@@ -617,12 +628,15 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
           float m = best;
 #pragma unroll
           for (int e = 0; e < 64; ++e) m = fmaxf(m, __uint_as_float(r[e]));
-          const float at = m == -INFINITY ? 0.f : m * LOG2E;  // (a row of -inf so far)
-          float s0 = total * rows::ex2(best == -INFINITY ? -INFINITY : fmaf(best, LOG2E, -at)), s1 = 0.f;
+          // exponentials of what is left of the largest value, whose own is then 1 and no other above
+          const float2 at = rows::both(m == -INFINITY ? 0.f : -m);  // (a row of -inf so far)
+          float s0 = total * rows::ex2((best + at.x) * LOG2E), s1 = 0.f;
 #pragma unroll
           for (int e = 0; e < 64; e += 2) {
-            s0 += rows::ex2(fmaf(__uint_as_float(r[e]), LOG2E, -at));
-            s1 += rows::ex2(fmaf(__uint_as_float(r[e + 1]), LOG2E, -at));
+            const float2 x = rows::mul2(rows::add2(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), at),
+                                        rows::both(LOG2E));
+            s0 += rows::ex2(x.x);
+            s1 += rows::ex2(x.y);
           }
           total = s0 + s1;
           best = m;
@@ -631,7 +645,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
           const int at = label - col0;
 #pragma unroll
           for (int e = 0; e < 64; ++e) {
-            const float d = rows::ex2(fmaf(__uint_as_float(r[e]), LOG2E, -lse2)) - (at == e ? 1.f : 0.f);
+            const float d = at == e ? own : rows::ex2(fmaf(__uint_as_float(r[e]), LOG2E, -lse2));
             r[e] = row < M ? __float_as_uint(d) : 0u;
           }
           box_free(j);

@@ -4,6 +4,8 @@ Bounds.  A logit of H terms is off by (H / 16 + 16) 2^-23 of its terms' magnitud
 core's sums, see test_gpu_linear), e at most over the rows; a loss by 2 e and 2^-20 of its parts;
 a softmax by 2 e + 2^-19 of itself; dz is rounded to bf16 (2^-8 of each term of the gradients'
 sums), and so are, for dw, the hidden states times the weights (as much again), dh and dw."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -136,6 +138,37 @@ def test_logits_far_from_zero():
     h, w, labels, weight = _case(33, 600, 64, std=1.0)
     w[77] *= 100
     _check(lx.head_loss(h, w, labels), h, w, labels)
+
+
+@pytest.mark.parametrize("T,V", [(40, 600), (300, 9000), (2100, 40000)])
+def test_sure_rows(T, V):
+    """Labels far above the rest: the loss, log(1 + sum of the others), is below 0.1 and never below 0, and the
+    label's dz is 1 - exp(-loss), seen in dh along a direction that only the label's row of w has.
+    Relative: the others' logits of 64 terms are off by less than 1e-4, 2e-3 covers it (and 2^-8 twice for dz and
+    dh in bf16).  Absolute: the sum is at least the label's 1 and below 2, so each addition after it rounds by at most
+    2^-24: 64 of them in the chain of its half tile, and with V <= 40000 at most 16 and 32 more where the
+    half tiles' sums are joined: 120 2^-24 < 2^-17."""
+    g = torch.Generator().manual_seed(1)
+    h = torch.zeros(T, 64)
+    h[:, :32] = torch.randn(T, 32, generator=g)
+    h[:, 32] = 1
+    w = torch.randn(V, 64, generator=g) * 0.1
+    w[:, 32:] = 0
+    w[7, :32] = 0
+    w[7, 32] = 5 + math.log(V)
+    scale = torch.linspace(1, 2, T)
+    h[:, 32] = scale
+    w[7, 40] = 1   # h is 0 there: dh's entry 40 is the label's dz
+    h, w = h.to(BF).cuda(), w.to(BF).cuda()
+    labels = torch.full((T,), 7, dtype=torch.int32, device="cuda")
+    got = lx.head_loss(h, w, labels)
+    z = h.double() @ w.double().t()
+    rest = torch.logsumexp(torch.cat([z[:, :7], z[:, 8:]], 1), 1) - z[:, 7]
+    want = torch.log1p(torch.exp(rest))
+    assert float(want.max()) < 0.1 and float(got.loss.min()) >= 0
+    assert float(((got.loss - want).abs() - 2e-3 * want).max()) <= 2.0 ** -17
+    p = -torch.expm1(-want)
+    assert float(((got.dh[:, 40].double() + p).abs() - (2e-3 + 2 * R) * p).max()) <= 2.0 ** -17
 
 
 def test_slices_of_wider_arrays_parts_and_the_same_bits():
