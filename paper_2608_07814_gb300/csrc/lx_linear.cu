@@ -210,36 +210,60 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) k_linear_few(const __grid_cons
   }
 }
 
+// How a product of few tokens is cut: tokens and blocks of K of a CTA, CTAs of a cluster, and
+// what it takes in ns, as measured.  Stages arrive at 110 bytes a ns an SM; two CTAs share one up
+// to 128 tokens (108 KiB each; with 128 columns of TMEM at most, so that neither waits for the
+// other's), above there is one.  A launch takes 3.1 us, with a cluster 4.8, and a tile's way out through
+// shared memory 30 ns a token, 60 where one CTA does it alone.  More than eight clusters of eight CTAs that
+// fill an SM wait for eight free SMs of a GPC (256 tokens of 2048 x 2048: 20.2 us with eight, 14 with four).
+struct FewPlan {
+  int tn, nt, tb, splits, per;
+  long ns;
+};
+FewPlan few_plan(long T, long N, long nkb) {
+  FewPlan best = {};
+  const long tb = (T + FEW_T - 1) / FEW_T, nt = (N + 127) / 128, tn = ((T + tb - 1) / tb + 15) / 16 * 16;
+  if (nt > 65535 || tb > 65535) return best;  // (a grid's limits: never few)
+  const long per_sm = tn <= 128 ? 2 : 1;
+  const int most = per_sm == 2 || nt * tb <= 8 ? FEW_SPLIT : FEW_SPLIT / 2;
+  for (int s = 1; s <= most && (s == 1 || nkb >= 4 * s); s *= 2) {
+    const long ctas = nt * tb * s, per = (nkb + s - 1) / s, waves = (ctas + SMS * per_sm - 1) / (SMS * per_sm);
+    const long sharing = std::min(per_sm, (ctas + SMS - 1) / SMS);
+    const long ns = (s > 1 ? 4800 + waves * 30 * tn : 3100 + waves * 60 * tn) +
+                    waves * (per * sharing * (A_BYTES + tn * KB) / 110);
+    if (s == 1 || ns <= best.ns) best = {(int)tn, (int)nt, (int)tb, s, (int)per, ns};
+  }
+  return best;
+}
+// What tiles of 256 x 256 by pairs of SMs take, in ns; 3 us more a round where they cannot leave by TMA
+long pairs_ns(long T, long N, long nkb, bool tma) {
+  const long tiles = ((T + BM - 1) / BM) * ((N + BN - 1) / BN);
+  return 4500 + (tiles + SMS / 2 - 1) / (SMS / 2) * (nkb * 290 + (tma ? 0 : 3000));
+}
+
 template <bool F8>
-lx_status launch_few(Few& P, int tb, int es, const lx_linear_desc* d, cudaStream_t st) {
+lx_status launch_few(Few& P, const FewPlan& L, int es, const lx_linear_desc* d, cudaStream_t st) {
   static bool cap[64] = {};
   int dev = 0;
   LX_CUDA(cudaGetDevice(&dev));
   LX_CUDA(smem_cap_once((const void*)k_linear_few<F8>, 224 * 1024, dev, cap));
+  P.tn = L.tn;
+  P.per = L.per;
   if (!encode_bytes_2d(&P.w, d->w, (long)d->K * es, d->N, d->ldw * es, 128) ||
       !encode_bytes_2d(&P.x, d->x, (long)d->K * es, d->T, d->ldx * es, P.tn))
     return fail(LX_ERR_CUDA, "cuTensorMapEncodeTiled(linear) failed");
-  const int stage = A_BYTES + P.tn * KB;
-  // Two CTAs an SM up to 128 tokens (108 KiB each; with 128 columns of TMEM at most, so that
-  // neither waits for the other's), one above.  (200 KiB for 128 CTAs or fewer: 64 tokens of 2048 x 8192
-  // in 8 bits 15.8 us instead of 9.9, as clusters of eight then need eight free SMs of a GPC.)
-  const int per_sm = P.tn <= 128 ? 2 : 1;
+  const int stage = A_BYTES + P.tn * KB, budget = P.tn <= 128 ? 108 * 1024 : 200 * 1024;
   P.cols = 32;
   while (P.cols < P.tn) P.cols *= 2;
-  const int nt = (d->N + 127) / 128;
-  int splits = 1;
-  while (splits < FEW_SPLIT && (long)nt * tb * splits * 2 <= (long)SMS * per_sm && P.nkb >= 8 * splits) splits *= 2;
-  P.per = (P.nkb + splits - 1) / splits;
-  const int budget = per_sm == 1 ? 200 * 1024 : 108 * 1024;
   P.stages = std::min(16, budget / stage);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(splits, nt, tb);
+  cfg.gridDim = dim3(L.splits, L.nt, L.tb);
   cfg.blockDim = dim3(FEW_THREADS);
   cfg.dynamicSmemBytes = budget + 1024;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = splits;
+  attr[0].val.clusterDim.x = L.splits;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
@@ -458,18 +482,18 @@ extern "C" lx_status lx_linear(const lx_linear_desc* d, void* y, int64_t ldy, vo
   P.act = d->act;
   auto wide = [](const void* p, long ld, int b) { return !p || (((uintptr_t)p | (uintptr_t)(2 * ld)) % b) == 0; };
   cudaStream_t st = (cudaStream_t)stream;
-  // Few tokens: tiles of 256 x 256 would leave more than half of the pairs of SMs without one
-  const long tiles = (((long)d->T + BM - 1) / BM) * (((long)d->N + BN - 1) / BN);
-  const int tb = (d->T + FEW_T - 1) / FEW_T;
-  if ((d->T <= 64 && d->N <= 65535 * 128) || tiles * 2 <= SMS / 2) {
+  // Few tokens or tiles, by what the two forms take (µs, 2048 x 2048: 128 tokens 10.0 and 14.2, 1024 18.4
+  // and 14.4; 512 x 8192 inputs: 21.8 and 40.8; 256 x 512 inputs: 13.8 and 7.5)
+  const long nkb = ((long)d->K * es + KB - 1) / KB;
+  const FewPlan few = few_plan(d->T, d->N, nkb);
+  if (few.splits && few.ns < pairs_ns(d->T, d->N, nkb, wide(y, ldy, 16))) {
     Few F = {};
     F.e = P;
     F.T = d->T;
     F.N = d->N;
-    F.nkb = (int)(((long)d->K * es + KB - 1) / KB);
-    F.tn = ((d->T + tb - 1) / tb + 15) / 16 * 16;
+    F.nkb = (int)nkb;
     F.vec = wide(y, ldy, 8) && wide(pre, d->N, 8) && wide(d->residual, d->ldr, 8);
-    return f8 ? launch_few<true>(F, tb, es, d, st) : launch_few<false>(F, tb, es, d, st);
+    return f8 ? launch_few<true>(F, few, es, d, st) : launch_few<false>(F, few, es, d, st);
   }
   P.tma_y = boxes(&P.map_y, y, d->N, d->T, ldy);
   P.tma_p = pre && boxes(&P.map_p, pre, d->N, d->T, d->N);
