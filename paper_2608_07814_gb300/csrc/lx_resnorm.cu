@@ -66,7 +66,7 @@ struct NormArgs {
 
 constexpr int REGS = 128;  // a thread: the launch bounds hold the compiler to these
 
-constexpr float E4M3_MAX = 448.f, TINY = 1.17549435e-38f;
+constexpr float E4M3_MAX = 448.f, TINY = 1.17549435e-38f, SMALL = 7.8886091e-31f;  // 2^-126, 2^-100
 
 // four values in e4m3, to the nearest, what is above 448 as 448
 __device__ __forceinline__ uint32_t to_e4m3(float2 a, float2 b) {
@@ -511,10 +511,10 @@ k_resnorm_fwd(const __grid_constant__ NormArgs A) {
           R.write(A.h_out, t, x);
         }
         const float top = s2 * __uint_as_float(m);
-        float scale = top / E4M3_MAX, by = s2 / scale;
-        if (top < E4M3_MAX * TINY) {  // (by itself would be above fp32's range)
-          scale = TINY;
-          by = 1.f / TINY;
+        const float scale = top < E4M3_MAX * TINY ? TINY : top / E4M3_MAX;
+        float by = s2 / scale;  // at most 448 over the row's largest,
+        if (__uint_as_float(m) < SMALL) {  // which is above fp32's range below 1.4e-36: its factors one by one
+          by = 1.f / scale;
 #pragma unroll
           for (int i = 0; i < N2; ++i) v[i] = muls(v[i], both(s2));
         }
