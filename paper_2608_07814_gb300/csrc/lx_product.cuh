@@ -403,12 +403,16 @@ __device__ __forceinline__ float column_sum(const float* part, int chunks, int n
 // statistics are taken of sums in parts of 1024 terms (16 blocks of K), each in an accumulator of
 // its own, added as fp32 on their way out.  (Losses were 1e-6 off, at 2560 terms 1.3e-6, and are
 // 3e-7 to 6e-7; it costs these tiles 3 %.  In the gradients' tiles the registers for it cost 10 to 50 %.)
+// The logits that become dz are summed in the same parts: they are those whose log-sum-exp is subtracted,
+// to the bit, and a row's dz adds up to 0.  (Summed in one accumulator, all of a row's are too small alike:
+// its dz added up to 0.017 for 4096 inputs and logits that share a part of 2000.)
 template <int MODE, bool F8, bool DEEP>
 __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ Launch P) {
   using C = Cfg<MODE, DEEP>;
   constexpr int STAGES = C::STAGES, NBUF = C::NBUF;
   constexpr bool PASS = MODE == LINEAR && !DEEP;  // takes a residual and keeps the sums
-  constexpr int PART = MODE == STATS ? 16 : 1 << 30;
+  constexpr bool PARTS = MODE == STATS || MODE == DLOGIT;
+  constexpr int PART = PARTS ? 16 : 1 << 30;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   char* staged = reinterpret_cast<char*>(smem + STAGES * STAGE);
@@ -749,7 +753,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
           }
         }
       };
-      if constexpr (MODE == STATS) {
+      if constexpr (PARTS) {
         uint32_t r[2][64];
         for (int k = 0; k < t.nkb; k += PART, ++nt) {
           arrived();
