@@ -630,7 +630,8 @@ LX_API lx_status lx_residual_norm_q8(const lx_resnorm_desc* desc, void* r_out, v
  *   x_scale fp32 [T], w_scale fp32 [N];  bias bf16 [N] or NULL;  residual bf16 [T][N] (ldr)
  *   or NULL
  *   y bf16 [T][N] (ldy), may be residual itself (ldr = ldy);  pre: bf16 [T][N] or NULL: z,
- *   which the backward of an activation reads;  outputs overlap nothing else
+ *   which the backward of an activation reads;  outputs overlap nothing else.  The bits of y and
+ *   pre do not go by where the rows lie
  * lx_linear_backward (LX_BF16; desc's scales, bias and residual are not read): from dy (rows
  * lddy apart) and pre (given exactly with an activation), with dz = dy act'(pre):
  *   dx [T][K] = dz w,  dw [N][K] = dz^T x,  dbias [N] = sum_t dz, all bf16 and 16-byte

@@ -235,10 +235,12 @@ FewPlan few_plan(long T, long N, long nkb) {
   }
   return best;
 }
-// What tiles of 256 x 256 by pairs of SMs take, in ns; 3 us more a round where they cannot leave by TMA
-long pairs_ns(long T, long N, long nkb, bool tma) {
+// What tiles of 256 x 256 by pairs of SMs take, in ns; 3 us more a round where rows of N side by side
+// cannot leave by TMA.  (Rows that lie otherwise do not count: the form, and with it the order of the
+// sums, goes by the sizes and the type, not by where the output is.)
+long pairs_ns(long T, long N, long nkb) {
   const long tiles = ((T + BM - 1) / BM) * ((N + BN - 1) / BN);
-  return 4500 + (tiles + SMS / 2 - 1) / (SMS / 2) * (nkb * 290 + (tma ? 0 : 3000));
+  return 4500 + (tiles + SMS / 2 - 1) / (SMS / 2) * (nkb * 290 + (N % 8 == 0 ? 0 : 3000));
 }
 
 template <bool F8>
@@ -486,7 +488,7 @@ extern "C" lx_status lx_linear(const lx_linear_desc* d, void* y, int64_t ldy, vo
   // and 14.4; 512 x 8192 inputs: 21.8 and 40.8; 256 x 512 inputs: 13.8 and 7.5)
   const long nkb = ((long)d->K * es + KB - 1) / KB;
   const FewPlan few = few_plan(d->T, d->N, nkb);
-  if (few.splits && few.ns < pairs_ns(d->T, d->N, nkb, wide(y, ldy, 16))) {
+  if (few.splits && few.ns < pairs_ns(d->T, d->N, nkb)) {
     Few F = {};
     F.e = P;
     F.T = d->T;
