@@ -122,8 +122,12 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) k_linear_few(const __grid_cons
   int ok = 1;
   if (lane == 0) {
     ok = wait_quiet(done, 0, nullptr, 2 * P.e.wait_cycles) ? 1 : 0;  // (the issuer may have waited for the bound)
-    if (!ok) *lost = 1;
-    else if (*lost) ok = 0;
+    if (!ok) {
+      *lost = 1;
+      wait_quiet(done, 0, nullptr, kDefaultWaitCycles);  // no product is in flight from here on
+    } else if (*lost) {
+      ok = 0;
+    }
   }
   ok = __shfl_sync(0xffffffffu, ok, 0);
   tc_fence_after();
@@ -131,7 +135,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) k_linear_few(const __grid_cons
     // copies in flight land before the sums take their place
     const uint32_t first = issued > (uint32_t)P.stages ? issued - P.stages : 0;
     for (uint32_t j = first; j < issued; ++j)
-      wait_quiet(full0 + 8 * (j % P.stages), (j / P.stages) & 1, nullptr, P.e.wait_cycles);
+      wait_quiet(full0 + 8 * (j % P.stages), (j / P.stages) & 1, nullptr, kDefaultWaitCycles);
   }
   __syncthreads();
   float* part = reinterpret_cast<float*>(smem);

@@ -47,6 +47,11 @@ constexpr int STG_LD = 80;             // rows TMA cannot take: 32 bf16, 16-byte
 constexpr int GROUP_M = 16, MAX_SLICES = 16;
 constexpr int LEAVING = 5;  // blocks of K whose products take as long as a tile's way out (1.9 us)
 
+// A CTA's words beside its barriers: whether one of its waits gave up, and whether one of the pair's
+// did; the address of its TMEM; and, at its end, blocks of K that it asked for, blocks that were
+// multiplied and sums that were committed (by the even CTA).
+enum Word { LOST = 0, LOST_PAIR = 1, TMEM = 2, ASKED = 3, MADE = 4, SUMS = 5, WORDS = 6 };
+
 enum Mode { LINEAR = 0, STATS = 1, DLOGIT = 2, GRAD = 3 };
 enum Act { NONE = 0, RELU = 1, SILU = 2, GELU = 3 };
 
@@ -60,7 +65,7 @@ struct Cfg {
   static constexpr int STAGES = MODE == STATS ? 5 : DEEP ? 6 : 5;
   static constexpr int PARAMS = MODE == LINEAR ? PRM : 0;
   static constexpr int BARS = 2 * STAGES + 5 + (MODE == LINEAR && !DEEP ? 2 * EPI : 0);
-  static constexpr int SMEM = STAGES * STAGE + EPI * (NBUF * STG + PARAMS) + 8 * BARS + 16 + 1024;
+  static constexpr int SMEM = STAGES * STAGE + EPI * (NBUF * STG + PARAMS) + 8 * BARS + 4 * WORDS + 1024;
   static_assert(SMEM <= 227 * 1024, "fits an SM");
 };
 
@@ -145,6 +150,18 @@ static __device__ __forceinline__ bool wait_quiet(uint32_t bar, uint32_t parity,
     if (clock64() - t0 > limit) return false;
   }
 }
+// a word of shared memory of the pair's CTA
+static __device__ __forceinline__ uint32_t get_word(const uint32_t* word, uint32_t rank) {
+  uint32_t at, v;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(word)), "r"(rank));
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  return v;
+}
+static __device__ __forceinline__ void set_word(uint32_t* word, uint32_t rank, uint32_t v) {
+  uint32_t at;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(word)), "r"(rank));
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory");
+}
 static __device__ __forceinline__ void arrive_remote(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
@@ -187,6 +204,31 @@ static __device__ __forceinline__ uint64_t desc_mn(uint32_t addr) {
 __host__ __device__ constexpr uint32_t idesc(bool f8, int a_mn, int b_mn, int M, int N) {
   return (1u << 4) | (f8 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) |
          ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+// After a wait of the pair that gave up, one thread of each CTA, both CTAs being there until it is
+// done: all copies asked for have landed, and all commits arrived, before shared memory and TMEM go
+// away.  The roles stopped where they were, so this goes by their counts; no CTA is more than the
+// stages ahead of the other, as a stage is asked for again once both halves of it were multiplied.  The
+// bound is the default: what is waited for here is on its way and needs no one's part.
+template <int STAGES>
+static __device__ __noinline__ void settle(const uint32_t* words, uint32_t full0, uint32_t empty0, uint32_t tfull0,
+                                           uint32_t rank) {
+  const uint32_t even = get_word(words + ASKED, 0), odd = get_word(words + ASKED, 1), most = max(even, odd);
+  const uint32_t made = get_word(words + MADE, 0), sums = get_word(words + SUMS, 0);
+  if (rank == 0)  // (whose barriers count both CTAs' bytes)
+    for (uint32_t j = most > STAGES ? most - STAGES : 0; j < most; ++j) {
+      const uint32_t bar = full0 + 8 * (j % STAGES);
+      if (j >= even)  // the odd CTA's half alone
+        mbar_expect_tx(bar, STAGE);
+      else if (j >= odd)  // the even one's: the other was expected, too
+        asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(STAGE) : "memory");
+      wait_quiet(bar, (j / STAGES) & 1, nullptr, kDefaultWaitCycles);
+    }
+  for (uint32_t j = made > STAGES ? made - STAGES : 0; j < made; ++j)
+    wait_quiet(empty0 + 8 * (j % STAGES), (j / STAGES) & 1, nullptr, kDefaultWaitCycles);
+  for (uint32_t j = sums > 2 ? sums - 2 : 0; j < sums; ++j)
+    wait_quiet(tfull0 + 8 * (j & 1), (j >> 1) & 1, nullptr, kDefaultWaitCycles);
 }
 
 constexpr float LOG2E = 1.4426950408889634f;
@@ -418,9 +460,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
   char* staged = reinterpret_cast<char*>(smem + STAGES * STAGE);
   uint64_t* bars = reinterpret_cast<uint64_t*>(staged + EPI * (NBUF * STG + C::PARAMS));
   const uint32_t base = smem_u32(smem), full0 = smem_u32(bars), empty0 = full0 + 8 * STAGES;
-  const uint32_t tfull0 = empty0 + 8 * STAGES, tempty0 = tfull0 + 16, drain = tempty0 + 16, res0 = drain + 8;
-  volatile int* lost = reinterpret_cast<volatile int*>(bars + C::BARS);
-  uint32_t* tmem_s = reinterpret_cast<uint32_t*>(bars + C::BARS + 1);
+  const uint32_t tfull0 = empty0 + 8 * STAGES, tempty0 = tfull0 + 16, never = tempty0 + 16, res0 = never + 8;
+  uint32_t* words = reinterpret_cast<uint32_t*>(bars + C::BARS);
+  volatile int* lost = reinterpret_cast<volatile int*>(words + LOST);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
 
@@ -433,14 +475,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
       mbar_init(tfull0 + 8 * b, 1);             // a commit
       mbar_init(tempty0 + 8 * b, 2 * EPI);      // the even CTA's: both CTAs' epilogue warps
     }
-    mbar_init(drain, 1);
+    mbar_init(never, 1);
     if (PASS)
       for (int i = 0; i < 2 * EPI; ++i) mbar_init(res0 + 8 * i, 1);
-    *lost = 0;
+    words[LOST] = words[LOST_PAIR] = words[ASKED] = words[MADE] = words[SUMS] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_s)) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(words + TMEM)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
   pdl_wait();
@@ -450,7 +492,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
   __syncthreads();
   cluster_sync();  // both CTAs' barriers are there
   tc_fence_after();
-  const uint32_t tmem = *tmem_s;
+  const uint32_t tmem = words[TMEM];
 
   Tile t;
   if (warp == 0) {
@@ -486,19 +528,13 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
       // the commits of the last stages have arrived before the CTA may end
       for (uint32_t j = it > STAGES ? it - STAGES : 0; ok && j < it; ++j)
         ok = wait_quiet(empty0 + 8 * (j % STAGES), (j / STAGES) & 1, lost, P.wait_cycles);
-      if (!ok) {
-        *lost = 1;
-        // copies in flight land before shared memory goes away (both CTAs': the even one's
-        // barriers count them)
-        if (rank == 0)
-          for (uint32_t j = it > STAGES ? it - STAGES : 0; j < it; ++j)
-            wait_quiet(full0 + 8 * (j % STAGES), (j / STAGES) & 1, nullptr, P.wait_cycles);
-      }
+      if (!ok) *lost = 1;
+      words[ASKED] = it;
     }
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
       uint32_t it = 0, nt = 0;
-      bool ok = !P.unmet || wait_quiet(drain, 0, lost, P.wait_cycles);
+      bool ok = !P.unmet || wait_quiet(never, 0, lost, P.wait_cycles);
       for (int i = 0; ok && S.at(i, t); ++i) {
         if (t.nkb == 0) continue;
         const Problem& p = P.p[t.p];
@@ -527,11 +563,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
         }
         if (ok) commit_pair(tfull0 + 8 * (nt++ & 1), 3);
       }
-      if (!ok) {
-        *lost = 1;
-        commit_pair(drain, 1);  // no product is in flight when TMEM is freed
-        wait_quiet(drain, 0, nullptr, P.wait_cycles);
-      }
+      if (!ok) *lost = 1;
+      words[MADE] = it;
+      words[SUMS] = nt;
     }
   } else if (MODE == GRAD && warp < 4) {
     for (int c = (blockIdx.x * 2 + warp - 2) * 32 + lane; c < P.db_n; c += gridDim.x * 64)
@@ -717,8 +751,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
             if (P.tma_r) {
               int got = 1;
               if (lane == 0)
-                got = wait_quiet(res + 8 * j, (res_turn >> j) & 1, nullptr, P.wait_cycles) ||
-                      wait_quiet(res + 8 * j, (res_turn >> j) & 1, nullptr, P.wait_cycles);
+                got = wait_quiet(res + 8 * j, (res_turn >> j) & 1, nullptr, kDefaultWaitCycles);  // (it is on its way)
               got = __shfl_sync(0xffffffffu, got, 0);
               res_turn ^= 1u << j;
               if (!got) {
@@ -813,7 +846,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_product(const __grid_constant__ 
   __syncwarp();
   tc_fence_before();
   __syncthreads();
+  if (threadIdx.x == 0 && *lost) set_word(words + LOST_PAIR, 0, 1), set_word(words + LOST_PAIR, 1, 1);
+  __syncwarp();
   cluster_sync();
+  if (*(volatile uint32_t*)(words + LOST_PAIR)) {  // in both CTAs
+    if (threadIdx.x == 0) settle<STAGES>(words, full0, empty0, tfull0, rank);
+    __syncwarp();
+    cluster_sync();
+  }
   if (warp == 1) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
