@@ -661,7 +661,7 @@ LX_API lx_status lx_linear_backward(const lx_linear_desc* desc, const void* dy, 
 
 /*
  * lx_head_loss: softmax cross-entropy over the vocabulary from the last hidden states h and
- * the head's weights w, with its gradients, the logits not kept:
+ * the head's weights w, with its gradients, without a [T][V] array of logits where that is large:
  *   z = h w^T,  loss_t = row_weight_t (log sum_v exp(z_tv) - z_t,label_t)
  *   dz_tv = softmax(z_t)_v - [v = label_t],  dh = row_weight (dz w),  dw = dz^T (row_weight h)
  * A token whose label is outside [0, V) or whose weight is 0 takes no part: loss 0, dh 0,
@@ -673,8 +673,10 @@ LX_API lx_status lx_linear_backward(const lx_linear_desc* desc, const void* dy, 
  *   loss fp32 [T] out;  dh bf16 [T][H], dw bf16 [V][H] out, 16-byte aligned, each or NULL:
  *   the gradients of the losses' sum
  *   workspace: device, 256-byte aligned, lx_head_loss_workspace bytes (which of dh and dw
- *   are wanted): it grows with T H and, eight bytes for 128 logits, with T V; the
- *   vocabulary is worked on in pieces whose dz takes at most 256 MiB, or 256 columns
+ *   are wanted): it grows with T H and, eight bytes for 128 logits, with T V (T in steps of
+ *   256).  For the gradients, logits that take at most 256 MiB in fp32 (T in steps of 32, V of 256)
+ *   are kept there, and their dz takes at most as much again; others are formed again, in
+ *   pieces of the vocabulary whose dz takes at most 256 MiB, or 256 columns
  * Errors: LX_ERR_ARG (NULL, alignment, overlap, workspace), LX_ERR_SHAPE (sizes, leading
  * dimensions).
  */

@@ -1,5 +1,5 @@
 // Softmax cross-entropy over the vocabulary from the last hidden states and the head's
-// weights (lx_head_loss), without the logits:
+// weights (lx_head_loss), without a [T][V] of logits where that is large:
 //   z = h W^T,  loss_t = w_t (log sum_v exp(z_tv) - z_t,label)
 //   dz_tv = softmax(z_t)_v - [v = label_t],  dh = w (dz W),  dW = dz^T (w h)
 // dz is rounded to bf16 as the tensor cores take it.  The weights stay outside of it: a label's
@@ -18,8 +18,8 @@
 // With the logits formed twice that is 8 T V H operations against the 6 that a kept [T][V]
 // needs, and a workspace that grows with T V by those 8 bytes alone.  The label's dz comes from step
 // 2 as well, from its loss.  Where all logits fit, as fp32, into the room of a piece, they are kept
-// there and step 3 reads them instead of W: few tokens would spend as long on reading W again as on
-// everything else.
+// in a room of their own and step 3 reads them instead of W: few tokens would spend as long on reading
+// W again as on everything else.
 #include "lx_product.cuh"
 
 namespace lx {
@@ -248,6 +248,7 @@ size_t al(size_t v) { return (v + 255) / 256 * 256; }
 // What a call's sizes come to, and where its arrays lie in the workspace
 struct Plan {
   long Tp, piece;  // columns of a piece, a multiple of 256
+  long Td;         // rows of dz
   int slots, slices;
   size_t hc, hw, label, weight, row, lse2, own, n, runs, part, dl, blocks, keep, bytes;
   int keep_cols;   // blocks of kept logits side by side, 0: not kept
@@ -278,12 +279,16 @@ Plan plan_of(int T, int V, int H, bool dh, bool dw) {  // (the same with weights
   p.n = take(4);
   p.runs = take(4 * (p.Tp / RUN + 1));
   p.part = take(8 * (size_t)p.slots * p.Tp);
+  p.Td = p.Tp;
   if (dh || dw) {
-    p.dl = take(2 * (size_t)p.Tp * p.piece);
-    if (4 * p.Tp * nt * BN <= PIECE_BYTES) {
+    const long Tk = ((long)T + 31) / 32 * 32;  // blocks of 32 rows are kept, and dz of 64: no whole tiles
+    if (4 * Tk * nt * BN <= PIECE_BYTES) {
       p.keep_cols = (int)(nt * BN / 32);
-      p.keep = take(4 * (size_t)p.Tp * nt * BN);
+      p.keep = take(4 * (size_t)Tk * nt * BN);
+      p.piece = nt * BN;
+      p.Td = ((long)T + 63) / 64 * 64;
     }
+    p.dl = take(2 * (size_t)p.Td * p.piece);
   }
   if (dh) p.blocks = take(4 * block_floats(p.Tp, H, p.slices));
   p.bytes = at;
@@ -397,7 +402,7 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
     const long n = std::min<long>(L.piece, V - v0);
     const __nv_bfloat16* wp = (const __nv_bfloat16*)w + v0 * ldw;
     if (L.keep_cols) {  // (one piece)
-      LX_TRY(launch_after(k_head_dz, dim3((L.keep_cols + 7) / 8, (unsigned)(L.Tp / 32)), dim3(256), 0, 1, st, A));
+      LX_TRY(launch_after(k_head_dz, dim3((L.keep_cols + 7) / 8, (unsigned)(L.Td / 32)), dim3(256), 0, 1, st, A));
     } else {
       P.v0 = (int)v0;
       p.N = (int)((n + 31) / 32 * 32);  // (whole blocks of dz; those behind the vocabulary are not read)
@@ -418,13 +423,13 @@ extern "C" lx_status lx_head_loss(const void* h, int64_t ldh, const void* w, int
         g.rows = A.n;
         g.blocks = (float*)(ws + L.blocks);
         g.add = v0 > 0;
-        ok = ok && operand(&g.a, A.dl, n, L.Tp, L.piece, 2, false) && operand(&g.b, wp, H, n, ldw, 2, true);
+        ok = ok && operand(&g.a, A.dl, n, L.Td, L.piece, 2, false) && operand(&g.b, wp, H, n, ldw, 2, true);
       } else {
         g.M = (int)n, g.N = H, g.K = (int)L.Tp, g.slices = 1;
         g.a_mn = 1;
         g.depth = A.n;
         ok = ok && boxes(&g.out, (__nv_bfloat16*)dw + v0 * H, H, n, H) &&
-             operand(&g.a, A.dl, n, L.Tp, L.piece, 2, true) && operand(&g.b, A.hw, H, L.Tp, H, 2, true);
+             operand(&g.a, A.dl, n, L.Td, L.piece, 2, true) && operand(&g.b, A.hw, H, L.Tp, H, 2, true);
       }
     }
     if (!ok) return fail(LX_ERR_CUDA, "cuTensorMapEncodeTiled(head) failed");

@@ -943,8 +943,9 @@ def head_loss_workspace_bytes(T: int, V: int, H: int, want_dh: bool = True, want
 
 def head_loss(h: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, *, row_weight=None, want_dh: bool = True,
               want_dw: bool = True, workspace=None, stream=None) -> HeadLoss:
-    """Softmax cross-entropy of the logits h w^T, which are not kept, against int32 labels
-    [T], of the last hidden states h [T, H] and the head's weights w [V, H] (bf16):
+    """Softmax cross-entropy of the logits h w^T against int32 labels [T], of the last hidden states
+    h [T, H] and the head's weights w [V, H] (bf16), without a [T, V] array of logits (for gradients they
+    are kept, in the workspace, where they take up to 256 MiB):
 
         loss = row_weight * (logsumexp(h w^T) - (h w^T)[label])
 
