@@ -666,7 +666,8 @@ LX_API lx_status lx_linear_backward(const lx_linear_desc* desc, const void* dy, 
  *   dz_tv = softmax(z_t)_v - [v = label_t],  dh = row_weight (dz w),  dw = dz^T (row_weight h)
  * A token whose label is outside [0, V) or whose weight is 0 takes no part: loss 0, dh 0,
  * and its hidden state, whatever it holds, is not used.  dz, and with weights row_weight h, are
- * rounded to bf16 for the two gradient products.
+ * rounded to bf16 for the two gradient products; with T up to 16 and V up to 2^21 row_weight dz is two bf16,
+ * its value and the rest, and h is as it is.
  *   h bf16 [T][H] (rows ldh apart), w bf16 [V][H] (ldw): 16-byte aligned; H, ldh and ldw
  *   multiples of 8;  T up to 2^24 (0: dw is zeroed), V up to 2^24, H up to 2^20
  *   labels int32 [T];  row_weight fp32 [T] or NULL for 1 (a mean's 1 / n goes here)

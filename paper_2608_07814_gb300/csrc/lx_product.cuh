@@ -891,6 +891,7 @@ struct Join {
   const int* place;   // a row's place, or NULL: itself,
   const float* scale; // and factor, or NULL: 1
   __nv_bfloat16* out; // rows of N (a multiple of 8)
+  int rest;           // so many rows on is what is added to a row of the first 32, or 0
 };
 __global__ void __launch_bounds__(256) k_join(const __grid_constant__ Join A) {
   __shared__ __nv_bfloat16 stage[32][40];
@@ -906,6 +907,10 @@ __global__ void __launch_bounds__(256) k_join(const __grid_constant__ Join A) {
   for (int s = 0; s < slices; ++s) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] += b[s * slice + 32 * e];
+  }
+  if (A.rest) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += __shfl_down_sync(0xffffffffu, v[e], A.rest);
   }
   const float f = A.scale && rb * 32 + lane < n ? A.scale[rb * 32 + lane] : 1.f;
   *(uint2*)&stage[lane][4 * warp] = make_uint2(rows::to_bf2(make_float2(v[0] * f, v[1] * f)),
