@@ -16,7 +16,7 @@ block's router sees: it has no part in the loss.
 
 With --labels, a dense expert shared by all tokens (`lx.linear`) is then added beside the
 last block's routed ones and trained, with the head and that block's norms, on the text's own
-next tokens (`lx.head_loss`, which keeps no logits); `shared_8bit` serves it in 8 bits, from the
+next tokens (`lx.head_loss`, from the last hidden states); `shared_8bit` serves it in 8 bits, from the
 norm's own 8-bit output (`lx.residual_norm_q8`).
 
     python examples/heal.py [--steps 30] [--labels 0]

@@ -275,14 +275,16 @@ LX_API lx_status lx_inject_unmet_wait(lx_layer* layer, int32_t site);
 LX_API lx_status lx_clear_device_error(lx_layer* layer);
 
 /*
- * The calls without a layer (lx_compress_factor, lx_align_cost, lx_distill_loss) have
- * bounded waits too (default bound), and no error word of a layer: when one gives up,
- * every value that the call writes is NaN (lx_distill_loss: the loss and the whole
- * gradient of every row that was not done by then, rows of weight 0 apart).
+ * The calls without a layer (lx_compress_factor, lx_align_cost, lx_distill_loss, lx_linear,
+ * lx_linear_backward, lx_head_loss) have bounded waits too (default bound), and no error word of
+ * a layer: when one gives up, every value that the call writes is NaN (lx_distill_loss: the
+ * loss and the whole gradient of every row that was not done by then, rows of weight 0
+ * apart; lx_linear, its backward and lx_head_loss: every value that was not done by then or is
+ * made of one).
  * lx_inject_unmet_wait_call (test hook): in the calling thread's next such call,
  * waits have the bound `cycles` (0: the default) and the one at `site` runs out --
- * LX_WAIT_CALL_PRODUCT: in the tensor-core products (bf16; lx_align_cost also needs
- * d_model a multiple of 256); LX_WAIT_CALL_JACOBI: in lx_compress_factor's Jacobi (l
+ * LX_WAIT_CALL_PRODUCT: in the tensor-core products (bf16, in lx_linear either type;
+ * lx_align_cost also needs d_model a multiple of 256; in lx_head_loss, that of the losses); LX_WAIT_CALL_JACOBI: in lx_compress_factor's Jacobi (l
  * above 2); in lx_distill_loss, LX_WAIT_CALL_SUMS: for the partial sums of a row,
  * LX_WAIT_CALL_AGAIN: for those of a row whose logits lie too far from zero for the
  * first ones, LX_WAIT_CALL_ENTRIES and LX_WAIT_CALL_WRITTEN: from a CTA's third row
@@ -626,7 +628,8 @@ LX_API lx_status lx_residual_norm_q8(const lx_resnorm_desc* desc, void* r_out, v
  *   dtype: of x and w: LX_BF16, or LX_E4M3 (what lx_residual_norm_q8 gives, and weights
  *          with a scale for each output)
  *   x [T][K] (rows ldx apart), w [N][K] (ldw): 16-byte aligned, K, ldx and ldw multiples of 16
- *   bytes; T tokens (0: no-op) up to 2^30, N and K up to 2^24
+ *   bytes; T tokens (0: no-op) up to 2^30, N, K, ldx and ldw up to 2^24, other rows up to
+ *   2^30 elements apart
  *   x_scale fp32 [T], w_scale fp32 [N];  bias bf16 [N] or NULL;  residual bf16 [T][N] (ldr)
  *   or NULL
  *   y bf16 [T][N] (ldy), may be residual itself (ldr = ldy);  pre: bf16 [T][N] or NULL: z,
@@ -669,7 +672,7 @@ LX_API lx_status lx_linear_backward(const lx_linear_desc* desc, const void* dy, 
  * rounded to bf16 for the two gradient products; with T up to 16 and V up to 2^21 row_weight dz is two bf16,
  * its value and the rest, and h is as it is.
  *   h bf16 [T][H] (rows ldh apart), w bf16 [V][H] (ldw): 16-byte aligned; H, ldh and ldw
- *   multiples of 8;  T up to 2^24 (0: dw is zeroed), V up to 2^24, H up to 2^20
+ *   multiples of 8, ldh and ldw up to 2^30;  T up to 2^24 (0: dw is zeroed), V up to 2^24, H up to 2^20
  *   labels int32 [T];  row_weight fp32 [T] or NULL for 1 (a mean's 1 / n goes here)
  *   loss fp32 [T] out;  dh bf16 [T][H], dw bf16 [V][H] out, 16-byte aligned, each or NULL:
  *   the gradients of the losses' sum

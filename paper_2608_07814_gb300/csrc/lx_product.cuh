@@ -15,7 +15,7 @@
 //                a tile's epilogue runs beside the next tile's products;
 //   warps 4..11  epilogue: 32 rows x 64 columns at a time from TMEM, what the caller's MODE
 //                makes of them, and TMA from a warp's buffers of shared memory to memory.
-// Tiles are dealt in an order that keeps 8 rows of tiles together, so that what runs at the
+// Tiles are dealt in an order that keeps 16 rows of tiles together, so that what runs at the
 // same time shares its operands in L2.  Every wait is bounded: when one gives up, the pair's
 // tiles from there on are NaN, copies and products in flight are waited for, and TMEM is freed.
 #pragma once
@@ -240,8 +240,10 @@ __device__ __forceinline__ float rcp(float x) {
   return y;
 }
 // The complementary error function by Abramowitz and Stegun 7.1.26: a polynomial in t = 1 / (1 + p x)
-// times exp(-x^2), 1.5e-7 off at most, a 2^-15 of bf16's step.  (With erff the epilogue took as
-// long as 2500 inputs' products.)
+// times exp(-x^2), 1.5e-7 off at most (and some 2^-23 for the approximate reciprocal and exponential).
+// That is a 2^-15 of bf16's step near 1; gelu's negative tail is |z| / 2 of it off, which relatively
+// is 1.6e-3 at z = -5, 3.6e-3 at -6, 1e-2 at -8 and 3e-2 at -12 (1 + erf in fp32 is further off there).
+// (With erff the epilogue took as long as 2500 inputs' products.)
 // (a NaN stays one)
 __device__ __forceinline__ float max_nan(float a, float b) {
   float y;
